@@ -469,6 +469,80 @@ int amq_lm_sequence_score(const uint32_t* Ep, const float* alpha_e, int64_t voca
                           int64_t steps, float* h, float* c, int64_t B, int k_a, int k_as, int T,
                           float* target_logprob, void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * Operators of quantization-aware training: what a training step does around the quantized weights (Sec. 4,
+ * "Training").  Data of three types, all arithmetic and every sum in binary32, results rounded once:
+ */
+#define AMQ_F32 0
+#define AMQ_BF16 1
+#define AMQ_F16 2
+
+/*
+ * Layer normalization of every row: mu = mean(x), r = 1 / sqrt(mean((x - mu)^2) + eps), y = (x - mu) r weight + bias.
+ *   x [rows][ld_x], y [rows][ld_y] of `type`, ld >= n, any alignment; y may be x itself (same stride)
+ *   weight, bias [n] of `param_type` (AMQ_F32 or `type`), or NULL for 1 and 0
+ *   mean, rstd [rows] float out (mu and r, which the backward pass takes), or NULL
+ * The backward pass takes the gradient dy of y and leaves dx = r (g - mean(g) - z mean(g z)) with g = dy weight,
+ * z = (x - mu) r, and the sums over all rows dweight = sum dy z, dbias = sum dy (of `param_type`; either or both may be
+ * NULL; added up in an order that depends on the sizes only).  dx may be dy or x itself (same stride).
+ *   workspace: at least amq_layer_norm_backward_workspace_bytes(rows, n) bytes, 256-byte aligned (may be NULL
+ *   where neither dweight nor dbias is wanted).
+ */
+int amq_layer_norm(const void* x, int64_t ld_x, int64_t rows, int64_t n, int type, const void* weight, const void* bias,
+                   int param_type, float eps, void* y, int64_t ld_y, float* mean, float* rstd, void* stream);
+size_t amq_layer_norm_backward_workspace_bytes(int64_t rows, int64_t n);
+int amq_layer_norm_backward(const void* dy, int64_t ld_dy, const void* x, int64_t ld_x, int64_t rows, int64_t n, int type,
+                            const void* weight, int param_type, const float* mean, const float* rstd, void* dx,
+                            int64_t ld_dx, void* dweight, void* dbias, void* workspace, size_t workspace_bytes,
+                            void* stream);
+
+/*
+ * Linear layer with everything behind its product in the same pass: z = x W^T + bias, y = act(z) + residual.
+ *   x [rows][ld_x] (k entries a row), W [n][ld_w] (k entries a row: the layout of amq_quantize_weights),
+ *   bias [n] or NULL, residual [rows][ld_r] or NULL, y [rows][ld_y]; all of `type`, any alignment and stride
+ *   pre [rows][ld_pre] or NULL: receives z, rounded to `type`, which the backward pass of an activation takes
+ *   y may be the residual itself (same stride).
+ * bfloat16 and half products go through the matrix cores as they are.  Float operands are scaled by a power of two per
+ * row and split into two halves of 11 bits each, so that three half products leave the error of binary32 products; entries
+ * 2^28 and more below their row's largest lose digits.  Up to 8 rows (a token's vector) are multiplied in binary32.
+ *   workspace: at least amq_linear_workspace_bytes(rows, k, n, type) bytes, 256-byte aligned.
+ * The backward pass takes dy [rows][ld_dy]: with d = dy act'(pre), dx = d W, dW = d^T x, dbias = sum over rows of d; any of
+ * the three may be NULL.  The residual's gradient is dy itself.  pre may be NULL for AMQ_ACT_NONE.
+ * With an activation d is rounded to 8 bits (bfloat16) or 11 (half, scaled per row or column) between the slope and the products.
+ *   workspace: at least amq_linear_backward_workspace_bytes(rows, k, n, type) bytes, 256-byte aligned.
+ */
+#define AMQ_ACT_NONE 0
+#define AMQ_ACT_RELU 1
+#define AMQ_ACT_GELU 2 /* z Phi(z), the exact form */
+#define AMQ_ACT_SILU 3 /* z sigmoid(z) */
+#define AMQ_ACT_SIGMOID 4
+#define AMQ_ACT_TANH 5
+size_t amq_linear_workspace_bytes(int64_t rows, int64_t k, int64_t n, int type);
+int amq_linear(const void* x, int64_t ld_x, const void* W, int64_t ld_w, int64_t rows, int64_t k, int64_t n, int type,
+               const void* bias, int activation, const void* residual, int64_t ld_r, void* y, int64_t ld_y, void* pre,
+               int64_t ld_pre, void* workspace, size_t workspace_bytes, void* stream);
+size_t amq_linear_backward_workspace_bytes(int64_t rows, int64_t k, int64_t n, int type);
+int amq_linear_backward(const void* dy, int64_t ld_dy, const void* x, int64_t ld_x, const void* W, int64_t ld_w,
+                        const void* pre, int64_t ld_pre, int64_t rows, int64_t k, int64_t n, int type, int activation,
+                        void* dx, int64_t ld_dx, void* dW, int64_t ld_dw, void* dbias, void* workspace,
+                        size_t workspace_bytes, void* stream);
+
+/*
+ * Orthogonalizes updates by Newton-Schulz products: X = G / (|G|_F + eps), then `steps` times
+ *   A = X X^T,  X = a X + (b A + c A A) X      (on the transpose where rows > cols)
+ * with coef = {a, b, c} (host); the result has the singular vectors of G and singular values driven towards 1.
+ *   G [batch][rows][ld], out [batch][rows][ld_out] of `type`, matrices batch_stride and batch_stride_out elements apart
+ *   (0 for densely stacked rows); out may be G itself (same strides).  steps >= 0, eps >= 0 and not both 0 for a zero matrix.
+ * Iterates are held as two halves of 11 bits, or as one (bfloat16 data, rows and cols >= 512: the result differs from the exact
+ * one by less than the rounding to bfloat16 does), scaled by 2^12: entries of an iterate at 16 and above, which only
+ * coefficients that diverge produce, become infinite.
+ *   workspace: at least amq_orthogonalize_workspace_bytes(batch, rows, cols, type) bytes, 256-byte aligned.
+ */
+size_t amq_orthogonalize_workspace_bytes(int64_t batch, int64_t rows, int64_t cols, int type);
+int amq_orthogonalize(const void* G, int64_t batch, int64_t batch_stride, int64_t rows, int64_t cols, int64_t ld, int type,
+                      int steps, const float* coef, float eps, void* out, int64_t batch_stride_out, int64_t ld_out,
+                      void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

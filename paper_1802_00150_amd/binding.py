@@ -35,6 +35,9 @@ EXPORTS = [
     "amq_quantize_refined_greedy", "amq_quantize_ternary", "amq_relative_mse",
     "amq_quantize_weights_ex", "amq_dequantize", "amq_quantize_reconstruct", "amq_clip",
     "amq_gru_reset_before_workspace_bytes", "amq_gru_step_reset_before",
+    "amq_layer_norm", "amq_layer_norm_backward_workspace_bytes", "amq_layer_norm_backward",
+    "amq_linear_workspace_bytes", "amq_linear", "amq_linear_backward_workspace_bytes", "amq_linear_backward",
+    "amq_orthogonalize_workspace_bytes", "amq_orthogonalize",
 ]
 
 _lib = None
@@ -123,6 +126,22 @@ def lib():
         L.amq_quantize_reconstruct.argtypes = [_p, _i64, _i64, _i64, _int, _int, _p, _i64, _p]
         L.amq_dequantize.argtypes = [_p, _p, _i64, _i64, _int, _p, _i64, _p]
         L.amq_clip.argtypes = [_p, _i64, C.c_float, C.c_float, _p]
+        L.amq_layer_norm.argtypes = [_p, _i64, _i64, _i64, _int, _p, _p, _int, C.c_float, _p, _i64, _p, _p, _p]
+        L.amq_layer_norm_backward_workspace_bytes.argtypes = [_i64, _i64]
+        L.amq_layer_norm_backward_workspace_bytes.restype = _sz
+        L.amq_layer_norm_backward.argtypes = [_p, _i64, _p, _i64, _i64, _i64, _int, _p, _int, _p, _p, _p, _i64, _p, _p, _p,
+                                              _sz, _p]
+        L.amq_linear_workspace_bytes.argtypes, L.amq_linear_workspace_bytes.restype = [_i64, _i64, _i64, _int], _sz
+        L.amq_linear.argtypes = [_p, _i64, _p, _i64, _i64, _i64, _i64, _int, _p, _int, _p, _i64, _p, _i64, _p, _i64, _p, _sz,
+                                 _p]
+        L.amq_linear_backward_workspace_bytes.argtypes = [_i64, _i64, _i64, _int]
+        L.amq_linear_backward_workspace_bytes.restype = _sz
+        L.amq_linear_backward.argtypes = [_p, _i64, _p, _i64, _p, _i64, _p, _i64, _i64, _i64, _i64, _int, _int, _p, _i64,
+                                          _p, _i64, _p, _p, _sz, _p]
+        L.amq_orthogonalize_workspace_bytes.argtypes = [_i64, _i64, _i64, _int]
+        L.amq_orthogonalize_workspace_bytes.restype = _sz
+        L.amq_orthogonalize.argtypes = [_p, _i64, _i64, _i64, _i64, _i64, _int, _int, C.POINTER(C.c_float), C.c_float, _p,
+                                        _i64, _i64, _p, _sz, _p]
         _lib = L
     return _lib
 
@@ -489,3 +508,68 @@ def fake_quantize(W, k, T=2):
     """w -> w_hat = sum_i alpha_i b_i (row-wise alternating quantization), differentiable with the straight-through
     gradient of Sec. 4: d f / d w = d f / d w_hat."""
     return (_native_module or _load_native()).fake_quantize(W, k, T)
+
+
+# ---- operators of quantization-aware training: float32, bfloat16 or float16 tensors [..., n] (a 2-D tensor's rows may be strided)
+
+ACTIVATIONS = {None: 0, "none": 0, "relu": 1, "gelu": 2, "silu": 3, "sigmoid": 4, "tanh": 5}
+
+
+def _activation(name):
+    if name not in ACTIVATIONS:
+        raise ValueError("activation: expected one of %s, got %r" % (", ".join(sorted(k for k in ACTIVATIONS if k)), name))
+    return ACTIVATIONS[name]
+
+
+def layer_norm(x, weight=None, bias=None, eps=1e-5, out=None):
+    """(x - mean) / sqrt(var + eps) * weight + bias over the last dimension -> y, mean, rstd (float32, one per row).
+    weight, bias: float32 or x's type; out may be x itself."""
+    return (_native_module or _load_native()).layer_norm(x, weight, bias, eps, out)
+
+
+def layer_norm_backward(dy, x, weight, mean, rstd, param_grads=True, ws=None, out=None):
+    """Gradients dx, dweight, dbias of layer_norm (the last two None without param_grads; of weight's type, or x's if
+    weight is None).  out receives dx and may be dy or x itself."""
+    return (_native_module or _load_native()).layer_norm_backward(dy, x, weight, mean, rstd, bool(param_grads), ws, out)
+
+
+def layer_norm_backward_workspace(rows, n, device):
+    return torch.empty(int(lib().amq_layer_norm_backward_workspace_bytes(rows, n)), dtype=torch.uint8, device=device)
+
+
+_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+
+def linear(x, W, bias=None, activation=None, residual=None, ws=None, out=None, pre=None):
+    """activation(x W^T + bias) + residual: x [..., k], W [n, k], bias [n], residual and result [..., n].
+    activation: None, "relu", "gelu" (exact), "silu", "sigmoid" or "tanh".  pre [..., n] (optional) receives
+    x W^T + bias, which linear_backward takes.  out may be the residual itself."""
+    return (_native_module or _load_native()).linear(x, W, bias, _activation(activation), residual, ws, out, pre)
+
+
+def linear_workspace(rows, k, n, dtype, device):
+    return torch.empty(int(lib().amq_linear_workspace_bytes(rows, k, n, _TYPES[dtype])), dtype=torch.uint8, device=device)
+
+
+def linear_backward(dy, x, W, pre=None, activation=None, input_grad=True, weight_grad=True, bias=True, ws=None):
+    """Gradients dx, dW, dbias of linear (None where not wanted); the residual's gradient is dy itself.  pre: what linear
+    left there, needed with an activation."""
+    wanted = (1 if input_grad else 0) | (2 if weight_grad else 0) | (4 if bias else 0)
+    return (_native_module or _load_native()).linear_backward(dy, x, W, pre, _activation(activation), wanted, ws)
+
+
+def linear_backward_workspace(rows, k, n, dtype, device):
+    return torch.empty(int(lib().amq_linear_backward_workspace_bytes(rows, k, n, _TYPES[dtype])), dtype=torch.uint8,
+                       device=device)
+
+
+def orthogonalize(G, steps=5, coefficients=(3.4445, -4.7750, 2.0315), eps=1e-7, ws=None, out=None):
+    """X = G / (|G| + eps), then `steps` times A = X X^T, X = a X + (b A + c A A) X, of a matrix [rows, cols] or a stack of
+    them [batch, rows, cols]: the singular vectors of G with singular values near 1.  out may be G itself."""
+    a, b, c = coefficients
+    return (_native_module or _load_native()).orthogonalize(G, steps, a, b, c, eps, ws, out)
+
+
+def orthogonalize_workspace(batch, rows, cols, dtype, device):
+    return torch.empty(int(lib().amq_orthogonalize_workspace_bytes(batch, rows, cols, _TYPES[dtype])), dtype=torch.uint8,
+                       device=device)

@@ -5,6 +5,7 @@
 #include <mutex>
 
 #include "amq_launch.h"
+#include "amq_train.h"
 
 // Scratch memory of amq_lstm_step_static, part of the code object: one copy per GPU the library
 // runs on, held until the process ends.  In host code this name is only a handle for
@@ -299,6 +300,8 @@ int quantize_common(const float* X, int64_t rows, int64_t n, int64_t ld, int k, 
 }
 
 }  // namespace
+
+int amq::status_of(hipError_t e) { return hip_status(e); }
 
 extern "C" {
 

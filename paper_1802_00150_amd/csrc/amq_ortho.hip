@@ -1,0 +1,302 @@
+// Orthogonalized updates: X = G / (|G|_F + eps), then `steps` times A = X X^T, B = b A + c A A, X = a X + B X.
+//
+// n <= m are the sizes of X (the transpose of G where G is tall).  Per step n^2 m + n^3 + 2 n^2 m operations, since A and
+// A A are symmetric and only tiles on and below the diagonal are computed: bound by the matrix cores from about n = 512 on,
+// by the chain of three dependent launches per step below.
+//
+// Iterates, A and B are held as half values times 2^12, in two planes (22 bits) for float and half data and small matrices,
+// in one for bfloat16 data from n = 512 on.  Singular values stay below about 1.2 with the usual coefficients, so nothing comes near 65504 / 4096 = 16,
+// and half's smallest step is 2^-36 of an entry of 1.  One plane loses 1.4e-3 of the result in the 2-norm over five
+// steps, and the rounding to bfloat16 1.7e-3; two planes lose 3e-7.
+// X is kept in both orders, as either is an operand whose contraction runs along rows: X X^T takes X, B X takes X^T.
+// The norm is summed in binary64, so that no gradient's scale overflows its square.
+#include "../../include/amq.h"
+
+#include "amq_device.h"
+#include "amq_matmul_body.h"
+#include "amq_train.h"
+
+namespace amq {
+namespace {
+
+constexpr float kScale = 4096.0f, kInvScale = 1.0f / 4096.0f;
+constexpr int kNormParts = 256;
+
+struct __attribute__((packed, aligned(8))) Half4 {
+  f16 v[4];
+};
+
+// A matrix of scaled values in NP planes, [batch][rows][ld], ld a multiple of 64; zeros from `cols` to ld.
+template <int NP>
+struct Planes {
+  f16* p;
+  int64_t ld, plane, batch;
+  int rows, cols;
+  // four values along a row (col a multiple of 4)
+  __device__ __forceinline__ f32x4 load(int z, int row, int col) const {
+    const f16* q = p + z * batch + row * ld + col;
+    const Half4 h = *reinterpret_cast<const Half4*>(q);
+    f32x4 v = {(float)h.v[0], (float)h.v[1], (float)h.v[2], (float)h.v[3]};
+    if constexpr (NP == 2) {
+      const Half4 l = *reinterpret_cast<const Half4*>(q + plane);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] += (float)l.v[i];
+    }
+    return v;
+  }
+  __device__ __forceinline__ bool has(int row, int col) const { return row < rows && col < ld; }
+  __device__ __forceinline__ void store(int z, int row, int col, f32x4 v) const {
+    f16* q = p + z * batch + row * ld + col;
+    Half4 h, l;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float s = col + i < cols ? v[i] : 0.0f;
+      h.v[i] = (f16)s;
+      l.v[i] = (f16)(s - (float)h.v[i]);
+    }
+    *reinterpret_cast<Half4*>(q) = h;
+    if constexpr (NP == 2) *reinterpret_cast<Half4*>(q + plane) = l;
+  }
+};
+
+// A = X X^T, both triangles from the lower tiles.
+template <int NP>
+struct GramStore {
+  static constexpr bool kTransposed = true;
+  Planes<NP> A;
+  __device__ __forceinline__ void along_n(int z, int m, int n, f32x4 v) const {
+    if (A.has(m, n)) A.store(z, m, n, v * kInvScale);
+  }
+  __device__ __forceinline__ void along_m(int z, int m, int n, f32x4 v) const { along_n(z, n, m, v); }
+};
+// B = b A + c A A.
+template <int NP>
+struct PolynomialStore {
+  static constexpr bool kTransposed = true;
+  Planes<NP> A, B;
+  float b, c;
+  __device__ __forceinline__ void along_n(int z, int m, int n, f32x4 v) const {
+    if (B.has(m, n)) B.store(z, m, n, A.load(z, m, n) * b + v * (c * kInvScale));
+  }
+  __device__ __forceinline__ void along_m(int z, int m, int n, f32x4 v) const { along_n(z, n, m, v); }
+};
+// X = a X + B X in both orders.
+template <int NP>
+struct UpdateStore {
+  static constexpr bool kTransposed = true;
+  Planes<NP> X, Xt, next_t;  // X in place, its transpose not: it is an operand of the product
+  float a;
+  __device__ __forceinline__ void along_n(int z, int m, int n, f32x4 v) const {
+    if (X.has(m, n)) X.store(z, m, n, X.load(z, m, n) * a + v * kInvScale);
+  }
+  __device__ __forceinline__ void along_m(int z, int m, int n, f32x4 v) const {
+    if (next_t.has(n, m)) next_t.store(z, n, m, Xt.load(z, n, m) * a + v * kInvScale);
+  }
+};
+// The last X, in the order of G.
+template <int NP, typename T, bool TALL>
+struct ResultStore {
+  static constexpr bool kTransposed = TALL;
+  Planes<NP> X, Xt;
+  T* out;
+  int64_t ld, batch;
+  float a;
+  __device__ __forceinline__ void put(int z, int row, int col, int cols, f32x4 v) const {
+    T* q = out + z * batch + row * ld + col;
+    struct __attribute__((packed, aligned(sizeof(T)))) {
+      T v[4];
+    } o;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o.v[i] = (T)(v[i] * kInvScale);
+    if (col + 4 <= cols) __builtin_memcpy(q, &o, sizeof(o));
+    else
+      for (int i = 0; i < cols - col; ++i) q[i] = (T)(v[i] * kInvScale);
+  }
+  __device__ __forceinline__ void along_n(int z, int m, int n, f32x4 v) const {
+    if constexpr (!TALL)
+      if (m < X.rows && n < X.cols) put(z, m, n, X.cols, X.load(z, m, n) * a + v * kInvScale);
+  }
+  __device__ __forceinline__ void along_m(int z, int m, int n, f32x4 v) const {
+    if constexpr (TALL)
+      if (n < Xt.rows && m < Xt.cols) put(z, n, m, Xt.cols, Xt.load(z, n, m) * a + v * kInvScale);
+  }
+};
+
+template <typename T>
+struct Gradient {
+  const T* p;
+  int64_t ld, batch;
+  int rows, cols;
+};
+
+// Sums of squares, kNormParts of them per matrix.
+template <typename T>
+__global__ __launch_bounds__(256) void ortho_norm_kernel(Gradient<T> G, double* parts) {
+  __shared__ double scratch[4];
+  constexpr int V = kPer16<T>;
+  const T* p = G.p + blockIdx.y * G.batch;
+  double s = 0.0;
+  // pieces of 256 x V values of a row, dealt to the workgroups in turn
+  const int64_t across = (G.cols + 256 * V - 1) / (256 * V), pieces = across * G.rows;
+  for (int64_t i = blockIdx.x; i < pieces; i += gridDim.x) {
+    const int64_t row = i / across;
+    const int col = ((int)(i % across) * 256 + (int)threadIdx.x) * V;
+    float v[V];
+    load16(p + row * G.ld + col, G.cols - col, v);
+#pragma unroll
+    for (int q = 0; q < V; ++q) s += (double)v[q] * (double)v[q];
+  }
+  s = block_sum<4>(s, scratch);
+  if (threadIdx.x == 0) parts[(int64_t)blockIdx.y * kNormParts + blockIdx.x] = s;
+}
+
+// 1 / (|G| + eps) of matrix z from its partial sums, by a whole workgroup of 256.
+__device__ __forceinline__ float inverse_norm(const double* parts, int z, int count, float eps, double* scratch) {
+  const double s = (int)threadIdx.x < count ? parts[(int64_t)z * kNormParts + threadIdx.x] : 0.0;
+  return (float)(1.0 / (sqrt(block_sum<4>(s, scratch)) + (double)eps));
+}
+
+// X_0 in both orders, 64 x 64 values per workgroup: `same` has the order of G, `turned` that of its transpose.
+template <typename T, int NP>
+__global__ __launch_bounds__(256) void ortho_begin_kernel(Gradient<T> G, const double* parts, int count, float eps, Planes<NP> same, Planes<NP> turned) {
+  __shared__ double scratch[4];
+  __shared__ float t[64][65];
+  const int z = blockIdx.z, r0 = blockIdx.y * 64, c0 = blockIdx.x * 64;
+  const float scale = inverse_norm(parts, z, count, eps, scratch) * kScale;
+  const T* p = G.p + z * G.batch;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int row = i * 16 + (threadIdx.x >> 4), col = (threadIdx.x & 15) * 4;
+    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (r0 + row < G.rows) {
+      load_params<T, 4>(p, (int64_t)(r0 + row) * G.ld + c0 + col, G.cols - c0 - col, 0.0f, v);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) v[q] *= scale;
+      same.store(z, r0 + row, c0 + col, f32x4{v[0], v[1], v[2], v[3]});
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) t[row][col + q] = v[q];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int col = i * 16 + (threadIdx.x >> 4), row = (threadIdx.x & 15) * 4;
+    if (c0 + col < G.cols) turned.store(z, c0 + col, r0 + row, f32x4{t[row][col], t[row + 1][col], t[row + 2][col], t[row + 3][col]});
+  }
+}
+
+// No steps: the scaled gradient itself.
+template <typename T>
+__global__ __launch_bounds__(256) void ortho_scale_kernel(Gradient<T> G, const double* parts, int count, float eps, T* out, int64_t ld, int64_t batch) {
+  __shared__ double scratch[4];
+  const int z = blockIdx.z;
+  const float scale = inverse_norm(parts, z, count, eps, scratch);
+  const int col = blockIdx.x * 256 + threadIdx.x;
+  if (col >= G.cols) return;
+  for (int64_t row = blockIdx.y; row < G.rows; row += gridDim.y)
+    out[z * batch + row * ld + col] = (T)((float)G.p[z * G.batch + row * G.ld + col] * scale);
+}
+
+struct Room {
+  f16 *X, *Xt[2], *A, *B;
+  double* parts;
+  float* part;
+  int64_t n, m, np, mp;
+  size_t total;
+};
+ProductPlan gram_plan(const Room& r, int planes, int64_t batch) { return plan_product(r.n, r.n, r.mp, planes, batch, true); }
+ProductPlan polynomial_plan(const Room& r, int planes, int64_t batch) { return plan_product(r.n, r.n, r.np, planes, batch, true); }
+ProductPlan update_plan(const Room& r, int planes, int64_t batch) { return plan_product(r.n, r.m, r.np, planes, batch, false); }
+
+Room room_of(void* ws, int64_t batch, int64_t rows, int64_t cols, int planes) {
+  Room r{};
+  r.n = rows < cols ? rows : cols;
+  r.m = rows < cols ? cols : rows;
+  r.np = pad64(r.n);
+  r.mp = pad64(r.m);
+  char* base = static_cast<char*>(ws);
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    void* p = base ? base + off : nullptr;
+    off += (bytes + 255) & ~size_t(255);
+    return p;
+  };
+  const size_t value = sizeof(f16) * (size_t)planes * batch;
+  r.X = (f16*)take(value * r.n * r.mp);
+  r.Xt[0] = (f16*)take(value * r.m * r.np);
+  r.Xt[1] = (f16*)take(value * r.m * r.np);
+  r.A = (f16*)take(value * r.n * r.np);
+  r.B = (f16*)take(value * r.n * r.np);
+  r.parts = (double*)take(sizeof(double) * kNormParts * (size_t)batch);
+  size_t most = gram_plan(r, planes, batch).part_bytes;
+  for (size_t b : {polynomial_plan(r, planes, batch).part_bytes, update_plan(r, planes, batch).part_bytes})
+    if (b > most) most = b;
+  r.part = (float*)take(most);
+  r.total = off;
+  return r;
+}
+
+// One plane's error grows as matrices shrink (2.0e-3 of a result in bfloat16 at n = 512, 2.4e-3 at n = 64, of which the
+// rounding is 1.7e-3), while small ones are bound by their launches and two planes cost them nothing.
+int planes_of(int type, int64_t rows, int64_t cols) { return type == AMQ_BF16 && (rows < cols ? rows : cols) >= 512 ? 1 : 2; }
+
+template <typename T, int NP>
+hipError_t run(const OrthoArgs& o, hipStream_t s) {
+  const Room r = room_of(o.ws, o.batch, o.rows, o.cols, NP);
+  const bool tall = o.rows > o.cols;
+  const Gradient<T> G{(const T*)o.G, o.ld_g, o.stride_g, o.rows, o.cols};
+  T* out = (T*)o.out;
+  auto planes = [&](f16* p, int64_t rows, int64_t ld, int64_t cols) { return Planes<NP>{p, ld, o.batch * rows * ld, rows * ld, (int)rows, (int)cols}; };
+  const Planes<NP> X = planes(r.X, r.n, r.mp, r.m), A = planes(r.A, r.n, r.np, r.n), B = planes(r.B, r.n, r.np, r.n);
+  const Planes<NP> Xt[2] = {planes(r.Xt[0], r.m, r.np, r.n), planes(r.Xt[1], r.m, r.np, r.n)};
+
+  const int64_t pieces = div_up(o.cols, 256 * kPer16<T>) * o.rows;
+  const int count = (int)(pieces < kNormParts ? pieces : kNormParts);
+  ortho_norm_kernel<T><<<dim3((unsigned)count, (unsigned)o.batch), dim3(256), 0, s>>>(G, r.parts);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  if (o.steps == 0) {
+    ortho_scale_kernel<T><<<dim3((unsigned)div_up(o.cols, 256), (unsigned)(o.rows < 1024 ? o.rows : 1024), (unsigned)o.batch), dim3(256), 0, s>>>(
+        G, r.parts, count, o.eps, out, o.ld_out, o.stride_out);
+    return hipGetLastError();
+  }
+  ortho_begin_kernel<T, NP><<<dim3((unsigned)div_up(o.cols, 64), (unsigned)div_up(o.rows, 64), (unsigned)o.batch), dim3(256), 0, s>>>(
+      G, r.parts, count, o.eps, tall ? Xt[0] : X, tall ? X : Xt[0]);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+
+  auto args = [&](const Planes<NP>& rows, const Planes<NP>& cols, int64_t k, bool lower) {
+    MatmulArgs g{};
+    g.r = {rows.p, rows.ld, rows.plane, rows.batch, rows.rows};
+    g.c = {cols.p, cols.ld, cols.plane, cols.batch, cols.rows};
+    g.M = rows.rows;
+    g.N = cols.rows;
+    g.tiles_k = (int)k;
+    g.lower = lower;
+    return g;
+  };
+  const ProductPlan gram = gram_plan(r, NP, o.batch), polynomial = polynomial_plan(r, NP, o.batch), update = update_plan(r, NP, o.batch);
+  for (int i = 0; i < o.steps; ++i) {
+    const Planes<NP>&now = Xt[i & 1], &next = Xt[(i + 1) & 1];
+    if ((e = launch_product<f16, NP>(args(X, X, r.mp, true), gram, o.batch, GramStore<NP>{A}, r.part, s)) != hipSuccess) return e;
+    if ((e = launch_product<f16, NP>(args(A, A, r.np, true), polynomial, o.batch, PolynomialStore<NP>{A, B, o.b, o.c}, r.part, s)) != hipSuccess)
+      return e;
+    const MatmulArgs g = args(B, now, r.np, false);
+    if (i + 1 < o.steps) e = launch_product<f16, NP>(g, update, o.batch, UpdateStore<NP>{X, now, next, o.a}, r.part, s);
+    else if (tall) e = launch_product<f16, NP>(g, update, o.batch, ResultStore<NP, T, true>{X, now, out, o.ld_out, o.stride_out, o.a}, r.part, s);
+    else e = launch_product<f16, NP>(g, update, o.batch, ResultStore<NP, T, false>{X, now, out, o.ld_out, o.stride_out, o.a}, r.part, s);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+}  // namespace
+
+size_t ortho_workspace(int64_t batch, int64_t rows, int64_t cols, int type) { return room_of(nullptr, batch, rows, cols, planes_of(type, rows, cols)).total; }
+
+hipError_t launch_ortho(const OrthoArgs& a, hipStream_t s) {
+  if (a.type == AMQ_F32) return run<float, 2>(a, s);
+  if (a.type == AMQ_F16) return run<f16, 2>(a, s);
+  return planes_of(a.type, a.rows, a.cols) == 1 ? run<bf16, 1>(a, s) : run<bf16, 2>(a, s);
+}
+
+}  // namespace amq

@@ -8,6 +8,7 @@
 #include <dlfcn.h>
 
 #include <string>
+#include <vector>
 
 #include <ATen/hip/EmptyTensor.h>
 #include <c10/hip/HIPStream.h>
@@ -27,7 +28,9 @@ namespace {
   X(amq_embedding_lookup) X(amq_log_softmax) X(amq_softmax_layer_workspace_bytes) X(amq_softmax_layer)              \
   X(amq_lm_workspace_bytes) X(amq_lm_step) X(amq_lm_sequence_workspace_bytes) X(amq_lm_sequence)                    \
   X(amq_lm_sequence_score_workspace_bytes) X(amq_lm_sequence_score) X(amq_dequantize)      \
-  X(amq_quantize_reconstruct)
+  X(amq_quantize_reconstruct) X(amq_layer_norm) X(amq_layer_norm_backward_workspace_bytes) X(amq_layer_norm_backward) \
+  X(amq_linear_workspace_bytes) X(amq_linear) X(amq_linear_backward_workspace_bytes) X(amq_linear_backward)          \
+  X(amq_orthogonalize_workspace_bytes) X(amq_orthogonalize)
 
 struct Api {
 #define AMQ_MEMBER(name) decltype(&::name) name = nullptr;
@@ -481,6 +484,226 @@ PyObject* fake_quantize(PyObject* const* a) {  // W, k, T
   return wrap(FakeQuantize::apply(tensor(a[0]), integer(a[1]), integer(a[2])));
 }
 
+// ---- training operators: float32, bfloat16 and float16 tensors, rows of any stride
+
+int type_of(const at::Tensor& t) {
+  switch (t.scalar_type()) {
+    case at::kFloat: return AMQ_F32;
+    case at::kBFloat16: return AMQ_BF16;
+    case at::kHalf: return AMQ_F16;
+    default: fail(amq_error, std::string("expected a float32, bfloat16 or float16 tensor, got ") + dtype_name(t.scalar_type()));
+  }
+}
+
+// A tensor [..., n] as rows: a 2-D tensor with unit column stride, or a contiguous one of any dimensions.
+struct Rows {
+  const at::Tensor* t = nullptr;
+  void* p = nullptr;
+  int64_t rows = 0, n = 0, ld = 0;
+  Rows() = default;
+  explicit Rows(const at::Tensor& x) : t(&x) {
+    if (!x.is_cuda()) fail(amq_error, "expected a GPU tensor");
+    if (x.dim() < 1) fail(PyExc_ValueError, "expected a tensor of at least one dimension");
+    n = x.size(-1);
+    if (x.dim() == 2 && (x.stride(1) == 1 || n == 1)) {
+      rows = x.size(0);
+      ld = rows > 1 ? x.stride(0) : n;
+      if (ld < n) fail(amq_error, "expected rows that do not overlap");
+    } else if (x.is_contiguous()) {
+      rows = n ? x.numel() / n : 0;
+      ld = n;
+    } else {
+      fail(amq_error, "expected a contiguous tensor, or a 2-D tensor with unit column stride");
+    }
+    p = x.data_ptr();
+  }
+  // the same, checked against what another tensor has
+  Rows(const at::Tensor& x, const char* name, int64_t want_rows, int64_t want_n, const at::Tensor& like) : Rows(x) {
+    if (rows != want_rows || n != want_n)
+      fail(PyExc_ValueError, std::string(name) + ": expected " + std::to_string(want_rows) + " rows of " + std::to_string(want_n) + ", got " +
+                                 std::to_string(rows) + " of " + std::to_string(n));
+    if (x.scalar_type() != like.scalar_type())
+      fail(amq_error, std::string(name) + ": expected " + dtype_name(like.scalar_type()) + ", got " + dtype_name(x.scalar_type()));
+    if (x.device() != like.device()) fail(amq_error, std::string(name) + ": expected a tensor on the same device");
+  }
+  static Rows optional(PyObject* o, const char* name, int64_t rows, int64_t n, const at::Tensor& like) {
+    return o == Py_None ? Rows() : Rows(tensor(o), name, rows, n, like);
+  }
+};
+
+// A contiguous vector of n entries of one of two types, or null.
+void* vector_of(PyObject* o, const char* name, int64_t n, at::ScalarType a, at::ScalarType b, const at::Tensor& like) {
+  if (o == Py_None) return nullptr;
+  const at::Tensor& t = tensor(o);
+  if (!t.is_cuda() || t.device() != like.device()) fail(amq_error, std::string(name) + ": expected a tensor on the same GPU");
+  if (t.scalar_type() != a && t.scalar_type() != b)
+    fail(amq_error, std::string(name) + ": expected " + dtype_name(a) + (a == b ? "" : std::string(" or ") + dtype_name(b)) + ", got " + dtype_name(t.scalar_type()));
+  if (t.dim() != 1 || t.size(0) != n || !t.is_contiguous())
+    fail(PyExc_ValueError, std::string(name) + ": expected a contiguous vector of " + std::to_string(n));
+  return t.data_ptr();
+}
+
+double real(PyObject* o) {
+  const double v = PyFloat_AsDouble(o);
+  if (v == -1.0 && PyErr_Occurred()) throw PythonError();
+  return v;
+}
+
+// A result of the same shape and type as another tensor: the caller's, or a new one.
+struct Result {
+  at::Tensor own;
+  Rows rows;
+  PyObject* given;
+  Result(PyObject* o, const char* name, at::IntArrayRef shape, int64_t want_rows, int64_t want_n, const at::Tensor& like) : given(o) {
+    if (o == Py_None) {
+      own = make(shape, like.scalar_type(), like);
+      rows = Rows(own, name, want_rows, want_n, like);
+    } else {
+      rows = Rows(tensor(o), name, want_rows, want_n, like);
+    }
+  }
+  PyObject* take() { return given == Py_None ? wrap(own) : again(given); }
+};
+
+PyObject* none() { return again(Py_None); }
+PyObject* triple(PyObject* a, PyObject* b, PyObject* c) {  // takes the references
+  PyObject* r = (a && b && c) ? PyTuple_Pack(3, a, b, c) : nullptr;
+  Py_XDECREF(a);
+  Py_XDECREF(b);
+  Py_XDECREF(c);
+  return r;
+}
+
+PyObject* layer_norm(PyObject* const* a) {  // x, weight, bias, eps, out
+  const at::Tensor& x = tensor(a[0]);
+  const int type = type_of(x);
+  const Rows r(x);
+  const float eps = (float)real(a[3]);
+  const void* w = vector_of(a[1], "weight", r.n, at::kFloat, x.scalar_type(), x);
+  const void* b = vector_of(a[2], "bias", r.n, at::kFloat, x.scalar_type(), x);
+  if (w && b && tensor(a[1]).scalar_type() != tensor(a[2]).scalar_type()) fail(amq_error, "weight and bias: expected the same type");
+  const int param_type = w ? type_of(tensor(a[1])) : b ? type_of(tensor(a[2])) : type;
+  Result y(a[4], "out", x.sizes(), r.rows, r.n, x);
+  const at::IntArrayRef lead = x.sizes().slice(0, x.dim() - 1);
+  at::Tensor mean = make(lead, at::kFloat, x), rstd = make(lead, at::kFloat, x);
+  float *m = static_cast<float*>(mean.data_ptr()), *q = static_cast<float*>(rstd.data_ptr());
+  void* s = stream();
+  call([&] { return api.amq_layer_norm(r.p, r.ld, r.rows, r.n, type, w, b, param_type, eps, y.rows.p, y.rows.ld, m, q, s); });
+  return triple(y.take(), wrap(mean), wrap(rstd));
+}
+
+PyObject* layer_norm_backward(PyObject* const* a) {  // dy, x, weight, mean, rstd, param_grads, ws, dx
+  const at::Tensor& x = tensor(a[1]);
+  const int type = type_of(x);
+  const Rows r(x), d(tensor(a[0]), "dy", r.rows, r.n, x);
+  const void* w = vector_of(a[2], "weight", r.n, at::kFloat, x.scalar_type(), x);
+  const at::ScalarType pt = w ? tensor(a[2]).scalar_type() : x.scalar_type();
+  const int param_type = w ? type_of(tensor(a[2])) : type;
+  const at::Tensor &mean = tensor(a[3]), &rstd = tensor(a[4]);
+  const float *m = static_cast<const float*>(dev(mean, at::kFloat)), *q = static_cast<const float*>(dev(rstd, at::kFloat));
+  if (mean.numel() != r.rows || rstd.numel() != r.rows) fail(PyExc_ValueError, "mean, rstd: expected one value per row");
+  const bool params = integer(a[5]) != 0;
+  Result dx(a[7], "dx", x.sizes(), r.rows, r.n, x);
+  at::Tensor dw, db;
+  if (params) {
+    dw = make({r.n}, pt, x);
+    db = make({r.n}, pt, x);
+  }
+  void *pw = params ? dw.data_ptr() : nullptr, *pb = params ? db.data_ptr() : nullptr;
+  Workspace ws(a[6], x, [&] { return params ? api.amq_layer_norm_backward_workspace_bytes(r.rows, r.n) : 0; });
+  void* s = stream();
+  call([&] {
+    return api.amq_layer_norm_backward(d.p, d.ld, r.p, r.ld, r.rows, r.n, type, w, param_type, m, q, dx.rows.p, dx.rows.ld, pw, pb, ws.ptr,
+                                       ws.bytes, s);
+  });
+  return triple(dx.take(), params ? wrap(dw) : none(), params ? wrap(db) : none());
+}
+
+// W [n][k] of a linear layer, against x [rows][k]
+Rows matrix(PyObject* o, const char* name, const at::Tensor& like) {
+  const at::Tensor& t = shaped(o, 2);
+  return Rows(t, name, t.size(0), t.size(1), like);
+}
+
+PyObject* linear(PyObject* const* a) {  // x, W, bias, activation, residual, ws, out, pre
+  const at::Tensor& x = tensor(a[0]);
+  const int type = type_of(x), act = (int)integer(a[3]);
+  const Rows r(x), W = matrix(a[1], "W", x);
+  if (W.n != r.n) fail(PyExc_ValueError, "W: expected rows of " + std::to_string(r.n) + ", got " + std::to_string(W.n));
+  const int64_t n = W.rows;
+  const void* b = vector_of(a[2], "bias", n, x.scalar_type(), x.scalar_type(), x);
+  const Rows res = Rows::optional(a[4], "residual", r.rows, n, x), pre = Rows::optional(a[7], "pre", r.rows, n, x);
+  std::vector<int64_t> shape(x.sizes().begin(), x.sizes().end());
+  shape.back() = n;
+  Result y(a[6], "out", shape, r.rows, n, x);
+  Workspace ws(a[5], x, [&] { return api.amq_linear_workspace_bytes(r.rows, r.n, n, type); });
+  void* s = stream();
+  call([&] {
+    return api.amq_linear(r.p, r.ld, W.p, W.ld, r.rows, r.n, n, type, b, act, res.p, res.ld, y.rows.p, y.rows.ld, pre.p, pre.ld, ws.ptr,
+                          ws.bytes, s);
+  });
+  return y.take();
+}
+
+PyObject* linear_backward(PyObject* const* a) {  // dy, x, W, pre, activation, wanted (1 dx, 2 dW, 4 dbias), ws
+  const at::Tensor &dy = tensor(a[0]), &x = tensor(a[1]);
+  const int type = type_of(x), act = (int)integer(a[4]), wanted = (int)integer(a[5]);
+  const Rows r(x), W = matrix(a[2], "W", x);
+  if (W.n != r.n) fail(PyExc_ValueError, "W: expected rows of " + std::to_string(r.n) + ", got " + std::to_string(W.n));
+  const int64_t n = W.rows, k = r.n;
+  const Rows d(dy, "dy", r.rows, n, x), pre = Rows::optional(a[3], "pre", r.rows, n, x);
+  at::Tensor dx, dW, db;
+  if (wanted & 1) dx = make(x.sizes(), x.scalar_type(), x);
+  if (wanted & 2) dW = make({n, k}, x.scalar_type(), x);
+  if (wanted & 4) db = make({n}, x.scalar_type(), x);
+  auto at_of = [](const at::Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; };
+  void *px = at_of(dx), *pw = at_of(dW), *pb = at_of(db);
+  Workspace ws(a[6], x, [&] { return api.amq_linear_backward_workspace_bytes(r.rows, k, n, type); });
+  void* s = stream();
+  call([&] {
+    return api.amq_linear_backward(d.p, d.ld, r.p, r.ld, W.p, W.ld, pre.p, pre.ld, r.rows, k, n, type, act, px, k, pw, k, pb, ws.ptr,
+                                   ws.bytes, s);
+  });
+  return triple(px ? wrap(dx) : none(), pw ? wrap(dW) : none(), pb ? wrap(db) : none());
+}
+
+// A matrix or a stack of matrices: [rows, cols] or [batch, rows, cols], unit column stride.
+struct Stack {
+  void* p;
+  int64_t batch, rows, cols, ld, stride;
+  explicit Stack(const at::Tensor& t) {
+    if (!t.is_cuda()) fail(amq_error, "expected a GPU tensor");
+    if (t.dim() != 2 && t.dim() != 3) fail(PyExc_ValueError, "expected a matrix or a stack of matrices");
+    batch = t.dim() == 3 ? t.size(0) : 1;
+    rows = t.size(-2);
+    cols = t.size(-1);
+    if (cols > 1 && t.stride(-1) != 1) fail(amq_error, "expected a tensor with unit column stride");
+    ld = rows > 1 ? t.stride(-2) : cols;
+    stride = batch > 1 ? t.stride(0) : 0;
+    if (ld < cols || (batch > 1 && stride < (rows - 1) * ld + cols)) fail(amq_error, "expected rows and matrices that do not overlap");
+    p = t.data_ptr();
+  }
+};
+
+PyObject* orthogonalize(PyObject* const* a) {  // G, steps, a, b, c, eps, ws, out
+  const at::Tensor& G = tensor(a[0]);
+  const int type = type_of(G), steps = (int)integer(a[1]);
+  const float coef[3] = {(float)real(a[2]), (float)real(a[3]), (float)real(a[4])}, eps = (float)real(a[5]);
+  const Stack g(G);
+  at::Tensor own;
+  if (a[7] == Py_None) own = make(G.sizes(), G.scalar_type(), G);
+  const at::Tensor& out = a[7] == Py_None ? own : tensor(a[7]);
+  if (out.sizes() != G.sizes()) fail(PyExc_ValueError, "out: expected the shape of G");
+  if (out.scalar_type() != G.scalar_type() || out.device() != G.device()) fail(amq_error, "out: expected the type and device of G");
+  const Stack o(out);
+  Workspace ws(a[6], G, [&] { return api.amq_orthogonalize_workspace_bytes(g.batch, g.rows, g.cols, type); });
+  void* s = stream();
+  call([&] {
+    return api.amq_orthogonalize(g.p, g.batch, g.stride, g.rows, g.cols, g.ld, type, steps, coef, eps, o.p, o.stride, o.ld, ws.ptr, ws.bytes, s);
+  });
+  return a[7] == Py_None ? wrap(own) : again(a[7]);
+}
+
 // ---- module
 
 template <PyObject* (*F)(PyObject* const*), int N>
@@ -532,6 +755,8 @@ PyMethodDef methods[] = {
     AMQ_METHOD(gru_sequence, 14), AMQ_METHOD(embedding_lookup, 4), AMQ_METHOD(log_softmax, 2),
     AMQ_METHOD(softmax_layer, 9), AMQ_METHOD(lm_step, 20), AMQ_METHOD(lm_sequence, 20),
     AMQ_METHOD(lm_sequence_score, 21), AMQ_METHOD(dequantize, 4), AMQ_METHOD(fake_quantize, 3),
+    AMQ_METHOD(layer_norm, 5), AMQ_METHOD(layer_norm_backward, 8), AMQ_METHOD(linear, 8), AMQ_METHOD(linear_backward, 7),
+    AMQ_METHOD(orthogonalize, 8),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_amq_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

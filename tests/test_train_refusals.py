@@ -1,0 +1,73 @@
+"""Argument validation of the training operators' C ABI, which precedes any launch (no GPU)."""
+import ctypes as C
+import os
+
+import pytest
+
+
+@pytest.fixture(scope="module")
+def L():
+    from paper_1802_00150_amd import binding
+    if not os.path.exists(binding.LIB_PATH):
+        from paper_1802_00150_amd import build
+        build.build()
+    return binding.lib()
+
+
+P, ODD, NULL = C.c_void_p(0x10000), C.c_void_p(0x10001), C.c_void_p(0)
+INVALID, UNSUPPORTED = 1, 2
+F32, BF16, F16 = 0, 1, 2
+
+
+def call(f, args, **changed):
+    a = dict(args, **changed)
+    return f(*a.values())
+
+
+def test_layer_norm(L):
+    args = dict(x=P, ld_x=8, rows=4, n=8, type=F32, weight=P, bias=P, param_type=F32, eps=C.c_float(1e-5), y=P, ld_y=8, mean=P, rstd=P, stream=None)
+    for bad in (dict(x=NULL), dict(y=NULL), dict(ld_x=7), dict(ld_y=7), dict(rows=0), dict(n=0), dict(type=3), dict(param_type=BF16),
+                dict(type=BF16, param_type=F16), dict(eps=C.c_float(-1.0)), dict(eps=C.c_float(float("nan"))), dict(x=ODD), dict(y=ODD),
+                dict(weight=ODD), dict(mean=ODD)):
+        assert call(L.amq_layer_norm, args, **bad) == INVALID, bad
+    assert call(L.amq_layer_norm, args, n=(1 << 20) + 1, ld_x=1 << 21, ld_y=1 << 21) == UNSUPPORTED
+    assert call(L.amq_layer_norm, args, rows=1 << 31) == UNSUPPORTED
+    need = L.amq_layer_norm_backward_workspace_bytes(4, 8)
+    assert need > 0 and need % 256 == 0 and L.amq_layer_norm_backward_workspace_bytes(0, 8) == 0
+    args = dict(dy=P, ld_dy=8, x=P, ld_x=8, rows=4, n=8, type=F32, weight=P, param_type=F32, mean=P, rstd=P, dx=P, ld_dx=8, dweight=P, dbias=P,
+                ws=P, bytes=need, stream=None)
+    for bad in (dict(dy=NULL), dict(x=NULL), dict(mean=NULL), dict(rstd=NULL), dict(dx=NULL), dict(ld_dy=7), dict(ld_dx=7), dict(type=-1),
+                dict(ws=NULL), dict(bytes=need - 1), dict(ws=C.c_void_p(0x10010)), dict(rows=-1), dict(dweight=ODD)):
+        assert call(L.amq_layer_norm_backward, args, **bad) == INVALID, bad
+
+
+def test_linear(L):
+    need = L.amq_linear_workspace_bytes(20, 8, 6, F32)
+    assert need > 0 and need % 256 == 0 and L.amq_linear_workspace_bytes(3, 8, 6, F32) == 0 and L.amq_linear_workspace_bytes(0, 8, 6, F32) == 0
+    args = dict(x=P, ld_x=8, W=P, ld_w=8, rows=20, k=8, n=6, type=F32, bias=P, act=0, residual=P, ld_r=6, y=P, ld_y=6, pre=P, ld_pre=6, ws=P,
+                bytes=need, stream=None)
+    for bad in (dict(x=NULL), dict(W=NULL), dict(y=NULL), dict(ld_x=7), dict(ld_w=7), dict(ld_r=5), dict(ld_y=5), dict(ld_pre=5), dict(rows=0),
+                dict(k=0), dict(n=-1), dict(type=3), dict(act=6), dict(act=-1), dict(ws=NULL), dict(bytes=need - 1), dict(x=ODD), dict(bias=ODD)):
+        assert call(L.amq_linear, args, **bad) == INVALID, bad
+    assert call(L.amq_linear, args, k=1 << 21, ld_x=1 << 21, ld_w=1 << 21) == UNSUPPORTED
+    assert call(L.amq_linear, args, ld_x=1 << 23) == UNSUPPORTED
+    need = L.amq_linear_backward_workspace_bytes(20, 8, 6, BF16)
+    args = dict(dy=P, ld_dy=6, x=P, ld_x=8, W=P, ld_w=8, pre=P, ld_pre=6, rows=20, k=8, n=6, type=BF16, act=1, dx=P, ld_dx=8, dW=P, ld_dw=8, dbias=P,
+                ws=P, bytes=need, stream=None)
+    for bad in (dict(dy=NULL), dict(x=NULL), dict(W=NULL), dict(pre=NULL), dict(dx=NULL, dW=NULL, dbias=NULL), dict(ld_dy=5), dict(ld_dx=7),
+                dict(ld_dw=7), dict(ld_pre=5), dict(act=7), dict(ws=NULL), dict(bytes=need - 1), dict(dy=ODD)):
+        assert call(L.amq_linear_backward, args, **bad) == INVALID, bad
+    assert call(L.amq_linear_backward, args, rows=1 << 23) == UNSUPPORTED
+
+
+def test_orthogonalize(L):
+    need = L.amq_orthogonalize_workspace_bytes(2, 8, 6, F32)
+    assert need > 0 and need % 256 == 0 and L.amq_orthogonalize_workspace_bytes(0, 8, 6, F32) == 0
+    coef = (C.c_float * 3)(3.4445, -4.775, 2.0315)
+    args = dict(G=P, batch=2, stride=0, rows=8, cols=6, ld=6, type=F32, steps=5, coef=coef, eps=C.c_float(1e-7), out=P, stride_out=0, ld_out=6, ws=P,
+                bytes=need, stream=None)
+    for bad in (dict(G=NULL), dict(out=NULL), dict(coef=None), dict(batch=0), dict(rows=0), dict(cols=0), dict(ld=5), dict(ld_out=5), dict(type=5),
+                dict(steps=-1), dict(eps=C.c_float(-1)), dict(stride_out=10), dict(stride=-1), dict(ws=NULL), dict(bytes=need - 1), dict(G=ODD)):
+        assert call(L.amq_orthogonalize, args, **bad) == INVALID, bad
+    assert call(L.amq_orthogonalize, args, batch=1 << 17) == UNSUPPORTED
+    assert call(L.amq_orthogonalize, args, rows=(1 << 20) + 1) == UNSUPPORTED

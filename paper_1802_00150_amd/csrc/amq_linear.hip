@@ -178,11 +178,11 @@ struct Source {
     }
   }
 };
-// One operand in the layout of the product kernel: rows of kp values (a multiple of 64), two planes for float.
+// One operand in the layout of the product kernel: rows of kp values (a multiple of 64), in two halves for float.
 struct Laid {
   uint16_t* p;
   int* exps;      // scale per row of the operand, or null: values as they are
-  int64_t plane;  // elements between the planes
+  int64_t ld;     // 16-bit values per row
   int rows, kp;
 };
 template <typename T>
@@ -217,9 +217,9 @@ __device__ __forceinline__ void put8(const Laid& to, int row, int at, float (&v)
     if constexpr (kFloat) split(v[i], hi.v[i], lo.v[i]);
     else hi.v[i] = __builtin_bit_cast(uint16_t, (T)v[i]);
   }
-  uint16_t* q = to.p + (int64_t)row * to.kp + at;
+  uint16_t* q = to.p + row * to.ld + (kFloat ? high_part(at) : at);
   *reinterpret_cast<uint4*>(q) = __builtin_bit_cast(uint4, hi);
-  if constexpr (kFloat) *reinterpret_cast<uint4*>(q + to.plane) = __builtin_bit_cast(uint4, lo);
+  if constexpr (kFloat) *reinterpret_cast<uint4*>(q + 32) = __builtin_bit_cast(uint4, lo);
 }
 
 // Operand rows = matrix rows: one wave per row (16 rows per workgroup).
@@ -351,17 +351,16 @@ struct Carve {
     return p;
   }
 };
+int planes_of(int type) { return type == AMQ_F32 ? 2 : 1; }
 Laid lay_room(Carve& w, int64_t rows, int64_t k, int type, bool scaled) {
   Laid l;
   l.rows = (int)rows;
   l.kp = (int)pad64(k);
-  l.plane = rows * l.kp;
-  l.p = (uint16_t*)w.take((type == AMQ_F32 ? 4 : 2) * (size_t)l.plane);
+  l.ld = planes_of(type) * (int64_t)l.kp;
+  l.p = (uint16_t*)w.take(2 * (size_t)(rows * l.ld));
   l.exps = scaled ? (int*)w.take(sizeof(int) * (size_t)rows) : nullptr;
   return l;
 }
-int planes_of(int type) { return type == AMQ_F32 ? 2 : 1; }
-
 struct ForwardRoom {
   Laid x, W;
   float* part;
@@ -431,7 +430,7 @@ hipError_t run_jobs(const Jobs<T>& jobs, hipStream_t s) {
   lay_kernel<T><<<dim3((unsigned)jobs.first[jobs.count]), dim3(256), 0, s>>>(jobs);
   return hipGetLastError();
 }
-MatmulOperand operand(const Laid& l) { return {l.p, l.kp, l.plane, 0, l.rows}; }
+MatmulOperand operand(const Laid& l) { return {l.p, l.ld, 0, l.rows}; }
 
 template <typename T>
 hipError_t product(const MatmulOperand& r, const MatmulOperand& c, int64_t k, const LinearStore<T>& out, float* part, hipStream_t s) {
@@ -464,17 +463,16 @@ ProductPlan plan_product(int64_t M, int64_t N, int64_t k, int planes, int64_t ba
     const int64_t a = div_up(M, t), b = div_up(N, t);
     return batch * (lower ? a * (a + 1) / 2 : a * b);
   };
-  const int bk = planes == 1 ? 64 : 32;
   ProductPlan p{};
   p.splits = 1;
-  p.tile = tiles(256) >= 192 ? 256 : tiles(128) >= 192 ? 128 : 64;
-  const int64_t steps = k / bk;
+  p.tile = planes == 1 && tiles(256) >= 192 ? 256 : tiles(128) >= 192 ? 128 : 64;
+  const int64_t steps = k / stage_of(planes);
   p.tiles_per_split = (int)steps;
   if (p.tile == 64 && tiles(64) < 256) {
     int64_t splits = 512 / tiles(64);
     if (splits > steps / 4) splits = steps / 4;
     if (splits > 1) {
-      p.tiles_per_split = (int)div_up(steps, splits);
+      p.tiles_per_split = (int)div_up(steps, 2 * splits) * 2;
       p.splits = (int)div_up(steps, p.tiles_per_split);
       if (p.splits > 1) p.part_bytes = sizeof(float) * (size_t)batch * p.splits * M * ((N + 3) & ~int64_t(3));
     }
@@ -491,7 +489,7 @@ hipError_t launch_linear(const LinearArgs& a, hipStream_t s) {
     if (a.rows <= kFewRows) return linear_few(a, out, s);
     const ForwardRoom room = forward_room(a.ws, a.rows, a.k, a.n, a.type);
     Jobs<T> jobs{};
-    MatmulOperand x{a.x, a.ld_x, 0, 0, a.rows}, W{a.W, a.ld_w, 0, 0, a.n};
+    MatmulOperand x{a.x, a.ld_x, 0, a.rows}, W{a.W, a.ld_w, 0, a.n};
     if (!in_place<T>(a.x, a.ld_x, a.k)) {
       add_job(jobs, Source<T>{(const T*)a.x, a.ld_x, nullptr, 0, a.rows, a.k, 0}, room.x, false);
       x = operand(room.x);
@@ -542,7 +540,7 @@ hipError_t launch_linear_grad(const LinearGradArgs& a, hipStream_t s) {
       if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     Jobs<T> jobs{};
-    MatmulOperand rows_of_d{a.dy, a.ld_dy, 0, 0, a.rows};
+    MatmulOperand rows_of_d{a.dy, a.ld_dy, 0, a.rows};
     if (a.dx) {
       if (sloped || !in_place<T>(a.dy, a.ld_dy, a.n)) {
         add_job(jobs, d, room.d, false);

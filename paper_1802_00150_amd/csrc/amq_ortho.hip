@@ -26,27 +26,28 @@ struct __attribute__((packed, aligned(8))) Half4 {
   f16 v[4];
 };
 
-// A matrix of scaled values in NP planes, [batch][rows][ld], ld a multiple of 64; zeros from `cols` to ld.
+// A matrix of scaled values of one or two halves, [batch][rows][ld]; zeros from `cols` to `padded`, a multiple of 64.
 template <int NP>
 struct Planes {
   f16* p;
-  int64_t ld, plane, batch;
-  int rows, cols;
+  int64_t ld, batch;
+  int rows, cols, padded;
+  __device__ __forceinline__ f16* at(int z, int row, int col) const { return p + z * batch + row * ld + (NP == 2 ? high_part(col) : col); }
   // four values along a row (col a multiple of 4)
   __device__ __forceinline__ f32x4 load(int z, int row, int col) const {
-    const f16* q = p + z * batch + row * ld + col;
+    const f16* q = at(z, row, col);
     const Half4 h = *reinterpret_cast<const Half4*>(q);
     f32x4 v = {(float)h.v[0], (float)h.v[1], (float)h.v[2], (float)h.v[3]};
     if constexpr (NP == 2) {
-      const Half4 l = *reinterpret_cast<const Half4*>(q + plane);
+      const Half4 l = *reinterpret_cast<const Half4*>(q + 32);
 #pragma unroll
       for (int i = 0; i < 4; ++i) v[i] += (float)l.v[i];
     }
     return v;
   }
-  __device__ __forceinline__ bool has(int row, int col) const { return row < rows && col < ld; }
+  __device__ __forceinline__ bool has(int row, int col) const { return row < rows && col < padded; }
   __device__ __forceinline__ void store(int z, int row, int col, f32x4 v) const {
-    f16* q = p + z * batch + row * ld + col;
+    f16* q = at(z, row, col);
     Half4 h, l;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -55,7 +56,7 @@ struct Planes {
       l.v[i] = (f16)(s - (float)h.v[i]);
     }
     *reinterpret_cast<Half4*>(q) = h;
-    if constexpr (NP == 2) *reinterpret_cast<Half4*>(q + plane) = l;
+    if constexpr (NP == 2) *reinterpret_cast<Half4*>(q + 32) = l;
   }
 };
 
@@ -246,7 +247,9 @@ hipError_t run(const OrthoArgs& o, hipStream_t s) {
   const bool tall = o.rows > o.cols;
   const Gradient<T> G{(const T*)o.G, o.ld_g, o.stride_g, o.rows, o.cols};
   T* out = (T*)o.out;
-  auto planes = [&](f16* p, int64_t rows, int64_t ld, int64_t cols) { return Planes<NP>{p, ld, o.batch * rows * ld, rows * ld, (int)rows, (int)cols}; };
+  auto planes = [&](f16* p, int64_t rows, int64_t padded, int64_t cols) {
+    return Planes<NP>{p, NP * padded, rows * NP * padded, (int)rows, (int)cols, (int)padded};
+  };
   const Planes<NP> X = planes(r.X, r.n, r.mp, r.m), A = planes(r.A, r.n, r.np, r.n), B = planes(r.B, r.n, r.np, r.n);
   const Planes<NP> Xt[2] = {planes(r.Xt[0], r.m, r.np, r.n), planes(r.Xt[1], r.m, r.np, r.n)};
 
@@ -266,8 +269,8 @@ hipError_t run(const OrthoArgs& o, hipStream_t s) {
 
   auto args = [&](const Planes<NP>& rows, const Planes<NP>& cols, int64_t k, bool lower) {
     MatmulArgs g{};
-    g.r = {rows.p, rows.ld, rows.plane, rows.batch, rows.rows};
-    g.c = {cols.p, cols.ld, cols.plane, cols.batch, cols.rows};
+    g.r = {rows.p, rows.ld, rows.batch, rows.rows};
+    g.c = {cols.p, cols.ld, cols.batch, cols.rows};
     g.M = rows.rows;
     g.N = cols.rows;
     g.tiles_k = (int)k;

@@ -1,13 +1,14 @@
 // Linear layers: y = act(x W^T + b) + residual, and the backward pass dx = d W, dW = d^T x, db = sum_rows d with
 // d = dy act'(z).
 //
-// The products run on the 16-bit matrix cores (amq_matmul_body.h).  bfloat16 and half operands whose rows lie on 16 bytes
-// and hold a multiple of 64 values are read where they are.  Anything else is laid out first: rows padded with zeros;
-// transposed where the contraction runs along columns (W in dx, d and x in dW); float values scaled by a power of two
-// per row of the operand and split into two halves, 22 bits together.  (A binary32 matrix instruction has 1/16 of the rate
-// of a half one; three half products of split operands have 1/3, with the error of binary32 products.)  The scale puts the
-// row's largest value into [2^14, 2^15), so no product overflows, and half's smallest step is 2^-38 of that value.  d in
-// half is scaled the same way before it is rounded: gradients divided by a batch's size lie where half has few digits.
+// The products run on the 16-bit matrix cores (amq_matmul_body.h), which take an operand's k along rows or down columns: W in
+// dx, d and x in dW are never transposed.  bfloat16 and half operands whose rows lie on 16 bytes and hold a multiple of 8
+// values are read where they are.  Anything else is laid out first: rows padded with zeros, d multiplied out, and
+// float values scaled by a power of two per row of the operand and split into two halves, 22 bits together.  (A binary32 matrix
+// instruction has 1/16 of the rate of a half one; three half products of split operands have 1/3, with the error of
+// binary32 products.)  The scale puts the row's largest value into [2^14, 2^15), so no product overflows, and half's smallest
+// step is 2^-38 of that value.  d in half is scaled too before it is rounded, by one power of two: gradients divided by a
+// batch's size lie where half has few digits.
 //
 // A few rows (a token's vector) are multiplied on the vector units: there W is read once, and nothing else matters.
 #include "../../include/amq.h"
@@ -61,7 +62,7 @@ struct LinearStore {
   static constexpr bool kTransposed = false;
   T *y, *pre;
   const T *bias, *residual;
-  const int *exp_r, *exp_c;  // scales of the operands' rows, or null
+  const int *exp_r, *exp_c, *exp_all;  // scales of the operands' rows, or of one operand, or null
   int64_t ld_y, ld_pre, ld_r;
   int M, N, act;
 
@@ -101,11 +102,14 @@ struct LinearStore {
     float v[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = v4[i];
-    if (exp_r || exp_c) {
-      const int e = exp_r ? exp_r[m] : 0;
+    if (exp_r) {
+      const int e = exp_r[m];
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        if (n + i < N) v[i] = ldexpf(v[i], -(e + (exp_c ? exp_c[n + i] : 0)));
+        if (n + i < N) v[i] = ldexpf(v[i], -(e + exp_c[n + i]));
+    } else if (exp_all) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = ldexpf(v[i], -*exp_all);
     }
     values<4>(m, n, v);
   }
@@ -178,18 +182,20 @@ struct Source {
     }
   }
 };
-// One operand in the layout of the product kernel: rows of kp values (a multiple of 64), in two halves for float.
+// One matrix in the layout of the product kernel: rows of `padded` values (a multiple of 64, zeros past the end), in two halves
+// for float.
 struct Laid {
   uint16_t* p;
-  int* exps;      // scale per row of the operand, or null: values as they are
-  int64_t ld;     // 16-bit values per row
-  int rows, kp;
+  int* exps;  // scales: per row, per column, or one
+  int64_t ld;
+  int rows, padded;
 };
+enum Scale { kAsIs, kPerRow, kPerColumn, kOne };  // per row: found and left here; the others are read
 template <typename T>
 struct Job {
   Source<T> from;
   Laid to;
-  bool columns;  // the operand's rows are the matrix's columns
+  Scale scale;
 };
 constexpr int kMaxJobs = 4;
 template <typename T>
@@ -200,99 +206,91 @@ struct Jobs {
 };
 
 __device__ __forceinline__ int scale_exponent(float largest) { return largest > 0.0f ? 14 - ilogbf(largest) : 0; }
-__device__ __forceinline__ void split(float v, uint16_t& hi, uint16_t& lo) {
-  const f16 h = (f16)v;
-  const f16 l = (f16)(v - (float)h);
-  hi = __builtin_bit_cast(uint16_t, h);
-  lo = __builtin_bit_cast(uint16_t, l);
-}
-// 8 values of an operand's row as the products take them.
+// 8 values of a row as the products take them.
 template <typename T>
-__device__ __forceinline__ void put8(const Laid& to, int row, int at, float (&v)[8], int e) {
-  constexpr bool kFloat = sizeof(T) == 4;
+__device__ __forceinline__ void put8(const Laid& to, int64_t row, int at, const float (&v)[8]) {
   Group<uint16_t, 8> hi, lo;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    if (to.exps) v[i] = ldexpf(v[i], e);
-    if constexpr (kFloat) split(v[i], hi.v[i], lo.v[i]);
-    else hi.v[i] = __builtin_bit_cast(uint16_t, (T)v[i]);
+    if constexpr (sizeof(T) == 4) {
+      const f16 h = (f16)v[i];
+      hi.v[i] = __builtin_bit_cast(uint16_t, h);
+      lo.v[i] = __builtin_bit_cast(uint16_t, (f16)(v[i] - (float)h));
+    } else {
+      hi.v[i] = __builtin_bit_cast(uint16_t, (T)v[i]);
+    }
   }
-  uint16_t* q = to.p + row * to.ld + (kFloat ? high_part(at) : at);
+  uint16_t* q = to.p + row * to.ld + (sizeof(T) == 4 ? high_part(at) : at);
   *reinterpret_cast<uint4*>(q) = __builtin_bit_cast(uint4, hi);
-  if constexpr (kFloat) *reinterpret_cast<uint4*>(q + 32) = __builtin_bit_cast(uint4, lo);
+  if constexpr (sizeof(T) == 4) *reinterpret_cast<uint4*>(q + 32) = __builtin_bit_cast(uint4, lo);
 }
 
-// Operand rows = matrix rows: one wave per row (16 rows per workgroup).
-template <typename T>
-__device__ __forceinline__ void lay_rows(const Job<T>& j, int block) {
-  for (int r = 0; r < 4; ++r) {
-    const int row = block * 16 + r * 4 + wave_id();
-    if (row >= j.to.rows) return;
-    int e = 0;
-    if (j.to.exps) {
-      float largest = 0.0f;
-      for (int c = lane_id() * 4; c < j.from.cols; c += 256) {
-        float v[4];
-        j.from.template load<4>(row, c, v);
-        largest = fmaxf(largest, fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3]))));
-      }
-#pragma unroll
-      for (int o = 32; o > 0; o >>= 1) largest = fmaxf(largest, __shfl_xor(largest, o, 64));
-      e = scale_exponent(largest);
-      if (lane_id() == 0) j.to.exps[row] = e;
-    }
-    for (int c = lane_id() * 8; c < j.to.kp; c += 512) {
-      float v[8];
-      j.from.template load<8>(row, c, v);  // zeros past the end
-      put8<T>(j.to, row, c, v, e);
-    }
-  }
-}
-
-// Operand rows = matrix columns: 64 x 64 values per workgroup, turned in LDS.
-template <typename T>
-__device__ __forceinline__ void lay_columns(const Job<T>& j, int block, float (*t)[65]) {
-  const int across = (j.from.cols + 63) / 64;
-  const int r0 = block / across * 64, c0 = block % across * 64;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int row = i * 16 + (threadIdx.x >> 4), col = (threadIdx.x & 15) * 4;
-    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (r0 + row < j.from.rows) j.from.template load<4>(r0 + row, c0 + col, v);
-#pragma unroll
-    for (int q = 0; q < 4; ++q) t[row][col + q] = v[q];
-  }
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int col = i * 32 + (threadIdx.x >> 3), row = (threadIdx.x & 7) * 8;
-    if (c0 + col < j.from.cols) {
-      float v[8];
-#pragma unroll
-      for (int q = 0; q < 8; ++q) v[q] = t[row + q][col];
-      put8<T>(j.to, c0 + col, r0 + row, v, j.to.exps ? j.to.exps[c0 + col] : 0);
-    }
-  }
-}
-
+// One wave per row.  Rows of up to 4096 values stay in registers between the search for the scale and the output.
 template <typename T>
 __global__ __launch_bounds__(256) void lay_kernel(Jobs<T> jobs) {
-  __shared__ float t[64][65];
-  int j = 0;
-  while (j + 1 < jobs.count && (int)blockIdx.x >= jobs.first[j + 1]) ++j;
-  const int block = blockIdx.x - jobs.first[j];
-  if (jobs.job[j].columns) lay_columns(jobs.job[j], block, t);
-  else lay_rows(jobs.job[j], block);
+  int k = 0;
+  while (k + 1 < jobs.count && (int)blockIdx.x >= jobs.first[k + 1]) ++k;
+  const Job<T>& j = jobs.job[k];
+  const int64_t row = (int64_t)(blockIdx.x - jobs.first[k]) * 4 + wave_id();
+  if (row >= j.to.rows) return;
+  constexpr int kHeld = 8;
+  float held[kHeld][8];
+  const int pieces = (j.to.padded + 511) / 512;
+#pragma unroll
+  for (int p = 0; p < kHeld; ++p)
+    if (p < pieces) j.from.template load<8>(row, p * 512 + lane_id() * 8, held[p]);  // zeros past the end
+  int e = 0;
+  if (j.scale == kPerRow) {
+    float largest = 0.0f;
+#pragma unroll
+    for (int p = 0; p < kHeld; ++p)
+      if (p < pieces)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) largest = fmaxf(largest, fabsf(held[p][i]));
+    for (int p = kHeld; p < pieces; ++p) {
+      float v[8];
+      j.from.template load<8>(row, p * 512 + lane_id() * 8, v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) largest = fmaxf(largest, fabsf(v[i]));
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) largest = fmaxf(largest, __shfl_xor(largest, o, 64));
+    e = scale_exponent(largest);
+    if (lane_id() == 0) j.to.exps[row] = e;
+  } else if (j.scale == kOne) {
+    e = *j.to.exps;
+  }
+  auto put = [&](int p, float (&v)[8]) __attribute__((always_inline)) {
+    const int at = p * 512 + lane_id() * 8;
+    if (at >= j.to.padded) return;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (j.scale == kPerColumn) v[i] = at + i < j.from.cols ? ldexpf(v[i], j.to.exps[at + i]) : 0.0f;
+      else if (j.scale != kAsIs) v[i] = ldexpf(v[i], e);
+    }
+    put8<T>(j.to, row, at, v);
+  };
+#pragma unroll
+  for (int p = 0; p < kHeld; ++p)
+    if (p < pieces) put(p, held[p]);
+  for (int p = kHeld; p < pieces; ++p) {
+    float v[8];
+    j.from.template load<8>(row, p * 512 + lane_id() * 8, v);
+    put(p, v);
+  }
 }
 
-// ---- sums and largest values of columns: partial ones over every gridDim.y-th row, then over those
-constexpr int kMaxColumnParts = 64;
+// ---- columns: sums and largest values, and on the way d itself where it needs no scale.  A workgroup takes 32 groups of V
+// columns and every 8 * gridDim.y-th row of them; what it finds are partial results, which a second launch puts together.
+constexpr int kColumnParts = 64;
 template <typename T>
 struct ColumnJob {
   Source<T> from;
   float *sums, *largest;  // [gridDim.y][cols], or null
-  void* total;            // T [cols]: the sums
-  int* exps;              // [cols]: scales
+  Laid to;                // p null: not wanted
+  T* total;               // [cols]: the sums, or null
+  int* exps;              // scales per column, or one, or null
+  bool one;
 };
 template <typename T>
 struct ColumnJobs {
@@ -300,30 +298,70 @@ struct ColumnJobs {
 };
 template <typename T>
 __global__ __launch_bounds__(256) void columns_kernel(ColumnJobs<T> jobs) {
+  constexpr int V = kPer16<T>;
+  __shared__ float part[2][8][32 * V + 4];
   const ColumnJob<T>& j = jobs.job[blockIdx.z];
-  const int c = blockIdx.x * 256 + threadIdx.x;
-  if (c >= j.from.cols) return;
-  float s = 0.0f, largest = 0.0f;
+  const int lane = threadIdx.x & 31, group = threadIdx.x >> 5, c = (blockIdx.x * 32 + lane) * V;
+  const int width = j.to.p ? j.to.padded : j.from.cols;
+  if ((int)blockIdx.x * 32 * V >= width) return;
+  float s[V], largest[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) s[i] = largest[i] = 0.0f;
+  if (c < width)
 #pragma unroll 4
-  for (int64_t row = blockIdx.y; row < j.from.rows; row += gridDim.y) {
-    float v = (float)j.from.p[row * j.from.ld + c];
-    if (j.from.pre) v *= slope((float)j.from.pre[row * j.from.ld_pre + c], j.from.act);
-    s += v;
-    largest = fmaxf(largest, fabsf(v));
+    for (int64_t row = blockIdx.y * 8 + group; row < j.from.rows; row += 8 * gridDim.y) {
+      float v[V];
+      j.from.template load<V>(row, c, v);
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        s[i] += v[i];
+        largest[i] = fmaxf(largest[i], fabsf(v[i]));
+      }
+      if constexpr (V == 8)
+        if (j.to.p) put8<T>(j.to, row, c, v);
+    }
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    part[0][group][lane * V + i] = s[i];
+    part[1][group][lane * V + i] = largest[i];
   }
-  if (j.sums) j.sums[(int64_t)blockIdx.y * j.from.cols + c] = s;
-  if (j.largest) j.largest[(int64_t)blockIdx.y * j.from.cols + c] = largest;
+  __syncthreads();
+  for (int i = threadIdx.x; i < 32 * V; i += 256) {
+    const int at = blockIdx.x * 32 * V + i;
+    if (at >= j.from.cols) continue;
+    float sum = 0.0f, top = 0.0f;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      sum += part[0][q][i];
+      top = fmaxf(top, part[1][q][i]);
+    }
+    if (j.sums) j.sums[(int64_t)blockIdx.y * j.from.cols + at] = sum;
+    if (j.largest) j.largest[(int64_t)blockIdx.y * j.from.cols + at] = top;
+  }
 }
+// 32 columns per workgroup; for one scale of all columns a last workgroup goes through all partial results.
 template <typename T>
 __global__ __launch_bounds__(256) void columns_sum_kernel(ColumnJobs<T> jobs, int parts) {
   const ColumnJob<T>& j = jobs.job[blockIdx.y];
   __shared__ float sums[8][33], tops[8][33];
-  const int lane = threadIdx.x & 31, group = threadIdx.x >> 5, c = blockIdx.x * 32 + lane, cols = j.from.cols;
-  if (blockIdx.x * 32 >= (unsigned)cols) return;
+  const int lane = threadIdx.x & 31, group = threadIdx.x >> 5, cols = j.from.cols;
+  if (blockIdx.x + 1 == gridDim.x) {
+    if (!j.one) return;
+    float top = 0.0f;
+    for (int64_t i = threadIdx.x; i < (int64_t)parts * cols; i += 256) top = fmaxf(top, j.largest[i]);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+    if (lane_id() == 0) tops[0][wave_id()] = top;
+    __syncthreads();
+    if (threadIdx.x == 0) *j.exps = scale_exponent(fmaxf(fmaxf(tops[0][0], tops[0][1]), fmaxf(tops[0][2], tops[0][3])));
+    return;
+  }
+  const int c = blockIdx.x * 32 + lane;
+  if ((int)blockIdx.x * 32 >= cols) return;
   float s = 0.0f, top = 0.0f;
   if (c < cols)
     for (int p = group; p < parts; p += 8) {
-      if (j.sums) s += j.sums[(int64_t)p * cols + c];
+      if (j.total) s += j.sums[(int64_t)p * cols + c];
       if (j.largest) top = fmaxf(top, j.largest[(int64_t)p * cols + c]);
     }
   sums[group][lane] = s;
@@ -336,8 +374,8 @@ __global__ __launch_bounds__(256) void columns_sum_kernel(ColumnJobs<T> jobs, in
     s += sums[g][lane];
     top = fmaxf(top, tops[g][lane]);
   }
-  if (j.total) ((T*)j.total)[c] = (T)s;
-  if (j.exps) j.exps[c] = scale_exponent(top);
+  if (j.total) j.total[c] = (T)s;
+  if (j.exps && !j.one) j.exps[c] = scale_exponent(top);
 }
 
 // ---- workspaces
@@ -352,15 +390,16 @@ struct Carve {
   }
 };
 int planes_of(int type) { return type == AMQ_F32 ? 2 : 1; }
-Laid lay_room(Carve& w, int64_t rows, int64_t k, int type, bool scaled) {
+Laid lay_room(Carve& w, int64_t rows, int64_t cols, int type, int64_t scales) {
   Laid l;
   l.rows = (int)rows;
-  l.kp = (int)pad64(k);
-  l.ld = planes_of(type) * (int64_t)l.kp;
+  l.padded = (int)pad64(cols);
+  l.ld = planes_of(type) * (int64_t)l.padded;
   l.p = (uint16_t*)w.take(2 * (size_t)(rows * l.ld));
-  l.exps = scaled ? (int*)w.take(sizeof(int) * (size_t)rows) : nullptr;
+  l.exps = scales ? (int*)w.take(sizeof(int) * (size_t)scales) : nullptr;
   return l;
 }
+
 struct ForwardRoom {
   Laid x, W;
   float* part;
@@ -370,38 +409,35 @@ ForwardRoom forward_room(void* ws, int64_t rows, int64_t k, int64_t n, int type)
   Carve w(ws);
   ForwardRoom r{};
   if (rows > kFewRows) {
-    r.x = lay_room(w, rows, k, type, type == AMQ_F32);
-    r.W = lay_room(w, n, k, type, type == AMQ_F32);
-    r.part = (float*)w.take(plan_product(rows, n, pad64(k), planes_of(type), 1, false).part_bytes);
+    const bool scaled = type == AMQ_F32;
+    r.x = lay_room(w, rows, k, type, scaled ? rows : 0);
+    r.W = lay_room(w, n, k, type, scaled ? n : 0);
+    r.part = (float*)w.take(plan_product(rows, n, k, planes_of(type), 1, false).part_bytes);
   }
   r.total = w.off;
   return r;
 }
 
 struct BackwardRoom {
-  Laid d, d_cols, W_cols, x_cols;
+  Laid d, d_columns, x, W;  // d for dx and (float: scaled otherwise) for dW
   float *sums, *tops[3];
   float* part;
-  int column_parts;
   size_t total;
 };
 BackwardRoom backward_room(void* ws, int64_t rows, int64_t k, int64_t n, int type) {
   Carve w(ws);
   BackwardRoom r{};
-  r.d = lay_room(w, rows, n, type, type != AMQ_BF16);
-  r.W_cols = lay_room(w, k, n, type, type == AMQ_F32);
-  r.d_cols = lay_room(w, n, rows, type, type != AMQ_BF16);
-  r.x_cols = lay_room(w, k, rows, type, type == AMQ_F32);
-  const int64_t most = rows > n ? rows : n;  // the longest column: of d and x, of W
-  r.column_parts = (int)(most < kMaxColumnParts ? most : kMaxColumnParts);
-  r.sums = (float*)w.take(sizeof(float) * r.column_parts * (size_t)n);
-  if (type != AMQ_BF16) r.tops[0] = (float*)w.take(sizeof(float) * r.column_parts * (size_t)n);
-  if (type == AMQ_F32) {
-    r.tops[1] = (float*)w.take(sizeof(float) * r.column_parts * (size_t)k);
-    r.tops[2] = (float*)w.take(sizeof(float) * r.column_parts * (size_t)k);
-  }
-  const size_t a = plan_product(rows, k, pad64(n), planes_of(type), 1, false).part_bytes;
-  const size_t b = plan_product(n, k, pad64(rows), planes_of(type), 1, false).part_bytes;
+  const bool wide = type == AMQ_F32;
+  r.d = lay_room(w, rows, n, type, wide ? rows : type == AMQ_F16 ? 1 : 0);
+  r.d_columns = wide ? lay_room(w, rows, n, type, n) : r.d;
+  r.x = lay_room(w, rows, k, type, wide ? k : 0);
+  r.W = lay_room(w, n, k, type, wide ? k : 0);
+  r.sums = (float*)w.take(sizeof(float) * kColumnParts * (size_t)n);
+  if (type != AMQ_BF16) r.tops[0] = (float*)w.take(sizeof(float) * kColumnParts * (size_t)n);
+  if (wide)
+    for (int i = 1; i < 3; ++i) r.tops[i] = (float*)w.take(sizeof(float) * kColumnParts * (size_t)k);
+  const size_t a = plan_product(rows, k, n, planes_of(type), 1, false).part_bytes;
+  const size_t b = plan_product(n, k, rows, planes_of(type), 1, false).part_bytes;
   r.part = (float*)w.take(a > b ? a : b);
   r.total = w.off;
   return r;
@@ -414,14 +450,13 @@ hipError_t with_type(int type, F f) {
 
 // Whether the product kernel can read a matrix where it is.
 template <typename T>
-bool in_place(const void* p, int64_t ld, int64_t k) {
-  return sizeof(T) == 2 && k % 64 == 0 && ld % 8 == 0 && (reinterpret_cast<uintptr_t>(p) & 15) == 0;
+bool in_place(const Source<T>& m) {
+  return sizeof(T) == 2 && !m.pre && m.cols % 8 == 0 && m.ld % 8 == 0 && (reinterpret_cast<uintptr_t>(m.p) & 15) == 0;
 }
 template <typename T>
-void add_job(Jobs<T>& jobs, const Source<T>& from, const Laid& to, bool columns) {
-  const int64_t blocks = columns ? pad64(from.rows) / 64 * div_up(from.cols, 64) : div_up(from.rows, 16);
-  jobs.job[jobs.count] = {from, to, columns};
-  jobs.first[jobs.count + 1] = jobs.first[jobs.count] + (int)blocks;
+void add_job(Jobs<T>& jobs, const Source<T>& from, const Laid& to, Scale scale) {
+  jobs.job[jobs.count] = {from, to, scale};
+  jobs.first[jobs.count + 1] = jobs.first[jobs.count] + (int)div_up(from.rows, 4);
   ++jobs.count;
 }
 template <typename T>
@@ -430,19 +465,25 @@ hipError_t run_jobs(const Jobs<T>& jobs, hipStream_t s) {
   lay_kernel<T><<<dim3((unsigned)jobs.first[jobs.count]), dim3(256), 0, s>>>(jobs);
   return hipGetLastError();
 }
-MatmulOperand operand(const Laid& l) { return {l.p, l.ld, 0, l.rows}; }
 
+// A matrix as an operand: its rows, or (`columns`) its columns.
 template <typename T>
+MatmulOperand operand(const Source<T>& m, bool columns) {
+  return {m.p, m.ld, 0, columns ? m.cols : m.rows};
+}
+MatmulOperand operand(const Laid& l, bool columns) { return {l.p, l.ld, 0, columns ? l.padded : l.rows}; }
+
+template <typename T, bool RC, bool CC>
 hipError_t product(const MatmulOperand& r, const MatmulOperand& c, int64_t k, const LinearStore<T>& out, float* part, hipStream_t s) {
   MatmulArgs g{};
   g.r = r;
   g.c = c;
   g.M = out.M;
   g.N = out.N;
-  g.tiles_k = (int)pad64(k);
-  const ProductPlan p = plan_product(out.M, out.N, pad64(k), sizeof(T) == 4 ? 2 : 1, 1, false);
-  if constexpr (sizeof(T) == 4) return launch_product<f16, 2>(g, p, 1, out, part, s);
-  else return launch_product<T, 1>(g, p, 1, out, part, s);
+  g.k = (int)k;
+  const ProductPlan p = plan_product(out.M, out.N, k, sizeof(T) == 4 ? 2 : 1, 1, false);
+  if constexpr (sizeof(T) == 4) return launch_product<f16, 2, RC, CC>(g, p, 1, out, part, s);
+  else return launch_product<T, 1, RC, CC>(g, p, 1, out, part, s);
 }
 
 template <typename T>
@@ -466,7 +507,7 @@ ProductPlan plan_product(int64_t M, int64_t N, int64_t k, int planes, int64_t ba
   ProductPlan p{};
   p.splits = 1;
   p.tile = planes == 1 && tiles(256) >= 192 ? 256 : tiles(128) >= 192 ? 128 : 64;
-  const int64_t steps = k / stage_of(planes);
+  const int64_t steps = div_up(k, stage_of(planes));
   p.tiles_per_split = (int)steps;
   if (p.tile == 64 && tiles(64) < 256) {
     int64_t splits = 512 / tiles(64);
@@ -485,26 +526,22 @@ size_t linear_workspace(int64_t rows, int64_t k, int64_t n, int type) { return f
 hipError_t launch_linear(const LinearArgs& a, hipStream_t s) {
   return with_type(a.type, [&](auto t) {
     using T = decltype(t);
-    LinearStore<T> out{(T*)a.y, (T*)a.pre, (const T*)a.bias, (const T*)a.residual, nullptr, nullptr, a.ld_y, a.ld_pre, a.ld_r, a.rows, a.n, a.act};
+    LinearStore<T> out{(T*)a.y, (T*)a.pre, (const T*)a.bias, (const T*)a.residual, nullptr, nullptr, nullptr, a.ld_y, a.ld_pre, a.ld_r, a.rows, a.n, a.act};
     if (a.rows <= kFewRows) return linear_few(a, out, s);
     const ForwardRoom room = forward_room(a.ws, a.rows, a.k, a.n, a.type);
+    const Source<T> x{(const T*)a.x, a.ld_x, nullptr, 0, a.rows, a.k, 0}, W{(const T*)a.W, a.ld_w, nullptr, 0, a.n, a.k, 0};
     Jobs<T> jobs{};
-    MatmulOperand x{a.x, a.ld_x, 0, a.rows}, W{a.W, a.ld_w, 0, a.n};
-    if (!in_place<T>(a.x, a.ld_x, a.k)) {
-      add_job(jobs, Source<T>{(const T*)a.x, a.ld_x, nullptr, 0, a.rows, a.k, 0}, room.x, false);
-      x = operand(room.x);
-    }
-    if (!in_place<T>(a.W, a.ld_w, a.k)) {
-      add_job(jobs, Source<T>{(const T*)a.W, a.ld_w, nullptr, 0, a.n, a.k, 0}, room.W, false);
-      W = operand(room.W);
-    }
+    const Scale scale = sizeof(T) == 4 ? kPerRow : kAsIs;
+    if (!in_place(x)) add_job(jobs, x, room.x, scale);
+    if (!in_place(W)) add_job(jobs, W, room.W, scale);
     const hipError_t e = run_jobs(jobs, s);
     if (e != hipSuccess) return e;
     if (sizeof(T) == 4) {
       out.exp_r = room.x.exps;
       out.exp_c = room.W.exps;
     }
-    return product(x, W, a.k, out, room.part, s);
+    return product<T, false, false>(in_place(x) ? operand(x, false) : operand(room.x, false), in_place(W) ? operand(W, false) : operand(room.W, false), a.k,
+                                    out, room.part, s);
   });
 }
 
@@ -514,64 +551,69 @@ hipError_t launch_linear_grad(const LinearGradArgs& a, hipStream_t s) {
   return with_type(a.type, [&](auto t) {
     using T = decltype(t);
     constexpr bool kFloat = sizeof(T) == 4;
-    BackwardRoom room = backward_room(a.ws, a.rows, a.k, a.n, a.type);
+    const BackwardRoom room = backward_room(a.ws, a.rows, a.k, a.n, a.type);
     const bool sloped = a.act != AMQ_ACT_NONE;
-    const bool scaled = kFloat || (a.type == AMQ_F16 && sloped);  // d, before it is rounded
-    if (!scaled) room.d.exps = room.d_cols.exps = nullptr;
     const Source<T> d{(const T*)a.dy, a.ld_dy, sloped ? (const T*)a.pre : nullptr, a.ld_pre, a.rows, a.n, a.act};
     const Source<T> x{(const T*)a.x, a.ld_x, nullptr, 0, a.rows, a.k, 0}, W{(const T*)a.W, a.ld_w, nullptr, 0, a.n, a.k, 0};
+    const bool scaled = kFloat || (a.type == AMQ_F16 && sloped);  // d, before it is rounded
+    const bool products = a.dx || a.dW, d_laid = products && !in_place(d);
     hipError_t e = hipSuccess;
-    // sums of d's columns, and the scales of operands whose rows are columns
+    // what goes by columns: sums of d; scales of float operands whose k runs down them, and of d in half; d itself without any
     ColumnJobs<T> columns{};
     int count = 0, widest = 0;
-    auto column_job = [&](const Source<T>& from, float* sums, float* tops, void* total, int* exps) {
-      columns.job[count++] = {from, sums, tops, total, exps};
-      widest = from.cols > widest ? from.cols : widest;
+    auto column_job = [&](const ColumnJob<T>& job) {
+      columns.job[count++] = job;
+      const int width = job.to.p ? job.to.padded : job.from.cols;
+      widest = width > widest ? width : widest;
     };
-    const bool scaled_columns = scaled && a.dW;
-    if (a.dbias || scaled_columns)
-      column_job(d, a.dbias ? room.sums : nullptr, scaled_columns ? room.tops[0] : nullptr, a.dbias, scaled_columns ? room.d_cols.exps : nullptr);
-    if (kFloat && a.dW) column_job(x, nullptr, room.tops[1], nullptr, room.x_cols.exps);
-    if (kFloat && a.dx) column_job(W, nullptr, room.tops[2], nullptr, room.W_cols.exps);
+    const bool d_scales = kFloat ? a.dW != nullptr : scaled && products, d_here = d_laid && !scaled;
+    if (a.dbias || d_scales || d_here)
+      column_job({d, a.dbias ? room.sums : nullptr, d_scales ? room.tops[0] : nullptr, d_here ? room.d : Laid{}, (T*)a.dbias,
+                  d_scales ? room.d_columns.exps : nullptr, d_scales && !kFloat});
+    if (kFloat && a.dW) column_job({x, nullptr, room.tops[1], Laid{}, nullptr, room.x.exps, false});
+    if (kFloat && a.dx) column_job({W, nullptr, room.tops[2], Laid{}, nullptr, room.W.exps, false});
     if (count) {
-      columns_kernel<T><<<dim3((unsigned)div_up(widest, 256), (unsigned)room.column_parts, (unsigned)count), dim3(256), 0, s>>>(columns);
+      columns_kernel<T><<<dim3((unsigned)div_up(widest, 32 * kPer16<T>), kColumnParts, (unsigned)count), dim3(256), 0, s>>>(columns);
       if ((e = hipGetLastError()) != hipSuccess) return e;
-      columns_sum_kernel<T><<<dim3((unsigned)div_up(widest, 32), (unsigned)count), dim3(256), 0, s>>>(columns, room.column_parts);
+      columns_sum_kernel<T><<<dim3((unsigned)div_up(widest, 32) + 1, (unsigned)count), dim3(256), 0, s>>>(columns, kColumnParts);
       if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     Jobs<T> jobs{};
-    MatmulOperand rows_of_d{a.dy, a.ld_dy, 0, a.rows};
-    if (a.dx) {
-      if (sloped || !in_place<T>(a.dy, a.ld_dy, a.n)) {
-        add_job(jobs, d, room.d, false);
-        rows_of_d = operand(room.d);
-      }
-      add_job(jobs, W, room.W_cols, true);
+    if (d_laid && scaled) {
+      if (!kFloat) add_job(jobs, d, room.d, kOne);
+      else if (a.dx) add_job(jobs, d, room.d, kPerRow);
+      if (kFloat && a.dW) add_job(jobs, d, room.d_columns, kPerColumn);
     }
-    if (a.dW) {
-      add_job(jobs, d, room.d_cols, true);
-      add_job(jobs, x, room.x_cols, true);
-    }
+    if (a.dx && !in_place(W)) add_job(jobs, W, room.W, kFloat ? kPerColumn : kAsIs);
+    if (a.dW && !in_place(x)) add_job(jobs, x, room.x, kFloat ? kPerColumn : kAsIs);
     if ((e = run_jobs(jobs, s)) != hipSuccess) return e;
     LinearStore<T> out{};
     out.act = AMQ_ACT_NONE;
+    if (!kFloat && scaled) out.exp_all = room.d.exps;
     if (a.dx) {
       out.y = (T*)a.dx;
       out.ld_y = a.ld_dx;
       out.M = a.rows;
       out.N = a.k;
-      out.exp_r = room.d.exps;
-      out.exp_c = room.W_cols.exps;
-      if ((e = product(rows_of_d, operand(room.W_cols), a.n, out, room.part, s)) != hipSuccess) return e;
+      if (kFloat) {
+        out.exp_r = room.d.exps;
+        out.exp_c = room.W.exps;
+      }
+      e = product<T, false, true>(d_laid ? operand(room.d, false) : operand(d, false), in_place(W) ? operand(W, true) : operand(room.W, true), a.n, out,
+                                  room.part, s);
+      if (e != hipSuccess) return e;
     }
     if (a.dW) {
       out.y = (T*)a.dW;
       out.ld_y = a.ld_dw;
       out.M = a.n;
       out.N = a.k;
-      out.exp_r = room.d_cols.exps;
-      out.exp_c = room.x_cols.exps;
-      e = product(operand(room.d_cols), operand(room.x_cols), a.rows, out, room.part, s);
+      if (kFloat) {
+        out.exp_r = room.d_columns.exps;
+        out.exp_c = room.x.exps;
+      }
+      e = product<T, true, true>(d_laid ? operand(room.d_columns, true) : operand(d, true), in_place(x) ? operand(x, true) : operand(room.x, true), a.rows, out,
+                                 room.part, s);
     }
     return e;
   });

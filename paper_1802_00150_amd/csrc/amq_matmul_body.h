@@ -1,11 +1,12 @@
 // Matrix products on the 16-bit matrix cores for the training operators: result[m][n] = sum_k R[m][k] C[n][k], both
 // operands with k running along their rows, fp32 accumulation, and an epilogue object that takes the finished values.
 //
-// An operand is one plane of bfloat16 or half values, or numbers of 22 bits as a high and a low half value: then
-// high*high + high*low + low*high is summed, and what is left out is 2^-22 of a product at most.  Rows are padded with zeros
-// to a multiple of 64 values and begin on 16 bytes; numbers of two halves lie in blocks of 32 high and 32 low parts.  So 128
-// bytes of a row are one stage of the contraction in either case (64 or 32 values), there is no remainder, and every
-// copy to LDS is 16 bytes per lane; rows past the operand's end are read as its last row and their results dropped.
+// An operand is bfloat16 or half values, or numbers of 22 bits as a high and a low half value: then
+// high*high + high*low + low*high is summed, and what is left out is 2^-22 of a product at most.  k runs along an operand's rows
+// in memory or down its columns.  Rows begin on 16 bytes and hold a multiple of 8 values or are padded with zeros to one; numbers of two halves lie in blocks of
+// 32 high and 32 low parts, padded with zeros to a multiple of 64 numbers.  64 steps of k (of numbers of two halves 32) are one
+// stage of the contraction; steps past the end are read as zeros, rows past the operand's end as its last ones, and
+// their results dropped.
 //
 // A workgroup of WR x WC waves owns BM x BN of the result and walks over the stages.  A stage goes from memory to LDS without
 // passing registers (global_load_lds, 16 bytes a lane), into a ring of PLACES stages: up to that many are under way while one is
@@ -25,14 +26,15 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 struct MatmulOperand {
   const void* p;
-  int64_t ld, batch;  // strides in 16-bit values: rows, batch entries
-  int rows;
+  int64_t ld, batch;  // strides in 16-bit values: rows of memory, batch entries
+  int rows;           // of the operand
 };
 // Where value k of a row of numbers of two halves has its high part; the low part follows 32 values on.
 __host__ __device__ inline int64_t high_part(int64_t k) { return (k >> 5) * 64 + (k & 31); }
 struct MatmulArgs {
   MatmulOperand r, c;
   int M, N;              // of the result
+  int k;                 // of the contraction
   int tiles_k;           // stages
   int nbm, nbn;          // tiles of the result
   int tiles_per_split;   // stages for each of gridDim.y
@@ -54,9 +56,7 @@ struct MatmulElement<f16> {
   static __device__ __forceinline__ f32x4 mfma(v8 a, v8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 };
 
-// Position, among the eight 16-byte pieces of a row in LDS, of piece `piece`.  The 64 banks serve 256 bytes a cycle, 16 lanes
-// of an operand read: 16 rows in a row put the same piece on 16 different positions of 256 bytes, two rows to that many.
-__device__ __forceinline__ int piece_at(int row, int piece) { return piece ^ ((row >> 1) & 7); }
+__device__ const uint4 kZeros = {0, 0, 0, 0};
 
 // Tile of the result for workgroup `id` of `count`.  Workgroups are dealt to the 8 dies in turn: each die gets a run of
 // consecutive tiles, in groups of 8 tile rows, so that what its L2 holds of both operands is used again.
@@ -108,17 +108,101 @@ __device__ __forceinline__ void copy_to_lds(const char* base, uint32_t offset, u
   const uint32_t at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint16_t*)to;
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at), "v"(offset), "s"(base));
 }
+// The same from an address per lane.
+__device__ __forceinline__ void copy_to_lds(const char* from, uint16_t* to) {
+  const uint32_t at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint16_t*)to;
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(from));
+}
 
-template <typename E, int NP, int BM, int BN, int WR, int WC, int PLACES, typename Epi>
+// One operand of a workgroup's tile: its copies to LDS, and its fragments for the matrix cores (16 rows, 32 steps of k: eight
+// values per lane, row lane % 16, steps (lane / 16) * 8 on).
+//
+// Rows (k runs along the rows of memory): LDS holds B rows of 128 bytes, one stage of each.
+// Columns (k runs down the columns of memory): LDS holds one stage's rows of memory, B operand rows wide.  A fragment is
+// gathered by two transposing reads: 16 lanes read 4 steps of k of 16 operand rows, and get them turned.  Its 32 lanes a cycle
+// cover 8 steps of k; those are given 8 different 32-byte parts of the 64 banks.
+template <typename E, int NP, int B, int kWaves, bool COLUMNS>
+struct Side {
+  using v8 = typename MatmulElement<E>::v8;
+  typedef short v4s __attribute__((ext_vector_type(4)));
+  static constexpr int kCopies = B / 8 / kWaves;         // of 1 KB that a wave makes per stage
+  static constexpr int kLine = COLUMNS ? B * NP * 2 : 128;  // bytes of a row in LDS
+  static constexpr int kLanes = kLine / 16;              // lanes per row of a copy
+  static constexpr int kSteps = NP == 1 ? 64 : 32;       // of k in a stage
+  static_assert(kCopies * 8 * kWaves == B, "copies");
+
+  const char* base;    // of the tile, uniform
+  int64_t stage;       // bytes from one stage to the next
+  uint32_t off[kCopies];
+  int k, lane, wave;
+
+  static __device__ __forceinline__ int swizzle(int row) {  // of 16-byte pieces
+    if (!COLUMNS) return (row >> 1) & 7;
+    if (kLine == 128) return (((row >> 1) & 1) | ((row >> 2) & 2)) << 1;
+    return ((row & 3) | ((row >> 1) & 4)) << 1;
+  }
+  __device__ __forceinline__ Side(const MatmulOperand& o, int z, int first_row, int k_, int lane_, int wave_) : k(k_), lane(lane_), wave(wave_) {
+    const uint16_t* p = (const uint16_t*)o.p + z * o.batch;
+    if constexpr (COLUMNS) {
+      base = (const char*)(p + (int64_t)first_row * NP);
+      stage = o.ld * kSteps * 2;
+    } else {
+      base = (const char*)(p + first_row * o.ld);
+      stage = 128;
+    }
+#pragma unroll
+    for (int j = 0; j < kCopies; ++j) {
+      const int row = row_of(j), piece = (lane % kLanes) ^ swizzle(row);
+      if constexpr (COLUMNS) {
+        // past the operand's last rows those again (their number is a multiple of 8)
+        const int left = (o.rows - first_row) * NP - 8, at = piece * 8;
+        off[j] = (uint32_t)(row * o.ld + (at < left ? at : left)) * 2u;
+      } else {
+        const int left = o.rows - 1 - first_row;
+        off[j] = (uint32_t)((row < left ? row : left) * o.ld + piece * 8) * 2u;
+      }
+    }
+  }
+  __device__ __forceinline__ int row_of(int j) const { return (wave + j * kWaves) * (64 / kLanes) + lane / kLanes; }
+  // Copy j of stage t.  Steps of k past the end are zeros (along rows: to the next multiple of 8 what lies there).
+  __device__ __forceinline__ void copy(uint16_t* s, int t, int j) const {
+    const char* from = base + t * stage;
+    uint16_t* to = s + (wave + j * kWaves) * 512;
+    if ((NP == 1 || COLUMNS) && (t + 1) * kSteps > k) {
+      const int step = t * kSteps + (COLUMNS ? row_of(j) : ((lane % kLanes) ^ swizzle(row_of(j))) * 8);
+      copy_to_lds(step < k ? from + off[j] : (const char*)&kZeros, to);
+    } else {
+      copy_to_lds(from, off[j], to);
+    }
+  }
+  // Fragment of 16 rows from row0 + 16 i on (row0: of the wave): half `half` of the stage, or of its numbers.
+  __device__ __forceinline__ v8 read(const uint16_t* s, int row0, int i, int half) const {
+    if constexpr (!COLUMNS) {
+      return *reinterpret_cast<const v8*>(s + (row0 + i * 16 + (lane & 15)) * 64 + ((half * 4 + (lane >> 4)) ^ swizzle(lane & 15)) * 8);
+    } else {
+      // bytes of the 32-byte part within a row: row0 takes the high bits, the fragment's number the low ones
+      const int step = (lane >> 4) * 8 + ((lane & 15) >> 2);
+      const int part = NP == 1 ? i : (i >> 1) * 4 + half * 2 + (i & 1);
+      const uint32_t at = ((uint32_t)(step * kLine + ((row0 * NP / 8) ^ swizzle(step)) * 16 + (lane & 3) * 8) ^ (uint32_t)(part * 32)) +
+                          (NP == 1 ? half * 32 * kLine : 0);
+      const auto* q = (__attribute__((address_space(3))) const char*)(__attribute__((address_space(3))) const uint16_t*)s + at;
+      const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)q);
+      const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(q + 4 * kLine));
+      return __builtin_bit_cast(v8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+  }
+};
+
+template <typename E, int NP, bool RC, bool CC, int BM, int BN, int WR, int WC, int PLACES, typename Epi>
 __global__ __launch_bounds__(WR * WC * 64, 2) void matmul_kernel(MatmulArgs g, Epi epi) {
   constexpr int kWaves = WR * WC, TM = BM / WR / 16, TN = BN / WC / 16;
-  constexpr int JR = BM / 8 / kWaves, JC = BN / 8 / kWaves;  // copies of 8 rows that a wave makes per stage
-  constexpr int kStage = (BM + BN) * 64;                     // 16-bit values
+  constexpr int kStage = (BM + BN) * 64;  // 16-bit values
   constexpr int KW = TN * 16, kStride = KW + 4;
-  static_assert(JR >= 1 && JC >= 1 && JR * 8 * kWaves == BM && JC * 8 * kWaves == BN, "copies");
   static_assert(TM % 2 == 0 && kWaves * 32 * kStride * 4 <= PLACES * kStage * 2, "the result's subtiles take the place of the operands");
   using Element = MatmulElement<E>;
   using v8 = typename Element::v8;
+  using R = Side<E, NP, BM, kWaves, RC>;
+  using C = Side<E, NP, BN, kWaves, CC>;
   __shared__ __align__(16) uint16_t lds[PLACES * kStage];
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -128,29 +212,17 @@ __global__ __launch_bounds__(WR * WC * 64, 2) void matmul_kernel(MatmulArgs g, E
   const int z = blockIdx.z;
   const int first = blockIdx.y * g.tiles_per_split;
   const int last = (first + g.tiles_per_split < g.tiles_k ? first + g.tiles_per_split : g.tiles_k) - 1;
-
-  const uint16_t* pr = (const uint16_t*)g.r.p + z * g.r.batch + (int64_t)bm * BM * g.r.ld;
-  const uint16_t* pc = (const uint16_t*)g.c.p + z * g.c.batch + (int64_t)bn * BN * g.c.ld;
-  uint32_t off_r[JR], off_c[JC];  // bytes from the tile's first row
-#pragma unroll
-  for (int j = 0; j < JR; ++j) {
-    const int row = (wave + j * kWaves) * 8 + (lane >> 3), left = g.r.rows - 1 - bm * BM;
-    off_r[j] = (uint32_t)((row < left ? row : left) * g.r.ld + piece_at(row, lane & 7) * 8) * 2u;
-  }
-#pragma unroll
-  for (int j = 0; j < JC; ++j) {
-    const int row = (wave + j * kWaves) * 8 + (lane >> 3), left = g.c.rows - 1 - bn * BN;
-    off_c[j] = (uint32_t)((row < left ? row : left) * g.c.ld + piece_at(row, lane & 7) * 8) * 2u;
-  }
+  const R r(g.r, z, bm * BM, g.k, lane, wave);
+  const C c(g.c, z, bn * BN, g.k, lane, wave);
   // copy j of stage t of the contraction to its place in the ring; past the end the last stage again, so that as many copies
   // are under way at every wait
   auto copy = [&](int t, int j) __attribute__((always_inline)) {
     uint16_t* s = lds + (unsigned)(t - first) % PLACES * kStage;
-    const int64_t at = (t < last ? t : last) * 64;
-    if (j < JR) copy_to_lds((const char*)(pr + at), off_r[j], s + (wave + j * kWaves) * 512);
-    else copy_to_lds((const char*)(pc + at), off_c[j - JR], s + BM * 64 + (wave + (j - JR) * kWaves) * 512);
+    const int at = t < last ? t : last;
+    if (j < R::kCopies) r.copy(s, at, j);
+    else c.copy(s + BM * 64, at, j - R::kCopies);
   };
-  constexpr int kCopies = JR + JC, kTiles = TM * TN;
+  constexpr int kCopies = R::kCopies + C::kCopies, kTiles = TM * TN;
   // This wave's reads have returned; of the copies that it issued all but the newest `LEFT` stages' have landed.  After the
   // barrier that holds for the other waves too.
   auto together = [](auto left) __attribute__((always_inline)) {
@@ -167,12 +239,10 @@ __global__ __launch_bounds__(WR * WC * 64, 2) void matmul_kernel(MatmulArgs g, E
     v8 r[TM], c[TN];
   };
   auto read_r = [&](int t, int half, int i) __attribute__((always_inline)) {
-    const uint16_t* s = lds + (unsigned)(t - first) % PLACES * kStage + (wr * (BM / WR) + i * 16) * 64;
-    return *reinterpret_cast<const v8*>(s + (lane & 15) * 64 + piece_at(lane & 15, half * 4 + (lane >> 4)) * 8);
+    return r.read(lds + (unsigned)(t - first) % PLACES * kStage, wr * (BM / WR), i, half);
   };
   auto read_c = [&](int t, int half, int j) __attribute__((always_inline)) {
-    const uint16_t* s = lds + (unsigned)(t - first) % PLACES * kStage + (BM + wc * KW + j * 16) * 64;
-    return *reinterpret_cast<const v8*>(s + (lane & 15) * 64 + piece_at(lane & 15, half * 4 + (lane >> 4)) * 8);
+    return c.read(lds + (unsigned)(t - first) % PLACES * kStage + BM * 64, wc * KW, j, half);
   };
   f32x4 acc[TM][TN];
 #pragma unroll
@@ -318,34 +388,34 @@ struct ProductPlan {
 };
 ProductPlan plan_product(int64_t M, int64_t N, int64_t k, int planes, int64_t batch, bool lower);
 
-template <typename E, int NP, int BM, int BN, int WR, int WC, int PLACES, typename Epi>
+template <typename E, int NP, bool RC, bool CC, int BM, int BN, int WR, int WC, int PLACES, typename Epi>
 hipError_t launch_tiles(MatmulArgs g, const ProductPlan& p, int batch, const Epi& epi, hipStream_t s) {
-  g.tiles_k /= stage_of(NP);  // (comes as k)
+  g.tiles_k = (int)div_up(g.k, stage_of(NP));
   g.tiles_per_split = p.tiles_per_split;
   g.nbm = (int)div_up(g.M, BM);
   g.nbn = (int)div_up(g.N, BN);
   const int64_t tiles = g.lower ? (int64_t)g.nbm * (g.nbm + 1) / 2 : (int64_t)g.nbm * g.nbn;
-  matmul_kernel<E, NP, BM, BN, WR, WC, PLACES, Epi><<<dim3((unsigned)tiles, (unsigned)p.splits, (unsigned)batch), dim3(WR * WC * 64), 0, s>>>(g, epi);
+  matmul_kernel<E, NP, RC, CC, BM, BN, WR, WC, PLACES, Epi><<<dim3((unsigned)tiles, (unsigned)p.splits, (unsigned)batch), dim3(WR * WC * 64), 0, s>>>(g, epi);
   return hipGetLastError();
 }
 
-// The product of g (g.tiles_k holds k, a multiple of 64) with the tiles of `p`.
-template <typename E, int NP, typename Epi>
+// The product of g with the tiles of `p`; RC, CC: whether k runs down the columns of the operand.
+template <typename E, int NP, bool RC, bool CC, typename Epi>
 hipError_t launch_product(const MatmulArgs& g, const ProductPlan& p, int batch, const Epi& epi, float* part, hipStream_t s) {
   if (p.splits > 1) {
     PartialStore store{part, (g.N + 3) & ~3, g.M};
-    const hipError_t e = p.tile == 128 ? launch_tiles<E, NP, 128, 128, 2, 2, 2>(g, p, batch, store, s)
-                                       : launch_tiles<E, NP, 64, 64, 2, 2, 3>(g, p, batch, store, s);
+    const hipError_t e = p.tile == 128 ? launch_tiles<E, NP, RC, CC, 128, 128, 2, 2, 2>(g, p, batch, store, s)
+                                       : launch_tiles<E, NP, RC, CC, 64, 64, 2, 2, 3>(g, p, batch, store, s);
     if (e != hipSuccess) return e;
     matmul_sum_kernel<Epi><<<dim3((unsigned)div_up(pad64(g.N), 128), (unsigned)(pad64(g.M) / 32), (unsigned)batch), dim3(256), 0, s>>>(
         part, p.splits, g.M, store.ld, p.tile, g.lower, epi);
     return hipGetLastError();
   }
   if constexpr (NP == 1) {
-    if (p.tile == 256) return launch_tiles<E, NP, 256, 256, 2, 4, 2>(g, p, batch, epi, s);
+    if (p.tile == 256) return launch_tiles<E, NP, RC, CC, 256, 256, 2, 4, 2>(g, p, batch, epi, s);
   }
-  if (p.tile == 128) return launch_tiles<E, NP, 128, 128, 2, 2, 2>(g, p, batch, epi, s);
-  return launch_tiles<E, NP, 64, 64, 2, 2, 3>(g, p, batch, epi, s);
+  if (p.tile == 128) return launch_tiles<E, NP, RC, CC, 128, 128, 2, 2, 2>(g, p, batch, epi, s);
+  return launch_tiles<E, NP, RC, CC, 64, 64, 2, 2, 3>(g, p, batch, epi, s);
 }
 
 }  // namespace amq

@@ -8,7 +8,8 @@
 // in one for bfloat16 data from n = 512 on.  Singular values stay below about 1.2 with the usual coefficients, so nothing comes near 65504 / 4096 = 16,
 // and half's smallest step is 2^-36 of an entry of 1.  One plane loses 1.4e-3 of the result in the 2-norm over five
 // steps, and the rounding to bfloat16 1.7e-3; two planes lose 3e-7.
-// X is kept in both orders, as either is an operand whose contraction runs along rows: X X^T takes X, B X takes X^T.
+// X lies as G does: of a wide G, X X^T contracts along rows and B X down the columns of X; of a tall one, which is the
+// transpose of X, X X^T contracts down its columns and B X along its rows.
 // The norm is summed in binary64, so that no gradient's scale overflows its square.
 #include "../../include/amq.h"
 
@@ -81,46 +82,39 @@ struct PolynomialStore {
   }
   __device__ __forceinline__ void along_m(int z, int m, int n, f32x4 v) const { along_n(z, n, m, v); }
 };
-// X = a X + B X in both orders.
+// X = a X + B X.  (Not in place: X is an operand of the product.)
 template <int NP>
 struct UpdateStore {
-  static constexpr bool kTransposed = true;
-  Planes<NP> X, Xt, next_t;  // X in place, its transpose not: it is an operand of the product
+  static constexpr bool kTransposed = false;
+  Planes<NP> X, next;
   float a;
   __device__ __forceinline__ void along_n(int z, int m, int n, f32x4 v) const {
-    if (X.has(m, n)) X.store(z, m, n, X.load(z, m, n) * a + v * kInvScale);
+    if (X.has(m, n)) next.store(z, m, n, X.load(z, m, n) * a + v * kInvScale);
   }
-  __device__ __forceinline__ void along_m(int z, int m, int n, f32x4 v) const {
-    if (next_t.has(n, m)) next_t.store(z, n, m, Xt.load(z, n, m) * a + v * kInvScale);
-  }
+  __device__ __forceinline__ void along_m(int, int, int, f32x4) const {}
 };
-// The last X, in the order of G.
-template <int NP, typename T, bool TALL>
+// The last X.
+template <int NP, typename T>
 struct ResultStore {
-  static constexpr bool kTransposed = TALL;
-  Planes<NP> X, Xt;
+  static constexpr bool kTransposed = false;
+  Planes<NP> X;
   T* out;
   int64_t ld, batch;
   float a;
-  __device__ __forceinline__ void put(int z, int row, int col, int cols, f32x4 v) const {
-    T* q = out + z * batch + row * ld + col;
-    struct __attribute__((packed, aligned(sizeof(T)))) {
+  __device__ __forceinline__ void along_n(int z, int m, int n, f32x4 v) const {
+    if (m >= X.rows || n >= X.cols) return;
+    v = (X.load(z, m, n) * a + v * kInvScale) * kInvScale;
+    T* q = out + z * batch + m * ld + n;
+    struct __attribute__((packed, aligned(sizeof(T)))) Four {
       T v[4];
     } o;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) o.v[i] = (T)(v[i] * kInvScale);
-    if (col + 4 <= cols) __builtin_memcpy(q, &o, sizeof(o));
+    for (int i = 0; i < 4; ++i) o.v[i] = (T)v[i];
+    if (n + 4 <= X.cols) *reinterpret_cast<Four*>(q) = o;
     else
-      for (int i = 0; i < cols - col; ++i) q[i] = (T)(v[i] * kInvScale);
+      for (int i = 0; i < X.cols - n; ++i) q[i] = (T)v[i];
   }
-  __device__ __forceinline__ void along_n(int z, int m, int n, f32x4 v) const {
-    if constexpr (!TALL)
-      if (m < X.rows && n < X.cols) put(z, m, n, X.cols, X.load(z, m, n) * a + v * kInvScale);
-  }
-  __device__ __forceinline__ void along_m(int z, int m, int n, f32x4 v) const {
-    if constexpr (TALL)
-      if (n < Xt.rows && m < Xt.cols) put(z, n, m, Xt.cols, Xt.load(z, n, m) * a + v * kInvScale);
-  }
+  __device__ __forceinline__ void along_m(int, int, int, f32x4) const {}
 };
 
 template <typename T>
@@ -157,32 +151,22 @@ __device__ __forceinline__ float inverse_norm(const double* parts, int z, int co
   return (float)(1.0 / (sqrt(block_sum<4>(s, scratch)) + (double)eps));
 }
 
-// X_0 in both orders, 64 x 64 values per workgroup: `same` has the order of G, `turned` that of its transpose.
+// X_0: 8 numbers per lane, rows dealt to the workgroups.
 template <typename T, int NP>
-__global__ __launch_bounds__(256) void ortho_begin_kernel(Gradient<T> G, const double* parts, int count, float eps, Planes<NP> same, Planes<NP> turned) {
+__global__ __launch_bounds__(256) void ortho_begin_kernel(Gradient<T> G, const double* parts, int count, float eps, Planes<NP> X) {
   __shared__ double scratch[4];
-  __shared__ float t[64][65];
-  const int z = blockIdx.z, r0 = blockIdx.y * 64, c0 = blockIdx.x * 64;
+  const int z = blockIdx.z;
   const float scale = inverse_norm(parts, z, count, eps, scratch) * kScale;
   const T* p = G.p + z * G.batch;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int row = i * 16 + (threadIdx.x >> 4), col = (threadIdx.x & 15) * 4;
-    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (r0 + row < G.rows) {
-      load_params<T, 4>(p, (int64_t)(r0 + row) * G.ld + c0 + col, G.cols - c0 - col, 0.0f, v);
-#pragma unroll
-      for (int q = 0; q < 4; ++q) v[q] *= scale;
-      same.store(z, r0 + row, c0 + col, f32x4{v[0], v[1], v[2], v[3]});
-    }
-#pragma unroll
-    for (int q = 0; q < 4; ++q) t[row][col + q] = v[q];
-  }
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int col = i * 16 + (threadIdx.x >> 4), row = (threadIdx.x & 15) * 4;
-    if (c0 + col < G.cols) turned.store(z, c0 + col, r0 + row, f32x4{t[row][col], t[row + 1][col], t[row + 2][col], t[row + 3][col]});
+  const int per_row = X.padded / 8;
+  const int64_t total = (int64_t)G.rows * per_row;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+    const int64_t row = i / per_row;
+    const int col = (int)(i % per_row) * 8;
+    float v[8];
+    load_params<T, 8>(p, row * G.ld + col, G.cols - col, 0.0f, v);
+    X.store(z, (int)row, col, f32x4{v[0], v[1], v[2], v[3]} * scale);
+    X.store(z, (int)row, col + 4, f32x4{v[4], v[5], v[6], v[7]} * scale);
   }
 }
 
@@ -199,22 +183,22 @@ __global__ __launch_bounds__(256) void ortho_scale_kernel(Gradient<T> G, const d
 }
 
 struct Room {
-  f16 *X, *Xt[2], *A, *B;
+  f16 *X[2], *A, *B;
   double* parts;
   float* part;
-  int64_t n, m, np, mp;
+  int64_t n, m;
   size_t total;
 };
-ProductPlan gram_plan(const Room& r, int planes, int64_t batch) { return plan_product(r.n, r.n, r.mp, planes, batch, true); }
-ProductPlan polynomial_plan(const Room& r, int planes, int64_t batch) { return plan_product(r.n, r.n, r.np, planes, batch, true); }
-ProductPlan update_plan(const Room& r, int planes, int64_t batch) { return plan_product(r.n, r.m, r.np, planes, batch, false); }
+ProductPlan gram_plan(const Room& r, int planes, int64_t batch) { return plan_product(r.n, r.n, r.m, planes, batch, true); }
+ProductPlan polynomial_plan(const Room& r, int planes, int64_t batch) { return plan_product(r.n, r.n, r.n, planes, batch, true); }
+ProductPlan update_plan(const Room& r, bool tall, int planes, int64_t batch) {
+  return plan_product(tall ? r.m : r.n, tall ? r.n : r.m, r.n, planes, batch, false);
+}
 
 Room room_of(void* ws, int64_t batch, int64_t rows, int64_t cols, int planes) {
   Room r{};
   r.n = rows < cols ? rows : cols;
   r.m = rows < cols ? cols : rows;
-  r.np = pad64(r.n);
-  r.mp = pad64(r.m);
   char* base = static_cast<char*>(ws);
   size_t off = 0;
   auto take = [&](size_t bytes) {
@@ -223,14 +207,12 @@ Room room_of(void* ws, int64_t batch, int64_t rows, int64_t cols, int planes) {
     return p;
   };
   const size_t value = sizeof(f16) * (size_t)planes * batch;
-  r.X = (f16*)take(value * r.n * r.mp);
-  r.Xt[0] = (f16*)take(value * r.m * r.np);
-  r.Xt[1] = (f16*)take(value * r.m * r.np);
-  r.A = (f16*)take(value * r.n * r.np);
-  r.B = (f16*)take(value * r.n * r.np);
+  for (f16*& x : r.X) x = (f16*)take(value * rows * pad64(cols));
+  r.A = (f16*)take(value * r.n * pad64(r.n));
+  r.B = (f16*)take(value * r.n * pad64(r.n));
   r.parts = (double*)take(sizeof(double) * kNormParts * (size_t)batch);
   size_t most = gram_plan(r, planes, batch).part_bytes;
-  for (size_t b : {polynomial_plan(r, planes, batch).part_bytes, update_plan(r, planes, batch).part_bytes})
+  for (size_t b : {polynomial_plan(r, planes, batch).part_bytes, update_plan(r, rows > cols, planes, batch).part_bytes})
     if (b > most) most = b;
   r.part = (float*)take(most);
   r.total = off;
@@ -247,11 +229,12 @@ hipError_t run(const OrthoArgs& o, hipStream_t s) {
   const bool tall = o.rows > o.cols;
   const Gradient<T> G{(const T*)o.G, o.ld_g, o.stride_g, o.rows, o.cols};
   T* out = (T*)o.out;
-  auto planes = [&](f16* p, int64_t rows, int64_t padded, int64_t cols) {
+  auto planes = [&](f16* p, int64_t rows, int64_t cols) {
+    const int64_t padded = pad64(cols);
     return Planes<NP>{p, NP * padded, rows * NP * padded, (int)rows, (int)cols, (int)padded};
   };
-  const Planes<NP> X = planes(r.X, r.n, r.mp, r.m), A = planes(r.A, r.n, r.np, r.n), B = planes(r.B, r.n, r.np, r.n);
-  const Planes<NP> Xt[2] = {planes(r.Xt[0], r.m, r.np, r.n), planes(r.Xt[1], r.m, r.np, r.n)};
+  const Planes<NP> X[2] = {planes(r.X[0], o.rows, o.cols), planes(r.X[1], o.rows, o.cols)};
+  const Planes<NP> A = planes(r.A, r.n, r.n), B = planes(r.B, r.n, r.n);
 
   const int64_t pieces = div_up(o.cols, 256 * kPer16<T>) * o.rows;
   const int count = (int)(pieces < kNormParts ? pieces : kNormParts);
@@ -263,30 +246,35 @@ hipError_t run(const OrthoArgs& o, hipStream_t s) {
         G, r.parts, count, o.eps, out, o.ld_out, o.stride_out);
     return hipGetLastError();
   }
-  ortho_begin_kernel<T, NP><<<dim3((unsigned)div_up(o.cols, 64), (unsigned)div_up(o.rows, 64), (unsigned)o.batch), dim3(256), 0, s>>>(
-      G, r.parts, count, o.eps, tall ? Xt[0] : X, tall ? X : Xt[0]);
+  const int64_t begin = div_up(o.rows * (int64_t)(X[0].padded / 8), 256);
+  ortho_begin_kernel<T, NP><<<dim3((unsigned)(begin < 2048 ? begin : 2048), 1, (unsigned)o.batch), dim3(256), 0, s>>>(G, r.parts, count, o.eps, X[0]);
   if ((e = hipGetLastError()) != hipSuccess) return e;
 
-  auto args = [&](const Planes<NP>& rows, const Planes<NP>& cols, int64_t k, bool lower) {
+  auto args = [&](const Planes<NP>& rows, bool rows_down, const Planes<NP>& cols, bool cols_down, int64_t k, bool lower) {
     MatmulArgs g{};
-    g.r = {rows.p, rows.ld, rows.batch, rows.rows};
-    g.c = {cols.p, cols.ld, cols.batch, cols.rows};
-    g.M = rows.rows;
-    g.N = cols.rows;
-    g.tiles_k = (int)k;
+    // (of an operand whose k runs down columns the padding counts as rows: zeros, and a multiple of 8)
+    g.r = {rows.p, rows.ld, rows.batch, rows_down ? rows.padded : rows.rows};
+    g.c = {cols.p, cols.ld, cols.batch, cols_down ? cols.padded : cols.rows};
+    g.M = rows_down ? rows.cols : rows.rows;
+    g.N = cols_down ? cols.cols : cols.rows;
+    g.k = (int)k;
     g.lower = lower;
     return g;
   };
-  const ProductPlan gram = gram_plan(r, NP, o.batch), polynomial = polynomial_plan(r, NP, o.batch), update = update_plan(r, NP, o.batch);
+  const ProductPlan gram = gram_plan(r, NP, o.batch), polynomial = polynomial_plan(r, NP, o.batch), update = update_plan(r, tall, NP, o.batch);
   for (int i = 0; i < o.steps; ++i) {
-    const Planes<NP>&now = Xt[i & 1], &next = Xt[(i + 1) & 1];
-    if ((e = launch_product<f16, NP>(args(X, X, r.mp, true), gram, o.batch, GramStore<NP>{A}, r.part, s)) != hipSuccess) return e;
-    if ((e = launch_product<f16, NP>(args(A, A, r.np, true), polynomial, o.batch, PolynomialStore<NP>{A, B, o.b, o.c}, r.part, s)) != hipSuccess)
-      return e;
-    const MatmulArgs g = args(B, now, r.np, false);
-    if (i + 1 < o.steps) e = launch_product<f16, NP>(g, update, o.batch, UpdateStore<NP>{X, now, next, o.a}, r.part, s);
-    else if (tall) e = launch_product<f16, NP>(g, update, o.batch, ResultStore<NP, T, true>{X, now, out, o.ld_out, o.stride_out, o.a}, r.part, s);
-    else e = launch_product<f16, NP>(g, update, o.batch, ResultStore<NP, T, false>{X, now, out, o.ld_out, o.stride_out, o.a}, r.part, s);
+    const Planes<NP>&now = X[i & 1], &next = X[(i + 1) & 1];
+    const MatmulArgs xx = args(now, tall, now, tall, r.m, true);
+    e = tall ? launch_product<f16, NP, true, true>(xx, gram, o.batch, GramStore<NP>{A}, r.part, s)
+             : launch_product<f16, NP, false, false>(xx, gram, o.batch, GramStore<NP>{A}, r.part, s);
+    if (e != hipSuccess) return e;
+    e = launch_product<f16, NP, false, false>(args(A, false, A, false, r.n, true), polynomial, o.batch, PolynomialStore<NP>{A, B, o.b, o.c}, r.part, s);
+    if (e != hipSuccess) return e;
+    auto multiply = [&](const auto& store) {
+      return tall ? launch_product<f16, NP, false, false>(args(now, false, B, false, r.n, false), update, o.batch, store, r.part, s)
+                  : launch_product<f16, NP, false, true>(args(B, false, now, true, r.n, false), update, o.batch, store, r.part, s);
+    };
+    e = i + 1 < o.steps ? multiply(UpdateStore<NP>{now, next, o.a}) : multiply(ResultStore<NP, T>{now, out, o.ld_out, o.stride_out, o.a});
     if (e != hipSuccess) return e;
   }
   return hipSuccess;

@@ -20,32 +20,54 @@
 namespace amq {
 namespace {
 
+// The activations and their slopes through the hardware's exponential and reciprocal (1 ulp each).
+__device__ __forceinline__ float logistic(float z) { return __builtin_amdgcn_rcpf(1.0f + __expf(-z)); }
+// (1 - e) / (1 + e) with e = exp(-2 |z|) loses digits near 0; there the series to z^9, 2e-9 off at 1/4.
+__device__ __forceinline__ float tanh_of(float z) {
+  const float s = z * z;
+  const float series = fmaf(fmaf(fmaf(fmaf(s, 62.0f / 2835.0f, -17.0f / 315.0f), s, 2.0f / 15.0f), s, -1.0f / 3.0f), s * z, z);
+  const float e = __expf(-2.0f * fabsf(z));
+  return fabsf(z) < 0.25f ? series : copysignf((1.0f - e) * __builtin_amdgcn_rcpf(1.0f + e), z);
+}
+// The normal distribution Phi(z) by Abramowitz and Stegun 7.1.26, erfc(x) = (a1 t + ... + a5 t^5) exp(-x^2), t = 1 / (1 + p x),
+// 1.5e-7 off at most; `density` receives exp(-z^2 / 2).
+__device__ __forceinline__ float normal_of(float z, float& density) {
+  const float x = fabsf(z) * 0.70710678118654752f;
+  const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.0f));
+  density = __expf(-x * x);
+  const float q = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f) * density;
+  return z < 0.0f ? 0.5f * q : 1.0f - 0.5f * q;
+}
 __device__ __forceinline__ float activate(float z, int act) {
+  float density;
   switch (act) {
     case AMQ_ACT_RELU: return z > 0.0f ? z : 0.0f;
-    case AMQ_ACT_GELU: return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
-    case AMQ_ACT_SILU: return z / (1.0f + expf(-z));
-    case AMQ_ACT_SIGMOID: return 1.0f / (1.0f + expf(-z));
-    case AMQ_ACT_TANH: return tanhf(z);
+    case AMQ_ACT_GELU: return z * normal_of(z, density);
+    case AMQ_ACT_SILU: return z * logistic(z);
+    case AMQ_ACT_SIGMOID: return logistic(z);
+    case AMQ_ACT_TANH: return tanh_of(z);
   }
   return z;
 }
 __device__ __forceinline__ float slope(float z, int act) {
+  float density;
   switch (act) {
     case AMQ_ACT_RELU: return z > 0.0f ? 1.0f : 0.0f;
-    case AMQ_ACT_GELU:
-      return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + z * (0.39894228040143268f * expf(-0.5f * z * z));
+    case AMQ_ACT_GELU: {
+      const float phi = normal_of(z, density);
+      return fmaf(z * 0.39894228040143268f, density, phi);
+    }
     case AMQ_ACT_SILU: {
-      const float s = 1.0f / (1.0f + expf(-z));
-      return s * (1.0f + z * (1.0f - s));
+      const float s = logistic(z);
+      return s * fmaf(z, 1.0f - s, 1.0f);
     }
     case AMQ_ACT_SIGMOID: {
-      const float s = 1.0f / (1.0f + expf(-z));
+      const float s = logistic(z);
       return s * (1.0f - s);
     }
     case AMQ_ACT_TANH: {
-      const float t = tanhf(z);
-      return 1.0f - t * t;
+      const float t = tanh_of(z);
+      return fmaf(-t, t, 1.0f);
     }
   }
   return 1.0f;
@@ -181,6 +203,20 @@ struct Source {
       for (int i = 0; i < V; ++i) v[i] *= slope(z[i], act);
     }
   }
+  // N rows `step` apart, zeros past the last.
+  template <int V, int N>
+  __device__ __forceinline__ void load_rows(int64_t row, int64_t step, int col, float (&v)[N][V]) const {
+    float z[N][V];
+#pragma unroll
+    for (int b = 0; b < N; ++b) load_params<T, V>(p, (row + b * step) * ld + col, row + b * step < rows ? cols - col : 0, 0.0f, v[b]);
+    if (!pre) return;
+#pragma unroll
+    for (int b = 0; b < N; ++b) load_params<T, V>(pre, (row + b * step) * ld_pre + col, row + b * step < rows ? cols - col : 0, 0.0f, z[b]);
+#pragma unroll
+    for (int b = 0; b < N; ++b)
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[b][i] *= slope(z[b][i], act);
+  }
 };
 // One matrix in the layout of the product kernel: rows of `padded` values (a multiple of 64, zeros past the end), in two halves
 // for float.
@@ -307,18 +343,23 @@ __global__ __launch_bounds__(256) void columns_kernel(ColumnJobs<T> jobs) {
   float s[V], largest[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) s[i] = largest[i] = 0.0f;
+  // four rows at a time, so that their loads are under way together
+  constexpr int kBatch = 4;
+  const int64_t step = 8 * gridDim.y;
   if (c < width)
-#pragma unroll 4
-    for (int64_t row = blockIdx.y * 8 + group; row < j.from.rows; row += 8 * gridDim.y) {
-      float v[V];
-      j.from.template load<V>(row, c, v);
+    for (int64_t row0 = blockIdx.y * 8 + group; row0 < j.from.rows; row0 += kBatch * step) {
+      float v[kBatch][V];
+      j.from.template load_rows<V, kBatch>(row0, step, c, v);
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
-        s[i] += v[i];
-        largest[i] = fmaxf(largest[i], fabsf(v[i]));
+      for (int b = 0; b < kBatch; ++b) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          s[i] += v[b][i];
+          largest[i] = fmaxf(largest[i], fabsf(v[b][i]));
+        }
+        if constexpr (V == 8)
+          if (j.to.p && row0 + b * step < j.from.rows) put8<T>(j.to, row0 + b * step, c, v[b]);
       }
-      if constexpr (V == 8)
-        if (j.to.p) put8<T>(j.to, row, c, v);
     }
 #pragma unroll
   for (int i = 0; i < V; ++i) {
@@ -509,11 +550,13 @@ ProductPlan plan_product(int64_t M, int64_t N, int64_t k, int planes, int64_t ba
   p.tile = planes == 1 && tiles(256) >= 192 ? 256 : tiles(128) >= 192 ? 128 : 64;
   const int64_t steps = div_up(k, stage_of(planes));
   p.tiles_per_split = (int)steps;
-  if (p.tile == 64 && tiles(64) < 256) {
-    int64_t splits = 512 / tiles(64);
-    if (splits > steps / 4) splits = steps / 4;
+  p.groups = 1;
+  if (p.tile == 64 && tiles(64) <= 256) {
+    p.groups = steps >= 8 ? 4 : 1;
+    int64_t splits = 256 / tiles(64);
+    if (splits > steps / 64) splits = steps / 64;
     if (splits > 1) {
-      p.tiles_per_split = (int)div_up(steps, 2 * splits) * 2;
+      p.tiles_per_split = (int)div_up(steps, 4 * splits) * 4;  // (a whole number of stages for each group)
       p.splits = (int)div_up(steps, p.tiles_per_split);
       if (p.splits > 1) p.part_bytes = sizeof(float) * (size_t)batch * p.splits * M * ((N + 3) & ~int64_t(3));
     }

@@ -79,23 +79,33 @@ __device__ __forceinline__ void tile_of(int id, int count, const MatmulArgs& g, 
   bn = at / rows;
 }
 
-// Hands a subtile of 32 x KW values (LDS, rows KW + 4 apart) to the epilogue, by one wave: four values along n per
-// call, consecutive lanes along n; then, where the epilogue wants the transpose too, four values along m per call.
-template <int KW, typename Epi>
-__device__ __forceinline__ void finish_subtile(const float* t, const Epi& epi, int z, int m0, int n0, bool mirror, int lane) {
+// Hands a subtile of 32 x KW values to the epilogue: four values along n per call, consecutive lanes along n; then, where
+// the epilogue wants the transpose too, four values along m per call.  The values lie in LDS, rows KW + 4 apart, as the sum of
+// KG parts `apart` values apart; KG waves share the subtile, this one is number `share`.
+template <int KW, int KG, typename Epi>
+__device__ __forceinline__ void finish_subtile(const float* t, int apart, int share, const Epi& epi, int z, int m0, int n0, bool mirror, int lane) {
   constexpr int kStride = KW + 4, kPerRow = KW / 4;
 #pragma unroll 1
-  for (int i = 0; i < 32 * kPerRow; i += 64) {
+  for (int i = share * 64; i < 32 * kPerRow; i += KG * 64) {
     const int row = (i + lane) / kPerRow, col = (i + lane) % kPerRow * 4;
-    epi.along_n(z, m0 + row, n0 + col, *reinterpret_cast<const f32x4*>(t + row * kStride + col));
+    const float* q = t + row * kStride + col;
+    f32x4 v = *reinterpret_cast<const f32x4*>(q);
+#pragma unroll
+    for (int g = 1; g < KG; ++g) v += *reinterpret_cast<const f32x4*>(q + g * apart);
+    epi.along_n(z, m0 + row, n0 + col, v);
   }
   if constexpr (Epi::kTransposed) {
     if (!mirror) return;
 #pragma unroll 1
-    for (int i = 0; i < 8 * KW; i += 64) {
+    for (int i = share * 64; i < 8 * KW; i += KG * 64) {
       const int col = (i + lane) >> 3, row = ((i + lane) & 7) * 4;
-      const float* q = t + row * kStride + col;
-      epi.along_m(z, m0 + row, n0 + col, f32x4{q[0], q[kStride], q[2 * kStride], q[3 * kStride]});
+      f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int g = 0; g < KG; ++g) {
+        const float* q = t + g * apart + row * kStride + col;
+        v += f32x4{q[0], q[kStride], q[2 * kStride], q[3 * kStride]};
+      }
+      epi.along_m(z, m0 + row, n0 + col, v);
     }
   }
 }
@@ -168,8 +178,9 @@ struct Side {
   __device__ __forceinline__ void copy(uint16_t* s, int t, int j) const {
     const char* from = base + t * stage;
     uint16_t* to = s + (wave + j * kWaves) * 512;
-    if ((NP == 1 || COLUMNS) && (t + 1) * kSteps > k) {
-      const int step = t * kSteps + (COLUMNS ? row_of(j) : ((lane % kLanes) ^ swizzle(row_of(j))) * 8);
+    if ((t + 1) * kSteps > k) {
+      const int piece = (lane % kLanes) ^ swizzle(row_of(j));
+      const int step = t * kSteps + (COLUMNS ? row_of(j) : (NP == 1 ? piece : piece & 3) * 8);
       copy_to_lds(step < k ? from + off[j] : (const char*)&kZeros, to);
     } else {
       copy_to_lds(from, off[j], to);
@@ -193,8 +204,9 @@ struct Side {
   }
 };
 
-template <typename E, int NP, bool RC, bool CC, int BM, int BN, int WR, int WC, int PLACES, typename Epi>
-__global__ __launch_bounds__(WR * WC * 64, 2) void matmul_kernel(MatmulArgs g, Epi epi) {
+// KG groups of WR x WC waves, each with its share of the stages and a ring of its own; their results are added up at the end.
+template <typename E, int NP, bool RC, bool CC, int BM, int BN, int WR, int WC, int KG, int PLACES, typename Epi>
+__global__ __launch_bounds__(KG * WR * WC * 64, KG * WR * WC >= 16 ? 4 : 2) void matmul_kernel(MatmulArgs g, Epi epi) {
   constexpr int kWaves = WR * WC, TM = BM / WR / 16, TN = BN / WC / 16;
   constexpr int kStage = (BM + BN) * 64;  // 16-bit values
   constexpr int KW = TN * 16, kStride = KW + 4;
@@ -203,15 +215,24 @@ __global__ __launch_bounds__(WR * WC * 64, 2) void matmul_kernel(MatmulArgs g, E
   using v8 = typename Element::v8;
   using R = Side<E, NP, BM, kWaves, RC>;
   using C = Side<E, NP, BN, kWaves, CC>;
-  __shared__ __align__(16) uint16_t lds[PLACES * kStage];
+  __shared__ __align__(16) uint16_t all_lds[KG * PLACES * kStage];
 
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63;
+  const int group = KG == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / kWaves;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) - group * kWaves;
+  uint16_t* lds = all_lds + group * (PLACES * kStage);
   const int wr = wave / WC, wc = wave % WC;
   int bm, bn;
   tile_of(blockIdx.x, gridDim.x, g, bm, bn);
   const int z = blockIdx.z;
-  const int first = blockIdx.y * g.tiles_per_split;
-  const int last = (first + g.tiles_per_split < g.tiles_k ? first + g.tiles_per_split : g.tiles_k) - 1;
+  // (the groups take as many stages each, so that they meet at every barrier; what lies past the end counts as zeros)
+  int first = blockIdx.y * g.tiles_per_split;
+  int last = (first + g.tiles_per_split < g.tiles_k ? first + g.tiles_per_split : g.tiles_k) - 1;
+  if constexpr (KG > 1) {
+    const int each = (last - first + KG) / KG;
+    first += group * each;
+    last = first + each - 1;
+  }
   const R r(g.r, z, bm * BM, g.k, lane, wave);
   const C c(g.c, z, bn * BN, g.k, lane, wave);
   // copy j of stage t of the contraction to its place in the ring; past the end the last stage again, so that as many copies
@@ -331,9 +352,12 @@ __global__ __launch_bounds__(WR * WC * 64, 2) void matmul_kernel(MatmulArgs g, E
 #pragma unroll
       for (int j = 0; j < TN; ++j)
         *reinterpret_cast<f32x4*>(mine + (h * 16 + (lane & 15)) * kStride + j * 16 + (lane >> 4) * 4) = acc[i + h][j];
-    __builtin_amdgcn_wave_barrier();
-    finish_subtile<KW>(mine, epi, z, bm * BM + wr * (BM / WR) + i * 16, bn * BN + wc * KW, mirror, lane);
-    __builtin_amdgcn_wave_barrier();
+    if constexpr (KG > 1) __syncthreads();
+    else __builtin_amdgcn_wave_barrier();
+    finish_subtile<KW, KG>(reinterpret_cast<float*>(all_lds) + wave * 32 * kStride, PLACES * kStage / 2, group, epi, z,
+                           bm * BM + wr * (BM / WR) + i * 16, bn * BN + wc * KW, mirror, lane);
+    if constexpr (KG > 1) __syncthreads();
+    else __builtin_amdgcn_wave_barrier();
   }
 }
 
@@ -372,7 +396,7 @@ __global__ __launch_bounds__(256) void matmul_sum_kernel(const float* part, int 
     *reinterpret_cast<f32x4*>(mine + row * 36 + col) = v;
   }
   __builtin_amdgcn_wave_barrier();
-  finish_subtile<32>(mine, epi, z, m0, n0, !lower || m0 / tile != n0 / tile, lane);
+  finish_subtile<32, 1>(mine, 0, 0, epi, z, m0, n0, !lower || m0 / tile != n0 / tile, lane);
 }
 
 // ---- host side
@@ -383,39 +407,40 @@ inline int stage_of(int planes) { return planes == 1 ? 64 : 32; }  // values of 
 
 struct ProductPlan {
   int tile;             // of the result: tile x tile values per workgroup
+  int groups;           // of waves that share a workgroup's stages (tile 64)
   int splits, tiles_per_split;
   size_t part_bytes;    // of partial results (splits > 1)
 };
 ProductPlan plan_product(int64_t M, int64_t N, int64_t k, int planes, int64_t batch, bool lower);
 
-template <typename E, int NP, bool RC, bool CC, int BM, int BN, int WR, int WC, int PLACES, typename Epi>
+template <typename E, int NP, bool RC, bool CC, int BM, int BN, int WR, int WC, int KG, int PLACES, typename Epi>
 hipError_t launch_tiles(MatmulArgs g, const ProductPlan& p, int batch, const Epi& epi, hipStream_t s) {
   g.tiles_k = (int)div_up(g.k, stage_of(NP));
   g.tiles_per_split = p.tiles_per_split;
   g.nbm = (int)div_up(g.M, BM);
   g.nbn = (int)div_up(g.N, BN);
   const int64_t tiles = g.lower ? (int64_t)g.nbm * (g.nbm + 1) / 2 : (int64_t)g.nbm * g.nbn;
-  matmul_kernel<E, NP, RC, CC, BM, BN, WR, WC, PLACES, Epi><<<dim3((unsigned)tiles, (unsigned)p.splits, (unsigned)batch), dim3(WR * WC * 64), 0, s>>>(g, epi);
+  matmul_kernel<E, NP, RC, CC, BM, BN, WR, WC, KG, PLACES, Epi><<<dim3((unsigned)tiles, (unsigned)p.splits, (unsigned)batch), dim3(KG * WR * WC * 64), 0, s>>>(g, epi);
   return hipGetLastError();
 }
 
 // The product of g with the tiles of `p`; RC, CC: whether k runs down the columns of the operand.
 template <typename E, int NP, bool RC, bool CC, typename Epi>
 hipError_t launch_product(const MatmulArgs& g, const ProductPlan& p, int batch, const Epi& epi, float* part, hipStream_t s) {
-  if (p.splits > 1) {
-    PartialStore store{part, (g.N + 3) & ~3, g.M};
-    const hipError_t e = p.tile == 128 ? launch_tiles<E, NP, RC, CC, 128, 128, 2, 2, 2>(g, p, batch, store, s)
-                                       : launch_tiles<E, NP, RC, CC, 64, 64, 2, 2, 3>(g, p, batch, store, s);
-    if (e != hipSuccess) return e;
-    matmul_sum_kernel<Epi><<<dim3((unsigned)div_up(pad64(g.N), 128), (unsigned)(pad64(g.M) / 32), (unsigned)batch), dim3(256), 0, s>>>(
-        part, p.splits, g.M, store.ld, p.tile, g.lower, epi);
-    return hipGetLastError();
-  }
-  if constexpr (NP == 1) {
-    if (p.tile == 256) return launch_tiles<E, NP, RC, CC, 256, 256, 2, 4, 2>(g, p, batch, epi, s);
-  }
-  if (p.tile == 128) return launch_tiles<E, NP, RC, CC, 128, 128, 2, 2, 2>(g, p, batch, epi, s);
-  return launch_tiles<E, NP, RC, CC, 64, 64, 2, 2, 3>(g, p, batch, epi, s);
+  auto run = [&](const auto& store) {
+    if constexpr (NP == 1)
+      if (p.tile == 256) return launch_tiles<E, NP, RC, CC, 256, 256, 2, 4, 1, 2>(g, p, batch, store, s);
+    if (p.tile == 128) return launch_tiles<E, NP, RC, CC, 128, 128, 2, 2, 1, 2>(g, p, batch, store, s);
+    if (p.groups == 4) return launch_tiles<E, NP, RC, CC, 64, 64, 2, 2, 4, 2>(g, p, batch, store, s);
+    return launch_tiles<E, NP, RC, CC, 64, 64, 2, 2, 1, 3>(g, p, batch, store, s);
+  };
+  if (p.splits == 1) return run(epi);
+  const PartialStore store{part, (g.N + 3) & ~3, g.M};
+  const hipError_t e = run(store);
+  if (e != hipSuccess) return e;
+  matmul_sum_kernel<Epi><<<dim3((unsigned)div_up(pad64(g.N), 128), (unsigned)(pad64(g.M) / 32), (unsigned)batch), dim3(256), 0, s>>>(
+      part, p.splits, g.M, store.ld, p.tile, g.lower, epi);
+  return hipGetLastError();
 }
 
 }  // namespace amq

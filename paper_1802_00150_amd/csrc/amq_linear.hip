@@ -13,6 +13,8 @@
 // A few rows (a token's vector) are multiplied on the vector units: there W is read once, and nothing else matters.
 #include "../../include/amq.h"
 
+#include <math.h>
+
 #include "amq_device.h"
 #include "amq_matmul_body.h"
 #include "amq_train.h"
@@ -38,39 +40,53 @@ __device__ __forceinline__ float normal_of(float z, float& density) {
   const float q = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f) * density;
   return z < 0.0f ? 0.5f * q : 1.0f - 0.5f * q;
 }
-__device__ __forceinline__ float activate(float z, int act) {
-  float density;
-  switch (act) {
-    case AMQ_ACT_RELU: return z > 0.0f ? z : 0.0f;
-    case AMQ_ACT_GELU: return z * normal_of(z, density);
-    case AMQ_ACT_SILU: return z * logistic(z);
-    case AMQ_ACT_SIGMOID: return logistic(z);
-    case AMQ_ACT_TANH: return tanh_of(z);
-  }
-  return z;
+// One of the functions below on V values: the choice is made once for all of them, so that they run side by side.
+template <int V, typename F>
+__device__ __forceinline__ void each(float (&v)[V], F f) {
+#pragma unroll
+  for (int i = 0; i < V; ++i) v[i] = f(v[i]);
 }
-__device__ __forceinline__ float slope(float z, int act) {
-  float density;
+template <int V>
+__device__ __forceinline__ void activate(float (&v)[V], int act) {
   switch (act) {
-    case AMQ_ACT_RELU: return z > 0.0f ? 1.0f : 0.0f;
-    case AMQ_ACT_GELU: {
-      const float phi = normal_of(z, density);
-      return fmaf(z * 0.39894228040143268f, density, phi);
-    }
-    case AMQ_ACT_SILU: {
-      const float s = logistic(z);
-      return s * fmaf(z, 1.0f - s, 1.0f);
-    }
-    case AMQ_ACT_SIGMOID: {
-      const float s = logistic(z);
-      return s * (1.0f - s);
-    }
-    case AMQ_ACT_TANH: {
-      const float t = tanh_of(z);
-      return fmaf(-t, t, 1.0f);
-    }
+    case AMQ_ACT_RELU: return each(v, [](float z) { return z > 0.0f ? z : 0.0f; });
+    case AMQ_ACT_GELU:
+      return each(v, [](float z) {
+        float density;
+        return z * normal_of(z, density);
+      });
+    case AMQ_ACT_SILU: return each(v, [](float z) { return z * logistic(z); });
+    case AMQ_ACT_SIGMOID: return each(v, [](float z) { return logistic(z); });
+    case AMQ_ACT_TANH: return each(v, [](float z) { return tanh_of(z); });
   }
-  return 1.0f;
+}
+template <int V>
+__device__ __forceinline__ void slopes(float (&v)[V], int act) {
+  switch (act) {
+    case AMQ_ACT_RELU: return each(v, [](float z) { return z > 0.0f ? 1.0f : 0.0f; });
+    case AMQ_ACT_GELU:
+      return each(v, [](float z) {
+        float density;
+        const float phi = normal_of(z, density);
+        return fmaf(z * 0.39894228040143268f, density, phi);
+      });
+    case AMQ_ACT_SILU:
+      return each(v, [](float z) {
+        const float s = logistic(z);
+        return s * fmaf(z, 1.0f - s, 1.0f);
+      });
+    case AMQ_ACT_SIGMOID:
+      return each(v, [](float z) {
+        const float s = logistic(z);
+        return s * (1.0f - s);
+      });
+    case AMQ_ACT_TANH:
+      return each(v, [](float z) {
+        const float t = tanh_of(z);
+        return fmaf(-t, t, 1.0f);
+      });
+  }
+  each(v, [](float) { return 1.0f; });
 }
 
 template <typename T, int V>
@@ -78,7 +94,21 @@ struct __attribute__((packed, aligned(sizeof(T)))) Group {
   T v[V];
 };
 
-// bias, activation, residual: what becomes of a product's values.
+template <typename T, int V>
+__device__ __forceinline__ void store_group(T* p, int valid, const float (&v)[V]) {
+  if (valid >= V) {
+    Group<T, V> o;
+#pragma unroll
+    for (int i = 0; i < V; ++i) o.v[i] = (T)v[i];
+    *reinterpret_cast<Group<T, V>*>(p) = o;
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (i < valid) p[i] = (T)v[i];
+  }
+}
+
+// Scales, bias, activation, residual: what becomes of a product's values.
 template <typename T>
 struct LinearStore {
   static constexpr bool kTransposed = false;
@@ -88,54 +118,48 @@ struct LinearStore {
   int64_t ld_y, ld_pre, ld_r;
   int M, N, act;
 
-  template <int V>
-  __device__ __forceinline__ void values(int m, int n, float (&v)[V]) const {
-    const int valid = N - n;
-    float b[V];
-    load_params<T, V>(bias, n, valid, 0.0f, b);
+  struct Column {
+    float bias[4];
+    int exp[4];
+  };
+  struct Extra {
+    float residual[4];
+    int exp;
+  };
+  __device__ __forceinline__ Column column(int, int n) const {
+    Column c;
+    load_params<T, 4>(bias, n, N - n, 0.0f, c.bias);
+    const int all = exp_all ? *exp_all : 0;
 #pragma unroll
-    for (int i = 0; i < V; ++i) v[i] += b[i];
-    if (pre) put<V>(pre + m * ld_pre + n, valid, v);
-    if (act != AMQ_ACT_NONE)
-#pragma unroll
-      for (int i = 0; i < V; ++i) v[i] = activate(v[i], act);
-    if (residual) {
-      load_params<T, V>(residual, m * ld_r + n, valid, 0.0f, b);
-#pragma unroll
-      for (int i = 0; i < V; ++i) v[i] += b[i];
-    }
-    put<V>(y + m * ld_y + n, valid, v);
+    for (int i = 0; i < 4; ++i) c.exp[i] = exp_c && n + i < N ? exp_c[n + i] : all;
+    return c;
   }
-  template <int V>
-  static __device__ __forceinline__ void put(T* p, int valid, const float (&v)[V]) {
-    if (valid >= V) {
-      Group<T, V> o;
-#pragma unroll
-      for (int i = 0; i < V; ++i) o.v[i] = (T)v[i];
-      *reinterpret_cast<Group<T, V>*>(p) = o;
-    } else {
-#pragma unroll
-      for (int i = 0; i < V; ++i)
-        if (i < valid) p[i] = (T)v[i];
-    }
+  __device__ __forceinline__ Extra fetch(int, int m, int n) const {
+    Extra e;
+    load_params<T, 4>(residual, m * ld_r + n, m < M ? N - n : 0, 0.0f, e.residual);
+    e.exp = exp_r && m < M ? exp_r[m] : 0;
+    return e;
   }
-  __device__ __forceinline__ void along_n(int, int m, int n, f32x4 v4) const {
+  __device__ __forceinline__ void put(int, int m, int n, f32x4 v4, const Column& c, const Extra& e) const {
     if (m >= M || n >= N) return;
     float v[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = v4[i];
-    if (exp_r) {
-      const int e = exp_r[m];
+    for (int i = 0; i < 4; ++i) v[i] = (exp_r || exp_all ? ldexpf(v4[i], -(e.exp + c.exp[i])) : v4[i]) + c.bias[i];
+    if (pre) store_group<T, 4>(pre + m * ld_pre + n, N - n, v);
+    activate(v, act);
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (n + i < N) v[i] = ldexpf(v[i], -(e + exp_c[n + i]));
-    } else if (exp_all) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = ldexpf(v[i], -*exp_all);
-    }
-    values<4>(m, n, v);
+    for (int i = 0; i < 4; ++i) v[i] += e.residual[i];
+    store_group<T, 4>(y + m * ld_y + n, N - n, v);
   }
-  __device__ __forceinline__ void along_m(int, int, int, f32x4) const {}
+  // one value
+  __device__ __forceinline__ void put1(int m, int n, float v) const {
+    if (bias) v += (float)bias[n];
+    if (pre) pre[m * ld_pre + n] = (T)v;
+    float one[1] = {v};
+    activate(one, act);
+    if (residual) one[0] += (float)residual[m * ld_r + n];
+    y[m * ld_y + n] = (T)one[0];
+  }
 };
 
 // ---- a few rows: workgroup = 4 rows of W, its waves share the row's k
@@ -177,10 +201,8 @@ __global__ __launch_bounds__(256) void linear_few_kernel(const T* x, int64_t ld_
   __syncthreads();
   if (threadIdx.x < R * M) {
     const int m = threadIdx.x / R, n = n0 + threadIdx.x % R;
-    if (m < out.M && n < out.N) {
-      float v[1] = {sums[0][threadIdx.x] + sums[1][threadIdx.x] + sums[2][threadIdx.x] + sums[3][threadIdx.x]};
-      out.template values<1>(m, n, v);
-    }
+    if (m < out.M && n < out.N)
+      out.put1(m, n, sums[0][threadIdx.x] + sums[1][threadIdx.x] + sums[2][threadIdx.x] + sums[3][threadIdx.x]);
   }
 }
 
@@ -199,8 +221,9 @@ struct Source {
     if (pre) {
       float z[V];
       load_params<T, V>(pre, row * ld_pre + col, cols - col, 0.0f, z);
+      slopes(z, act);
 #pragma unroll
-      for (int i = 0; i < V; ++i) v[i] *= slope(z[i], act);
+      for (int i = 0; i < V; ++i) v[i] *= z[i];
     }
   }
   // N rows `step` apart, zeros past the last.
@@ -213,9 +236,11 @@ struct Source {
 #pragma unroll
     for (int b = 0; b < N; ++b) load_params<T, V>(pre, (row + b * step) * ld_pre + col, row + b * step < rows ? cols - col : 0, 0.0f, z[b]);
 #pragma unroll
-    for (int b = 0; b < N; ++b)
+    for (int b = 0; b < N; ++b) {
+      slopes(z[b], act);
 #pragma unroll
-      for (int i = 0; i < V; ++i) v[b][i] *= slope(z[b][i], act);
+      for (int i = 0; i < V; ++i) v[b][i] *= z[b][i];
+    }
   }
 };
 // One matrix in the layout of the product kernel: rows of `padded` values (a multiple of 64, zeros past the end), in two halves
@@ -540,28 +565,51 @@ hipError_t linear_few(const LinearArgs& a, const LinearStore<T>& out, hipStream_
 
 }  // namespace
 
+// The form of a product that takes the least time by these estimates, in us, with `load` tiles per compute unit and `stages`
+// stages each.  Fitted to 22 shapes from 64 x 1024 x 1024 to 8960 x 4096 x 1024, bfloat16 and float, within 15 %; examples
+// (bfloat16 with gelu, tile 256 / 128 / 64 / 64 with four groups): 8960 x 4096 x 1024 134 / 120 / 145 / 247, 4096^3 116 / 138 /
+// 205 / 260, 2240 x 1024 x 1024 41 / 23 / 15 / 22, 1024 x 1024 x 2240 61 / 33 / 18 / 13, 300 x 300 x 1216 43 / 23 / 12 / 9.
+//   256 (one workgroup per unit): a round 24 + 1.3 per stage
+//   128 (two): 10 + a tile 4 + 0.55 per stage, and a last round that is not full counts half as one
+//   64 (three): 6.5 + a tile 0.9 + 0.2 per stage, alone 5.5 + 0.32 per stage
+//   64 with four groups (one): 2 + a round 3.4 + 0.17 per stage
+// Numbers of two halves take half of a stage's steps, and 1.15 to 1.3 times its time.  A contraction split among workgroups
+// costs a second launch of 6 us and the partial results twice through memory at 3 TB/s.
 ProductPlan plan_product(int64_t M, int64_t N, int64_t k, int planes, int64_t batch, bool lower) {
-  auto tiles = [&](int64_t t) {
-    const int64_t a = div_up(M, t), b = div_up(N, t);
-    return batch * (lower ? a * (a + 1) / 2 : a * b);
-  };
-  ProductPlan p{};
-  p.splits = 1;
-  p.tile = planes == 1 && tiles(256) >= 192 ? 256 : tiles(128) >= 192 ? 128 : 64;
-  const int64_t steps = div_up(k, stage_of(planes));
-  p.tiles_per_split = (int)steps;
-  p.groups = 1;
-  if (p.tile == 64 && tiles(64) <= 256) {
-    p.groups = steps >= 8 ? 4 : 1;
-    int64_t splits = 256 / tiles(64);
-    if (splits > steps / 64) splits = steps / 64;
-    if (splits > 1) {
-      p.tiles_per_split = (int)div_up(steps, 4 * splits) * 4;  // (a whole number of stages for each group)
-      p.splits = (int)div_up(steps, p.tiles_per_split);
-      if (p.splits > 1) p.part_bytes = sizeof(float) * (size_t)batch * p.splits * M * ((N + 3) & ~int64_t(3));
+  const int64_t stages = div_up(k, stage_of(planes));
+  ProductPlan best{};
+  double least = 1e300;
+  auto consider = [&](int tile, int groups, int64_t splits) {
+    const int64_t a = div_up(M, tile), b = div_up(N, tile);
+    const int64_t tiles = batch * (lower ? a * (a + 1) / 2 : a * b);
+    ProductPlan p{};
+    p.tile = tile;
+    p.groups = groups;
+    // (a whole number of stages for each group)
+    p.tiles_per_split = (int)(splits == 1 ? stages : div_up(stages, 4 * splits) * 4);
+    p.splits = (int)div_up(stages, p.tiles_per_split);
+    const double load = (double)tiles * p.splits / 256.0, rounds = (double)div_up(tiles * p.splits, 256), s = p.tiles_per_split;
+    double us;
+    if (tile == 256) us = rounds * (24.0 + 1.3 * s);
+    else if (tile == 128) us = 10.0 + 0.5 * (rounds + load) * (4.0 + (planes == 1 ? 0.55 : 0.68) * s);
+    else if (groups == 4) us = 2.0 + rounds * (3.4 + (planes == 1 ? 0.17 : 0.22) * s);
+    else us = fmax(5.5 + (planes == 1 ? 0.32 : 0.4) * s, 6.5 + load * (0.9 + (planes == 1 ? 0.2 : 0.23) * s));
+    if (p.splits > 1) {
+      p.part_bytes = sizeof(float) * (size_t)batch * p.splits * M * ((N + 3) & ~int64_t(3));
+      us += 6.0 + 2.0 * (double)p.part_bytes / 3e6;
     }
+    if (us < least) {
+      least = us;
+      best = p;
+    }
+  };
+  if (planes == 1) consider(256, 1, 1);
+  for (int64_t splits = 1; splits <= 32 && (splits == 1 || stages >= 16 * splits); splits *= 2) {
+    consider(128, 1, splits);
+    consider(64, 1, splits);
+    if (stages >= 4) consider(64, 4, splits);
   }
-  return p;
+  return best;
 }
 
 size_t linear_workspace(int64_t rows, int64_t k, int64_t n, int type) { return forward_room(nullptr, rows, k, n, type).total; }

@@ -79,33 +79,52 @@ __device__ __forceinline__ void tile_of(int id, int count, const MatmulArgs& g, 
   bn = at / rows;
 }
 
-// Hands a subtile of 32 x KW values to the epilogue: four values along n per call, consecutive lanes along n; then, where
-// the epilogue wants the transpose too, four values along m per call.  The values lie in LDS, rows KW + 4 apart, as the sum of
-// KG parts `apart` values apart; KG waves share the subtile, this one is number `share`.
+// An epilogue takes four values along n at a time, in three parts, so that what it reads is under way before it is needed:
+//   Column column(z, n)             what goes with columns n .. n + 3, once per wave (a lane keeps its columns)
+//   Extra fetch(z, m, n)            what goes with the values, for several rows ahead
+//   put(z, m, n, v, column, extra)  the values
+// With kTransposed it gets the transpose of tiles off the diagonal too, by fetch and put with m and n exchanged.
+//
+// Hands over a subtile of 32 x KW values.  They lie in LDS, rows KW + 4 apart, as the sum of KG parts `apart` values apart; KG
+// waves share the subtile, this one is number `share`.
+template <int KW>
+__device__ __forceinline__ int column_of(int lane) {
+  return lane % (KW / 4) * 4;
+}
 template <int KW, int KG, typename Epi>
-__device__ __forceinline__ void finish_subtile(const float* t, int apart, int share, const Epi& epi, int z, int m0, int n0, bool mirror, int lane) {
-  constexpr int kStride = KW + 4, kPerRow = KW / 4;
+__device__ __forceinline__ void finish_subtile(const float* t, int apart, int share, const Epi& epi, const typename Epi::Column& column, int z, int m0,
+                                               int n0, bool mirror, int lane) {
+  constexpr int kStride = KW + 4, kPerRow = KW / 4, kCalls = 32 * kPerRow / 64 / KG, kAhead = kCalls < 4 ? kCalls : 4;
+  static_assert(64 % kPerRow == 0 && kCalls * KG * 64 == 32 * kPerRow, "whole rows");
+  const int col = column_of<KW>(lane);
 #pragma unroll 1
-  for (int i = share * 64; i < 32 * kPerRow; i += KG * 64) {
-    const int row = (i + lane) / kPerRow, col = (i + lane) % kPerRow * 4;
-    const float* q = t + row * kStride + col;
-    f32x4 v = *reinterpret_cast<const f32x4*>(q);
+  for (int c = 0; c < kCalls; c += kAhead) {
+    typename Epi::Extra extra[kAhead];
 #pragma unroll
-    for (int g = 1; g < KG; ++g) v += *reinterpret_cast<const f32x4*>(q + g * apart);
-    epi.along_n(z, m0 + row, n0 + col, v);
+    for (int u = 0; u < kAhead; ++u) extra[u] = epi.fetch(z, m0 + (((c + u) * KG + share) * 64 + lane) / kPerRow, n0 + col);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int row = (((c + u) * KG + share) * 64 + lane) / kPerRow;
+      const float* q = t + row * kStride + col;
+      f32x4 v = *reinterpret_cast<const f32x4*>(q);
+#pragma unroll
+      for (int g = 1; g < KG; ++g) v += *reinterpret_cast<const f32x4*>(q + g * apart);
+      epi.put(z, m0 + row, n0 + col, v, column, extra[u]);
+    }
   }
   if constexpr (Epi::kTransposed) {
     if (!mirror) return;
-#pragma unroll 1
-    for (int i = share * 64; i < 8 * KW; i += KG * 64) {
-      const int col = (i + lane) >> 3, row = ((i + lane) & 7) * 4;
+    constexpr int kTurned = 8 * KW / 64;  // pieces of 64 lanes
+    for (int c = share; c < kTurned; c += KG) {
+      const int n = (c * 64 + lane) >> 3, m = ((c * 64 + lane) & 7) * 4;
+      const typename Epi::Extra extra = epi.fetch(z, n0 + n, m0 + m);
       f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int g = 0; g < KG; ++g) {
-        const float* q = t + g * apart + row * kStride + col;
+        const float* q = t + g * apart + m * kStride + n;
         v += f32x4{q[0], q[kStride], q[2 * kStride], q[3 * kStride]};
       }
-      epi.along_m(z, m0 + row, n0 + col, v);
+      epi.put(z, n0 + n, m0 + m, v, typename Epi::Column{}, extra);
     }
   }
 }
@@ -141,9 +160,16 @@ struct Side {
   static constexpr int kSteps = NP == 1 ? 64 : 32;       // of k in a stage
   static_assert(kCopies * 8 * kWaves == B, "copies");
 
+  // Rows of memory that the copies of a wave are apart.  Down columns every 16 rows have the same offsets within their rows, so
+  // that one offset serves several copies (rows may end inside a tile and need one each).
+  static constexpr int kApart = kWaves * 64 / kLanes;
+  static constexpr int kOffsets = COLUMNS ? (kApart >= 16 ? 1 : 16 / kApart) : kCopies;
+  static_assert(kApart >= 16 || 16 % kApart == 0, "copies and the order of pieces");
+
   const char* base;    // of the tile, uniform
   int64_t stage;       // bytes from one stage to the next
-  uint32_t off[kCopies];
+  int64_t line;        // bytes from one row of memory to the next
+  uint32_t off[kOffsets];
   int k, lane, wave;
 
   static __device__ __forceinline__ int swizzle(int row) {  // of 16-byte pieces
@@ -153,6 +179,7 @@ struct Side {
   }
   __device__ __forceinline__ Side(const MatmulOperand& o, int z, int first_row, int k_, int lane_, int wave_) : k(k_), lane(lane_), wave(wave_) {
     const uint16_t* p = (const uint16_t*)o.p + z * o.batch;
+    line = o.ld * 2;
     if constexpr (COLUMNS) {
       base = (const char*)(p + (int64_t)first_row * NP);
       stage = o.ld * kSteps * 2;
@@ -161,7 +188,7 @@ struct Side {
       stage = 128;
     }
 #pragma unroll
-    for (int j = 0; j < kCopies; ++j) {
+    for (int j = 0; j < kOffsets; ++j) {
       const int row = row_of(j), piece = (lane % kLanes) ^ swizzle(row);
       if constexpr (COLUMNS) {
         // past the operand's last rows those again (their number is a multiple of 8)
@@ -176,14 +203,15 @@ struct Side {
   __device__ __forceinline__ int row_of(int j) const { return (wave + j * kWaves) * (64 / kLanes) + lane / kLanes; }
   // Copy j of stage t.  Steps of k past the end are zeros (along rows: to the next multiple of 8 what lies there).
   __device__ __forceinline__ void copy(uint16_t* s, int t, int j) const {
-    const char* from = base + t * stage;
+    const char* from = base + t * stage + (COLUMNS ? j / kOffsets * (kOffsets * kApart) * line : 0);
+    const uint32_t at = off[j % kOffsets];
     uint16_t* to = s + (wave + j * kWaves) * 512;
     if ((t + 1) * kSteps > k) {
       const int piece = (lane % kLanes) ^ swizzle(row_of(j));
       const int step = t * kSteps + (COLUMNS ? row_of(j) : (NP == 1 ? piece : piece & 3) * 8);
-      copy_to_lds(step < k ? from + off[j] : (const char*)&kZeros, to);
+      copy_to_lds(step < k ? from + at : (const char*)&kZeros, to);
     } else {
-      copy_to_lds(from, off[j], to);
+      copy_to_lds(from, at, to);
     }
   }
   // Fragment of 16 rows from row0 + 16 i on (row0: of the wave): half `half` of the stage, or of its numbers.
@@ -191,12 +219,13 @@ struct Side {
     if constexpr (!COLUMNS) {
       return *reinterpret_cast<const v8*>(s + (row0 + i * 16 + (lane & 15)) * 64 + ((half * 4 + (lane >> 4)) ^ swizzle(lane & 15)) * 8);
     } else {
-      // bytes of the 32-byte part within a row: row0 takes the high bits, the fragment's number the low ones
+      // The 32-byte part within a row: row0 takes the high bits, the fragment's number the low ones.  (The number comes in last, so
+      // that an address is one operation on the place's and not a register held for each fragment.)
       const int step = (lane >> 4) * 8 + ((lane & 15) >> 2);
       const int part = NP == 1 ? i : (i >> 1) * 4 + half * 2 + (i & 1);
-      const uint32_t at = ((uint32_t)(step * kLine + ((row0 * NP / 8) ^ swizzle(step)) * 16 + (lane & 3) * 8) ^ (uint32_t)(part * 32)) +
-                          (NP == 1 ? half * 32 * kLine : 0);
-      const auto* q = (__attribute__((address_space(3))) const char*)(__attribute__((address_space(3))) const uint16_t*)s + at;
+      const uint32_t place = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint16_t*)s;
+      const uint32_t at = (place + (uint32_t)(step * kLine + ((row0 * NP / 8) ^ swizzle(step)) * 16 + (lane & 3) * 8)) ^ (uint32_t)(part * 32);
+      const auto* q = (__attribute__((address_space(3))) const char*)(uintptr_t)at + (NP == 1 ? half * 32 * kLine : 0);
       const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)q);
       const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(q + 4 * kLine));
       return __builtin_bit_cast(v8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
@@ -215,7 +244,7 @@ __global__ __launch_bounds__(KG * WR * WC * 64, KG * WR * WC >= 16 ? 4 : 2) void
   using v8 = typename Element::v8;
   using R = Side<E, NP, BM, kWaves, RC>;
   using C = Side<E, NP, BN, kWaves, CC>;
-  __shared__ __align__(16) uint16_t all_lds[KG * PLACES * kStage];
+  __shared__ __align__(256) uint16_t all_lds[KG * PLACES * kStage];
 
   const int lane = threadIdx.x & 63;
   const int group = KG == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / kWaves;
@@ -345,6 +374,8 @@ __global__ __launch_bounds__(KG * WR * WC * 64, KG * WR * WC >= 16 ? 4 : 2) void
   // epilogue's code
   float* mine = reinterpret_cast<float*>(lds) + wave * 32 * kStride;
   const bool mirror = !g.lower || bm != bn;
+  const int n0 = bn * BN + wc * KW;
+  const typename Epi::Column column = epi.column(z, n0 + column_of<KW>(lane));
 #pragma unroll
   for (int i = 0; i < TM; i += 2) {
 #pragma unroll
@@ -354,8 +385,8 @@ __global__ __launch_bounds__(KG * WR * WC * 64, KG * WR * WC >= 16 ? 4 : 2) void
         *reinterpret_cast<f32x4*>(mine + (h * 16 + (lane & 15)) * kStride + j * 16 + (lane >> 4) * 4) = acc[i + h][j];
     if constexpr (KG > 1) __syncthreads();
     else __builtin_amdgcn_wave_barrier();
-    finish_subtile<KW, KG>(reinterpret_cast<float*>(all_lds) + wave * 32 * kStride, PLACES * kStage / 2, group, epi, z,
-                           bm * BM + wr * (BM / WR) + i * 16, bn * BN + wc * KW, mirror, lane);
+    finish_subtile<KW, KG>(reinterpret_cast<float*>(all_lds) + wave * 32 * kStride, PLACES * kStage / 2, group, epi, column, z,
+                           bm * BM + wr * (BM / WR) + i * 16, n0, mirror, lane);
     if constexpr (KG > 1) __syncthreads();
     else __builtin_amdgcn_wave_barrier();
   }
@@ -367,11 +398,14 @@ struct PartialStore {
   float* part;        // [batch][splits][M][ld]
   int64_t ld;         // a multiple of 4
   int M;
-  __device__ __forceinline__ void along_n(int z, int m, int n, f32x4 v) const {
+  struct Column {};
+  struct Extra {};
+  __device__ __forceinline__ Column column(int, int) const { return {}; }
+  __device__ __forceinline__ Extra fetch(int, int, int) const { return {}; }
+  __device__ __forceinline__ void put(int z, int m, int n, f32x4 v, const Column&, const Extra&) const {
     if (m < M && n < ld)
       *reinterpret_cast<f32x4*>(part + (((int64_t)z * gridDim.y + blockIdx.y) * M + m) * ld + n) = v;
   }
-  __device__ __forceinline__ void along_m(int, int, int, f32x4) const {}
 };
 
 // One wave per 32 x 32 values, up to the next multiple of 64 in both directions (operands of further products want zeros
@@ -396,7 +430,7 @@ __global__ __launch_bounds__(256) void matmul_sum_kernel(const float* part, int 
     *reinterpret_cast<f32x4*>(mine + row * 36 + col) = v;
   }
   __builtin_amdgcn_wave_barrier();
-  finish_subtile<32, 1>(mine, 0, 0, epi, z, m0, n0, !lower || m0 / tile != n0 / tile, lane);
+  finish_subtile<32, 1>(mine, 0, 0, epi, epi.column(z, n0 + column_of<32>(lane)), z, m0, n0, !lower || m0 / tile != n0 / tile, lane);
 }
 
 // ---- host side

@@ -61,49 +61,60 @@ struct Planes {
   }
 };
 
+// What the epilogues below have in common: nothing per column, four scaled values of a matrix per call.
+struct OrthoStore {
+  struct Column {};
+  typedef f32x4 Extra;
+  __device__ __forceinline__ Column column(int, int) const { return {}; }
+};
 // A = X X^T, both triangles from the lower tiles.
 template <int NP>
-struct GramStore {
+struct GramStore : OrthoStore {
   static constexpr bool kTransposed = true;
   Planes<NP> A;
-  __device__ __forceinline__ void along_n(int z, int m, int n, f32x4 v) const {
+  explicit GramStore(const Planes<NP>& a) : A(a) {}
+  __device__ __forceinline__ f32x4 fetch(int, int, int) const { return f32x4{}; }
+  __device__ __forceinline__ void put(int z, int m, int n, f32x4 v, const Column&, const f32x4&) const {
     if (A.has(m, n)) A.store(z, m, n, v * kInvScale);
   }
-  __device__ __forceinline__ void along_m(int z, int m, int n, f32x4 v) const { along_n(z, n, m, v); }
 };
-// B = b A + c A A.
+// B = b A + c A A, A being symmetric as well.
 template <int NP>
-struct PolynomialStore {
+struct PolynomialStore : OrthoStore {
   static constexpr bool kTransposed = true;
   Planes<NP> A, B;
   float b, c;
-  __device__ __forceinline__ void along_n(int z, int m, int n, f32x4 v) const {
-    if (B.has(m, n)) B.store(z, m, n, A.load(z, m, n) * b + v * (c * kInvScale));
+  PolynomialStore(const Planes<NP>& a_, const Planes<NP>& b_, float fb, float fc) : A(a_), B(b_), b(fb), c(fc) {}
+  __device__ __forceinline__ f32x4 fetch(int z, int m, int n) const { return A.has(m, n) ? A.load(z, m, n) : f32x4{}; }
+  __device__ __forceinline__ void put(int z, int m, int n, f32x4 v, const Column&, const f32x4& a) const {
+    if (B.has(m, n)) B.store(z, m, n, a * b + v * (c * kInvScale));
   }
-  __device__ __forceinline__ void along_m(int z, int m, int n, f32x4 v) const { along_n(z, n, m, v); }
 };
 // X = a X + B X.  (Not in place: X is an operand of the product.)
 template <int NP>
-struct UpdateStore {
+struct UpdateStore : OrthoStore {
   static constexpr bool kTransposed = false;
   Planes<NP> X, next;
   float a;
-  __device__ __forceinline__ void along_n(int z, int m, int n, f32x4 v) const {
-    if (X.has(m, n)) next.store(z, m, n, X.load(z, m, n) * a + v * kInvScale);
+  UpdateStore(const Planes<NP>& x, const Planes<NP>& n, float fa) : X(x), next(n), a(fa) {}
+  __device__ __forceinline__ f32x4 fetch(int z, int m, int n) const { return X.has(m, n) ? X.load(z, m, n) : f32x4{}; }
+  __device__ __forceinline__ void put(int z, int m, int n, f32x4 v, const Column&, const f32x4& x) const {
+    if (X.has(m, n)) next.store(z, m, n, x * a + v * kInvScale);
   }
-  __device__ __forceinline__ void along_m(int, int, int, f32x4) const {}
 };
 // The last X.
 template <int NP, typename T>
-struct ResultStore {
+struct ResultStore : OrthoStore {
   static constexpr bool kTransposed = false;
   Planes<NP> X;
   T* out;
   int64_t ld, batch;
   float a;
-  __device__ __forceinline__ void along_n(int z, int m, int n, f32x4 v) const {
+  ResultStore(const Planes<NP>& x, T* o, int64_t l, int64_t b, float fa) : X(x), out(o), ld(l), batch(b), a(fa) {}
+  __device__ __forceinline__ f32x4 fetch(int z, int m, int n) const { return X.has(m, n) ? X.load(z, m, n) : f32x4{}; }
+  __device__ __forceinline__ void put(int z, int m, int n, f32x4 v, const Column&, const f32x4& x) const {
     if (m >= X.rows || n >= X.cols) return;
-    v = (X.load(z, m, n) * a + v * kInvScale) * kInvScale;
+    v = (x * a + v * kInvScale) * kInvScale;
     T* q = out + z * batch + m * ld + n;
     struct __attribute__((packed, aligned(sizeof(T)))) Four {
       T v[4];
@@ -114,7 +125,6 @@ struct ResultStore {
     else
       for (int i = 0; i < X.cols - n; ++i) q[i] = (T)v[i];
   }
-  __device__ __forceinline__ void along_m(int, int, int, f32x4) const {}
 };
 
 template <typename T>
@@ -265,16 +275,16 @@ hipError_t run(const OrthoArgs& o, hipStream_t s) {
   for (int i = 0; i < o.steps; ++i) {
     const Planes<NP>&now = X[i & 1], &next = X[(i + 1) & 1];
     const MatmulArgs xx = args(now, tall, now, tall, r.m, true);
-    e = tall ? launch_product<f16, NP, true, true>(xx, gram, o.batch, GramStore<NP>{A}, r.part, s)
-             : launch_product<f16, NP, false, false>(xx, gram, o.batch, GramStore<NP>{A}, r.part, s);
+    e = tall ? launch_product<f16, NP, true, true>(xx, gram, o.batch, GramStore<NP>(A), r.part, s)
+             : launch_product<f16, NP, false, false>(xx, gram, o.batch, GramStore<NP>(A), r.part, s);
     if (e != hipSuccess) return e;
-    e = launch_product<f16, NP, false, false>(args(A, false, A, false, r.n, true), polynomial, o.batch, PolynomialStore<NP>{A, B, o.b, o.c}, r.part, s);
+    e = launch_product<f16, NP, false, false>(args(A, false, A, false, r.n, true), polynomial, o.batch, PolynomialStore<NP>(A, B, o.b, o.c), r.part, s);
     if (e != hipSuccess) return e;
     auto multiply = [&](const auto& store) {
       return tall ? launch_product<f16, NP, false, false>(args(now, false, B, false, r.n, false), update, o.batch, store, r.part, s)
                   : launch_product<f16, NP, false, true>(args(B, false, now, true, r.n, false), update, o.batch, store, r.part, s);
     };
-    e = i + 1 < o.steps ? multiply(UpdateStore<NP>{now, next, o.a}) : multiply(ResultStore<NP, T>{now, out, o.ld_out, o.stride_out, o.a});
+    e = i + 1 < o.steps ? multiply(UpdateStore<NP>(now, next, o.a)) : multiply(ResultStore<NP, T>(now, out, o.ld_out, o.stride_out, o.a));
     if (e != hipSuccess) return e;
   }
   return hipSuccess;

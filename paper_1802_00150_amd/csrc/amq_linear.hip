@@ -89,25 +89,6 @@ __device__ __forceinline__ void slopes(float (&v)[V], int act) {
   each(v, [](float) { return 1.0f; });
 }
 
-template <typename T, int V>
-struct __attribute__((packed, aligned(sizeof(T)))) Group {
-  T v[V];
-};
-
-template <typename T, int V>
-__device__ __forceinline__ void store_group(T* p, int valid, const float (&v)[V]) {
-  if (valid >= V) {
-    Group<T, V> o;
-#pragma unroll
-    for (int i = 0; i < V; ++i) o.v[i] = (T)v[i];
-    *reinterpret_cast<Group<T, V>*>(p) = o;
-  } else {
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-      if (i < valid) p[i] = (T)v[i];
-  }
-}
-
 // Scales, bias, activation, residual: what becomes of a product's values.
 template <typename T>
 struct LinearStore {
@@ -145,11 +126,11 @@ struct LinearStore {
     float v[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = (exp_r || exp_all ? ldexpf(v4[i], -(e.exp + c.exp[i])) : v4[i]) + c.bias[i];
-    if (pre) store_group<T, 4>(pre + m * ld_pre + n, N - n, v);
+    if (pre) store<T, 4>(pre + m * ld_pre + n, N - n, v);
     activate(v, act);
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] += e.residual[i];
-    store_group<T, 4>(y + m * ld_y + n, N - n, v);
+    store<T, 4>(y + m * ld_y + n, N - n, v);
   }
   // one value
   __device__ __forceinline__ void put1(int m, int n, float v) const {
@@ -270,7 +251,7 @@ __device__ __forceinline__ int scale_exponent(float largest) { return largest > 
 // 8 values of a row as the products take them.
 template <typename T>
 __device__ __forceinline__ void put8(const Laid& to, int64_t row, int at, const float (&v)[8]) {
-  Group<uint16_t, 8> hi, lo;
+  Elements<uint16_t, 8> hi, lo;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     if constexpr (sizeof(T) == 4) {

@@ -236,10 +236,10 @@ enum Scale { kAsIs, kPerRow, kPerColumn, kOne };  // per row: found and left her
 template <typename T>
 struct Job {
   Source<T> from;
-  Laid to;
+  Laid to, also;  // also: the same once more, scaled per column (p null: not wanted)
   Scale scale;
 };
-constexpr int kMaxJobs = 4;
+constexpr int kMaxJobs = 3;
 template <typename T>
 struct Jobs {
   Job<T> job[kMaxJobs];
@@ -302,13 +302,21 @@ __global__ __launch_bounds__(256) void lay_kernel(Jobs<T> jobs) {
   } else if (j.scale == kOne) {
     e = *j.to.exps;
   }
+  auto by_columns = [&](const Laid& to, int at, const float (&v)[8]) __attribute__((always_inline)) {
+    const Elements<int, 8> exps = fetch<int, 8>(to.exps + at, j.from.cols - at);
+    float o[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] = ldexpf(v[i], exps.v[i]);
+    put8<T>(to, row, at, o);
+  };
   auto put = [&](int p, float (&v)[8]) __attribute__((always_inline)) {
     const int at = p * 512 + lane_id() * 8;
     if (at >= j.to.padded) return;
+    if (j.scale == kPerColumn) return by_columns(j.to, at, v);
+    if (j.also.p) by_columns(j.also, at, v);
+    if (j.scale != kAsIs) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if (j.scale == kPerColumn) v[i] = at + i < j.from.cols ? ldexpf(v[i], j.to.exps[at + i]) : 0.0f;
-      else if (j.scale != kAsIs) v[i] = ldexpf(v[i], e);
+      for (int i = 0; i < 8; ++i) v[i] = ldexpf(v[i], e);
     }
     put8<T>(j.to, row, at, v);
   };
@@ -388,14 +396,15 @@ __global__ __launch_bounds__(256) void columns_kernel(ColumnJobs<T> jobs) {
 }
 // 32 columns per workgroup; for one scale of all columns a last workgroup goes through all partial results.
 template <typename T>
-__global__ __launch_bounds__(256) void columns_sum_kernel(ColumnJobs<T> jobs, int parts) {
+__global__ __launch_bounds__(256) void columns_sum_kernel(ColumnJobs<T> jobs) {
   const ColumnJob<T>& j = jobs.job[blockIdx.y];
   __shared__ float sums[8][33], tops[8][33];
   const int lane = threadIdx.x & 31, group = threadIdx.x >> 5, cols = j.from.cols;
   if (blockIdx.x + 1 == gridDim.x) {
     if (!j.one) return;
     float top = 0.0f;
-    for (int64_t i = threadIdx.x; i < (int64_t)parts * cols; i += 256) top = fmaxf(top, j.largest[i]);
+#pragma unroll 8
+    for (int i = threadIdx.x; i < cols * kColumnParts; i += 256) top = fmaxf(top, j.largest[i]);
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
     if (lane_id() == 0) tops[0][wave_id()] = top;
@@ -406,11 +415,14 @@ __global__ __launch_bounds__(256) void columns_sum_kernel(ColumnJobs<T> jobs, in
   const int c = blockIdx.x * 32 + lane;
   if ((int)blockIdx.x * 32 >= cols) return;
   float s = 0.0f, top = 0.0f;
-  if (c < cols)
-    for (int p = group; p < parts; p += 8) {
-      if (j.total) s += j.sums[(int64_t)p * cols + c];
-      if (j.largest) top = fmaxf(top, j.largest[(int64_t)p * cols + c]);
-    }
+  if (c < cols) {
+    if (j.total)
+#pragma unroll
+      for (int p = 0; p < kColumnParts; p += 8) s += j.sums[(int64_t)(p + group) * cols + c];
+    if (j.exps && !j.one)
+#pragma unroll
+      for (int p = 0; p < kColumnParts; p += 8) top = fmaxf(top, j.largest[(int64_t)(p + group) * cols + c]);
+  }
   sums[group][lane] = s;
   tops[group][lane] = top;
   __syncthreads();
@@ -501,8 +513,8 @@ bool in_place(const Source<T>& m) {
   return sizeof(T) == 2 && !m.pre && m.cols % 8 == 0 && m.ld % 8 == 0 && (reinterpret_cast<uintptr_t>(m.p) & 15) == 0;
 }
 template <typename T>
-void add_job(Jobs<T>& jobs, const Source<T>& from, const Laid& to, Scale scale) {
-  jobs.job[jobs.count] = {from, to, scale};
+void add_job(Jobs<T>& jobs, const Source<T>& from, const Laid& to, Scale scale, const Laid& also = Laid{}) {
+  jobs.job[jobs.count] = {from, to, also, scale};
   jobs.first[jobs.count + 1] = jobs.first[jobs.count] + (int)div_up(from.rows, 4);
   ++jobs.count;
 }
@@ -554,6 +566,7 @@ hipError_t linear_few(const LinearArgs& a, const LinearStore<T>& out, hipStream_
 //   128 (two): 10 + a tile 4 + 0.55 per stage, and a last round that is not full counts half as one
 //   64 (three): 6.5 + a tile 0.9 + 0.2 per stage, alone 5.5 + 0.32 per stage
 //   64 with four groups (one): 2 + a round 3.4 + 0.17 per stage
+//   32 with eight groups (one): 0.5 + a round 3.7 + 0.085 per stage (64 x 1024 x 1024 5.3 against 8.0, 512^3 4.9 against 6.6)
 // Numbers of two halves take half of a stage's steps, and 1.15 to 1.3 times its time.  A contraction split among workgroups
 // costs a second launch of 6 us and the partial results twice through memory at 3 TB/s.
 ProductPlan plan_product(int64_t M, int64_t N, int64_t k, int planes, int64_t batch, bool lower) {
@@ -567,12 +580,13 @@ ProductPlan plan_product(int64_t M, int64_t N, int64_t k, int planes, int64_t ba
     p.tile = tile;
     p.groups = groups;
     // (a whole number of stages for each group)
-    p.tiles_per_split = (int)(splits == 1 ? stages : div_up(stages, 4 * splits) * 4);
+    p.tiles_per_split = (int)(splits == 1 ? stages : div_up(stages, groups * splits) * groups);
     p.splits = (int)div_up(stages, p.tiles_per_split);
     const double load = (double)tiles * p.splits / 256.0, rounds = (double)div_up(tiles * p.splits, 256), s = p.tiles_per_split;
     double us;
     if (tile == 256) us = rounds * (24.0 + 1.3 * s);
     else if (tile == 128) us = 10.0 + 0.5 * (rounds + load) * (4.0 + (planes == 1 ? 0.55 : 0.68) * s);
+    else if (tile == 32) us = 0.5 + rounds * (3.7 + (planes == 1 ? 0.085 : 0.1) * s);
     else if (groups == 4) us = 2.0 + rounds * (3.4 + (planes == 1 ? 0.17 : 0.22) * s);
     else us = fmax(5.5 + (planes == 1 ? 0.32 : 0.4) * s, 6.5 + load * (0.9 + (planes == 1 ? 0.2 : 0.23) * s));
     if (p.splits > 1) {
@@ -589,6 +603,7 @@ ProductPlan plan_product(int64_t M, int64_t N, int64_t k, int planes, int64_t ba
     consider(128, 1, splits);
     consider(64, 1, splits);
     if (stages >= 4) consider(64, 4, splits);
+    consider(32, 8, splits);
   }
   return best;
 }
@@ -647,14 +662,14 @@ hipError_t launch_linear_grad(const LinearGradArgs& a, hipStream_t s) {
     if (count) {
       columns_kernel<T><<<dim3((unsigned)div_up(widest, 32 * kPer16<T>), kColumnParts, (unsigned)count), dim3(256), 0, s>>>(columns);
       if ((e = hipGetLastError()) != hipSuccess) return e;
-      columns_sum_kernel<T><<<dim3((unsigned)div_up(widest, 32) + 1, (unsigned)count), dim3(256), 0, s>>>(columns, kColumnParts);
+      columns_sum_kernel<T><<<dim3((unsigned)div_up(widest, 32) + 1, (unsigned)count), dim3(256), 0, s>>>(columns);
       if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     Jobs<T> jobs{};
     if (d_laid && scaled) {
       if (!kFloat) add_job(jobs, d, room.d, kOne);
-      else if (a.dx) add_job(jobs, d, room.d, kPerRow);
-      if (kFloat && a.dW) add_job(jobs, d, room.d_columns, kPerColumn);
+      else if (a.dx) add_job(jobs, d, room.d, kPerRow, a.dW ? room.d_columns : Laid{});
+      else add_job(jobs, d, room.d_columns, kPerColumn);
     }
     if (a.dx && !in_place(W)) add_job(jobs, W, room.W, kFloat ? kPerColumn : kAsIs);
     if (a.dW && !in_place(x)) add_job(jobs, x, room.x, kFloat ? kPerColumn : kAsIs);

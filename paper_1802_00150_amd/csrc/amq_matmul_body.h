@@ -94,11 +94,12 @@ __device__ __forceinline__ int column_of(int lane) {
 template <int KW, int KG, typename Epi>
 __device__ __forceinline__ void finish_subtile(const float* t, int apart, int share, const Epi& epi, const typename Epi::Column& column, int z, int m0,
                                                int n0, bool mirror, int lane) {
-  constexpr int kStride = KW + 4, kPerRow = KW / 4, kCalls = 32 * kPerRow / 64 / KG, kAhead = kCalls < 4 ? kCalls : 4;
-  static_assert(64 % kPerRow == 0 && kCalls * KG * 64 == 32 * kPerRow, "whole rows");
+  constexpr int kStride = KW + 4, kPerRow = KW / 4, kAll = 32 * kPerRow / 64;  // calls of a whole wave
+  constexpr int kCalls = kAll > KG ? kAll / KG : 1, kAhead = kCalls < 4 ? kCalls : 4;
+  static_assert(64 % kPerRow == 0 && (kAll % KG == 0 || KG % kAll == 0), "whole rows");
   const int col = column_of<KW>(lane);
 #pragma unroll 1
-  for (int c = 0; c < kCalls; c += kAhead) {
+  for (int c = 0; c < kCalls && (KG <= kAll || share < kAll); c += kAhead) {
     typename Epi::Extra extra[kAhead];
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) extra[u] = epi.fetch(z, m0 + (((c + u) * KG + share) * 64 + lane) / kPerRow, n0 + col);
@@ -174,6 +175,7 @@ struct Side {
 
   static __device__ __forceinline__ int swizzle(int row) {  // of 16-byte pieces
     if (!COLUMNS) return (row >> 1) & 7;
+    if (kLine == 64) return ((row >> 3) & 1) << 1;
     if (kLine == 128) return (((row >> 1) & 1) | ((row >> 2) & 2)) << 1;
     return ((row & 3) | ((row >> 1) & 4)) << 1;
   }
@@ -441,7 +443,7 @@ inline int stage_of(int planes) { return planes == 1 ? 64 : 32; }  // values of 
 
 struct ProductPlan {
   int tile;             // of the result: tile x tile values per workgroup
-  int groups;           // of waves that share a workgroup's stages (tile 64)
+  int groups;           // of waves that share a workgroup's stages (tile 32 and 64)
   int splits, tiles_per_split;
   size_t part_bytes;    // of partial results (splits > 1)
 };
@@ -465,6 +467,7 @@ hipError_t launch_product(const MatmulArgs& g, const ProductPlan& p, int batch, 
     if constexpr (NP == 1)
       if (p.tile == 256) return launch_tiles<E, NP, RC, CC, 256, 256, 2, 4, 1, 2>(g, p, batch, store, s);
     if (p.tile == 128) return launch_tiles<E, NP, RC, CC, 128, 128, 2, 2, 1, 2>(g, p, batch, store, s);
+    if (p.tile == 32) return launch_tiles<E, NP, RC, CC, 32, 32, 1, 1, 8, 2>(g, p, batch, store, s);
     if (p.groups == 4) return launch_tiles<E, NP, RC, CC, 64, 64, 2, 2, 4, 2>(g, p, batch, store, s);
     return launch_tiles<E, NP, RC, CC, 64, 64, 2, 2, 1, 3>(g, p, batch, store, s);
   };

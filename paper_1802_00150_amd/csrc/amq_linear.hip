@@ -564,6 +564,7 @@ hipError_t linear_few(const LinearArgs& a, const LinearStore<T>& out, hipStream_
 // 205 / 260, 2240 x 1024 x 1024 41 / 23 / 15 / 22, 1024 x 1024 x 2240 61 / 33 / 18 / 13, 300 x 300 x 1216 43 / 23 / 12 / 9.
 //   256 (one workgroup per unit): a round 24 + 1.3 per stage
 //   128 (two): 10 + a tile 4 + 0.55 per stage, and a last round that is not full counts half as one
+//   128 with two groups (one): 2 + a round 7.5 + 0.47 per stage (2048^3 24.6 against 29.7, 1024 x 4096 x 8960 75 against 88)
 //   64 (three): 6.5 + a tile 0.9 + 0.2 per stage, alone 5.5 + 0.32 per stage
 //   64 with four groups (one): 2 + a round 3.4 + 0.17 per stage
 //   32 with eight groups (one): 0.5 + a round 3.7 + 0.085 per stage (64 x 1024 x 1024 5.3 against 8.0, 512^3 4.9 against 6.6)
@@ -585,6 +586,7 @@ ProductPlan plan_product(int64_t M, int64_t N, int64_t k, int planes, int64_t ba
     const double load = (double)tiles * p.splits / 256.0, rounds = (double)div_up(tiles * p.splits, 256), s = p.tiles_per_split;
     double us;
     if (tile == 256) us = rounds * (24.0 + 1.3 * s);
+    else if (tile == 128 && groups == 2) us = 2.0 + rounds * (7.5 + (planes == 1 ? 0.47 : 0.65) * s);
     else if (tile == 128) us = 10.0 + 0.5 * (rounds + load) * (4.0 + (planes == 1 ? 0.55 : 0.68) * s);
     else if (tile == 32) us = 0.5 + rounds * (3.7 + (planes == 1 ? 0.085 : 0.1) * s);
     else if (groups == 4) us = 2.0 + rounds * (3.4 + (planes == 1 ? 0.17 : 0.22) * s);
@@ -601,6 +603,7 @@ ProductPlan plan_product(int64_t M, int64_t N, int64_t k, int planes, int64_t ba
   if (planes == 1) consider(256, 1, 1);
   for (int64_t splits = 1; splits <= 32 && (splits == 1 || stages >= 16 * splits); splits *= 2) {
     consider(128, 1, splits);
+    if (stages >= 4) consider(128, 2, splits);
     consider(64, 1, splits);
     if (stages >= 4) consider(64, 4, splits);
     consider(32, 8, splits);

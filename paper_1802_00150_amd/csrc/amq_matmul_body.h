@@ -443,7 +443,7 @@ inline int stage_of(int planes) { return planes == 1 ? 64 : 32; }  // values of 
 
 struct ProductPlan {
   int tile;             // of the result: tile x tile values per workgroup
-  int groups;           // of waves that share a workgroup's stages (tile 32 and 64)
+  int groups;           // of waves that share a workgroup's stages
   int splits, tiles_per_split;
   size_t part_bytes;    // of partial results (splits > 1)
 };
@@ -466,6 +466,7 @@ hipError_t launch_product(const MatmulArgs& g, const ProductPlan& p, int batch, 
   auto run = [&](const auto& store) {
     if constexpr (NP == 1)
       if (p.tile == 256) return launch_tiles<E, NP, RC, CC, 256, 256, 2, 4, 1, 2>(g, p, batch, store, s);
+    if (p.tile == 128 && p.groups == 2) return launch_tiles<E, NP, RC, CC, 128, 128, 2, 2, 2, 2>(g, p, batch, store, s);
     if (p.tile == 128) return launch_tiles<E, NP, RC, CC, 128, 128, 2, 2, 1, 2>(g, p, batch, store, s);
     if (p.tile == 32) return launch_tiles<E, NP, RC, CC, 32, 32, 1, 1, 8, 2>(g, p, batch, store, s);
     if (p.groups == 4) return launch_tiles<E, NP, RC, CC, 64, 64, 2, 2, 4, 2>(g, p, batch, store, s);

@@ -269,11 +269,11 @@ __device__ __forceinline__ void put8(const Laid& to, int64_t row, int at, const 
 
 // One wave per row.  Rows of up to 4096 values stay in registers between the search for the scale and the output.
 template <typename T>
-__global__ __launch_bounds__(256) void lay_kernel(Jobs<T> jobs) {
+__device__ __forceinline__ void lay(const Jobs<T>& jobs, int block) {
   int k = 0;
-  while (k + 1 < jobs.count && (int)blockIdx.x >= jobs.first[k + 1]) ++k;
+  while (k + 1 < jobs.count && block >= jobs.first[k + 1]) ++k;
   const Job<T>& j = jobs.job[k];
-  const int64_t row = (int64_t)(blockIdx.x - jobs.first[k]) * 4 + wave_id();
+  const int64_t row = (int64_t)(block - jobs.first[k]) * 4 + wave_id();
   if (row >= j.to.rows) return;
   constexpr int kHeld = 8;
   float held[kHeld][8];
@@ -330,13 +330,20 @@ __global__ __launch_bounds__(256) void lay_kernel(Jobs<T> jobs) {
   }
 }
 
+template <typename T>
+__global__ __launch_bounds__(256) void lay_kernel(Jobs<T> jobs) {
+  lay(jobs, blockIdx.x);
+}
+
 // ---- columns: sums and largest values, and on the way d itself where it needs no scale.  A workgroup takes 32 groups of V
-// columns and every 8 * gridDim.y-th row of them; what it finds are partial results, which a second launch puts together.
+// columns and every 8 * parts-th row of them; what it finds are partial results, which a second launch puts together.  Of at
+// most 128 rows one part is all (16 rows per thread; a launch costs more).
 constexpr int kColumnParts = 64;
+int column_parts(int64_t rows) { return rows <= 128 ? 1 : kColumnParts; }
 template <typename T>
 struct ColumnJob {
   Source<T> from;
-  float *sums, *largest;  // [gridDim.y][cols], or null
+  float *sums, *largest;  // [parts][cols], or null
   Laid to;                // p null: not wanted
   T* total;               // [cols]: the sums, or null
   int* exps;              // scales per column, or one, or null
@@ -345,23 +352,29 @@ struct ColumnJob {
 template <typename T>
 struct ColumnJobs {
   ColumnJob<T> job[3];
+  int blocks;  // workgroups per part
+  int parts, count;
 };
+// The column jobs, and behind them what is to be laid out and does not depend on them.
 template <typename T>
-__global__ __launch_bounds__(256) void columns_kernel(ColumnJobs<T> jobs) {
+__global__ __launch_bounds__(256) void columns_kernel(ColumnJobs<T> jobs, Jobs<T> beside) {
+  const int own = jobs.blocks * jobs.parts * jobs.count;
+  if ((int)blockIdx.x >= own) return lay(beside, blockIdx.x - own);
   constexpr int V = kPer16<T>;
   __shared__ float part[2][8][32 * V + 4];
-  const ColumnJob<T>& j = jobs.job[blockIdx.z];
-  const int lane = threadIdx.x & 31, group = threadIdx.x >> 5, c = (blockIdx.x * 32 + lane) * V;
+  const int block = blockIdx.x % jobs.blocks, part_of = blockIdx.x / jobs.blocks % jobs.parts;
+  const ColumnJob<T>& j = jobs.job[blockIdx.x / (jobs.blocks * jobs.parts)];
+  const int lane = threadIdx.x & 31, group = threadIdx.x >> 5, c = (block * 32 + lane) * V;
   const int width = j.to.p ? j.to.padded : j.from.cols;
-  if ((int)blockIdx.x * 32 * V >= width) return;
+  if (block * 32 * V >= width) return;
   float s[V], largest[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) s[i] = largest[i] = 0.0f;
   // four rows at a time, so that their loads are under way together
   constexpr int kBatch = 4;
-  const int64_t step = 8 * gridDim.y;
+  const int64_t step = 8 * jobs.parts;
   if (c < width)
-    for (int64_t row0 = blockIdx.y * 8 + group; row0 < j.from.rows; row0 += kBatch * step) {
+    for (int64_t row0 = part_of * 8 + group; row0 < j.from.rows; row0 += kBatch * step) {
       float v[kBatch][V];
       j.from.template load_rows<V, kBatch>(row0, step, c, v);
 #pragma unroll
@@ -382,7 +395,7 @@ __global__ __launch_bounds__(256) void columns_kernel(ColumnJobs<T> jobs) {
   }
   __syncthreads();
   for (int i = threadIdx.x; i < 32 * V; i += 256) {
-    const int at = blockIdx.x * 32 * V + i;
+    const int at = block * 32 * V + i;
     if (at >= j.from.cols) continue;
     float sum = 0.0f, top = 0.0f;
 #pragma unroll
@@ -390,11 +403,17 @@ __global__ __launch_bounds__(256) void columns_kernel(ColumnJobs<T> jobs) {
       sum += part[0][q][i];
       top = fmaxf(top, part[1][q][i]);
     }
-    if (j.sums) j.sums[(int64_t)blockIdx.y * j.from.cols + at] = sum;
-    if (j.largest) j.largest[(int64_t)blockIdx.y * j.from.cols + at] = top;
+    if (jobs.parts == 1) {
+      if (j.total) j.total[at] = (T)sum;
+      if (j.exps && !j.one) j.exps[at] = scale_exponent(top);
+    } else if (j.sums) {
+      j.sums[(int64_t)part_of * j.from.cols + at] = sum;
+    }
+    if (j.largest && (jobs.parts > 1 || j.one)) j.largest[(int64_t)part_of * j.from.cols + at] = top;
   }
 }
-// 32 columns per workgroup; for one scale of all columns a last workgroup goes through all partial results.
+// 32 columns per workgroup; for one scale of all columns a last workgroup goes through all partial results.  (kColumnParts
+// parts, or one, of which only that scale is to be found.)
 template <typename T>
 __global__ __launch_bounds__(256) void columns_sum_kernel(ColumnJobs<T> jobs) {
   const ColumnJob<T>& j = jobs.job[blockIdx.y];
@@ -404,7 +423,7 @@ __global__ __launch_bounds__(256) void columns_sum_kernel(ColumnJobs<T> jobs) {
     if (!j.one) return;
     float top = 0.0f;
 #pragma unroll 8
-    for (int i = threadIdx.x; i < cols * kColumnParts; i += 256) top = fmaxf(top, j.largest[i]);
+    for (int64_t i = threadIdx.x; i < (int64_t)cols * jobs.parts; i += 256) top = fmaxf(top, j.largest[i]);
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
     if (lane_id() == 0) tops[0][wave_id()] = top;
@@ -413,7 +432,7 @@ __global__ __launch_bounds__(256) void columns_sum_kernel(ColumnJobs<T> jobs) {
     return;
   }
   const int c = blockIdx.x * 32 + lane;
-  if ((int)blockIdx.x * 32 >= cols) return;
+  if ((int)blockIdx.x * 32 >= cols || jobs.parts == 1) return;
   float s = 0.0f, top = 0.0f;
   if (c < cols) {
     if (j.total)
@@ -662,12 +681,6 @@ hipError_t launch_linear_grad(const LinearGradArgs& a, hipStream_t s) {
                   d_scales ? room.d_columns.exps : nullptr, d_scales && !kFloat});
     if (kFloat && a.dW) column_job({x, nullptr, room.tops[1], Laid{}, nullptr, room.x.exps, false});
     if (kFloat && a.dx) column_job({W, nullptr, room.tops[2], Laid{}, nullptr, room.W.exps, false});
-    if (count) {
-      columns_kernel<T><<<dim3((unsigned)div_up(widest, 32 * kPer16<T>), kColumnParts, (unsigned)count), dim3(256), 0, s>>>(columns);
-      if ((e = hipGetLastError()) != hipSuccess) return e;
-      columns_sum_kernel<T><<<dim3((unsigned)div_up(widest, 32) + 1, (unsigned)count), dim3(256), 0, s>>>(columns);
-      if ((e = hipGetLastError()) != hipSuccess) return e;
-    }
     Jobs<T> jobs{};
     if (d_laid && scaled) {
       if (!kFloat) add_job(jobs, d, room.d, kOne);
@@ -676,7 +689,20 @@ hipError_t launch_linear_grad(const LinearGradArgs& a, hipStream_t s) {
     }
     if (a.dx && !in_place(W)) add_job(jobs, W, room.W, kFloat ? kPerColumn : kAsIs);
     if (a.dW && !in_place(x)) add_job(jobs, x, room.x, kFloat ? kPerColumn : kAsIs);
-    if ((e = run_jobs(jobs, s)) != hipSuccess) return e;
+    if (count) {
+      const int64_t longest = kFloat && a.dx && a.n > a.rows ? a.n : a.rows;
+      columns.parts = column_parts(longest);
+      columns.count = count;
+      columns.blocks = (int)div_up(widest, 32 * kPer16<T>);
+      const Jobs<T> beside = scaled ? Jobs<T>{} : jobs;
+      columns_kernel<T><<<dim3((unsigned)(columns.blocks * columns.parts * count + beside.first[beside.count])), dim3(256), 0, s>>>(columns, beside);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+      if (columns.parts > 1 ? a.dbias || scaled : !kFloat && d_scales) {
+        columns_sum_kernel<T><<<dim3((unsigned)div_up(widest, 32) + 1, (unsigned)count), dim3(256), 0, s>>>(columns);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+      }
+    }
+    if ((!count || scaled) && (e = run_jobs(jobs, s)) != hipSuccess) return e;
     LinearStore<T> out{};
     out.act = AMQ_ACT_NONE;
     if (!kFloat && scaled) out.exp_all = room.d.exps;

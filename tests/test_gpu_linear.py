@@ -141,9 +141,10 @@ def test_any_subset_of_the_gradients(amq):
             assert got[j] is None or torch.equal(got[j], full[j])
 
 
-def test_rows_of_unlike_scale(amq):
-    """Float rows 2^60 apart, entries 2^24 apart within one, rows of zeros, subnormal rows: the scale is each row's own."""
-    rows, k, n = 40, 96, 72
+@pytest.mark.parametrize("rows,k,n", [(40, 96, 72), (1200, 640, 1300)])
+def test_rows_of_unlike_scale(amq, rows, k, n):
+    """Float rows 2^60 apart, entries 2^24 apart within one, rows of zeros, subnormal rows: the scale is each row's own.
+    (Few numbers are multiplied in binary32, many as split ones.)"""
     x, W = rand(4, rows, k), rand(5, n, k)
     x *= 2.0 ** (torch.arange(rows) % 7 * 20 - 60)[:, None]
     x[:, ::3] *= 2.0 ** -24

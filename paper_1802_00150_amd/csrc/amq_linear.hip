@@ -551,14 +551,19 @@ MatmulOperand operand(const Source<T>& m, bool columns) {
 }
 MatmulOperand operand(const Laid& l, bool columns) { return {l.p, l.ld, 0, columns ? l.padded : l.rows}; }
 
-template <typename T, bool RC, bool CC>
-hipError_t product(const MatmulOperand& r, const MatmulOperand& c, int64_t k, const LinearStore<T>& out, float* part, hipStream_t s) {
+template <typename T>
+MatmulArgs product_args(const MatmulOperand& r, const MatmulOperand& c, int64_t k, const LinearStore<T>& out) {
   MatmulArgs g{};
   g.r = r;
   g.c = c;
   g.M = out.M;
   g.N = out.N;
   g.k = (int)k;
+  return g;
+}
+template <typename T, bool RC, bool CC>
+hipError_t product(const MatmulArgs& g, const LinearStore<T>& out, float* part, hipStream_t s) {
+  const int64_t k = g.k;
   const ProductPlan p = plan_product(out.M, out.N, k, sizeof(T) == 4 ? 2 : 1, 1, false);
   if constexpr (sizeof(T) == 4) return launch_product<f16, 2, RC, CC>(g, p, 1, out, part, s);
   else return launch_product<T, 1, RC, CC>(g, p, 1, out, part, s);
@@ -589,10 +594,19 @@ hipError_t linear_few(const LinearArgs& a, const LinearStore<T>& out, hipStream_
 //   32 with eight groups (one): 0.5 + a round 3.7 + 0.085 per stage (64 x 1024 x 1024 5.3 against 8.0, 512^3 4.9 against 6.6)
 // Numbers of two halves take half of a stage's steps, and 1.15 to 1.3 times its time.  A contraction split among workgroups
 // costs a second launch of 6 us and the partial results twice through memory at 3 TB/s.
+static double form_us(int tile, int groups, int planes, int64_t tiles, double s) {
+  const double load = (double)tiles / 256.0, rounds = (double)div_up(tiles, 256);
+  if (tile == 256) return rounds * (24.0 + 1.3 * s);
+  if (tile == 128 && groups == 2) return 2.0 + rounds * (7.5 + (planes == 1 ? 0.47 : 0.65) * s);
+  if (tile == 128) return 10.0 + 0.5 * (rounds + load) * (4.0 + (planes == 1 ? 0.55 : 0.68) * s);
+  if (tile == 32) return 0.5 + rounds * (3.7 + (planes == 1 ? 0.085 : 0.1) * s);
+  if (groups == 4) return 2.0 + rounds * (3.4 + (planes == 1 ? 0.17 : 0.22) * s);
+  return fmax(5.5 + (planes == 1 ? 0.32 : 0.4) * s, 6.5 + load * (0.9 + (planes == 1 ? 0.2 : 0.23) * s));
+}
+
 ProductPlan plan_product(int64_t M, int64_t N, int64_t k, int planes, int64_t batch, bool lower) {
   const int64_t stages = div_up(k, stage_of(planes));
   ProductPlan best{};
-  double least = 1e300;
   auto consider = [&](int tile, int groups, int64_t splits) {
     const int64_t a = div_up(M, tile), b = div_up(N, tile);
     const int64_t tiles = batch * (lower ? a * (a + 1) / 2 : a * b);
@@ -602,22 +616,12 @@ ProductPlan plan_product(int64_t M, int64_t N, int64_t k, int planes, int64_t ba
     // (a whole number of stages for each group)
     p.tiles_per_split = (int)(splits == 1 ? stages : div_up(stages, groups * splits) * groups);
     p.splits = (int)div_up(stages, p.tiles_per_split);
-    const double load = (double)tiles * p.splits / 256.0, rounds = (double)div_up(tiles * p.splits, 256), s = p.tiles_per_split;
-    double us;
-    if (tile == 256) us = rounds * (24.0 + 1.3 * s);
-    else if (tile == 128 && groups == 2) us = 2.0 + rounds * (7.5 + (planes == 1 ? 0.47 : 0.65) * s);
-    else if (tile == 128) us = 10.0 + 0.5 * (rounds + load) * (4.0 + (planes == 1 ? 0.55 : 0.68) * s);
-    else if (tile == 32) us = 0.5 + rounds * (3.7 + (planes == 1 ? 0.085 : 0.1) * s);
-    else if (groups == 4) us = 2.0 + rounds * (3.4 + (planes == 1 ? 0.17 : 0.22) * s);
-    else us = fmax(5.5 + (planes == 1 ? 0.32 : 0.4) * s, 6.5 + load * (0.9 + (planes == 1 ? 0.2 : 0.23) * s));
+    p.us = form_us(tile, groups, planes, tiles * p.splits, p.tiles_per_split);
     if (p.splits > 1) {
       p.part_bytes = sizeof(float) * (size_t)batch * p.splits * M * ((N + 3) & ~int64_t(3));
-      us += 6.0 + 2.0 * (double)p.part_bytes / 3e6;
+      p.us += 6.0 + 2.0 * (double)p.part_bytes / 3e6;
     }
-    if (us < least) {
-      least = us;
-      best = p;
-    }
+    if (best.tile == 0 || p.us < best.us) best = p;
   };
   if (planes == 1) consider(256, 1, 1);
   for (int64_t splits = 1; splits <= 32 && (splits == 1 || stages >= 16 * splits); splits *= 2) {
@@ -626,6 +630,26 @@ ProductPlan plan_product(int64_t M, int64_t N, int64_t k, int planes, int64_t ba
     consider(64, 1, splits);
     if (stages >= 4) consider(64, 4, splits);
     consider(32, 8, splits);
+  }
+  return best;
+}
+
+ProductPlan plan_pair(int64_t M, int64_t N, int64_t k, int64_t M2, int64_t N2, int64_t k2, int planes) {
+  const double s = (double)div_up(k, stage_of(planes)), s2 = (double)div_up(k2, stage_of(planes));
+  const struct {
+    int tile, groups;
+  } forms[] = {{128, 1}, {128, 2}, {64, 1}, {64, 4}, {32, 8}};
+  ProductPlan best{};
+  for (const auto& f : forms) {
+    const int64_t tiles = div_up(M, f.tile) * div_up(N, f.tile), tiles2 = div_up(M2, f.tile) * div_up(N2, f.tile), all = tiles + tiles2;
+    // one round takes as long as the longer of both, several as their mean
+    const double mean = (s * tiles + s2 * tiles2) / all, longest = s > s2 ? s : s2;
+    ProductPlan p{};
+    p.tile = f.tile;
+    p.groups = f.groups;
+    p.splits = 1;
+    p.us = fmax(form_us(f.tile, f.groups, planes, all, mean), form_us(f.tile, f.groups, planes, 256, longest));
+    if (best.tile == 0 || p.us < best.us) best = p;
   }
   return best;
 }
@@ -649,7 +673,8 @@ hipError_t launch_linear(const LinearArgs& a, hipStream_t s) {
       out.exp_r = room.x.exps;
       out.exp_c = room.W.exps;
     }
-    return product<T, false, false>(in_place(x) ? operand(x, false) : operand(room.x, false), in_place(W) ? operand(W, false) : operand(room.W, false), a.k,
+    return product<T, false, false>(product_args(in_place(x) ? operand(x, false) : operand(room.x, false),
+                                                 in_place(W) ? operand(W, false) : operand(room.W, false), a.k, out),
                                     out, room.part, s);
   });
 }
@@ -703,34 +728,37 @@ hipError_t launch_linear_grad(const LinearGradArgs& a, hipStream_t s) {
       }
     }
     if ((!count || scaled) && (e = run_jobs(jobs, s)) != hipSuccess) return e;
-    LinearStore<T> out{};
-    out.act = AMQ_ACT_NONE;
-    if (!kFloat && scaled) out.exp_all = room.d.exps;
-    if (a.dx) {
-      out.y = (T*)a.dx;
-      out.ld_y = a.ld_dx;
-      out.M = a.rows;
+    if (!products) return hipSuccess;
+    auto store_of = [&](void* y, int64_t ld, int M, const int* exp_r, const int* exp_c) {
+      LinearStore<T> out{};
+      out.act = AMQ_ACT_NONE;
+      out.y = (T*)y;
+      out.ld_y = ld;
+      out.M = M;
       out.N = a.k;
       if (kFloat) {
-        out.exp_r = room.d.exps;
-        out.exp_c = room.W.exps;
+        out.exp_r = exp_r;
+        out.exp_c = exp_c;
+      } else if (scaled) {
+        out.exp_all = room.d.exps;
       }
-      e = product<T, false, true>(d_laid ? operand(room.d, false) : operand(d, false), in_place(W) ? operand(W, true) : operand(room.W, true), a.n, out,
-                                  room.part, s);
-      if (e != hipSuccess) return e;
-    }
-    if (a.dW) {
-      out.y = (T*)a.dW;
-      out.ld_y = a.ld_dw;
-      out.M = a.n;
-      out.N = a.k;
-      if (kFloat) {
-        out.exp_r = room.d_columns.exps;
-        out.exp_c = room.x.exps;
+      return out;
+    };
+    const LinearStore<T> to_x = store_of(a.dx, a.ld_dx, a.rows, room.d.exps, room.W.exps);
+    const LinearStore<T> to_W = store_of(a.dW, a.ld_dw, a.n, room.d_columns.exps, room.x.exps);
+    const MatmulArgs for_x = product_args(d_laid ? operand(room.d, false) : operand(d, false), in_place(W) ? operand(W, true) : operand(room.W, true), a.n, to_x);
+    const MatmulArgs for_W = product_args(d_laid ? operand(room.d_columns, true) : operand(d, true), in_place(x) ? operand(x, true) : operand(room.x, true),
+                                          a.rows, to_W);
+    if (a.dx && a.dW) {
+      const int planes = planes_of(a.type);
+      const ProductPlan pair = plan_pair(a.rows, a.k, a.n, a.n, a.k, a.rows, planes);
+      if (pair.us < plan_product(a.rows, a.k, a.n, planes, 1, false).us + plan_product(a.n, a.k, a.rows, planes, 1, false).us) {
+        if constexpr (kFloat) return launch_pair<f16, 2>(for_x, to_x, for_W, to_W, pair, s);
+        else return launch_pair<T, 1>(for_x, to_x, for_W, to_W, pair, s);
       }
-      e = product<T, true, true>(d_laid ? operand(room.d_columns, true) : operand(d, true), in_place(x) ? operand(x, true) : operand(room.x, true), a.rows, out,
-                                 room.part, s);
     }
+    if (a.dx) e = product<T, false, true>(for_x, to_x, room.part, s);
+    if (e == hipSuccess && a.dW) e = product<T, true, true>(for_W, to_W, room.part, s);
     return e;
   });
 }

@@ -597,6 +597,7 @@ hipError_t linear_few(const LinearArgs& a, const LinearStore<T>& out, hipStream_
 static double form_us(int tile, int groups, int planes, int64_t tiles, double s) {
   const double load = (double)tiles / 256.0, rounds = (double)div_up(tiles, 256);
   if (tile == 256) return rounds * (24.0 + 1.3 * s);
+  if (tile == 192) return rounds * (16.0 + 1.07 * s);
   if (tile == 128 && groups == 2) return 2.0 + rounds * (7.5 + (planes == 1 ? 0.47 : 0.65) * s);
   if (tile == 128) return 10.0 + 0.5 * (rounds + load) * (4.0 + (planes == 1 ? 0.55 : 0.68) * s);
   if (tile == 32) return 0.5 + rounds * (3.7 + (planes == 1 ? 0.085 : 0.1) * s);
@@ -623,7 +624,10 @@ ProductPlan plan_product(int64_t M, int64_t N, int64_t k, int planes, int64_t ba
     }
     if (best.tile == 0 || p.us < best.us) best = p;
   };
-  if (planes == 1) consider(256, 1, 1);
+  if (planes == 1) {
+    consider(256, 1, 1);
+    consider(192, 1, 1);
+  }
   for (int64_t splits = 1; splits <= 32 && (splits == 1 || stages >= 16 * splits); splits *= 2) {
     consider(128, 1, splits);
     if (stages >= 4) consider(128, 2, splits);

@@ -94,18 +94,22 @@ __device__ __forceinline__ int column_of(int lane) {
 template <int KW, int KG, typename Epi>
 __device__ __forceinline__ void finish_subtile(const float* t, int apart, int share, const Epi& epi, const typename Epi::Column& column, int z, int m0,
                                                int n0, bool mirror, int lane) {
-  constexpr int kStride = KW + 4, kPerRow = KW / 4, kAll = 32 * kPerRow / 64;  // calls of a whole wave
+  constexpr int kStride = KW + 4, kPerRow = KW / 4, kRows = 64 / kPerRow, kAll = (32 + kRows - 1) / kRows;  // calls of a whole wave
+  constexpr bool kWhole = 64 % kPerRow == 0;  // else the last lanes are left out, and rows past the last
   constexpr int kCalls = kAll > KG ? kAll / KG : 1, kAhead = kCalls < 4 ? kCalls : 4;
-  static_assert(64 % kPerRow == 0 && (kAll % KG == 0 || KG % kAll == 0), "whole rows");
-  const int col = column_of<KW>(lane);
+  static_assert(kWhole ? kAll % KG == 0 || KG % kAll == 0 : KG == 1, "whole calls");
+  const int col = column_of<KW>(lane), line = lane / kPerRow;
+  auto row_of = [&](int call) __attribute__((always_inline)) { return call * kRows + line; };
+  auto counts = [&](int row) __attribute__((always_inline)) { return kWhole || (line < kRows && row < 32); };
 #pragma unroll 1
   for (int c = 0; c < kCalls && (KG <= kAll || share < kAll); c += kAhead) {
     typename Epi::Extra extra[kAhead];
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) extra[u] = epi.fetch(z, m0 + (((c + u) * KG + share) * 64 + lane) / kPerRow, n0 + col);
+    for (int u = 0; u < kAhead; ++u) extra[u] = epi.fetch(z, m0 + row_of((c + u) * KG + share), n0 + col);
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
-      const int row = (((c + u) * KG + share) * 64 + lane) / kPerRow;
+      const int row = row_of((c + u) * KG + share);
+      if (!counts(row)) continue;
       const float* q = t + row * kStride + col;
       f32x4 v = *reinterpret_cast<const f32x4*>(q);
 #pragma unroll
@@ -164,8 +168,10 @@ struct Side {
   // Rows of memory that the copies of a wave are apart.  Down columns every 16 rows have the same offsets within their rows, so
   // that one offset serves several copies (rows may end inside a tile and need one each).
   static constexpr int kApart = kWaves * 64 / kLanes;
-  static constexpr int kOffsets = COLUMNS ? (kApart >= 16 ? 1 : 16 / kApart) : kCopies;
-  static_assert(kApart >= 16 || 16 % kApart == 0, "copies and the order of pieces");
+  static constexpr bool kWhole = 64 % kLanes == 0;  // a copy has whole rows
+  static constexpr int kOffsets = COLUMNS && kWhole ? (kApart >= 16 ? 1 : 16 / kApart) : kCopies;
+  static_assert(!kWhole || kApart >= 16 || 16 % kApart == 0, "copies and the order of pieces");
+  static_assert(kWhole || kLine % 256 == 128, "order of pieces");
 
   const char* base;    // of the tile, uniform
   int64_t stage;       // bytes from one stage to the next
@@ -176,7 +182,8 @@ struct Side {
   static __device__ __forceinline__ int swizzle(int row) {  // of 16-byte pieces
     if (!COLUMNS) return (row >> 1) & 7;
     if (kLine == 64) return ((row >> 3) & 1) << 1;
-    if (kLine == 128) return (((row >> 1) & 1) | ((row >> 2) & 2)) << 1;
+    // (rows an odd multiple of 128 bytes apart: every other one begins in the other half of the banks)
+    if (kLine % 256 == 128) return (((row >> 1) & 1) | ((row >> 2) & 2)) << 1;
     return ((row & 3) | ((row >> 1) & 4)) << 1;
   }
   __device__ __forceinline__ Side(const MatmulOperand& o, int z, int first_row, int k_, int lane_, int wave_) : k(k_), lane(lane_), wave(wave_) {
@@ -191,7 +198,7 @@ struct Side {
     }
 #pragma unroll
     for (int j = 0; j < kOffsets; ++j) {
-      const int row = row_of(j), piece = (lane % kLanes) ^ swizzle(row);
+      const int row = row_of(j), piece = piece_of(j) ^ swizzle(row);
       if constexpr (COLUMNS) {
         // past the operand's last rows those again (their number is a multiple of 8)
         const int left = (o.rows - first_row) * NP - 8, at = piece * 8;
@@ -202,14 +209,18 @@ struct Side {
       }
     }
   }
-  __device__ __forceinline__ int row_of(int j) const { return (wave + j * kWaves) * (64 / kLanes) + lane / kLanes; }
+  // The lane's row of copy j in LDS, and its place there.
+  __device__ __forceinline__ int row_of(int j) const {
+    return kWhole ? (wave + j * kWaves) * (64 / kLanes) + lane / kLanes : ((wave + j * kWaves) * 64 + lane) / kLanes;
+  }
+  __device__ __forceinline__ int piece_of(int j) const { return kWhole ? lane % kLanes : ((wave + j * kWaves) * 64 + lane) % kLanes; }
   // Copy j of stage t.  Steps of k past the end are zeros (along rows: to the next multiple of 8 what lies there).
   __device__ __forceinline__ void copy(uint16_t* s, int t, int j) const {
     const char* from = base + t * stage + (COLUMNS ? j / kOffsets * (kOffsets * kApart) * line : 0);
     const uint32_t at = off[j % kOffsets];
     uint16_t* to = s + (wave + j * kWaves) * 512;
     if ((t + 1) * kSteps > k) {
-      const int piece = (lane % kLanes) ^ swizzle(row_of(j));
+      const int piece = piece_of(j) ^ swizzle(row_of(j));
       const int step = t * kSteps + (COLUMNS ? row_of(j) : (NP == 1 ? piece : piece & 3) * 8);
       copy_to_lds(step < k ? from + at : (const char*)&kZeros, to);
     } else {
@@ -226,7 +237,14 @@ struct Side {
       const int step = (lane >> 4) * 8 + ((lane & 15) >> 2);
       const int part = NP == 1 ? i : (i >> 1) * 4 + half * 2 + (i & 1);
       const uint32_t place = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint16_t*)s;
-      const uint32_t at = (place + (uint32_t)(step * kLine + ((row0 * NP / 8) ^ swizzle(step)) * 16 + (lane & 3) * 8)) ^ (uint32_t)(part * 32);
+      uint32_t at;
+      if constexpr (kWhole) {
+        at = (place + (uint32_t)(step * kLine + ((row0 * NP / 8) ^ swizzle(step)) * 16 + (lane & 3) * 8)) ^ (uint32_t)(part * 32);
+      } else {  // row0 is a multiple of 16 only: the order goes by 128 bytes
+        static_assert(NP == 1, "tiles of numbers of two halves are powers of two");
+        const int bytes = (row0 + i * 16) * 2;
+        at = ((place + (uint32_t)(step * kLine + swizzle(step) * 16 + (lane & 3) * 8)) ^ (uint32_t)(bytes & 127)) + (uint32_t)(bytes & ~127);
+      }
       const auto* q = (__attribute__((address_space(3))) const char*)(uintptr_t)at + (NP == 1 ? half * 32 * kLine : 0);
       const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)q);
       const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(q + 4 * kLine));
@@ -488,6 +506,8 @@ hipError_t launch_product(const MatmulArgs& g, const ProductPlan& p, int batch, 
   auto run = [&](const auto& store) {
     if constexpr (NP == 1)
       if (p.tile == 256) return launch_tiles<E, NP, RC, CC, 256, 256, 2, 4, 1, 2>(g, p, batch, store, s);
+    if constexpr (NP == 1)
+      if (p.tile == 192) return launch_tiles<E, NP, RC, CC, 192, 192, 2, 4, 1, 2>(g, p, batch, store, s);
     if (p.tile == 128 && p.groups == 2) return launch_tiles<E, NP, RC, CC, 128, 128, 2, 2, 2, 2>(g, p, batch, store, s);
     if (p.tile == 128) return launch_tiles<E, NP, RC, CC, 128, 128, 2, 2, 1, 2>(g, p, batch, store, s);
     if (p.tile == 32) return launch_tiles<E, NP, RC, CC, 32, 32, 1, 1, 8, 2>(g, p, batch, store, s);

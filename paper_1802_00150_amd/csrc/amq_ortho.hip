@@ -21,7 +21,7 @@ namespace amq {
 namespace {
 
 constexpr float kScale = 4096.0f, kInvScale = 1.0f / 4096.0f;
-constexpr int kNormParts = 256;
+constexpr int kNormParts = 1024;  // sums of squares per matrix: four workgroups of 256 per compute unit
 
 struct __attribute__((packed, aligned(8))) Half4 {
   f16 v[4];
@@ -143,13 +143,19 @@ __global__ __launch_bounds__(256) void ortho_norm_kernel(Gradient<T> G, double* 
   double s = 0.0;
   // pieces of 256 x V values of a row, dealt to the workgroups in turn
   const int64_t across = (G.cols + 256 * V - 1) / (256 * V), pieces = across * G.rows;
-  for (int64_t i = blockIdx.x; i < pieces; i += gridDim.x) {
-    const int64_t row = i / across;
-    const int col = ((int)(i % across) * 256 + (int)threadIdx.x) * V;
-    float v[V];
-    load16(p + row * G.ld + col, G.cols - col, v);
+  constexpr int kAhead = 4;  // pieces under way
+  for (int64_t i = blockIdx.x; i < pieces; i += (int64_t)kAhead * gridDim.x) {
+    float v[kAhead][V];
 #pragma unroll
-    for (int q = 0; q < V; ++q) s += (double)v[q] * (double)v[q];
+    for (int u = 0; u < kAhead; ++u) {
+      const int64_t at = i + (int64_t)u * gridDim.x, row = at / across;
+      const int col = ((int)(at % across) * 256 + (int)threadIdx.x) * V;
+      load16(p + row * G.ld + col, at < pieces ? G.cols - col : 0, v[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+      for (int q = 0; q < V; ++q) s += (double)v[u][q] * (double)v[u][q];
   }
   s = block_sum<4>(s, scratch);
   if (threadIdx.x == 0) parts[(int64_t)blockIdx.y * kNormParts + blockIdx.x] = s;
@@ -157,7 +163,8 @@ __global__ __launch_bounds__(256) void ortho_norm_kernel(Gradient<T> G, double* 
 
 // 1 / (|G| + eps) of matrix z from its partial sums, by a whole workgroup of 256.
 __device__ __forceinline__ float inverse_norm(const double* parts, int z, int count, float eps, double* scratch) {
-  const double s = (int)threadIdx.x < count ? parts[(int64_t)z * kNormParts + threadIdx.x] : 0.0;
+  double s = 0.0;
+  for (int i = threadIdx.x; i < count; i += 256) s += parts[(int64_t)z * kNormParts + i];
   return (float)(1.0 / (sqrt(block_sum<4>(s, scratch)) + (double)eps));
 }
 

@@ -1,0 +1,69 @@
+"""Products whose results fill the card with tiles of 192 and 256, in the three orders of their operands, against the formulas
+in binary64 (computed on the card: library products of binary64).
+
+Tolerances are those of the smaller products, per element: (terms + 16) U of the sum of magnitudes, a rounding of the result.
+"""
+import pytest
+import torch
+
+from train_util import DEV, U, half_ulp, rand, smallest
+
+pytestmark = pytest.mark.gpu
+HALVES = [torch.bfloat16, torch.float16]
+
+
+@pytest.fixture(scope="module")
+def amq():
+    import paper_1802_00150_amd as amq
+    return amq
+
+
+def operand(seed, rows, cols, dtype, scale=1.0):
+    return rand(seed, rows, cols, scale=scale).to(dtype).to(DEV)
+
+
+def check(got, a, b, dtype, terms, bias=None):
+    """got = a b (binary64) + bias"""
+    ref, size = a @ b, a.abs() @ b.abs()
+    if bias is not None:
+        ref, size = ref + bias, size + bias.abs()
+    tol = (terms + 16) * U * size + half_ulp(dtype) * ref.abs() * 1.01 + smallest(dtype)
+    assert got.dtype == dtype and got.shape == ref.shape
+    assert bool(((got.double() - ref).abs() <= tol).all())  # (NaN counts as off)
+
+
+# result M x N over k: 16 x 16 tiles of 192 with ragged ends, 16 x 16 of 256; k a multiple of neither 64 nor 8 too
+@pytest.mark.parametrize("M,N,k", [(3000, 3050, 1000), (3010, 2960, 1001), (4000, 4090, 600), (4096, 3900, 333)])
+@pytest.mark.parametrize("dtype", HALVES)
+def test_every_order_of_operands(amq, M, N, k, dtype):
+    x, W, bias = operand(1, M, k, dtype), operand(2, N, k, dtype, k ** -0.5), operand(3, 1, N, dtype)[0]
+    check(amq.linear(x, W, bias), x.double(), W.double().t().contiguous(), dtype, k, bias.double())
+    # dx = dy W: M x N over k features out
+    dy, W = operand(4, M, k, dtype), operand(5, k, N, dtype, k ** -0.5)
+    x = operand(6, M, N, dtype)
+    dx, dW, db = amq.linear_backward(dy, x, W, None, None, True, False, False)
+    assert dW is None and db is None
+    check(dx, dy.double(), W.double(), dtype, k)
+    # dW = dy^T x: M x N over k rows
+    dy, x = operand(7, k, M, dtype, k ** -0.5), operand(8, k, N, dtype)
+    W = operand(9, M, N, dtype)
+    dx, dW, db = amq.linear_backward(dy, x, W, None, None, False, True, False)
+    assert dx is None and db is None
+    check(dW, dy.double().t().contiguous(), x.double(), dtype, k)
+
+
+@pytest.mark.parametrize("rows,cols", [(3900, 4200), (4200, 3900), (5500, 5610)])
+def test_orthogonalized_updates(amq, rows, cols):
+    """Two steps: the symmetric products' lower tiles, the update, and the last one's result."""
+    a, b, c = 3.4445, -4.7750, 2.0315
+    G = rand(rows, rows, cols).to(torch.bfloat16).to(DEV)
+    got = amq.orthogonalize(G, steps=2)
+    X = G.double() if rows <= cols else G.double().t().contiguous()
+    X = X / X.norm()
+    for _ in range(2):
+        A = X @ X.t().contiguous()
+        X = a * X + (b * A + c * (A @ A)) @ X
+    ref = X if rows <= cols else X.t()
+    # iterates of 11 bits: 1.5e-3 over five steps, beside the rounding of the result
+    assert float((got.double() - ref).norm() / ref.norm()) <= 1.5e-3 + half_ulp(torch.bfloat16)
+    assert float((got.double() - ref).abs().max()) <= 0.02 * float(ref.abs().max())

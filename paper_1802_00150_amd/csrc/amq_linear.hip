@@ -247,6 +247,11 @@ struct Jobs {
   int count;
 };
 
+// Scales go by the largest finite value: an infinity or NaN spoils the results that it enters, and no others.
+__device__ __forceinline__ float magnitude(float v) {
+  const float a = fabsf(v);
+  return a < INFINITY ? a : 0.0f;
+}
 __device__ __forceinline__ int scale_exponent(float largest) { return largest > 0.0f ? 14 - ilogbf(largest) : 0; }
 // 8 values of a row as the products take them.
 template <typename T>
@@ -288,12 +293,12 @@ __device__ __forceinline__ void lay(const Jobs<T>& jobs, int block) {
     for (int p = 0; p < kHeld; ++p)
       if (p < pieces)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) largest = fmaxf(largest, fabsf(held[p][i]));
+        for (int i = 0; i < 8; ++i) largest = fmaxf(largest, magnitude(held[p][i]));
     for (int p = kHeld; p < pieces; ++p) {
       float v[8];
       j.from.template load<8>(row, p * 512 + lane_id() * 8, v);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) largest = fmaxf(largest, fabsf(v[i]));
+      for (int i = 0; i < 8; ++i) largest = fmaxf(largest, magnitude(v[i]));
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) largest = fmaxf(largest, __shfl_xor(largest, o, 64));
@@ -382,7 +387,7 @@ __global__ __launch_bounds__(256) void columns_kernel(ColumnJobs<T> jobs, Jobs<T
 #pragma unroll
         for (int i = 0; i < V; ++i) {
           s[i] += v[b][i];
-          largest[i] = fmaxf(largest[i], fabsf(v[b][i]));
+          largest[i] = fmaxf(largest[i], magnitude(v[b][i]));
         }
         if constexpr (V == 8)
           if (j.to.p && row0 + b * step < j.from.rows) put8<T>(j.to, row0 + b * step, c, v[b]);

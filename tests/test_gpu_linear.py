@@ -179,6 +179,42 @@ def test_small_half_gradients_keep_their_digits(amq):
     assert relative(dW, ref) <= norm_bound(torch.float16, 2) + smallest(torch.float16) / float(ref.square().mean().sqrt())
 
 
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_infinities_and_nan_stay_where_they_enter(amq, bad, dtype):
+    """One entry of x, of W and of dy: results that do not depend on it are those of a zero in its place, bit for bit; the
+    others are not finite."""
+    for rows, k, n in ((5, 70, 33), (150, 90, 130)):
+        x, W, b, dy = (t.to(DEV) for t in inputs(14, rows, k, n, dtype))
+        pre = amq.linear(x, W, b)
+
+        def with_entry(t, i, j, v):
+            t = t.clone()
+            t[i, j] = v
+            return t
+
+        def same_but(got, ref, spoiled):
+            assert torch.equal(got[~spoiled], ref[~spoiled]) and not torch.isfinite(got[spoiled]).any()
+
+        def line(t, row=None, col=None):
+            m = torch.zeros(t.shape, dtype=torch.bool, device=DEV)
+            m[(row if row is not None else slice(None), col if col is not None else slice(None))] = True
+            return m
+
+        y = [amq.linear(with_entry(x, 3, 7, v), W, b) for v in (bad, 0.0)]
+        same_but(*y, line(y[0], row=3))
+        y = [amq.linear(x, with_entry(W, 4, 6, v), b) for v in (bad, 0.0)]
+        same_but(*y, line(y[0], col=4))
+        for act in (None, "sigmoid"):
+            got, ref = (amq.linear_backward(with_entry(dy, 2, 5, v), x, W, pre, act) for v in (bad, 0.0))
+            same_but(got[0], ref[0], line(got[0], row=2))
+            same_but(got[1], ref[1], line(got[1], row=5))
+            assert torch.equal(got[2][:5], ref[2][:5]) and torch.equal(got[2][6:], ref[2][6:]) and not torch.isfinite(got[2][5])
+            got, ref = (amq.linear_backward(dy, with_entry(x, 3, 7, v), with_entry(W, 4, 6, v), pre, act) for v in (bad, 0.0))
+            same_but(got[0], ref[0], line(got[0], col=6))
+            same_but(got[1], ref[1], line(got[1], col=7))
+
+
 def test_workspaces_streams_and_repeats(amq):
     """The caller's workspace with anything in it; another stream; the same results every time."""
     for dtype in DTYPES:

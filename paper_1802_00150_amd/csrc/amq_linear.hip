@@ -188,7 +188,8 @@ __global__ __launch_bounds__(256) void linear_few_kernel(const T* x, int64_t ld_
 }
 
 // ---- laying operands out
-// One matrix as it lies in memory; with `pre`, times the slope of the activation there.
+// One matrix as it lies in memory; with `pre`, times the slope of the activation there.  (SLOPED: whether the launch has such a
+// matrix.  The activations' code, once per piece of a row, takes the time to fetch it even where it does not run.)
 template <typename T>
 struct Source {
   const T* p;
@@ -196,10 +197,10 @@ struct Source {
   const T* pre;
   int64_t ld_pre;
   int rows, cols, act;
-  template <int V>
+  template <bool SLOPED, int V>
   __device__ __forceinline__ void load(int64_t row, int col, float (&v)[V]) const {
     load_params<T, V>(p, row * ld + col, cols - col, 0.0f, v);
-    if (pre) {
+    if (SLOPED && pre) {
       float z[V];
       load_params<T, V>(pre, row * ld_pre + col, cols - col, 0.0f, z);
       slopes(z, act);
@@ -208,12 +209,12 @@ struct Source {
     }
   }
   // N rows `step` apart, zeros past the last.
-  template <int V, int N>
+  template <bool SLOPED, int V, int N>
   __device__ __forceinline__ void load_rows(int64_t row, int64_t step, int col, float (&v)[N][V]) const {
     float z[N][V];
 #pragma unroll
     for (int b = 0; b < N; ++b) load_params<T, V>(p, (row + b * step) * ld + col, row + b * step < rows ? cols - col : 0, 0.0f, v[b]);
-    if (!pre) return;
+    if (!SLOPED || !pre) return;
 #pragma unroll
     for (int b = 0; b < N; ++b) load_params<T, V>(pre, (row + b * step) * ld_pre + col, row + b * step < rows ? cols - col : 0, 0.0f, z[b]);
 #pragma unroll
@@ -232,7 +233,7 @@ struct Laid {
   int64_t ld;
   int rows, padded;
 };
-enum Scale { kAsIs, kPerRow, kPerColumn, kOne };  // per row: found and left here; the others are read
+enum Scale { kAsIs, kPerRow, kPerColumn, kOne };  // per row (found and left here) or column (read): float; as is, or by one that is read: 16 bits
 template <typename T>
 struct Job {
   Source<T> from;
@@ -273,21 +274,22 @@ __device__ __forceinline__ void put8(const Laid& to, int64_t row, int at, const 
 }
 
 // One wave per row.  Rows of up to 4096 values stay in registers between the search for the scale and the output.
-template <typename T>
+template <typename T, bool SLOPED>
 __device__ __forceinline__ void lay(const Jobs<T>& jobs, int block) {
   int k = 0;
   while (k + 1 < jobs.count && block >= jobs.first[k + 1]) ++k;
   const Job<T>& j = jobs.job[k];
   const int64_t row = (int64_t)(block - jobs.first[k]) * 4 + wave_id();
   if (row >= j.to.rows) return;
+  constexpr bool kFloat = sizeof(T) == 4;
   constexpr int kHeld = 8;
   float held[kHeld][8];
   const int pieces = (j.to.padded + 511) / 512;
 #pragma unroll
   for (int p = 0; p < kHeld; ++p)
-    if (p < pieces) j.from.template load<8>(row, p * 512 + lane_id() * 8, held[p]);  // zeros past the end
+    if (p < pieces) j.from.template load<SLOPED, 8>(row, p * 512 + lane_id() * 8, held[p]);  // zeros past the end
   int e = 0;
-  if (j.scale == kPerRow) {
+  if (kFloat && j.scale == kPerRow) {
     float largest = 0.0f;
 #pragma unroll
     for (int p = 0; p < kHeld; ++p)
@@ -296,7 +298,7 @@ __device__ __forceinline__ void lay(const Jobs<T>& jobs, int block) {
         for (int i = 0; i < 8; ++i) largest = fmaxf(largest, magnitude(held[p][i]));
     for (int p = kHeld; p < pieces; ++p) {
       float v[8];
-      j.from.template load<8>(row, p * 512 + lane_id() * 8, v);
+      j.from.template load<SLOPED, 8>(row, p * 512 + lane_id() * 8, v);
 #pragma unroll
       for (int i = 0; i < 8; ++i) largest = fmaxf(largest, magnitude(v[i]));
     }
@@ -304,7 +306,7 @@ __device__ __forceinline__ void lay(const Jobs<T>& jobs, int block) {
     for (int o = 32; o > 0; o >>= 1) largest = fmaxf(largest, __shfl_xor(largest, o, 64));
     e = scale_exponent(largest);
     if (lane_id() == 0) j.to.exps[row] = e;
-  } else if (j.scale == kOne) {
+  } else if (!kFloat && j.scale == kOne) {
     e = *j.to.exps;
   }
   auto by_columns = [&](const Laid& to, int at, const float (&v)[8]) __attribute__((always_inline)) {
@@ -317,9 +319,9 @@ __device__ __forceinline__ void lay(const Jobs<T>& jobs, int block) {
   auto put = [&](int p, float (&v)[8]) __attribute__((always_inline)) {
     const int at = p * 512 + lane_id() * 8;
     if (at >= j.to.padded) return;
-    if (j.scale == kPerColumn) return by_columns(j.to, at, v);
-    if (j.also.p) by_columns(j.also, at, v);
-    if (j.scale != kAsIs) {
+    if (kFloat && j.scale == kPerColumn) return by_columns(j.to, at, v);
+    if (kFloat && j.also.p) by_columns(j.also, at, v);
+    if (kFloat || j.scale != kAsIs) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] = ldexpf(v[i], e);
     }
@@ -330,14 +332,14 @@ __device__ __forceinline__ void lay(const Jobs<T>& jobs, int block) {
     if (p < pieces) put(p, held[p]);
   for (int p = kHeld; p < pieces; ++p) {
     float v[8];
-    j.from.template load<8>(row, p * 512 + lane_id() * 8, v);
+    j.from.template load<SLOPED, 8>(row, p * 512 + lane_id() * 8, v);
     put(p, v);
   }
 }
 
-template <typename T>
+template <typename T, bool SLOPED>
 __global__ __launch_bounds__(256) void lay_kernel(Jobs<T> jobs) {
-  lay(jobs, blockIdx.x);
+  lay<T, SLOPED>(jobs, blockIdx.x);
 }
 
 // ---- columns: sums and largest values, and on the way d itself where it needs no scale.  A workgroup takes 32 groups of V
@@ -361,10 +363,10 @@ struct ColumnJobs {
   int parts, count;
 };
 // The column jobs, and behind them what is to be laid out and does not depend on them.
-template <typename T>
+template <typename T, bool SLOPED>
 __global__ __launch_bounds__(256) void columns_kernel(ColumnJobs<T> jobs, Jobs<T> beside) {
   const int own = jobs.blocks * jobs.parts * jobs.count;
-  if ((int)blockIdx.x >= own) return lay(beside, blockIdx.x - own);
+  if ((int)blockIdx.x >= own) return lay<T, SLOPED>(beside, blockIdx.x - own);
   constexpr int V = kPer16<T>;
   __shared__ float part[2][8][32 * V + 4];
   const int block = blockIdx.x % jobs.blocks, part_of = blockIdx.x / jobs.blocks % jobs.parts;
@@ -381,7 +383,7 @@ __global__ __launch_bounds__(256) void columns_kernel(ColumnJobs<T> jobs, Jobs<T
   if (c < width)
     for (int64_t row0 = part_of * 8 + group; row0 < j.from.rows; row0 += kBatch * step) {
       float v[kBatch][V];
-      j.from.template load_rows<V, kBatch>(row0, step, c, v);
+      j.from.template load_rows<SLOPED, V, kBatch>(row0, step, c, v);
 #pragma unroll
       for (int b = 0; b < kBatch; ++b) {
 #pragma unroll
@@ -542,10 +544,10 @@ void add_job(Jobs<T>& jobs, const Source<T>& from, const Laid& to, Scale scale, 
   jobs.first[jobs.count + 1] = jobs.first[jobs.count] + (int)div_up(from.rows, 4);
   ++jobs.count;
 }
-template <typename T>
+template <typename T, bool SLOPED>
 hipError_t run_jobs(const Jobs<T>& jobs, hipStream_t s) {
   if (!jobs.count) return hipSuccess;
-  lay_kernel<T><<<dim3((unsigned)jobs.first[jobs.count]), dim3(256), 0, s>>>(jobs);
+  lay_kernel<T, SLOPED><<<dim3((unsigned)jobs.first[jobs.count]), dim3(256), 0, s>>>(jobs);
   return hipGetLastError();
 }
 
@@ -676,7 +678,7 @@ hipError_t launch_linear(const LinearArgs& a, hipStream_t s) {
     const Scale scale = sizeof(T) == 4 ? kPerRow : kAsIs;
     if (!in_place(x)) add_job(jobs, x, room.x, scale);
     if (!in_place(W)) add_job(jobs, W, room.W, scale);
-    const hipError_t e = run_jobs(jobs, s);
+    const hipError_t e = run_jobs<T, false>(jobs, s);
     if (e != hipSuccess) return e;
     if (sizeof(T) == 4) {
       out.exp_r = room.x.exps;
@@ -729,14 +731,16 @@ hipError_t launch_linear_grad(const LinearGradArgs& a, hipStream_t s) {
       columns.count = count;
       columns.blocks = (int)div_up(widest, 32 * kPer16<T>);
       const Jobs<T> beside = scaled ? Jobs<T>{} : jobs;
-      columns_kernel<T><<<dim3((unsigned)(columns.blocks * columns.parts * count + beside.first[beside.count])), dim3(256), 0, s>>>(columns, beside);
+      const dim3 grid((unsigned)(columns.blocks * columns.parts * count + beside.first[beside.count]));
+      if (sloped) columns_kernel<T, true><<<grid, dim3(256), 0, s>>>(columns, beside);
+      else columns_kernel<T, false><<<grid, dim3(256), 0, s>>>(columns, beside);
       if ((e = hipGetLastError()) != hipSuccess) return e;
       if (columns.parts > 1 ? a.dbias || scaled : !kFloat && d_scales) {
         columns_sum_kernel<T><<<dim3((unsigned)div_up(widest, 32) + 1, (unsigned)count), dim3(256), 0, s>>>(columns);
         if ((e = hipGetLastError()) != hipSuccess) return e;
       }
     }
-    if ((!count || scaled) && (e = run_jobs(jobs, s)) != hipSuccess) return e;
+    if ((!count || scaled) && (e = sloped ? run_jobs<T, true>(jobs, s) : run_jobs<T, false>(jobs, s)) != hipSuccess) return e;
     if (!products) return hipSuccess;
     auto store_of = [&](void* y, int64_t ld, int M, const int* exp_r, const int* exp_c) {
       LinearStore<T> out{};

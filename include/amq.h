@@ -471,7 +471,10 @@ int amq_lm_sequence_score(const uint32_t* Ep, const float* alpha_e, int64_t voca
 
 /*
  * Operators of quantization-aware training: what a training step does around the quantized weights (Sec. 4,
- * "Training").  Data of three types, all arithmetic and every sum in binary32, results rounded once:
+ * "Training").  Data of three types, all arithmetic and every sum in binary32, results rounded once.
+ * AMQ_ERR_UNSUPPORTED beyond these limits: rows of 2^20 entries (k and n of a linear layer too); 2^31 - 1 rows of a layer norm, 2^22
+ * of a linear layer, 2^20 of an update; 2^38 entries per matrix of a linear layer, whose x, W and dy have strides of at most 2^22; 65535
+ * matrices per call.
  */
 #define AMQ_F32 0
 #define AMQ_BF16 1
@@ -505,6 +508,7 @@ int amq_layer_norm_backward(const void* dy, int64_t ld_dy, const void* x, int64_
  * bfloat16 and half products go through the matrix cores as they are.  Float operands are scaled by a power of two per
  * row and split into two halves of 11 bits each, so that three half products leave the error of binary32 products; entries
  * 2^28 and more below their row's largest lose digits.  Up to 8 rows (a token's vector) are multiplied in binary32.
+ * An infinity or NaN in an operand spoils the results that it enters (NaN, or the infinity) and no others.
  *   workspace: at least amq_linear_workspace_bytes(rows, k, n, type) bytes, 256-byte aligned.
  * The backward pass takes dy [rows][ld_dy]: with d = dy act'(pre), dx = d W, dW = d^T x, dbias = sum over rows of d; any of
  * the three may be NULL.  The residual's gradient is dy itself.  pre may be NULL for AMQ_ACT_NONE.

@@ -10,7 +10,7 @@
 // step is 2^-38 of that value.  d in half is scaled too before it is rounded, by one power of two: gradients divided by a
 // batch's size lie where half has few digits.
 //
-// A few rows (a token's vector) are multiplied on the vector units: there W is read once, and nothing else matters.
+// A few rows (a token's vector) are multiplied on the vector units where the matrix cores' layout would cost more than it gives.
 #include "../../include/amq.h"
 
 #include <math.h>
@@ -143,8 +143,16 @@ struct LinearStore {
   }
 };
 
-// ---- a few rows: workgroup = 4 rows of W, its waves share the row's k
-constexpr int kFewRows = 8;
+// ---- a few rows: workgroup = 4 rows of W, its waves share the row's k.  Bound by reading W once, or for small W by latency: one row
+// of 1024 float numbers by 4096 5.3 us (of which a launch alone 2), 3.2 TB/s from the last-level cache.
+//
+// Which rows come here: the matrix cores take 16 rows for the price of one, but float operands and those that do not lie as they need them
+// have to be laid out first.  us here with 1 / 2 / 4 / 8 rows, and there:
+//   float     1024 x 4096 4.1 / 4.9 / 6.4 / 9.3, 19;  1024 x 42000 25 / 26 / 32 / 63, 93              up to 8
+//   16 bits, to be laid out: 300 x 300 3.9 / 4.6 / 5.9 / 8.6, 7.4                                      up to 4
+//   16 bits, in place: 1024 x 1024 3.5 / 4.1 / 5.3 / 7.6, 5.0;  4096 x 4096 11.6 / 13.9 / 18.6 / 36, 8.8    rows k n below 2^22
+constexpr int kFewRows = 8, kFewLaid = 4;
+constexpr int64_t kFewInPlace = int64_t(1) << 22;
 template <typename T, int M>
 __global__ __launch_bounds__(256) void linear_few_kernel(const T* x, int64_t ld_x, const T* W, int64_t ld_w, int k, LinearStore<T> out) {
   constexpr int V = kPer16<T>, R = 4;
@@ -273,7 +281,8 @@ __device__ __forceinline__ void put8(const Laid& to, int64_t row, int at, const 
   if constexpr (sizeof(T) == 4) *reinterpret_cast<uint4*>(q + 32) = __builtin_bit_cast(uint4, lo);
 }
 
-// One wave per row.  Rows of up to 4096 values stay in registers between the search for the scale and the output.
+// One wave per row.  Rows of up to 4096 values stay in registers between the search for the scale and the output.  Bound by
+// memory or, for few rows, latency: 700 + 1300 rows of 650 float numbers (10 MB read and written) 8 us, of 2048 11 us = 3 TB/s.
 template <typename T, bool SLOPED>
 __device__ __forceinline__ void lay(const Jobs<T>& jobs, int block) {
   int k = 0;
@@ -342,7 +351,8 @@ __global__ __launch_bounds__(256) void lay_kernel(Jobs<T> jobs) {
   lay<T, SLOPED>(jobs, blockIdx.x);
 }
 
-// ---- columns: sums and largest values, and on the way d itself where it needs no scale.  A workgroup takes 32 groups of V
+// ---- columns: sums and largest values, and on the way d itself where it needs no scale.  Bound by memory: 8960 x 4096 bfloat16
+// (73 MB) 21 us = 3.5 TB/s, and 4 us for the second launch.  A workgroup takes 32 groups of V
 // columns and every 8 * parts-th row of them; what it finds are partial results, which a second launch puts together.  Of at
 // most 128 rows one part is all (16 rows per thread; a launch costs more).
 constexpr int kColumnParts = 64;
@@ -493,12 +503,12 @@ struct ForwardRoom {
 ForwardRoom forward_room(void* ws, int64_t rows, int64_t k, int64_t n, int type) {
   Carve w(ws);
   ForwardRoom r{};
-  if (rows > kFewRows) {
-    const bool scaled = type == AMQ_F32;
+  const bool scaled = type == AMQ_F32;
+  if (rows > (scaled ? kFewRows : kFewLaid)) {
     r.x = lay_room(w, rows, k, type, scaled ? rows : 0);
     r.W = lay_room(w, n, k, type, scaled ? n : 0);
-    r.part = (float*)w.take(plan_product(rows, n, k, planes_of(type), 1, false).part_bytes);
   }
+  if (!scaled || rows > kFewRows) r.part = (float*)w.take(plan_product(rows, n, k, planes_of(type), 1, false).part_bytes);
   r.total = w.off;
   return r;
 }
@@ -594,6 +604,7 @@ hipError_t linear_few(const LinearArgs& a, const LinearStore<T>& out, hipStream_
 // (bfloat16 with gelu, tile 256 / 128 / 64 / 64 with four groups): 8960 x 4096 x 1024 134 / 120 / 145 / 247, 4096^3 116 / 138 /
 // 205 / 260, 2240 x 1024 x 1024 41 / 23 / 15 / 22, 1024 x 1024 x 2240 61 / 33 / 18 / 13, 300 x 300 x 1216 43 / 23 / 12 / 9.
 //   256 (one workgroup per unit): a round 24 + 1.3 per stage
+//   192 (one): a round 16 + 1.07 per stage (the lower half of 4096 x 4096 over 16384, 136 tiles of 256 or 253 of 192: 338 and 287)
 //   128 (two): 10 + a tile 4 + 0.55 per stage, and a last round that is not full counts half as one
 //   128 with two groups (one): 2 + a round 7.5 + 0.47 per stage (2048^3 24.6 against 29.7, 1024 x 4096 x 8960 75 against 88)
 //   64 (three): 6.5 + a tile 0.9 + 0.2 per stage, alone 5.5 + 0.32 per stage
@@ -671,9 +682,10 @@ hipError_t launch_linear(const LinearArgs& a, hipStream_t s) {
   return with_type(a.type, [&](auto t) {
     using T = decltype(t);
     LinearStore<T> out{(T*)a.y, (T*)a.pre, (const T*)a.bias, (const T*)a.residual, nullptr, nullptr, nullptr, a.ld_y, a.ld_pre, a.ld_r, a.rows, a.n, a.act};
-    if (a.rows <= kFewRows) return linear_few(a, out, s);
-    const ForwardRoom room = forward_room(a.ws, a.rows, a.k, a.n, a.type);
     const Source<T> x{(const T*)a.x, a.ld_x, nullptr, 0, a.rows, a.k, 0}, W{(const T*)a.W, a.ld_w, nullptr, 0, a.n, a.k, 0};
+    const bool as_is = in_place(x) && in_place(W);
+    if (a.rows <= (sizeof(T) == 4 || as_is ? kFewRows : kFewLaid) && (!as_is || (int64_t)a.rows * a.k * a.n < kFewInPlace)) return linear_few(a, out, s);
+    const ForwardRoom room = forward_room(a.ws, a.rows, a.k, a.n, a.type);
     Jobs<T> jobs{};
     const Scale scale = sizeof(T) == 4 ? kPerRow : kAsIs;
     if (!in_place(x)) add_job(jobs, x, room.x, scale);

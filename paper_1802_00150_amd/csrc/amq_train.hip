@@ -99,7 +99,7 @@ int amq_linear_backward(const void* dy, int64_t ld_dy, const void* x, int64_t ld
   if (!on_elements(dy, type) || !on_elements(x, type) || !on_elements(W, type) || !on_elements(pre, type) || !on_elements(dx, type) ||
       !on_elements(dW, type) || !on_elements(dbias, type))
     return AMQ_ERR_INVALID;
-  if (!linear_sizes_supported(rows, k, n) || ld_dy > kMaxStride) return AMQ_ERR_UNSUPPORTED;
+  if (!linear_sizes_supported(rows, k, n) || ld_dy > kMaxStride || (dW && ld_x > kMaxStride) || (dx && ld_w > kMaxStride)) return AMQ_ERR_UNSUPPORTED;
   if (!workspace_ok(workspace, workspace_bytes, amq::linear_grad_workspace(rows, k, n, type))) return AMQ_ERR_INVALID;
   return amq::status_of(amq::launch_linear_grad({dy, x, W, pre, dx, dW, dbias, ld_dy, ld_x, ld_w, ld_pre, ld_dx, ld_dw, (int)rows, (int)k,
                                                  (int)n, type, activation, workspace},

@@ -23,11 +23,11 @@ def operand(seed, rows, cols, dtype, scale=1.0):
 
 
 def check(got, a, b, dtype, terms, bias=None):
-    """got = a b (binary64) + bias"""
+    """got = a b (binary64) + bias; float operands are split into 22 bits"""
     ref, size = a @ b, a.abs() @ b.abs()
     if bias is not None:
         ref, size = ref + bias, size + bias.abs()
-    tol = (terms + 16) * U * size + half_ulp(dtype) * ref.abs() * 1.01 + smallest(dtype)
+    tol = ((terms + 16) * U + (2.0 ** -21 if dtype == torch.float32 else 0.0)) * size + half_ulp(dtype) * ref.abs() * 1.01 + smallest(dtype)
     assert got.dtype == dtype and got.shape == ref.shape
     assert bool(((got.double() - ref).abs() <= tol).all())  # (NaN counts as off)
 
@@ -50,6 +50,18 @@ def test_every_order_of_operands(amq, M, N, k, dtype):
     dx, dW, db = amq.linear_backward(dy, x, W, None, None, False, True, False)
     assert dx is None and db is None
     check(dW, dy.double().t().contiguous(), x.double(), dtype, k)
+
+
+# both gradients in one launch or in two, with tiles of 64 and 128, the longer contraction in either of them
+@pytest.mark.parametrize("rows,k,n", [(2000, 2200, 1700), (1700, 2200, 2010), (3300, 2250, 700), (700, 2250, 3300), (2390, 3990, 320), (330, 3810, 380), (1130, 3920, 480),
+                                      (430, 3810, 390), (8960, 300, 310), (300, 1500, 8000)])
+@pytest.mark.parametrize("dtype", [torch.float32] + HALVES)
+def test_both_gradients(amq, rows, k, n, dtype):
+    dy, x, W = operand(1, rows, n, dtype), operand(2, rows, k, dtype), operand(3, n, k, dtype, n ** -0.5)
+    dx, dW, db = amq.linear_backward(dy, x, W)
+    check(dx, dy.double(), W.double(), dtype, n)
+    check(dW, dy.double().t().contiguous(), x.double(), dtype, rows)
+    check(db[None], torch.ones(1, rows, dtype=torch.float64, device=DEV), dy.double(), dtype, rows)
 
 
 @pytest.mark.parametrize("rows,cols", [(3900, 4200), (4200, 3900), (5500, 5610)])

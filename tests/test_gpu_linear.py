@@ -59,6 +59,17 @@ def test_forward(amq, rows, k, n, dtype):
     check_forward(amq, rows, k, n, dtype, ACTS[(rows + k + n) % 6])
 
 
+@pytest.mark.parametrize("k,n", [(2048, 2056), (1000, 3000), (999, 1501), (24, 40)])
+@pytest.mark.parametrize("rows", [1, 2, 4, 5, 8])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_few_rows(amq, rows, k, n, dtype):
+    """On either side of the choice between the vector units and the matrix cores; the caller's workspace too."""
+    check_forward(amq, rows, k, n, dtype, "silu")
+    x, W, b, r = (t.to(DEV) for t in inputs(rows, rows, k, n, dtype))
+    y = amq.linear(x, W, b, None, r)
+    assert torch.equal(y, amq.linear(x, W, b, None, r, ws=amq.linear_workspace(rows, k, n, dtype, DEV).fill_(0xFF)))
+
+
 @pytest.mark.parametrize("rows,k,n", LARGE)
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_forward_large_tiles(amq, rows, k, n, dtype):

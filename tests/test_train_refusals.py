@@ -71,3 +71,15 @@ def test_orthogonalize(L):
         assert call(L.amq_orthogonalize, args, **bad) == INVALID, bad
     assert call(L.amq_orthogonalize, args, batch=1 << 17) == UNSUPPORTED
     assert call(L.amq_orthogonalize, args, rows=(1 << 20) + 1) == UNSUPPORTED
+
+
+def test_strides_of_the_linear_backward(L):
+    """Strides that the products' 32-bit offsets cannot hold are refused where the operand is read, and only there."""
+    need = L.amq_linear_backward_workspace_bytes(20, 8, 6, BF16)
+    args = dict(dy=P, ld_dy=6, x=P, ld_x=8, W=P, ld_w=8, pre=P, ld_pre=6, rows=20, k=8, n=6, type=BF16, act=0, dx=P, ld_dx=8, dW=P, ld_dw=8, dbias=P,
+                ws=NULL, bytes=need, stream=None)  # (no workspace: what is not refused as unsupported is invalid, so nothing is launched)
+    wide = (1 << 22) + 8
+    for bad in (dict(ld_dy=wide), dict(ld_x=wide), dict(ld_w=wide)):
+        assert call(L.amq_linear_backward, args, **bad) == UNSUPPORTED, bad
+    for good in (dict(ld_x=wide, dW=NULL), dict(ld_w=wide, dx=NULL), dict(ld_x=1 << 22), dict(ld_dx=wide, ld_dw=wide)):
+        assert call(L.amq_linear_backward, args, **good) == INVALID, good

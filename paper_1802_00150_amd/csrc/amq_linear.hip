@@ -40,6 +40,14 @@ __device__ __forceinline__ float normal_of(float z, float& density) {
   const float q = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f) * density;
   return z < 0.0f ? 0.5f * q : 1.0f - 0.5f * q;
 }
+// z Phi(z) = max(z, 0) - |z| erfc(|z| / sqrt 2) / 2 by the same series, its constants halved: 20 instruction slots
+// instead of 23 through Phi (a reciprocal and an exponential take four each), where the epilogue is bound by them.  (Beyond 30 the second term is 0, and |z| stops there for infinities.)
+__device__ __forceinline__ float gelu_of(float z) {
+  const float a = fminf(fabsf(z), 30.0f), t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678118654752f, a, 1.0f));
+  const float density = __expf(a * a * -0.5f);
+  const float half_q = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 0.5307027145f, -0.7265760135f), 0.7107068705f), -0.142248368f), 0.127414796f) * density;
+  return fmaf(-a, half_q, fmaxf(z, 0.0f));
+}
 // One of the functions below on V values: the choice is made once for all of them, so that they run side by side.
 template <int V, typename F>
 __device__ __forceinline__ void each(float (&v)[V], F f) {
@@ -50,11 +58,7 @@ template <int V>
 __device__ __forceinline__ void activate(float (&v)[V], int act) {
   switch (act) {
     case AMQ_ACT_RELU: return each(v, [](float z) { return z > 0.0f ? z : 0.0f; });
-    case AMQ_ACT_GELU:
-      return each(v, [](float z) {
-        float density;
-        return z * normal_of(z, density);
-      });
+    case AMQ_ACT_GELU: return each(v, [](float z) { return gelu_of(z); });
     case AMQ_ACT_SILU: return each(v, [](float z) { return z * logistic(z); });
     case AMQ_ACT_SIGMOID: return each(v, [](float z) { return logistic(z); });
     case AMQ_ACT_TANH: return each(v, [](float z) { return tanh_of(z); });
@@ -351,12 +355,17 @@ __global__ __launch_bounds__(256) void lay_kernel(Jobs<T> jobs) {
   lay<T, SLOPED>(jobs, blockIdx.x);
 }
 
-// ---- columns: sums and largest values, and on the way d itself where it needs no scale.  Bound by memory: 8960 x 4096 bfloat16
-// (73 MB) 21 us = 3.5 TB/s, and 4 us for the second launch.  A workgroup takes 32 groups of V
+// ---- columns: sums and largest values, and on the way d itself where it needs no scale.  Bound by memory, or where slopes are
+// formed by those: d of 8960 x 1024 bfloat16 with its slopes (55 MB) 14.5 us = 3.8 TB/s, and 5 us for the second launch.  Many rows of few columns are
+// dealt to more parts, three workgroups per compute unit (with one, 64 parts, 22.7 us).  A workgroup takes 32 groups of V
 // columns and every 8 * parts-th row of them; what it finds are partial results, which a second launch puts together.  Of at
 // most 128 rows one part is all (16 rows per thread; a launch costs more).
-constexpr int kColumnParts = 64;
-int column_parts(int64_t rows) { return rows <= 128 ? 1 : kColumnParts; }
+constexpr int kColumnParts = 64, kMostColumnParts = 192;
+int column_parts(int64_t rows, int64_t blocks) {  // blocks: workgroups per part, of all jobs
+  if (rows <= 128) return 1;
+  const int64_t parts = 768 / blocks & ~int64_t(7);
+  return (int)(rows <= 32 * kMostColumnParts || parts < kColumnParts ? kColumnParts : parts < kMostColumnParts ? parts : kMostColumnParts);
+}
 template <typename T>
 struct ColumnJob {
   Source<T> from;
@@ -429,7 +438,7 @@ __global__ __launch_bounds__(256) void columns_kernel(ColumnJobs<T> jobs, Jobs<T
     if (j.largest && (jobs.parts > 1 || j.one)) j.largest[(int64_t)part_of * j.from.cols + at] = top;
   }
 }
-// 32 columns per workgroup; for one scale of all columns a last workgroup goes through all partial results.  (kColumnParts
+// 32 columns per workgroup; for one scale of all columns a last workgroup goes through all partial results.  (A multiple of 8
 // parts, or one, of which only that scale is to be found.)
 template <typename T>
 __global__ __launch_bounds__(256) void columns_sum_kernel(ColumnJobs<T> jobs) {
@@ -453,11 +462,11 @@ __global__ __launch_bounds__(256) void columns_sum_kernel(ColumnJobs<T> jobs) {
   float s = 0.0f, top = 0.0f;
   if (c < cols) {
     if (j.total)
-#pragma unroll
-      for (int p = 0; p < kColumnParts; p += 8) s += j.sums[(int64_t)(p + group) * cols + c];
+#pragma unroll 8
+      for (int p = 0; p < jobs.parts; p += 8) s += j.sums[(int64_t)(p + group) * cols + c];
     if (j.exps && !j.one)
-#pragma unroll
-      for (int p = 0; p < kColumnParts; p += 8) top = fmaxf(top, j.largest[(int64_t)(p + group) * cols + c]);
+#pragma unroll 8
+      for (int p = 0; p < jobs.parts; p += 8) top = fmaxf(top, j.largest[(int64_t)(p + group) * cols + c]);
   }
   sums[group][lane] = s;
   tops[group][lane] = top;
@@ -527,10 +536,10 @@ BackwardRoom backward_room(void* ws, int64_t rows, int64_t k, int64_t n, int typ
   r.d_columns = wide ? lay_room(w, rows, n, type, n) : r.d;
   r.x = lay_room(w, rows, k, type, wide ? k : 0);
   r.W = lay_room(w, n, k, type, wide ? k : 0);
-  r.sums = (float*)w.take(sizeof(float) * kColumnParts * (size_t)n);
-  if (type != AMQ_BF16) r.tops[0] = (float*)w.take(sizeof(float) * kColumnParts * (size_t)n);
+  r.sums = (float*)w.take(sizeof(float) * kMostColumnParts * (size_t)n);
+  if (type != AMQ_BF16) r.tops[0] = (float*)w.take(sizeof(float) * kMostColumnParts * (size_t)n);
   if (wide)
-    for (int i = 1; i < 3; ++i) r.tops[i] = (float*)w.take(sizeof(float) * kColumnParts * (size_t)k);
+    for (int i = 1; i < 3; ++i) r.tops[i] = (float*)w.take(sizeof(float) * kMostColumnParts * (size_t)k);
   const size_t a = plan_product(rows, k, n, planes_of(type), 1, false).part_bytes;
   const size_t b = plan_product(n, k, rows, planes_of(type), 1, false).part_bytes;
   r.part = (float*)w.take(a > b ? a : b);
@@ -739,9 +748,9 @@ hipError_t launch_linear_grad(const LinearGradArgs& a, hipStream_t s) {
     if (a.dW && !in_place(x)) add_job(jobs, x, room.x, kFloat ? kPerColumn : kAsIs);
     if (count) {
       const int64_t longest = kFloat && a.dx && a.n > a.rows ? a.n : a.rows;
-      columns.parts = column_parts(longest);
       columns.count = count;
       columns.blocks = (int)div_up(widest, 32 * kPer16<T>);
+      columns.parts = column_parts(longest, (int64_t)columns.blocks * count);
       const Jobs<T> beside = scaled ? Jobs<T>{} : jobs;
       const dim3 grid((unsigned)(columns.blocks * columns.parts * count + beside.first[beside.count]));
       if (sloped) columns_kernel<T, true><<<grid, dim3(256), 0, s>>>(columns, beside);

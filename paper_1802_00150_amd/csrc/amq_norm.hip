@@ -12,7 +12,7 @@
 // Longer rows are read once per sum (general kernels at the end).
 //
 // Measured (bytes read and written once, of a large copy's 5.1 TB/s): forward 8960 x 1024 half 7.7 us = 4.7 TB/s, 35840 x 1024
-// float 6.3 TB/s; backward 8960 x 1500 bfloat16 28.4 us = 2.8 TB/s, of which 6.6 are the parameters' sums, 35840 x 1024 float
+// float 6.3 TB/s; backward 8960 x 1500 bfloat16 26.9 us = 3.0 TB/s, of which 6.3 are the parameters' sums, 35840 x 1024 float
 // 5.1 TB/s; one row of 1024 2 us (and the launch).
 #include "../../include/amq.h"
 
@@ -154,11 +154,15 @@ __global__ __launch_bounds__(W > 4 ? W * 64 : 256) void norm_kernel(NormArgs a) 
   }
 }
 
-// Rows that a workgroup of the backward pass has at a time.
-constexpr int grad_rows(int waves) { return waves == 1 ? 8 : waves == 4 ? 2 : 1; }
+// Rows that a workgroup of the backward pass has at a time: 16 waves where the registers allow it, which hide each other's sums and barriers
+// (8960 x 1500 bfloat16 26.9 us, with 8 waves 28.0).
+constexpr int grad_rows(int waves, int entries) {
+  const int twice = entries <= 8 ? 2 : 1;
+  return waves == 1 ? 8 * twice : waves == 4 ? 2 * twice : 1;
+}
 template <typename T, typename P, int W, int NV>
-__global__ __launch_bounds__(grad_rows(W) * W * 64) void norm_grad_kernel(NormGradArgs a) {
-  constexpr int V = kPer16<T>, kRows = grad_rows(W), kEntries = W * 64 * NV * V;
+__global__ __launch_bounds__(grad_rows(W, NV * kPer16<T>) * W * 64) void norm_grad_kernel(NormGradArgs a) {
+  constexpr int V = kPer16<T>, kRows = grad_rows(W, NV * V), kEntries = W * 64 * NV * V;
   __shared__ float slots[2 * kRows * W][2];
   __shared__ float shared_sums[kRows > 1 ? kRows * 2 * kEntries : 1];
   int turn = 0;
@@ -421,7 +425,8 @@ int norm_grad_parts(int64_t rows, int n) {
   int64_t parts = 1;
   for (int per16 : {4, 8}) {
     const Shape h = shape_of(rows, n, per16);
-    const int64_t tasks = (rows + grad_rows(h.waves) - 1) / grad_rows(h.waves);
+    const int at_a_time = grad_rows(h.waves, h.pieces * per16);
+    const int64_t tasks = (rows + at_a_time - 1) / at_a_time;
     const int64_t p = h.waves ? even_blocks(tasks, kMostParts) : (rows < 64 ? rows : 64);
     parts = p > parts ? p : parts;
   }
@@ -467,9 +472,9 @@ hipError_t launch_norm_grad(const NormGradArgs& a0, hipStream_t s) {
       }
     } else {
       e = with_shape<T>(h, [&](auto w, auto nv) {
-        constexpr int W = decltype(w)::value;
-        parts = even_blocks((a.rows + grad_rows(W) - 1) / grad_rows(W), kMostParts);
-        norm_grad_kernel<T, P, W, decltype(nv)::value><<<dim3((unsigned)parts), dim3(grad_rows(W) * W * 64), 0, s>>>(a);
+        constexpr int W = decltype(w)::value, NV = decltype(nv)::value, kRows = grad_rows(W, NV * kPer16<T>);
+        parts = even_blocks((a.rows + kRows - 1) / kRows, kMostParts);
+        norm_grad_kernel<T, P, W, NV><<<dim3((unsigned)parts), dim3(kRows * W * 64), 0, s>>>(a);
         return hipGetLastError();
       });
     }

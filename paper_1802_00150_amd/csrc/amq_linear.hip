@@ -40,14 +40,6 @@ __device__ __forceinline__ float normal_of(float z, float& density) {
   const float q = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f) * density;
   return z < 0.0f ? 0.5f * q : 1.0f - 0.5f * q;
 }
-// z Phi(z) = max(z, 0) - |z| erfc(|z| / sqrt 2) / 2 by the same series, its constants halved: 20 instruction slots
-// instead of 23 through Phi (a reciprocal and an exponential take four each), where the epilogue is bound by them.  (Beyond 30 the second term is 0, and |z| stops there for infinities.)
-__device__ __forceinline__ float gelu_of(float z) {
-  const float a = fminf(fabsf(z), 30.0f), t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678118654752f, a, 1.0f));
-  const float density = __expf(a * a * -0.5f);
-  const float half_q = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 0.5307027145f, -0.7265760135f), 0.7107068705f), -0.142248368f), 0.127414796f) * density;
-  return fmaf(-a, half_q, fmaxf(z, 0.0f));
-}
 // One of the functions below on V values: the choice is made once for all of them, so that they run side by side.
 template <int V, typename F>
 __device__ __forceinline__ void each(float (&v)[V], F f) {
@@ -58,7 +50,11 @@ template <int V>
 __device__ __forceinline__ void activate(float (&v)[V], int act) {
   switch (act) {
     case AMQ_ACT_RELU: return each(v, [](float z) { return z > 0.0f ? z : 0.0f; });
-    case AMQ_ACT_GELU: return each(v, [](float z) { return gelu_of(z); });
+    case AMQ_ACT_GELU:
+      return each(v, [](float z) {
+        float density;
+        return z * normal_of(z, density);
+      });
     case AMQ_ACT_SILU: return each(v, [](float z) { return z * logistic(z); });
     case AMQ_ACT_SIGMOID: return each(v, [](float z) { return logistic(z); });
     case AMQ_ACT_TANH: return each(v, [](float z) { return tanh_of(z); });

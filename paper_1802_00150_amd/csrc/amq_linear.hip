@@ -241,12 +241,14 @@ struct Laid {
   int64_t ld;
   int rows, padded;
 };
-enum Scale { kAsIs, kPerRow, kPerColumn, kOne };  // per row (found and left here) or column (read): float; as is, or by one that is read: 16 bits
+enum Scale { kAsIs, kPerRow, kPerColumn, kOne };  // per row (found and left here) or column (read): float; as is, or all by one: 16 bits
 template <typename T>
 struct Job {
   Source<T> from;
   Laid to, also;  // also: the same once more, scaled per column (p null: not wanted)
   Scale scale;
+  const float* tops;  // kOne: what the scale is found from, left in to.exps
+  int top_count;
 };
 constexpr int kMaxJobs = 3;
 template <typename T>
@@ -316,7 +318,14 @@ __device__ __forceinline__ void lay(const Jobs<T>& jobs, int block) {
     e = scale_exponent(largest);
     if (lane_id() == 0) j.to.exps[row] = e;
   } else if (!kFloat && j.scale == kOne) {
-    e = *j.to.exps;
+    // (each row's wave for itself, of a quarter of a row's length: less than a launch in between costs)
+    float largest = 0.0f;
+#pragma unroll 4
+    for (int i = lane_id(); i < j.top_count; i += 64) largest = fmaxf(largest, j.tops[i]);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) largest = fmaxf(largest, __shfl_xor(largest, o, 64));
+    e = scale_exponent(largest);
+    if (row == 0 && lane_id() == 0) *j.to.exps = e;
   }
   auto by_columns = [&](const Laid& to, int at, const float (&v)[8]) __attribute__((always_inline)) {
     const Elements<int, 8> exps = fetch<int, 8>(to.exps + at, j.from.cols - at);
@@ -346,11 +355,6 @@ __device__ __forceinline__ void lay(const Jobs<T>& jobs, int block) {
   }
 }
 
-template <typename T, bool SLOPED>
-__global__ __launch_bounds__(256) void lay_kernel(Jobs<T> jobs) {
-  lay<T, SLOPED>(jobs, blockIdx.x);
-}
-
 // ---- columns: sums and largest values, and on the way d itself where it needs no scale.  Bound by memory, or where slopes are
 // formed by those: d of 8960 x 1024 bfloat16 with its slopes (55 MB) 14.5 us = 3.8 TB/s, and 5 us for the second launch.  Many rows of few columns are
 // dealt to more parts, three workgroups per compute unit (with one, 64 parts, 22.7 us).  A workgroup takes 32 groups of V
@@ -365,7 +369,7 @@ int column_parts(int64_t rows, int64_t blocks) {  // blocks: workgroups per part
 template <typename T>
 struct ColumnJob {
   Source<T> from;
-  float *sums, *largest;  // [parts][cols], or null
+  float *sums, *largest;  // [parts][cols], or null; of one scale for all columns [parts][blocks]
   Laid to;                // p null: not wanted
   T* total;               // [cols]: the sums, or null
   int* exps;              // scales per column, or one, or null
@@ -377,11 +381,11 @@ struct ColumnJobs {
   int blocks;  // workgroups per part
   int parts, count;
 };
-// The column jobs, and behind them what is to be laid out and does not depend on them.
+// The column jobs, and behind them what is to be laid out and does not depend on them (d itself is not among it).
 template <typename T, bool SLOPED>
 __global__ __launch_bounds__(256) void columns_kernel(ColumnJobs<T> jobs, Jobs<T> beside) {
   const int own = jobs.blocks * jobs.parts * jobs.count;
-  if ((int)blockIdx.x >= own) return lay<T, SLOPED>(beside, blockIdx.x - own);
+  if ((int)blockIdx.x >= own) return lay<T, false>(beside, blockIdx.x - own);
   constexpr int V = kPer16<T>;
   __shared__ float part[2][8][32 * V + 4];
   const int block = blockIdx.x % jobs.blocks, part_of = blockIdx.x / jobs.blocks % jobs.parts;
@@ -416,6 +420,7 @@ __global__ __launch_bounds__(256) void columns_kernel(ColumnJobs<T> jobs, Jobs<T
     part[1][group][lane * V + i] = largest[i];
   }
   __syncthreads();
+  float all = 0.0f;
   for (int i = threadIdx.x; i < 32 * V; i += 256) {
     const int at = block * 32 * V + i;
     if (at >= j.from.cols) continue;
@@ -431,30 +436,24 @@ __global__ __launch_bounds__(256) void columns_kernel(ColumnJobs<T> jobs, Jobs<T
     } else if (j.sums) {
       j.sums[(int64_t)part_of * j.from.cols + at] = sum;
     }
-    if (j.largest && (jobs.parts > 1 || j.one)) j.largest[(int64_t)part_of * j.from.cols + at] = top;
+    if (j.largest && jobs.parts > 1 && !j.one) j.largest[(int64_t)part_of * j.from.cols + at] = top;
+    all = top;
   }
+  if (!j.one) return;
+  __shared__ float tops[4];
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) all = fmaxf(all, __shfl_xor(all, o, 64));
+  if (lane_id() == 0) tops[wave_id()] = all;
+  __syncthreads();
+  if (threadIdx.x == 0) j.largest[part_of * jobs.blocks + block] = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
 }
-// 32 columns per workgroup; for one scale of all columns a last workgroup goes through all partial results.  (A multiple of 8
-// parts, or one, of which only that scale is to be found.)
+// 32 columns per workgroup.
 template <typename T>
-__global__ __launch_bounds__(256) void columns_sum_kernel(ColumnJobs<T> jobs) {
-  const ColumnJob<T>& j = jobs.job[blockIdx.y];
+__device__ __forceinline__ void add_columns(const ColumnJobs<T>& jobs, const ColumnJob<T>& j, int block) {
   __shared__ float sums[8][33], tops[8][33];
   const int lane = threadIdx.x & 31, group = threadIdx.x >> 5, cols = j.from.cols;
-  if (blockIdx.x + 1 == gridDim.x) {
-    if (!j.one) return;
-    float top = 0.0f;
-#pragma unroll 8
-    for (int64_t i = threadIdx.x; i < (int64_t)cols * jobs.parts; i += 256) top = fmaxf(top, j.largest[i]);
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
-    if (lane_id() == 0) tops[0][wave_id()] = top;
-    __syncthreads();
-    if (threadIdx.x == 0) *j.exps = scale_exponent(fmaxf(fmaxf(tops[0][0], tops[0][1]), fmaxf(tops[0][2], tops[0][3])));
-    return;
-  }
-  const int c = blockIdx.x * 32 + lane;
-  if ((int)blockIdx.x * 32 >= cols || jobs.parts == 1) return;
+  const int c = block * 32 + lane;
+  if (block * 32 >= cols) return;
   float s = 0.0f, top = 0.0f;
   if (c < cols) {
     if (j.total)
@@ -476,6 +475,22 @@ __global__ __launch_bounds__(256) void columns_sum_kernel(ColumnJobs<T> jobs) {
   }
   if (j.total) j.total[c] = (T)s;
   if (j.exps && !j.one) j.exps[c] = scale_exponent(top);
+}
+template <typename T>
+__global__ __launch_bounds__(256) void columns_sum_kernel(ColumnJobs<T> jobs) {
+  add_columns(jobs, jobs.job[blockIdx.y], blockIdx.x);
+}
+template <typename T, bool SLOPED>
+__global__ __launch_bounds__(256) void lay_kernel(Jobs<T> jobs) {
+  lay<T, SLOPED>(jobs, blockIdx.x);
+}
+// The same for d in half, and behind it the sums of its columns.  (With a launch in between that finds the scale and adds the columns the backward pass
+// of 700 x 650 by 1300 took 45 us, 2240 x 1024 by 1024 53; so 30.5 and 43.)
+template <typename T>
+__global__ __launch_bounds__(256) void lay_and_add_kernel(Jobs<T> jobs, ColumnJobs<T> beside) {
+  const int own = jobs.first[jobs.count];
+  if ((int)blockIdx.x >= own) return add_columns(beside, beside.job[0], blockIdx.x - own);
+  lay<T, true>(jobs, blockIdx.x);
 }
 
 // ---- workspaces
@@ -555,7 +570,7 @@ bool in_place(const Source<T>& m) {
 }
 template <typename T>
 void add_job(Jobs<T>& jobs, const Source<T>& from, const Laid& to, Scale scale, const Laid& also = Laid{}) {
-  jobs.job[jobs.count] = {from, to, also, scale};
+  jobs.job[jobs.count] = {from, to, also, scale, nullptr, 0};
   jobs.first[jobs.count + 1] = jobs.first[jobs.count] + (int)div_up(from.rows, 4);
   ++jobs.count;
 }
@@ -728,10 +743,10 @@ hipError_t launch_linear_grad(const LinearGradArgs& a, hipStream_t s) {
       const int width = job.to.p ? job.to.padded : job.from.cols;
       widest = width > widest ? width : widest;
     };
-    const bool d_scales = kFloat ? a.dW != nullptr : scaled && products, d_here = d_laid && !scaled;
+    const bool d_scales = kFloat ? a.dW != nullptr : scaled && products, d_here = d_laid && !scaled, one = d_scales && !kFloat;
     if (a.dbias || d_scales || d_here)
       column_job({d, a.dbias ? room.sums : nullptr, d_scales ? room.tops[0] : nullptr, d_here ? room.d : Laid{}, (T*)a.dbias,
-                  d_scales ? room.d_columns.exps : nullptr, d_scales && !kFloat});
+                  d_scales ? room.d_columns.exps : nullptr, one});
     if (kFloat && a.dW) column_job({x, nullptr, room.tops[1], Laid{}, nullptr, room.x.exps, false});
     if (kFloat && a.dx) column_job({W, nullptr, room.tops[2], Laid{}, nullptr, room.W.exps, false});
     Jobs<T> jobs{};
@@ -752,12 +767,26 @@ hipError_t launch_linear_grad(const LinearGradArgs& a, hipStream_t s) {
       if (sloped) columns_kernel<T, true><<<grid, dim3(256), 0, s>>>(columns, beside);
       else columns_kernel<T, false><<<grid, dim3(256), 0, s>>>(columns, beside);
       if ((e = hipGetLastError()) != hipSuccess) return e;
-      if (columns.parts > 1 ? a.dbias || scaled : !kFloat && d_scales) {
-        columns_sum_kernel<T><<<dim3((unsigned)div_up(widest, 32) + 1, (unsigned)count), dim3(256), 0, s>>>(columns);
+      const bool to_add = columns.parts > 1 && (a.dbias || scaled);
+      if (one) {
+        if constexpr (std::is_same<T, f16>::value) {
+          jobs.job[0].tops = room.tops[0];
+          jobs.job[0].top_count = columns.parts * columns.blocks;
+          const int64_t sum_blocks = to_add && a.dbias ? div_up(a.n, 32) : 0;
+          lay_and_add_kernel<T><<<dim3((unsigned)(jobs.first[jobs.count] + sum_blocks)), dim3(256), 0, s>>>(jobs, columns);
+          if ((e = hipGetLastError()) != hipSuccess) return e;
+        }
+      } else if (to_add) {
+        columns_sum_kernel<T><<<dim3((unsigned)div_up(widest, 32), (unsigned)count), dim3(256), 0, s>>>(columns);
         if ((e = hipGetLastError()) != hipSuccess) return e;
       }
     }
-    if ((!count || scaled) && (e = sloped ? run_jobs<T, true>(jobs, s) : run_jobs<T, false>(jobs, s)) != hipSuccess) return e;
+    // (what was not laid out beside the columns; of 16 bits that is without an activation)
+    if (!count || (scaled && !one)) {
+      if constexpr (kFloat) e = sloped ? run_jobs<T, true>(jobs, s) : run_jobs<T, false>(jobs, s);
+      else e = run_jobs<T, false>(jobs, s);
+      if (e != hipSuccess) return e;
+    }
     if (!products) return hipSuccess;
     auto store_of = [&](void* y, int64_t ld, int M, const int* exp_r, const int* exp_c) {
       LinearStore<T> out{};

@@ -5,7 +5,7 @@ are clipped to [-1, 1]).
     normed = layer_norm(h);  y = h + W2_hat gelu(W1_hat normed + b1) + b2,   W_hat = fake_quantize(W)
 
 `layer_norm` and `linear` are the package's operators with their gradients for torch's autograd; `ResidualBlock.step`
-runs forward, backward and the update: momentum, orthogonalized matrices (as Muon does), plain steps for vectors, clip.
+runs forward, backward and the update: momentum, orthogonalized matrices, plain steps for vectors, clip.
 
     python -m paper_1802_00150_amd.training          # a small run that prints its loss
 """

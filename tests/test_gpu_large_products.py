@@ -79,3 +79,32 @@ def test_orthogonalized_updates(amq, rows, cols):
     # iterates of 11 bits: 1.5e-3 over five steps, beside the rounding of the result
     assert float((got.double() - ref).norm() / ref.norm()) <= 1.5e-3 + half_ulp(torch.bfloat16)
     assert float((got.double() - ref).abs().max()) <= 0.02 * float(ref.abs().max())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32] + HALVES)
+def test_offsets_past_32_bits(amq, dtype):
+    """Rows 2^22 entries apart, the last ones beyond 2^32 entries: the results are those of the same rows side by side."""
+    rows, k, n, apart = 1100, 304, 208, 1 << 22
+
+    def spread(t, first):
+        wide = torch.empty(rows, apart, dtype=dtype, device=DEV)[:, first:first + t.shape[1]]
+        return wide.copy_(t)
+
+    x, dy, W, bias = operand(1, rows, k, dtype), operand(2, rows, n, dtype), operand(3, n, k, dtype, k ** -0.5), operand(4, 1, n, dtype)[0]
+    far_x, far_dy = spread(x, 8), spread(dy, apart - n)
+    assert torch.equal(amq.linear(far_x, W, bias, "relu", far_dy, out=far_dy), amq.linear(x, W, bias, "relu", dy))
+    far_dy.copy_(dy)
+    pre = amq.linear(x, W)
+    far_pre = spread(pre, 16)
+    for got, ref in zip(amq.linear_backward(far_dy, far_x, W, far_pre, "tanh") + amq.linear_backward(far_dy, far_x, W),
+                        amq.linear_backward(dy, x, W, pre, "tanh") + amq.linear_backward(dy, x, W)):
+        assert torch.equal(got, ref)
+    assert torch.equal(amq.orthogonalize(far_x, out=spread(x, 0)), amq.orthogonalize(x))
+    y, mean, rstd = amq.layer_norm(x)
+    far_y, far_mean, far_rstd = amq.layer_norm(far_x, out=spread(x, 0))
+    assert torch.equal(far_y, y) and torch.equal(far_mean, mean) and torch.equal(far_rstd, rstd)
+    g = operand(5, rows, k, dtype)
+    for got, ref in zip(amq.layer_norm_backward(spread(g, 8), far_x, None, mean, rstd), amq.layer_norm_backward(g, x, None, mean, rstd)):
+        assert torch.equal(got, ref)
+    del far_x, far_dy, far_pre, far_y
+    torch.cuda.empty_cache()

@@ -537,9 +537,8 @@ int amq_linear_backward(const void* dy, int64_t ld_dy, const void* x, int64_t ld
  * with coef = {a, b, c} (host); the result has the singular vectors of G and singular values driven towards 1.
  *   G [batch][rows][ld], out [batch][rows][ld_out] of `type`, matrices batch_stride and batch_stride_out elements apart
  *   (0 for densely stacked rows); out may be G itself (same strides).  steps >= 0, eps >= 0 and not both 0 for a zero matrix.
- * Iterates are held as two halves of 11 bits, or as one (bfloat16 data, rows and cols >= 512: the result differs from the exact
- * one by less than the rounding to bfloat16 does), scaled by 2^12: entries of an iterate at 16 and above, which only
- * coefficients that diverge produce, become infinite.
+ * Iterates are held as two halves of 11 bits, scaled by 2^12: entries of an iterate at 16 and above, which only coefficients
+ * that diverge produce, become infinite.
  *   workspace: at least amq_orthogonalize_workspace_bytes(batch, rows, cols, type) bytes, 256-byte aligned.
  */
 size_t amq_orthogonalize_workspace_bytes(int64_t batch, int64_t rows, int64_t cols, int type);

@@ -2,14 +2,13 @@
 //
 // n <= m are the sizes of X (the transpose of G where G is tall).  Per step n^2 m + n^3 + 2 n^2 m operations, since A and
 // A A are symmetric and only tiles on and below the diagonal are computed: bound by the matrix cores from about n = 512 on,
-// by the chain of three dependent launches per step below.  Measured: 16384 x 4096 bfloat16 4.3 ms, 4.5 Pflop (290 us for A, 87 for B,
-// 470 for X, per step: 1060 to 1170 TFLOP/s, but for B, whose rounds are short);
-// two float matrices of 1200 x 300 135 us, 17 launches of 5 to 9.
+// by the chain of three dependent launches per step below.  Measured: 16384 x 4096 bfloat16 14.4 ms for 4.5 Tflop, as three half products
+// 930 TFLOP/s; two float matrices of 1200 x 300 135 us, 17 launches of 5 to 9.
 //
-// Iterates, A and B are held as half values times 2^12, in two planes (22 bits) for float and half data and small matrices,
-// in one for bfloat16 data from n = 512 on.  Singular values stay below about 1.2 with the usual coefficients, so nothing comes near 65504 / 4096 = 16,
-// and half's smallest step is 2^-36 of an entry of 1.  One plane loses 1.4e-3 of the result in the 2-norm over five
-// steps, and the rounding to bfloat16 1.7e-3; two planes lose 3e-7.
+// Iterates, A and B are held as half values times 2^12, in two planes (22 bits).  Singular values stay below about 1.2 with the usual coefficients, so
+// nothing comes near 65504 / 4096 = 16, and half's smallest step is 2^-36 of an entry of 1.  Two planes lose 3e-7 of the result in the 2-norm
+// over five steps.  One plane would lose 1.4e-3, as much as the rounding to bfloat16 (1.7e-3) once more, in a third of the
+// products: 16384 x 4096 took 4.4 ms with one.
 // X lies as G does: of a wide G, X X^T contracts along rows and B X down the columns of X; of a tall one, which is the
 // transpose of X, X X^T contracts down its columns and B X along its rows.
 // The norm is summed in binary64, so that no gradient's scale overflows its square.
@@ -29,23 +28,22 @@ struct __attribute__((packed, aligned(8))) Half4 {
   f16 v[4];
 };
 
-// A matrix of scaled values of one or two halves, [batch][rows][ld]; zeros from `cols` to `padded`, a multiple of 64.
-template <int NP>
+constexpr int kPlanes = 2;
+
+// A matrix of scaled values of two halves, [batch][rows][ld]; zeros from `cols` to `padded`, a multiple of 64.
 struct Planes {
   f16* p;
   int64_t ld, batch;
   int rows, cols, padded;
-  __device__ __forceinline__ f16* at(int z, int row, int col) const { return p + z * batch + row * ld + (NP == 2 ? high_part(col) : col); }
+  __device__ __forceinline__ f16* at(int z, int row, int col) const { return p + z * batch + row * ld + high_part(col); }
   // four values along a row (col a multiple of 4)
   __device__ __forceinline__ f32x4 load(int z, int row, int col) const {
     const f16* q = at(z, row, col);
     const Half4 h = *reinterpret_cast<const Half4*>(q);
-    f32x4 v = {(float)h.v[0], (float)h.v[1], (float)h.v[2], (float)h.v[3]};
-    if constexpr (NP == 2) {
-      const Half4 l = *reinterpret_cast<const Half4*>(q + 32);
+    const Half4 l = *reinterpret_cast<const Half4*>(q + 32);
+    f32x4 v;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] += (float)l.v[i];
-    }
+    for (int i = 0; i < 4; ++i) v[i] = (float)h.v[i] + (float)l.v[i];
     return v;
   }
   __device__ __forceinline__ bool has(int row, int col) const { return row < rows && col < padded; }
@@ -59,7 +57,7 @@ struct Planes {
       l.v[i] = (f16)(s - (float)h.v[i]);
     }
     *reinterpret_cast<Half4*>(q) = h;
-    if constexpr (NP == 2) *reinterpret_cast<Half4*>(q + 32) = l;
+    *reinterpret_cast<Half4*>(q + 32) = l;
   }
 };
 
@@ -70,49 +68,46 @@ struct OrthoStore {
   __device__ __forceinline__ Column column(int, int) const { return {}; }
 };
 // A = X X^T, both triangles from the lower tiles.
-template <int NP>
 struct GramStore : OrthoStore {
   static constexpr bool kTransposed = true;
-  Planes<NP> A;
-  explicit GramStore(const Planes<NP>& a) : A(a) {}
+  Planes A;
+  explicit GramStore(const Planes& a) : A(a) {}
   __device__ __forceinline__ f32x4 fetch(int, int, int) const { return f32x4{}; }
   __device__ __forceinline__ void put(int z, int m, int n, f32x4 v, const Column&, const f32x4&) const {
     if (A.has(m, n)) A.store(z, m, n, v * kInvScale);
   }
 };
 // B = b A + c A A, A being symmetric as well.
-template <int NP>
 struct PolynomialStore : OrthoStore {
   static constexpr bool kTransposed = true;
-  Planes<NP> A, B;
+  Planes A, B;
   float b, c;
-  PolynomialStore(const Planes<NP>& a_, const Planes<NP>& b_, float fb, float fc) : A(a_), B(b_), b(fb), c(fc) {}
+  PolynomialStore(const Planes& a_, const Planes& b_, float fb, float fc) : A(a_), B(b_), b(fb), c(fc) {}
   __device__ __forceinline__ f32x4 fetch(int z, int m, int n) const { return A.has(m, n) ? A.load(z, m, n) : f32x4{}; }
   __device__ __forceinline__ void put(int z, int m, int n, f32x4 v, const Column&, const f32x4& a) const {
     if (B.has(m, n)) B.store(z, m, n, a * b + v * (c * kInvScale));
   }
 };
 // X = a X + B X.  (Not in place: X is an operand of the product.)
-template <int NP>
 struct UpdateStore : OrthoStore {
   static constexpr bool kTransposed = false;
-  Planes<NP> X, next;
+  Planes X, next;
   float a;
-  UpdateStore(const Planes<NP>& x, const Planes<NP>& n, float fa) : X(x), next(n), a(fa) {}
+  UpdateStore(const Planes& x, const Planes& n, float fa) : X(x), next(n), a(fa) {}
   __device__ __forceinline__ f32x4 fetch(int z, int m, int n) const { return X.has(m, n) ? X.load(z, m, n) : f32x4{}; }
   __device__ __forceinline__ void put(int z, int m, int n, f32x4 v, const Column&, const f32x4& x) const {
     if (X.has(m, n)) next.store(z, m, n, x * a + v * kInvScale);
   }
 };
 // The last X.
-template <int NP, typename T>
+template <typename T>
 struct ResultStore : OrthoStore {
   static constexpr bool kTransposed = false;
-  Planes<NP> X;
+  Planes X;
   T* out;
   int64_t ld, batch;
   float a;
-  ResultStore(const Planes<NP>& x, T* o, int64_t l, int64_t b, float fa) : X(x), out(o), ld(l), batch(b), a(fa) {}
+  ResultStore(const Planes& x, T* o, int64_t l, int64_t b, float fa) : X(x), out(o), ld(l), batch(b), a(fa) {}
   __device__ __forceinline__ f32x4 fetch(int z, int m, int n) const { return X.has(m, n) ? X.load(z, m, n) : f32x4{}; }
   __device__ __forceinline__ void put(int z, int m, int n, f32x4 v, const Column&, const f32x4& x) const {
     if (m >= X.rows || n >= X.cols) return;
@@ -172,8 +167,8 @@ __device__ __forceinline__ float inverse_norm(const double* parts, int z, int co
 }
 
 // X_0: 8 numbers per lane, rows dealt to the workgroups.  Bound by memory: 16384 x 4096 bfloat16 (268 MB) 45 us = 6.0 TB/s.
-template <typename T, int NP>
-__global__ __launch_bounds__(256) void ortho_begin_kernel(Gradient<T> G, const double* parts, int count, float eps, Planes<NP> X) {
+template <typename T>
+__global__ __launch_bounds__(256) void ortho_begin_kernel(Gradient<T> G, const double* parts, int count, float eps, Planes X) {
   __shared__ double scratch[4];
   const int z = blockIdx.z;
   const float scale = inverse_norm(parts, z, count, eps, scratch) * kScale;
@@ -209,13 +204,13 @@ struct Room {
   int64_t n, m;
   size_t total;
 };
-ProductPlan gram_plan(const Room& r, int planes, int64_t batch) { return plan_product(r.n, r.n, r.m, planes, batch, true); }
-ProductPlan polynomial_plan(const Room& r, int planes, int64_t batch) { return plan_product(r.n, r.n, r.n, planes, batch, true); }
-ProductPlan update_plan(const Room& r, bool tall, int planes, int64_t batch) {
-  return plan_product(tall ? r.m : r.n, tall ? r.n : r.m, r.n, planes, batch, false);
+ProductPlan gram_plan(const Room& r, int64_t batch) { return plan_product(r.n, r.n, r.m, kPlanes, batch, true); }
+ProductPlan polynomial_plan(const Room& r, int64_t batch) { return plan_product(r.n, r.n, r.n, kPlanes, batch, true); }
+ProductPlan update_plan(const Room& r, bool tall, int64_t batch) {
+  return plan_product(tall ? r.m : r.n, tall ? r.n : r.m, r.n, kPlanes, batch, false);
 }
 
-Room room_of(void* ws, int64_t batch, int64_t rows, int64_t cols, int planes) {
+Room room_of(void* ws, int64_t batch, int64_t rows, int64_t cols) {
   Room r{};
   r.n = rows < cols ? rows : cols;
   r.m = rows < cols ? cols : rows;
@@ -226,35 +221,31 @@ Room room_of(void* ws, int64_t batch, int64_t rows, int64_t cols, int planes) {
     off += (bytes + 255) & ~size_t(255);
     return p;
   };
-  const size_t value = sizeof(f16) * (size_t)planes * batch;
+  const size_t value = sizeof(f16) * (size_t)kPlanes * batch;
   for (f16*& x : r.X) x = (f16*)take(value * rows * pad64(cols));
   r.A = (f16*)take(value * r.n * pad64(r.n));
   r.B = (f16*)take(value * r.n * pad64(r.n));
   r.parts = (double*)take(sizeof(double) * kNormParts * (size_t)batch);
-  size_t most = gram_plan(r, planes, batch).part_bytes;
-  for (size_t b : {polynomial_plan(r, planes, batch).part_bytes, update_plan(r, rows > cols, planes, batch).part_bytes})
+  size_t most = gram_plan(r, batch).part_bytes;
+  for (size_t b : {polynomial_plan(r, batch).part_bytes, update_plan(r, rows > cols, batch).part_bytes})
     if (b > most) most = b;
   r.part = (float*)take(most);
   r.total = off;
   return r;
 }
 
-// One plane's error grows as matrices shrink (2.0e-3 of a result in bfloat16 at n = 512, 2.4e-3 at n = 64, of which the
-// rounding is 1.7e-3), while small ones are bound by their launches and two planes cost them nothing.
-int planes_of(int type, int64_t rows, int64_t cols) { return type == AMQ_BF16 && (rows < cols ? rows : cols) >= 512 ? 1 : 2; }
-
-template <typename T, int NP>
+template <typename T>
 hipError_t run(const OrthoArgs& o, hipStream_t s) {
-  const Room r = room_of(o.ws, o.batch, o.rows, o.cols, NP);
+  const Room r = room_of(o.ws, o.batch, o.rows, o.cols);
   const bool tall = o.rows > o.cols;
   const Gradient<T> G{(const T*)o.G, o.ld_g, o.stride_g, o.rows, o.cols};
   T* out = (T*)o.out;
   auto planes = [&](f16* p, int64_t rows, int64_t cols) {
     const int64_t padded = pad64(cols);
-    return Planes<NP>{p, NP * padded, rows * NP * padded, (int)rows, (int)cols, (int)padded};
+    return Planes{p, kPlanes * padded, rows * kPlanes * padded, (int)rows, (int)cols, (int)padded};
   };
-  const Planes<NP> X[2] = {planes(r.X[0], o.rows, o.cols), planes(r.X[1], o.rows, o.cols)};
-  const Planes<NP> A = planes(r.A, r.n, r.n), B = planes(r.B, r.n, r.n);
+  const Planes X[2] = {planes(r.X[0], o.rows, o.cols), planes(r.X[1], o.rows, o.cols)};
+  const Planes A = planes(r.A, r.n, r.n), B = planes(r.B, r.n, r.n);
 
   const int64_t pieces = div_up(o.cols, 256 * kPer16<T>) * o.rows;
   const int count = (int)(pieces < kNormParts ? pieces : kNormParts);
@@ -267,10 +258,10 @@ hipError_t run(const OrthoArgs& o, hipStream_t s) {
     return hipGetLastError();
   }
   const int64_t begin = div_up(o.rows * (int64_t)(X[0].padded / 8), 256);
-  ortho_begin_kernel<T, NP><<<dim3((unsigned)(begin < 2048 ? begin : 2048), 1, (unsigned)o.batch), dim3(256), 0, s>>>(G, r.parts, count, o.eps, X[0]);
+  ortho_begin_kernel<T><<<dim3((unsigned)(begin < 2048 ? begin : 2048), 1, (unsigned)o.batch), dim3(256), 0, s>>>(G, r.parts, count, o.eps, X[0]);
   if ((e = hipGetLastError()) != hipSuccess) return e;
 
-  auto args = [&](const Planes<NP>& rows, bool rows_down, const Planes<NP>& cols, bool cols_down, int64_t k, bool lower) {
+  auto args = [&](const Planes& rows, bool rows_down, const Planes& cols, bool cols_down, int64_t k, bool lower) {
     MatmulArgs g{};
     // (of an operand whose k runs down columns the padding counts as rows: zeros, and a multiple of 8)
     g.r = {rows.p, rows.ld, rows.batch, rows_down ? rows.padded : rows.rows};
@@ -281,20 +272,20 @@ hipError_t run(const OrthoArgs& o, hipStream_t s) {
     g.lower = lower;
     return g;
   };
-  const ProductPlan gram = gram_plan(r, NP, o.batch), polynomial = polynomial_plan(r, NP, o.batch), update = update_plan(r, tall, NP, o.batch);
+  const ProductPlan gram = gram_plan(r, o.batch), polynomial = polynomial_plan(r, o.batch), update = update_plan(r, tall, o.batch);
   for (int i = 0; i < o.steps; ++i) {
-    const Planes<NP>&now = X[i & 1], &next = X[(i + 1) & 1];
+    const Planes&now = X[i & 1], &next = X[(i + 1) & 1];
     const MatmulArgs xx = args(now, tall, now, tall, r.m, true);
-    e = tall ? launch_product<f16, NP, true, true>(xx, gram, o.batch, GramStore<NP>(A), r.part, s)
-             : launch_product<f16, NP, false, false>(xx, gram, o.batch, GramStore<NP>(A), r.part, s);
+    e = tall ? launch_product<f16, kPlanes, true, true>(xx, gram, o.batch, GramStore(A), r.part, s)
+             : launch_product<f16, kPlanes, false, false>(xx, gram, o.batch, GramStore(A), r.part, s);
     if (e != hipSuccess) return e;
-    e = launch_product<f16, NP, false, false>(args(A, false, A, false, r.n, true), polynomial, o.batch, PolynomialStore<NP>(A, B, o.b, o.c), r.part, s);
+    e = launch_product<f16, kPlanes, false, false>(args(A, false, A, false, r.n, true), polynomial, o.batch, PolynomialStore(A, B, o.b, o.c), r.part, s);
     if (e != hipSuccess) return e;
     auto multiply = [&](const auto& store) {
-      return tall ? launch_product<f16, NP, false, false>(args(now, false, B, false, r.n, false), update, o.batch, store, r.part, s)
-                  : launch_product<f16, NP, false, true>(args(B, false, now, true, r.n, false), update, o.batch, store, r.part, s);
+      return tall ? launch_product<f16, kPlanes, false, false>(args(now, false, B, false, r.n, false), update, o.batch, store, r.part, s)
+                  : launch_product<f16, kPlanes, false, true>(args(B, false, now, true, r.n, false), update, o.batch, store, r.part, s);
     };
-    e = i + 1 < o.steps ? multiply(UpdateStore<NP>(now, next, o.a)) : multiply(ResultStore<NP, T>(now, out, o.ld_out, o.stride_out, o.a));
+    e = i + 1 < o.steps ? multiply(UpdateStore(now, next, o.a)) : multiply(ResultStore<T>(now, out, o.ld_out, o.stride_out, o.a));
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
@@ -302,12 +293,11 @@ hipError_t run(const OrthoArgs& o, hipStream_t s) {
 
 }  // namespace
 
-size_t ortho_workspace(int64_t batch, int64_t rows, int64_t cols, int type) { return room_of(nullptr, batch, rows, cols, planes_of(type, rows, cols)).total; }
+size_t ortho_workspace(int64_t batch, int64_t rows, int64_t cols) { return room_of(nullptr, batch, rows, cols).total; }
 
 hipError_t launch_ortho(const OrthoArgs& a, hipStream_t s) {
-  if (a.type == AMQ_F32) return run<float, 2>(a, s);
-  if (a.type == AMQ_F16) return run<f16, 2>(a, s);
-  return planes_of(a.type, a.rows, a.cols) == 1 ? run<bf16, 1>(a, s) : run<bf16, 2>(a, s);
+  if (a.type == AMQ_F32) return run<float>(a, s);
+  return a.type == AMQ_F16 ? run<f16>(a, s) : run<bf16>(a, s);
 }
 
 }  // namespace amq

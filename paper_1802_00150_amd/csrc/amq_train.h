@@ -63,7 +63,7 @@ struct OrthoArgs {
   float a, b, c, eps;
   void* ws;
 };
-size_t ortho_workspace(int64_t batch, int64_t rows, int64_t cols, int type);
+size_t ortho_workspace(int64_t batch, int64_t rows, int64_t cols);
 hipError_t launch_ortho(const OrthoArgs& a, hipStream_t s);
 
 }  // namespace amq

@@ -110,7 +110,7 @@ static bool ortho_supported(int64_t batch, int64_t rows, int64_t cols) { return 
 
 size_t amq_orthogonalize_workspace_bytes(int64_t batch, int64_t rows, int64_t cols, int type) {
   if (batch <= 0 || rows <= 0 || cols <= 0 || !type_ok(type) || !ortho_supported(batch, rows, cols)) return 0;
-  return amq::ortho_workspace(batch, rows, cols, type);
+  return amq::ortho_workspace(batch, rows, cols);
 }
 
 int amq_orthogonalize(const void* G, int64_t batch, int64_t batch_stride, int64_t rows, int64_t cols, int64_t ld, int type,
@@ -123,7 +123,7 @@ int amq_orthogonalize(const void* G, int64_t batch, int64_t batch_stride, int64_
   if (batch_stride_out == 0) batch_stride_out = rows * ld_out;
   // (matrices of the output must not share entries)
   if (batch_stride < 0 || (batch > 1 && batch_stride_out < (rows - 1) * ld_out + cols)) return AMQ_ERR_INVALID;
-  if (!workspace_ok(workspace, workspace_bytes, amq::ortho_workspace(batch, rows, cols, type))) return AMQ_ERR_INVALID;
+  if (!workspace_ok(workspace, workspace_bytes, amq::ortho_workspace(batch, rows, cols))) return AMQ_ERR_INVALID;
   return amq::status_of(amq::launch_ortho({G, out, batch_stride, ld, batch_stride_out, ld_out, (int)batch, (int)rows, (int)cols, type, steps,
                                            coef[0], coef[1], coef[2], eps, workspace},
                                           static_cast<hipStream_t>(stream)));

@@ -463,13 +463,14 @@ hipError_t launch_norm_grad(const NormGradArgs& a0, hipStream_t s) {
     int64_t parts = 0;
     hipError_t e;
     if (!h.waves) {
-      norm_grad_long_kernel<T, P><<<dim3((unsigned)a.rows), dim3(1024), 0, s>>>(a);
-      e = hipGetLastError();
-      if (e == hipSuccess && sums) {
+      // (the columns' sums first: dx may lie where dy or x does)
+      if (sums) {
         parts = a.rows < 64 ? a.rows : 64;
         norm_grad_columns_kernel<T><<<dim3((unsigned)((a.n + 255) / 256), (unsigned)parts), dim3(256), 0, s>>>(a);
-        e = hipGetLastError();
+        if ((e = hipGetLastError()) != hipSuccess) return e;
       }
+      norm_grad_long_kernel<T, P><<<dim3((unsigned)a.rows), dim3(1024), 0, s>>>(a);
+      e = hipGetLastError();
     } else {
       e = with_shape<T>(h, [&](auto w, auto nv) {
         constexpr int W = decltype(w)::value, NV = decltype(nv)::value, kRows = grad_rows(W, NV * kPer16<T>);

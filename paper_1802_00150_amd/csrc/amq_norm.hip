@@ -9,7 +9,7 @@
 // of squares, since the entries are there anyway.  Workgroups walk over rows, with the parameters, and in the backward pass
 // the columns' sums of dy z and dy, in registers; those leave one partial row of sums per workgroup, added up by a second
 // launch in a fixed order, so results do not depend on the order of execution.  Statistics and sums are binary32.
-// Longer rows are read once per sum (general kernels at the end).
+// Rows of less than 16 bytes belong to a lane each; rows of more than 16384 entries are read once per sum (kernels at the end).
 //
 // Measured (bytes read and written once, of a large copy's 5.1 TB/s): forward 8960 x 1024 half 7.7 us = 4.7 TB/s, 35840 x 1024
 // float 6.3 TB/s; backward 8960 x 1500 bfloat16 26.9 us = 3.0 TB/s, of which 6.3 are the parameters' sums, 35840 x 1024 float
@@ -279,29 +279,104 @@ __global__ __launch_bounds__(grad_rows(W, NV * kPer16<T>) * W * 64) void norm_gr
   }
 }
 
-// Rows of any length, one workgroup per row, the row read once per sum and once for the output.
+// Rows of less than 16 bytes, one per lane: 10^6 rows of 4 bfloat16 entries 8.7 us, backward 26.5 (of which 256 workgroups' loads, one row of each lane
+// under way, are the most).
+template <typename T, typename P>
+__global__ __launch_bounds__(256) void norm_short_kernel(NormArgs a) {
+  constexpr int V = kPer16<T>;
+  float w[V], b[V];
+  load_params<P, V>((const P*)a.weight, 0, a.n, 1.0f, w);
+  load_params<P, V>((const P*)a.bias, 0, a.n, 0.0f, b);
+  const float inv_n = 1.0f / (float)a.n;
+  for (int64_t row = (int64_t)blockIdx.x * 256 + threadIdx.x; row < a.rows; row += (int64_t)gridDim.x * 256) {
+    float x[V], s = 0.0f, q = 0.0f;
+    load16((const T*)a.x + row * a.ld_x, a.n, x);  // zeros past the end
+#pragma unroll
+    for (int i = 0; i < V; ++i) s += x[i];
+    const float mean = s * inv_n;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      x[i] = i < a.n ? x[i] - mean : 0.0f;
+      q = fmaf(x[i], x[i], q);
+    }
+    const float rstd = 1.0f / sqrtf(q * inv_n + a.eps);
+#pragma unroll
+    for (int i = 0; i < V; ++i) x[i] = fmaf(x[i] * rstd, w[i], b[i]);
+    store16((T*)a.y + row * a.ld_y, a.n, x);
+    if (a.mean) a.mean[row] = mean;
+    if (a.rstd) a.rstd[row] = rstd;
+  }
+}
+template <typename T, typename P>
+__global__ __launch_bounds__(256) void norm_grad_short_kernel(NormGradArgs a) {
+  constexpr int V = kPer16<T>;
+  __shared__ float sums[4][2 * V];
+  float w[V], dw[V], db[V];
+  load_params<P, V>((const P*)a.weight, 0, a.n, 1.0f, w);
+#pragma unroll
+  for (int i = 0; i < V; ++i) dw[i] = db[i] = 0.0f;
+  const float inv_n = 1.0f / (float)a.n;
+  for (int64_t row = (int64_t)blockIdx.x * 256 + threadIdx.x; row < a.rows; row += (int64_t)gridDim.x * 256) {
+    float z[V], d[V], s = 0.0f, q = 0.0f;
+    load16((const T*)a.x + row * a.ld_x, a.n, z);
+    load16((const T*)a.dy + row * a.ld_dy, a.n, d);  // zeros past the end: nothing of them counts
+    const float mean = a.mean[row], rstd = a.rstd[row];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      z[i] = i < a.n ? (z[i] - mean) * rstd : 0.0f;
+      dw[i] = fmaf(d[i], z[i], dw[i]);
+      db[i] += d[i];
+      d[i] *= w[i];
+      s += d[i];
+      q = fmaf(d[i], z[i], q);
+    }
+    s *= inv_n;
+    q *= inv_n;
+#pragma unroll
+    for (int i = 0; i < V; ++i) d[i] = rstd * (d[i] - s - z[i] * q);
+    store16((T*)a.dx + row * a.ld_dx, a.n, d);
+  }
+  if (!a.part) return;
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const float u = sum64(dw[i]), v = sum64(db[i]);
+    if (lane_id() == 0) {
+      sums[wave_id()][i] = u;
+      sums[wave_id()][V + i] = v;
+    }
+  }
+  __syncthreads();
+  const int i = threadIdx.x % V;
+  if (threadIdx.x < 2 * V && i < a.n)
+    a.part[((int64_t)blockIdx.x * 2 + threadIdx.x / V) * a.n + i] =
+        sums[0][threadIdx.x] + sums[1][threadIdx.x] + sums[2][threadIdx.x] + sums[3][threadIdx.x];
+}
+
+// Rows of any length, a workgroup for each, read once per sum and once for the output.
 template <typename T, typename P>
 __global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs a) {
   __shared__ float slots[32][2];
   int turn = 0;
-  const T* px = (const T*)a.x + (int64_t)blockIdx.x * a.ld_x;
-  T* py = (T*)a.y + (int64_t)blockIdx.x * a.ld_y;
-  float s = 0.0f;
-  for (int c = threadIdx.x; c < a.n; c += 1024) s += (float)px[c];
-  const float mean = row_sum<16>(s, slots, turn) / (float)a.n;
-  s = 0.0f;
-  for (int c = threadIdx.x; c < a.n; c += 1024) {
-    const float d = (float)px[c] - mean;
-    s = fmaf(d, d, s);
-  }
-  const float rstd = 1.0f / sqrtf(row_sum<16>(s, slots, turn) / (float)a.n + a.eps);
-  for (int c = threadIdx.x; c < a.n; c += 1024) {
-    const float w = a.weight ? (float)((const P*)a.weight)[c] : 1.0f, b = a.bias ? (float)((const P*)a.bias)[c] : 0.0f;
-    py[c] = (T)fmaf(((float)px[c] - mean) * rstd, w, b);
-  }
-  if (threadIdx.x == 0) {
-    if (a.mean) a.mean[blockIdx.x] = mean;
-    if (a.rstd) a.rstd[blockIdx.x] = rstd;
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const T* px = (const T*)a.x + row * a.ld_x;
+    T* py = (T*)a.y + row * a.ld_y;
+    float s = 0.0f;
+    for (int c = threadIdx.x; c < a.n; c += 1024) s += (float)px[c];
+    const float mean = row_sum<16>(s, slots, turn) / (float)a.n;
+    s = 0.0f;
+    for (int c = threadIdx.x; c < a.n; c += 1024) {
+      const float d = (float)px[c] - mean;
+      s = fmaf(d, d, s);
+    }
+    const float rstd = 1.0f / sqrtf(row_sum<16>(s, slots, turn) / (float)a.n + a.eps);
+    for (int c = threadIdx.x; c < a.n; c += 1024) {
+      const float w = a.weight ? (float)((const P*)a.weight)[c] : 1.0f, b = a.bias ? (float)((const P*)a.bias)[c] : 0.0f;
+      py[c] = (T)fmaf(((float)px[c] - mean) * rstd, w, b);
+    }
+    if (threadIdx.x == 0) {
+      if (a.mean) a.mean[row] = mean;
+      if (a.rstd) a.rstd[row] = rstd;
+    }
   }
 }
 
@@ -309,22 +384,23 @@ template <typename T, typename P>
 __global__ __launch_bounds__(1024) void norm_grad_long_kernel(NormGradArgs a) {
   __shared__ float slots[32][2];
   int turn = 0;
-  const int64_t row = blockIdx.x;
-  const T *px = (const T*)a.x + row * a.ld_x, *pd = (const T*)a.dy + row * a.ld_dy;
-  T* po = (T*)a.dx + row * a.ld_dx;
-  const float mean = a.mean[row], rstd = a.rstd[row];
-  float s = 0.0f, q = 0.0f;
-  for (int c = threadIdx.x; c < a.n; c += 1024) {
-    const float g = (float)pd[c] * (a.weight ? (float)((const P*)a.weight)[c] : 1.0f);
-    s += g;
-    q = fmaf(g, ((float)px[c] - mean) * rstd, q);
-  }
-  row_sum2<16>(s, q, slots, turn);
-  s /= (float)a.n;
-  q /= (float)a.n;
-  for (int c = threadIdx.x; c < a.n; c += 1024) {
-    const float g = (float)pd[c] * (a.weight ? (float)((const P*)a.weight)[c] : 1.0f);
-    po[c] = (T)(rstd * (g - s - ((float)px[c] - mean) * rstd * q));
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const T *px = (const T*)a.x + row * a.ld_x, *pd = (const T*)a.dy + row * a.ld_dy;
+    T* po = (T*)a.dx + row * a.ld_dx;
+    const float mean = a.mean[row], rstd = a.rstd[row];
+    float s = 0.0f, q = 0.0f;
+    for (int c = threadIdx.x; c < a.n; c += 1024) {
+      const float g = (float)pd[c] * (a.weight ? (float)((const P*)a.weight)[c] : 1.0f);
+      s += g;
+      q = fmaf(g, ((float)px[c] - mean) * rstd, q);
+    }
+    row_sum2<16>(s, q, slots, turn);
+    s /= (float)a.n;
+    q /= (float)a.n;
+    for (int c = threadIdx.x; c < a.n; c += 1024) {
+      const float g = (float)pd[c] * (a.weight ? (float)((const P*)a.weight)[c] : 1.0f);
+      po[c] = (T)(rstd * (g - s - ((float)px[c] - mean) * rstd * q));
+    }
   }
 }
 
@@ -371,7 +447,7 @@ __global__ __launch_bounds__(1024) void norm_grad_sum_kernel(const float* part, 
 
 // Waves per row and 16-byte pieces per lane.
 struct Shape {
-  int waves, pieces;  // waves 0: the general kernels (rows of less than 16 bytes too)
+  int waves, pieces;  // waves 0: rows read once per sum; pieces 0 too: a row per lane
 };
 // 16 entries per lane at most: with 32 the backward pass needs more than 256 registers.  Few rows go to four waves each from 512 entries on, where the row's latency counts.
 constexpr int kPerLane = 16;
@@ -384,7 +460,7 @@ Shape shape_of(int64_t rows, int n, int per16) {
     if (n <= 256 * p * per16) return {4, p};
   if (n <= 512 * kPerLane) return {8, most};
   if (n <= 1024 * kPerLane) return {16, most};
-  return {0, 0};
+  return {0, 1};
 }
 
 template <typename F>
@@ -417,6 +493,7 @@ int64_t even_blocks(int64_t tasks, int64_t most) {
 }
 
 constexpr int64_t kMostParts = 256;  // one workgroup per compute unit: more partial rows cost more than they hide
+constexpr int64_t kMostLong = 2048;  // workgroups of the kernels for long rows: four rounds of the card
 
 }  // namespace
 
@@ -425,9 +502,9 @@ int norm_grad_parts(int64_t rows, int n) {
   int64_t parts = 1;
   for (int per16 : {4, 8}) {
     const Shape h = shape_of(rows, n, per16);
-    const int at_a_time = grad_rows(h.waves, h.pieces * per16);
+    const int at_a_time = h.waves ? grad_rows(h.waves, h.pieces * per16) : 256;
     const int64_t tasks = (rows + at_a_time - 1) / at_a_time;
-    const int64_t p = h.waves ? even_blocks(tasks, kMostParts) : (rows < 64 ? rows : 64);
+    const int64_t p = h.waves || !h.pieces ? even_blocks(tasks, kMostParts) : (rows < 64 ? rows : 64);
     parts = p > parts ? p : parts;
   }
   return (int)parts;
@@ -439,7 +516,8 @@ hipError_t launch_norm(const NormArgs& a, hipStream_t s) {
     using P = decltype(p);
     const Shape h = shape_of(a.rows, a.n, kPer16<T>);
     if (!h.waves) {
-      norm_long_kernel<T, P><<<dim3((unsigned)a.rows), dim3(1024), 0, s>>>(a);
+      if (!h.pieces) norm_short_kernel<T, P><<<dim3((unsigned)even_blocks((a.rows + 255) / 256, 2048)), dim3(256), 0, s>>>(a);
+      else norm_long_kernel<T, P><<<dim3((unsigned)even_blocks(a.rows, kMostLong)), dim3(1024), 0, s>>>(a);
       return hipGetLastError();
     }
     return with_shape<T>(h, [&](auto w, auto nv) {
@@ -462,14 +540,18 @@ hipError_t launch_norm_grad(const NormGradArgs& a0, hipStream_t s) {
     const Shape h = shape_of(a.rows, a.n, kPer16<T>);
     int64_t parts = 0;
     hipError_t e;
-    if (!h.waves) {
+    if (!h.waves && !h.pieces) {
+      parts = even_blocks((a.rows + 255) / 256, kMostParts);
+      norm_grad_short_kernel<T, P><<<dim3((unsigned)parts), dim3(256), 0, s>>>(a);
+      e = hipGetLastError();
+    } else if (!h.waves) {
       // (the columns' sums first: dx may lie where dy or x does)
       if (sums) {
         parts = a.rows < 64 ? a.rows : 64;
         norm_grad_columns_kernel<T><<<dim3((unsigned)((a.n + 255) / 256), (unsigned)parts), dim3(256), 0, s>>>(a);
         if ((e = hipGetLastError()) != hipSuccess) return e;
       }
-      norm_grad_long_kernel<T, P><<<dim3((unsigned)a.rows), dim3(1024), 0, s>>>(a);
+      norm_grad_long_kernel<T, P><<<dim3((unsigned)even_blocks(a.rows, kMostLong)), dim3(1024), 0, s>>>(a);
       e = hipGetLastError();
     } else {
       e = with_shape<T>(h, [&](auto w, auto nv) {

@@ -508,7 +508,8 @@ int amq_layer_norm_backward(const void* dy, int64_t ld_dy, const void* x, int64_
  * bfloat16 and half products go through the matrix cores as they are.  Float operands are scaled by a power of two per
  * row and split into two halves of 11 bits each, so that three half products leave the error of binary32 products; entries
  * 2^28 and more below their row's largest lose digits.  Up to 8 rows (a token's vector) are multiplied in binary32.
- * An infinity or NaN in an operand spoils the results that it enters (NaN, or the infinity) and no others.
+ * An infinity or NaN in an operand spoils the sums that it enters (NaN, or the infinity) and no others; every activation and
+ * every slope passes a NaN on.
  *   workspace: at least amq_linear_workspace_bytes(rows, k, n, type) bytes, 256-byte aligned.
  * The backward pass takes dy [rows][ld_dy]: with d = dy act'(pre), dx = d W, dW = d^T x, dbias = sum over rows of d; any of
  * the three may be NULL.  The residual's gradient is dy itself.  pre may be NULL for AMQ_ACT_NONE.

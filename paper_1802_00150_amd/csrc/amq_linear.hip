@@ -22,7 +22,7 @@
 namespace amq {
 namespace {
 
-// The activations and their slopes through the hardware's exponential and reciprocal (1 ulp each).
+// The activations and their slopes through the hardware's exponential and reciprocal (1 ulp each).  Each passes a NaN on.
 __device__ __forceinline__ float logistic(float z) { return __builtin_amdgcn_rcpf(1.0f + __expf(-z)); }
 // (1 - e) / (1 + e) with e = exp(-2 |z|) loses digits near 0; there the series to z^9, 2e-9 off at 1/4.
 __device__ __forceinline__ float tanh_of(float z) {
@@ -49,7 +49,7 @@ __device__ __forceinline__ void each(float (&v)[V], F f) {
 template <int V>
 __device__ __forceinline__ void activate(float (&v)[V], int act) {
   switch (act) {
-    case AMQ_ACT_RELU: return each(v, [](float z) { return z > 0.0f ? z : 0.0f; });
+    case AMQ_ACT_RELU: return each(v, [](float z) { return z <= 0.0f ? 0.0f : z; });
     case AMQ_ACT_GELU:
       return each(v, [](float z) {
         float density;
@@ -63,7 +63,7 @@ __device__ __forceinline__ void activate(float (&v)[V], int act) {
 template <int V>
 __device__ __forceinline__ void slopes(float (&v)[V], int act) {
   switch (act) {
-    case AMQ_ACT_RELU: return each(v, [](float z) { return z > 0.0f ? 1.0f : 0.0f; });
+    case AMQ_ACT_RELU: return each(v, [](float z) { return z > 0.0f ? 1.0f : z <= 0.0f ? 0.0f : z; });
     case AMQ_ACT_GELU:
       return each(v, [](float z) {
         float density;

@@ -510,7 +510,9 @@ def fake_quantize(W, k, T=2):
     return (_native_module or _load_native()).fake_quantize(W, k, T)
 
 
-# ---- operators of quantization-aware training: float32, bfloat16 or float16 tensors [..., n] (a 2-D tensor's rows may be strided)
+# ---- operators of quantization-aware training: float32, bfloat16 or float16 tensors [..., n] (a 2-D tensor's rows may be strided).
+# They record no graph: with gradients on, layer_norm, linear and orthogonalize refuse operands that require one (training.layer_norm and
+# training.linear are the differentiable forms).
 
 ACTIVATIONS = {None: 0, "none": 0, "relu": 1, "gelu": 2, "silu": 3, "sigmoid": 4, "tanh": 5}
 

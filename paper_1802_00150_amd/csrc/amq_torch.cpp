@@ -7,6 +7,7 @@
 #include <Python.h>
 #include <dlfcn.h>
 
+#include <initializer_list>
 #include <string>
 #include <vector>
 
@@ -486,6 +487,14 @@ PyObject* fake_quantize(PyObject* const* a) {  // W, k, T
 
 // ---- training operators: float32, bfloat16 and float16 tensors, rows of any stride
 
+// These calls record no graph: an operand whose gradient is wanted is refused, rather than the gradient dropped.
+void no_graph(const char* name, const char* instead, std::initializer_list<PyObject*> operands) {
+  if (!at::GradMode::is_enabled()) return;
+  for (PyObject* o : operands)
+    if (THPVariable_Check(o) && THPVariable_Unpack(o).requires_grad())
+      fail(amq_error, std::string(name) + " records no graph, and an operand requires a gradient: " + instead + "call it under torch.no_grad()");
+}
+
 int type_of(const at::Tensor& t) {
   switch (t.scalar_type()) {
     case at::kFloat: return AMQ_F32;
@@ -575,6 +584,7 @@ PyObject* triple(PyObject* a, PyObject* b, PyObject* c) {  // takes the referenc
 }
 
 PyObject* layer_norm(PyObject* const* a) {  // x, weight, bias, eps, out
+  no_graph("layer_norm", "take training.layer_norm, or ", {a[0], a[1], a[2]});
   const at::Tensor& x = tensor(a[0]);
   const int type = type_of(x);
   const Rows r(x);
@@ -626,6 +636,7 @@ Rows matrix(PyObject* o, const char* name, const at::Tensor& like) {
 }
 
 PyObject* linear(PyObject* const* a) {  // x, W, bias, activation, residual, ws, out, pre
+  no_graph("linear", "take training.linear, or ", {a[0], a[1], a[2], a[4]});
   const at::Tensor& x = tensor(a[0]);
   const int type = type_of(x), act = (int)integer(a[3]);
   const Rows r(x), W = matrix(a[1], "W", x);
@@ -686,6 +697,7 @@ struct Stack {
 };
 
 PyObject* orthogonalize(PyObject* const* a) {  // G, steps, a, b, c, eps, ws, out
+  no_graph("orthogonalize", "", {a[0]});
   const at::Tensor& G = tensor(a[0]);
   const int type = type_of(G), steps = (int)integer(a[1]);
   const float coef[3] = {(float)real(a[2]), (float)real(a[3]), (float)real(a[4])}, eps = (float)real(a[5]);

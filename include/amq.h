@@ -513,7 +513,8 @@ int amq_layer_norm_backward(const void* dy, int64_t ld_dy, const void* x, int64_
  *   workspace: at least amq_linear_workspace_bytes(rows, k, n, type) bytes, 256-byte aligned.
  * The backward pass takes dy [rows][ld_dy]: with d = dy act'(pre), dx = d W, dW = d^T x, dbias = sum over rows of d; any of
  * the three may be NULL.  The residual's gradient is dy itself.  pre may be NULL for AMQ_ACT_NONE.
- * With an activation d is rounded to 8 bits (bfloat16) or 11 (half, scaled by a power of two) between the slope and the products.
+ * d of 16-bit data goes through the products as two values, 16 bits of it in bfloat16 and 22 in half (scaled by a power of two);
+ * with AMQ_ACT_RELU or none it has no more digits than dy.
  *   workspace: at least amq_linear_backward_workspace_bytes(rows, k, n, type) bytes, 256-byte aligned.
  */
 #define AMQ_ACT_NONE 0

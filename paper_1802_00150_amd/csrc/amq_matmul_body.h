@@ -8,6 +8,10 @@
 // stage of the contraction; steps past the end are read as zeros, rows past the operand's end as its last ones, and
 // their results dropped.
 //
+// A product may take two passes over k (TWO), the second over the low parts of one operand, which lie apart from its high ones; the
+// other operand's values are read again.  That makes an operand of two parts times one of one, in half the rate.  (Known only at run time, the
+// number of passes cost the products of one 2.5 to 3.5 %.)
+//
 // A workgroup of WR x WC waves owns BM x BN of the result and walks over the stages.  A stage goes from memory to LDS without
 // passing registers (global_load_lds, 16 bytes a lane), into a ring of PLACES stages: up to that many are under way while one is
 // multiplied.  The copy writes consecutive 16-byte pieces of LDS per lane, so the order that keeps
@@ -35,6 +39,7 @@ struct MatmulOperand {
   const void* p;
   int64_t ld, batch;  // strides in 16-bit values: rows of memory, batch entries
   int rows;           // of the operand
+  int64_t second;     // of a product in two passes: how far from the first pass's values the second's lie (0: the same ones)
 };
 // Where value k of a row of numbers of two halves has its high part; the low part follows 32 values on.
 __host__ __device__ inline int64_t high_part(int64_t k) { return (k >> 5) * 64 + (k & 31); }
@@ -42,7 +47,7 @@ struct MatmulArgs {
   MatmulOperand r, c;
   int M, N;              // of the result
   int k;                 // of the contraction
-  int tiles_k;           // stages
+  int pass_k, tiles_k;   // stages of a pass, and in all
   int nbm, nbn;          // tiles of the result
   int tiles_per_split;   // stages for each of gridDim.y
   int lower;             // symmetric result (r = c): only tiles with bm >= bn
@@ -162,7 +167,7 @@ __device__ __forceinline__ void copy_to_lds(const char* from, uint16_t* to) {
 // Columns (k runs down the columns of memory): LDS holds one stage's rows of memory, B operand rows wide.  A fragment is
 // gathered by two transposing reads: 16 lanes read 4 steps of k of 16 operand rows, and get them turned.  Its 32 lanes a cycle
 // cover 8 steps of k; those are given 8 different 32-byte parts of the 64 banks.
-template <typename E, int NP, int B, int kWaves, bool COLUMNS>
+template <typename E, int NP, bool TWO, int B, int kWaves, bool COLUMNS>
 struct Side {
   using v8 = typename MatmulElement<E>::v8;
   typedef short v4s __attribute__((ext_vector_type(4)));
@@ -183,8 +188,9 @@ struct Side {
   const char* base;    // of the tile, uniform
   int64_t stage;       // bytes from one stage to the next
   int64_t line;        // bytes from one row of memory to the next
+  int64_t second;      // bytes from the first pass's values to the second's
   uint32_t off[kOffsets];
-  int k, lane, wave;
+  int k, pass_k, lane, wave;
 
   static __device__ __forceinline__ int swizzle(int row) {  // of 16-byte pieces
     if (!COLUMNS) return (row >> 1) & 7;
@@ -193,9 +199,11 @@ struct Side {
     if (kLine % 256 == 128) return (((row >> 1) & 1) | ((row >> 2) & 2)) << 1;
     return ((row & 3) | ((row >> 1) & 4)) << 1;
   }
-  __device__ __forceinline__ Side(const MatmulOperand& o, int z, int first_row, int k_, int lane_, int wave_) : k(k_), lane(lane_), wave(wave_) {
+  __device__ __forceinline__ Side(const MatmulOperand& o, const MatmulArgs& g, int z, int first_row, int lane_, int wave_)
+      : k(g.k), pass_k(g.pass_k), lane(lane_), wave(wave_) {
     const uint16_t* p = (const uint16_t*)o.p + z * o.batch;
     line = o.ld * 2;
+    second = o.second * 2;
     if constexpr (COLUMNS) {
       base = (const char*)(p + (int64_t)first_row * NP);
       stage = o.ld * kSteps * 2;
@@ -223,7 +231,12 @@ struct Side {
   __device__ __forceinline__ int piece_of(int j) const { return kWhole ? lane % kLanes : ((wave + j * kWaves) * 64 + lane) % kLanes; }
   // Copy j of stage t.  Steps of k past the end are zeros (along rows: to the next multiple of 8 what lies there).
   __device__ __forceinline__ void copy(uint16_t* s, int t, int j) const {
-    const char* from = base + t * stage + (COLUMNS ? j / kOffsets * (kOffsets * kApart) * line : 0);
+    const char* start = base;
+    if (TWO && t >= pass_k) {
+      t -= pass_k;
+      start += second;
+    }
+    const char* from = start + t * stage + (COLUMNS ? j / kOffsets * (kOffsets * kApart) * line : 0);
     const uint32_t at = off[j % kOffsets];
     uint16_t* to = s + (wave + j * kWaves) * 512;
     if ((t + 1) * kSteps > k) {
@@ -264,7 +277,7 @@ struct Side {
 // `id` of `count`: the tile; `split`: the part of the stages; `z`: the batch entry.
 template <int BM, int BN, int KG, int PLACES>
 constexpr int kTileLds = KG * PLACES * (BM + BN) * 64;  // 16-bit values
-template <typename E, int NP, bool RC, bool CC, int BM, int BN, int WR, int WC, int KG, int PLACES, typename Epi>
+template <typename E, int NP, bool TWO, bool RC, bool CC, int BM, int BN, int WR, int WC, int KG, int PLACES, typename Epi>
 __device__ __forceinline__ void matmul_tile(uint16_t* all_lds, const MatmulArgs& g, const Epi& epi, int id, int count, int split, int z) {
   constexpr int kWaves = WR * WC, TM = BM / WR / 16, TN = BN / WC / 16;
   constexpr int kStage = (BM + BN) * 64;  // 16-bit values
@@ -272,8 +285,8 @@ __device__ __forceinline__ void matmul_tile(uint16_t* all_lds, const MatmulArgs&
   static_assert(TM % 2 == 0 && kWaves * 32 * kStride * 4 <= PLACES * kStage * 2, "the result's subtiles take the place of the operands");
   using Element = MatmulElement<E>;
   using v8 = typename Element::v8;
-  using R = Side<E, NP, BM, kWaves, RC>;
-  using C = Side<E, NP, BN, kWaves, CC>;
+  using R = Side<E, NP, TWO, BM, kWaves, RC>;
+  using C = Side<E, NP, TWO, BN, kWaves, CC>;
 
   const int lane = threadIdx.x & 63;
   const int group = KG == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / kWaves;
@@ -290,8 +303,8 @@ __device__ __forceinline__ void matmul_tile(uint16_t* all_lds, const MatmulArgs&
     first += group * each;
     last = first + each - 1;
   }
-  const R r(g.r, z, bm * BM, g.k, lane, wave);
-  const C c(g.c, z, bn * BN, g.k, lane, wave);
+  const R r(g.r, g, z, bm * BM, lane, wave);
+  const C c(g.c, g, z, bn * BN, lane, wave);
   // copy j of stage t of the contraction to its place in the ring; past the end the last stage again, so that as many copies
   // are under way at every wait
   auto copy = [&](int t, int j) __attribute__((always_inline)) {
@@ -420,22 +433,22 @@ __device__ __forceinline__ void matmul_tile(uint16_t* all_lds, const MatmulArgs&
   }
 }
 
-template <typename E, int NP, bool RC, bool CC, int BM, int BN, int WR, int WC, int KG, int PLACES, typename Epi>
+template <typename E, int NP, bool TWO, bool RC, bool CC, int BM, int BN, int WR, int WC, int KG, int PLACES, typename Epi>
 __global__ __launch_bounds__(KG * WR * WC * 64, KG * WR * WC >= 16 ? 4 : 2) void matmul_kernel(MatmulArgs g, Epi epi) {
   __shared__ __align__(256) uint16_t lds[kTileLds<BM, BN, KG, PLACES>];
-  matmul_tile<E, NP, RC, CC, BM, BN, WR, WC, KG, PLACES>(lds, g, epi, blockIdx.x, gridDim.x, blockIdx.y, blockIdx.z);
+  matmul_tile<E, NP, TWO, RC, CC, BM, BN, WR, WC, KG, PLACES>(lds, g, epi, blockIdx.x, gridDim.x, blockIdx.y, blockIdx.z);
 }
 // Two products that do not depend on each other, d W and d^T x, in one launch: the tiles of the one with the longer contraction come
 // first, so that what is left at the end is small. One launch instead of two took the bf16 backward of 700 x 650 by 1300 from 29.5 us
 // to 24.8 and of 20 x 100 by 100 from 14.8 to 10.3; plan_pair() leaves the two apart where that is estimated to be faster.
-template <typename E, int NP, int BM, int BN, int WR, int WC, int KG, int PLACES, typename Epi>
+template <typename E, int NP, bool TWO, int BM, int BN, int WR, int WC, int KG, int PLACES, typename Epi>
 __global__ __launch_bounds__(KG * WR * WC * 64, KG * WR * WC >= 16 ? 4 : 2) void matmul_pair_kernel(MatmulArgs g, Epi epi, MatmulArgs g2, Epi epi2) {
   __shared__ __align__(256) uint16_t lds[kTileLds<BM, BN, KG, PLACES>];
   const int tiles = g.nbm * g.nbn, tiles2 = g2.nbm * g2.nbn;
   const bool ahead = g.k > g2.k;
   const int id = blockIdx.x, i = ahead ? id : id - tiles2, i2 = ahead ? id - tiles : id;
-  if (i2 >= 0 && i2 < tiles2) matmul_tile<E, NP, true, true, BM, BN, WR, WC, KG, PLACES>(lds, g2, epi2, i2, tiles2, 0, 0);
-  else matmul_tile<E, NP, false, true, BM, BN, WR, WC, KG, PLACES>(lds, g, epi, i, tiles, 0, 0);
+  if (i2 >= 0 && i2 < tiles2) matmul_tile<E, NP, TWO, true, true, BM, BN, WR, WC, KG, PLACES>(lds, g2, epi2, i2, tiles2, 0, 0);
+  else matmul_tile<E, NP, TWO, false, true, BM, BN, WR, WC, KG, PLACES>(lds, g, epi, i, tiles, 0, 0);
 }
 
 // ---- contractions split over k: partial results, added up in the order of the splits
@@ -492,35 +505,41 @@ struct ProductPlan {
   size_t part_bytes;    // of partial results (splits > 1)
   double us;            // estimated time
 };
-ProductPlan plan_product(int64_t M, int64_t N, int64_t k, int planes, int64_t batch, bool lower);
-// The best form for two products in one launch (M x N over k, M2 x N2 over k2).
-ProductPlan plan_pair(int64_t M, int64_t N, int64_t k, int64_t M2, int64_t N2, int64_t k2, int planes);
+// Stages of g's contraction, all passes.
+inline void set_stages(MatmulArgs& g, int planes, bool two) {
+  g.pass_k = (int)div_up(g.k, stage_of(planes));
+  g.tiles_k = two ? 2 * g.pass_k : g.pass_k;
+}
 
-template <typename E, int NP, bool RC, bool CC, int BM, int BN, int WR, int WC, int KG, int PLACES, typename Epi>
+ProductPlan plan_product(int64_t M, int64_t N, int64_t k, int planes, int64_t batch, bool lower, int passes = 1);
+// The best form for two products in one launch (M x N over k, M2 x N2 over k2).
+ProductPlan plan_pair(int64_t M, int64_t N, int64_t k, int64_t M2, int64_t N2, int64_t k2, int planes, int passes);
+
+template <typename E, int NP, bool TWO, bool RC, bool CC, int BM, int BN, int WR, int WC, int KG, int PLACES, typename Epi>
 hipError_t launch_tiles(MatmulArgs g, const ProductPlan& p, int batch, const Epi& epi, hipStream_t s) {
-  g.tiles_k = (int)div_up(g.k, stage_of(NP));
+  set_stages(g, NP, TWO);
   g.tiles_per_split = p.tiles_per_split;
   g.nbm = (int)div_up(g.M, BM);
   g.nbn = (int)div_up(g.N, BN);
   const int64_t tiles = g.lower ? (int64_t)g.nbm * (g.nbm + 1) / 2 : (int64_t)g.nbm * g.nbn;
-  matmul_kernel<E, NP, RC, CC, BM, BN, WR, WC, KG, PLACES, Epi><<<dim3((unsigned)tiles, (unsigned)p.splits, (unsigned)batch), dim3(KG * WR * WC * 64), 0, s>>>(g, epi);
+  matmul_kernel<E, NP, TWO, RC, CC, BM, BN, WR, WC, KG, PLACES, Epi><<<dim3((unsigned)tiles, (unsigned)p.splits, (unsigned)batch), dim3(KG * WR * WC * 64), 0, s>>>(g, epi);
   return hipGetLastError();
 }
 
-// The product of g with the tiles of `p`; RC, CC: whether k runs down the columns of the operand.
-template <typename E, int NP, bool RC, bool CC, typename Epi>
+// The product of g with the tiles of `p`; RC, CC: whether k runs down the columns of the operand; TWO: in two passes.
+template <typename E, int NP, bool RC, bool CC, bool TWO = false, typename Epi>
 hipError_t launch_product(const MatmulArgs& g, const ProductPlan& p, int batch, const Epi& epi, float* part, hipStream_t s) {
   auto run = [&](const auto& store) {
     if constexpr (NP == 1)
-      if (p.tile == 256) return launch_tiles<E, NP, RC, CC, 256, 256, 2, 4, 1, 2>(g, p, batch, store, s);
+      if (p.tile == 256) return launch_tiles<E, NP, TWO, RC, CC, 256, 256, 2, 4, 1, 2>(g, p, batch, store, s);
     // (8 waves; with 4 that hold twice the values each 416 us against 287, with 12 or a ring of three places the same)
     if constexpr (NP == 1)
-      if (p.tile == 192) return launch_tiles<E, NP, RC, CC, 192, 192, 2, 4, 1, 2>(g, p, batch, store, s);
-    if (p.tile == 128 && p.groups == 2) return launch_tiles<E, NP, RC, CC, 128, 128, 2, 2, 2, 2>(g, p, batch, store, s);
-    if (p.tile == 128) return launch_tiles<E, NP, RC, CC, 128, 128, 2, 2, 1, 2>(g, p, batch, store, s);
-    if (p.tile == 32) return launch_tiles<E, NP, RC, CC, 32, 32, 1, 1, 8, 2>(g, p, batch, store, s);
-    if (p.groups == 4) return launch_tiles<E, NP, RC, CC, 64, 64, 2, 2, 4, 2>(g, p, batch, store, s);
-    return launch_tiles<E, NP, RC, CC, 64, 64, 2, 2, 1, 3>(g, p, batch, store, s);
+      if (p.tile == 192) return launch_tiles<E, NP, TWO, RC, CC, 192, 192, 2, 4, 1, 2>(g, p, batch, store, s);
+    if (p.tile == 128 && p.groups == 2) return launch_tiles<E, NP, TWO, RC, CC, 128, 128, 2, 2, 2, 2>(g, p, batch, store, s);
+    if (p.tile == 128) return launch_tiles<E, NP, TWO, RC, CC, 128, 128, 2, 2, 1, 2>(g, p, batch, store, s);
+    if (p.tile == 32) return launch_tiles<E, NP, TWO, RC, CC, 32, 32, 1, 1, 8, 2>(g, p, batch, store, s);
+    if (p.groups == 4) return launch_tiles<E, NP, TWO, RC, CC, 64, 64, 2, 2, 4, 2>(g, p, batch, store, s);
+    return launch_tiles<E, NP, TWO, RC, CC, 64, 64, 2, 2, 1, 3>(g, p, batch, store, s);
   };
   if (p.splits == 1) return run(epi);
   const PartialStore store{part, (g.N + 3) & ~3, g.M};
@@ -531,28 +550,29 @@ hipError_t launch_product(const MatmulArgs& g, const ProductPlan& p, int batch, 
   return hipGetLastError();
 }
 
-template <typename E, int NP, int BM, int BN, int WR, int WC, int KG, int PLACES, typename Epi>
+template <typename E, int NP, bool TWO, int BM, int BN, int WR, int WC, int KG, int PLACES, typename Epi>
 hipError_t launch_pair_tiles(MatmulArgs g, const Epi& epi, MatmulArgs g2, const Epi& epi2, hipStream_t s) {
   int64_t tiles[2];
   MatmulArgs* both[2] = {&g, &g2};
   for (int i = 0; i < 2; ++i) {
     MatmulArgs& a = *both[i];
-    a.tiles_k = a.tiles_per_split = (int)div_up(a.k, stage_of(NP));
+    set_stages(a, NP, TWO);
+    a.tiles_per_split = a.tiles_k;
     a.nbm = (int)div_up(a.M, BM);
     a.nbn = (int)div_up(a.N, BN);
     tiles[i] = (int64_t)a.nbm * a.nbn;
   }
-  matmul_pair_kernel<E, NP, BM, BN, WR, WC, KG, PLACES, Epi>
+  matmul_pair_kernel<E, NP, TWO, BM, BN, WR, WC, KG, PLACES, Epi>
       <<<dim3((unsigned)(tiles[0] + tiles[1])), dim3(KG * WR * WC * 64), 0, s>>>(g, epi, g2, epi2);
   return hipGetLastError();
 }
-template <typename E, int NP, typename Epi>
+template <typename E, int NP, bool TWO, typename Epi>
 hipError_t launch_pair(const MatmulArgs& g, const Epi& epi, const MatmulArgs& g2, const Epi& epi2, const ProductPlan& p, hipStream_t s) {
-  if (p.tile == 128 && p.groups == 2) return launch_pair_tiles<E, NP, 128, 128, 2, 2, 2, 2>(g, epi, g2, epi2, s);
-  if (p.tile == 128) return launch_pair_tiles<E, NP, 128, 128, 2, 2, 1, 2>(g, epi, g2, epi2, s);
-  if (p.tile == 32) return launch_pair_tiles<E, NP, 32, 32, 1, 1, 8, 2>(g, epi, g2, epi2, s);
-  if (p.groups == 4) return launch_pair_tiles<E, NP, 64, 64, 2, 2, 4, 2>(g, epi, g2, epi2, s);
-  return launch_pair_tiles<E, NP, 64, 64, 2, 2, 1, 3>(g, epi, g2, epi2, s);
+  if (p.tile == 128 && p.groups == 2) return launch_pair_tiles<E, NP, TWO, 128, 128, 2, 2, 2, 2>(g, epi, g2, epi2, s);
+  if (p.tile == 128) return launch_pair_tiles<E, NP, TWO, 128, 128, 2, 2, 1, 2>(g, epi, g2, epi2, s);
+  if (p.tile == 32) return launch_pair_tiles<E, NP, TWO, 32, 32, 1, 1, 8, 2>(g, epi, g2, epi2, s);
+  if (p.groups == 4) return launch_pair_tiles<E, NP, TWO, 64, 64, 2, 2, 4, 2>(g, epi, g2, epi2, s);
+  return launch_pair_tiles<E, NP, TWO, 64, 64, 2, 2, 1, 3>(g, epi, g2, epi2, s);
 }
 
 }  // namespace amq

@@ -529,10 +529,15 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, out=None):
     return (_native_module or _load_native()).layer_norm(x, weight, bias, eps, out)
 
 
-def layer_norm_backward(dy, x, weight, mean, rstd, param_grads=True, ws=None, out=None):
-    """Gradients dx, dweight, dbias of layer_norm (the last two None without param_grads; of weight's type, or x's if
-    weight is None).  out receives dx and may be dy or x itself."""
-    return (_native_module or _load_native()).layer_norm_backward(dy, x, weight, mean, rstd, bool(param_grads), ws, out)
+def layer_norm_backward(dy, x, weight, mean, rstd, param_grads=True, ws=None, out=None, param_dtype=None):
+    """Gradients dx, dweight, dbias of layer_norm (the last two None without param_grads; of weight's type, or if weight is
+    None of param_dtype: torch.float32 or x's type, which is the default).  out receives dx and may be dy or x itself."""
+    grads = 1 if param_grads else 0
+    if grads and param_dtype is not None and param_dtype != (x if weight is None else weight).dtype:
+        if param_dtype != torch.float32:
+            raise ValueError("param_dtype: expected torch.float32 or the type of x, got %s" % param_dtype)
+        grads = 2
+    return (_native_module or _load_native()).layer_norm_backward(dy, x, weight, mean, rstd, grads, ws, out)
 
 
 def layer_norm_backward_workspace(rows, n, device):

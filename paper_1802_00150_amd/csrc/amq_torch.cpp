@@ -602,17 +602,19 @@ PyObject* layer_norm(PyObject* const* a) {  // x, weight, bias, eps, out
   return triple(y.take(), wrap(mean), wrap(rstd));
 }
 
-PyObject* layer_norm_backward(PyObject* const* a) {  // dy, x, weight, mean, rstd, param_grads, ws, dx
+PyObject* layer_norm_backward(PyObject* const* a) {  // dy, x, weight, mean, rstd, param_grads (1 of weight's or x's type, 2 float32), ws, dx
   const at::Tensor& x = tensor(a[1]);
   const int type = type_of(x);
   const Rows r(x), d(tensor(a[0]), "dy", r.rows, r.n, x);
   const void* w = vector_of(a[2], "weight", r.n, at::kFloat, x.scalar_type(), x);
-  const at::ScalarType pt = w ? tensor(a[2]).scalar_type() : x.scalar_type();
-  const int param_type = w ? type_of(tensor(a[2])) : type;
+  const int64_t grads = integer(a[5]);
+  const at::ScalarType pt = w ? tensor(a[2]).scalar_type() : grads == 2 ? at::kFloat : x.scalar_type();
+  if (grads == 2 && pt != at::kFloat) fail(amq_error, std::string("param_dtype: the weight is ") + dtype_name(pt));
+  const int param_type = w ? type_of(tensor(a[2])) : grads == 2 ? AMQ_F32 : type;
   const at::Tensor &mean = tensor(a[3]), &rstd = tensor(a[4]);
   const float *m = static_cast<const float*>(dev(mean, at::kFloat)), *q = static_cast<const float*>(dev(rstd, at::kFloat));
   if (mean.numel() != r.rows || rstd.numel() != r.rows) fail(PyExc_ValueError, "mean, rstd: expected one value per row");
-  const bool params = integer(a[5]) != 0;
+  const bool params = grads != 0;
   Result dx(a[7], "dx", x.sizes(), r.rows, r.n, x);
   at::Tensor dw, db;
   if (params) {

@@ -27,10 +27,9 @@ class _LayerNorm(torch.autograd.Function):
     def backward(ctx, dy):
         x, weight, bias, mean, rstd = ctx.saved_tensors
         params = ctx.needs_input_grad[1] or ctx.needs_input_grad[2]
-        # without a weight the bias's gradient comes in x's type
-        dx, dw, db = binding.layer_norm_backward(dy.contiguous(), x, weight, mean, rstd, params)
-        return (dx, dw if ctx.needs_input_grad[1] else None,
-                db.to(bias.dtype) if ctx.needs_input_grad[2] else None, None)
+        dx, dw, db = binding.layer_norm_backward(dy.contiguous(), x, weight, mean, rstd, params,
+                                                 param_dtype=bias.dtype if weight is None and params else None)
+        return dx, dw if ctx.needs_input_grad[1] else None, db if ctx.needs_input_grad[2] else None, None
 
 
 def layer_norm(x, weight=None, bias=None, eps=1e-5):

@@ -21,7 +21,8 @@
 namespace amq {
 namespace {
 
-constexpr float kScale = 4096.0f, kInvScale = 1.0f / 4096.0f;
+constexpr int kScaleBits = 12;
+constexpr float kInvScale = 1.0f / 4096.0f;
 constexpr int kNormParts = 1024;  // sums of squares per matrix: four workgroups of 256 per compute unit
 
 struct __attribute__((packed, aligned(8))) Half4 {
@@ -159,11 +160,19 @@ __global__ __launch_bounds__(256) void ortho_norm_kernel(Gradient<T> G, double* 
   if (threadIdx.x == 0) parts[(int64_t)blockIdx.y * kNormParts + blockIdx.x] = s;
 }
 
-// 1 / (|G| + eps) of matrix z from its partial sums, by a whole workgroup of 256.
-__device__ __forceinline__ float inverse_norm(const double* parts, int z, int count, float eps, double* scratch) {
+// 1 / (|G| + eps) of matrix z from its partial sums, by a whole workgroup of 256: as a number in [1/2, 1) and an exponent, since without
+// eps it may be larger than binary32 numbers are.
+struct Factor {
+  float m;
+  int e;
+  __device__ __forceinline__ float times(float v) const { return ldexpf(v, e) * m; }
+};
+__device__ __forceinline__ Factor inverse_norm(const double* parts, int z, int count, float eps, double* scratch) {
   double s = 0.0;
   for (int i = threadIdx.x; i < count; i += 256) s += parts[(int64_t)z * kNormParts + i];
-  return (float)(1.0 / (sqrt(block_sum<4>(s, scratch)) + (double)eps));
+  Factor f;
+  f.m = (float)frexp(1.0 / (sqrt(block_sum<4>(s, scratch)) + (double)eps), &f.e);
+  return f;
 }
 
 // X_0: 8 numbers per lane, rows dealt to the workgroups.  Bound by memory: 16384 x 4096 bfloat16 (268 MB) 45 us = 6.0 TB/s.
@@ -171,7 +180,8 @@ template <typename T>
 __global__ __launch_bounds__(256) void ortho_begin_kernel(Gradient<T> G, const double* parts, int count, float eps, Planes X) {
   __shared__ double scratch[4];
   const int z = blockIdx.z;
-  const float scale = inverse_norm(parts, z, count, eps, scratch) * kScale;
+  Factor scale = inverse_norm(parts, z, count, eps, scratch);
+  scale.e += kScaleBits;
   const T* p = G.p + z * G.batch;
   const int per_row = X.padded / 8;
   const int64_t total = (int64_t)G.rows * per_row;
@@ -180,8 +190,10 @@ __global__ __launch_bounds__(256) void ortho_begin_kernel(Gradient<T> G, const d
     const int col = (int)(i % per_row) * 8;
     float v[8];
     load_params<T, 8>(p, row * G.ld + col, G.cols - col, 0.0f, v);
-    X.store(z, (int)row, col, f32x4{v[0], v[1], v[2], v[3]} * scale);
-    X.store(z, (int)row, col + 4, f32x4{v[4], v[5], v[6], v[7]} * scale);
+#pragma unroll
+    for (float& u : v) u = scale.times(u);
+    X.store(z, (int)row, col, f32x4{v[0], v[1], v[2], v[3]});
+    X.store(z, (int)row, col + 4, f32x4{v[4], v[5], v[6], v[7]});
   }
 }
 
@@ -190,11 +202,11 @@ template <typename T>
 __global__ __launch_bounds__(256) void ortho_scale_kernel(Gradient<T> G, const double* parts, int count, float eps, T* out, int64_t ld, int64_t batch) {
   __shared__ double scratch[4];
   const int z = blockIdx.z;
-  const float scale = inverse_norm(parts, z, count, eps, scratch);
+  const Factor scale = inverse_norm(parts, z, count, eps, scratch);
   const int col = blockIdx.x * 256 + threadIdx.x;
   if (col >= G.cols) return;
   for (int64_t row = blockIdx.y; row < G.rows; row += gridDim.y)
-    out[z * batch + row * ld + col] = (T)((float)G.p[z * G.batch + row * G.ld + col] * scale);
+    out[z * batch + row * ld + col] = (T)scale.times((float)G.p[z * G.batch + row * G.ld + col]);
 }
 
 struct Room {

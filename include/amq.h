@@ -505,9 +505,11 @@ int amq_layer_norm_backward(const void* dy, int64_t ld_dy, const void* x, int64_
  *   bias [n] or NULL, residual [rows][ld_r] or NULL, y [rows][ld_y]; all of `type`, any alignment and stride
  *   pre [rows][ld_pre] or NULL: receives z, rounded to `type`, which the backward pass of an activation takes
  *   y may be the residual itself (same stride).
- * bfloat16 and half products go through the matrix cores as they are.  Float operands are scaled by a power of two per
- * row and split into two halves of 11 bits each, so that three half products leave the error of binary32 products; entries
- * 2^28 and more below their row's largest lose digits.  Up to 8 rows (a token's vector) are multiplied in binary32.
+ * bfloat16 and half products go through the matrix cores as they are.  Float operands of more than 8 rows are scaled by a power of two per
+ * row and split into two halves of 11 bits each, multiplied in three half products.  An entry is held to 2^-23 of itself, or to
+ * 2^-39 of its row's largest where that is more: from 2^-16 of the largest down it has fewer digits (2^-20: 19, 2^-28: 11), which counts
+ * where the other operand is 0 at the large ones.  Of a product of two entries 2^-22 is left out.  (The backward pass: the same, rows being
+ * those of d in dx and the columns of d, x and W where k runs down them.)  Up to 8 rows (a token's vector) are multiplied in binary32.
  * An infinity or NaN in an operand spoils the sums that it enters (NaN, or the infinity) and no others; every activation and
  * every slope passes a NaN on.
  *   workspace: at least amq_linear_workspace_bytes(rows, k, n, type) bytes, 256-byte aligned.

@@ -5,9 +5,10 @@
 // dx, d and x in dW are never transposed.  bfloat16 and half operands whose rows lie on 16 bytes and hold a multiple of 8
 // values are read where they are.  Anything else is laid out first: rows padded with zeros, d multiplied out, and
 // float values scaled by a power of two per row of the operand and split into two halves, 22 bits together.  (A binary32 matrix
-// instruction has 1/16 of the rate of a half one; three half products of split operands have 1/3, with the error of
-// binary32 products.)  The scale puts the row's largest value into [2^14, 2^15), so no product overflows, and half's smallest
-// step is 2^-38 of that value.
+// instruction has 1/16 of the rate of a half one; three half products of split operands have 1/3.)  The scale puts the row's
+// largest value into [2^14, 2^15), so no product overflows.  The first half is off by 2^-11 of a value at most; the second holds that to 2^-12 of
+// the most it can be, or to half of half's smallest step, 2^-25: a value is held to 2^-23 of itself, but to no less than 2^-39 of its row's largest.  In the
+// norm of a result that is the error of binary32 products; a result that only small entries enter has the fewer digits of those.
 //
 // d of 16-bit data is a value of binary32 behind a slope.  It is laid out as two values of the type, the second what the first leaves (16 bits together in
 // bfloat16, 22 in half), and each product takes two passes over its contraction, one for either.  Rounded to one value it cost the gradients

@@ -6,7 +6,7 @@ got = round(ref + e), and the distance of a value to its nearest number of a typ
 import pytest
 import torch
 
-from train_util import DEV, U, slope64
+from train_util import DEV, U, assert_within, rand, slope64
 from test_gpu_linear import inputs
 
 pytestmark = pytest.mark.gpu
@@ -37,3 +37,21 @@ def test_the_gradient_between_slope_and_products(amq, rows, k, n, dtype, act):
         e = share * float(terms.sum().sqrt())
         assert float((got.double() - ref).norm()) <= rounding + 2 * e, (what, float((got.double() - ref).norm()), rounding, e)
     assert float((db.double() - d.sum(0)).norm()) <= float((d.sum(0).to(dtype).double() - d.sum(0)).norm()) + 2 * share * float((d * d).sum().sqrt())
+
+
+@pytest.mark.parametrize("rows", [9, 40, 300])
+@pytest.mark.parametrize("far", [10, 18, 24, 28])
+def test_float_entries_far_below_the_largest_of_their_row(amq, rows, far):
+    """Entries 2^-far of their row's largest, whose own products are all that a result has (W is 0 at the large ones).  An entry of a split
+    operand is off by 2^-23 of itself or 2^-39 of its row's largest; the product of two low parts, 2^-22, is left out."""
+    k, n = 200, 72
+    x, W = rand(far, rows, k), rand(far + 1, n, k)
+    x[:, ::2] *= 2.0 ** -far
+    W[:, 1::2] = 0
+
+    def off(t):
+        return torch.maximum(2.0 ** -23 * t.abs(), 2.0 ** -39 * t.abs().amax(1, keepdim=True)) * (t != 0)
+
+    ref, a, w = x.double() @ W.double().t(), x.double().abs(), W.double().abs()
+    tol = ((k + 16) * U + 2.0 ** -22) * (a @ w.t()) + off(x.double()) @ w.t() + a @ off(W.double()).t() + off(x.double()) @ off(W.double()).t()
+    assert_within(amq.linear(x.to(DEV), W.to(DEV)), ref, tol + U * ref.abs(), "y")

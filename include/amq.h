@@ -474,7 +474,7 @@ int amq_lm_sequence_score(const uint32_t* Ep, const float* alpha_e, int64_t voca
  * "Training").  Data of three types, all arithmetic and every sum in binary32, results rounded once.
  * AMQ_ERR_UNSUPPORTED beyond these limits: rows of 2^20 entries (k and n of a linear layer too); 2^31 - 1 rows of a layer norm, 2^22
  * of a linear layer, 2^20 of an update; 2^38 entries per matrix of a linear layer, whose x, W and dy have strides of at most 2^22; 65535
- * matrices per call.
+ * matrices per call.  AMQ_ERR_INVALID where a result overlaps an operand or another result, but for the cases that are named.
  */
 #define AMQ_F32 0
 #define AMQ_BF16 1
@@ -540,7 +540,8 @@ int amq_linear_backward(const void* dy, int64_t ld_dy, const void* x, int64_t ld
  *   A = X X^T,  X = a X + (b A + c A A) X      (on the transpose where rows > cols)
  * with coef = {a, b, c} (host); the result has the singular vectors of G and singular values driven towards 1.
  *   G [batch][rows][ld], out [batch][rows][ld_out] of `type`, matrices batch_stride and batch_stride_out elements apart
- *   (0 for densely stacked rows); out may be G itself (same strides).  steps >= 0, eps >= 0 and not both 0 for a zero matrix.
+ *   (0 for densely stacked rows); out may be G itself (same strides), and overlap it in any way where steps > 0.
+ *   steps >= 0; eps >= 0, and not 0 for a zero matrix.
  * Iterates are held as two halves of 11 bits, scaled by 2^12: entries of an iterate at 16 and above, which only coefficients
  * that diverge produce, become infinite.
  *   workspace: at least amq_orthogonalize_workspace_bytes(batch, rows, cols, type) bytes, 256-byte aligned.

@@ -23,6 +23,50 @@ bool linear_sizes_supported(int64_t rows, int64_t k, int64_t n) {
   return rows <= kMaxRows && k <= kMaxSize && n <= kMaxSize && rows * k <= kMaxEntries && rows * n <= kMaxEntries && n * k <= kMaxEntries;
 }
 
+// ---- overlap.  A result's entries are written while other workgroups still read the operands.
+// A matrix in memory, in bytes: `rows` pieces of `width`, `step` apart.  (p null: none.)
+struct Extent {
+  uintptr_t p;
+  int64_t rows, width, step;
+};
+Extent matrix(const void* p, int64_t rows, int64_t n, int64_t ld, int type) {
+  const int64_t size = (int64_t)size_of(type);
+  return {reinterpret_cast<uintptr_t>(p), rows, n * size, (rows > 1 ? ld : n) * size};
+}
+Extent vector(const void* p, int64_t n, int type) { return matrix(p, 1, n, n, type); }
+int64_t floor_div(int64_t a, int64_t b) { return a / b - (a % b < 0); }
+// Whether the two have a byte in common.  Columns of one wider matrix (equal steps) take one division, anything else that may meet a division
+// per row.
+bool overlap(const Extent& a, const Extent& b) {
+  if (!a.p || !b.p) return false;
+  const int64_t from = (int64_t)(b.p - a.p);  // where b begins, with a at 0
+  if (from >= (a.rows - 1) * a.step + a.width || from + (b.rows - 1) * b.step + b.width <= 0) return false;
+  if (a.step == b.step && a.rows > 1 && b.rows > 1) {
+    // row i of a meets row i + d of b where -b.width < from + d step < a.width
+    const int64_t d = floor_div(-b.width - from, a.step) + 1;
+    const int64_t last = floor_div(a.width - 1 - from, a.step);
+    return d <= last && d < b.rows && last > -a.rows;
+  }
+  const bool swap = a.rows > b.rows;
+  const Extent &few = swap ? b : a, &many = swap ? a : b;
+  const int64_t begin = swap ? -from : from;  // of `many`, with `few` at 0
+  for (int64_t i = 0; i < few.rows; ++i) {
+    const int64_t at = i * few.step - begin;  // of the row, with `many` at 0
+    // row j of `many` meets it where at - many.width < j step < at + few.width
+    const int64_t j = floor_div(at - many.width, many.step) + 1;
+    if ((j > 0 ? j : 0) * many.step < at + few.width && (j > 0 ? j : 0) < many.rows) return true;
+  }
+  return false;
+}
+// The same entries, one by one.
+bool same(const Extent& a, const Extent& b) { return a.p == b.p && a.rows == b.rows && a.width == b.width && a.step == b.step; }
+template <int N>
+bool meets(const Extent& result, const Extent (&others)[N]) {
+  for (const Extent& o : others)
+    if (overlap(result, o)) return true;
+  return false;
+}
+
 }  // namespace
 
 extern "C" {
@@ -35,6 +79,10 @@ int amq_layer_norm(const void* x, int64_t ld_x, int64_t rows, int64_t n, int typ
       !on_elements(mean, AMQ_F32) || !on_elements(rstd, AMQ_F32))
     return AMQ_ERR_INVALID;
   if (rows > 0x7fffffffLL || n > kMaxSize) return AMQ_ERR_UNSUPPORTED;
+  const Extent in = matrix(x, rows, n, ld_x, type), out = matrix(y, rows, n, ld_y, type), m = vector(mean, rows, AMQ_F32), r = vector(rstd, rows, AMQ_F32);
+  const Extent params[] = {vector(weight, n, param_type), vector(bias, n, param_type)};
+  if ((!same(in, out) && overlap(in, out)) || meets(out, params) || meets(m, params) || meets(r, params) || meets(m, {in, out, r}) || meets(r, {in, out}))
+    return AMQ_ERR_INVALID;
   return amq::status_of(amq::launch_norm({x, weight, bias, y, mean, rstd, rows, ld_x, ld_y, (int)n, type, param_type, eps},
                                          static_cast<hipStream_t>(stream)));
 }
@@ -54,6 +102,12 @@ int amq_layer_norm_backward(const void* dy, int64_t ld_dy, const void* x, int64_
       !on_elements(dweight, param_type) || !on_elements(dbias, param_type) || !on_elements(mean, AMQ_F32) || !on_elements(rstd, AMQ_F32))
     return AMQ_ERR_INVALID;
   if (rows > 0x7fffffffLL || n > kMaxSize) return AMQ_ERR_UNSUPPORTED;
+  const Extent d = matrix(dy, rows, n, ld_dy, type), in = matrix(x, rows, n, ld_x, type), out = matrix(dx, rows, n, ld_dx, type);
+  const Extent m = vector(mean, rows, AMQ_F32), r = vector(rstd, rows, AMQ_F32), w = vector(weight, n, param_type);
+  const Extent dw = vector(dweight, n, param_type), db = vector(dbias, n, param_type);
+  if ((!same(d, out) && overlap(d, out)) || (!same(in, out) && overlap(in, out)) || meets(out, {m, r, w, dw, db}) || meets(dw, {d, in, m, r, w, db}) ||
+      meets(db, {d, in, m, r, w}))
+    return AMQ_ERR_INVALID;
   if ((dweight || dbias) && !workspace_ok(workspace, workspace_bytes, amq_layer_norm_backward_workspace_bytes(rows, n)))
     return AMQ_ERR_INVALID;
   return amq::status_of(amq::launch_norm_grad({dy, x, weight, mean, rstd, dx, dweight, dbias, static_cast<float*>(workspace), rows,
@@ -76,6 +130,9 @@ int amq_linear(const void* x, int64_t ld_x, const void* W, int64_t ld_w, int64_t
       !on_elements(residual, type) || !on_elements(pre, type))
     return AMQ_ERR_INVALID;
   if (!linear_sizes_supported(rows, k, n) || ld_x > kMaxStride || ld_w > kMaxStride) return AMQ_ERR_UNSUPPORTED;
+  const Extent ex = matrix(x, rows, k, ld_x, type), eW = matrix(W, n, k, ld_w, type), eb = vector(bias, n, type), er = matrix(residual, rows, n, ld_r, type);
+  const Extent ey = matrix(y, rows, n, ld_y, type), ep = matrix(pre, rows, n, ld_pre, type);
+  if (meets(ey, {ex, eW, eb, ep}) || meets(ep, {ex, eW, eb, er}) || (!same(ey, er) && overlap(ey, er))) return AMQ_ERR_INVALID;
   if (!workspace_ok(workspace, workspace_bytes, amq::linear_workspace(rows, k, n, type))) return AMQ_ERR_INVALID;
   return amq::status_of(amq::launch_linear({x, W, bias, residual, y, pre, ld_x, ld_w, ld_r, ld_y, ld_pre, (int)rows, (int)k, (int)n,
                                             type, activation, workspace},
@@ -100,6 +157,11 @@ int amq_linear_backward(const void* dy, int64_t ld_dy, const void* x, int64_t ld
       !on_elements(dW, type) || !on_elements(dbias, type))
     return AMQ_ERR_INVALID;
   if (!linear_sizes_supported(rows, k, n) || ld_dy > kMaxStride || (dW && ld_x > kMaxStride) || (dx && ld_w > kMaxStride)) return AMQ_ERR_UNSUPPORTED;
+  // (x and W are read for dW and dx alone)
+  const Extent none{}, ed = matrix(dy, rows, n, ld_dy, type), ep = activation != AMQ_ACT_NONE ? matrix(pre, rows, n, ld_pre, type) : none;
+  const Extent ex = dW ? matrix(x, rows, k, ld_x, type) : none, eW = dx ? matrix(W, n, k, ld_w, type) : none;
+  const Extent edx = matrix(dx, rows, k, ld_dx, type), edW = matrix(dW, n, k, ld_dw, type), edb = vector(dbias, n, type);
+  if (meets(edx, {ed, ep, ex, eW, edW, edb}) || meets(edW, {ed, ep, ex, eW, edb}) || meets(edb, {ed, ep, ex, eW})) return AMQ_ERR_INVALID;
   if (!workspace_ok(workspace, workspace_bytes, amq::linear_grad_workspace(rows, k, n, type))) return AMQ_ERR_INVALID;
   return amq::status_of(amq::launch_linear_grad({dy, x, W, pre, dx, dW, dbias, ld_dy, ld_x, ld_w, ld_pre, ld_dx, ld_dw, (int)rows, (int)k,
                                                  (int)n, type, activation, workspace},
@@ -123,6 +185,17 @@ int amq_orthogonalize(const void* G, int64_t batch, int64_t batch_stride, int64_
   if (batch_stride_out == 0) batch_stride_out = rows * ld_out;
   // (matrices of the output must not share entries)
   if (batch_stride < 0 || (batch > 1 && batch_stride_out < (rows - 1) * ld_out + cols)) return AMQ_ERR_INVALID;
+  // (with steps G is read to its end before the result is written)
+  if (steps == 0 && !(G == out && ld == ld_out && (batch == 1 || batch_stride == batch_stride_out))) {
+    const int64_t size = (int64_t)size_of(type), apart = batch_stride_out * size, room = ((rows - 1) * ld_out + cols) * size;
+    for (int64_t z = 0; z < batch; ++z) {
+      const Extent g = matrix(static_cast<const char*>(G) + z * batch_stride * size, rows, cols, ld, type);
+      const int64_t from = (int64_t)(g.p - reinterpret_cast<uintptr_t>(out));
+      int64_t w = batch > 1 ? floor_div(from - room, apart) : 0;  // the first whose room may reach g
+      for (w = w > 0 ? w : 0; w < batch && w * apart < from + (rows - 1) * g.step + g.width; ++w)
+        if (overlap(g, matrix(static_cast<const char*>(out) + w * apart, rows, cols, ld_out, type))) return AMQ_ERR_INVALID;
+    }
+  }
   if (!workspace_ok(workspace, workspace_bytes, amq::ortho_workspace(batch, rows, cols))) return AMQ_ERR_INVALID;
   return amq::status_of(amq::launch_ortho({G, out, batch_stride, ld, batch_stride_out, ld_out, (int)batch, (int)rows, (int)cols, type, steps,
                                            coef[0], coef[1], coef[2], eps, workspace},

@@ -369,8 +369,9 @@ __device__ __forceinline__ void lay(const Jobs<T>& jobs, int block) {
 }
 
 // ---- columns: sums and largest values, and on the way d itself where it needs no scale.  Bound by memory, or where slopes are
-// formed by those: d of 8960 x 1024 bfloat16 with its slopes (55 MB) 14.5 us = 3.8 TB/s, and 5 us for the second launch.  Many rows of few columns are
-// dealt to more parts, three workgroups per compute unit (with one, 64 parts, 22.7 us).  A workgroup takes 32 groups of V
+// formed by those: d of 8960 x 1024 bfloat16 with relu's slopes (55 MB) 14.9 us = 3.7 TB/s, with gelu's and in two values (73 MB) 20.0, and 5 us
+// for the second launch.  Many rows of few columns are
+// dealt to more parts, three workgroups per compute unit (with one, 64 parts, 22.7 us for 14.5).  A workgroup takes 32 groups of V
 // columns and every 8 * parts-th row of them; what it finds are partial results, which a second launch puts together.  Of at
 // most 128 rows one part is all (16 rows per thread; a launch costs more).
 constexpr int kColumnParts = 64, kMostColumnParts = 192;
@@ -497,8 +498,8 @@ template <typename T, bool SLOPED>
 __global__ __launch_bounds__(256) void lay_kernel(Jobs<T> jobs) {
   lay<T, SLOPED>(jobs, blockIdx.x);
 }
-// The same for d in half, and behind it the sums of its columns.  (With a launch in between that finds the scale and adds the columns the backward pass
-// of 700 x 650 by 1300 took 45 us, 2240 x 1024 by 1024 53; so 30.5 and 43.)
+// The same for d in half, and behind it the sums of its columns.  (A launch in between that finds the scale and adds the columns cost the backward pass
+// of 700 x 650 by 1300 14.5 us, 2240 x 1024 by 1024 10 of now 64.)
 template <typename T>
 __global__ __launch_bounds__(256) void lay_and_add_kernel(Jobs<T> jobs, ColumnJobs<T> beside) {
   const int own = jobs.first[jobs.count];
@@ -644,7 +645,7 @@ hipError_t linear_few(const LinearArgs& a, const LinearStore<T>& out, hipStream_
 // (bfloat16 with gelu, tile 256 / 128 / 64 / 64 with four groups): 8960 x 4096 x 1024 134 / 120 / 145 / 247, 4096^3 116 / 138 /
 // 205 / 260, 2240 x 1024 x 1024 41 / 23 / 15 / 22, 1024 x 1024 x 2240 61 / 33 / 18 / 13, 300 x 300 x 1216 43 / 23 / 12 / 9.
 //   256 (one workgroup per unit): a round 24 + 1.3 per stage
-//   192 (one): a round 16 + 1.07 per stage (the lower half of 4096 x 4096 over 16384, 136 tiles of 256 or 253 of 192: 338 and 287)
+//   192 (one): a round 16 + 1.07 per stage (one round over 16384, 136 tiles of 256 or 253 of 192: 338 and 287)
 //   128 (two): 10 + a tile 4 + 0.55 per stage, and a last round that is not full counts half as one
 //   128 with two groups (one): 2 + a round 7.5 + 0.47 per stage (2048^3 24.6 against 29.7, 1024 x 4096 x 8960 75 against 88)
 //   64 (three): 6.5 + a tile 0.9 + 0.2 per stage, alone 5.5 + 0.32 per stage

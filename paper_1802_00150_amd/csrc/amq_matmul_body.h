@@ -17,12 +17,13 @@
 // multiplied.  The copy writes consecutive 16-byte pieces of LDS per lane, so the order that keeps
 // the operand reads free of bank conflicts is made on the reading side of memory: piece p of row r holds piece p ^ f(r).
 //
-// Bounds and figures.  Large products are bound by the matrix cores at the clock that the card's power leaves them (1.4 to 1.7 of
-// 2.4 GHz): 16384 x 4096 over 4096 with tiles of 256 470 us = 1170 TFLOP/s, the lower half of 4096 x 4096 over 16384 with tiles
-// of 192 290 us = 1060, where a library's product of 16384^3 reaches 1560.  Tiles of 128 take 64 bytes of operands per cycle
-// from the cache above the L2, all it gives: 2048^3 24.6 us = 700 TFLOP/s.  Small products are bound by latency: a launch, a first load, the ring's
-// start, the epilogue, 4 to 5 us together; so what has few tiles gets small ones, and groups of waves that share a tile's stages
-// (64 x 1024 x 1024 5.3 us).
+// Bounds and figures.  Large products: bfloat16 16384 x 4096 over 4096 with tiles of 256 432 us = 1270 TFLOP/s, where a library's product of 16384^3
+// reaches 1560; numbers of two halves, tiles of 128 with two groups of waves, 1443 us = 1140 TFLOP/s of half products. Counters: the matrix
+// cores are busy for 58 and 51 % of the cycles, at 2.1 GHz; the rest are waits for copies at the barriers, starts and epilogues. LDS has conflicts of 256 to 1024 cycles per tile
+// (of symmetric results 1700) whatever its number of stages, 1 to 5 % of its use: those are the epilogue's, operand reads have none.  At the matrix cores' full rate tiles of 128 would
+// take 64 bytes of operands per cycle, all that the cache above the L2 gives: 2048^3 24.6 us = 700 TFLOP/s.  Small products are bound by
+// latency: a launch, a first load, the ring's start, the epilogue, 4 to 5 us together; so what has few tiles gets small ones, and groups of
+// waves that share a tile's stages (64 x 1024 x 1024 5.3 us).
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -53,8 +54,7 @@ struct MatmulArgs {
   int lower;             // symmetric result (r = c): only tiles with bm >= bn
 };
 
-// 16 x 16 values, 32 steps of k.  (The card's power limits large products: this form takes 8 KB from and to the registers for
-// 16384 multiplications, 32 x 32 x 16 takes 10 KB.)
+// 16 x 16 values, 32 steps of k.  (This form takes 8 KB from and to the registers for 16384 multiplications, 32 x 32 x 16 takes 10 KB.)
 template <typename E>
 struct MatmulElement;
 template <>
@@ -440,7 +440,7 @@ __global__ __launch_bounds__(KG * WR * WC * 64, KG * WR * WC >= 16 ? 4 : 2) void
 }
 // Two products that do not depend on each other, d W and d^T x, in one launch: the tiles of the one with the longer contraction come
 // first, so that what is left at the end is small. One launch instead of two took the bf16 backward of 700 x 650 by 1300 from 29.5 us
-// to 24.8 and of 20 x 100 by 100 from 14.8 to 10.3; plan_pair() leaves the two apart where that is estimated to be faster.
+// to 24.8 and of 20 x 100 by 100 from 14.8 to 10.3 (d of one value); plan_pair() leaves the two apart where that is estimated to be faster.
 template <typename E, int NP, bool TWO, int BM, int BN, int WR, int WC, int KG, int PLACES, typename Epi>
 __global__ __launch_bounds__(KG * WR * WC * 64, KG * WR * WC >= 16 ? 4 : 2) void matmul_pair_kernel(MatmulArgs g, Epi epi, MatmulArgs g2, Epi epi2) {
   __shared__ __align__(256) uint16_t lds[kTileLds<BM, BN, KG, PLACES>];
@@ -532,7 +532,7 @@ hipError_t launch_product(const MatmulArgs& g, const ProductPlan& p, int batch, 
   auto run = [&](const auto& store) {
     if constexpr (NP == 1)
       if (p.tile == 256) return launch_tiles<E, NP, TWO, RC, CC, 256, 256, 2, 4, 1, 2>(g, p, batch, store, s);
-    // (8 waves; with 4 that hold twice the values each 416 us against 287, with 12 or a ring of three places the same)
+    // (8 waves: 253 tiles over 16384 287 us; with 4 that hold twice the values each 416, with 12 or a ring of three places the same)
     if constexpr (NP == 1)
       if (p.tile == 192) return launch_tiles<E, NP, TWO, RC, CC, 192, 192, 2, 4, 1, 2>(g, p, batch, store, s);
     if (p.tile == 128 && p.groups == 2) return launch_tiles<E, NP, TWO, RC, CC, 128, 128, 2, 2, 2, 2>(g, p, batch, store, s);

@@ -2,8 +2,9 @@
 //
 // n <= m are the sizes of X (the transpose of G where G is tall).  Per step n^2 m + n^3 + 2 n^2 m operations, since A and
 // A A are symmetric and only tiles on and below the diagonal are computed: bound by the matrix cores from about n = 512 on,
-// by the chain of three dependent launches per step below.  Measured: 16384 x 4096 bfloat16 14.4 ms for 4.5 Tflop, as three half products
-// 930 TFLOP/s; two float matrices of 1200 x 300 135 us, 17 launches of 5 to 9.
+// by the chain of three dependent launches per step below.  Measured: 16384 x 4096 bfloat16 or half 14.0 to 14.4 ms for 4.5 Tflop, each as three half
+// products: per step A 1069 us and B 271 = 770 and 760 TFLOP/s of half products (528 tiles in 512 places: the second round is almost empty, the
+// matrix cores busy for 36 % of the cycles), X 1443 = 1140.  Two float matrices of 1200 x 300 135 us, 17 launches of 6 to 10; one half matrix of 2048 x 512 155.
 //
 // Iterates, A and B are held as half values times 2^12, in two planes (22 bits).  Singular values stay below about 1.2 with the usual coefficients, so
 // nothing comes near 65504 / 4096 = 16, and half's smallest step is 2^-36 of an entry of 1.  Two planes lose 3e-7 of the result in the 2-norm
@@ -132,7 +133,7 @@ struct Gradient {
   int rows, cols;
 };
 
-// Sums of squares, kNormParts of them per matrix.  Bound by memory: 16384 x 4096 bfloat16 (134 MB) 36 us = 3.7 TB/s (one piece of
+// Sums of squares, kNormParts of them per matrix.  Bound by memory: 16384 x 4096 bfloat16 (134 MB) 35 us = 3.8 TB/s (one piece of
 // a row under way instead of four, and a quarter of the workgroups: 85).
 template <typename T>
 __global__ __launch_bounds__(256) void ortho_norm_kernel(Gradient<T> G, double* parts) {
@@ -175,7 +176,7 @@ __device__ __forceinline__ Factor inverse_norm(const double* parts, int z, int c
   return f;
 }
 
-// X_0: 8 numbers per lane, rows dealt to the workgroups.  Bound by memory: 16384 x 4096 bfloat16 (268 MB) 45 us = 6.0 TB/s.
+// X_0: 8 numbers per lane, rows dealt to the workgroups.  Bound by memory: 16384 x 4096 bfloat16 (403 MB) 110 us = 3.7 TB/s.
 template <typename T>
 __global__ __launch_bounds__(256) void ortho_begin_kernel(Gradient<T> G, const double* parts, int count, float eps, Planes X) {
   __shared__ double scratch[4];

@@ -39,6 +39,28 @@ def test_the_gradient_between_slope_and_products(amq, rows, k, n, dtype, act):
     assert float((db.double() - d.sum(0)).norm()) <= float((d.sum(0).to(dtype).double() - d.sum(0)).norm()) + 2 * share * float((d * d).sum().sqrt())
 
 
+# each gradient in a launch of its own, where tiles of 64, 128, 192 and 256 and splits of either contraction are taken; k, n and rows odd, and multiples
+# of 8 that are read in place
+@pytest.mark.parametrize("rows,k,n", [(9000, 72, 200), (20001, 40, 47), (1500, 300, 8000), (3000, 1000, 3050), (3000, 3050, 500), (500, 3050, 3000), (8960, 2050, 1024),
+                                      (8960, 4096, 200), (1024, 4096, 8960)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_each_gradient_alone(amq, rows, k, n, dtype):
+    """The same bound for the product of either gradient by itself."""
+    x, W, _, dy = inputs(rows + k + n, rows, k, n, dtype)
+    x, W, dy = x.to(DEV), W.to(DEV), (dy.float() / rows).to(dtype).to(DEV)
+    pre = amq.linear(x, W)
+    d = dy.double() * slope64(pre.double(), "gelu")
+    dx, none, none2 = amq.linear_backward(dy, x, W, pre, "gelu", True, False, False)
+    assert none is None and none2 is None
+    dW = amq.linear_backward(dy, x, W, pre, "gelu", False, True, False)[1]
+    share = 2.0 ** -16 + 2.0 ** -20 + 8 * U * 16
+    for got, a, b, what in ((dx, d, W.double(), "dx"), (dW, d.t().contiguous(), x.double(), "dW")):
+        ref = a @ b
+        e, rounding = share * float(((a * a) @ (b * b)).sum().sqrt()), float((ref.to(dtype).double() - ref).norm())
+        assert float((got.double() - ref).norm()) <= rounding + 2 * e, (what, float((got.double() - ref).norm()), rounding, e)
+        assert float((got.double() - ref).abs().max()) <= 0.02 * float(ref.abs().max()), what
+
+
 @pytest.mark.parametrize("rows", [9, 40, 300])
 @pytest.mark.parametrize("far", [10, 18, 24, 28])
 def test_float_entries_far_below_the_largest_of_their_row(amq, rows, far):

@@ -343,7 +343,7 @@ def _own(state, case):
     if case["kind"] == "block_norm_grad":
         results = amq.block_norm_backward(state["dy"], state["dnormed"], state["x"], state["y"], state["stats"], state["weight"],
                                           state["bias"], gate=state["gate"], activation=case["gate"], scale=state["scale"],
-                                          next_weight=state["next_weight"])
+                                          next_weight=state["next_weight"], next_bias=state["next_bias"])
         keys = ("dx", "dresidual", "dgate", "dweight", "dbias", "dscale", "dnext_weight", "dnext_bias")
         return {key: v for key, v in zip(keys, results) if v is not None}
     norm = amq.clip_gradients(state["grads"], state["max_norm"], out=state["out"])

@@ -551,6 +551,86 @@ int amq_orthogonalize(const void* G, int64_t batch, int64_t batch_stride, int64_
                       int steps, const float* coef, float eps, void* out, int64_t batch_stride_out, int64_t ld_out,
                       void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * Linear recurrences: every channel of every batch entry has a state of its own, and no product of the state stands between two
+ * steps, so that a whole sequence is one pass.
+ *   AMQ_RECURRENCE_BLEND: f = sigmoid(gate_t), h_t = f h_{t-1} + (1 - f) x_t   (the update of amq_gru_step, its gate given)
+ *   AMQ_RECURRENCE_DECAY: h_t = gate_t h_{t-1} + x_t   (products of the factors over any 128 steps must be finite)
+ *   gate, x, hs [steps][B][n] of `type`, n entries side by side, steps and batch entries *_step and *_batch elements apart, any alignment: columns of a
+ *   wider projection and tensors whose outer dimension is the batch are taken as they are (gate and x also with strides of 0)
+ *   lengths [B] int64 or NULL: entry b has lengths[b] steps (taken as 0 below 0 and as `steps` above).  gate and x behind them are
+ *   not read, hs is 0 there, and the state stays what it is
+ *   h0 [B][n] float or NULL for zeros;  h_last [B][n] float or NULL: the state behind the last step; may be h0 itself
+ *   states [(steps - 1) / AMQ_STATE_STEPS][B][n] float or NULL: the states in front of steps 128, 256, ..., which the backward pass takes
+ *   workspace: at least amq_linear_recurrence_workspace_bytes(steps, B, n, type) bytes, 256-byte aligned (0: may be NULL).
+ * One step with h0 and h_last is the form for single tokens.
+ * The backward pass takes dhs [steps][B][n] and dh_last [B][n] (NULL: zeros), the gradients of hs and h_last, and leaves those of gate, x and
+ * h0 (dh0 float, may be NULL): with e_t = dhs_t + f_{t+1} e_{t+1},  dx = (1 - f) e,  dgate = e (h_{t-1} - x) f (1 - f),  dh0 = f_0 e_0;
+ * of a decay  dx = e,  dgate = e h_{t-1}.  h_{t-1} is formed again in binary32 from `states` (NULL up to 128 steps).  Behind lengths[b] dhs is not read, and
+ * dgate and dx are 0.
+ * Results do not depend on the order of execution.
+ * AMQ_ERR_UNSUPPORTED beyond 2^24 steps, 2^22 batch entries, 2^20 channels, 2^30 of both, strides of 2^36.
+ */
+#define AMQ_RECURRENCE_BLEND 0
+#define AMQ_RECURRENCE_DECAY 1
+#define AMQ_STATE_STEPS 128
+size_t amq_linear_recurrence_workspace_bytes(int64_t steps, int64_t B, int64_t n, int type);
+int amq_linear_recurrence(const void* gate, int64_t gate_step, int64_t gate_batch, const void* x, int64_t x_step, int64_t x_batch,
+                          int64_t steps, int64_t B, int64_t n, int type, int mode, const int64_t* lengths, const float* h0,
+                          void* hs, int64_t hs_step, int64_t hs_batch, float* h_last, float* states, void* workspace,
+                          size_t workspace_bytes, void* stream);
+size_t amq_linear_recurrence_backward_workspace_bytes(int64_t steps, int64_t B, int64_t n, int type);
+int amq_linear_recurrence_backward(const void* dhs, int64_t dhs_step, int64_t dhs_batch, const void* gate, int64_t gate_step,
+                                   int64_t gate_batch, const void* x, int64_t x_step, int64_t x_batch, int64_t steps, int64_t B,
+                                   int64_t n, int type, int mode, const int64_t* lengths, const float* h0, const float* states,
+                                   const float* dh_last, void* dgate, int64_t dgate_step, int64_t dgate_batch, void* dx,
+                                   int64_t dx_step, int64_t dx_batch, float* dh0, void* workspace, size_t workspace_bytes,
+                                   void* stream);
+
+/*
+ * The join of a block with the residual stream: the norm behind the block with its gate and scale, the residual, and the norm
+ * in front of the next block, in one pass over rows.
+ *   y = residual + scale act(gate) norm(x; weight, bias),   normed = norm(y; next_weight, next_bias),   norm as in amq_layer_norm
+ *   x, gate, normed [rows][ld] of `type`; residual, y [rows][ld] of `residual_type` (AMQ_F32 or `type`); any alignment, ld >= n
+ *   gate NULL: none.  activation: AMQ_ACT_NONE (the gate itself), AMQ_ACT_SIGMOID or AMQ_ACT_SILU
+ *   weight, bias, scale, next_weight, next_bias [n] of `param_type` (AMQ_F32 or `type`), or NULL for 1 and 0
+ *   normed NULL: y alone;  y may be the residual itself (same stride)
+ *   stats [4][rows] float out or NULL: mean and 1 / sqrt(var + eps) of x, then of y (the last two only with normed), which the backward pass takes
+ * normed and the statistics are formed from y before its rounding.
+ * The backward pass takes the gradients dy and dnormed (either may be NULL: zeros), x, gate, stats and y (which dnormed needs) and leaves those of x, the residual
+ * (may be NULL; may be dy itself), the gate (NULL without one) and of the parameters (each may be NULL; sums over all rows in an order that depends on the sizes only).
+ *   workspace: at least amq_block_norm_backward_workspace_bytes(rows, n) bytes, 256-byte aligned (may be NULL
+ *   where no parameter's gradient is wanted).
+ * AMQ_ERR_UNSUPPORTED beyond rows of 16384 entries and 2^31 - 1 rows.
+ */
+int amq_block_norm(const void* x, int64_t ld_x, const void* residual, int64_t ld_r, const void* gate, int64_t ld_g, int64_t rows,
+                   int64_t n, int type, int residual_type, int param_type, int activation, const void* weight, const void* bias,
+                   const void* scale, const void* next_weight, const void* next_bias, float eps, void* y, int64_t ld_y,
+                   void* normed, int64_t ld_n, float* stats, void* stream);
+size_t amq_block_norm_backward_workspace_bytes(int64_t rows, int64_t n);
+int amq_block_norm_backward(const void* dy, int64_t ld_dy, const void* dnormed, int64_t ld_dn, const void* x, int64_t ld_x,
+                            const void* y, int64_t ld_y, const void* gate, int64_t ld_g, int64_t rows, int64_t n, int type,
+                            int residual_type, int param_type, int activation, const void* weight, const void* bias,
+                            const void* scale, const void* next_weight, const float* stats, void* dx, int64_t ld_dx,
+                            void* dresidual, int64_t ld_dr, void* dgate, int64_t ld_dg, void* dweight, void* dbias, void* dscale,
+                            void* dnext_weight, void* dnext_bias, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The 2-norm over all entries of `count` tensors, and the tensors scaled to a largest norm:
+ *   norm = sqrt(sum g^2),   out = c g,   c = max_norm / norm where norm is finite and more than max_norm, else 1
+ *   tensors, out [count] (host arrays of device pointers), sizes [count] (host; entries, 0 for an empty tensor), types [count] (host);
+ *   the arrays are read before the call returns
+ *   out[i] may be tensors[i] (then nothing is written where c is 1); else it overlaps no tensor and no other result.  out NULL: the norm alone
+ *   max_norm >= 0 (infinity: scales nothing);  norm: float out
+ * Squares are summed in binary64, in an order that depends on the sizes and types only.  A norm beyond binary32 is stored as infinity
+ * and still scales; a norm that is infinite or NaN because an entry is scales nothing.
+ *   workspace: at least amq_clip_gradients_workspace_bytes(count) bytes, 256-byte aligned.
+ * AMQ_ERR_UNSUPPORTED beyond 2^20 tensors and 2^40 entries of one.
+ */
+size_t amq_clip_gradients_workspace_bytes(int64_t count);
+int amq_clip_gradients(int64_t count, const void* const* tensors, const int64_t* sizes, const int* types, float max_norm,
+                       void* const* out, float* norm, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -38,6 +38,10 @@ EXPORTS = [
     "amq_layer_norm", "amq_layer_norm_backward_workspace_bytes", "amq_layer_norm_backward",
     "amq_linear_workspace_bytes", "amq_linear", "amq_linear_backward_workspace_bytes", "amq_linear_backward",
     "amq_orthogonalize_workspace_bytes", "amq_orthogonalize",
+    "amq_linear_recurrence_workspace_bytes", "amq_linear_recurrence",
+    "amq_linear_recurrence_backward_workspace_bytes", "amq_linear_recurrence_backward",
+    "amq_block_norm", "amq_block_norm_backward_workspace_bytes", "amq_block_norm_backward",
+    "amq_clip_gradients_workspace_bytes", "amq_clip_gradients",
 ]
 
 _lib = None
@@ -142,6 +146,20 @@ def lib():
         L.amq_orthogonalize_workspace_bytes.restype = _sz
         L.amq_orthogonalize.argtypes = [_p, _i64, _i64, _i64, _i64, _i64, _int, _int, C.POINTER(C.c_float), C.c_float, _p,
                                         _i64, _i64, _p, _sz, _p]
+        for name in ("amq_linear_recurrence_workspace_bytes", "amq_linear_recurrence_backward_workspace_bytes"):
+            getattr(L, name).argtypes, getattr(L, name).restype = [_i64, _i64, _i64, _int], _sz
+        L.amq_linear_recurrence.argtypes = [_p, _i64, _i64, _p, _i64, _i64, _i64, _i64, _i64, _int, _int, _p, _p, _p, _i64, _i64, _p,
+                                            _p, _p, _sz, _p]
+        L.amq_linear_recurrence_backward.argtypes = [_p, _i64, _i64, _p, _i64, _i64, _p, _i64, _i64, _i64, _i64, _i64, _int, _int, _p,
+                                                     _p, _p, _p, _p, _i64, _i64, _p, _i64, _i64, _p, _p, _sz, _p]
+        L.amq_block_norm.argtypes = [_p, _i64, _p, _i64, _p, _i64, _i64, _i64, _int, _int, _int, _int, _p, _p, _p, _p, _p, C.c_float,
+                                     _p, _i64, _p, _i64, _p, _p]
+        L.amq_block_norm_backward_workspace_bytes.argtypes = [_i64, _i64]
+        L.amq_block_norm_backward_workspace_bytes.restype = _sz
+        L.amq_block_norm_backward.argtypes = [_p, _i64, _p, _i64, _p, _i64, _p, _i64, _p, _i64, _i64, _i64, _int, _int, _int, _int,
+                                              _p, _p, _p, _p, _p, _p, _i64, _p, _i64, _p, _i64, _p, _p, _p, _p, _p, _p, _sz, _p]
+        L.amq_clip_gradients_workspace_bytes.argtypes, L.amq_clip_gradients_workspace_bytes.restype = [_i64], _sz
+        L.amq_clip_gradients.argtypes = [_i64, _p, _p, _p, C.c_float, _p, _p, _p, _sz, _p]
         _lib = L
     return _lib
 
@@ -511,8 +529,8 @@ def fake_quantize(W, k, T=2):
 
 
 # ---- operators of quantization-aware training: float32, bfloat16 or float16 tensors [..., n] (a 2-D tensor's rows may be strided).
-# They record no graph: with gradients on, layer_norm, linear and orthogonalize refuse operands that require one (training.layer_norm and
-# training.linear are the differentiable forms).
+# They record no graph: with gradients on, layer_norm, linear, orthogonalize, linear_recurrence, block_norm and clip_gradients refuse operands that
+# require one (the functions of the same names in training are the differentiable forms).
 
 ACTIVATIONS = {None: 0, "none": 0, "relu": 1, "gelu": 2, "silu": 3, "sigmoid": 4, "tanh": 5}
 
@@ -580,3 +598,86 @@ def orthogonalize(G, steps=5, coefficients=(3.4445, -4.7750, 2.0315), eps=1e-7, 
 def orthogonalize_workspace(batch, rows, cols, dtype, device):
     return torch.empty(int(lib().amq_orthogonalize_workspace_bytes(batch, rows, cols, _TYPES[dtype])), dtype=torch.uint8,
                        device=device)
+
+
+STATE_STEPS = 128  # AMQ_STATE_STEPS: linear_recurrence leaves the state in front of every 128th step for its backward pass
+RECURRENCES = {"blend": 0, "decay": 1}
+
+
+def _recurrence(name):
+    if name not in RECURRENCES:
+        raise ValueError("mode: expected one of %s, got %r" % (", ".join(sorted(RECURRENCES)), name))
+    return RECURRENCES[name]
+
+
+def linear_recurrence(gate, x, h0=None, mode="blend", lengths=None, states=False, ws=None, out=None, h_out=None):
+    """All steps of a recurrence whose channels do not mix -> hs [steps, batch, n] of x's type, the last state [batch, n] (float32),
+    and with states=True beyond 128 steps what linear_recurrence_backward takes (else None).
+    mode "blend": f = sigmoid(gate_t), h_t = f h_{t-1} + (1 - f) x_t;  "decay": h_t = gate_t h_{t-1} + x_t.
+    gate, x [steps, batch, n]: float32, bfloat16 or float16, channels side by side, other strides as they are (columns of a wider projection;
+    a batch-first tensor transposed).  h0 [batch, n] float32, None for zeros.  lengths [batch] int64: entry b has lengths[b] steps, behind which
+    nothing is read, hs is 0 and the state stays.  h_out receives the last state and may be h0 itself."""
+    return (_native_module or _load_native()).linear_recurrence(gate, x, h0, _recurrence(mode), lengths, 1 if states else 0, ws, out, h_out)
+
+
+def linear_recurrence_workspace(steps, batch, n, dtype, device):
+    return torch.empty(int(lib().amq_linear_recurrence_workspace_bytes(steps, batch, n, _TYPES[dtype])), dtype=torch.uint8, device=device)
+
+
+def linear_recurrence_backward(dhs, gate, x, h0=None, states=None, dh_last=None, mode="blend", lengths=None, ws=None, dgate=None, dx=None):
+    """Gradients dgate, dx (of x's type) and dh0 (float32; None without h0) of linear_recurrence, from those of hs and of the last
+    state (None: zeros).  states: what linear_recurrence left, needed beyond 128 steps.  dgate and dx may be given as results."""
+    return (_native_module or _load_native()).linear_recurrence_backward(dhs, gate, x, h0, states, dh_last, _recurrence(mode), lengths, ws, dgate, dx)
+
+
+def linear_recurrence_backward_workspace(steps, batch, n, dtype, device):
+    return torch.empty(int(lib().amq_linear_recurrence_backward_workspace_bytes(steps, batch, n, _TYPES[dtype])), dtype=torch.uint8,
+                       device=device)
+
+
+GATES = (None, "none", "sigmoid", "silu")
+
+
+def _gate(name):
+    if name not in GATES:
+        raise ValueError("activation: expected none, sigmoid or silu for a gate, got %r" % (name,))
+    return ACTIVATIONS[name]
+
+
+def block_norm(x, residual, weight=None, bias=None, gate=None, activation="sigmoid", scale=None, next_weight=None, next_bias=None,
+               eps=1e-5, normed=True, out=None, out_normed=None):
+    """y = residual + scale * activation(gate) * norm(x; weight, bias) and norm(y; next_weight, next_bias), norm as in layer_norm -> y,
+    the normed y (of x's type; None without normed), statistics [4, rows] (mean and 1 / sqrt(var + eps) of x, of y).
+    x, gate: float32, bfloat16 or float16; residual and y: float32 or x's type; parameters [n]: all float32 or all x's type; None for 1, 0 and
+    no gate.  activation: None (the gate itself), "sigmoid" or "silu".  out receives y and may be the residual itself."""
+    return (_native_module or _load_native()).block_norm(x, residual, weight, bias, gate, _gate(activation), scale, next_weight, next_bias, eps,
+                                                         1 if normed else 0, out, out_normed)
+
+
+def block_norm_backward(dy, dnormed, x, y, stats, weight=None, bias=None, gate=None, activation="sigmoid", scale=None, next_weight=None,
+                        next_bias=None, param_grads=True, ws=None):
+    """Gradients dx, dresidual, dgate, dweight, dbias, dscale, dnext_weight, dnext_bias of block_norm from those of y and of the
+    normed y (one of them may be None).  Those of operands that are None, and without param_grads those of the parameters, are None.
+    next_bias has no part in the gradients; it says whether its own is wanted."""
+    return (_native_module or _load_native()).block_norm_backward(dy, dnormed, x, y, stats, weight, bias, gate, _gate(activation), scale, next_weight,
+                                                                  next_bias, 1 if param_grads else 0, ws)
+
+
+def block_norm_backward_workspace(rows, n, device):
+    return torch.empty(int(lib().amq_block_norm_backward_workspace_bytes(rows, n)), dtype=torch.uint8, device=device)
+
+
+def gradient_norm(grads, ws=None):
+    """The 2-norm over all entries of a sequence of dense tensors (float32, bfloat16, float16, mixed) -> a float32 scalar on the GPU."""
+    return (_native_module or _load_native()).clip_gradients(list(grads), None, 0.0, ws)
+
+
+def clip_gradients(grads, max_norm, out=None, ws=None):
+    """Scales a sequence of dense tensors by max_norm / norm where their norm (as in gradient_norm, which is returned) is finite and more than
+    max_norm; in place, or into `out`, a sequence of as many tensors of the same shapes."""
+    grads = list(grads)
+    return (_native_module or _load_native()).clip_gradients(grads, grads if out is None else list(out), max_norm, ws)
+
+
+def clip_gradients_workspace(count, device):
+    return torch.empty(int(lib().amq_clip_gradients_workspace_bytes(count)), dtype=torch.uint8, device=device)

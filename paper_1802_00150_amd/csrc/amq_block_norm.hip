@@ -1,0 +1,492 @@
+// The join of a block with the residual stream, forward and backward: the norm behind the block, its gate and scale, the
+// residual, and the norm in front of the next block, in one pass.
+//
+//   z = (x - mu) r,  u = z w + b,  y = residual + s act(gate) u,  zy = (y - mu') r',  normed = zy w' + b'
+//   G = dy + r' (g' - mean g' - zy mean(g' zy)),  g' = dnormed w';     dresidual = G,  dgate = G s u act'(gate)
+//   g = G s act w:  dx = r (g - mean g - z mean(g z));   dw = s S1, db = s S0, ds = w S1 + b S0,  S1 = sum G act z,  S0 = sum G act
+//   dw' = sum dnormed zy,  db' = sum dnormed  (sums over rows)
+//
+// About 30 operations per entry forward and 60 backward, against 10 and 16 bytes (16-bit types): bound by memory, or by latency
+// for few rows.  So every entry is read once and kept in registers between the four sums of a row and the results; a row belongs to one
+// wave (its sums need no barrier) or to a workgroup of 4, 8 or 16.  Workgroups walk over rows, with the parameters and, in the
+// backward pass, four sums per column in registers; those leave one partial row per workgroup, added up by a second launch in a
+// fixed order.  normed is formed from y before its rounding; statistics and sums are binary32.
+#include "../../include/amq.h"
+
+#include <type_traits>
+
+#include "amq_device.h"
+#include "amq_train.h"
+#include "amq_typed.h"
+
+namespace amq {
+namespace {
+
+__device__ __forceinline__ float sum64(float v) { return group_sum(v, 6); }
+
+// Sums of two values over the W waves that share a row.  One barrier, of all groups of W waves in the workgroup: the slots of
+// consecutive calls alternate.
+template <int W>
+__device__ __forceinline__ void row_sum2(float& a, float& b, float (*slots)[2], int& turn) {
+  a = sum64(a);
+  b = sum64(b);
+  if constexpr (W > 1) {
+    const int waves = blockDim.x / 64, group = wave_id() / W * W;
+    float(*s)[2] = slots + turn * waves;
+    turn ^= 1;
+    if (lane_id() == 0) {
+      s[wave_id()][0] = a;
+      s[wave_id()][1] = b;
+    }
+    lds_barrier();
+    a = b = 0.0f;
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+      a += s[group + i][0];
+      b += s[group + i][1];
+    }
+  }
+}
+template <int W>
+__device__ __forceinline__ float row_sum(float a, float (*slots)[2], int& turn) {
+  float b = 0.0f;
+  row_sum2<W>(a, b, slots, turn);
+  return a;
+}
+
+// Piece j of a row's pieces of V entries for thread `tid` of W waves.  The last one ends with the row and overlaps the one before
+// it (its first `repeated` entries count there); threads past the end hold it once more with nothing that counts, and store
+// nothing.  (n >= V.)
+template <int W, int V>
+struct Piece {
+  int start, repeated;
+  __device__ __forceinline__ Piece(int j, int tid, int n) {
+    const int c = (j * W * 64 + tid) * V;
+    start = c < n - V ? c : n - V;
+    repeated = c - start < V ? c - start : V;
+  }
+  __device__ __forceinline__ bool counts(int i) const { return i >= repeated; }
+  __device__ __forceinline__ bool any() const { return repeated < V; }
+  // a result; entries that the piece before has are stored there (they may lie where an operand did)
+  template <typename T>
+  __device__ __forceinline__ void put(T* row, const float (&v)[V]) const {
+    T* p = row + start;
+    if (repeated == 0) {
+      store<T, V>(p, V, v);
+    } else if (any()) {
+#pragma unroll
+      for (int i = 1; i < V; ++i)
+        if (i >= repeated) p[i] = (T)v[i];
+    }
+  }
+};
+
+// act(z) and its slope.
+__device__ __forceinline__ void gate_of(int act, float z, float& value, float& slope) {
+  if (act == AMQ_ACT_NONE) {
+    value = z;
+    slope = 1.0f;
+    return;
+  }
+  const float e = __expf(-fabsf(z)), r = __builtin_amdgcn_rcpf(1.0f + e), small = e * r;
+  const float p = z >= 0.0f ? r : small, q = z >= 0.0f ? small : r;  // sigmoid(z), 1 - sigmoid(z)
+  if (act == AMQ_ACT_SIGMOID) {
+    value = p;
+    slope = p * q;
+  } else {
+    value = z * p;
+    slope = p * fmaf(z, q, 1.0f);
+  }
+}
+
+template <typename T, int V, int NV, typename F>
+__device__ __forceinline__ void ask(Elements<T, V> (&r)[NV], const void* base, int64_t offset, F piece) {
+  const T* p = (const T*)base + offset;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) r[j] = fetch<T, V>(p + piece(j).start, V);
+}
+
+constexpr int row_groups(int waves, int most) { return waves >= most ? 1 : most / waves; }
+
+// T: x, gate and normed; R: residual and y; P: parameters.  W waves per row, NV pieces of V entries per lane.
+template <typename T, typename R, typename P, int V, int W, int NV>
+__global__ __launch_bounds__(W > 4 ? W * 64 : 256) void block_norm_kernel(BlockNormArgs a) {
+  constexpr int kRows = row_groups(W, 4);
+  __shared__ float slots[2 * W * kRows][2];
+  int turn = 0;
+  const int group = wave_id() / W, tid = (int)threadIdx.x - group * W * 64;
+  auto piece = [&](int j) __attribute__((always_inline)) { return Piece<W, V>(j, tid, a.n); };
+  // the scale is folded into the first norm's parameters
+  float w[NV][V], b[NV][V], w2[NV][V], b2[NV][V];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    float s[V];
+    load_params<P, V>((const P*)a.weight, piece(j).start, V, 1.0f, w[j]);
+    load_params<P, V>((const P*)a.bias, piece(j).start, V, 0.0f, b[j]);
+    load_params<P, V>((const P*)a.scale, piece(j).start, V, 1.0f, s);
+    load_params<P, V>((const P*)a.next_weight, piece(j).start, V, 1.0f, w2[j]);
+    load_params<P, V>((const P*)a.next_bias, piece(j).start, V, 0.0f, b2[j]);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      w[j][i] *= s[i];
+      b[j][i] *= s[i];
+    }
+  }
+  const float inv_n = 1.0f / (float)a.n;
+  Elements<T, V> rx[NV], rg[NV];
+  Elements<R, V> rr[NV];
+  auto fetch_row = [&](int64_t row) __attribute__((always_inline)) {
+    if (row >= a.rows) return;
+    ask(rx, a.x, row * a.ld_x, piece);
+    ask(rr, a.residual, row * a.ld_r, piece);
+    if (a.gate) ask(rg, a.gate, row * a.ld_g, piece);
+  };
+  const int64_t step = (int64_t)gridDim.x * kRows;
+  int64_t first = (int64_t)blockIdx.x * kRows;  // of the workgroup's rows: its groups meet at barriers, so they leave together
+  fetch_row(first + group);
+  for (; first < a.rows; first += step) {
+    const int64_t row = first + group;
+    const bool here = row < a.rows;
+    float x[NV][V], y[NV][V], act[NV][V], s = 0.0f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        x[j][i] = here ? (float)rx[j].v[i] : 0.0f;
+        y[j][i] = here ? (float)rr[j].v[i] : 0.0f;
+        act[j][i] = 1.0f;
+        if (a.gate) {
+          float slope;
+          gate_of(a.act, here ? (float)rg[j].v[i] : 0.0f, act[j][i], slope);
+        }
+        s += piece(j).counts(i) ? x[j][i] : 0.0f;
+      }
+    fetch_row(row + step);
+    const float mean = row_sum<W>(s, slots, turn) * inv_n;
+    s = 0.0f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        x[j][i] -= mean;
+        s = fmaf(piece(j).counts(i) ? x[j][i] : 0.0f, x[j][i], s);
+      }
+    const float rstd = 1.0f / sqrtf(row_sum<W>(s, slots, turn) * inv_n + a.eps);
+    s = 0.0f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        y[j][i] = fmaf(fmaf(x[j][i] * rstd, w[j][i], b[j][i]), act[j][i], y[j][i]);
+        s += piece(j).counts(i) ? y[j][i] : 0.0f;
+      }
+      if (here) piece(j).put((R*)a.y + row * a.ld_y, y[j]);
+    }
+    float mean_y = 0.0f, rstd_y = 0.0f;
+    if (a.normed) {
+      mean_y = row_sum<W>(s, slots, turn) * inv_n;
+      s = 0.0f;
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          y[j][i] -= mean_y;
+          s = fmaf(piece(j).counts(i) ? y[j][i] : 0.0f, y[j][i], s);
+        }
+      rstd_y = 1.0f / sqrtf(row_sum<W>(s, slots, turn) * inv_n + a.eps);
+      if (here)
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+#pragma unroll
+          for (int i = 0; i < V; ++i) y[j][i] = fmaf(y[j][i] * rstd_y, w2[j][i], b2[j][i]);
+          piece(j).put((T*)a.normed + row * a.ld_n, y[j]);
+        }
+    }
+    if (tid == 0 && here && a.stats) {
+      a.stats[row] = mean;
+      a.stats[a.rows + row] = rstd;
+      if (a.normed) {
+        a.stats[2 * a.rows + row] = mean_y;
+        a.stats[3 * a.rows + row] = rstd_y;
+      }
+    }
+  }
+}
+
+template <typename T, typename R, typename P, int V, int W, int NV>
+__global__ __launch_bounds__(row_groups(W, 8) * W * 64) void block_norm_grad_kernel(BlockNormGradArgs a) {
+  constexpr int kRows = row_groups(W, 8), kThreads = W * 64, kEntries = kThreads * NV * V;
+  __shared__ float slots[2 * W * kRows][2];
+  // [group][sum][j][i][thread]: consecutive lanes on consecutive banks
+  __shared__ float shared_sums[kRows > 1 ? kRows * 2 * kEntries : 1];
+  int turn = 0;
+  const int group = wave_id() / W, tid = (int)threadIdx.x - group * kThreads;
+  auto piece = [&](int j) __attribute__((always_inline)) { return Piece<W, V>(j, tid, a.n); };
+  // sums[0..3]: G act z, G act, dnormed zy, dnormed
+  float w[NV][V], b[NV][V], sc[NV][V], w2[NV][V], sums[4][NV][V];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    load_params<P, V>((const P*)a.weight, piece(j).start, V, 1.0f, w[j]);
+    load_params<P, V>((const P*)a.bias, piece(j).start, V, 0.0f, b[j]);
+    load_params<P, V>((const P*)a.scale, piece(j).start, V, 1.0f, sc[j]);
+    load_params<P, V>((const P*)a.next_weight, piece(j).start, V, 1.0f, w2[j]);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int i = 0; i < V; ++i) sums[k][j][i] = 0.0f;
+  }
+  const float inv_n = 1.0f / (float)a.n;
+  const int64_t step = (int64_t)gridDim.x * kRows;
+  for (int64_t first = (int64_t)blockIdx.x * kRows; first < a.rows; first += step) {
+    const int64_t row = first + group;
+    const bool here = row < a.rows;
+    Elements<T, V> rx[NV], rg[NV], rn[NV];
+    Elements<R, V> ry[NV], rd[NV];
+    float mean = 0.0f, rstd = 0.0f, mean_y = 0.0f, rstd_y = 0.0f;
+    if (here) {
+      ask(rx, a.x, row * a.ld_x, piece);
+      if (a.gate) ask(rg, a.gate, row * a.ld_g, piece);
+      if (a.dnormed) {
+        ask(rn, a.dnormed, row * a.ld_dn, piece);
+        ask(ry, a.y, row * a.ld_y, piece);
+        mean_y = a.stats[2 * a.rows + row];
+        rstd_y = a.stats[3 * a.rows + row];
+      }
+      if (a.dy) ask(rd, a.dy, row * a.ld_dy, piece);
+      mean = a.stats[row];
+      rstd = a.stats[a.rows + row];
+    }
+    float G[NV][V], s = 0.0f, q = 0.0f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int i = 0; i < V; ++i) G[j][i] = here && a.dy ? (float)rd[j].v[i] : 0.0f;
+    if (a.dnormed) {
+      if (here)
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+          for (int i = 0; i < V; ++i) {
+            const float zy = ((float)ry[j].v[i] - mean_y) * rstd_y, d = piece(j).counts(i) ? (float)rn[j].v[i] : 0.0f;
+            sums[2][j][i] = fmaf(d, zy, sums[2][j][i]);
+            sums[3][j][i] += d;
+            const float g = d * w2[j][i];
+            s += g;
+            q = fmaf(g, zy, q);
+          }
+      row_sum2<W>(s, q, slots, turn);
+      s *= inv_n;
+      q *= inv_n;
+      if (here)
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+          for (int i = 0; i < V; ++i) {
+            const float zy = ((float)ry[j].v[i] - mean_y) * rstd_y;
+            G[j][i] = fmaf(rstd_y, fmaf((float)rn[j].v[i], w2[j][i], -s) - zy * q, G[j][i]);
+          }
+    }
+    s = q = 0.0f;
+    float g[NV][V];
+    if (here)
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        if (a.dresidual) piece(j).put((R*)a.dresidual + row * a.ld_dr, G[j]);
+        float dg[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          float act = 1.0f, slope = 0.0f;
+          if (a.gate) gate_of(a.act, (float)rg[j].v[i], act, slope);
+          const float z = ((float)rx[j].v[i] - mean) * rstd, scaled = G[j][i] * sc[j][i], t = piece(j).counts(i) ? G[j][i] * act : 0.0f;
+          dg[i] = scaled * fmaf(z, w[j][i], b[j][i]) * slope;
+          sums[0][j][i] = fmaf(t, z, sums[0][j][i]);
+          sums[1][j][i] += t;
+          g[j][i] = scaled * act * w[j][i];
+          const float counted = piece(j).counts(i) ? g[j][i] : 0.0f;
+          s += counted;
+          q = fmaf(counted, z, q);
+        }
+        if (a.dgate) piece(j).put((T*)a.dgate + row * a.ld_dg, dg);
+      }
+    row_sum2<W>(s, q, slots, turn);
+    s *= inv_n;
+    q *= inv_n;
+    if (here)
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        float o[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) o[i] = rstd * (g[j][i] - s - ((float)rx[j].v[i] - mean) * rstd * q);
+        piece(j).put((T*)a.dx + row * a.ld_dx, o);
+      }
+  }
+  if (!a.part) return;
+  float* part = a.part + (int64_t)blockIdx.x * 4 * a.n;
+  if constexpr (kRows > 1) {
+    for (int half = 0; half < 2; ++half) {
+      if (half) __syncthreads();
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+          for (int i = 0; i < V; ++i)
+            shared_sums[((group * 2 + k) * NV * V + j * V + i) * kThreads + tid] = half ? sums[2 + k][j][i] : sums[k][j][i];
+      __syncthreads();
+      for (int at = threadIdx.x; at < 2 * kEntries; at += kRows * kThreads) {
+        const int of = at % kEntries, ji = of / kThreads, i = ji % V;
+        float sum = 0.0f;
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) sum += shared_sums[r * 2 * kEntries + at];
+        const Piece<W, V> p(ji / V, of % kThreads, a.n);
+        if (p.counts(i)) part[(int64_t)(half * 2 + at / kEntries) * a.n + p.start + i] = sum;
+      }
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+          if (piece(j).counts(i)) part[(int64_t)k * a.n + piece(j).start + i] = sums[k][j][i];
+  }
+}
+
+// Adds up the partial rows and forms the parameters' gradients: 16 columns per workgroup, 64 groups of partial rows side by side.
+template <typename P>
+__global__ __launch_bounds__(1024) void block_norm_sum_kernel(BlockNormGradArgs a, int parts) {
+  __shared__ float sums[4][64][17];
+  const int lane = threadIdx.x & 15, group = threadIdx.x >> 4, c = blockIdx.x * 16 + lane;
+  float s[4] = {};
+  if (c < a.n)
+    for (int p = group; p < parts; p += 64)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) s[k] += a.part[((int64_t)p * 4 + k) * a.n + c];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) sums[k][group][lane] = s[k];
+  __syncthreads();
+  if (group < 4) {  // one wave: 16 groups each, then the four of them
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      s[k] = 0.0f;
+#pragma unroll
+      for (int g = 0; g < 16; ++g) s[k] += sums[k][group * 16 + g][lane];
+      s[k] += __shfl_xor(s[k], 16, 64);
+      s[k] += __shfl_xor(s[k], 32, 64);
+    }
+    if (group == 0 && c < a.n) {
+      const float w = a.weight ? (float)((const P*)a.weight)[c] : 1.0f, b = a.bias ? (float)((const P*)a.bias)[c] : 0.0f;
+      const float sc = a.scale ? (float)((const P*)a.scale)[c] : 1.0f;
+      if (a.dweight) ((P*)a.dweight)[c] = (P)(sc * s[0]);
+      if (a.dbias) ((P*)a.dbias)[c] = (P)(sc * s[1]);
+      if (a.dscale) ((P*)a.dscale)[c] = (P)fmaf(w, s[0], b * s[1]);
+      if (a.dnext_weight) ((P*)a.dnext_weight)[c] = (P)s[2];
+      if (a.dnext_bias) ((P*)a.dnext_bias)[c] = (P)s[3];
+    }
+  }
+}
+
+// Entries per lane, and waves per row, of rows of n entries.
+struct Shape {
+  int waves, pieces;
+};
+// 16 entries per lane at most forward (one wave up to 1024), 8 backward, where four sums per column stay in registers too; 16 of
+// either where 16 waves have no more.  Few rows go to four waves each from 512 entries on, where the row's latency counts.
+template <int V, bool GRAD>
+Shape shape_of(int64_t rows, int n) {
+  if constexpr (V == 1) return {1, 1};  // rows of less than 16 bytes
+  constexpr int per_lane = GRAD ? 8 : 16;
+  for (int p = 1; p * V <= per_lane; p *= 2)
+    if (n <= 64 * p * V && (rows > 512 || n <= 512)) return {1, p};
+  for (int p = 1; p * V <= per_lane; p *= 2)
+    if (n <= 256 * p * V) return {4, p};
+  if (n <= 512 * per_lane) return {8, per_lane / V};
+  if (n <= 1024 * per_lane) return {16, per_lane / V};
+  return {16, 16 / V};
+}
+
+template <typename F>
+hipError_t with_types(int type, int residual, int param, F f) {
+  auto params = [&](auto t, auto r) { return param == AMQ_F32 ? f(t, r, float()) : f(t, r, t); };
+  if (type == AMQ_F32) return f(float(), float(), float());
+  if (type == AMQ_BF16) return residual == AMQ_F32 ? params(bf16(), float()) : params(bf16(), bf16());
+  return residual == AMQ_F32 ? params(f16(), float()) : params(f16(), f16());
+}
+template <int V, bool GRAD, typename F>
+hipError_t with_shape(Shape h, F f) {
+#define AMQ_SHAPE(W, NV) \
+  if (h.waves == W && h.pieces == NV) return f(std::integral_constant<int, V>(), std::integral_constant<int, W>(), std::integral_constant<int, NV>())
+  AMQ_SHAPE(1, 1);
+  if constexpr (V > 1) {
+    constexpr int per_lane = GRAD ? 8 : 16, most = per_lane / V;
+    if constexpr (most >= 2) AMQ_SHAPE(1, 2);
+    if constexpr (most >= 4) AMQ_SHAPE(1, 4);
+    AMQ_SHAPE(4, 1);
+    if constexpr (most >= 2) AMQ_SHAPE(4, 2);
+    if constexpr (most >= 4) AMQ_SHAPE(4, 4);
+    AMQ_SHAPE(8, most);
+    AMQ_SHAPE(16, most);
+    if constexpr (GRAD) AMQ_SHAPE(16, 16 / V);
+  }
+#undef AMQ_SHAPE
+  return hipErrorInvalidValue;
+}
+// The kernels' entries per piece: 16 bytes of T, or one where a row has less.
+template <typename T, bool GRAD, typename F>
+hipError_t with_pieces(int64_t rows, int n, F f) {
+  constexpr int V = kPer16<T>;
+  if (n < V) return with_shape<1, GRAD>(shape_of<1, GRAD>(rows, n), f);
+  return with_shape<V, GRAD>(shape_of<V, GRAD>(rows, n), f);
+}
+
+// Rows that a grid of at most `most` workgroups takes at a time, spread evenly over its rounds.
+int64_t even_blocks(int64_t tasks, int64_t most) {
+  const int64_t rounds = (tasks + most - 1) / most;
+  return (tasks + rounds - 1) / rounds;
+}
+
+constexpr int64_t kMostParts = 256;  // one workgroup per compute unit: more partial rows cost more than they hide
+
+template <int W>
+int64_t grad_blocks(int64_t rows) { return even_blocks((rows + row_groups(W, 8) - 1) / row_groups(W, 8), kMostParts); }
+
+}  // namespace
+
+int block_norm_grad_parts(int64_t rows, int) { return (int)(rows < kMostParts ? rows : kMostParts); }
+
+hipError_t launch_block_norm(const BlockNormArgs& a, hipStream_t s) {
+  return with_types(a.type, a.residual_type, a.param_type, [&](auto t, auto r, auto p) {
+    using T = decltype(t);
+    return with_pieces<T, false>(a.rows, a.n, [&](auto v, auto w, auto nv) {
+      constexpr int W = decltype(w)::value, kRows = row_groups(W, 4);
+      const int64_t tasks = (a.rows + kRows - 1) / kRows;
+      block_norm_kernel<T, decltype(r), decltype(p), decltype(v)::value, W, decltype(nv)::value>
+          <<<dim3((unsigned)even_blocks(tasks, W >= 8 ? 512 : 1024)), dim3(kRows * W * 64), 0, s>>>(a);
+      return hipGetLastError();
+    });
+  });
+}
+
+hipError_t launch_block_norm_grad(const BlockNormGradArgs& a0, hipStream_t s) {
+  BlockNormGradArgs a = a0;
+  const bool sums = a.dweight || a.dbias || a.dscale || a.dnext_weight || a.dnext_bias;
+  if (!sums) a.part = nullptr;
+  return with_types(a.type, a.residual_type, a.param_type, [&](auto t, auto r, auto p) {
+    using T = decltype(t);
+    using P = decltype(p);
+    int64_t parts = 0;
+    const hipError_t e = with_pieces<T, true>(a.rows, a.n, [&](auto v, auto w, auto nv) {
+      constexpr int W = decltype(w)::value;
+      parts = grad_blocks<W>(a.rows);
+      block_norm_grad_kernel<T, decltype(r), P, decltype(v)::value, W, decltype(nv)::value>
+          <<<dim3((unsigned)parts), dim3(row_groups(W, 8) * W * 64), 0, s>>>(a);
+      return hipGetLastError();
+    });
+    if (e != hipSuccess || !sums) return e;
+    block_norm_sum_kernel<P><<<dim3((unsigned)((a.n + 15) / 16)), dim3(1024), 0, s>>>(a, (int)parts);
+    return hipGetLastError();
+  });
+}
+
+}  // namespace amq

@@ -12,6 +12,7 @@
 #include <vector>
 
 #include <ATen/hip/EmptyTensor.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/custom_function.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -31,7 +32,11 @@ namespace {
   X(amq_lm_sequence_score_workspace_bytes) X(amq_lm_sequence_score) X(amq_dequantize)      \
   X(amq_quantize_reconstruct) X(amq_layer_norm) X(amq_layer_norm_backward_workspace_bytes) X(amq_layer_norm_backward) \
   X(amq_linear_workspace_bytes) X(amq_linear) X(amq_linear_backward_workspace_bytes) X(amq_linear_backward)          \
-  X(amq_orthogonalize_workspace_bytes) X(amq_orthogonalize)
+  X(amq_orthogonalize_workspace_bytes) X(amq_orthogonalize)                                                          \
+  X(amq_linear_recurrence_workspace_bytes) X(amq_linear_recurrence)                                                  \
+  X(amq_linear_recurrence_backward_workspace_bytes) X(amq_linear_recurrence_backward) X(amq_block_norm)               \
+  X(amq_block_norm_backward_workspace_bytes) X(amq_block_norm_backward) X(amq_clip_gradients_workspace_bytes)         \
+  X(amq_clip_gradients)
 
 struct Api {
 #define AMQ_MEMBER(name) decltype(&::name) name = nullptr;
@@ -718,6 +723,243 @@ PyObject* orthogonalize(PyObject* const* a) {  // G, steps, a, b, c, eps, ws, ou
   return a[7] == Py_None ? wrap(own) : again(a[7]);
 }
 
+// ---- linear recurrences, joined norms, clipping: on the operands' device and its current stream
+
+const at::Tensor& on_gpu(PyObject* o) {
+  const at::Tensor& t = tensor(o);
+  if (!t.is_cuda()) fail(amq_error, "expected a GPU tensor");
+  return t;
+}
+// A tuple of results (takes the references).
+PyObject* tuple(std::initializer_list<PyObject*> items) {
+  PyObject* r = PyTuple_New((Py_ssize_t)items.size());
+  bool all = r != nullptr;
+  Py_ssize_t i = 0;
+  for (PyObject* o : items) {
+    all = all && o;
+    if (r) PyTuple_SET_ITEM(r, i++, o);
+    else Py_XDECREF(o);
+  }
+  if (!all) Py_CLEAR(r);
+  return r;
+}
+
+// A tensor [steps, batch, n] with n side by side.
+struct Steps {
+  void* p = nullptr;
+  int64_t steps = 0, batch = 0, n = 0, step = 0, entry = 0;
+  explicit Steps(const at::Tensor& t) {
+    if (!t.is_cuda()) fail(amq_error, "expected a GPU tensor");
+    if (t.dim() != 3) fail(PyExc_ValueError, "expected a tensor [steps, batch, n], got " + std::to_string(t.dim()) + " dimensions");
+    steps = t.size(0), batch = t.size(1), n = t.size(2);
+    if (t.stride(2) != 1 && n > 1) fail(amq_error, "expected the channels side by side (a last stride of 1)");
+    step = t.stride(0), entry = t.stride(1);
+    p = t.data_ptr();
+  }
+  Steps(const at::Tensor& t, const char* name, const Steps& like, const at::Tensor& of) : Steps(t) {
+    if (steps != like.steps || batch != like.batch || n != like.n)
+      fail(PyExc_ValueError, std::string(name) + ": expected [" + std::to_string(like.steps) + ", " + std::to_string(like.batch) + ", " + std::to_string(like.n) + "]");
+    if (t.scalar_type() != of.scalar_type())
+      fail(amq_error, std::string(name) + ": expected " + dtype_name(of.scalar_type()) + ", got " + dtype_name(t.scalar_type()));
+    if (t.device() != of.device()) fail(amq_error, std::string(name) + ": expected a tensor on the same device");
+  }
+};
+// A contiguous tensor of the given type and shape, or null.
+void* exactly(PyObject* o, const char* name, at::IntArrayRef shape, at::ScalarType dt, const at::Tensor& like) {
+  if (o == Py_None) return nullptr;
+  const at::Tensor& t = tensor(o);
+  if (t.device() != like.device()) fail(amq_error, std::string(name) + ": expected a tensor on the same device");
+  if (t.scalar_type() != dt) fail(amq_error, std::string(name) + ": expected " + dtype_name(dt) + ", got " + dtype_name(t.scalar_type()));
+  if (t.sizes() != shape || !t.is_contiguous()) {
+    std::string want;
+    for (int64_t d : shape) want += (want.empty() ? "" : ", ") + std::to_string(d);
+    fail(PyExc_ValueError, std::string(name) + ": expected a contiguous tensor [" + want + "]");
+  }
+  return t.data_ptr();
+}
+
+PyObject* linear_recurrence(PyObject* const* a) {  // gate, x, h0, mode, lengths, states, ws, out, h_out
+  no_graph("linear_recurrence", "take training.linear_recurrence, or ", {a[0], a[1], a[2]});
+  const at::Tensor& x = on_gpu(a[1]);
+  const c10::DeviceGuard guard(x.device());
+  const int type = type_of(x), mode = (int)integer(a[3]);
+  const Steps r(x), g(tensor(a[0]), "gate", r, x);
+  const float* h0 = static_cast<const float*>(exactly(a[2], "h0", {r.batch, r.n}, at::kFloat, x));
+  const int64_t* lengths = static_cast<const int64_t*>(exactly(a[4], "lengths", {r.batch}, at::kLong, x));
+  at::Tensor hs, last, states;
+  if (a[7] == Py_None) hs = make(x.sizes(), x.scalar_type(), x);
+  else hs = tensor(a[7]);
+  const Steps y(hs, "out", r, x);
+  if (a[8] == Py_None) last = make({r.batch, r.n}, at::kFloat, x);
+  float* h = static_cast<float*>(a[8] == Py_None ? last.data_ptr() : exactly(a[8], "h_out", {r.batch, r.n}, at::kFloat, x));
+  const int64_t kept = r.steps > 0 ? (r.steps - 1) / AMQ_STATE_STEPS : 0;
+  if (integer(a[5]) && kept > 0) states = make({kept, r.batch, r.n}, at::kFloat, x);
+  float* st = states.defined() ? static_cast<float*>(states.data_ptr()) : nullptr;
+  Workspace ws(a[6], x, [&] { return api.amq_linear_recurrence_workspace_bytes(r.steps, r.batch, r.n, type); });
+  void* s = stream();
+  call([&] {
+    return api.amq_linear_recurrence(g.p, g.step, g.entry, r.p, r.step, r.entry, r.steps, r.batch, r.n, type, mode, lengths, h0, y.p, y.step, y.entry, h,
+                                     st, ws.ptr, ws.bytes, s);
+  });
+  return tuple({a[7] == Py_None ? wrap(hs) : again(a[7]), a[8] == Py_None ? wrap(last) : again(a[8]), states.defined() ? wrap(states) : none()});
+}
+
+PyObject* linear_recurrence_backward(PyObject* const* a) {  // dhs, gate, x, h0, states, dh_last, mode, lengths, ws, dgate, dx
+  const at::Tensor& x = on_gpu(a[2]);
+  const c10::DeviceGuard guard(x.device());
+  const int type = type_of(x), mode = (int)integer(a[6]);
+  const Steps r(x), g(tensor(a[1]), "gate", r, x), d(tensor(a[0]), "dhs", r, x);
+  const float* h0 = static_cast<const float*>(exactly(a[3], "h0", {r.batch, r.n}, at::kFloat, x));
+  const int64_t kept = r.steps > 0 ? (r.steps - 1) / AMQ_STATE_STEPS : 0;
+  if (kept > 0 && a[4] == Py_None) fail(PyExc_ValueError, "states: needed beyond " + std::to_string(AMQ_STATE_STEPS) + " steps (linear_recurrence leaves them with states=True)");
+  const float* st = kept > 0 ? static_cast<const float*>(exactly(a[4], "states", {kept, r.batch, r.n}, at::kFloat, x)) : nullptr;
+  const float* dl = static_cast<const float*>(exactly(a[5], "dh_last", {r.batch, r.n}, at::kFloat, x));
+  const int64_t* lengths = static_cast<const int64_t*>(exactly(a[7], "lengths", {r.batch}, at::kLong, x));
+  at::Tensor dg = a[9] == Py_None ? make(x.sizes(), x.scalar_type(), x) : tensor(a[9]);
+  at::Tensor dx = a[10] == Py_None ? make(x.sizes(), x.scalar_type(), x) : tensor(a[10]);
+  const Steps rg(dg, "dgate", r, x), rx(dx, "dx", r, x);
+  at::Tensor dh0;
+  if (h0) dh0 = make({r.batch, r.n}, at::kFloat, x);
+  float* r0 = h0 ? static_cast<float*>(dh0.data_ptr()) : nullptr;
+  Workspace ws(a[8], x, [&] { return api.amq_linear_recurrence_backward_workspace_bytes(r.steps, r.batch, r.n, type); });
+  void* s = stream();
+  call([&] {
+    return api.amq_linear_recurrence_backward(d.p, d.step, d.entry, g.p, g.step, g.entry, r.p, r.step, r.entry, r.steps, r.batch, r.n, type, mode, lengths,
+                                              h0, st, dl, rg.p, rg.step, rg.entry, rx.p, rx.step, rx.entry, r0, ws.ptr, ws.bytes, s);
+  });
+  return tuple({a[9] == Py_None ? wrap(dg) : again(a[9]), a[10] == Py_None ? wrap(dx) : again(a[10]), h0 ? wrap(dh0) : none()});
+}
+
+// The parameters of a joined norm: vectors of one type.
+struct Parameters {
+  const at::Tensor& x;
+  int64_t n;
+  const at::Tensor* first = nullptr;
+  const void* add(PyObject* o, const char* name) {
+    const void* p = vector_of(o, name, n, at::kFloat, x.scalar_type(), x);
+    if (!p) return p;
+    const at::Tensor& t = tensor(o);
+    if (first && first->scalar_type() != t.scalar_type()) fail(amq_error, std::string(name) + ": expected the same type as the other parameters");
+    if (!first) first = &t;
+    return p;
+  }
+  int type() const { return type_of(first ? *first : x); }
+};
+void residual_type_ok(const at::Tensor& t, const char* name, const at::Tensor& x) {
+  if (t.scalar_type() != at::kFloat && t.scalar_type() != x.scalar_type())
+    fail(amq_error, std::string(name) + ": expected torch.float32 or the type of x, got " + dtype_name(t.scalar_type()));
+  if (t.device() != x.device()) fail(amq_error, std::string(name) + ": expected a tensor on the same device");
+}
+
+PyObject* block_norm(PyObject* const* a) {  // x, residual, weight, bias, gate, activation, scale, next_weight, next_bias, eps, normed, out, out_normed
+  no_graph("block_norm", "take training.block_norm, or ", {a[0], a[1], a[2], a[3], a[4], a[6], a[7], a[8]});
+  const at::Tensor &x = on_gpu(a[0]), &residual = tensor(a[1]);
+  const c10::DeviceGuard guard(x.device());
+  const int type = type_of(x), act = (int)integer(a[5]);
+  const Rows r(x), h(residual, "residual", r.rows, r.n, residual), g = Rows::optional(a[4], "gate", r.rows, r.n, x);
+  residual_type_ok(residual, "residual", x);
+  Parameters params{x, r.n};
+  const void *w = params.add(a[2], "weight"), *b = params.add(a[3], "bias"), *sc = params.add(a[6], "scale");
+  const void *w2 = params.add(a[7], "next_weight"), *b2 = params.add(a[8], "next_bias");
+  const float eps = (float)real(a[9]);
+  const bool normed = integer(a[10]) != 0;
+  if (!normed && (w2 || b2 || a[12] != Py_None)) fail(PyExc_ValueError, "next_weight, next_bias, out_normed: given without normed");
+  Result y(a[11], "out", residual.sizes(), r.rows, r.n, residual);
+  std::vector<Result> n;
+  if (normed) n.emplace_back(a[12], "out_normed", x.sizes(), r.rows, r.n, x);
+  at::Tensor stats = make({4, r.rows}, at::kFloat, x);
+  float* q = static_cast<float*>(stats.data_ptr());
+  const int residual_type = type_of(residual), param_type = params.type();
+  void *pn = normed ? n[0].rows.p : nullptr, *s = stream();
+  const int64_t ld_n = normed ? n[0].rows.ld : 0;
+  call([&] {
+    return api.amq_block_norm(r.p, r.ld, h.p, h.ld, g.p, g.ld, r.rows, r.n, type, residual_type, param_type, act, w, b, sc, w2, b2, eps, y.rows.p, y.rows.ld,
+                              pn, ld_n, q, s);
+  });
+  return tuple({y.take(), normed ? n[0].take() : none(), wrap(stats)});
+}
+
+PyObject* block_norm_backward(PyObject* const* a) {  // dy, dnormed, x, y, stats, weight, bias, gate, activation, scale, next_weight, next_bias, param_grads, ws
+  const at::Tensor &x = on_gpu(a[2]), &y = tensor(a[3]);
+  const c10::DeviceGuard guard(x.device());
+  const int type = type_of(x), act = (int)integer(a[8]);
+  const Rows r(x), h(y, "y", r.rows, r.n, y), g = Rows::optional(a[7], "gate", r.rows, r.n, x);
+  residual_type_ok(y, "y", x);
+  if (a[0] == Py_None && a[1] == Py_None) fail(PyExc_ValueError, "dy, dnormed: expected one of them at least");
+  const Rows d = Rows::optional(a[0], "dy", r.rows, r.n, y), dn = Rows::optional(a[1], "dnormed", r.rows, r.n, x);
+  const float* stats = static_cast<const float*>(exactly(a[4], "stats", {4, r.rows}, at::kFloat, x));
+  if (!stats) fail(PyExc_ValueError, "stats: expected what block_norm left");
+  Parameters params{x, r.n};
+  const void *w = params.add(a[5], "weight"), *b = params.add(a[6], "bias"), *sc = params.add(a[9], "scale"), *w2 = params.add(a[10], "next_weight");
+  const bool next_bias = params.add(a[11], "next_bias") != nullptr;
+  const bool sums = integer(a[12]) != 0;
+  const at::ScalarType pt = params.first ? params.first->scalar_type() : x.scalar_type();
+  at::Tensor dx = make(x.sizes(), x.scalar_type(), x), dr = make(y.sizes(), y.scalar_type(), x), dg, p[5];
+  const Rows rx(dx), rr(dr);
+  Rows rg;
+  if (g.p) {
+    dg = make(x.sizes(), x.scalar_type(), x);
+    rg = Rows(dg);
+  }
+  // gradients of the parameters that are there (those of the second norm: zeros of a sum where dnormed is none)
+  const bool wanted[5] = {w != nullptr, b != nullptr, sc != nullptr, w2 != nullptr, next_bias};
+  void* q[5] = {};
+  for (int i = 0; i < 5; ++i)
+    if (sums && wanted[i]) {
+      p[i] = make({r.n}, pt, x);
+      q[i] = p[i].data_ptr();
+    }
+  const bool any = q[0] || q[1] || q[2] || q[3] || q[4];
+  Workspace ws(a[13], x, [&] { return any ? api.amq_block_norm_backward_workspace_bytes(r.rows, r.n) : 0; });
+  const int residual_type = type_of(y), param_type = params.type();
+  void* s = stream();
+  call([&] {
+    return api.amq_block_norm_backward(d.p, d.ld, dn.p, dn.ld, r.p, r.ld, h.p, h.ld, g.p, g.ld, r.rows, r.n, type, residual_type, param_type, act, w, b, sc,
+                                       w2, stats, rx.p, rx.ld, rr.p, rr.ld, rg.p, rg.ld, q[0], q[1], q[2], q[3], q[4], ws.ptr, ws.bytes, s);
+  });
+  auto take = [&](const at::Tensor& t) { return t.defined() ? wrap(t) : none(); };
+  return tuple({wrap(dx), wrap(dr), take(dg), take(p[0]), take(p[1]), take(p[2]), take(p[3]), take(p[4])});
+}
+
+PyObject* clip_gradients(PyObject* const* a) {  // list of tensors, list of results or None (the norm alone), max_norm, ws
+  if (!PyList_Check(a[0]) || (a[1] != Py_None && !PyList_Check(a[1]))) fail(PyExc_TypeError, "expected lists of tensors");
+  const Py_ssize_t count = PyList_GET_SIZE(a[0]);
+  const bool scale = a[1] != Py_None;
+  if (scale && PyList_GET_SIZE(a[1]) != count) fail(PyExc_ValueError, "out: expected as many tensors as gradients");
+  if (count == 0) fail(PyExc_ValueError, "expected at least one tensor");
+  const at::Tensor& like = on_gpu(PyList_GET_ITEM(a[0], 0));
+  const c10::DeviceGuard guard(like.device());
+  std::vector<const void*> in((size_t)count);
+  std::vector<void*> out((size_t)count);
+  std::vector<int64_t> sizes((size_t)count);
+  std::vector<int> types((size_t)count);
+  for (Py_ssize_t i = 0; i < count; ++i) {
+    PyObject* o = PyList_GET_ITEM(a[0], i);
+    no_graph("clip_gradients", "", {o});
+    const at::Tensor& t = on_gpu(o);
+    if (t.device() != like.device()) fail(amq_error, "expected tensors on the same device");
+    if (!t.is_non_overlapping_and_dense()) fail(amq_error, "expected dense tensors (no entries apart in memory)");
+    in[i] = t.data_ptr();
+    sizes[i] = t.numel();
+    types[i] = type_of(t);
+    if (!scale) continue;
+    const at::Tensor& q = tensor(PyList_GET_ITEM(a[1], i));
+    if (q.device() != like.device()) fail(amq_error, "out: expected tensors on the same device");
+    if (q.scalar_type() != t.scalar_type()) fail(amq_error, std::string("out: expected ") + dtype_name(t.scalar_type()) + ", got " + dtype_name(q.scalar_type()));
+    if (q.sizes() != t.sizes() || (!(q.is_contiguous() && t.is_contiguous()) && q.strides() != t.strides()))
+      fail(PyExc_ValueError, "out: expected the gradients' shapes and strides");
+    no_graph("clip_gradients", "", {PyList_GET_ITEM(a[1], i)});
+    out[i] = q.data_ptr();
+  }
+  const float max_norm = (float)real(a[2]);
+  at::Tensor norm = make({}, at::kFloat, like);
+  float* pn = static_cast<float*>(norm.data_ptr());
+  Workspace ws(a[3], like, [&] { return api.amq_clip_gradients_workspace_bytes(count); });
+  void* s = stream();
+  call([&] { return api.amq_clip_gradients(count, in.data(), sizes.data(), types.data(), max_norm, scale ? out.data() : nullptr, pn, ws.ptr, ws.bytes, s); });
+  return wrap(norm);
+}
+
 // ---- module
 
 template <PyObject* (*F)(PyObject* const*), int N>
@@ -770,7 +1012,8 @@ PyMethodDef methods[] = {
     AMQ_METHOD(softmax_layer, 9), AMQ_METHOD(lm_step, 20), AMQ_METHOD(lm_sequence, 20),
     AMQ_METHOD(lm_sequence_score, 21), AMQ_METHOD(dequantize, 4), AMQ_METHOD(fake_quantize, 3),
     AMQ_METHOD(layer_norm, 5), AMQ_METHOD(layer_norm_backward, 8), AMQ_METHOD(linear, 8), AMQ_METHOD(linear_backward, 7),
-    AMQ_METHOD(orthogonalize, 8),
+    AMQ_METHOD(orthogonalize, 8), AMQ_METHOD(linear_recurrence, 9), AMQ_METHOD(linear_recurrence_backward, 11), AMQ_METHOD(block_norm, 13),
+    AMQ_METHOD(block_norm_backward, 14), AMQ_METHOD(clip_gradients, 4),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_amq_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

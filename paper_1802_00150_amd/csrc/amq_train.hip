@@ -2,6 +2,10 @@
 // the caller's stream.
 #include "amq_train.h"
 
+#include <algorithm>
+#include <memory>
+#include <new>
+
 #include "../../include/amq.h"
 
 namespace {
@@ -66,6 +70,69 @@ bool meets(const Extent& result, const Extent (&others)[N]) {
     if (overlap(result, o)) return true;
   return false;
 }
+
+// A tensor [steps][B][n]: `count` matrices, `apart` bytes from one to the next.
+struct Volume {
+  Extent matrix;
+  int64_t count, apart;
+};
+Volume volume(const void* p, int64_t steps, int64_t B, int64_t n, int64_t step, int64_t batch, int type) {
+  const int64_t size = (int64_t)size_of(type), width = n * size;
+  int64_t rows[2] = {steps, B}, by[2] = {step * size, batch * size};
+  for (int i = 0; i < 2; ++i)
+    if (rows[i] == 1 || by[i] == 0) rows[i] = 1, by[i] = width;  // (the same rows again)
+  const int large = by[0] >= by[1] ? 0 : 1, small = 1 - large;
+  const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+  if (rows[large] == 1) return {{at, rows[small], width, by[small]}, 1, 0};
+  if (rows[small] == 1) return {{at, rows[large], width, by[large]}, 1, 0};
+  if (by[large] == rows[small] * by[small]) return {{at, rows[0] * rows[1], width, by[small]}, 1, 0};
+  // matrices that lie one behind the other meet few others; many of them are taken the other way
+  const int outer = rows[large] <= 4096 || rows[large] <= rows[small] ? large : small, inner = 1 - outer;
+  return {{at, rows[inner], width, by[inner]}, rows[outer], by[outer]};
+}
+int64_t extent_bytes(const Extent& e) { return (e.rows - 1) * e.step + e.width; }
+bool overlap(const Volume& a, const Volume& b) {
+  if (!a.matrix.p || !b.matrix.p) return false;
+  const int64_t room_a = extent_bytes(a.matrix), room_b = extent_bytes(b.matrix);
+  for (int64_t i = 0; i < a.count; ++i) {
+    const Extent m{a.matrix.p + i * a.apart, a.matrix.rows, a.matrix.width, a.matrix.step};
+    const int64_t from = (int64_t)(m.p - b.matrix.p);
+    int64_t j = b.count > 1 ? floor_div(from - room_b, b.apart) : 0;  // the first that may reach m
+    for (j = j > 0 ? j : 0; j < b.count && j * b.apart < from + room_a; ++j)
+      if (overlap(m, {b.matrix.p + j * b.apart, b.matrix.rows, b.matrix.width, b.matrix.step})) return true;
+  }
+  return false;
+}
+Volume of(const Extent& e) { return {e, 1, 0}; }
+template <int N>
+bool meets(const Volume& result, const Volume (&others)[N]) {
+  for (const Volume& o : others)
+    if (overlap(result, o)) return true;
+  return false;
+}
+
+// Tensors [steps][B][n] of a recurrence: rows are told apart by steps in batch entries or by batch entries in steps.
+bool apart(int64_t steps, int64_t B, int64_t n, int64_t step, int64_t batch) {
+  if (steps == 1) return B == 1 || batch >= n;
+  if (B == 1) return step >= n;
+  return (batch >= n && step >= (B - 1) * batch + n) || (step >= n && batch >= (steps - 1) * step + n);
+}
+bool recurrence_sizes_ok(int64_t steps, int64_t B, int64_t n) { return steps > 0 && B > 0 && n > 0; }
+bool recurrence_sizes_supported(int64_t steps, int64_t B, int64_t n) {
+  return steps <= (1 << 24) && B <= (1 << 22) && n <= kMaxSize && B * n <= (1 << 30);
+}
+bool strides_ok(int64_t step, int64_t batch) { return step >= 0 && batch >= 0; }
+bool strides_supported(int64_t step, int64_t batch) { return step <= (1LL << 36) && batch <= (1LL << 36); }
+int64_t states_of(int64_t steps) { return (steps - 1) / AMQ_STATE_STEPS; }
+
+// Limits of the joined norms: a row stays in the registers of one workgroup.
+constexpr int64_t kMaxJoined = 16384;
+bool gate_act_ok(int act) { return act == AMQ_ACT_NONE || act == AMQ_ACT_SIGMOID || act == AMQ_ACT_SILU; }
+
+struct Interval {
+  uintptr_t begin, end;
+  int64_t index;
+};
 
 }  // namespace
 
@@ -200,6 +267,193 @@ int amq_orthogonalize(const void* G, int64_t batch, int64_t batch_stride, int64_
   return amq::status_of(amq::launch_ortho({G, out, batch_stride, ld, batch_stride_out, ld_out, (int)batch, (int)rows, (int)cols, type, steps,
                                            coef[0], coef[1], coef[2], eps, workspace},
                                           static_cast<hipStream_t>(stream)));
+}
+
+size_t amq_linear_recurrence_workspace_bytes(int64_t steps, int64_t B, int64_t n, int type) {
+  if (!recurrence_sizes_ok(steps, B, n) || !recurrence_sizes_supported(steps, B, n) || !type_ok(type)) return 0;
+  return amq::recurrence_workspace(steps, B, n, type);
+}
+
+int amq_linear_recurrence(const void* gate, int64_t gate_step, int64_t gate_batch, const void* x, int64_t x_step, int64_t x_batch,
+                          int64_t steps, int64_t B, int64_t n, int type, int mode, const int64_t* lengths, const float* h0,
+                          void* hs, int64_t hs_step, int64_t hs_batch, float* h_last, float* states, void* workspace,
+                          size_t workspace_bytes, void* stream) {
+  if (!gate || !x || !hs || !type_ok(type) || (mode != AMQ_RECURRENCE_BLEND && mode != AMQ_RECURRENCE_DECAY)) return AMQ_ERR_INVALID;
+  if (!recurrence_sizes_ok(steps, B, n) || !strides_ok(gate_step, gate_batch) || !strides_ok(x_step, x_batch) || !strides_ok(hs_step, hs_batch))
+    return AMQ_ERR_INVALID;
+  if (!on_elements(gate, type) || !on_elements(x, type) || !on_elements(hs, type) || !on_elements(h0, AMQ_F32) || !on_elements(h_last, AMQ_F32) ||
+      !on_elements(states, AMQ_F32) || (reinterpret_cast<uintptr_t>(lengths) & 7))
+    return AMQ_ERR_INVALID;
+  if (!recurrence_sizes_supported(steps, B, n) || !strides_supported(gate_step, gate_batch) || !strides_supported(x_step, x_batch) ||
+      !strides_supported(hs_step, hs_batch))
+    return AMQ_ERR_UNSUPPORTED;
+  if (!apart(steps, B, n, hs_step, hs_batch)) return AMQ_ERR_INVALID;
+  if (states_of(steps) == 0) states = nullptr;
+  const Volume eg = volume(gate, steps, B, n, gate_step, gate_batch, type), ex = volume(x, steps, B, n, x_step, x_batch, type);
+  const Volume out = volume(hs, steps, B, n, hs_step, hs_batch, type);
+  const Extent h = vector(h0, B * n, AMQ_F32), last = vector(h_last, B * n, AMQ_F32);
+  const Volume st = of(vector(states, states_of(steps) * B * n, AMQ_F32)), len = of(vector(lengths, 2 * B, AMQ_F32));
+  if (meets(out, {eg, ex, of(h), of(last), st, len}) || meets(of(last), {eg, ex, st, len}) || meets(st, {eg, ex, of(h), len}) ||
+      (!same(h, last) && overlap(h, last)))
+    return AMQ_ERR_INVALID;
+  if (!workspace_ok(workspace, workspace_bytes, amq::recurrence_workspace(steps, B, n, type))) return AMQ_ERR_INVALID;
+  // batch entries side by side are channels of one wider entry
+  if (!lengths && (B == 1 || (gate_batch == n && x_batch == n && hs_batch == n))) n *= B, B = 1;
+  return amq::status_of(amq::launch_recurrence({gate, x, hs, gate_step, gate_batch, x_step, x_batch, hs_step, hs_batch, steps, B, (int)n, type, mode,
+                                                lengths, h0, h_last, states, workspace},
+                                               static_cast<hipStream_t>(stream)));
+}
+
+size_t amq_linear_recurrence_backward_workspace_bytes(int64_t steps, int64_t B, int64_t n, int type) {
+  if (!recurrence_sizes_ok(steps, B, n) || !recurrence_sizes_supported(steps, B, n) || !type_ok(type)) return 0;
+  return amq::recurrence_grad_workspace(steps, B, n, type);
+}
+
+int amq_linear_recurrence_backward(const void* dhs, int64_t dhs_step, int64_t dhs_batch, const void* gate, int64_t gate_step,
+                                   int64_t gate_batch, const void* x, int64_t x_step, int64_t x_batch, int64_t steps, int64_t B,
+                                   int64_t n, int type, int mode, const int64_t* lengths, const float* h0, const float* states,
+                                   const float* dh_last, void* dgate, int64_t dgate_step, int64_t dgate_batch, void* dx,
+                                   int64_t dx_step, int64_t dx_batch, float* dh0, void* workspace, size_t workspace_bytes,
+                                   void* stream) {
+  if (!dhs || !gate || !x || !dgate || !dx || !type_ok(type) || (mode != AMQ_RECURRENCE_BLEND && mode != AMQ_RECURRENCE_DECAY)) return AMQ_ERR_INVALID;
+  if (!recurrence_sizes_ok(steps, B, n) || !strides_ok(dhs_step, dhs_batch) || !strides_ok(gate_step, gate_batch) || !strides_ok(x_step, x_batch) ||
+      !strides_ok(dgate_step, dgate_batch) || !strides_ok(dx_step, dx_batch) || (states_of(steps) > 0 && !states))
+    return AMQ_ERR_INVALID;
+  if (!on_elements(dhs, type) || !on_elements(gate, type) || !on_elements(x, type) || !on_elements(dgate, type) || !on_elements(dx, type) ||
+      !on_elements(h0, AMQ_F32) || !on_elements(states, AMQ_F32) || !on_elements(dh_last, AMQ_F32) || !on_elements(dh0, AMQ_F32) ||
+      (reinterpret_cast<uintptr_t>(lengths) & 7))
+    return AMQ_ERR_INVALID;
+  if (!recurrence_sizes_supported(steps, B, n) || !strides_supported(dhs_step, dhs_batch) || !strides_supported(gate_step, gate_batch) ||
+      !strides_supported(x_step, x_batch) || !strides_supported(dgate_step, dgate_batch) || !strides_supported(dx_step, dx_batch))
+    return AMQ_ERR_UNSUPPORTED;
+  if (!apart(steps, B, n, dgate_step, dgate_batch) || !apart(steps, B, n, dx_step, dx_batch)) return AMQ_ERR_INVALID;
+  if (states_of(steps) == 0) states = nullptr;
+  const Volume ed = volume(dhs, steps, B, n, dhs_step, dhs_batch, type), eg = volume(gate, steps, B, n, gate_step, gate_batch, type);
+  const Volume ex = volume(x, steps, B, n, x_step, x_batch, type), rg = volume(dgate, steps, B, n, dgate_step, dgate_batch, type);
+  const Volume rx = volume(dx, steps, B, n, dx_step, dx_batch, type), r0 = of(vector(dh0, B * n, AMQ_F32));
+  const Volume h = of(vector(h0, B * n, AMQ_F32)), st = of(vector(states, states_of(steps) * B * n, AMQ_F32));
+  const Volume dl = of(vector(dh_last, B * n, AMQ_F32)), len = of(vector(lengths, 2 * B, AMQ_F32));
+  if (meets(rg, {ed, eg, ex, h, st, dl, len, rx, r0}) || meets(rx, {ed, eg, ex, h, st, dl, len, r0}) || meets(r0, {ed, eg, ex, h, st, dl, len}))
+    return AMQ_ERR_INVALID;
+  if (!workspace_ok(workspace, workspace_bytes, amq::recurrence_grad_workspace(steps, B, n, type))) return AMQ_ERR_INVALID;
+  if (!lengths && (B == 1 || (dhs_batch == n && gate_batch == n && x_batch == n && dgate_batch == n && dx_batch == n))) n *= B, B = 1;
+  return amq::status_of(amq::launch_recurrence_grad({dhs, gate, x, dgate, dx, dhs_step, dhs_batch, gate_step, gate_batch, x_step, x_batch, dgate_step,
+                                                     dgate_batch, dx_step, dx_batch, steps, B, (int)n, type, mode, lengths, h0, states, dh_last,
+                                                     dh0, workspace},
+                                                    static_cast<hipStream_t>(stream)));
+}
+
+int amq_block_norm(const void* x, int64_t ld_x, const void* residual, int64_t ld_r, const void* gate, int64_t ld_g, int64_t rows,
+                   int64_t n, int type, int residual_type, int param_type, int activation, const void* weight, const void* bias,
+                   const void* scale, const void* next_weight, const void* next_bias, float eps, void* y, int64_t ld_y,
+                   void* normed, int64_t ld_n, float* stats, void* stream) {
+  if (!x || !residual || !y || !type_ok(type) || (residual_type != AMQ_F32 && residual_type != type) || (param_type != AMQ_F32 && param_type != type) ||
+      !gate_act_ok(activation))
+    return AMQ_ERR_INVALID;
+  if (rows <= 0 || n <= 0 || ld_x < n || ld_r < n || (gate && ld_g < n) || ld_y < n || (normed && ld_n < n) || !(eps >= 0.0f)) return AMQ_ERR_INVALID;
+  if (!on_elements(x, type) || !on_elements(residual, residual_type) || !on_elements(gate, type) || !on_elements(y, residual_type) ||
+      !on_elements(normed, type) || !on_elements(weight, param_type) || !on_elements(bias, param_type) || !on_elements(scale, param_type) ||
+      !on_elements(next_weight, param_type) || !on_elements(next_bias, param_type) || !on_elements(stats, AMQ_F32))
+    return AMQ_ERR_INVALID;
+  if (rows > 0x7fffffffLL || n > kMaxJoined) return AMQ_ERR_UNSUPPORTED;
+  const Extent ex = matrix(x, rows, n, ld_x, type), er = matrix(residual, rows, n, ld_r, residual_type), eg = matrix(gate, rows, n, ld_g, type);
+  const Extent ey = matrix(y, rows, n, ld_y, residual_type), en = matrix(normed, rows, n, ld_n, type), es = vector(stats, 4 * rows, AMQ_F32);
+  const Extent params[] = {vector(weight, n, param_type), vector(bias, n, param_type), vector(scale, n, param_type),
+                           vector(next_weight, n, param_type), vector(next_bias, n, param_type)};
+  if (meets(ey, params) || meets(en, params) || meets(es, params) || meets(ey, {ex, eg, en, es}) || (!same(ey, er) && overlap(ey, er)) ||
+      meets(en, {ex, er, eg, es}) || meets(es, {ex, er, eg}))
+    return AMQ_ERR_INVALID;
+  return amq::status_of(amq::launch_block_norm({x, residual, gate, weight, bias, scale, next_weight, next_bias, y, normed, stats, rows, ld_x, ld_r, ld_g,
+                                                ld_y, ld_n, (int)n, type, residual_type, param_type, activation, eps},
+                                               static_cast<hipStream_t>(stream)));
+}
+
+size_t amq_block_norm_backward_workspace_bytes(int64_t rows, int64_t n) {
+  if (rows <= 0 || n <= 0 || rows > 0x7fffffffLL || n > kMaxJoined) return 0;
+  return (sizeof(float) * 4 * (size_t)amq::block_norm_grad_parts(rows, (int)n) * n + 255) & ~size_t(255);
+}
+
+int amq_block_norm_backward(const void* dy, int64_t ld_dy, const void* dnormed, int64_t ld_dn, const void* x, int64_t ld_x,
+                            const void* y, int64_t ld_y, const void* gate, int64_t ld_g, int64_t rows, int64_t n, int type,
+                            int residual_type, int param_type, int activation, const void* weight, const void* bias,
+                            const void* scale, const void* next_weight, const float* stats, void* dx, int64_t ld_dx,
+                            void* dresidual, int64_t ld_dr, void* dgate, int64_t ld_dg, void* dweight, void* dbias, void* dscale,
+                            void* dnext_weight, void* dnext_bias, void* workspace, size_t workspace_bytes, void* stream) {
+  if ((!dy && !dnormed) || !x || (dnormed && !y) || !stats || !dx || (dgate && !gate) || !type_ok(type) ||
+      (residual_type != AMQ_F32 && residual_type != type) || (param_type != AMQ_F32 && param_type != type) || !gate_act_ok(activation))
+    return AMQ_ERR_INVALID;
+  if (rows <= 0 || n <= 0 || (dy && ld_dy < n) || (dnormed && (ld_dn < n || ld_y < n)) || ld_x < n || (gate && ld_g < n) || ld_dx < n ||
+      (dresidual && ld_dr < n) || (dgate && ld_dg < n))
+    return AMQ_ERR_INVALID;
+  if (!on_elements(dy, residual_type) || !on_elements(dnormed, type) || !on_elements(x, type) || !on_elements(y, residual_type) ||
+      !on_elements(gate, type) || !on_elements(dx, type) || !on_elements(dresidual, residual_type) || !on_elements(dgate, type) ||
+      !on_elements(weight, param_type) || !on_elements(bias, param_type) || !on_elements(scale, param_type) ||
+      !on_elements(next_weight, param_type) || !on_elements(stats, AMQ_F32) || !on_elements(dweight, param_type) || !on_elements(dbias, param_type) ||
+      !on_elements(dscale, param_type) || !on_elements(dnext_weight, param_type) || !on_elements(dnext_bias, param_type))
+    return AMQ_ERR_INVALID;
+  if (rows > 0x7fffffffLL || n > kMaxJoined) return AMQ_ERR_UNSUPPORTED;
+  const Extent none{}, ed = matrix(dy, rows, n, ld_dy, residual_type), en = matrix(dnormed, rows, n, ld_dn, type), ex = matrix(x, rows, n, ld_x, type);
+  const Extent ey = dnormed ? matrix(y, rows, n, ld_y, residual_type) : none, eg = matrix(gate, rows, n, ld_g, type), es = vector(stats, 4 * rows, AMQ_F32);
+  const Extent operands[] = {en, ex, ey, eg, es, vector(weight, n, param_type), vector(bias, n, param_type), vector(scale, n, param_type),
+                             vector(next_weight, n, param_type)};
+  const Extent rx = matrix(dx, rows, n, ld_dx, type), rr = matrix(dresidual, rows, n, ld_dr, residual_type), rg = matrix(dgate, rows, n, ld_dg, type);
+  const Extent sums[] = {vector(dweight, n, param_type), vector(dbias, n, param_type), vector(dscale, n, param_type),
+                         vector(dnext_weight, n, param_type), vector(dnext_bias, n, param_type)};
+  if (meets(rx, operands) || meets(rr, operands) || meets(rg, operands) || meets(rx, sums) || meets(rr, sums) || meets(rg, sums) ||
+      meets(rx, {ed, rr, rg}) || meets(rg, {ed, rr}) || (!same(rr, ed) && overlap(rr, ed)))
+    return AMQ_ERR_INVALID;
+  for (int i = 0; i < 5; ++i) {
+    if (meets(sums[i], operands) || overlap(sums[i], ed)) return AMQ_ERR_INVALID;
+    for (int j = 0; j < i; ++j)
+      if (overlap(sums[i], sums[j])) return AMQ_ERR_INVALID;
+  }
+  if ((dweight || dbias || dscale || dnext_weight || dnext_bias) &&
+      !workspace_ok(workspace, workspace_bytes, amq_block_norm_backward_workspace_bytes(rows, n)))
+    return AMQ_ERR_INVALID;
+  return amq::status_of(amq::launch_block_norm_grad({dy, dnormed, x, y, gate, weight, bias, scale, next_weight, stats, dx, dresidual, dgate, dweight, dbias,
+                                                     dscale, dnext_weight, dnext_bias, static_cast<float*>(workspace), rows, ld_dy, ld_dn, ld_x, ld_y,
+                                                     ld_g, ld_dx, ld_dr, ld_dg, (int)n, type, residual_type, param_type, activation},
+                                                    static_cast<hipStream_t>(stream)));
+}
+
+size_t amq_clip_gradients_workspace_bytes(int64_t count) {
+  if (count < 0 || count > kMaxSize) return 0;
+  return amq::clip_workspace(count);
+}
+
+int amq_clip_gradients(int64_t count, const void* const* tensors, const int64_t* sizes, const int* types, float max_norm,
+                       void* const* out, float* norm, void* workspace, size_t workspace_bytes, void* stream) {
+  if (count < 0 || (count > 0 && (!tensors || !sizes || !types)) || !norm || !on_elements(norm, AMQ_F32) || (out && !(max_norm >= 0.0f)))
+    return AMQ_ERR_INVALID;
+  if (count > kMaxSize) return AMQ_ERR_UNSUPPORTED;
+  for (int64_t i = 0; i < count; ++i) {
+    if (sizes[i] < 0 || !type_ok(types[i])) return AMQ_ERR_INVALID;
+    if (sizes[i] == 0) continue;
+    if (!tensors[i] || !on_elements(tensors[i], types[i]) || (out && (!out[i] || !on_elements(out[i], types[i])))) return AMQ_ERR_INVALID;
+    if (sizes[i] > (1LL << 40)) return AMQ_ERR_UNSUPPORTED;
+  }
+  // results in the order of their addresses: none may meet the next one, the norm, or a tensor that is not its own
+  std::unique_ptr<Interval[]> results(new (std::nothrow) Interval[count + 1]);
+  if (!results) return amq::status_of(hipErrorOutOfMemory);
+  int64_t n = 0;
+  const uintptr_t at_norm = reinterpret_cast<uintptr_t>(norm);
+  results[n++] = {at_norm, at_norm + sizeof(float), -1};
+  for (int64_t i = 0; out && i < count; ++i)
+    if (sizes[i] > 0) {
+      const uintptr_t p = reinterpret_cast<uintptr_t>(out[i]);
+      results[n++] = {p, p + sizes[i] * size_of(types[i]), i};
+    }
+  std::sort(results.get(), results.get() + n, [](const Interval& a, const Interval& b) { return a.begin < b.begin; });
+  for (int64_t i = 1; i < n; ++i)
+    if (results[i].begin < results[i - 1].end) return AMQ_ERR_INVALID;
+  for (int64_t i = 0; i < count; ++i) {
+    if (sizes[i] == 0) continue;
+    const uintptr_t begin = reinterpret_cast<uintptr_t>(tensors[i]), end = begin + sizes[i] * size_of(types[i]);
+    const Interval* r = std::lower_bound(results.get(), results.get() + n, begin, [](const Interval& a, uintptr_t b) { return a.end <= b; });
+    if (r != results.get() + n && r->begin < end && !(r->index == i && r->begin == begin)) return AMQ_ERR_INVALID;
+  }
+  if (!workspace_ok(workspace, workspace_bytes, amq::clip_workspace(count))) return AMQ_ERR_INVALID;
+  return amq::status_of(amq::launch_clip_gradients({tensors, out, sizes, types, count}, max_norm, norm, workspace, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

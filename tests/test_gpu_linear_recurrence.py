@@ -112,6 +112,15 @@ def test_without_first_state_and_last_gradient(amq, mode, dtype):
         check_grad(amq, gate, x, None, mode, dh_last=False)
 
 
+@pytest.mark.parametrize("mode", MODES)
+def test_channels_enough_for_the_card(amq, mode):
+    """Tiles one after the other in one workgroup: more than 512 groups of 128 channels, which T > 128 else gives workgroups of their own."""
+    for T, B, n in ((137, 1, 66001), (260, 3, 22100)):
+        gate, x, h0 = case(T, T, B, n, torch.bfloat16, mode)
+        check(amq, gate, x, h0, mode)
+        check_grad(amq, gate, x, h0, mode)
+
+
 def layouts(gate, x):
     """The same tensors as columns of one projection, batch first, and as a slice of more steps, entries and channels at an odd offset."""
     T, B, n = x.shape

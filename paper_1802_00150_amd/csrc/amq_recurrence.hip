@@ -74,25 +74,6 @@ struct Step {
   }
 };
 
-// A workgroup's batch entry, the first of its channels, and the steps that count.
-struct Place {
-  int64_t b;
-  int c;
-  int64_t length;
-};
-template <int V, typename A>
-__device__ __forceinline__ Place place_of(const A& a, int64_t group) {
-  const int pieces = (a.n + 64 * V - 1) / (64 * V);
-  Place p;
-  p.b = group / pieces;
-  p.c = (int)(group - p.b * pieces) * 64 * V;
-  p.length = a.steps;
-  if (a.lengths) {
-    const int64_t l = a.lengths[p.b];
-    p.length = l < 0 ? 0 : l < a.steps ? l : a.steps;
-  }
-  return p;
-}
 // The V channels of a lane behind `row` (the same address in all lanes).  n is a multiple of V; lanes past the end read the last ones.
 template <int V>
 struct Lane {
@@ -154,44 +135,49 @@ __device__ __forceinline__ void mark_end(const Chain& c, int64_t tile) {
   arrived();
   if (lane_id() == 0) leave(c.marks + tile, 2u);
 }
-// One wave: the state that tile > 0 starts in.
+// The state that tile > 0 starts in, for one wave: it polls the marks, all waves of the workgroup bring the maps between to LDS, and it
+// folds them.  (One wave that read up to 63 maps by itself was most of the time of a long sequence.)
+constexpr int kWindow = 64;
 template <int V>
-__device__ __forceinline__ void look_back(const Chain& c, int64_t tile, float (&h)[V]) {
+__device__ __forceinline__ void look_back(const Chain& c, int64_t tile, uint64_t (*stage)[64 * V], int& found, int w, bool mine, float (&h)[V]) {
   const int l = lane_id();
-  int back = -1;  // the nearest tile whose end is known, and all between have left their maps
-  for (unsigned polls = 0; polls < kPollLimit; ++polls) {
-    const uint32_t mark = l < tile ? look(c.marks + tile - 1 - l) : 0u;
-    const unsigned long long ends = __ballot(mark == 2u), none = __ballot(mark == 0u);
-    if (ends) {
-      const int at = __ffsll(ends) - 1;
-      if ((none & ((1ull << at) - 1)) == 0) {
-        back = at;
-        break;
+  if (mine) {
+    int back = -1;  // the nearest tile whose end is known, and all between have left their maps
+    for (unsigned polls = 0; polls < kPollLimit; ++polls) {
+      const uint32_t mark = l < tile ? look(c.marks + tile - 1 - l) : 0u;
+      const unsigned long long ends = __ballot(mark == 2u), none = __ballot(mark == 0u);
+      if (ends) {
+        const int at = __ffsll(ends) - 1;
+        if ((none & ((1ull << at) - 1)) == 0) {
+          back = at;
+          break;
+        }
       }
+      __builtin_amdgcn_s_sleep(1);
     }
-    __builtin_amdgcn_s_sleep(1);
+    if (l == 0) found = back;
   }
-  back = __builtin_amdgcn_readfirstlane(back);
-  if (back < 0) {
+  lds_barrier();  // (and what the stage held has been read)
+  const int back = __builtin_amdgcn_readfirstlane(found);
+  if (mine)
 #pragma unroll
-    for (int j = 0; j < V; ++j) h[j] = __builtin_nanf("");
-    return;
+    for (int j = 0; j < V; ++j) h[j] = back < 0 ? __builtin_nanf("") : __uint_as_float(look(c.ends + ((tile - 1 - (back < 0 ? 0 : back)) * 64 + l) * V + j));
+#pragma unroll
+  for (int i = 0; i < kWindow / kTileWaves; ++i) {
+    const int u = w + i * kTileWaves;
+    if (u < back)
+#pragma unroll
+      for (int j = 0; j < V; ++j) stage[u][l * V + j] = look(c.maps + ((tile - back + u) * 64 + l) * V + j);
   }
+  lds_barrier();
+  if (mine)
+#pragma unroll 8
+    for (int u = 0; u < back; ++u)
 #pragma unroll
-  for (int j = 0; j < V; ++j) h[j] = __uint_as_float(look(c.ends + ((tile - 1 - back) * 64 + l) * V + j));
-  constexpr int kAtOnce = 8;
-  for (int64_t t = tile - back; t < tile; t += kAtOnce) {
-    uint64_t m[kAtOnce][V];
-#pragma unroll
-    for (int u = 0; u < kAtOnce; ++u)
-#pragma unroll
-      for (int j = 0; j < V; ++j) m[u][j] = look(c.maps + ((t + u < tile ? t + u : tile - 1) * 64 + l) * V + j);
-#pragma unroll
-    for (int u = 0; u < kAtOnce; ++u)
-      if (t + u < tile)
-#pragma unroll
-        for (int j = 0; j < V; ++j) h[j] = fmaf(__uint_as_float((uint32_t)m[u][j]), h[j], __uint_as_float((uint32_t)(m[u][j] >> 32)));
-  }
+      for (int j = 0; j < V; ++j) {
+        const uint64_t m = stage[u][l * V + j];
+        h[j] = fmaf(__uint_as_float((uint32_t)m), h[j], __uint_as_float((uint32_t)(m >> 32)));
+      }
 }
 // What a launch with workgroups of their own keeps in the workspace: the counter, then the marks (both cleared first), maps and ends.
 struct SplitLayout {
@@ -216,109 +202,82 @@ template <int V>
 __device__ __forceinline__ Chain chain_of(const Split& s, int64_t group) {
   return {s.marks + group * s.tiles, s.maps + group * s.tiles * 64 * V, s.ends + group * s.tiles * 64 * V};
 }
+// The number of a tile that nobody has begun, the same in all threads.
+__device__ __forceinline__ uint32_t take_tile(const Split& s, uint32_t& shared) {
+  if (threadIdx.x == 0) shared = __hip_atomic_fetch_add(s.counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __syncthreads();
+  return __builtin_amdgcn_readfirstlane(shared);
+}
 __global__ __launch_bounds__(256) void split_clear_kernel(uint32_t* p, int64_t words) {
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < words; i += (int64_t)gridDim.x * 256) p[i] = 0;
 }
 
 // ---- forward
 
-// A wave's steps: asked for, and turned into what they do.
-template <typename T, int V>
-struct Asked {
-  Elements<T, V> g[kSpan], x[kSpan];
+// Where a group of 64 V channels lies, and the steps of its batch entry that count.
+template <int V, typename A>
+struct Group {
+  int64_t b, length, state;  // batch entry; its steps; of the group's first channel in [B][n]
+  uint32_t c;                // first channel
+  Lane<V> ch;
+  __device__ __forceinline__ Group(const A& a, uint32_t group) : ch(0, V) {
+    const uint32_t pieces = ((uint32_t)a.n + 64 * V - 1) / (64 * V), entry = group / pieces;
+    b = entry;
+    c = (group - entry * pieces) * 64 * V;
+    state = b * a.n + c;
+    ch = Lane<V>((int)c, a.n);
+    length = a.steps;
+    if (a.lengths) {
+      const int64_t l = a.lengths[b];
+      length = l < 0 ? 0 : l < a.steps ? l : a.steps;
+    }
+  }
+  template <typename T>
+  __device__ __forceinline__ T* row(T* p, int64_t t, int64_t step, int64_t entry) const { return p + t * step + b * entry + c; }
 };
 
-template <typename T, int MODE, int V, bool SPLIT>
-__global__ __launch_bounds__(64 * kTileWaves) void recurrence_kernel(RecurrenceArgs a, Split split) {
-  __shared__ float maps[2][kTileWaves][2][64 * V];
-  __shared__ float begin[64 * V];
-  __shared__ uint32_t ticket;
-  const int w = __builtin_amdgcn_readfirstlane(wave_id()), waves = blockDim.x / 64, lane = lane_id();
-  int64_t group = blockIdx.x, tile = 0;
-  if constexpr (SPLIT) {
-    if (threadIdx.x == 0) ticket = __hip_atomic_fetch_add(split.counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    __syncthreads();
-    const uint32_t t = __builtin_amdgcn_readfirstlane(ticket);
-    tile = t / split.groups;
-    group = t - (uint32_t)tile * split.groups;
-  }
-  const Place at = place_of<V>(a, group);
-  const Lane<V> ch(at.c, a.n);
-  const T* pg = (const T*)a.gate + at.b * a.gate_batch + at.c;
-  const T* px = (const T*)a.x + at.b * a.x_batch + at.c;
-  T* py = (T*)a.hs + at.b * a.hs_batch + at.c;
-  const int64_t state = at.b * a.n + at.c;
-  auto first_state = [&](float (&h)[V]) __attribute__((always_inline)) {
-#pragma unroll
-    for (int j = 0; j < V; ++j) h[j] = 0.0f;
-    if (a.h0) {
-      const Elements<float, V> e = ch.get(a.h0 + state);
-#pragma unroll
-      for (int j = 0; j < V; ++j) h[j] = e.v[j];
-    }
-  };
-  Asked<T, V> in;
-  auto ask = [&](int64_t t0) __attribute__((always_inline)) {
+template <typename T, int V>
+struct Inputs {
+  Elements<T, V> g[kSpan], x[kSpan];
+  // asks for the steps from t0 on
+  template <typename A>
+  __device__ __forceinline__ void ask(const A& a, const Group<V, A>& at, int64_t t0) {
+    const T *pg = at.row((const T*)a.gate, t0, a.gate_step, a.gate_batch), *px = at.row((const T*)a.x, t0, a.x_step, a.x_batch);
     if (t0 + kSpan <= at.length) {
 #pragma unroll
-      for (int k = 0; k < kSpan; ++k) {
-        in.g[k] = ch.get(pg + (t0 + k) * a.gate_step);
-        in.x[k] = ch.get(px + (t0 + k) * a.x_step);
+      for (int k = 0; k < kSpan; ++k, pg += a.gate_step, px += a.x_step) {
+        g[k] = at.ch.get(pg);
+        x[k] = at.ch.get(px);
       }
     } else {
 #pragma unroll
-      for (int k = 0; k < kSpan; ++k)
+      for (int k = 0; k < kSpan; ++k, pg += a.gate_step, px += a.x_step)
         if (t0 + k < at.length) {
-          in.g[k] = ch.get(pg + (t0 + k) * a.gate_step);
-          in.x[k] = ch.get(px + (t0 + k) * a.x_step);
+          g[k] = at.ch.get(pg);
+          x[k] = at.ch.get(px);
         }
     }
-  };
+  }
+};
+template <typename T, int MODE, int V>
+struct Steps {
   Step<MODE> s[kSpan][V];
-  auto turn_into_steps = [&](int64_t t0) __attribute__((always_inline)) {
+  __device__ __forceinline__ void set(const Inputs<T, V>& in, int64_t t0, int64_t length) {
 #pragma unroll
     for (int k = 0; k < kSpan; ++k)
 #pragma unroll
       for (int j = 0; j < V; ++j) s[k][j].set((float)in.g[k].v[j], (float)in.x[k].v[j]);
-    if (t0 + kSpan > at.length)
+    if (t0 + kSpan > length)
 #pragma unroll
       for (int k = 0; k < kSpan; ++k)
-        if (t0 + k >= at.length)
+        if (t0 + k >= length)
 #pragma unroll
           for (int j = 0; j < V; ++j) s[k][j].hold();
-  };
-  // the wave's steps from the state in front of them
-  auto replay = [&](int64_t t0, float (&h)[V]) __attribute__((always_inline)) {
-    if (t0 >= a.steps) return;
-    const bool whole = t0 + kSpan <= at.length;
-    if (ch.any) {
+  }
+  // The map of all: A the product of what is kept, B continued from what it holds.
+  __device__ __forceinline__ void map(float (&A)[V], float (&B)[V]) const {
 #pragma unroll
-      for (int k = 0; k < kSpan; ++k) {
-#pragma unroll
-        for (int j = 0; j < V; ++j) h[j] = s[k][j].next(h[j]);
-        if (whole || t0 + k < a.steps) {
-          float out[V];
-#pragma unroll
-          for (int j = 0; j < V; ++j) out[j] = whole || t0 + k < at.length ? h[j] : 0.0f;
-          ch.put(py + (t0 + k) * a.hs_step, out);
-        }
-      }
-      if (a.h_last && t0 + kSpan >= a.steps) ch.put(a.h_last + state, h);
-      if (a.states && (t0 + kSpan) % kTile == 0 && t0 + kSpan < a.steps)
-        ch.put(a.states + ((t0 + kSpan) / kTile - 1) * (int64_t)a.batch * a.n + state, h);
-    }
-  };
-
-  if constexpr (SPLIT) {
-    const int64_t t0 = tile * kTile + w * kSpan;
-    ask(t0);
-    turn_into_steps(t0);
-    float A[V], B[V], h[V];
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-      A[j] = 1.0f;
-      B[j] = 0.0f;
-    }
+    for (int j = 0; j < V; ++j) A[j] = 1.0f;
 #pragma unroll
     for (int k = 0; k < kSpan; ++k)
 #pragma unroll
@@ -326,63 +285,64 @@ __global__ __launch_bounds__(64 * kTileWaves) void recurrence_kernel(RecurrenceA
         A[j] = s[k][j].keep(A[j]);
         B[j] = s[k][j].next(B[j]);
       }
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-      maps[0][w][0][lane * V + j] = A[j];
-      maps[0][w][1][lane * V + j] = B[j];
-    }
-    lds_barrier();
-    // the maps of the waves before it as one; wave 0 takes those of all
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-      A[j] = 1.0f;
-      B[j] = 0.0f;
-    }
-    const int before = w == 0 ? kTileWaves : w;
-#pragma unroll 4
-    for (int u = 0; u < before; ++u)
-#pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const float fa = maps[0][u][0][lane * V + j];
-        A[j] *= fa;
-        B[j] = fmaf(fa, B[j], maps[0][u][1][lane * V + j]);
-      }
-    if (w == 0) {
-      const Chain chain = chain_of<V>(split, group);
-      if (tile == 0) {
-        first_state(h);
-      } else {
-        leave_map(chain, tile, A, B);
-        look_back(chain, tile, h);
-      }
-      float end[V];
-#pragma unroll
-      for (int j = 0; j < V; ++j) {
-        begin[lane * V + j] = h[j];
-        end[j] = fmaf(A[j], h[j], B[j]);
-      }
-      leave_end(chain, tile, end);
-      lds_barrier();
-      mark_end(chain, tile);
-    } else {
-      lds_barrier();
-#pragma unroll
-      for (int j = 0; j < V; ++j) h[j] = fmaf(A[j], begin[lane * V + j], B[j]);
-    }
-    replay(t0, h);
-    return;
   }
+  // From the state in front of them to the one behind, with everything that is written on the way.
+  __device__ __forceinline__ void replay(const RecurrenceArgs& a, const Group<V, RecurrenceArgs>& at, int64_t t0, float (&h)[V]) const {
+    if (t0 >= a.steps || !at.ch.any) return;
+    T* py = at.row((T*)a.hs, t0, a.hs_step, a.hs_batch);
+    if (t0 + kSpan <= at.length) {
+#pragma unroll
+      for (int k = 0; k < kSpan; ++k, py += a.hs_step) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) h[j] = s[k][j].next(h[j]);
+        at.ch.put(py, h);
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < kSpan; ++k, py += a.hs_step) {
+        float out[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          h[j] = s[k][j].next(h[j]);
+          out[j] = t0 + k < at.length ? h[j] : 0.0f;
+        }
+        if (t0 + k < a.steps) at.ch.put(py, out);
+      }
+    }
+    const int64_t end = t0 + kSpan;
+    if (a.h_last && end >= a.steps) at.ch.put(a.h_last + at.state, h);
+    if (a.states && end % kTile == 0 && end < a.steps) at.ch.put(a.states + (end / kTile - 1) * (int64_t)a.batch * a.n + at.state, h);
+  }
+};
+template <int V, typename A>
+__device__ __forceinline__ void given(const float* p, const Group<V, A>& at, float (&h)[V]) {
+#pragma unroll
+  for (int j = 0; j < V; ++j) h[j] = 0.0f;
+  if (p) {
+    const Elements<float, V> e = at.ch.get(p + at.state);
+#pragma unroll
+    for (int j = 0; j < V; ++j) h[j] = e.v[j];
+  }
+}
 
+// A workgroup per group of channels, tile after tile.
+template <typename T, int MODE, int V>
+__global__ __launch_bounds__(64 * kTileWaves) void recurrence_kernel(RecurrenceArgs a) {
+  __shared__ float maps[2][kTileWaves][2][64 * V];
+  const int w = __builtin_amdgcn_readfirstlane(wave_id()), waves = blockDim.x / 64, lane = lane_id();
+  const Group<V, RecurrenceArgs> at(a, blockIdx.x);
+  Inputs<T, V> in;
+  Steps<T, MODE, V> steps;
   float carry[V];  // (wave 0 alone has it, and reads h0: h_last, written behind a barrier, may lie there)
 #pragma unroll
   for (int j = 0; j < V; ++j) carry[j] = 0.0f;
-  if (w == 0) first_state(carry);
+  if (w == 0) given<V>(a.h0, at, carry);
   int turn = 0;
-  ask(w * kSpan);
+  in.ask(a, at, w * kSpan);
   for (int64_t first = 0; first < a.steps; first += waves * kSpan, turn ^= 1) {
     const int64_t t0 = first + w * kSpan;
-    turn_into_steps(t0);
-    if (first + waves * kSpan < a.steps) ask(t0 + waves * kSpan);
+    steps.set(in, t0, at.length);
+    in.ask(a, at, t0 + waves * kSpan);
     float h[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) h[j] = carry[j];
@@ -390,29 +350,17 @@ __global__ __launch_bounds__(64 * kTileWaves) void recurrence_kernel(RecurrenceA
       // the wave's map; wave 0 knows the state it starts in, and leaves the one that it ends in
       float A[V], B[V];
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        A[j] = 1.0f;
-        B[j] = carry[j];
-      }
-#pragma unroll
-      for (int k = 0; k < kSpan; ++k)
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-          A[j] = s[k][j].keep(A[j]);
-          B[j] = s[k][j].next(B[j]);
-        }
+      for (int j = 0; j < V; ++j) B[j] = carry[j];
+      steps.map(A, B);
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         maps[turn][w][0][lane * V + j] = A[j];
         maps[turn][w][1][lane * V + j] = B[j];
       }
       lds_barrier();
-      if (w > 0)
-#pragma unroll
-        for (int j = 0; j < V; ++j) h[j] = maps[turn][0][1][lane * V + j];
       float f[V];
 #pragma unroll
-      for (int j = 0; j < V; ++j) f[j] = w == 0 ? B[j] : h[j];
+      for (int j = 0; j < V; ++j) f[j] = w == 0 ? B[j] : maps[turn][0][1][lane * V + j];
       const int before = w == 0 ? waves : w;
 #pragma unroll 4
       for (int u = 1; u < before; ++u)
@@ -424,190 +372,292 @@ __global__ __launch_bounds__(64 * kTileWaves) void recurrence_kernel(RecurrenceA
         else h[j] = f[j];
       }
     }
-    replay(t0, h);
+    steps.replay(a, at, t0, h);
     if (waves == 1)
 #pragma unroll
       for (int j = 0; j < V; ++j) carry[j] = h[j];
   }
 }
 
-// ---- backward
-
-template <typename T, int MODE, int V, bool SPLIT>
-__global__ __launch_bounds__(64 * kTileWaves) void recurrence_grad_kernel(RecurrenceGradArgs a, Split split) {
-  __shared__ float maps[2][kTileWaves][3][64 * V];
+// A workgroup per tile.
+template <typename T, int MODE, int V>
+__global__ __launch_bounds__(64 * kTileWaves, 8) void recurrence_tiles_kernel(RecurrenceArgs a, Split split) {
+  __shared__ uint64_t stage[kWindow][64 * V];
   __shared__ float begin[64 * V];
-  __shared__ uint32_t ticket;
-  const int w = __builtin_amdgcn_readfirstlane(wave_id()), waves = blockDim.x / 64, lane = lane_id();
-  const int64_t tiles = (a.steps + waves * kSpan - 1) / (waves * kSpan);  // (one tile, or tiles of kTile steps)
-  int64_t group = blockIdx.x, tile = tiles - 1;
-  if constexpr (SPLIT) {
-    if (threadIdx.x == 0) ticket = __hip_atomic_fetch_add(split.counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    __syncthreads();
-    const uint32_t t = __builtin_amdgcn_readfirstlane(ticket), order = t / split.groups;
-    tile = tiles - 1 - order;
-    group = t - order * split.groups;
+  __shared__ uint32_t number;
+  __shared__ int found;
+  auto maps = reinterpret_cast<float(*)[2][64 * V]>(stage);  // [kTileWaves]
+  const int w = __builtin_amdgcn_readfirstlane(wave_id()), lane = lane_id();
+  const uint32_t now = take_tile(split, number), tile = now / split.groups, group = now - tile * split.groups;
+  const Group<V, RecurrenceArgs> at(a, group);
+  const int64_t t0 = (int64_t)tile * kTile + w * kSpan;
+  Steps<T, MODE, V> steps;
+  {
+    Inputs<T, V> in;
+    in.ask(a, at, t0);
+    steps.set(in, t0, at.length);
   }
-  const Place at = place_of<V>(a, group);
-  const Lane<V> ch(at.c, a.n);
-  const T* pg = (const T*)a.gate + at.b * a.gate_batch + at.c;
-  const T* px = (const T*)a.x + at.b * a.x_batch + at.c;
-  const T* pd = (const T*)a.dhs + at.b * a.dhs_batch + at.c;
-  T* qg = (T*)a.dgate + at.b * a.dgate_batch + at.c;
-  T* qx = (T*)a.dx + at.b * a.dx_batch + at.c;
-  const int64_t state = at.b * a.n + at.c;
-  auto last_gradient = [&](float (&r)[V]) __attribute__((always_inline)) {
+  float A[V], B[V], h[V];
 #pragma unroll
-    for (int j = 0; j < V; ++j) r[j] = 0.0f;
-    if (a.dh_last) {
-      const Elements<float, V> e = ch.get(a.dh_last + state);
+  for (int j = 0; j < V; ++j) B[j] = 0.0f;
+  steps.map(A, B);
 #pragma unroll
-      for (int j = 0; j < V; ++j) r[j] = e.v[j];
-    }
-  };
-  float back[V];  // the gradient that reaches a tile's last state from the steps behind it
-  if constexpr (!SPLIT) last_gradient(back);
-  int turn = 0;
-  for (; tile >= 0; --tile, turn ^= 1) {
-    const int64_t t0 = tile * waves * kSpan + w * kSpan;
-    const bool whole = t0 + kSpan <= at.length;
-    Elements<T, V> g[kSpan], x[kSpan], d[kSpan];
-    float h[V], r[V];
-    const float* from = tile == 0 ? a.h0 : a.states + (tile - 1) * (int64_t)a.batch * a.n;
+  for (int j = 0; j < V; ++j) {
+    maps[w][0][lane * V + j] = A[j];
+    maps[w][1][lane * V + j] = B[j];
+  }
+  lds_barrier();
+  // the maps of the waves before it as one; wave 0 takes those of all
 #pragma unroll
-    for (int j = 0; j < V; ++j) h[j] = 0.0f;
-    auto ask = [&](int k) __attribute__((always_inline)) {
-      g[k] = ch.get(pg + (t0 + k) * a.gate_step);
-      x[k] = ch.get(px + (t0 + k) * a.x_step);
-      d[k] = ch.get(pd + (t0 + k) * a.dhs_step);
-    };
-    if (whole) {
-#pragma unroll
-      for (int k = 0; k < kSpan; ++k) ask(k);
-    } else {
-#pragma unroll
-      for (int k = 0; k < kSpan; ++k)
-        if (t0 + k < at.length) ask(k);
-    }
-    if (from) {
-      const Elements<float, V> e = ch.get(from + state);
-#pragma unroll
-      for (int j = 0; j < V; ++j) h[j] = e.v[j];
-    }
-    Step<MODE> s[kSpan][V];
-#pragma unroll
-    for (int k = 0; k < kSpan; ++k)
-#pragma unroll
-      for (int j = 0; j < V; ++j) s[k][j].set((float)g[k].v[j], (float)x[k].v[j]);
-    if (!whole)
-#pragma unroll
-      for (int k = 0; k < kSpan; ++k)
-        if (t0 + k >= at.length)
-#pragma unroll
-          for (int j = 0; j < V; ++j) {
-            s[k][j].hold();
-            d[k].v[j] = (T)0.0f;
-          }
-    // the wave's maps: of the state along time, and of the gradient against it (the same factor)
+  for (int j = 0; j < V; ++j) {
+    A[j] = 1.0f;
+    B[j] = 0.0f;
+  }
+  const int before = w == 0 ? kTileWaves : w;
+#pragma unroll 4
+  for (int u = 0; u < before; ++u)
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      float A = 1.0f, B = 0.0f, R = 0.0f;
+      const float fa = maps[u][0][lane * V + j];
+      A[j] *= fa;
+      B[j] = fmaf(fa, B[j], maps[u][1][lane * V + j]);
+    }
+  const Chain chain = chain_of<V>(split, group);
+  if (tile > 0) {
+    if (w == 0) leave_map(chain, tile, A, B);
+    look_back<V>(chain, tile, stage, found, w, w == 0, h);
+  } else if (w == 0) {
+    given<V>(a.h0, at, h);
+  }
+  if (w == 0) {
+    float end[V];
 #pragma unroll
-      for (int k = 0; k < kSpan; ++k) {
-        A = s[k][j].keep(A);
-        B = s[k][j].next(B);
-        R = s[kSpan - 1 - k][j].keep(R + (float)d[kSpan - 1 - k].v[j]);
+    for (int j = 0; j < V; ++j) {
+      begin[lane * V + j] = h[j];
+      end[j] = fmaf(A[j], h[j], B[j]);
+    }
+    leave_end(chain, tile, end);
+    lds_barrier();
+    mark_end(chain, tile);
+  } else {
+    lds_barrier();
+#pragma unroll
+    for (int j = 0; j < V; ++j) h[j] = fmaf(A[j], begin[lane * V + j], B[j]);
+  }
+  steps.replay(a, at, t0, h);
+}
+
+// ---- backward
+
+template <typename T, int V>
+struct GradInputs {
+  Inputs<T, V> in;
+  Elements<T, V> d[kSpan];
+  Elements<float, V> h;  // the state in front of the tile
+  bool some;             // (there is one)
+  __device__ __forceinline__ void ask(const RecurrenceGradArgs& a, const Group<V, RecurrenceGradArgs>& at, int64_t tile, int64_t t0) {
+    in.ask(a, at, t0);
+    const T* pd = at.row((const T*)a.dhs, t0, a.dhs_step, a.dhs_batch);
+    if (t0 + kSpan <= at.length) {
+#pragma unroll
+      for (int k = 0; k < kSpan; ++k, pd += a.dhs_step) d[k] = at.ch.get(pd);
+    } else {
+#pragma unroll
+      for (int k = 0; k < kSpan; ++k, pd += a.dhs_step)
+        if (t0 + k < at.length) d[k] = at.ch.get(pd);
+    }
+    const float* from = tile == 0 ? a.h0 : a.states + (tile - 1) * (int64_t)a.batch * a.n;
+    some = from != nullptr;
+    if (some) h = at.ch.get(from + at.state);
+  }
+  __device__ __forceinline__ void clear_behind(int64_t t0, int64_t length) {
+    if (t0 + kSpan > length)
+#pragma unroll
+      for (int k = 0; k < kSpan; ++k)
+        if (t0 + k >= length)
+#pragma unroll
+          for (int j = 0; j < V; ++j) d[k].v[j] = (T)0.0f;
+  }
+};
+// The map of a wave's gradient against time, from nothing behind it.
+template <typename T, int MODE, int V>
+__device__ __forceinline__ void map_back(const Steps<T, MODE, V>& steps, const Elements<T, V> (&d)[kSpan], float (&R)[V]) {
+#pragma unroll
+  for (int j = 0; j < V; ++j) R[j] = 0.0f;
+#pragma unroll
+  for (int k = kSpan - 1; k >= 0; --k)
+#pragma unroll
+    for (int j = 0; j < V; ++j) R[j] = steps.s[k][j].keep(R[j] + (float)d[k].v[j]);
+}
+// From the state h in front of a wave's steps and the gradient r that reaches the last of them from behind, to the one that leaves the first.
+template <typename T, int MODE, int V>
+__device__ __forceinline__ void replay_back(const RecurrenceGradArgs& a, const Group<V, RecurrenceGradArgs>& at, const Steps<T, MODE, V>& steps,
+                                            const GradInputs<T, V>& in, int64_t t0, float (&h)[V], float (&r)[V]) {
+  if (t0 >= a.steps || !at.ch.any) return;
+  T *qg = at.row((T*)a.dgate, t0, a.dgate_step, a.dgate_batch), *qx = at.row((T*)a.dx, t0, a.dx_step, a.dx_batch);
+  float before[kSpan][V];
+#pragma unroll
+  for (int k = 0; k < kSpan; ++k)
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      before[k][j] = h[j];
+      h[j] = steps.s[k][j].next(h[j]);
+    }
+  auto step = [&](int k, float (&og)[V], float (&ox)[V]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const float e = r[j] + (float)in.d[k].v[j];
+      og[j] = steps.s[k][j].dgate(e, before[k][j], (float)in.in.x[k].v[j]);
+      ox[j] = steps.s[k][j].dx(e);
+      r[j] = steps.s[k][j].keep(e);
+    }
+  };
+  if (t0 + kSpan <= at.length) {
+#pragma unroll
+    for (int k = kSpan - 1; k >= 0; --k) {
+      float og[V], ox[V];
+      step(k, og, ox);
+      at.ch.put(qg + k * a.dgate_step, og);
+      at.ch.put(qx + k * a.dx_step, ox);
+    }
+  } else {
+#pragma unroll
+    for (int k = kSpan - 1; k >= 0; --k) {
+      float og[V], ox[V];
+      step(k, og, ox);
+      if (t0 + k >= at.length)
+#pragma unroll
+        for (int j = 0; j < V; ++j) og[j] = ox[j] = 0.0f;
+      if (t0 + k < a.steps) {
+        at.ch.put(qg + k * a.dgate_step, og);
+        at.ch.put(qx + k * a.dx_step, ox);
       }
-      maps[turn][w][0][lane * V + j] = A;
-      maps[turn][w][1][lane * V + j] = B;
-      maps[turn][w][2][lane * V + j] = R;
+    }
+  }
+  if (t0 == 0 && a.dh0) at.ch.put(a.dh0 + at.state, r);
+}
+
+template <typename T, int MODE, int V>
+__global__ __launch_bounds__(64 * kTileWaves) void recurrence_grad_kernel(RecurrenceGradArgs a) {
+  __shared__ float maps[2][kTileWaves][3][64 * V];
+  const int w = __builtin_amdgcn_readfirstlane(wave_id()), waves = blockDim.x / 64, lane = lane_id();
+  const Group<V, RecurrenceGradArgs> at(a, blockIdx.x);
+  float back[V];  // the gradient that reaches a tile's last state from the steps behind it
+  given<V>(a.dh_last, at, back);
+  int turn = 0;
+  // (one tile, or tiles of kTile steps)
+  for (int64_t tile = (a.steps + waves * kSpan - 1) / (waves * kSpan) - 1; tile >= 0; --tile, turn ^= 1) {
+    const int64_t t0 = tile * waves * kSpan + w * kSpan;
+    GradInputs<T, V> in;
+    Steps<T, MODE, V> steps;
+    in.ask(a, at, tile, t0);
+    steps.set(in.in, t0, at.length);
+    in.clear_behind(t0, at.length);
+    // the wave's maps: of the state along time, and of the gradient against it (the same factor)
+    float A[V], B[V], R[V], h[V], r[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) B[j] = 0.0f;
+    steps.map(A, B);
+    map_back(steps, in.d, R);
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      maps[turn][w][0][lane * V + j] = A[j];
+      maps[turn][w][1][lane * V + j] = B[j];
+      maps[turn][w][2][lane * V + j] = R[j];
+      h[j] = in.some ? in.h.v[j] : 0.0f;
     }
     lds_barrier();
 #pragma unroll 4
     for (int u = 0; u < w; ++u)
 #pragma unroll
       for (int j = 0; j < V; ++j) h[j] = fmaf(maps[turn][u][0][lane * V + j], h[j], maps[turn][u][1][lane * V + j]);
-    if constexpr (SPLIT) {
-      // the maps of the waves behind it as one; the last wave takes those of all
-      float A[V], R[V];
-#pragma unroll
-      for (int j = 0; j < V; ++j) {
-        A[j] = 1.0f;
-        R[j] = 0.0f;
-      }
-      const int until = w == kTileWaves - 1 ? 0 : w + 1;
 #pragma unroll 4
-      for (int u = kTileWaves - 1; u >= until; --u)
+    for (int u = waves - 1; u > w; --u)
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-          const float fa = maps[turn][u][0][lane * V + j];
-          A[j] *= fa;
-          R[j] = fmaf(fa, R[j], maps[turn][u][2][lane * V + j]);
-        }
-      if (w == kTileWaves - 1) {
-        const Chain chain = chain_of<V>(split, group);
-        const int64_t order = tiles - 1 - tile;
-        if (order == 0) {
-          last_gradient(r);
-        } else {
-          leave_map(chain, order, A, R);
-          look_back(chain, order, r);
-        }
-        float end[V];
+      for (int j = 0; j < V; ++j) back[j] = fmaf(maps[turn][u][0][lane * V + j], back[j], maps[turn][u][2][lane * V + j]);
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-          begin[lane * V + j] = r[j];
-          end[j] = fmaf(A[j], r[j], R[j]);
-        }
-        leave_end(chain, order, end);
-        lds_barrier();
-        mark_end(chain, order);
-      } else {
-        lds_barrier();
-#pragma unroll
-        for (int j = 0; j < V; ++j) r[j] = fmaf(A[j], begin[lane * V + j], R[j]);
-      }
-    } else {
-#pragma unroll 4
-      for (int u = waves - 1; u > w; --u)
-#pragma unroll
-        for (int j = 0; j < V; ++j) back[j] = fmaf(maps[turn][u][0][lane * V + j], back[j], maps[turn][u][2][lane * V + j]);
-#pragma unroll
-      for (int j = 0; j < V; ++j) r[j] = back[j];
+    for (int j = 0; j < V; ++j) r[j] = back[j];
+    if (tile > 0)
 #pragma unroll 4
       for (int u = w; u >= 0; --u)
 #pragma unroll
         for (int j = 0; j < V; ++j) back[j] = fmaf(maps[turn][u][0][lane * V + j], back[j], maps[turn][u][2][lane * V + j]);
-    }
-    if (t0 < a.steps && ch.any) {
-      float before[kSpan][V];
-#pragma unroll
-      for (int k = 0; k < kSpan; ++k)
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-          before[k][j] = h[j];
-          h[j] = s[k][j].next(h[j]);
-        }
-#pragma unroll
-      for (int k = kSpan - 1; k >= 0; --k) {
-        float og[V], ox[V];
-        const bool here = whole || t0 + k < at.length;
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-          const float e = r[j] + (float)d[k].v[j];
-          og[j] = here ? s[k][j].dgate(e, before[k][j], (float)x[k].v[j]) : 0.0f;
-          ox[j] = here ? s[k][j].dx(e) : 0.0f;
-          r[j] = s[k][j].keep(e);
-        }
-        if (whole || t0 + k < a.steps) {
-          ch.put(qg + (t0 + k) * a.dgate_step, og);
-          ch.put(qx + (t0 + k) * a.dx_step, ox);
-        }
-      }
-      if (tile == 0 && w == 0 && a.dh0) ch.put(a.dh0 + state, r);
-    }
-    if constexpr (SPLIT) return;
+    replay_back(a, at, steps, in, t0, h, r);
   }
+}
+
+template <typename T, int MODE, int V>
+__global__ __launch_bounds__(64 * kTileWaves) void recurrence_grad_tiles_kernel(RecurrenceGradArgs a, Split split) {
+  __shared__ uint64_t stage[kWindow][64 * V];
+  __shared__ float begin[64 * V];
+  __shared__ uint32_t number;
+  __shared__ int found;
+  auto maps = reinterpret_cast<float(*)[3][64 * V]>(stage);  // [kTileWaves]
+  const int w = __builtin_amdgcn_readfirstlane(wave_id()), lane = lane_id();
+  const bool mine = w == kTileWaves - 1;
+  const uint32_t now = take_tile(split, number), order = now / split.groups, group = now - order * split.groups;
+  const int64_t tile = split.tiles - 1 - order, t0 = tile * kTile + w * kSpan;
+  const Group<V, RecurrenceGradArgs> at(a, group);
+  GradInputs<T, V> in;
+  in.ask(a, at, tile, t0);
+  Steps<T, MODE, V> steps;
+  steps.set(in.in, t0, at.length);
+  in.clear_behind(t0, at.length);
+  float A[V], B[V], R[V], h[V], r[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) B[j] = 0.0f;
+  steps.map(A, B);
+  map_back(steps, in.d, R);
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    maps[w][0][lane * V + j] = A[j];
+    maps[w][1][lane * V + j] = B[j];
+    maps[w][2][lane * V + j] = R[j];
+    h[j] = in.some ? in.h.v[j] : 0.0f;
+  }
+  lds_barrier();
+#pragma unroll 4
+  for (int u = 0; u < w; ++u)
+#pragma unroll
+    for (int j = 0; j < V; ++j) h[j] = fmaf(maps[u][0][lane * V + j], h[j], maps[u][1][lane * V + j]);
+  // the maps of the waves behind it as one; the last wave takes those of all
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    A[j] = 1.0f;
+    R[j] = 0.0f;
+  }
+  const int until = mine ? 0 : w + 1;
+#pragma unroll 4
+  for (int u = kTileWaves - 1; u >= until; --u)
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const float fa = maps[u][0][lane * V + j];
+      A[j] *= fa;
+      R[j] = fmaf(fa, R[j], maps[u][2][lane * V + j]);
+    }
+  const Chain chain = chain_of<V>(split, group);
+  if (order > 0) {
+    if (mine) leave_map(chain, order, A, R);
+    look_back<V>(chain, order, stage, found, w, mine, r);
+  } else if (mine) {
+    given<V>(a.dh_last, at, r);
+  }
+  if (mine) {
+    float end[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      begin[lane * V + j] = r[j];
+      end[j] = fmaf(A[j], r[j], R[j]);
+    }
+    leave_end(chain, order, end);
+    lds_barrier();
+    mark_end(chain, order);
+  } else {
+    lds_barrier();
+#pragma unroll
+    for (int j = 0; j < V; ++j) r[j] = fmaf(A[j], begin[lane * V + j], R[j]);
+  }
+  replay_back(a, at, steps, in, t0, h, r);
 }
 
 // ---- launches
@@ -625,9 +675,10 @@ hipError_t with_type(int type, int mode, int n, F f) {
   return n % 2 == 0 ? modes(f16(), two) : modes(f16(), one);
 }
 
-int waves_of(int64_t steps) {
-  const int64_t w = (steps + kSpan - 1) / kSpan;
-  return (int)(w < kTileWaves ? w : kTileWaves);
+// Waves of a tile: 16 where a tile begins where a state was left or has a workgroup of its own, else as many as share the steps evenly.
+int waves_of(int64_t steps, bool even) {
+  const int64_t spans = (steps + kSpan - 1) / kSpan, tiles = (spans + kTileWaves - 1) / kTileWaves;
+  return (int)(tiles == 1 ? spans : even ? (spans + tiles - 1) / tiles : kTileWaves);
 }
 int64_t groups_of(int64_t batch, int64_t n, int V) { return batch * ((n + 64 * V - 1) / (64 * V)); }
 // Workgroups of their own for tiles: where the channels alone leave compute units without one.
@@ -644,19 +695,18 @@ hipError_t split_of(int64_t groups, int64_t steps, int channels, void* ws, hipSt
   split_clear_kernel<<<dim3((unsigned)(words / 1024 < 256 ? words / 1024 + 1 : 256)), dim3(256), 0, s>>>(out.counter, words);
   return hipGetLastError();
 }
-template <typename A, typename F>
-hipError_t launch(const A& a, hipStream_t s, F kernel) {
+template <typename A, typename F, typename G>
+hipError_t launch(const A& a, bool even, hipStream_t s, F kernel, G tiles_kernel) {
   return with_type(a.type, a.mode, a.n, [&](auto t, auto v, auto m) {
     constexpr int V = decltype(v)::value;
     const int64_t groups = groups_of(a.batch, a.n, V);
-    const int waves = waves_of(a.steps);
     if (splits(groups, a.steps)) {
       Split split;
       const hipError_t e = split_of(groups, a.steps, 64 * V, a.ws, s, split);
       if (e != hipSuccess) return e;
-      kernel(t, v, m, std::true_type())<<<dim3((unsigned)(groups * split.tiles)), dim3(64 * waves), 0, s>>>(a, split);
+      tiles_kernel(t, v, m)<<<dim3((unsigned)(groups * split.tiles)), dim3(64 * kTileWaves), 0, s>>>(a, split);
     } else {
-      kernel(t, v, m, std::false_type())<<<dim3((unsigned)groups), dim3(64 * waves), 0, s>>>(a, Split());
+      kernel(t, v, m)<<<dim3((unsigned)groups), dim3(64 * waves_of(a.steps, even)), 0, s>>>(a);
     }
     return hipGetLastError();
   });
@@ -680,15 +730,13 @@ size_t recurrence_workspace(int64_t steps, int64_t batch, int64_t n, int) { retu
 size_t recurrence_grad_workspace(int64_t steps, int64_t batch, int64_t n, int) { return workspace(steps, batch, n); }
 
 hipError_t launch_recurrence(const RecurrenceArgs& a, hipStream_t s) {
-  return launch(a, s, [](auto t, auto v, auto m, auto split) {
-    return recurrence_kernel<decltype(t), decltype(m)::value, decltype(v)::value, decltype(split)::value>;
-  });
+  return launch(a, true, s, [](auto t, auto v, auto m) { return recurrence_kernel<decltype(t), decltype(m)::value, decltype(v)::value>; },
+                [](auto t, auto v, auto m) { return recurrence_tiles_kernel<decltype(t), decltype(m)::value, decltype(v)::value>; });
 }
 
 hipError_t launch_recurrence_grad(const RecurrenceGradArgs& a, hipStream_t s) {
-  return launch(a, s, [](auto t, auto v, auto m, auto split) {
-    return recurrence_grad_kernel<decltype(t), decltype(m)::value, decltype(v)::value, decltype(split)::value>;
-  });
+  return launch(a, false, s, [](auto t, auto v, auto m) { return recurrence_grad_kernel<decltype(t), decltype(m)::value, decltype(v)::value>; },
+                [](auto t, auto v, auto m) { return recurrence_grad_tiles_kernel<decltype(t), decltype(m)::value, decltype(v)::value>; });
 }
 
 }  // namespace amq

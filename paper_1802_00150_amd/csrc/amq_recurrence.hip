@@ -325,10 +325,10 @@ __device__ __forceinline__ void given(const float* p, const Group<V, A>& at, flo
   }
 }
 
-// A workgroup per group of channels, tile after tile.
-template <typename T, int MODE, int V>
+// A workgroup per group of channels, tile after tile; ONE: there is one.
+template <typename T, int MODE, int V, bool ONE>
 __global__ __launch_bounds__(64 * kTileWaves) void recurrence_kernel(RecurrenceArgs a) {
-  __shared__ float maps[2][kTileWaves][2][64 * V];
+  __shared__ float maps[ONE ? 1 : 2][kTileWaves][2][64 * V];
   const int w = __builtin_amdgcn_readfirstlane(wave_id()), waves = blockDim.x / 64, lane = lane_id();
   const Group<V, RecurrenceArgs> at(a, blockIdx.x);
   Inputs<T, V> in;
@@ -342,7 +342,7 @@ __global__ __launch_bounds__(64 * kTileWaves) void recurrence_kernel(RecurrenceA
   for (int64_t first = 0; first < a.steps; first += waves * kSpan, turn ^= 1) {
     const int64_t t0 = first + w * kSpan;
     steps.set(in, t0, at.length);
-    in.ask(a, at, t0 + waves * kSpan);
+    if constexpr (!ONE) in.ask(a, at, t0 + waves * kSpan);
     float h[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) h[j] = carry[j];
@@ -361,7 +361,7 @@ __global__ __launch_bounds__(64 * kTileWaves) void recurrence_kernel(RecurrenceA
       float f[V];
 #pragma unroll
       for (int j = 0; j < V; ++j) f[j] = w == 0 ? B[j] : maps[turn][0][1][lane * V + j];
-      const int before = w == 0 ? waves : w;
+      const int before = w > 0 ? w : ONE ? 0 : waves;
 #pragma unroll 4
       for (int u = 1; u < before; ++u)
 #pragma unroll
@@ -373,9 +373,7 @@ __global__ __launch_bounds__(64 * kTileWaves) void recurrence_kernel(RecurrenceA
       }
     }
     steps.replay(a, at, t0, h);
-    if (waves == 1)
-#pragma unroll
-      for (int j = 0; j < V; ++j) carry[j] = h[j];
+    if constexpr (ONE) return;
   }
 }
 
@@ -537,17 +535,16 @@ __device__ __forceinline__ void replay_back(const RecurrenceGradArgs& a, const G
   if (t0 == 0 && a.dh0) at.ch.put(a.dh0 + at.state, r);
 }
 
-template <typename T, int MODE, int V>
+template <typename T, int MODE, int V, bool ONE>
 __global__ __launch_bounds__(64 * kTileWaves) void recurrence_grad_kernel(RecurrenceGradArgs a) {
-  __shared__ float maps[2][kTileWaves][3][64 * V];
+  __shared__ float maps[ONE ? 1 : 2][kTileWaves][3][64 * V];
   const int w = __builtin_amdgcn_readfirstlane(wave_id()), waves = blockDim.x / 64, lane = lane_id();
   const Group<V, RecurrenceGradArgs> at(a, blockIdx.x);
   float back[V];  // the gradient that reaches a tile's last state from the steps behind it
   given<V>(a.dh_last, at, back);
   int turn = 0;
-  // (one tile, or tiles of kTile steps)
-  for (int64_t tile = (a.steps + waves * kSpan - 1) / (waves * kSpan) - 1; tile >= 0; --tile, turn ^= 1) {
-    const int64_t t0 = tile * waves * kSpan + w * kSpan;
+  for (int64_t tile = ONE ? 0 : (a.steps - 1) / kTile; tile >= 0; --tile, turn ^= 1) {
+    const int64_t t0 = tile * kTile + w * kSpan;
     GradInputs<T, V> in;
     Steps<T, MODE, V> steps;
     in.ask(a, at, tile, t0);
@@ -583,6 +580,7 @@ __global__ __launch_bounds__(64 * kTileWaves) void recurrence_grad_kernel(Recurr
 #pragma unroll
         for (int j = 0; j < V; ++j) back[j] = fmaf(maps[turn][u][0][lane * V + j], back[j], maps[turn][u][2][lane * V + j]);
     replay_back(a, at, steps, in, t0, h, r);
+    if constexpr (ONE) return;
   }
 }
 
@@ -663,30 +661,37 @@ __global__ __launch_bounds__(64 * kTileWaves) void recurrence_grad_tiles_kernel(
 // ---- launches
 
 template <typename F>
-hipError_t with_type(int type, int mode, int n, F f) {
-  auto modes = [&](auto t, auto v) {
-    return mode == AMQ_RECURRENCE_BLEND ? f(t, v, std::integral_constant<int, AMQ_RECURRENCE_BLEND>())
-                                        : f(t, v, std::integral_constant<int, AMQ_RECURRENCE_DECAY>());
+hipError_t with_type(int type, int mode, F f) {
+  auto modes = [&](auto t) {
+    return mode == AMQ_RECURRENCE_BLEND ? f(t, std::integral_constant<int, AMQ_RECURRENCE_BLEND>())
+                                        : f(t, std::integral_constant<int, AMQ_RECURRENCE_DECAY>());
   };
-  const std::integral_constant<int, 1> one;
-  const std::integral_constant<int, 2> two;
-  if (type == AMQ_F32) return modes(float(), one);
-  if (type == AMQ_BF16) return n % 2 == 0 ? modes(bf16(), two) : modes(bf16(), one);
-  return n % 2 == 0 ? modes(f16(), two) : modes(f16(), one);
+  return type == AMQ_F32 ? modes(float()) : type == AMQ_BF16 ? modes(bf16()) : modes(f16());
 }
 
-// Waves of a tile: 16 where a tile begins where a state was left or has a workgroup of its own, else as many as share the steps evenly.
+// Waves of a tile: 16 where a tile begins where a state was left, else as many as share the steps evenly.
 int waves_of(int64_t steps, bool even) {
   const int64_t spans = (steps + kSpan - 1) / kSpan, tiles = (spans + kTileWaves - 1) / kTileWaves;
   return (int)(tiles == 1 ? spans : even ? (spans + tiles - 1) / tiles : kTileWaves);
 }
 int64_t groups_of(int64_t batch, int64_t n, int V) { return batch * ((n + 64 * V - 1) / (64 * V)); }
-// Workgroups of their own for tiles: where the channels alone leave compute units without one.
-constexpr int64_t kMostSplit = 512;
-bool splits(int64_t groups, int64_t steps) { return steps > kTile && groups <= kMostSplit; }
+int64_t tiles_of(int64_t steps) { return (steps + kTile - 1) / kTile; }
+
+// The form with the least time, by measurement (us; g groups of 64 channels, t tiles).  One workgroup per group takes 3 + c t while the card
+// holds all groups at once; a workgroup per tile 9 + e t g / 256, of which 4 are the clearing of the marks.  c and e: 16-bit types
+// 2.5 and 2.9 (2000 x 8192 entries 48 and 31, 2000 x 16384 48 and 50, 300 x 8192 10.5 and 13.0), backward 4.3 and 6.1 (16.4 million entries: 2000 x 8192 71
+// and 55, 1000 x 16384 43 and 54, 300 x 8192 14.6 and 16.6); float 2.7 and 4.8 (2000 x 8192 46 and 46), backward 4.5 and 9.
+bool splits(int64_t batch, int64_t n, int64_t steps, bool wide, bool backward) {
+  const int64_t g = groups_of(batch, n, 1), t = tiles_of(steps);
+  const double c = wide ? backward ? 4.5 : 2.7 : backward ? 4.3 : 2.5, e = wide ? backward ? 9.0 : 4.8 : backward ? 6.1 : 2.9;
+  return t > 1 && g < 256 && (double)t * (c - e * (double)g / 256) > 6.0;
+}
+// Channels of a lane: two of 16 bits where a tile has its own workgroup, and forward where groups of 128 channels still fill the card
+// (1000 x 32768 entries 41 us, with one 50; 2000 x 16384 65 and 48); one otherwise (35 x 262144 backward 21.2, with two 23.8).
+bool two_channels(int64_t batch, int64_t n) { return n % 2 == 0 && groups_of(batch, n, 2) >= 256; }
 
 hipError_t split_of(int64_t groups, int64_t steps, int channels, void* ws, hipStream_t s, Split& out) {
-  const int64_t tiles = (steps + kTile - 1) / kTile;
+  const int64_t tiles = tiles_of(steps);
   const SplitLayout l(groups, tiles, channels);
   char* p = static_cast<char*>(ws);
   out = {reinterpret_cast<uint32_t*>(p), reinterpret_cast<uint32_t*>(p + l.marks), reinterpret_cast<uint64_t*>(p + l.maps),
@@ -695,48 +700,68 @@ hipError_t split_of(int64_t groups, int64_t steps, int channels, void* ws, hipSt
   split_clear_kernel<<<dim3((unsigned)(words / 1024 < 256 ? words / 1024 + 1 : 256)), dim3(256), 0, s>>>(out.counter, words);
   return hipGetLastError();
 }
-template <typename A, typename F, typename G>
-hipError_t launch(const A& a, bool even, hipStream_t s, F kernel, G tiles_kernel) {
-  return with_type(a.type, a.mode, a.n, [&](auto t, auto v, auto m) {
-    constexpr int V = decltype(v)::value;
-    const int64_t groups = groups_of(a.batch, a.n, V);
-    if (splits(groups, a.steps)) {
-      Split split;
-      const hipError_t e = split_of(groups, a.steps, 64 * V, a.ws, s, split);
-      if (e != hipSuccess) return e;
-      tiles_kernel(t, v, m)<<<dim3((unsigned)(groups * split.tiles)), dim3(64 * kTileWaves), 0, s>>>(a, split);
-    } else {
-      kernel(t, v, m)<<<dim3((unsigned)groups), dim3(64 * waves_of(a.steps, even)), 0, s>>>(a);
-    }
-    return hipGetLastError();
-  });
+template <typename A, typename F>
+hipError_t launch_tiles(const A& a, int channels, hipStream_t s, F kernel) {
+  const int64_t groups = groups_of(a.batch, a.n, channels);
+  Split split;
+  const hipError_t e = split_of(groups, a.steps, 64 * channels, a.ws, s, split);
+  if (e != hipSuccess) return e;
+  kernel<<<dim3((unsigned)(groups * split.tiles)), dim3(64 * kTileWaves), 0, s>>>(a, split);
+  return hipGetLastError();
+}
+template <typename A, typename F>
+hipError_t launch_groups(const A& a, int channels, bool even, hipStream_t s, F kernel) {
+  kernel<<<dim3((unsigned)groups_of(a.batch, a.n, channels)), dim3(64 * waves_of(a.steps, even)), 0, s>>>(a);
+  return hipGetLastError();
 }
 // (batch entries may count as channels of one entry in the launch, so the larger need of either)
-size_t workspace(int64_t steps, int64_t batch, int64_t n) {
+size_t workspace(int64_t steps, int64_t batch, int64_t n, int type, bool backward) {
   size_t most = 0;
-  for (int V : {1, 2})
-    for (int flat = 0; flat < 2; ++flat) {
-      const int64_t groups = flat ? groups_of(1, batch * n, V) : groups_of(batch, n, V);
-      if (!splits(groups, steps)) continue;
-      const size_t need = SplitLayout(groups, (steps + kTile - 1) / kTile, 64 * V).bytes;
-      most = need > most ? need : most;
-    }
+  for (int flat = 0; flat < 2; ++flat) {
+    const int64_t b = flat ? 1 : batch, c = flat ? batch * n : n;
+    if (!splits(b, c, steps, type == AMQ_F32, backward)) continue;
+    const int V = type != AMQ_F32 && c % 2 == 0 ? 2 : 1;
+    const size_t need = SplitLayout(groups_of(b, c, V), tiles_of(steps), 64 * V).bytes;
+    most = need > most ? need : most;
+  }
   return most;
 }
 
 }  // namespace
 
-size_t recurrence_workspace(int64_t steps, int64_t batch, int64_t n, int) { return workspace(steps, batch, n); }
-size_t recurrence_grad_workspace(int64_t steps, int64_t batch, int64_t n, int) { return workspace(steps, batch, n); }
+size_t recurrence_workspace(int64_t steps, int64_t batch, int64_t n, int type) { return workspace(steps, batch, n, type, false); }
+size_t recurrence_grad_workspace(int64_t steps, int64_t batch, int64_t n, int type) { return workspace(steps, batch, n, type, true); }
 
 hipError_t launch_recurrence(const RecurrenceArgs& a, hipStream_t s) {
-  return launch(a, true, s, [](auto t, auto v, auto m) { return recurrence_kernel<decltype(t), decltype(m)::value, decltype(v)::value>; },
-                [](auto t, auto v, auto m) { return recurrence_tiles_kernel<decltype(t), decltype(m)::value, decltype(v)::value>; });
+  return with_type(a.type, a.mode, [&](auto t, auto m) {
+    using T = decltype(t);
+    constexpr int M = decltype(m)::value;
+    constexpr bool wide = sizeof(T) == 4;
+    if (splits(a.batch, a.n, a.steps, wide, false)) {
+      if constexpr (!wide)
+        if (a.n % 2 == 0) return launch_tiles(a, 2, s, recurrence_tiles_kernel<T, M, 2>);
+      return launch_tiles(a, 1, s, recurrence_tiles_kernel<T, M, 1>);
+    }
+    if (a.steps <= kTile) return launch_groups(a, 1, true, s, recurrence_kernel<T, M, 1, true>);
+    if constexpr (!wide)
+      if (two_channels(a.batch, a.n)) return launch_groups(a, 2, true, s, recurrence_kernel<T, M, 2, false>);
+    return launch_groups(a, 1, true, s, recurrence_kernel<T, M, 1, false>);
+  });
 }
 
 hipError_t launch_recurrence_grad(const RecurrenceGradArgs& a, hipStream_t s) {
-  return launch(a, false, s, [](auto t, auto v, auto m) { return recurrence_grad_kernel<decltype(t), decltype(m)::value, decltype(v)::value>; },
-                [](auto t, auto v, auto m) { return recurrence_grad_tiles_kernel<decltype(t), decltype(m)::value, decltype(v)::value>; });
+  return with_type(a.type, a.mode, [&](auto t, auto m) {
+    using T = decltype(t);
+    constexpr int M = decltype(m)::value;
+    constexpr bool wide = sizeof(T) == 4;
+    if (splits(a.batch, a.n, a.steps, wide, true)) {
+      if constexpr (!wide)
+        if (a.n % 2 == 0) return launch_tiles(a, 2, s, recurrence_grad_tiles_kernel<T, M, 2>);
+      return launch_tiles(a, 1, s, recurrence_grad_tiles_kernel<T, M, 1>);
+    }
+    if (a.steps <= kTile) return launch_groups(a, 1, false, s, recurrence_grad_kernel<T, M, 1, true>);
+    return launch_groups(a, 1, false, s, recurrence_grad_kernel<T, M, 1, false>);
+  });
 }
 
 }  // namespace amq

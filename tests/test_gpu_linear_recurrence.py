@@ -10,7 +10,7 @@ pytestmark = pytest.mark.gpu
 MODES = ["blend", "decay"]
 # steps, batch, channels: one of each, part of a wave's 8 steps, a tile's 128, the states' positions, many tiles; pieces that end inside a row
 SIZES = [(1, 1, 1), (1, 3, 5), (1, 2, 1024), (7, 2, 64), (8, 1, 65), (9, 2, 127), (35, 4, 33), (64, 1, 300), (127, 1, 130), (128, 2, 64), (129, 2, 66),
-         (130, 1, 1), (257, 1, 3), (700, 2, 70), (1000, 3, 129), (2500, 1, 40)]
+         (130, 1, 1), (257, 1, 3), (700, 2, 70), (1000, 3, 129), (2500, 1, 40), (9000, 1, 2)]
 
 
 @pytest.fixture(scope="module")
@@ -114,9 +114,9 @@ def test_without_first_state_and_last_gradient(amq, mode, dtype):
 
 @pytest.mark.parametrize("mode", MODES)
 def test_channels_enough_for_the_card(amq, mode):
-    """Tiles one after the other in one workgroup: more than 512 groups of 128 channels, which T > 128 else gives workgroups of their own."""
-    for T, B, n in ((137, 1, 66001), (260, 3, 22100)):
-        gate, x, h0 = case(T, T, B, n, torch.bfloat16, mode)
+    """Tiles one after the other in one workgroup, with one channel and with two in a lane."""
+    for T, B, n, dtype in ((137, 1, 40001, torch.bfloat16), (260, 3, 22100, torch.bfloat16), (400, 1, 17001, torch.float32), (300, 1, 8192, torch.float16)):
+        gate, x, h0 = case(T, T, B, n, dtype, mode)
         check(amq, gate, x, h0, mode)
         check_grad(amq, gate, x, h0, mode)
 

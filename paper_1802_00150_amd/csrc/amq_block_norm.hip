@@ -54,14 +54,31 @@ __device__ __forceinline__ float row_sum(float a, float (*slots)[2], int& turn) 
   return a;
 }
 
-// Piece j of a row's pieces of V entries for thread `tid` of W waves.  The last one ends with the row and overlaps the one before
+// The same over `waves` waves, up to 16, beginning with wave `first`: a lane reads one wave's sums each.
+__device__ __forceinline__ void row_sum2(float& a, float& b, float (*slots)[2], int& turn, int first, int waves) {
+  a = sum64(a);
+  b = sum64(b);
+  if (waves == 1) return;
+  float(*s)[2] = slots + turn * 16;
+  turn ^= 1;
+  if (lane_id() == 0) {
+    s[wave_id()][0] = a;
+    s[wave_id()][1] = b;
+  }
+  lds_barrier();
+  const int l = lane_id() & 15;
+  a = group_sum(l < waves ? s[first + l][0] : 0.0f, 4);
+  b = group_sum(l < waves ? s[first + l][1] : 0.0f, 4);
+}
+
+// Piece j of a row's pieces of V entries for thread `tid` of `threads`.  The last one ends with the row and overlaps the one before
 // it (its first `repeated` entries count there); threads past the end hold it once more with nothing that counts, and store
 // nothing.  (n >= V.)
-template <int W, int V>
+template <int V>
 struct Piece {
   int start, repeated;
-  __device__ __forceinline__ Piece(int j, int tid, int n) {
-    const int c = (j * W * 64 + tid) * V;
+  __device__ __forceinline__ Piece(int j, int tid, int n, int threads) {
+    const int c = (j * threads + tid) * V;
     start = c < n - V ? c : n - V;
     repeated = c - start < V ? c - start : V;
   }
@@ -81,21 +98,37 @@ struct Piece {
   }
 };
 
-// act(z) and its slope.
-__device__ __forceinline__ void gate_of(int act, float z, float& value, float& slope) {
+// act(z) and its slope for V entries.
+template <typename T, int V>
+__device__ __forceinline__ void gates_of(int act, const Elements<T, V>& z, float (&value)[V], float (&slope)[V]) {
   if (act == AMQ_ACT_NONE) {
-    value = z;
-    slope = 1.0f;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      value[i] = (float)z.v[i];
+      slope[i] = 1.0f;
+    }
     return;
   }
-  const float e = __expf(-fabsf(z)), r = __builtin_amdgcn_rcpf(1.0f + e), small = e * r;
-  const float p = z >= 0.0f ? r : small, q = z >= 0.0f ? small : r;  // sigmoid(z), 1 - sigmoid(z)
+  float p[V], q[V];  // sigmoid(z), 1 - sigmoid(z)
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const float v = (float)z.v[i], e = __expf(-fabsf(v)), r = __builtin_amdgcn_rcpf(1.0f + e), small = e * r;
+    p[i] = v >= 0.0f ? r : small;
+    q[i] = v >= 0.0f ? small : r;
+  }
   if (act == AMQ_ACT_SIGMOID) {
-    value = p;
-    slope = p * q;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      value[i] = p[i];
+      slope[i] = p[i] * q[i];
+    }
   } else {
-    value = z * p;
-    slope = p * fmaf(z, q, 1.0f);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const float v = (float)z.v[i];
+      value[i] = v * p[i];
+      slope[i] = p[i] * fmaf(v, q[i], 1.0f);
+    }
   }
 }
 
@@ -115,7 +148,7 @@ __global__ __launch_bounds__(W > 4 ? W * 64 : 256) void block_norm_kernel(BlockN
   __shared__ float slots[2 * W * kRows][2];
   int turn = 0;
   const int group = wave_id() / W, tid = (int)threadIdx.x - group * W * 64;
-  auto piece = [&](int j) __attribute__((always_inline)) { return Piece<W, V>(j, tid, a.n); };
+  auto piece = [&](int j) __attribute__((always_inline)) { return Piece<V>(j, tid, a.n, W * 64); };
   // the scale is folded into the first norm's parameters
   float w[NV][V], b[NV][V], w2[NV][V], b2[NV][V];
 #pragma unroll
@@ -149,18 +182,19 @@ __global__ __launch_bounds__(W > 4 ? W * 64 : 256) void block_norm_kernel(BlockN
     const bool here = row < a.rows;
     float x[NV][V], y[NV][V], act[NV][V], s = 0.0f;
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
+    for (int j = 0; j < NV; ++j) {
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         x[j][i] = here ? (float)rx[j].v[i] : 0.0f;
         y[j][i] = here ? (float)rr[j].v[i] : 0.0f;
         act[j][i] = 1.0f;
-        if (a.gate) {
-          float slope;
-          gate_of(a.act, here ? (float)rg[j].v[i] : 0.0f, act[j][i], slope);
-        }
         s += piece(j).counts(i) ? x[j][i] : 0.0f;
       }
+      if (a.gate && here) {
+        float slope[V];
+        gates_of(a.act, rg[j], act[j], slope);
+      }
+    }
     fetch_row(row + step);
     const float mean = row_sum<W>(s, slots, turn) * inv_n;
     s = 0.0f;
@@ -213,102 +247,140 @@ __global__ __launch_bounds__(W > 4 ? W * 64 : 256) void block_norm_kernel(BlockN
   }
 }
 
-template <typename T, typename R, typename P, int V, int W, int NV>
-__global__ __launch_bounds__(row_groups(W, 8) * W * 64) void block_norm_grad_kernel(BlockNormGradArgs a) {
-  constexpr int kRows = row_groups(W, 8), kThreads = W * 64, kEntries = kThreads * NV * V;
-  __shared__ float slots[2 * W * kRows][2];
+// `waves` waves per row, as many rows in a workgroup as 16 waves have room for.
+template <typename T, typename R, typename P, int V, int NV>
+__global__ __launch_bounds__(1024) void block_norm_grad_kernel(BlockNormGradArgs a, int waves) {
+  __shared__ float slots[2 * 16][2];
   // [group][sum][j][i][thread]: consecutive lanes on consecutive banks
-  __shared__ float shared_sums[kRows > 1 ? kRows * 2 * kEntries : 1];
+  __shared__ float shared_sums[2 * 1024 * NV * V];
   int turn = 0;
-  const int group = wave_id() / W, tid = (int)threadIdx.x - group * kThreads;
-  auto piece = [&](int j) __attribute__((always_inline)) { return Piece<W, V>(j, tid, a.n); };
-  // sums[0..3]: G act z, G act, dnormed zy, dnormed
-  float w[NV][V], b[NV][V], sc[NV][V], w2[NV][V], sums[4][NV][V];
-#pragma unroll
-  for (int j = 0; j < NV; ++j) {
+  const int threads = waves * 64, groups = blockDim.x / threads, entries = threads * NV * V;
+  const int group = __builtin_amdgcn_readfirstlane(wave_id() / waves), tid = (int)threadIdx.x - group * threads;
+  auto piece = [&](int j) __attribute__((always_inline)) { return Piece<V>(j, tid, a.n, threads); };
+  // With one piece a lane has room for the parameters and asks for a row ahead; with more it reads the parameters again for every row (from
+  // L2: 16 bytes an entry, where spilled registers would be 38).
+  constexpr bool kRoom = NV == 1;
+  float w[NV][V], b[NV][V], sc[NV][V], w2[NV][V];
+  auto first_parameters = [&](int j) __attribute__((always_inline)) {
     load_params<P, V>((const P*)a.weight, piece(j).start, V, 1.0f, w[j]);
     load_params<P, V>((const P*)a.bias, piece(j).start, V, 0.0f, b[j]);
     load_params<P, V>((const P*)a.scale, piece(j).start, V, 1.0f, sc[j]);
+  };
+  auto next_parameters = [&](int j) __attribute__((always_inline)) {
     load_params<P, V>((const P*)a.next_weight, piece(j).start, V, 1.0f, w2[j]);
+  };
+  // sums over the rows of G act z, G act, dnormed zy, dnormed
+  float sums[4][NV][V];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    if constexpr (kRoom) {
+      first_parameters(j);
+      next_parameters(j);
+    }
 #pragma unroll
     for (int k = 0; k < 4; ++k)
 #pragma unroll
       for (int i = 0; i < V; ++i) sums[k][j][i] = 0.0f;
   }
   const float inv_n = 1.0f / (float)a.n;
-  const int64_t step = (int64_t)gridDim.x * kRows;
-  for (int64_t first = (int64_t)blockIdx.x * kRows; first < a.rows; first += step) {
+  struct Row {
+    Elements<T, V> x[NV], g[NV], n[NV];
+    Elements<R, V> y[NV], d[NV];
+    float mean, rstd, mean_y, rstd_y;
+  };
+  auto ask_row = [&](Row& r, int64_t row) __attribute__((always_inline)) {
+    if (row >= a.rows) return;
+    ask(r.x, a.x, row * a.ld_x, piece);
+    if (a.gate) ask(r.g, a.gate, row * a.ld_g, piece);
+    if (a.dnormed) {
+      ask(r.n, a.dnormed, row * a.ld_dn, piece);
+      ask(r.y, a.y, row * a.ld_y, piece);
+      r.mean_y = a.stats[2 * a.rows + row];
+      r.rstd_y = a.stats[3 * a.rows + row];
+    }
+    if (a.dy) ask(r.d, a.dy, row * a.ld_dy, piece);
+    r.mean = a.stats[row];
+    r.rstd = a.stats[a.rows + row];
+  };
+  const int64_t step = (int64_t)gridDim.x * groups;
+  Row ahead;
+  if constexpr (kRoom) ask_row(ahead, (int64_t)blockIdx.x * groups + group);
+  for (int64_t first = (int64_t)blockIdx.x * groups; first < a.rows; first += step) {
     const int64_t row = first + group;
     const bool here = row < a.rows;
-    Elements<T, V> rx[NV], rg[NV], rn[NV];
-    Elements<R, V> ry[NV], rd[NV];
-    float mean = 0.0f, rstd = 0.0f, mean_y = 0.0f, rstd_y = 0.0f;
-    if (here) {
-      ask(rx, a.x, row * a.ld_x, piece);
-      if (a.gate) ask(rg, a.gate, row * a.ld_g, piece);
-      if (a.dnormed) {
-        ask(rn, a.dnormed, row * a.ld_dn, piece);
-        ask(ry, a.y, row * a.ld_y, piece);
-        mean_y = a.stats[2 * a.rows + row];
-        rstd_y = a.stats[3 * a.rows + row];
-      }
-      if (a.dy) ask(rd, a.dy, row * a.ld_dy, piece);
-      mean = a.stats[row];
-      rstd = a.stats[a.rows + row];
+    Row now;
+    if constexpr (kRoom) {
+      now = ahead;
+      ask_row(ahead, row + step);
+    } else {
+      ask_row(now, row);
     }
     float G[NV][V], s = 0.0f, q = 0.0f;
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
-      for (int i = 0; i < V; ++i) G[j][i] = here && a.dy ? (float)rd[j].v[i] : 0.0f;
+      for (int i = 0; i < V; ++i) G[j][i] = a.dy ? (float)now.d[j].v[i] : 0.0f;
     if (a.dnormed) {
       if (here)
 #pragma unroll
-        for (int j = 0; j < NV; ++j)
+        for (int j = 0; j < NV; ++j) {
+          if constexpr (!kRoom) next_parameters(j);
 #pragma unroll
           for (int i = 0; i < V; ++i) {
-            const float zy = ((float)ry[j].v[i] - mean_y) * rstd_y, d = piece(j).counts(i) ? (float)rn[j].v[i] : 0.0f;
+            const float zy = ((float)now.y[j].v[i] - now.mean_y) * now.rstd_y, d = piece(j).counts(i) ? (float)now.n[j].v[i] : 0.0f;
             sums[2][j][i] = fmaf(d, zy, sums[2][j][i]);
             sums[3][j][i] += d;
             const float g = d * w2[j][i];
             s += g;
             q = fmaf(g, zy, q);
           }
-      row_sum2<W>(s, q, slots, turn);
+        }
+      row_sum2(s, q, slots, turn, group * waves, waves);
       s *= inv_n;
       q *= inv_n;
       if (here)
 #pragma unroll
-        for (int j = 0; j < NV; ++j)
+        for (int j = 0; j < NV; ++j) {
+          if constexpr (!kRoom) next_parameters(j);
 #pragma unroll
           for (int i = 0; i < V; ++i) {
-            const float zy = ((float)ry[j].v[i] - mean_y) * rstd_y;
-            G[j][i] = fmaf(rstd_y, fmaf((float)rn[j].v[i], w2[j][i], -s) - zy * q, G[j][i]);
+            const float zy = ((float)now.y[j].v[i] - now.mean_y) * now.rstd_y;
+            G[j][i] = fmaf(now.rstd_y, fmaf((float)now.n[j].v[i], w2[j][i], -s) - zy * q, G[j][i]);
           }
+        }
     }
     s = q = 0.0f;
     float g[NV][V];
     if (here)
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
+        if constexpr (!kRoom) first_parameters(j);
         if (a.dresidual) piece(j).put((R*)a.dresidual + row * a.ld_dr, G[j]);
-        float dg[V];
+        float act[V], slope[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) act[i] = 1.0f;
+        if (a.gate) {
+          gates_of(a.act, now.g[j], act, slope);
+          if (a.dgate) {
+            float dg[V];
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+              dg[i] = G[j][i] * sc[j][i] * fmaf(((float)now.x[j].v[i] - now.mean) * now.rstd, w[j][i], b[j][i]) * slope[i];
+            piece(j).put((T*)a.dgate + row * a.ld_dg, dg);
+          }
+        }
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-          float act = 1.0f, slope = 0.0f;
-          if (a.gate) gate_of(a.act, (float)rg[j].v[i], act, slope);
-          const float z = ((float)rx[j].v[i] - mean) * rstd, scaled = G[j][i] * sc[j][i], t = piece(j).counts(i) ? G[j][i] * act : 0.0f;
-          dg[i] = scaled * fmaf(z, w[j][i], b[j][i]) * slope;
+          const float z = ((float)now.x[j].v[i] - now.mean) * now.rstd, through = G[j][i] * act[i], t = piece(j).counts(i) ? through : 0.0f;
           sums[0][j][i] = fmaf(t, z, sums[0][j][i]);
           sums[1][j][i] += t;
-          g[j][i] = scaled * act * w[j][i];
+          g[j][i] = through * (sc[j][i] * w[j][i]);
           const float counted = piece(j).counts(i) ? g[j][i] : 0.0f;
           s += counted;
           q = fmaf(counted, z, q);
         }
-        if (a.dgate) piece(j).put((T*)a.dgate + row * a.ld_dg, dg);
       }
-    row_sum2<W>(s, q, slots, turn);
+    row_sum2(s, q, slots, turn, group * waves, waves);
     s *= inv_n;
     q *= inv_n;
     if (here)
@@ -316,13 +388,13 @@ __global__ __launch_bounds__(row_groups(W, 8) * W * 64) void block_norm_grad_ker
       for (int j = 0; j < NV; ++j) {
         float o[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) o[i] = rstd * (g[j][i] - s - ((float)rx[j].v[i] - mean) * rstd * q);
+        for (int i = 0; i < V; ++i) o[i] = now.rstd * (g[j][i] - s - ((float)now.x[j].v[i] - now.mean) * now.rstd * q);
         piece(j).put((T*)a.dx + row * a.ld_dx, o);
       }
   }
   if (!a.part) return;
   float* part = a.part + (int64_t)blockIdx.x * 4 * a.n;
-  if constexpr (kRows > 1) {
+  if (groups > 1) {
     for (int half = 0; half < 2; ++half) {
       if (half) __syncthreads();
 #pragma unroll
@@ -331,15 +403,14 @@ __global__ __launch_bounds__(row_groups(W, 8) * W * 64) void block_norm_grad_ker
         for (int j = 0; j < NV; ++j)
 #pragma unroll
           for (int i = 0; i < V; ++i)
-            shared_sums[((group * 2 + k) * NV * V + j * V + i) * kThreads + tid] = half ? sums[2 + k][j][i] : sums[k][j][i];
+            shared_sums[((group * 2 + k) * NV * V + j * V + i) * threads + tid] = half ? sums[2 + k][j][i] : sums[k][j][i];
       __syncthreads();
-      for (int at = threadIdx.x; at < 2 * kEntries; at += kRows * kThreads) {
-        const int of = at % kEntries, ji = of / kThreads, i = ji % V;
+      for (int at = threadIdx.x; at < 2 * entries; at += groups * threads) {
+        const int k = at >= entries, of = at - k * entries, ji = of / threads, i = ji % V;
         float sum = 0.0f;
-#pragma unroll
-        for (int r = 0; r < kRows; ++r) sum += shared_sums[r * 2 * kEntries + at];
-        const Piece<W, V> p(ji / V, of % kThreads, a.n);
-        if (p.counts(i)) part[(int64_t)(half * 2 + at / kEntries) * a.n + p.start + i] = sum;
+        for (int r = 0; r < groups; ++r) sum += shared_sums[r * 2 * entries + at];
+        const Piece<V> p(ji / V, of - ji * threads, a.n, threads);
+        if (p.counts(i)) part[(int64_t)(half * 2 + k) * a.n + p.start + i] = sum;
       }
     }
   } else {
@@ -387,23 +458,20 @@ __global__ __launch_bounds__(1024) void block_norm_sum_kernel(BlockNormGradArgs 
   }
 }
 
-// Entries per lane, and waves per row, of rows of n entries.
+// Forward: waves per row and pieces per lane.  16 entries per lane at most (one wave up to 1024).  Few rows go to four waves each from 512
+// entries on, where the row's latency counts.
 struct Shape {
   int waves, pieces;
 };
-// 16 entries per lane at most forward (one wave up to 1024), 8 backward, where four sums per column stay in registers too; 16 of
-// either where 16 waves have no more.  Few rows go to four waves each from 512 entries on, where the row's latency counts.
-template <int V, bool GRAD>
+constexpr int kPerLane = 16;
+template <int V>
 Shape shape_of(int64_t rows, int n) {
   if constexpr (V == 1) return {1, 1};  // rows of less than 16 bytes
-  constexpr int per_lane = GRAD ? 8 : 16;
-  for (int p = 1; p * V <= per_lane; p *= 2)
+  for (int p = 1; p * V <= kPerLane; p *= 2)
     if (n <= 64 * p * V && (rows > 512 || n <= 512)) return {1, p};
-  for (int p = 1; p * V <= per_lane; p *= 2)
+  for (int p = 1; p * V <= kPerLane; p *= 2)
     if (n <= 256 * p * V) return {4, p};
-  if (n <= 512 * per_lane) return {8, per_lane / V};
-  if (n <= 1024 * per_lane) return {16, per_lane / V};
-  return {16, 16 / V};
+  return {n <= 512 * kPerLane ? 8 : 16, kPerLane / V};
 }
 
 template <typename F>
@@ -413,31 +481,35 @@ hipError_t with_types(int type, int residual, int param, F f) {
   if (type == AMQ_BF16) return residual == AMQ_F32 ? params(bf16(), float()) : params(bf16(), bf16());
   return residual == AMQ_F32 ? params(f16(), float()) : params(f16(), f16());
 }
-template <int V, bool GRAD, typename F>
+template <int V, typename F>
 hipError_t with_shape(Shape h, F f) {
 #define AMQ_SHAPE(W, NV) \
   if (h.waves == W && h.pieces == NV) return f(std::integral_constant<int, V>(), std::integral_constant<int, W>(), std::integral_constant<int, NV>())
   AMQ_SHAPE(1, 1);
   if constexpr (V > 1) {
-    constexpr int per_lane = GRAD ? 8 : 16, most = per_lane / V;
-    if constexpr (most >= 2) AMQ_SHAPE(1, 2);
+    constexpr int most = kPerLane / V;
+    AMQ_SHAPE(1, 2);
     if constexpr (most >= 4) AMQ_SHAPE(1, 4);
     AMQ_SHAPE(4, 1);
-    if constexpr (most >= 2) AMQ_SHAPE(4, 2);
+    AMQ_SHAPE(4, 2);
     if constexpr (most >= 4) AMQ_SHAPE(4, 4);
     AMQ_SHAPE(8, most);
     AMQ_SHAPE(16, most);
-    if constexpr (GRAD) AMQ_SHAPE(16, 16 / V);
   }
 #undef AMQ_SHAPE
   return hipErrorInvalidValue;
 }
-// The kernels' entries per piece: 16 bytes of T, or one where a row has less.
-template <typename T, bool GRAD, typename F>
-hipError_t with_pieces(int64_t rows, int n, F f) {
-  constexpr int V = kPer16<T>;
-  if (n < V) return with_shape<1, GRAD>(shape_of<1, GRAD>(rows, n), f);
-  return with_shape<V, GRAD>(shape_of<V, GRAD>(rows, n), f);
+
+// Backward: pieces of 4 entries, one per lane where 16 waves have room for the row, else 2 or 4.  Four parameters, four sums and what is read take
+// 27 registers per entry: with 8 entries a lane, as 16-byte loads would have, a compute unit had room for 8 waves.
+constexpr int kGradPiece = 4;
+template <typename F>
+hipError_t with_grad_pieces(int n, F f) {
+  if (n < kGradPiece) return f(std::integral_constant<int, 1>(), std::integral_constant<int, 1>());
+  const std::integral_constant<int, kGradPiece> v;
+  if (n <= 1024 * kGradPiece) return f(v, std::integral_constant<int, 1>());
+  if (n <= 2048 * kGradPiece) return f(v, std::integral_constant<int, 2>());
+  return f(v, std::integral_constant<int, 4>());
 }
 
 // Rows that a grid of at most `most` workgroups takes at a time, spread evenly over its rounds.
@@ -448,8 +520,6 @@ int64_t even_blocks(int64_t tasks, int64_t most) {
 
 constexpr int64_t kMostParts = 256;  // one workgroup per compute unit: more partial rows cost more than they hide
 
-template <int W>
-int64_t grad_blocks(int64_t rows) { return even_blocks((rows + row_groups(W, 8) - 1) / row_groups(W, 8), kMostParts); }
 
 }  // namespace
 
@@ -458,13 +528,15 @@ int block_norm_grad_parts(int64_t rows, int) { return (int)(rows < kMostParts ? 
 hipError_t launch_block_norm(const BlockNormArgs& a, hipStream_t s) {
   return with_types(a.type, a.residual_type, a.param_type, [&](auto t, auto r, auto p) {
     using T = decltype(t);
-    return with_pieces<T, false>(a.rows, a.n, [&](auto v, auto w, auto nv) {
+    auto f = [&](auto v, auto w, auto nv) {
       constexpr int W = decltype(w)::value, kRows = row_groups(W, 4);
       const int64_t tasks = (a.rows + kRows - 1) / kRows;
       block_norm_kernel<T, decltype(r), decltype(p), decltype(v)::value, W, decltype(nv)::value>
           <<<dim3((unsigned)even_blocks(tasks, W >= 8 ? 512 : 1024)), dim3(kRows * W * 64), 0, s>>>(a);
       return hipGetLastError();
-    });
+    };
+    constexpr int V = kPer16<T>;
+    return a.n < V ? with_shape<1>(shape_of<1>(a.rows, a.n), f) : with_shape<V>(shape_of<V>(a.rows, a.n), f);
   });
 }
 
@@ -476,11 +548,11 @@ hipError_t launch_block_norm_grad(const BlockNormGradArgs& a0, hipStream_t s) {
     using T = decltype(t);
     using P = decltype(p);
     int64_t parts = 0;
-    const hipError_t e = with_pieces<T, true>(a.rows, a.n, [&](auto v, auto w, auto nv) {
-      constexpr int W = decltype(w)::value;
-      parts = grad_blocks<W>(a.rows);
-      block_norm_grad_kernel<T, decltype(r), P, decltype(v)::value, W, decltype(nv)::value>
-          <<<dim3((unsigned)parts), dim3(row_groups(W, 8) * W * 64), 0, s>>>(a);
+    const hipError_t e = with_grad_pieces(a.n, [&](auto v, auto nv) {
+      constexpr int V = decltype(v)::value, NV = decltype(nv)::value;
+      const int waves = (a.n + 64 * V * NV - 1) / (64 * V * NV), groups = 16 / waves;
+      parts = even_blocks((a.rows + groups - 1) / groups, kMostParts);
+      block_norm_grad_kernel<T, decltype(r), P, V, NV><<<dim3((unsigned)parts), dim3(groups * waves * 64), 0, s>>>(a, waves);
       return hipGetLastError();
     });
     if (e != hipSuccess || !sums) return e;

@@ -22,78 +22,85 @@
 namespace amq {
 namespace {
 
-__device__ __forceinline__ float sum64(float v) { return group_sum(v, 6); }
-
-// Sums of two values over the W waves that share a row.  One barrier, of all groups of W waves in the workgroup: the slots of
-// consecutive calls alternate.
-template <int W>
-__device__ __forceinline__ void row_sum2(float& a, float& b, float (*slots)[2], int& turn) {
-  a = sum64(a);
-  b = sum64(b);
-  if constexpr (W > 1) {
-    const int waves = blockDim.x / 64, group = wave_id() / W * W;
-    float(*s)[2] = slots + turn * waves;
-    turn ^= 1;
-    if (lane_id() == 0) {
-      s[wave_id()][0] = a;
-      s[wave_id()][1] = b;
-    }
-    lds_barrier();
-    a = b = 0.0f;
-#pragma unroll
-    for (int i = 0; i < W; ++i) {
-      a += s[group + i][0];
-      b += s[group + i][1];
-    }
-  }
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
 }
-template <int W>
-__device__ __forceinline__ float row_sum(float a, float (*slots)[2], int& turn) {
-  float b = 0.0f;
-  row_sum2<W>(a, b, slots, turn);
-  return a;
+// v + its value 16 or 32 lanes away (the swap of two copies leaves one half's values twice in either).
+__device__ __forceinline__ float add_16_away(float v) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float add_32_away(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float lane_of(float v, int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane)); }
+// Sums over the even lanes and over the odd lanes of a value; every lane ends with that of its kind.
+__device__ __forceinline__ float sums_by_parity(float v) {
+  v += dpp<0x4E>(v);   // quad_perm [2,3,0,1]
+  v += dpp<0x124>(v);  // row_ror 4
+  v += dpp<0x128>(v);  // row_ror 8
+  return add_32_away(add_16_away(v));
 }
 
-// The same over `waves` waves, up to 16, beginning with wave `first`: a lane reads one wave's sums each.
+// Sums of two values over the `waves` waves, up to 16, that share a row, beginning with wave `first`: a in even lanes and b in odd ones
+// take one reduction together.  One barrier, of all that meet in the workgroup: the slots of consecutive calls alternate.
 __device__ __forceinline__ void row_sum2(float& a, float& b, float (*slots)[2], int& turn, int first, int waves) {
-  a = sum64(a);
-  b = sum64(b);
-  if (waves == 1) return;
-  float(*s)[2] = slots + turn * 16;
-  turn ^= 1;
-  if (lane_id() == 0) {
-    s[wave_id()][0] = a;
-    s[wave_id()][1] = b;
+  const bool odd = lane_id() & 1;
+  float v = (odd ? b : a) + dpp<0xB1>(odd ? a : b);  // quad_perm [1,0,3,2]
+  v = sums_by_parity(v);
+  if (waves > 1) {
+    float(*s)[2] = slots + turn * 16;
+    turn ^= 1;
+    if (lane_id() < 2) s[wave_id()][lane_id()] = v;
+    lds_barrier();
+    v = lane_id() < 2 * waves ? s[first + (lane_id() >> 1)][lane_id() & 1] : 0.0f;
+    v = sums_by_parity(v);
   }
-  lds_barrier();
-  const int l = lane_id() & 15;
-  a = group_sum(l < waves ? s[first + l][0] : 0.0f, 4);
-  b = group_sum(l < waves ? s[first + l][1] : 0.0f, 4);
+  a = lane_of(v, 0);
+  b = lane_of(v, 1);
+}
+__device__ __forceinline__ float row_sum(float a, float (*slots)[2], int& turn, int first, int waves) {
+  float b = 0.0f;
+  row_sum2(a, b, slots, turn, first, waves);
+  return a;
 }
 
 // Piece j of a row's pieces of V entries for thread `tid` of `threads`.  The last one ends with the row and overlaps the one before
 // it (its first `repeated` entries count there); threads past the end hold it once more with nothing that counts, and store
-// nothing.  (n >= V.)
+// nothing.  (n >= V.)  Rows are the same in all lanes of a wave: an address is theirs and 32 bits of a lane.
 template <int V>
 struct Piece {
-  int start, repeated;
+  uint32_t start;
+  int repeated;
+  bool even;  // the row is a number of whole pieces (the same in all lanes)
   __device__ __forceinline__ Piece(int j, int tid, int n, int threads) {
-    const int c = (j * threads + tid) * V;
-    start = c < n - V ? c : n - V;
-    repeated = c - start < V ? c - start : V;
+    const int c = (j * threads + tid) * V, s = c < n - V ? c : n - V;
+    start = (uint32_t)s;
+    repeated = c - s < V ? c - s : V;
+    even = n % V == 0;
   }
   __device__ __forceinline__ bool counts(int i) const { return i >= repeated; }
   __device__ __forceinline__ bool any() const { return repeated < V; }
-  // a result; entries that the piece before has are stored there (they may lie where an operand did)
+  template <typename T>
+  __device__ __forceinline__ Elements<T, V> get(const T* row) const {
+    return *reinterpret_cast<const Elements<T, V>*>(reinterpret_cast<const char*>(row) + start * (uint32_t)sizeof(T));
+  }
+  // A result; entries that the piece before has are stored there (they may lie where an operand did).  (The values of the row's end are
+  // made new ones, so that the compiler does not join both ways of storing into one of single entries.)
   template <typename T>
   __device__ __forceinline__ void put(T* row, const float (&v)[V]) const {
-    T* p = row + start;
+    T* p = reinterpret_cast<T*>(reinterpret_cast<char*>(row) + start * (uint32_t)sizeof(T));
     if (repeated == 0) {
-      store<T, V>(p, V, v);
-    } else if (any()) {
+      store_whole<T, V>(p, v);
+    } else if (!even && any()) {
 #pragma unroll
-      for (int i = 1; i < V; ++i)
-        if (i >= repeated) p[i] = (T)v[i];
+      for (int i = 1; i < V; ++i) {
+        float e = v[i];
+        asm volatile("" : "+v"(e));
+        if (i >= repeated) p[i] = (T)e;
+      }
     }
   }
 };
@@ -134,9 +141,8 @@ __device__ __forceinline__ void gates_of(int act, const Elements<T, V>& z, float
 
 template <typename T, int V, int NV, typename F>
 __device__ __forceinline__ void ask(Elements<T, V> (&r)[NV], const void* base, int64_t offset, F piece) {
-  const T* p = (const T*)base + offset;
 #pragma unroll
-  for (int j = 0; j < NV; ++j) r[j] = fetch<T, V>(p + piece(j).start, V);
+  for (int j = 0; j < NV; ++j) r[j] = piece(j).get((const T*)base + offset);
 }
 
 constexpr int row_groups(int waves, int most) { return waves >= most ? 1 : most / waves; }
@@ -145,9 +151,9 @@ constexpr int row_groups(int waves, int most) { return waves >= most ? 1 : most 
 template <typename T, typename R, typename P, int V, int W, int NV>
 __global__ __launch_bounds__(W > 4 ? W * 64 : 256) void block_norm_kernel(BlockNormArgs a) {
   constexpr int kRows = row_groups(W, 4);
-  __shared__ float slots[2 * W * kRows][2];
+  __shared__ float slots[2 * 16][2];
   int turn = 0;
-  const int group = wave_id() / W, tid = (int)threadIdx.x - group * W * 64;
+  const int group = __builtin_amdgcn_readfirstlane(wave_id() / W), tid = (int)threadIdx.x - group * W * 64;
   auto piece = [&](int j) __attribute__((always_inline)) { return Piece<V>(j, tid, a.n, W * 64); };
   // the scale is folded into the first norm's parameters
   float w[NV][V], b[NV][V], w2[NV][V], b2[NV][V];
@@ -196,7 +202,7 @@ __global__ __launch_bounds__(W > 4 ? W * 64 : 256) void block_norm_kernel(BlockN
       }
     }
     fetch_row(row + step);
-    const float mean = row_sum<W>(s, slots, turn) * inv_n;
+    const float mean = row_sum(s, slots, turn, group * W, W) * inv_n;
     s = 0.0f;
 #pragma unroll
     for (int j = 0; j < NV; ++j)
@@ -205,7 +211,7 @@ __global__ __launch_bounds__(W > 4 ? W * 64 : 256) void block_norm_kernel(BlockN
         x[j][i] -= mean;
         s = fmaf(piece(j).counts(i) ? x[j][i] : 0.0f, x[j][i], s);
       }
-    const float rstd = 1.0f / sqrtf(row_sum<W>(s, slots, turn) * inv_n + a.eps);
+    const float rstd = 1.0f / sqrtf(row_sum(s, slots, turn, group * W, W) * inv_n + a.eps);
     s = 0.0f;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
@@ -218,7 +224,7 @@ __global__ __launch_bounds__(W > 4 ? W * 64 : 256) void block_norm_kernel(BlockN
     }
     float mean_y = 0.0f, rstd_y = 0.0f;
     if (a.normed) {
-      mean_y = row_sum<W>(s, slots, turn) * inv_n;
+      mean_y = row_sum(s, slots, turn, group * W, W) * inv_n;
       s = 0.0f;
 #pragma unroll
       for (int j = 0; j < NV; ++j)
@@ -227,7 +233,7 @@ __global__ __launch_bounds__(W > 4 ? W * 64 : 256) void block_norm_kernel(BlockN
           y[j][i] -= mean_y;
           s = fmaf(piece(j).counts(i) ? y[j][i] : 0.0f, y[j][i], s);
         }
-      rstd_y = 1.0f / sqrtf(row_sum<W>(s, slots, turn) * inv_n + a.eps);
+      rstd_y = 1.0f / sqrtf(row_sum(s, slots, turn, group * W, W) * inv_n + a.eps);
       if (here)
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
@@ -252,25 +258,43 @@ template <typename T, typename R, typename P, int V, int NV>
 __global__ __launch_bounds__(1024) void block_norm_grad_kernel(BlockNormGradArgs a, int waves) {
   __shared__ float slots[2 * 16][2];
   // [group][sum][j][i][thread]: consecutive lanes on consecutive banks
-  __shared__ float shared_sums[2 * 1024 * NV * V];
+  constexpr bool kInLds = NV == 2;  // the sums themselves lie there (one row per workgroup), for want of registers
+  __shared__ float shared_sums[(kInLds ? 4 : NV == 1 ? 2 : 1) * (NV > 2 ? 1 : 1024 * NV * V)];
   int turn = 0;
   const int threads = waves * 64, groups = blockDim.x / threads, entries = threads * NV * V;
   const int group = __builtin_amdgcn_readfirstlane(wave_id() / waves), tid = (int)threadIdx.x - group * threads;
   auto piece = [&](int j) __attribute__((always_inline)) { return Piece<V>(j, tid, a.n, threads); };
-  // With one piece a lane has room for the parameters and asks for a row ahead; with more it reads the parameters again for every row (from
-  // L2: 16 bytes an entry, where spilled registers would be 38).
+  // scale x weight, scale x bias, next_weight; 0 where an entry does not count, so that sums along the row leave it out.  With one piece a lane
+  // has room for them and for a row ahead; with more it reads them again for every row (from L2).
   constexpr bool kRoom = NV == 1;
-  float w[NV][V], b[NV][V], sc[NV][V], w2[NV][V];
+  float sw[NV][V], sb[NV][V], w2[NV][V];
   auto first_parameters = [&](int j) __attribute__((always_inline)) {
-    load_params<P, V>((const P*)a.weight, piece(j).start, V, 1.0f, w[j]);
-    load_params<P, V>((const P*)a.bias, piece(j).start, V, 0.0f, b[j]);
-    load_params<P, V>((const P*)a.scale, piece(j).start, V, 1.0f, sc[j]);
+    const Piece<V> p = piece(j);
+    float sc[V];
+    load_params<P, V>((const P*)a.scale, p.start, V, 1.0f, sc);
+    load_params<P, V>((const P*)a.weight, p.start, V, 1.0f, sw[j]);
+    load_params<P, V>((const P*)a.bias, p.start, V, 0.0f, sb[j]);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      sw[j][i] = p.counts(i) ? sw[j][i] * sc[i] : 0.0f;
+      sb[j][i] *= sc[i];
+    }
   };
   auto next_parameters = [&](int j) __attribute__((always_inline)) {
-    load_params<P, V>((const P*)a.next_weight, piece(j).start, V, 1.0f, w2[j]);
+    const Piece<V> p = piece(j);
+    load_params<P, V>((const P*)a.next_weight, p.start, V, 1.0f, w2[j]);
+#pragma unroll
+    for (int i = 0; i < V; ++i) w2[j][i] = p.counts(i) ? w2[j][i] : 0.0f;
   };
   // sums over the rows of G act z, G act, dnormed zy, dnormed
   float sums[4][NV][V];
+  auto in_lds = [&](int k, int j, int i) __attribute__((always_inline)) -> float& {
+    return shared_sums[((k * NV + j) * V + i) * 1024 + threadIdx.x];
+  };
+  auto sum_up = [&](int k, int j, int i, float u, float v) __attribute__((always_inline)) {
+    if constexpr (kInLds) in_lds(k, j, i) = fmaf(u, v, in_lds(k, j, i));
+    else sums[k][j][i] = fmaf(u, v, sums[k][j][i]);
+  };
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     if constexpr (kRoom) {
@@ -280,7 +304,10 @@ __global__ __launch_bounds__(1024) void block_norm_grad_kernel(BlockNormGradArgs
 #pragma unroll
     for (int k = 0; k < 4; ++k)
 #pragma unroll
-      for (int i = 0; i < V; ++i) sums[k][j][i] = 0.0f;
+      for (int i = 0; i < V; ++i) {
+        if constexpr (kInLds) in_lds(k, j, i) = 0.0f;
+        else sums[k][j][i] = 0.0f;
+      }
   }
   const float inv_n = 1.0f / (float)a.n;
   struct Row {
@@ -288,10 +315,8 @@ __global__ __launch_bounds__(1024) void block_norm_grad_kernel(BlockNormGradArgs
     Elements<R, V> y[NV], d[NV];
     float mean, rstd, mean_y, rstd_y;
   };
-  auto ask_row = [&](Row& r, int64_t row) __attribute__((always_inline)) {
+  auto ask_first = [&](Row& r, int64_t row) __attribute__((always_inline)) {
     if (row >= a.rows) return;
-    ask(r.x, a.x, row * a.ld_x, piece);
-    if (a.gate) ask(r.g, a.gate, row * a.ld_g, piece);
     if (a.dnormed) {
       ask(r.n, a.dnormed, row * a.ld_dn, piece);
       ask(r.y, a.y, row * a.ld_y, piece);
@@ -299,21 +324,33 @@ __global__ __launch_bounds__(1024) void block_norm_grad_kernel(BlockNormGradArgs
       r.rstd_y = a.stats[3 * a.rows + row];
     }
     if (a.dy) ask(r.d, a.dy, row * a.ld_dy, piece);
+  };
+  auto ask_second = [&](Row& r, int64_t row) __attribute__((always_inline)) {
+    if (row >= a.rows) return;
+    ask(r.x, a.x, row * a.ld_x, piece);
+    if (a.gate) ask(r.g, a.gate, row * a.ld_g, piece);
     r.mean = a.stats[row];
     r.rstd = a.stats[a.rows + row];
   };
+  auto apart = [] __attribute__((always_inline)) {
+    if constexpr (!kRoom) __builtin_amdgcn_sched_barrier(0);
+  };
   const int64_t step = (int64_t)gridDim.x * groups;
   Row ahead;
-  if constexpr (kRoom) ask_row(ahead, (int64_t)blockIdx.x * groups + group);
+  if constexpr (kRoom) {
+    ask_first(ahead, (int64_t)blockIdx.x * groups + group);
+    ask_second(ahead, (int64_t)blockIdx.x * groups + group);
+  }
   for (int64_t first = (int64_t)blockIdx.x * groups; first < a.rows; first += step) {
     const int64_t row = first + group;
     const bool here = row < a.rows;
     Row now;
     if constexpr (kRoom) {
       now = ahead;
-      ask_row(ahead, row + step);
+      ask_first(ahead, row + step);
+      ask_second(ahead, row + step);
     } else {
-      ask_row(now, row);
+      ask_first(now, row);
     }
     float G[NV][V], s = 0.0f, q = 0.0f;
 #pragma unroll
@@ -321,65 +358,69 @@ __global__ __launch_bounds__(1024) void block_norm_grad_kernel(BlockNormGradArgs
 #pragma unroll
       for (int i = 0; i < V; ++i) G[j][i] = a.dy ? (float)now.d[j].v[i] : 0.0f;
     if (a.dnormed) {
+      float zy[NV][V], g[NV][V];
+      const float shift = -now.mean_y * now.rstd_y;
       if (here)
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
+          apart();
           if constexpr (!kRoom) next_parameters(j);
 #pragma unroll
           for (int i = 0; i < V; ++i) {
-            const float zy = ((float)now.y[j].v[i] - now.mean_y) * now.rstd_y, d = piece(j).counts(i) ? (float)now.n[j].v[i] : 0.0f;
-            sums[2][j][i] = fmaf(d, zy, sums[2][j][i]);
-            sums[3][j][i] += d;
-            const float g = d * w2[j][i];
-            s += g;
-            q = fmaf(g, zy, q);
+            const float d = (float)now.n[j].v[i];
+            zy[j][i] = fmaf((float)now.y[j].v[i], now.rstd_y, shift);
+            sum_up(2, j, i, d, zy[j][i]);
+            sum_up(3, j, i, d, 1.0f);
+            g[j][i] = d * w2[j][i];
+            s += g[j][i];
+            q = fmaf(g[j][i], zy[j][i], q);
           }
         }
+      apart();
       row_sum2(s, q, slots, turn, group * waves, waves);
       s *= inv_n;
       q *= inv_n;
       if (here)
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-          if constexpr (!kRoom) next_parameters(j);
+        for (int j = 0; j < NV; ++j)
 #pragma unroll
-          for (int i = 0; i < V; ++i) {
-            const float zy = ((float)now.y[j].v[i] - now.mean_y) * now.rstd_y;
-            G[j][i] = fmaf(now.rstd_y, fmaf((float)now.n[j].v[i], w2[j][i], -s) - zy * q, G[j][i]);
-          }
-        }
+          for (int i = 0; i < V; ++i) G[j][i] = fmaf(now.rstd_y, fmaf(-zy[j][i], q, g[j][i] - s), G[j][i]);
     }
     s = q = 0.0f;
-    float g[NV][V];
-    if (here)
+    apart();
+    if constexpr (!kRoom) ask_second(now, row);
+    float g[NV][V], z[NV][V];
+    if (here) {
+      const float shift = -now.mean * now.rstd;
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
+        apart();
         if constexpr (!kRoom) first_parameters(j);
         if (a.dresidual) piece(j).put((R*)a.dresidual + row * a.ld_dr, G[j]);
-        float act[V], slope[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) act[i] = 1.0f;
+        for (int i = 0; i < V; ++i) z[j][i] = fmaf((float)now.x[j].v[i], now.rstd, shift);
         if (a.gate) {
+          float act[V], slope[V];
           gates_of(a.act, now.g[j], act, slope);
           if (a.dgate) {
             float dg[V];
 #pragma unroll
-            for (int i = 0; i < V; ++i)
-              dg[i] = G[j][i] * sc[j][i] * fmaf(((float)now.x[j].v[i] - now.mean) * now.rstd, w[j][i], b[j][i]) * slope[i];
+            for (int i = 0; i < V; ++i) dg[i] = G[j][i] * fmaf(z[j][i], sw[j][i], sb[j][i]) * slope[i];
             piece(j).put((T*)a.dgate + row * a.ld_dg, dg);
           }
+#pragma unroll
+          for (int i = 0; i < V; ++i) G[j][i] *= act[i];
         }
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-          const float z = ((float)now.x[j].v[i] - now.mean) * now.rstd, through = G[j][i] * act[i], t = piece(j).counts(i) ? through : 0.0f;
-          sums[0][j][i] = fmaf(t, z, sums[0][j][i]);
-          sums[1][j][i] += t;
-          g[j][i] = through * (sc[j][i] * w[j][i]);
-          const float counted = piece(j).counts(i) ? g[j][i] : 0.0f;
-          s += counted;
-          q = fmaf(counted, z, q);
+          sum_up(0, j, i, G[j][i], z[j][i]);
+          sum_up(1, j, i, G[j][i], 1.0f);
+          g[j][i] = G[j][i] * sw[j][i];
+          s += g[j][i];
+          q = fmaf(g[j][i], z[j][i], q);
         }
       }
+    }
     row_sum2(s, q, slots, turn, group * waves, waves);
     s *= inv_n;
     q *= inv_n;
@@ -388,28 +429,25 @@ __global__ __launch_bounds__(1024) void block_norm_grad_kernel(BlockNormGradArgs
       for (int j = 0; j < NV; ++j) {
         float o[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) o[i] = now.rstd * (g[j][i] - s - ((float)now.x[j].v[i] - now.mean) * now.rstd * q);
+        for (int i = 0; i < V; ++i) o[i] = now.rstd * fmaf(-z[j][i], q, g[j][i] - s);
         piece(j).put((T*)a.dx + row * a.ld_dx, o);
       }
   }
   if (!a.part) return;
   float* part = a.part + (int64_t)blockIdx.x * 4 * a.n;
-  if (groups > 1) {
+  if (NV == 1 && groups > 1) {
     for (int half = 0; half < 2; ++half) {
       if (half) __syncthreads();
 #pragma unroll
       for (int k = 0; k < 2; ++k)
 #pragma unroll
-        for (int j = 0; j < NV; ++j)
-#pragma unroll
-          for (int i = 0; i < V; ++i)
-            shared_sums[((group * 2 + k) * NV * V + j * V + i) * threads + tid] = half ? sums[2 + k][j][i] : sums[k][j][i];
+        for (int i = 0; i < V; ++i) shared_sums[((group * 2 + k) * V + i) * threads + tid] = half ? sums[2 + k][0][i] : sums[k][0][i];
       __syncthreads();
       for (int at = threadIdx.x; at < 2 * entries; at += groups * threads) {
-        const int k = at >= entries, of = at - k * entries, ji = of / threads, i = ji % V;
+        const int k = at >= entries, of = at - k * entries, i = of / threads;
         float sum = 0.0f;
         for (int r = 0; r < groups; ++r) sum += shared_sums[r * 2 * entries + at];
-        const Piece<V> p(ji / V, of - ji * threads, a.n, threads);
+        const Piece<V> p(0, of - i * threads, a.n, threads);
         if (p.counts(i)) part[(int64_t)(half * 2 + k) * a.n + p.start + i] = sum;
       }
     }
@@ -420,7 +458,7 @@ __global__ __launch_bounds__(1024) void block_norm_grad_kernel(BlockNormGradArgs
       for (int j = 0; j < NV; ++j)
 #pragma unroll
         for (int i = 0; i < V; ++i)
-          if (piece(j).counts(i)) part[(int64_t)k * a.n + piece(j).start + i] = sums[k][j][i];
+          if (piece(j).counts(i)) part[(int64_t)k * a.n + piece(j).start + i] = kInLds ? in_lds(k, j, i) : sums[k][j][i];
   }
 }
 
@@ -550,7 +588,10 @@ hipError_t launch_block_norm_grad(const BlockNormGradArgs& a0, hipStream_t s) {
     int64_t parts = 0;
     const hipError_t e = with_grad_pieces(a.n, [&](auto v, auto nv) {
       constexpr int V = decltype(v)::value, NV = decltype(nv)::value;
-      const int waves = (a.n + 64 * V * NV - 1) / (64 * V * NV), groups = 16 / waves;
+      const int waves = (a.n + 64 * V * NV - 1) / (64 * V * NV);
+      // few rows: one each for as many compute units as there are
+      const int64_t share = (a.rows + kMostParts - 1) / kMostParts;
+      const int groups = share < 16 / waves ? (int)share : 16 / waves;
       parts = even_blocks((a.rows + groups - 1) / groups, kMostParts);
       block_norm_grad_kernel<T, decltype(r), P, V, NV><<<dim3((unsigned)parts), dim3(groups * waves * 64), 0, s>>>(a, waves);
       return hipGetLastError();

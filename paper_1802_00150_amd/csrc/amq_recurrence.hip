@@ -90,10 +90,7 @@ struct Lane {
   }
   template <typename T>
   __device__ __forceinline__ void put(T* row, const float (&v)[V]) const {
-    Elements<T, V> e;
-#pragma unroll
-    for (int j = 0; j < V; ++j) e.v[j] = (T)v[j];
-    *reinterpret_cast<Elements<T, V>*>(reinterpret_cast<char*>(row) + first * (uint32_t)sizeof(T)) = e;
+    store_whole<T, V>(reinterpret_cast<T*>(reinterpret_cast<char*>(row) + first * (uint32_t)sizeof(T)), v);
   }
 };
 

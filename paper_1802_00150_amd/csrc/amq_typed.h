@@ -73,6 +73,32 @@ __device__ __forceinline__ void store(T* p, int valid, const float (&in)[V]) {
       at += n;
     }
 }
+// All V of them in one store, which the compiler makes of single elements only at times.
+template <typename T, int V>
+__device__ __forceinline__ void store_whole(T* p, const float (&in)[V]) {
+  Elements<T, V> b;
+#pragma unroll
+  for (int i = 0; i < V; ++i) b.v[i] = (T)in[i];
+  constexpr int kBytes = V * (int)sizeof(T);
+  if constexpr (kBytes % 4 == 0) {
+    typedef uint32_t Words __attribute__((ext_vector_type(kBytes / 4)));
+    struct __attribute__((packed, aligned(sizeof(T)))) Unaligned {
+      Words w;
+    };
+    reinterpret_cast<Unaligned*>(p)->w = __builtin_bit_cast(Words, b);
+  } else {
+    *reinterpret_cast<Elements<T, V>*>(p) = b;
+  }
+}
+// The same past the caches: results that are not read again soon.
+template <typename T, int V>
+__device__ __forceinline__ void store_streaming(T* p, const float (&in)[V]) {
+  Elements<T, V> b;
+#pragma unroll
+  for (int i = 0; i < V; ++i) b.v[i] = (T)in[i];
+  typedef uint32_t Words __attribute__((ext_vector_type(V * sizeof(T) / 4), aligned(sizeof(T))));
+  __builtin_nontemporal_store(__builtin_bit_cast(Words, b), reinterpret_cast<Words*>(p));
+}
 template <typename T>
 __device__ __forceinline__ void store16(T* p, int valid, const float (&in)[kPer16<T>]) {
   if (valid > 0) store<T, kPer16<T>>(p, valid, in);

@@ -83,15 +83,32 @@ struct Piece {
   }
   __device__ __forceinline__ bool counts(int i) const { return i >= repeated; }
   __device__ __forceinline__ bool any() const { return repeated < V; }
+  // (A new value at every use: the compiler made 64-bit addresses of lanes that it kept over all rows, most of the registers.)
+  template <typename T>
+  __device__ __forceinline__ uint32_t offset() const {
+    uint32_t bytes = start * (uint32_t)sizeof(T);
+    asm volatile("" : "+v"(bytes));
+    return bytes;
+  }
   template <typename T>
   __device__ __forceinline__ Elements<T, V> get(const T* row) const {
-    return *reinterpret_cast<const Elements<T, V>*>(reinterpret_cast<const char*>(row) + start * (uint32_t)sizeof(T));
+    return *reinterpret_cast<const Elements<T, V>*>(reinterpret_cast<const char*>(row) + offset<T>());
+  }
+  // parameters, absent ones (null) as `absent`
+  template <typename P>
+  __device__ __forceinline__ void get(const void* p, float absent, float (&out)[V]) const {
+#pragma unroll
+    for (int i = 0; i < V; ++i) out[i] = absent;
+    if (!p) return;
+    const Elements<P, V> e = get((const P*)p);
+#pragma unroll
+    for (int i = 0; i < V; ++i) out[i] = (float)e.v[i];
   }
   // A result; entries that the piece before has are stored there (they may lie where an operand did).  (The values of the row's end are
   // made new ones, so that the compiler does not join both ways of storing into one of single entries.)
   template <typename T>
   __device__ __forceinline__ void put(T* row, const float (&v)[V]) const {
-    T* p = reinterpret_cast<T*>(reinterpret_cast<char*>(row) + start * (uint32_t)sizeof(T));
+    T* p = reinterpret_cast<T*>(reinterpret_cast<char*>(row) + offset<T>());
     if (repeated == 0) {
       store_whole<T, V>(p, v);
     } else if (!even && any()) {
@@ -145,6 +162,22 @@ __device__ __forceinline__ void ask(Elements<T, V> (&r)[NV], const void* base, i
   for (int j = 0; j < NV; ++j) r[j] = piece(j).get((const T*)base + offset);
 }
 
+// Makes the compiler take what was read as new values, so that it does not keep what was formed from them.
+template <typename T, int V>
+__device__ __forceinline__ void again(Elements<T, V>& e) {
+  if constexpr (sizeof(e) % 4 == 0) {
+    typedef uint32_t Words __attribute__((ext_vector_type(sizeof(e) / 4)));
+    Words w = __builtin_bit_cast(Words, e);
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(e) / 4; ++i) {
+      uint32_t v = w[i];
+      asm volatile("" : "+v"(v));
+      w[i] = v;
+    }
+    e = __builtin_bit_cast(Elements<T, V>, w);
+  }
+}
+
 constexpr int row_groups(int waves, int most) { return waves >= most ? 1 : most / waves; }
 
 // T: x, gate and normed; R: residual and y; P: parameters.  W waves per row, NV pieces of V entries per lane.
@@ -160,11 +193,11 @@ __global__ __launch_bounds__(W > 4 ? W * 64 : 256) void block_norm_kernel(BlockN
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     float s[V];
-    load_params<P, V>((const P*)a.weight, piece(j).start, V, 1.0f, w[j]);
-    load_params<P, V>((const P*)a.bias, piece(j).start, V, 0.0f, b[j]);
-    load_params<P, V>((const P*)a.scale, piece(j).start, V, 1.0f, s);
-    load_params<P, V>((const P*)a.next_weight, piece(j).start, V, 1.0f, w2[j]);
-    load_params<P, V>((const P*)a.next_bias, piece(j).start, V, 0.0f, b2[j]);
+    piece(j).template get<P>(a.weight, 1.0f, w[j]);
+    piece(j).template get<P>(a.bias, 0.0f, b[j]);
+    piece(j).template get<P>(a.scale, 1.0f, s);
+    piece(j).template get<P>(a.next_weight, 1.0f, w2[j]);
+    piece(j).template get<P>(a.next_bias, 0.0f, b2[j]);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       w[j][i] *= s[i];
@@ -271,9 +304,9 @@ __global__ __launch_bounds__(1024) void block_norm_grad_kernel(BlockNormGradArgs
   auto first_parameters = [&](int j) __attribute__((always_inline)) {
     const Piece<V> p = piece(j);
     float sc[V];
-    load_params<P, V>((const P*)a.scale, p.start, V, 1.0f, sc);
-    load_params<P, V>((const P*)a.weight, p.start, V, 1.0f, sw[j]);
-    load_params<P, V>((const P*)a.bias, p.start, V, 0.0f, sb[j]);
+    p.template get<P>(a.scale, 1.0f, sc);
+    p.template get<P>(a.weight, 1.0f, sw[j]);
+    p.template get<P>(a.bias, 0.0f, sb[j]);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       sw[j][i] = p.counts(i) ? sw[j][i] * sc[i] : 0.0f;
@@ -282,7 +315,7 @@ __global__ __launch_bounds__(1024) void block_norm_grad_kernel(BlockNormGradArgs
   };
   auto next_parameters = [&](int j) __attribute__((always_inline)) {
     const Piece<V> p = piece(j);
-    load_params<P, V>((const P*)a.next_weight, p.start, V, 1.0f, w2[j]);
+    p.template get<P>(a.next_weight, 1.0f, w2[j]);
 #pragma unroll
     for (int i = 0; i < V; ++i) w2[j][i] = p.counts(i) ? w2[j][i] : 0.0f;
   };
@@ -377,6 +410,9 @@ __global__ __launch_bounds__(1024) void block_norm_grad_kernel(BlockNormGradArgs
           }
         }
       apart();
+      if constexpr (!kRoom)
+#pragma unroll
+        for (int j = 0; j < NV; ++j) again(now.y[j]), again(now.n[j]);
       row_sum2(s, q, slots, turn, group * waves, waves);
       s *= inv_n;
       q *= inv_n;
@@ -384,14 +420,21 @@ __global__ __launch_bounds__(1024) void block_norm_grad_kernel(BlockNormGradArgs
 #pragma unroll
         for (int j = 0; j < NV; ++j)
 #pragma unroll
-          for (int i = 0; i < V; ++i) G[j][i] = fmaf(now.rstd_y, fmaf(-zy[j][i], q, g[j][i] - s), G[j][i]);
+          for (int i = 0; i < V; ++i) {
+            if constexpr (!kRoom) {  // (formed again: what was read takes less room)
+              if (i == 0) next_parameters(j);
+              zy[j][i] = fmaf((float)now.y[j].v[i], now.rstd_y, shift);
+              g[j][i] = (float)now.n[j].v[i] * w2[j][i];
+            }
+            G[j][i] = fmaf(now.rstd_y, fmaf(-zy[j][i], q, g[j][i] - s), G[j][i]);
+          }
     }
     s = q = 0.0f;
     apart();
     if constexpr (!kRoom) ask_second(now, row);
     float g[NV][V], z[NV][V];
+    const float shift = -now.mean * now.rstd;
     if (here) {
-      const float shift = -now.mean * now.rstd;
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
         apart();
@@ -421,6 +464,9 @@ __global__ __launch_bounds__(1024) void block_norm_grad_kernel(BlockNormGradArgs
         }
       }
     }
+    if constexpr (!kRoom)
+#pragma unroll
+      for (int j = 0; j < NV; ++j) again(now.x[j]);
     row_sum2(s, q, slots, turn, group * waves, waves);
     s *= inv_n;
     q *= inv_n;
@@ -429,7 +475,10 @@ __global__ __launch_bounds__(1024) void block_norm_grad_kernel(BlockNormGradArgs
       for (int j = 0; j < NV; ++j) {
         float o[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) o[i] = now.rstd * fmaf(-z[j][i], q, g[j][i] - s);
+        for (int i = 0; i < V; ++i) {
+          if constexpr (!kRoom) z[j][i] = fmaf((float)now.x[j].v[i], now.rstd, shift);
+          o[i] = now.rstd * fmaf(-z[j][i], q, g[j][i] - s);
+        }
         piece(j).put((T*)a.dx + row * a.ld_dx, o);
       }
   }

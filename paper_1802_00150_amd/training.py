@@ -1,13 +1,15 @@
-"""Quantization-aware training of a residual block on top of a recurrent layer's hidden states (Sec. 4, "Training":
-the forward pass uses the quantized weights, the gradient passes straight through to the full-precision ones, which
-are clipped to [-1, 1]).
+"""Quantization-aware training (Sec. 4, "Training": the forward pass uses the quantized weights, the gradient passes
+straight through to the full-precision ones, which are clipped to [-1, 1]) of a residual block on top of a recurrent
+layer's hidden states, and of a block with a recurrence of its own over whole sequences.
 
     normed = layer_norm(h);  y = h + W2_hat gelu(W1_hat normed + b1) + b2,   W_hat = fake_quantize(W)
+    g, x, o = W1_hat normed + b1;  s = linear_recurrence(g, x);  y = h + scale silu(o) norm(W2_hat s),  next = norm(y)
 
-`layer_norm` and `linear` are the package's operators with their gradients for torch's autograd; `ResidualBlock.step`
-runs forward, backward and the update: momentum, orthogonalized matrices, plain steps for vectors, clip.
+`layer_norm`, `linear`, `linear_recurrence` and `block_norm` are the package's operators with their gradients for torch's
+autograd; `ResidualBlock.step` and `RecurrentBlock.step` run forward, backward and the update: clipping by the norm of all
+gradients, momentum, orthogonalized matrices, plain steps for vectors, clip.
 
-    python -m paper_1802_00150_amd.training          # a small run that prints its loss
+    python -m paper_1802_00150_amd.training          # two small runs that print their loss
 """
 import torch
 from torch.autograd.function import once_differentiable
@@ -63,23 +65,103 @@ def linear(x, W, bias=None, activation=None, residual=None):
     return _Linear.apply(x, W, bias, activation, residual)
 
 
-class ResidualBlock:
-    """y = h + W2_hat gelu(W1_hat layer_norm(h) + b1) + b2 with k-bit weights; parameters and momenta in float32."""
+class _LinearRecurrence(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, gate, x, h0, mode, lengths):
+        ctx.mode = mode
+        ctx.set_materialize_grads(False)
+        hs, last, states = binding.linear_recurrence(gate, x, h0, mode, lengths, states=any(ctx.needs_input_grad[:3]))
+        ctx.save_for_backward(gate, x, h0, lengths, states)
+        return hs, last
 
-    def __init__(self, units, inner, k=2, T=2, device="cuda", seed=0, lr=0.02, momentum=0.95):
-        g = torch.Generator(device=device).manual_seed(seed)
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dhs, dlast):
+        gate, x, h0, lengths, states = ctx.saved_tensors
+        dhs = torch.zeros(x.shape, dtype=x.dtype, device=x.device) if dhs is None else dhs.contiguous()
+        dlast = None if dlast is None else dlast.contiguous()
+        dgate, dx, dh0 = binding.linear_recurrence_backward(dhs, gate, x, h0, states, dlast, ctx.mode, lengths)
+        need = ctx.needs_input_grad
+        return dgate if need[0] else None, dx if need[1] else None, dh0 if need[2] else None, None, None
 
-        def matrix(rows, cols):
-            return (torch.randn(rows, cols, generator=g, device=device) * cols ** -0.5).requires_grad_()
 
-        self.k, self.T, self.lr, self.momentum = k, T, lr, momentum
+def linear_recurrence(gate, x, h0=None, mode="blend", lengths=None):
+    """binding.linear_recurrence's states and last state, differentiable in gate, x and h0."""
+    return _LinearRecurrence.apply(gate, x, h0, mode, lengths)
+
+
+class _BlockNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, residual, gate, weight, bias, scale, next_weight, next_bias, activation, eps):
+        ctx.activation = activation
+        ctx.set_materialize_grads(False)
+        y, normed, stats = binding.block_norm(x, residual, weight, bias, gate, activation, scale, next_weight, next_bias, eps)
+        ctx.save_for_backward(x, y, stats, gate, weight, bias, scale, next_weight, next_bias)
+        return y, normed
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy, dnormed):
+        if dy is None and dnormed is None:
+            return (None,) * 10
+        x, y, stats, gate, weight, bias, scale, next_weight, next_bias = ctx.saved_tensors
+        dy, dnormed = (None if d is None else d.contiguous() for d in (dy, dnormed))
+        need = ctx.needs_input_grad
+        dx, dr, dgate, *params = binding.block_norm_backward(dy, dnormed, x, y, stats, weight, bias, gate, ctx.activation, scale, next_weight,
+                                                             next_bias, param_grads=any(need[3:8]))
+        return tuple(g if n else None for g, n in zip((dx, dr, dgate, *params), need[:8])) + (None, None)
+
+
+def block_norm(x, residual, weight=None, bias=None, gate=None, activation="sigmoid", scale=None, next_weight=None, next_bias=None,
+               eps=1e-5):
+    """binding.block_norm's y and normed y, differentiable in x, residual, gate and the parameters."""
+    return _BlockNorm.apply(x, residual, gate, weight, bias, scale, next_weight, next_bias, activation, eps)
+
+
+class _Block:
+    """What the blocks below share: parameters in float32 with their momenta, and the update."""
+
+    def _begin(self, matrices, vectors, k, T, lr, momentum, max_norm):
+        self.k, self.T, self.lr, self.momentum, self.max_norm = k, T, lr, momentum, max_norm
+        self.matrices, self.vectors = matrices, vectors
+        self.moments = [torch.zeros_like(p) for p in matrices + vectors]
+
+    def _update(self, value):
+        params = self.matrices + self.vectors
+        grads = torch.autograd.grad(value, params)
+        with torch.no_grad():
+            if self.max_norm is not None:
+                self.gradient_norm = binding.clip_gradients(grads, self.max_norm)
+            for p, g, m in zip(params, grads, self.moments):
+                m.mul_(self.momentum).add_(g)
+                if p.dim() == 2:
+                    # the update's singular values are near 1: its size follows the matrix's, not the gradient's
+                    p.add_(binding.orthogonalize(m), alpha=-self.lr * max(1.0, p.shape[0] / p.shape[1]) ** 0.5)
+                    binding.clip_(p)
+                else:
+                    p.sub_(m, alpha=self.lr)
+        return value.detach()
+
+
+def _matrices(seed, device):
+    g = torch.Generator(device=device).manual_seed(seed)
+    return lambda rows, cols: (torch.randn(rows, cols, generator=g, device=device) * cols ** -0.5).requires_grad_()
+
+
+def _vector(n, value, device):
+    return torch.full((n,), float(value), device=device, requires_grad=True)
+
+
+class ResidualBlock(_Block):
+    """y = h + W2_hat gelu(W1_hat layer_norm(h) + b1) + b2 with k-bit weights; parameters and momenta in float32.
+    max_norm: the largest norm of all gradients of a step (None: any), which `gradient_norm` holds in front of clipping."""
+
+    def __init__(self, units, inner, k=2, T=2, device="cuda", seed=0, lr=0.02, momentum=0.95, max_norm=None):
+        matrix = _matrices(seed, device)
         self.W1, self.W2 = matrix(inner, units), matrix(units, inner)
-        self.b1 = torch.zeros(inner, device=device, requires_grad=True)
-        self.b2 = torch.zeros(units, device=device, requires_grad=True)
-        self.weight = torch.ones(units, device=device, requires_grad=True)
-        self.bias = torch.zeros(units, device=device, requires_grad=True)
-        self.matrices, self.vectors = [self.W1, self.W2], [self.b1, self.b2, self.weight, self.bias]
-        self.moments = [torch.zeros_like(p) for p in self.matrices + self.vectors]
+        self.b1, self.b2 = _vector(inner, 0, device), _vector(units, 0, device)
+        self.weight, self.bias = _vector(units, 1, device), _vector(units, 0, device)
+        self._begin([self.W1, self.W2], [self.b1, self.b2, self.weight, self.bias], k, T, lr, momentum, max_norm)
 
     def forward(self, h):
         """h [..., units] in float32, bfloat16 or float16; the products run in its type."""
@@ -90,19 +172,43 @@ class ResidualBlock:
 
     def step(self, h, loss):
         """One step on `loss` (a function of the block's output); returns its value."""
-        value = loss(self.forward(h))
-        params = self.matrices + self.vectors
-        grads = torch.autograd.grad(value, params)
-        with torch.no_grad():
-            for p, g, m in zip(params, grads, self.moments):
-                m.mul_(self.momentum).add_(g)
-                if p.dim() == 2:
-                    # the update's singular values are near 1: its size follows the matrix's, not the gradient's
-                    p.add_(binding.orthogonalize(m), alpha=-self.lr * max(1.0, p.shape[0] / p.shape[1]) ** 0.5)
-                    binding.clip_(p)
-                else:
-                    p.sub_(m, alpha=self.lr)
-        return value.detach()
+        return self._update(loss(self.forward(h)))
+
+
+class RecurrentBlock(_Block):
+    """A block of k-bit weights whose recurrence runs over whole sequences [steps, batch, units]: gate, candidate and output gate are one
+    projection of the normed stream, the recurrence blends the candidates, and its states' projection joins the residual stream
+    behind a norm, its gate and a scale.  Parameters and momenta in float32; max_norm as in ResidualBlock."""
+
+    def __init__(self, units, k=2, T=2, device="cuda", seed=0, lr=0.02, momentum=0.95, max_norm=1.0):
+        matrix = _matrices(seed, device)
+        self.units = units
+        self.W1, self.W2 = matrix(3 * units, units), matrix(units, units)
+        self.b1 = _vector(3 * units, 0, device)
+        with torch.no_grad():  # units that forget within a few steps and units that hold for hundreds
+            self.b1[:units] = torch.linspace(-1, 5, units, device=device)
+        self.first_weight, self.first_bias = _vector(units, 1, device), _vector(units, 0, device)
+        self.weight, self.bias, self.scale = _vector(units, 1, device), _vector(units, 0, device), _vector(units, 0.5, device)
+        self.next_weight, self.next_bias = _vector(units, 1, device), _vector(units, 0, device)
+        self._begin([self.W1, self.W2], [self.b1, self.first_weight, self.first_bias, self.weight, self.bias, self.scale, self.next_weight,
+                                         self.next_bias], k, T, lr, momentum, max_norm)
+
+    def forward(self, h, state=None, lengths=None):
+        """h [steps, batch, units] in float32, bfloat16 or float16; state [batch, units] float32 or None; lengths as in linear_recurrence
+        -> the residual stream behind the block, the same normed for the next one, the last state."""
+        n = self.units
+        W1, W2 = (binding.fake_quantize(W, self.k, self.T).to(h.dtype) for W in self.matrices)
+        normed = layer_norm(h, self.first_weight, self.first_bias)
+        gate, candidate, out = linear(normed, W1, self.b1.to(h.dtype)).chunk(3, -1)
+        states, last = linear_recurrence(gate, candidate, state, lengths=lengths)
+        block = linear(states, W2)
+        y, following = block_norm(block.view(-1, n), h.reshape(-1, n), self.weight, self.bias, out.flatten(0, 1), "silu", self.scale,
+                                  self.next_weight, self.next_bias)
+        return y.view(h.shape), following.view(h.shape), last
+
+    def step(self, h, loss, lengths=None):
+        """One step on `loss` (a function of the stream behind the block and of the same normed); returns its value."""
+        return self._update(loss(*self.forward(h, lengths=lengths)[:2]))
 
 
 def main():
@@ -115,6 +221,14 @@ def main():
         value = block.step(h, lambda y: (y - target).square().mean())
         if i % 10 == 0 or i == 49:
             print("step %d: mean squared error %.5f" % (i, value.item()), flush=True)
+    # the mean of all steps so far, which takes a state
+    h = torch.randn(35, 20, units, generator=g, device="cuda")
+    target = h + h.cumsum(0) / torch.arange(1, 36, device="cuda")[:, None, None]
+    block = RecurrentBlock(units)
+    for i in range(50):
+        value = block.step(h, lambda y, _: (y - target).square().mean())
+        if i % 10 == 0 or i == 49:
+            print("recurrent step %d: mean squared error %.5f, norm of the gradients %.4f" % (i, value.item(), block.gradient_norm.item()), flush=True)
 
 
 if __name__ == "__main__":

@@ -1,0 +1,140 @@
+"""The recurrent block's operators as they are used together: a training step, its gradients, and single tokens with the state handed on."""
+import pytest
+import torch
+
+from train_util import DEV, DTYPES, U, rand, relative
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def amq():
+    import paper_1802_00150_amd as amq
+    return amq
+
+
+@pytest.fixture(scope="module")
+def training():
+    from paper_1802_00150_amd import training
+    return training
+
+
+def reference(block, amq, h, state, lengths):
+    """The block in binary64 on the CPU, on the weights that the quantizer gives, with leaves for its gradients."""
+    n = block.units
+    p = {k: getattr(block, k).detach().cpu().double() for k in ("b1", "first_weight", "first_bias", "weight", "bias", "scale", "next_weight", "next_bias")}
+    with torch.no_grad():
+        p["W1"], p["W2"] = (amq.fake_quantize(W.detach(), block.k, block.T).cpu().double() for W in block.matrices)
+    p = {k: v.requires_grad_() for k, v in p.items()}
+    h = h.detach().cpu().double().requires_grad_()
+    normed = torch.nn.functional.layer_norm(h, (n,), p["first_weight"], p["first_bias"])
+    gate, x, out = (normed @ p["W1"].t() + p["b1"]).chunk(3, -1)
+    s = torch.zeros(h.shape[1], n, dtype=torch.float64) if state is None else state.detach().cpu().double()
+    states = []
+    for t in range(h.shape[0]):
+        f = torch.sigmoid(gate[t])
+        new = f * s + (1 - f) * x[t]
+        here = torch.ones(h.shape[1], 1, dtype=torch.bool) if lengths is None else (lengths.cpu() > t)[:, None]
+        s = torch.where(here, new, s)
+        states.append(torch.where(here, new, torch.zeros_like(new)))
+    block_out = torch.stack(states) @ p["W2"].t()
+    u = torch.nn.functional.layer_norm(block_out, (n,), p["weight"], p["bias"])
+    y = h + p["scale"] * torch.nn.functional.silu(out) * u
+    return h, p, y, torch.nn.functional.layer_norm(y, (n,), p["next_weight"], p["next_bias"]), s
+
+
+@pytest.mark.parametrize("T,B,n,ragged", [(5, 3, 20, False), (35, 4, 66, True), (200, 2, 36, False)])
+def test_forward_and_gradients(amq, training, T, B, n, ragged):
+    """Against binary64: eight operators in a row, each within about 100 U of its result's norm (their own tests), whose slopes are below 4 in
+    norm: 8 * 100 U * 4 = 2e-4 of a result's or gradient's norm.  A row of a padded step is a block output of zeros, whose norm has a
+    slope of eps^-1/2 = 316: padding is left out of the loss."""
+    block = training.RecurrentBlock(n, device=DEV, seed=T)
+    h = rand(T, T, B, n).to(DEV).requires_grad_()
+    state = rand(1, B, n).to(DEV)
+    lengths = torch.tensor([T, max(1, T // 2), 1, T - 1][:B]).to(DEV) if ragged else None
+    here = torch.ones(T, B, 1) if lengths is None else (torch.arange(T)[:, None] < lengths.cpu()).float()[:, :, None]
+    wy, wn, ws = rand(2, T, B, n) * here, rand(3, T, B, n) * here, rand(4, B, n)
+    y, following, last = block.forward(h, state, lengths)
+    rh, p, ry, rf, rs = reference(block, amq, h, state, lengths)
+    tol = 2e-4
+    hd = here.to(DEV)
+    assert relative(y * hd, (ry * here).detach()) < tol and relative(following * hd, (rf * here).detach()) < tol and relative(last, rs.detach()) < tol
+    params = block.matrices + block.vectors
+    grads = torch.autograd.grad((y * wy.to(DEV)).sum() + (following * wn.to(DEV)).sum() + (last * ws.to(DEV)).sum(), [h] + params)
+    names = ["W1", "W2", "b1", "first_weight", "first_bias", "weight", "bias", "scale", "next_weight", "next_bias"]
+    refs = torch.autograd.grad((ry * wy).sum() + (rf * wn).sum() + (rs * ws).sum(), [rh] + [p[k] for k in names])
+    for name, g, r in zip(["h"] + names, grads, refs):
+        assert g.shape == r.shape and relative(g, r) < tol, name
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_tokens_one_by_one(amq, training, dtype):
+    """Serving: one step at a time with the state handed on is the whole sequence.  The products of few and of many rows round differently, by less than
+    2^-7 of a value in bfloat16 through the block's slopes."""
+    n, T = 64, 9
+    block = training.RecurrentBlock(n, device=DEV, seed=1)
+    h = rand(5, T, 3, n).to(dtype).to(DEV)
+    with torch.no_grad():
+        y, following, last = block.forward(h)
+        state, ys = None, []
+        for t in range(T):
+            one, _, state = block.forward(h[t:t + 1], state)
+            ys.append(one)
+    tol = 16 * torch.finfo(dtype).eps if dtype != torch.float32 else 2e-4
+    assert relative(torch.cat(ys), y.cpu()) < tol and relative(state, last.cpu()) < tol
+
+
+def test_step_is_its_operators(amq, training):
+    """A step's gradients are clipped together, in front of the momenta."""
+    block, other = (training.RecurrentBlock(48, device=DEV, seed=2, max_norm=limit) for limit in (0.05, None))
+    h = rand(6, 35, 4, 48).to(DEV)
+
+    def loss(y, following):
+        return (y.square().mean() + (following - 0.5).square().mean())
+
+    params = other.matrices + other.vectors
+    grads = torch.autograd.grad(loss(*other.forward(h)[:2]), params)
+    want = float(amq.gradient_norm(grads))
+    block.step(h, loss)
+    assert abs(float(block.gradient_norm) - want) <= 2 * U * want and want > 0.05
+    amq.clip_gradients(grads, 0.05)
+    for m, g in zip(block.moments, grads):
+        assert torch.equal(m, g)
+    plain = training.ResidualBlock(48, 96, device=DEV, seed=3)
+    clipped = training.ResidualBlock(48, 96, device=DEV, seed=3, max_norm=1e9)
+    for b in (plain, clipped):
+        b.step(h.view(-1, 48), lambda y: y.square().mean())
+    assert all(torch.equal(a, b) for a, b in zip(plain.matrices + plain.vectors, clipped.matrices + clipped.vectors))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_autograd_forms(amq, training, dtype):
+    """Only what is asked for gets a gradient, and what is unused counts as zeros."""
+    T, B, n = 140, 2, 24
+    gate, x, h0 = rand(1, T, B, n).to(dtype).to(DEV), rand(2, T, B, n).to(dtype).to(DEV), rand(3, B, n).to(DEV)
+    w = rand(4, T, B, n).to(dtype).to(DEV)
+    states = amq.linear_recurrence(gate, x, h0, states=True)[2]
+    want = amq.linear_recurrence_backward(w, gate, x, h0, states)
+    leaves = [t.clone().requires_grad_() for t in (gate, x, h0)]
+    hs, last = training.linear_recurrence(*leaves)
+    got = torch.autograd.grad((hs * w).sum(), leaves)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    only = gate.clone().requires_grad_()
+    hs, last = training.linear_recurrence(only, x)
+    zeros = torch.zeros_like(x)
+    g, = torch.autograd.grad(last.sum(), only)
+    states = amq.linear_recurrence(gate, x, None, states=True)[2]
+    assert torch.equal(g, amq.linear_recurrence_backward(zeros, gate, x, None, states, torch.ones(B, n, device=DEV))[0])
+    a, r = rand(5, 30, n).to(dtype).to(DEV), rand(6, 30, n).to(dtype).to(DEV).requires_grad_()
+    weight = torch.ones(n, device=DEV).requires_grad_()
+    y, normed = training.block_norm(a, r, weight)
+    dr, dw = torch.autograd.grad(normed.float().square().sum(), [r, weight])
+    y2, n2, stats = amq.block_norm(a, r.detach(), weight.detach())
+    want = amq.block_norm_backward(None, (2 * n2.float()).to(dtype), a, y2, stats, weight.detach())
+    assert torch.equal(dr, want[1]) and torch.equal(dw, want[3])
+
+
+def test_the_module_runs(training, capsys):
+    training.main()
+    out = capsys.readouterr().out
+    assert "recurrent step 49" in out and "nan" not in out

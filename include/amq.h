@@ -561,7 +561,8 @@ int amq_orthogonalize(const void* G, int64_t batch, int64_t batch_stride, int64_
  *   lengths [B] int64 or NULL: entry b has lengths[b] steps (taken as 0 below 0 and as `steps` above).  gate and x behind them are
  *   not read, hs is 0 there, and the state stays what it is
  *   h0 [B][n] float or NULL for zeros;  h_last [B][n] float or NULL: the state behind the last step; may be h0 itself
- *   states [(steps - 1) / AMQ_STATE_STEPS][B][n] float or NULL: the states in front of steps 128, 256, ..., which the backward pass takes
+ *   states [(steps - 1) / AMQ_STATE_STEPS][B][n] float or NULL: the states in front of steps 128, 256, ..., which the backward pass takes (of
+ *   each entry those in front of its lengths[b]; the others are not written)
  *   workspace: at least amq_linear_recurrence_workspace_bytes(steps, B, n, type) bytes, 256-byte aligned (0: may be NULL).
  * One step with h0 and h_last is the form for single tokens.
  * The backward pass takes dhs [steps][B][n] and dh_last [B][n] (NULL: zeros), the gradients of hs and h_last, and leaves those of gate, x and

@@ -176,6 +176,17 @@ __device__ __forceinline__ void look_back(const Chain& c, int64_t tile, uint64_t
         h[j] = fmaf(__uint_as_float((uint32_t)m), h[j], __uint_as_float((uint32_t)(m >> 32)));
       }
 }
+// One wave: the state behind a tile, once it is there.
+template <int V>
+__device__ __forceinline__ void end_of(const Chain& c, int64_t tile, float (&h)[V]) {
+  bool there = false;
+  for (unsigned polls = 0; polls < kPollLimit && !there; ++polls) {
+    there = __ballot(look(c.marks + tile) == 2u) != 0;
+    if (!there) __builtin_amdgcn_s_sleep(8);
+  }
+#pragma unroll
+  for (int j = 0; j < V; ++j) h[j] = there ? __uint_as_float(look(c.ends + (tile * 64 + lane_id()) * V + j)) : __builtin_nanf("");
+}
 // What a launch with workgroups of their own keeps in the workspace: the counter, then the marks (both cleared first), maps and ends.
 struct SplitLayout {
   int64_t groups, tiles;
@@ -311,6 +322,15 @@ struct Steps {
     if (a.states && end % kTile == 0 && end < a.steps) at.ch.put(a.states + (end / kTile - 1) * (int64_t)a.batch * a.n + at.state, h);
   }
 };
+// Rows behind the end of a batch entry: zeros, every `by`-th from t on.
+template <typename T, int V, typename A>
+__device__ __forceinline__ void clear_rows(const A& a, const Group<V, A>& at, T* p, int64_t t, int64_t end, int by, int64_t step, int64_t entry) {
+  float zero[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) zero[j] = 0.0f;
+  if (at.ch.any)
+    for (T* row = at.row(p, t, step, entry); t < end; t += by, row += by * step) at.ch.put(row, zero);
+}
 template <int V, typename A>
 __device__ __forceinline__ void given(const float* p, const Group<V, A>& at, float (&h)[V]) {
 #pragma unroll
@@ -324,7 +344,7 @@ __device__ __forceinline__ void given(const float* p, const Group<V, A>& at, flo
 
 // A workgroup per group of channels, tile after tile; ONE: there is one.
 template <typename T, int MODE, int V, bool ONE>
-__global__ __launch_bounds__(64 * kTileWaves) void recurrence_kernel(RecurrenceArgs a) {
+__global__ __launch_bounds__(64 * kTileWaves, ONE ? 8 : 4) void recurrence_kernel(RecurrenceArgs a) {
   __shared__ float maps[ONE ? 1 : 2][kTileWaves][2][64 * V];
   const int w = __builtin_amdgcn_readfirstlane(wave_id()), waves = blockDim.x / 64, lane = lane_id();
   const Group<V, RecurrenceArgs> at(a, blockIdx.x);
@@ -336,7 +356,8 @@ __global__ __launch_bounds__(64 * kTileWaves) void recurrence_kernel(RecurrenceA
   if (w == 0) given<V>(a.h0, at, carry);
   int turn = 0;
   in.ask(a, at, w * kSpan);
-  for (int64_t first = 0; first < a.steps; first += waves * kSpan, turn ^= 1) {
+  int64_t first = 0;
+  for (; first < at.length; first += waves * kSpan, turn ^= 1) {
     const int64_t t0 = first + w * kSpan;
     steps.set(in, t0, at.length);
     if constexpr (!ONE) in.ask(a, at, t0 + waves * kSpan);
@@ -372,6 +393,9 @@ __global__ __launch_bounds__(64 * kTileWaves) void recurrence_kernel(RecurrenceA
     steps.replay(a, at, t0, h);
     if constexpr (ONE) return;
   }
+  if (first >= a.steps) return;
+  clear_rows(a, at, (T*)a.hs, first + w, a.steps, waves, a.hs_step, a.hs_batch);
+  if (w == 0 && a.h_last && at.ch.any) at.ch.put(a.h_last + at.state, carry);
 }
 
 // A workgroup per tile.
@@ -386,6 +410,17 @@ __global__ __launch_bounds__(64 * kTileWaves, 8) void recurrence_tiles_kernel(Re
   const uint32_t now = take_tile(split, number), tile = now / split.groups, group = now - tile * split.groups;
   const Group<V, RecurrenceArgs> at(a, group);
   const int64_t t0 = (int64_t)tile * kTile + w * kSpan;
+  const Chain chain = chain_of<V>(split, group);
+  if ((int64_t)tile * kTile >= at.length) {  // behind the entry's end
+    clear_rows(a, at, (T*)a.hs, t0, t0 + kSpan < a.steps ? t0 + kSpan : a.steps, 1, a.hs_step, a.hs_batch);
+    if (w == 0 && a.h_last && tile == split.tiles - 1) {
+      float h[V];
+      if (at.length == 0) given<V>(a.h0, at, h);
+      else end_of(chain, (at.length - 1) / kTile, h);
+      if (at.ch.any) at.ch.put(a.h_last + at.state, h);
+    }
+    return;
+  }
   Steps<T, MODE, V> steps;
   {
     Inputs<T, V> in;
@@ -417,7 +452,6 @@ __global__ __launch_bounds__(64 * kTileWaves, 8) void recurrence_tiles_kernel(Re
       A[j] *= fa;
       B[j] = fmaf(fa, B[j], maps[u][1][lane * V + j]);
     }
-  const Chain chain = chain_of<V>(split, group);
   if (tile > 0) {
     if (w == 0) leave_map(chain, tile, A, B);
     look_back<V>(chain, tile, stage, found, w, w == 0, h);
@@ -533,14 +567,23 @@ __device__ __forceinline__ void replay_back(const RecurrenceGradArgs& a, const G
 }
 
 template <typename T, int MODE, int V, bool ONE>
-__global__ __launch_bounds__(64 * kTileWaves) void recurrence_grad_kernel(RecurrenceGradArgs a) {
+__global__ __launch_bounds__(64 * kTileWaves, ONE ? 8 : 4) void recurrence_grad_kernel(RecurrenceGradArgs a) {
   __shared__ float maps[ONE ? 1 : 2][kTileWaves][3][64 * V];
   const int w = __builtin_amdgcn_readfirstlane(wave_id()), waves = blockDim.x / 64, lane = lane_id();
   const Group<V, RecurrenceGradArgs> at(a, blockIdx.x);
   float back[V];  // the gradient that reaches a tile's last state from the steps behind it
   given<V>(a.dh_last, at, back);
   int turn = 0;
-  for (int64_t tile = ONE ? 0 : (a.steps - 1) / kTile; tile >= 0; --tile, turn ^= 1) {
+  const int64_t end = at.length == 0 ? 0 : ONE ? kTile : ((at.length - 1) / kTile + 1) * kTile;  // of its last tile
+  if (end < a.steps) {
+    clear_rows(a, at, (T*)a.dgate, end + w, a.steps, waves, a.dgate_step, a.dgate_batch);
+    clear_rows(a, at, (T*)a.dx, end + w, a.steps, waves, a.dx_step, a.dx_batch);
+  }
+  if (end == 0) {
+    if (w == 0 && a.dh0 && at.ch.any) at.ch.put(a.dh0 + at.state, back);
+    return;
+  }
+  for (int64_t tile = ONE ? 0 : end / kTile - 1; tile >= 0; --tile, turn ^= 1) {
     const int64_t t0 = tile * kTile + w * kSpan;
     GradInputs<T, V> in;
     Steps<T, MODE, V> steps;
@@ -582,7 +625,7 @@ __global__ __launch_bounds__(64 * kTileWaves) void recurrence_grad_kernel(Recurr
 }
 
 template <typename T, int MODE, int V>
-__global__ __launch_bounds__(64 * kTileWaves) void recurrence_grad_tiles_kernel(RecurrenceGradArgs a, Split split) {
+__global__ __launch_bounds__(64 * kTileWaves, 8) void recurrence_grad_tiles_kernel(RecurrenceGradArgs a, Split split) {
   __shared__ uint64_t stage[kWindow][64 * V];
   __shared__ float begin[64 * V];
   __shared__ uint32_t number;
@@ -590,9 +633,21 @@ __global__ __launch_bounds__(64 * kTileWaves) void recurrence_grad_tiles_kernel(
   auto maps = reinterpret_cast<float(*)[3][64 * V]>(stage);  // [kTileWaves]
   const int w = __builtin_amdgcn_readfirstlane(wave_id()), lane = lane_id();
   const bool mine = w == kTileWaves - 1;
-  const uint32_t now = take_tile(split, number), order = now / split.groups, group = now - order * split.groups;
-  const int64_t tile = split.tiles - 1 - order, t0 = tile * kTile + w * kSpan;
+  const uint32_t now = take_tile(split, number), turn = now / split.groups, group = now - turn * split.groups;
+  const int64_t tile = split.tiles - 1 - turn, t0 = tile * kTile + w * kSpan;
   const Group<V, RecurrenceGradArgs> at(a, group);
+  if (tile * kTile >= at.length) {  // behind the entry's end
+    const int64_t end = t0 + kSpan < a.steps ? t0 + kSpan : a.steps;
+    clear_rows(a, at, (T*)a.dgate, t0, end, 1, a.dgate_step, a.dgate_batch);
+    clear_rows(a, at, (T*)a.dx, t0, end, 1, a.dx_step, a.dx_batch);
+    if (t0 == 0 && a.dh0 && at.ch.any) {
+      float r[V];
+      given<V>(a.dh_last, at, r);
+      at.ch.put(a.dh0 + at.state, r);
+    }
+    return;
+  }
+  const int64_t order = (at.length - 1) / kTile - tile;  // in the chain, which begins at the entry's end
   GradInputs<T, V> in;
   in.ask(a, at, tile, t0);
   Steps<T, MODE, V> steps;
@@ -675,15 +730,15 @@ int64_t groups_of(int64_t batch, int64_t n, int V) { return batch * ((n + 64 * V
 int64_t tiles_of(int64_t steps) { return (steps + kTile - 1) / kTile; }
 
 // The form with the least time, by measurement (us; g groups of 64 channels, t tiles).  One workgroup per group takes 3 + c t while the card
-// holds all groups at once; a workgroup per tile 9 + e t g / 256, of which 4 are the clearing of the marks.  c and e: 16-bit types
-// 2.5 and 2.9 (2000 x 8192 entries 48 and 31, 2000 x 16384 48 and 50, 300 x 8192 10.5 and 13.0), backward 4.3 and 6.1 (16.4 million entries: 2000 x 8192 71
-// and 55, 1000 x 16384 43 and 54, 300 x 8192 14.6 and 16.6); float 2.7 and 4.8 (2000 x 8192 46 and 46), backward 4.5 and 9.
+// holds all groups at once; a workgroup per tile 9 + e t g / 256, of which 4 are the clearing of the marks.  Steps x channels, one form and
+// the other: 16-bit types 1000 x 4096 23.5 and 14.2, 1000 x 8192 24.1 and 21.1, 1000 x 12288 24.7 and 27.1; backward 34 and 21, 35 and 31, 39 and 43; float
+// 1000 x 4096 22 and 19, 2000 x 8192 50 and 45, 1000 x 12288 31 and 37; backward 2000 x 8192 95 and 73, 1000 x 12288 53 and 55, 300 x 8192 14.8 and 18.9.
 bool splits(int64_t batch, int64_t n, int64_t steps, bool wide, bool backward) {
   const int64_t g = groups_of(batch, n, 1), t = tiles_of(steps);
-  const double c = wide ? backward ? 4.5 : 2.7 : backward ? 4.3 : 2.5, e = wide ? backward ? 9.0 : 4.8 : backward ? 6.1 : 2.9;
+  const double c = wide ? backward ? 5.5 : 2.8 : backward ? 4.3 : 2.6, e = wide ? backward ? 8.0 : 4.6 : backward ? 5.5 : 2.95;
   return t > 1 && g < 256 && (double)t * (c - e * (double)g / 256) > 6.0;
 }
-// Channels of a lane: two of 16 bits where a tile has its own workgroup, and forward where groups of 128 channels still fill the card
+// Channels of a lane forward: two of 16 bits where a tile has its own workgroup, and where groups of 128 channels still fill the card
 // (1000 x 32768 entries 41 us, with one 50; 2000 x 16384 65 and 48); one otherwise (35 x 262144 backward 21.2, with two 23.8).
 bool two_channels(int64_t batch, int64_t n) { return n % 2 == 0 && groups_of(batch, n, 2) >= 256; }
 
@@ -717,7 +772,7 @@ size_t workspace(int64_t steps, int64_t batch, int64_t n, int type, bool backwar
   for (int flat = 0; flat < 2; ++flat) {
     const int64_t b = flat ? 1 : batch, c = flat ? batch * n : n;
     if (!splits(b, c, steps, type == AMQ_F32, backward)) continue;
-    const int V = type != AMQ_F32 && c % 2 == 0 ? 2 : 1;
+    const int V = !backward && type != AMQ_F32 && c % 2 == 0 ? 2 : 1;
     const size_t need = SplitLayout(groups_of(b, c, V), tiles_of(steps), 64 * V).bytes;
     most = need > most ? need : most;
   }
@@ -751,11 +806,7 @@ hipError_t launch_recurrence_grad(const RecurrenceGradArgs& a, hipStream_t s) {
     using T = decltype(t);
     constexpr int M = decltype(m)::value;
     constexpr bool wide = sizeof(T) == 4;
-    if (splits(a.batch, a.n, a.steps, wide, true)) {
-      if constexpr (!wide)
-        if (a.n % 2 == 0) return launch_tiles(a, 2, s, recurrence_grad_tiles_kernel<T, M, 2>);
-      return launch_tiles(a, 1, s, recurrence_grad_tiles_kernel<T, M, 1>);
-    }
+    if (splits(a.batch, a.n, a.steps, wide, true)) return launch_tiles(a, 1, s, recurrence_grad_tiles_kernel<T, M, 1>);
     if (a.steps <= kTile) return launch_groups(a, 1, false, s, recurrence_grad_kernel<T, M, 1, true>);
     return launch_groups(a, 1, false, s, recurrence_grad_kernel<T, M, 1, false>);
   });

@@ -555,7 +555,7 @@ int amq_orthogonalize(const void* G, int64_t batch, int64_t batch_stride, int64_
  * Linear recurrences: every channel of every batch entry has a state of its own, and no product of the state stands between two
  * steps, so that a whole sequence is one pass.
  *   AMQ_RECURRENCE_BLEND: f = sigmoid(gate_t), h_t = f h_{t-1} + (1 - f) x_t   (the update of amq_gru_step, its gate given)
- *   AMQ_RECURRENCE_DECAY: h_t = gate_t h_{t-1} + x_t   (products of the factors over any 128 steps must be finite)
+ *   AMQ_RECURRENCE_DECAY: h_t = gate_t h_{t-1} + x_t   (products of the factors over any 256 steps must be finite)
  *   gate, x, hs [steps][B][n] of `type`, n entries side by side, steps and batch entries *_step and *_batch elements apart, any alignment: columns of a
  *   wider projection and tensors whose outer dimension is the batch are taken as they are (gate and x also with strides of 0)
  *   lengths [B] int64 or NULL: entry b has lengths[b] steps (taken as 0 below 0 and as `steps` above).  gate and x behind them are

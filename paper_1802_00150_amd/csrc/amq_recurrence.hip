@@ -35,6 +35,8 @@ namespace {
 constexpr int kSpan = 8;                   // steps of a wave in a tile
 constexpr int kTileWaves = 16;             // waves of a full tile
 constexpr int kTile = kSpan * kTileWaves;  // its steps
+constexpr int kLongSpan = 16, kLongTile = kLongSpan * kTileWaves;  // of tiles with workgroups of their own, forward
+static_assert(kLongTile % AMQ_STATE_STEPS == 0 && AMQ_STATE_STEPS % kLongSpan == 0, "states are left behind a wave's steps");
 static_assert(kTile == AMQ_STATE_STEPS, "a backward tile begins where a state was left");
 
 // What a step does to the state: h -> keep(h) + add.
@@ -191,7 +193,8 @@ __device__ __forceinline__ void end_of(const Chain& c, int64_t tile, float (&h)[
 struct SplitLayout {
   int64_t groups, tiles;
   size_t marks, maps, ends, bytes;
-  SplitLayout(int64_t g, int64_t t, int channels) : groups(g), tiles(t) {
+  SplitLayout(int64_t g, int64_t t) : groups(g), tiles(t) {
+    constexpr int channels = 64;
     marks = 256;
     maps = (marks + sizeof(uint32_t) * g * t + 255) & ~size_t(255);
     ends = maps + sizeof(uint64_t) * g * t * channels;
@@ -244,22 +247,22 @@ struct Group {
   __device__ __forceinline__ T* row(T* p, int64_t t, int64_t step, int64_t entry) const { return p + t * step + b * entry + c; }
 };
 
-template <typename T, int V>
+template <typename T, int V, int K = kSpan>
 struct Inputs {
-  Elements<T, V> g[kSpan], x[kSpan];
+  Elements<T, V> g[K], x[K];
   // asks for the steps from t0 on
   template <typename A>
   __device__ __forceinline__ void ask(const A& a, const Group<V, A>& at, int64_t t0) {
     const T *pg = at.row((const T*)a.gate, t0, a.gate_step, a.gate_batch), *px = at.row((const T*)a.x, t0, a.x_step, a.x_batch);
-    if (t0 + kSpan <= at.length) {
+    if (t0 + K <= at.length) {
 #pragma unroll
-      for (int k = 0; k < kSpan; ++k, pg += a.gate_step, px += a.x_step) {
+      for (int k = 0; k < K; ++k, pg += a.gate_step, px += a.x_step) {
         g[k] = at.ch.get(pg);
         x[k] = at.ch.get(px);
       }
     } else {
 #pragma unroll
-      for (int k = 0; k < kSpan; ++k, pg += a.gate_step, px += a.x_step)
+      for (int k = 0; k < K; ++k, pg += a.gate_step, px += a.x_step)
         if (t0 + k < at.length) {
           g[k] = at.ch.get(pg);
           x[k] = at.ch.get(px);
@@ -267,17 +270,17 @@ struct Inputs {
     }
   }
 };
-template <typename T, int MODE, int V>
+template <typename T, int MODE, int V, int K = kSpan>
 struct Steps {
-  Step<MODE> s[kSpan][V];
-  __device__ __forceinline__ void set(const Inputs<T, V>& in, int64_t t0, int64_t length) {
+  Step<MODE> s[K][V];
+  __device__ __forceinline__ void set(const Inputs<T, V, K>& in, int64_t t0, int64_t length) {
 #pragma unroll
-    for (int k = 0; k < kSpan; ++k)
+    for (int k = 0; k < K; ++k)
 #pragma unroll
       for (int j = 0; j < V; ++j) s[k][j].set((float)in.g[k].v[j], (float)in.x[k].v[j]);
-    if (t0 + kSpan > length)
+    if (t0 + K > length)
 #pragma unroll
-      for (int k = 0; k < kSpan; ++k)
+      for (int k = 0; k < K; ++k)
         if (t0 + k >= length)
 #pragma unroll
           for (int j = 0; j < V; ++j) s[k][j].hold();
@@ -287,7 +290,7 @@ struct Steps {
 #pragma unroll
     for (int j = 0; j < V; ++j) A[j] = 1.0f;
 #pragma unroll
-    for (int k = 0; k < kSpan; ++k)
+    for (int k = 0; k < K; ++k)
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         A[j] = s[k][j].keep(A[j]);
@@ -298,16 +301,16 @@ struct Steps {
   __device__ __forceinline__ void replay(const RecurrenceArgs& a, const Group<V, RecurrenceArgs>& at, int64_t t0, float (&h)[V]) const {
     if (t0 >= a.steps || !at.ch.any) return;
     T* py = at.row((T*)a.hs, t0, a.hs_step, a.hs_batch);
-    if (t0 + kSpan <= at.length) {
+    if (t0 + K <= at.length) {
 #pragma unroll
-      for (int k = 0; k < kSpan; ++k, py += a.hs_step) {
+      for (int k = 0; k < K; ++k, py += a.hs_step) {
 #pragma unroll
         for (int j = 0; j < V; ++j) h[j] = s[k][j].next(h[j]);
         at.ch.put(py, h);
       }
     } else {
 #pragma unroll
-      for (int k = 0; k < kSpan; ++k, py += a.hs_step) {
+      for (int k = 0; k < K; ++k, py += a.hs_step) {
         float out[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) {
@@ -317,9 +320,9 @@ struct Steps {
         if (t0 + k < a.steps) at.ch.put(py, out);
       }
     }
-    const int64_t end = t0 + kSpan;
+    const int64_t end = t0 + K;
     if (a.h_last && end >= a.steps) at.ch.put(a.h_last + at.state, h);
-    if (a.states && end % kTile == 0 && end < a.steps) at.ch.put(a.states + (end / kTile - 1) * (int64_t)a.batch * a.n + at.state, h);
+    if (a.states && end % AMQ_STATE_STEPS == 0 && end < a.steps) at.ch.put(a.states + (end / AMQ_STATE_STEPS - 1) * (int64_t)a.batch * a.n + at.state, h);
   }
 };
 // Rows behind the end of a batch entry: zeros, every `by`-th from t on.
@@ -398,9 +401,11 @@ __global__ __launch_bounds__(64 * kTileWaves, ONE ? 8 : 4) void recurrence_kerne
   if (w == 0 && a.h_last && at.ch.any) at.ch.put(a.h_last + at.state, carry);
 }
 
-// A workgroup per tile.
-template <typename T, int MODE, int V>
+// A workgroup per tile, of 16 steps of 16 waves of one channel a lane: a longer tile waits less for others than a wider one (32768 x 1024 bfloat16 57 us, 8
+// steps of two channels 61, 12 steps of one 61; 16384 x 1024 float 50, 51 and 49), and needs no even number of channels.
+template <typename T, int MODE>
 __global__ __launch_bounds__(64 * kTileWaves, 8) void recurrence_tiles_kernel(RecurrenceArgs a, Split split) {
+  constexpr int V = 1, K = kLongSpan;
   __shared__ uint64_t stage[kWindow][64 * V];
   __shared__ float begin[64 * V];
   __shared__ uint32_t number;
@@ -409,21 +414,21 @@ __global__ __launch_bounds__(64 * kTileWaves, 8) void recurrence_tiles_kernel(Re
   const int w = __builtin_amdgcn_readfirstlane(wave_id()), lane = lane_id();
   const uint32_t now = take_tile(split, number), tile = now / split.groups, group = now - tile * split.groups;
   const Group<V, RecurrenceArgs> at(a, group);
-  const int64_t t0 = (int64_t)tile * kTile + w * kSpan;
+  const int64_t t0 = (int64_t)tile * kLongTile + w * K;
   const Chain chain = chain_of<V>(split, group);
-  if ((int64_t)tile * kTile >= at.length) {  // behind the entry's end
-    clear_rows(a, at, (T*)a.hs, t0, t0 + kSpan < a.steps ? t0 + kSpan : a.steps, 1, a.hs_step, a.hs_batch);
+  if ((int64_t)tile * kLongTile >= at.length) {  // behind the entry's end
+    clear_rows(a, at, (T*)a.hs, t0, t0 + K < a.steps ? t0 + K : a.steps, 1, a.hs_step, a.hs_batch);
     if (w == 0 && a.h_last && tile == split.tiles - 1) {
       float h[V];
       if (at.length == 0) given<V>(a.h0, at, h);
-      else end_of(chain, (at.length - 1) / kTile, h);
+      else end_of(chain, (at.length - 1) / kLongTile, h);
       if (at.ch.any) at.ch.put(a.h_last + at.state, h);
     }
     return;
   }
-  Steps<T, MODE, V> steps;
+  Steps<T, MODE, V, K> steps;
   {
-    Inputs<T, V> in;
+    Inputs<T, V, K> in;
     in.ask(a, at, t0);
     steps.set(in, t0, at.length);
   }
@@ -624,8 +629,9 @@ __global__ __launch_bounds__(64 * kTileWaves, ONE ? 8 : 4) void recurrence_grad_
   }
 }
 
-template <typename T, int MODE, int V>
+template <typename T, int MODE>
 __global__ __launch_bounds__(64 * kTileWaves, 8) void recurrence_grad_tiles_kernel(RecurrenceGradArgs a, Split split) {
+  constexpr int V = 1;
   __shared__ uint64_t stage[kWindow][64 * V];
   __shared__ float begin[64 * V];
   __shared__ uint32_t number;
@@ -727,24 +733,23 @@ int waves_of(int64_t steps, bool even) {
   return (int)(tiles == 1 ? spans : even ? (spans + tiles - 1) / tiles : kTileWaves);
 }
 int64_t groups_of(int64_t batch, int64_t n, int V) { return batch * ((n + 64 * V - 1) / (64 * V)); }
-int64_t tiles_of(int64_t steps) { return (steps + kTile - 1) / kTile; }
+int64_t tiles_of(int64_t steps, int tile) { return (steps + tile - 1) / tile; }
 
 // The form with the least time, by measurement (us; g groups of 64 channels, t tiles).  One workgroup per group takes 3 + c t while the card
 // holds all groups at once; a workgroup per tile 9 + e t g / 256, of which 4 are the clearing of the marks.  Steps x channels, one form and
 // the other: 16-bit types 1000 x 4096 23.5 and 14.2, 1000 x 8192 24.1 and 21.1, 1000 x 12288 24.7 and 27.1; backward 34 and 21, 35 and 31, 39 and 43; float
 // 1000 x 4096 22 and 19, 2000 x 8192 50 and 45, 1000 x 12288 31 and 37; backward 2000 x 8192 95 and 73, 1000 x 12288 53 and 55, 300 x 8192 14.8 and 18.9.
 bool splits(int64_t batch, int64_t n, int64_t steps, bool wide, bool backward) {
-  const int64_t g = groups_of(batch, n, 1), t = tiles_of(steps);
+  const int64_t g = groups_of(batch, n, 1), t = tiles_of(steps, kTile);
   const double c = wide ? backward ? 5.5 : 2.8 : backward ? 4.3 : 2.6, e = wide ? backward ? 8.0 : 4.6 : backward ? 5.5 : 2.95;
   return t > 1 && g < 256 && (double)t * (c - e * (double)g / 256) > 6.0;
 }
-// Channels of a lane forward: two of 16 bits where a tile has its own workgroup, and where groups of 128 channels still fill the card
+// Channels of a lane: two of 16 bits where a workgroup walks over tiles forward and groups of 128 channels still fill the card
 // (1000 x 32768 entries 41 us, with one 50; 2000 x 16384 65 and 48); one otherwise (35 x 262144 backward 21.2, with two 23.8).
 bool two_channels(int64_t batch, int64_t n) { return n % 2 == 0 && groups_of(batch, n, 2) >= 256; }
 
-hipError_t split_of(int64_t groups, int64_t steps, int channels, void* ws, hipStream_t s, Split& out) {
-  const int64_t tiles = tiles_of(steps);
-  const SplitLayout l(groups, tiles, channels);
+hipError_t split_of(int64_t groups, int64_t tiles, void* ws, hipStream_t s, Split& out) {
+  const SplitLayout l(groups, tiles);
   char* p = static_cast<char*>(ws);
   out = {reinterpret_cast<uint32_t*>(p), reinterpret_cast<uint32_t*>(p + l.marks), reinterpret_cast<uint64_t*>(p + l.maps),
          reinterpret_cast<uint32_t*>(p + l.ends), tiles, (uint32_t)groups};
@@ -753,10 +758,10 @@ hipError_t split_of(int64_t groups, int64_t steps, int channels, void* ws, hipSt
   return hipGetLastError();
 }
 template <typename A, typename F>
-hipError_t launch_tiles(const A& a, int channels, hipStream_t s, F kernel) {
-  const int64_t groups = groups_of(a.batch, a.n, channels);
+hipError_t launch_tiles(const A& a, int tile, hipStream_t s, F kernel) {
+  const int64_t groups = groups_of(a.batch, a.n, 1);
   Split split;
-  const hipError_t e = split_of(groups, a.steps, 64 * channels, a.ws, s, split);
+  const hipError_t e = split_of(groups, tiles_of(a.steps, tile), a.ws, s, split);
   if (e != hipSuccess) return e;
   kernel<<<dim3((unsigned)(groups * split.tiles)), dim3(64 * kTileWaves), 0, s>>>(a, split);
   return hipGetLastError();
@@ -772,8 +777,7 @@ size_t workspace(int64_t steps, int64_t batch, int64_t n, int type, bool backwar
   for (int flat = 0; flat < 2; ++flat) {
     const int64_t b = flat ? 1 : batch, c = flat ? batch * n : n;
     if (!splits(b, c, steps, type == AMQ_F32, backward)) continue;
-    const int V = !backward && type != AMQ_F32 && c % 2 == 0 ? 2 : 1;
-    const size_t need = SplitLayout(groups_of(b, c, V), tiles_of(steps), 64 * V).bytes;
+    const size_t need = SplitLayout(groups_of(b, c, 1), tiles_of(steps, backward ? kTile : kLongTile)).bytes;
     most = need > most ? need : most;
   }
   return most;
@@ -789,11 +793,7 @@ hipError_t launch_recurrence(const RecurrenceArgs& a, hipStream_t s) {
     using T = decltype(t);
     constexpr int M = decltype(m)::value;
     constexpr bool wide = sizeof(T) == 4;
-    if (splits(a.batch, a.n, a.steps, wide, false)) {
-      if constexpr (!wide)
-        if (a.n % 2 == 0) return launch_tiles(a, 2, s, recurrence_tiles_kernel<T, M, 2>);
-      return launch_tiles(a, 1, s, recurrence_tiles_kernel<T, M, 1>);
-    }
+    if (splits(a.batch, a.n, a.steps, wide, false)) return launch_tiles(a, kLongTile, s, recurrence_tiles_kernel<T, M>);
     if (a.steps <= kTile) return launch_groups(a, 1, true, s, recurrence_kernel<T, M, 1, true>);
     if constexpr (!wide)
       if (two_channels(a.batch, a.n)) return launch_groups(a, 2, true, s, recurrence_kernel<T, M, 2, false>);
@@ -806,7 +806,7 @@ hipError_t launch_recurrence_grad(const RecurrenceGradArgs& a, hipStream_t s) {
     using T = decltype(t);
     constexpr int M = decltype(m)::value;
     constexpr bool wide = sizeof(T) == 4;
-    if (splits(a.batch, a.n, a.steps, wide, true)) return launch_tiles(a, 1, s, recurrence_grad_tiles_kernel<T, M, 1>);
+    if (splits(a.batch, a.n, a.steps, wide, true)) return launch_tiles(a, kTile, s, recurrence_grad_tiles_kernel<T, M>);
     if (a.steps <= kTile) return launch_groups(a, 1, false, s, recurrence_grad_kernel<T, M, 1, true>);
     return launch_groups(a, 1, false, s, recurrence_grad_kernel<T, M, 1, false>);
   });

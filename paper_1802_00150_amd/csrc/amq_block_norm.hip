@@ -188,6 +188,18 @@ __global__ __launch_bounds__(W > 4 ? W * 64 : 256) void block_norm_kernel(BlockN
   int turn = 0;
   const int group = __builtin_amdgcn_readfirstlane(wave_id() / W), tid = (int)threadIdx.x - group * W * 64;
   auto piece = [&](int j) __attribute__((always_inline)) { return Piece<V>(j, tid, a.n, W * 64); };
+  const float inv_n = 1.0f / (float)a.n;
+  Elements<T, V> rx[NV], rg[NV];
+  Elements<R, V> rr[NV];
+  auto fetch_row = [&](int64_t row) __attribute__((always_inline)) {
+    if (row >= a.rows) return;
+    ask(rx, a.x, row * a.ld_x, piece);
+    ask(rr, a.residual, row * a.ld_r, piece);
+    if (a.gate) ask(rg, a.gate, row * a.ld_g, piece);
+  };
+  const int64_t step = (int64_t)gridDim.x * kRows;
+  int64_t first = (int64_t)blockIdx.x * kRows;  // of the workgroup's rows: its groups meet at barriers, so they leave together
+  fetch_row(first + group);
   // the scale is folded into the first norm's parameters
   float w[NV][V], b[NV][V], w2[NV][V], b2[NV][V];
 #pragma unroll
@@ -204,18 +216,6 @@ __global__ __launch_bounds__(W > 4 ? W * 64 : 256) void block_norm_kernel(BlockN
       b[j][i] *= s[i];
     }
   }
-  const float inv_n = 1.0f / (float)a.n;
-  Elements<T, V> rx[NV], rg[NV];
-  Elements<R, V> rr[NV];
-  auto fetch_row = [&](int64_t row) __attribute__((always_inline)) {
-    if (row >= a.rows) return;
-    ask(rx, a.x, row * a.ld_x, piece);
-    ask(rr, a.residual, row * a.ld_r, piece);
-    if (a.gate) ask(rg, a.gate, row * a.ld_g, piece);
-  };
-  const int64_t step = (int64_t)gridDim.x * kRows;
-  int64_t first = (int64_t)blockIdx.x * kRows;  // of the workgroup's rows: its groups meet at barriers, so they leave together
-  fetch_row(first + group);
   for (; first < a.rows; first += step) {
     const int64_t row = first + group;
     const bool here = row < a.rows;
@@ -328,20 +328,6 @@ __global__ __launch_bounds__(1024) void block_norm_grad_kernel(BlockNormGradArgs
     if constexpr (kInLds) in_lds(k, j, i) = fmaf(u, v, in_lds(k, j, i));
     else sums[k][j][i] = fmaf(u, v, sums[k][j][i]);
   };
-#pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    if constexpr (kRoom) {
-      first_parameters(j);
-      next_parameters(j);
-    }
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        if constexpr (kInLds) in_lds(k, j, i) = 0.0f;
-        else sums[k][j][i] = 0.0f;
-      }
-  }
   const float inv_n = 1.0f / (float)a.n;
   struct Row {
     Elements<T, V> x[NV], g[NV], n[NV];
@@ -373,6 +359,20 @@ __global__ __launch_bounds__(1024) void block_norm_grad_kernel(BlockNormGradArgs
   if constexpr (kRoom) {
     ask_first(ahead, (int64_t)blockIdx.x * groups + group);
     ask_second(ahead, (int64_t)blockIdx.x * groups + group);
+  }
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    if constexpr (kRoom) {
+      first_parameters(j);
+      next_parameters(j);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        if constexpr (kInLds) in_lds(k, j, i) = 0.0f;
+        else sums[k][j][i] = 0.0f;
+      }
   }
   for (int64_t first = (int64_t)blockIdx.x * groups; first < a.rows; first += step) {
     const int64_t row = first + group;
@@ -518,6 +518,7 @@ __global__ __launch_bounds__(1024) void block_norm_sum_kernel(BlockNormGradArgs 
   const int lane = threadIdx.x & 15, group = threadIdx.x >> 4, c = blockIdx.x * 16 + lane;
   float s[4] = {};
   if (c < a.n)
+#pragma unroll 4
     for (int p = group; p < parts; p += 64)
 #pragma unroll
       for (int k = 0; k < 4; ++k) s[k] += a.part[((int64_t)p * 4 + k) * a.n + c];

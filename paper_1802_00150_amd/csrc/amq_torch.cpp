@@ -830,6 +830,14 @@ PyObject* linear_recurrence_backward(PyObject* const* a) {  // dhs, gate, x, h0,
   return tuple({a[9] == Py_None ? wrap(dg) : again(a[9]), a[10] == Py_None ? wrap(dx) : again(a[10]), h0 ? wrap(dh0) : none()});
 }
 
+// n entries of a vector from `at` on, as a tensor on the same storage.
+at::Tensor part_of(const at::Tensor& all, int64_t at, int64_t n) {
+  at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(all.storage()), all.key_set(), all.dtype());
+  t.unsafeGetTensorImpl()->set_sizes_contiguous({n});
+  t.unsafeGetTensorImpl()->set_storage_offset(at);
+  return t;
+}
+
 // The parameters of a joined norm: vectors of one type.
 struct Parameters {
   const at::Tensor& x;
@@ -901,15 +909,22 @@ PyObject* block_norm_backward(PyObject* const* a) {  // dy, dnormed, x, y, stats
     dg = make(x.sizes(), x.scalar_type(), x);
     rg = Rows(dg);
   }
-  // gradients of the parameters that are there (those of the second norm: zeros of a sum where dnormed is none)
+  // gradients of the parameters that are there (those of the second norm: zeros of a sum where dnormed is none), in one allocation
   const bool wanted[5] = {w != nullptr, b != nullptr, sc != nullptr, w2 != nullptr, next_bias};
   void* q[5] = {};
-  for (int i = 0; i < 5; ++i)
-    if (sums && wanted[i]) {
-      p[i] = make({r.n}, pt, x);
-      q[i] = p[i].data_ptr();
-    }
-  const bool any = q[0] || q[1] || q[2] || q[3] || q[4];
+  const int64_t count = sums ? wanted[0] + wanted[1] + wanted[2] + wanted[3] + wanted[4] : 0;
+  const bool any = count > 0;
+  if (any) {
+    const int64_t apart = (r.n + 63) & ~int64_t(63);
+    const at::Tensor all = make({count * apart}, pt, x);
+    int64_t at = 0;
+    for (int i = 0; i < 5; ++i)
+      if (wanted[i]) {
+        p[i] = part_of(all, at, r.n);
+        q[i] = p[i].data_ptr();
+        at += apart;
+      }
+  }
   Workspace ws(a[13], x, [&] { return any ? api.amq_block_norm_backward_workspace_bytes(r.rows, r.n) : 0; });
   const int residual_type = type_of(y), param_type = params.type();
   void* s = stream();

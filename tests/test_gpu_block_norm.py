@@ -276,3 +276,20 @@ def test_captured(amq):
         want = both()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out, want)), i
+
+
+def test_long_offsets(amq):
+    """Rows whose offsets pass 32 bits."""
+    x, h, g, p = case(15, 70, 66, TYPES[2])
+    params = {k: on(v) for k, v in p.items()}
+    step = (1 << 26) + 6
+    room = torch.zeros(69 * step + 5 * 66, dtype=x.dtype, device=DEV)
+    a, b, c, d, e = (room.as_strided((70, 66), (step, 1), i * 66) for i in range(5))
+    a.copy_(x), b.copy_(h), c.copy_(g)
+    want = amq.block_norm(on(x), on(h), gate=on(g), **params)
+    got = amq.block_norm(a, b, gate=c, out=d, out_normed=e, **params)
+    assert all(torch.equal(u, v) for u, v in zip(got, want))
+    dy, dn = on(rand(1, 70, 66).to(h.dtype)), on(rand(2, 70, 66).to(x.dtype))
+    plain = amq.block_norm_backward(dy, dn, on(x), want[0], want[2], gate=on(g), **params)
+    far = amq.block_norm_backward(dy, dn, a, d, want[2], gate=c, **params)
+    assert all(torch.equal(u, v) for u, v in zip(plain, far))

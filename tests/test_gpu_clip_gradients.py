@@ -188,3 +188,17 @@ def test_captured(amq):
         want = [amq.clip_gradients(tensors, 1.0, out=out)] + out
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want)), i
+
+
+def test_more_than_32_bits_of_entries(amq):
+    """All entries but a few are 2^-8: the sum of their squares is exact."""
+    n = (1 << 32) + 12345
+    t = torch.full((n,), 2.0 ** -8, dtype=BF16, device=DEV)
+    t[-1], t[(1 << 32) + 3] = 256.0, -512.0
+    want = math.sqrt((n - 2) * 2.0 ** -16 + 256.0 ** 2 + 512.0 ** 2)
+    out = torch.empty_like(t)
+    norm = float(amq.clip_gradients([t], want / 2, out=[out]))
+    assert abs(norm - want) <= 2 * U * want
+    # halves, but for the rounding of the limit and of the factor
+    assert bool((out[:1 << 32] - 2.0 ** -9).abs().max() <= 2.0 ** -9 * 2.0 ** -7) and abs(float(out[-1]) - 128) <= 1 and abs(float(out[(1 << 32) + 3]) + 256) <= 2
+    assert abs(float(out[(1 << 31) + 5]) - 2.0 ** -9) <= 2.0 ** -16

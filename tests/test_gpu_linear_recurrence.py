@@ -332,3 +332,49 @@ def test_long_offsets(amq):
     v.copy_(x)
     check(amq, gate, x, h0, "blend", views=(g, v))
     check_grad(amq, gate, x, h0, "blend", views=(g, v))
+
+
+@pytest.mark.parametrize("T,n", [((1 << 20) + 77, 2050), ((1 << 17) + 5, 17000)])
+def test_more_than_32_bits_of_entries(amq, T, n):
+    """Over 2^31 entries, with tiles in workgroups of their own and without: the sequence's end is that of its last steps alone, taken up from a state that
+    the forward pass left; the backward pass's first steps are those of the beginning alone, with the gradient that reaches them.  (Two folds of
+    the same maps in other places: the bound of the roundings behind that state.)"""
+    g = torch.Generator(device=DEV).manual_seed(1)
+    gate = torch.empty(T, 1, n, dtype=torch.bfloat16, device=DEV).normal_(generator=g)
+    x = torch.empty_like(gate).normal_(generator=g)
+    hs, last, states = amq.linear_recurrence(gate, x, states=True)
+    at = (T - 1) // 128 * 128
+    assert at * n > 1 << 31
+    for view in ((gate[at - 128:], x[at - 128:], states[at // 128 - 2]),):
+        tail, end, _ = amq.linear_recurrence(*view)
+        ref, tol, _ = recurrence64(view[0].cpu().double(), view[1].cpu().double(), view[2].cpu().double(), "blend")
+        assert_within(hs[at - 128:], ref, tol + half_ulp(torch.bfloat16) * ref.abs(), "hs")
+        assert_within(last, ref[-1], tol[-1], "h_last")
+    # the gradient of the last 300 steps' states, which reaches their beginning and no further than f decays
+    dhs = torch.zeros_like(gate)
+    dhs[-300:] = 1.0
+    dgate, dx, dh0 = amq.linear_recurrence_backward(dhs, gate, x, torch.zeros(1, n, device=DEV), states)
+    cut = at - 384
+    tail = amq.linear_recurrence_backward(dhs[cut:], gate[cut:], x[cut:], states[cut // 128 - 1], amq.linear_recurrence(gate[cut:], x[cut:], states[cut // 128 - 1], states=True)[2])
+    ref, tol = recurrence_grad64(dhs[cut:].cpu().double(), gate[cut:].cpu().double(), x[cut:].cpu().double(), states[cut // 128 - 1].cpu().double(),
+                                 torch.zeros(1, n, dtype=torch.float64), "blend")
+    for name, got, part, r, t in (("dgate", dgate, tail[0], ref[0], tol[0]), ("dx", dx, tail[1], ref[1], tol[1])):
+        # (the gradient decays below 2^-126, the least normal number of either type, where no rounding is relative)
+        t = t + half_ulp(torch.bfloat16) * r.abs() + 2.0 ** -126
+        assert_within(got[cut:], r, t, name)
+        assert_within(part, r, t, name + " of the part")
+    assert bool((dx[:cut - 4000] == 0).all())
+
+
+def test_many_at_once(amq):
+    """Launches whose workgroups wait for each other, on several streams, more of them than the card holds."""
+    cases = [[t.to(DEV) for t in case(i, 4000, 1, 512, torch.float32, "blend")] for i in range(4)]
+    want = [amq.linear_recurrence(*c)[1] for c in cases]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in cases], []
+    for _ in range(5):
+        for s, c in zip(streams, cases):
+            with torch.cuda.stream(s):
+                got.append(amq.linear_recurrence(*c)[1])
+    torch.cuda.synchronize()
+    assert all(torch.equal(g, want[i % 4]) for i, g in enumerate(got))

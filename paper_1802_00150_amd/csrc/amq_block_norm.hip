@@ -61,7 +61,19 @@ __device__ __forceinline__ void row_sum2(float& a, float& b, float (*slots)[2], 
   a = lane_of(v, 0);
   b = lane_of(v, 1);
 }
+// Sum over 16 or 32 lanes that share a row.
+template <int L>
+__device__ __forceinline__ float lanes_sum(float v) {
+  static_assert(L == 16 || L == 32, "lanes of a row");
+  v = v + dpp<0xB1>(v);  // quad_perm [1,0,3,2]
+  v += dpp<0x4E>(v);     // quad_perm [2,3,0,1]
+  v += dpp<0x124>(v);    // row_ror 4
+  v += dpp<0x128>(v);    // row_ror 8
+  return L == 32 ? add_16_away(v) : v;
+}
+template <int L>
 __device__ __forceinline__ float row_sum(float a, float (*slots)[2], int& turn, int first, int waves) {
+  if constexpr (L < 64) return lanes_sum<L>(a);
   float b = 0.0f;
   row_sum2(a, b, slots, turn, first, waves);
   return a;
@@ -178,16 +190,16 @@ __device__ __forceinline__ void again(Elements<T, V>& e) {
   }
 }
 
-constexpr int row_groups(int waves, int most) { return waves >= most ? 1 : most / waves; }
-
-// T: x, gate and normed; R: residual and y; P: parameters.  W waves per row, NV pieces of V entries per lane.
-template <typename T, typename R, typename P, int V, int W, int NV>
+// T: x, gate and normed; R: residual and y; P: parameters.  W waves per row (or L lanes of one wave, short rows sharing it), NV pieces of V
+// entries per lane.
+template <typename T, typename R, typename P, int V, int W, int NV, int L>
 __global__ __launch_bounds__(W > 4 ? W * 64 : 256) void block_norm_kernel(BlockNormArgs a) {
-  constexpr int kRows = row_groups(W, 4);
+  constexpr int kLanes = L < 64 ? L : W * 64, kRows = (W > 4 ? W * 64 : 256) / kLanes;
   __shared__ float slots[2 * 16][2];
   int turn = 0;
-  const int group = __builtin_amdgcn_readfirstlane(wave_id() / W), tid = (int)threadIdx.x - group * W * 64;
-  auto piece = [&](int j) __attribute__((always_inline)) { return Piece<V>(j, tid, a.n, W * 64); };
+  const int wave = L < 64 ? 0 : __builtin_amdgcn_readfirstlane(wave_id() / W * W);  // the row's first
+  const int group = L < 64 ? (int)threadIdx.x / L : wave / W, tid = (int)threadIdx.x - group * kLanes;
+  auto piece = [&](int j) __attribute__((always_inline)) { return Piece<V>(j, tid, a.n, kLanes); };
   const float inv_n = 1.0f / (float)a.n;
   Elements<T, V> rx[NV], rg[NV];
   Elements<R, V> rr[NV];
@@ -235,7 +247,7 @@ __global__ __launch_bounds__(W > 4 ? W * 64 : 256) void block_norm_kernel(BlockN
       }
     }
     fetch_row(row + step);
-    const float mean = row_sum(s, slots, turn, group * W, W) * inv_n;
+    const float mean = row_sum<L>(s, slots, turn, wave, W) * inv_n;
     s = 0.0f;
 #pragma unroll
     for (int j = 0; j < NV; ++j)
@@ -244,7 +256,7 @@ __global__ __launch_bounds__(W > 4 ? W * 64 : 256) void block_norm_kernel(BlockN
         x[j][i] -= mean;
         s = fmaf(piece(j).counts(i) ? x[j][i] : 0.0f, x[j][i], s);
       }
-    const float rstd = 1.0f / sqrtf(row_sum(s, slots, turn, group * W, W) * inv_n + a.eps);
+    const float rstd = 1.0f / sqrtf(row_sum<L>(s, slots, turn, wave, W) * inv_n + a.eps);
     s = 0.0f;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
@@ -257,7 +269,7 @@ __global__ __launch_bounds__(W > 4 ? W * 64 : 256) void block_norm_kernel(BlockN
     }
     float mean_y = 0.0f, rstd_y = 0.0f;
     if (a.normed) {
-      mean_y = row_sum(s, slots, turn, group * W, W) * inv_n;
+      mean_y = row_sum<L>(s, slots, turn, wave, W) * inv_n;
       s = 0.0f;
 #pragma unroll
       for (int j = 0; j < NV; ++j)
@@ -266,7 +278,7 @@ __global__ __launch_bounds__(W > 4 ? W * 64 : 256) void block_norm_kernel(BlockN
           y[j][i] -= mean_y;
           s = fmaf(piece(j).counts(i) ? y[j][i] : 0.0f, y[j][i], s);
         }
-      rstd_y = 1.0f / sqrtf(row_sum(s, slots, turn, group * W, W) * inv_n + a.eps);
+      rstd_y = 1.0f / sqrtf(row_sum<L>(s, slots, turn, wave, W) * inv_n + a.eps);
       if (here)
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
@@ -286,16 +298,24 @@ __global__ __launch_bounds__(W > 4 ? W * 64 : 256) void block_norm_kernel(BlockN
   }
 }
 
-// `waves` waves per row, as many rows in a workgroup as 16 waves have room for.
-template <typename T, typename R, typename P, int V, int NV>
+// `waves` waves per row (or L lanes of one wave), as many rows in a workgroup as 16 waves have room for.
+template <typename T, typename R, typename P, int V, int NV, int L>
 __global__ __launch_bounds__(1024) void block_norm_grad_kernel(BlockNormGradArgs a, int waves) {
   __shared__ float slots[2 * 16][2];
   // [group][sum][j][i][thread]: consecutive lanes on consecutive banks
   constexpr bool kInLds = NV == 2;  // the sums themselves lie there (one row per workgroup), for want of registers
   __shared__ float shared_sums[(kInLds ? 4 : NV == 1 ? 2 : 1) * (NV > 2 ? 1 : 1024 * NV * V)];
   int turn = 0;
-  const int threads = waves * 64, groups = blockDim.x / threads, entries = threads * NV * V;
-  const int group = __builtin_amdgcn_readfirstlane(wave_id() / waves), tid = (int)threadIdx.x - group * threads;
+  const int threads = L < 64 ? L : waves * 64, groups = blockDim.x / threads, entries = threads * NV * V;
+  const int group = L < 64 ? (int)threadIdx.x / L : __builtin_amdgcn_readfirstlane(wave_id() / waves), tid = (int)threadIdx.x - group * threads;
+  auto row_sums = [&](float& u, float& v) __attribute__((always_inline)) {
+    if constexpr (L < 64) {
+      u = lanes_sum<L>(u);
+      v = lanes_sum<L>(v);
+    } else {
+      row_sum2(u, v, slots, turn, group * waves, waves);
+    }
+  };
   auto piece = [&](int j) __attribute__((always_inline)) { return Piece<V>(j, tid, a.n, threads); };
   // scale x weight, scale x bias, next_weight; 0 where an entry does not count, so that sums along the row leave it out.  With one piece a lane
   // has room for them and for a row ahead; with more it reads them again for every row (from L2).
@@ -413,7 +433,7 @@ __global__ __launch_bounds__(1024) void block_norm_grad_kernel(BlockNormGradArgs
       if constexpr (!kRoom)
 #pragma unroll
         for (int j = 0; j < NV; ++j) again(now.y[j]), again(now.n[j]);
-      row_sum2(s, q, slots, turn, group * waves, waves);
+      row_sums(s, q);
       s *= inv_n;
       q *= inv_n;
       if (here)
@@ -467,7 +487,7 @@ __global__ __launch_bounds__(1024) void block_norm_grad_kernel(BlockNormGradArgs
     if constexpr (!kRoom)
 #pragma unroll
       for (int j = 0; j < NV; ++j) again(now.x[j]);
-    row_sum2(s, q, slots, turn, group * waves, waves);
+    row_sums(s, q);
     s *= inv_n;
     q *= inv_n;
     if (here)
@@ -546,20 +566,21 @@ __global__ __launch_bounds__(1024) void block_norm_sum_kernel(BlockNormGradArgs 
   }
 }
 
-// Forward: waves per row and pieces per lane.  16 entries per lane at most (one wave up to 1024).  Few rows go to four waves each from 512
-// entries on, where the row's latency counts.
+// Forward: waves per row, pieces per lane, and lanes per row.  16 entries per lane at most (one wave up to 1024).  Few rows go to four waves each
+// from 512 entries on, where the row's latency counts; short ones share a wave (35000 x 64 bfloat16 29 us with a wave each, backward 30).
 struct Shape {
-  int waves, pieces;
+  int waves, pieces, lanes;
 };
 constexpr int kPerLane = 16;
 template <int V>
 Shape shape_of(int64_t rows, int n) {
-  if constexpr (V == 1) return {1, 1};  // rows of less than 16 bytes
+  if (n <= 16 * V) return {1, 1, 16};
+  if (n <= 32 * V) return {1, 1, 32};
   for (int p = 1; p * V <= kPerLane; p *= 2)
-    if (n <= 64 * p * V && (rows > 512 || n <= 512)) return {1, p};
+    if (n <= 64 * p * V && (rows > 512 || n <= 512)) return {1, p, 64};
   for (int p = 1; p * V <= kPerLane; p *= 2)
-    if (n <= 256 * p * V) return {4, p};
-  return {n <= 512 * kPerLane ? 8 : 16, kPerLane / V};
+    if (n <= 256 * p * V) return {4, p, 64};
+  return {n <= 512 * kPerLane ? 8 : 16, kPerLane / V, 64};
 }
 
 template <typename F>
@@ -571,18 +592,21 @@ hipError_t with_types(int type, int residual, int param, F f) {
 }
 template <int V, typename F>
 hipError_t with_shape(Shape h, F f) {
-#define AMQ_SHAPE(W, NV) \
-  if (h.waves == W && h.pieces == NV) return f(std::integral_constant<int, V>(), std::integral_constant<int, W>(), std::integral_constant<int, NV>())
-  AMQ_SHAPE(1, 1);
-  if constexpr (V > 1) {
+#define AMQ_SHAPE(W, NV, L)                                     \
+  if (h.waves == W && h.pieces == NV && h.lanes == L)           \
+  return f(std::integral_constant<int, V>(), std::integral_constant<int, W>(), std::integral_constant<int, NV>(), std::integral_constant<int, L>())
+  AMQ_SHAPE(1, 1, 16);
+  if constexpr (V > 1) {  // (rows of less than 16 bytes have pieces of one entry, and 16 lanes)
     constexpr int most = kPerLane / V;
-    AMQ_SHAPE(1, 2);
-    if constexpr (most >= 4) AMQ_SHAPE(1, 4);
-    AMQ_SHAPE(4, 1);
-    AMQ_SHAPE(4, 2);
-    if constexpr (most >= 4) AMQ_SHAPE(4, 4);
-    AMQ_SHAPE(8, most);
-    AMQ_SHAPE(16, most);
+    AMQ_SHAPE(1, 1, 32);
+    AMQ_SHAPE(1, 1, 64);
+    AMQ_SHAPE(1, 2, 64);
+    if constexpr (most >= 4) AMQ_SHAPE(1, 4, 64);
+    AMQ_SHAPE(4, 1, 64);
+    AMQ_SHAPE(4, 2, 64);
+    if constexpr (most >= 4) AMQ_SHAPE(4, 4, 64);
+    AMQ_SHAPE(8, most, 64);
+    AMQ_SHAPE(16, most, 64);
   }
 #undef AMQ_SHAPE
   return hipErrorInvalidValue;
@@ -593,11 +617,17 @@ hipError_t with_shape(Shape h, F f) {
 constexpr int kGradPiece = 4;
 template <typename F>
 hipError_t with_grad_pieces(int n, F f) {
-  if (n < kGradPiece) return f(std::integral_constant<int, 1>(), std::integral_constant<int, 1>());
+  const std::integral_constant<int, 1> one;
   const std::integral_constant<int, kGradPiece> v;
-  if (n <= 1024 * kGradPiece) return f(v, std::integral_constant<int, 1>());
-  if (n <= 2048 * kGradPiece) return f(v, std::integral_constant<int, 2>());
-  return f(v, std::integral_constant<int, 4>());
+  const std::integral_constant<int, 16> short_row;
+  const std::integral_constant<int, 32> half;
+  const std::integral_constant<int, 64> whole;
+  if (n < kGradPiece) return f(one, one, short_row);
+  if (n <= 16 * kGradPiece) return f(v, one, short_row);
+  if (n <= 32 * kGradPiece) return f(v, one, half);
+  if (n <= 1024 * kGradPiece) return f(v, one, whole);
+  if (n <= 2048 * kGradPiece) return f(v, std::integral_constant<int, 2>(), whole);
+  return f(v, std::integral_constant<int, 4>(), whole);
 }
 
 // Rows that a grid of at most `most` workgroups takes at a time, spread evenly over its rounds.
@@ -616,15 +646,15 @@ int block_norm_grad_parts(int64_t rows, int) { return (int)(rows < kMostParts ? 
 hipError_t launch_block_norm(const BlockNormArgs& a, hipStream_t s) {
   return with_types(a.type, a.residual_type, a.param_type, [&](auto t, auto r, auto p) {
     using T = decltype(t);
-    auto f = [&](auto v, auto w, auto nv) {
-      constexpr int W = decltype(w)::value, kRows = row_groups(W, 4);
+    auto f = [&](auto v, auto w, auto nv, auto l) {
+      constexpr int W = decltype(w)::value, L = decltype(l)::value, kThreads = W > 4 ? W * 64 : 256, kRows = kThreads / (L < 64 ? L : W * 64);
       const int64_t tasks = (a.rows + kRows - 1) / kRows;
-      block_norm_kernel<T, decltype(r), decltype(p), decltype(v)::value, W, decltype(nv)::value>
-          <<<dim3((unsigned)even_blocks(tasks, W >= 8 ? 512 : 1024)), dim3(kRows * W * 64), 0, s>>>(a);
+      block_norm_kernel<T, decltype(r), decltype(p), decltype(v)::value, W, decltype(nv)::value, L>
+          <<<dim3((unsigned)even_blocks(tasks, W >= 8 ? 512 : 1024)), dim3(kThreads), 0, s>>>(a);
       return hipGetLastError();
     };
     constexpr int V = kPer16<T>;
-    return a.n < V ? with_shape<1>(shape_of<1>(a.rows, a.n), f) : with_shape<V>(shape_of<V>(a.rows, a.n), f);
+    return a.n < V ? with_shape<1>({1, 1, 16}, f) : with_shape<V>(shape_of<V>(a.rows, a.n), f);
   });
 }
 
@@ -636,14 +666,14 @@ hipError_t launch_block_norm_grad(const BlockNormGradArgs& a0, hipStream_t s) {
     using T = decltype(t);
     using P = decltype(p);
     int64_t parts = 0;
-    const hipError_t e = with_grad_pieces(a.n, [&](auto v, auto nv) {
-      constexpr int V = decltype(v)::value, NV = decltype(nv)::value;
+    const hipError_t e = with_grad_pieces(a.n, [&](auto v, auto nv, auto l) {
+      constexpr int V = decltype(v)::value, NV = decltype(nv)::value, L = decltype(l)::value, kPerWave = 64 / L;
       const int waves = (a.n + 64 * V * NV - 1) / (64 * V * NV);
-      // few rows: one each for as many compute units as there are
-      const int64_t share = (a.rows + kMostParts - 1) / kMostParts;
-      const int groups = share < 16 / waves ? (int)share : 16 / waves;
+      // few rows: one each (or a wave's) for as many compute units as there are
+      const int64_t share = (a.rows + kMostParts * kPerWave - 1) / (kMostParts * kPerWave);
+      const int groups = (share < 16 / waves ? (int)share : 16 / waves) * kPerWave;
       parts = even_blocks((a.rows + groups - 1) / groups, kMostParts);
-      block_norm_grad_kernel<T, decltype(r), P, V, NV><<<dim3((unsigned)parts), dim3(groups * waves * 64), 0, s>>>(a, waves);
+      block_norm_grad_kernel<T, decltype(r), P, V, NV, L><<<dim3((unsigned)parts), dim3(L < 64 ? groups * L : groups * waves * 64), 0, s>>>(a, waves);
       return hipGetLastError();
     });
     if (e != hipSuccess || !sums) return e;

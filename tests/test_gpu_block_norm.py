@@ -9,7 +9,7 @@ pytestmark = pytest.mark.gpu
 
 # every form: rows of less than 16 bytes, a wave per row, four waves, eight, sixteen; odd lengths, rows that share no alignment, few and many rows
 SIZES = [(1, 2), (5, 3), (3, 7), (9, 8), (7, 64), (33, 129), (700, 300), (1030, 65), (2, 512), (3, 513), (600, 513), (2, 1024), (515, 1024), (520, 1025),
-         (600, 2047), (3, 4097), (2, 8192), (3, 8193), (2, 16384)]
+         (600, 2047), (1, 16), (1300, 17), (70, 100), (2050, 128), (900, 130), (1111, 256), (3, 4097), (2, 8192), (3, 8193), (2, 16384)]
 TYPES = [(torch.float32, torch.float32, torch.float32)] + [(t, r, p) for t in DTYPES[1:] for r in (t, torch.float32) for p in (t, torch.float32)]
 EPS = 1e-5
 

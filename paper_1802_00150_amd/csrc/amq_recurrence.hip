@@ -735,14 +735,15 @@ int waves_of(int64_t steps, bool even) {
 int64_t groups_of(int64_t batch, int64_t n, int V) { return batch * ((n + 64 * V - 1) / (64 * V)); }
 int64_t tiles_of(int64_t steps, int tile) { return (steps + tile - 1) / tile; }
 
-// The form with the least time, by measurement (us; g groups of 64 channels, t tiles).  One workgroup per group takes 3 + c t while the card
-// holds all groups at once; a workgroup per tile 9 + e t g / 256, of which 4 are the clearing of the marks.  Steps x channels, one form and
-// the other: 16-bit types 1000 x 4096 23.5 and 14.2, 1000 x 8192 24.1 and 21.1, 1000 x 12288 24.7 and 27.1; backward 34 and 21, 35 and 31, 39 and 43; float
-// 1000 x 4096 22 and 19, 2000 x 8192 50 and 45, 1000 x 12288 31 and 37; backward 2000 x 8192 95 and 73, 1000 x 12288 53 and 55, 300 x 8192 14.8 and 18.9.
+// The form with the least time, by measurement (us; g groups of 64 channels, t tiles of 128 steps).  One workgroup per group takes about 3 + c t for
+// every 256 of them, which is what the card holds at once; a workgroup per tile 9 + e t g / 256, of which 4 are the clearing of the marks.  Steps x
+// channels, one form and the other: 16-bit types 1000 x 4096 23.5 and 14.2, 1000 x 8192 24.1 and 21.1, 1000 x 12288 24.7 and 27.1, 3000 x 16500 137 and
+// 91; backward 34 and 21, 35 and 31, 39 and 43, 257 and 162; float 1000 x 4096 22 and 19, 2000 x 8192 50 and 45, 1000 x 12288 31 and 37; backward
+// 2000 x 8192 95 and 73, 1000 x 12288 53 and 55, 300 x 8192 14.8 and 18.9, 1000 x 20480 110 and 88.
 bool splits(int64_t batch, int64_t n, int64_t steps, bool wide, bool backward) {
-  const int64_t g = groups_of(batch, n, 1), t = tiles_of(steps, kTile);
+  const int64_t g = groups_of(batch, n, 1), t = tiles_of(steps, kTile), rounds = (g + 255) / 256;
   const double c = wide ? backward ? 5.5 : 2.8 : backward ? 4.3 : 2.6, e = wide ? backward ? 8.0 : 4.6 : backward ? 5.5 : 2.95;
-  return t > 1 && g < 256 && (double)t * (c - e * (double)g / 256) > 6.0;
+  return t > 1 && (double)t * (c * (double)rounds - e * (double)g / 256) > 6.0;
 }
 // Channels of a lane: two of 16 bits where a workgroup walks over tiles forward and groups of 128 channels still fill the card
 // (1000 x 32768 entries 41 us, with one 50; 2000 x 16384 65 and 48); one otherwise (35 x 262144 backward 21.2, with two 23.8).

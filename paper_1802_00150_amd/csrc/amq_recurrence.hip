@@ -98,8 +98,8 @@ struct Lane {
 
 // ---- Tiles of one sequence in workgroups of their own.
 //
-// Tiles are taken in the order of a counter, those that others wait for first, so that a workgroup waits only for ones that have begun
-// (and those for earlier ones): every wait ends, whatever part of the grid has room at a time.  A tile leaves {A, B} of every channel, raises its mark to 1,
+// Tiles are taken in the order of counters, those that others wait for first, so that a workgroup waits only
+// for ones that have begun (and those for earlier ones): every wait ends, whatever part of the grid has room at a time.  A tile leaves {A, B} of every channel, raises its mark to 1,
 // and once it knows the state that it starts in leaves the one it ends in and raises it to 2.  The one it starts in is that of the
 // nearest earlier tile with mark 2 folded through the maps between: the same operations in the same order wherever that one is,
 // so results do not depend on the order of execution.  Up to 64 tiles back are looked at.
@@ -189,13 +189,14 @@ __device__ __forceinline__ void end_of(const Chain& c, int64_t tile, float (&h)[
 #pragma unroll
   for (int j = 0; j < V; ++j) h[j] = there ? __uint_as_float(look(c.ends + (tile * 64 + lane_id()) * V + j)) : __builtin_nanf("");
 }
-// What a launch with workgroups of their own keeps in the workspace: the counter, then the marks (both cleared first), maps and ends.
+// What a launch with workgroups of their own keeps in the workspace: the counters, then the marks (both cleared first), maps and ends.
+constexpr uint32_t kCounters = 4, kCounterWords = 32;  // a cache line each
 struct SplitLayout {
   int64_t groups, tiles;
   size_t marks, maps, ends, bytes;
   SplitLayout(int64_t g, int64_t t) : groups(g), tiles(t) {
     constexpr int channels = 64;
-    marks = 256;
+    marks = sizeof(uint32_t) * kCounters * kCounterWords;
     maps = (marks + sizeof(uint32_t) * g * t + 255) & ~size_t(255);
     ends = maps + sizeof(uint64_t) * g * t * channels;
     bytes = (ends + sizeof(uint32_t) * g * t * channels + 255) & ~size_t(255);
@@ -207,17 +208,24 @@ struct Split {
   uint64_t* maps;
   uint32_t* ends;
   int64_t tiles;
-  uint32_t groups;
+  uint32_t groups, kinds;
 };
 template <int V>
 __device__ __forceinline__ Chain chain_of(const Split& s, int64_t group) {
   return {s.marks + group * s.tiles, s.maps + group * s.tiles * 64 * V, s.ends + group * s.tiles * 64 * V};
 }
-// The number of a tile that nobody has begun, the same in all threads.
-__device__ __forceinline__ uint32_t take_tile(const Split& s, uint32_t& shared) {
-  if (threadIdx.x == 0) shared = __hip_atomic_fetch_add(s.counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+// A tile that nobody has begun, by its order in the chain of its group, the same in all threads; false if there is none.  Every
+// `kinds`th group shares a counter: four of them (1000 x 8192 bfloat16 18.0 us, with one for all 22.1; 4001 x 2100 float 28.4 and
+// 31.1; backward 1000 x 4096 bfloat16 17.1 and 21.3; with eight, whose groups each keep to one die, 32768 x 1024 takes 61 us and not
+// 55.6), but one where a row of tiles fills the card (3000 x 16500 90 us, with four 96).
+__device__ __forceinline__ bool take_tile(const Split& s, uint32_t& shared, uint32_t& order, uint32_t& group) {
+  const uint32_t kinds = s.kinds, kind = blockIdx.x % kinds;
+  if (threadIdx.x == 0) shared = __hip_atomic_fetch_add(s.counter + kind * kCounterWords, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   __syncthreads();
-  return __builtin_amdgcn_readfirstlane(shared);
+  const uint32_t now = __builtin_amdgcn_readfirstlane(shared), of_kind = (s.groups - kind + kinds - 1) / kinds;
+  order = now / of_kind;
+  group = (now - order * of_kind) * kinds + kind;
+  return order < (uint32_t)s.tiles;
 }
 __global__ __launch_bounds__(256) void split_clear_kernel(uint32_t* p, int64_t words) {
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < words; i += (int64_t)gridDim.x * 256) p[i] = 0;
@@ -412,7 +420,8 @@ __global__ __launch_bounds__(64 * kTileWaves, 8) void recurrence_tiles_kernel(Re
   __shared__ int found;
   auto maps = reinterpret_cast<float(*)[2][64 * V]>(stage);  // [kTileWaves]
   const int w = __builtin_amdgcn_readfirstlane(wave_id()), lane = lane_id();
-  const uint32_t now = take_tile(split, number), tile = now / split.groups, group = now - tile * split.groups;
+  uint32_t tile, group;
+  if (!take_tile(split, number, tile, group)) return;
   const Group<V, RecurrenceArgs> at(a, group);
   const int64_t t0 = (int64_t)tile * kLongTile + w * K;
   const Chain chain = chain_of<V>(split, group);
@@ -639,7 +648,8 @@ __global__ __launch_bounds__(64 * kTileWaves, 8) void recurrence_grad_tiles_kern
   auto maps = reinterpret_cast<float(*)[3][64 * V]>(stage);  // [kTileWaves]
   const int w = __builtin_amdgcn_readfirstlane(wave_id()), lane = lane_id();
   const bool mine = w == kTileWaves - 1;
-  const uint32_t now = take_tile(split, number), turn = now / split.groups, group = now - turn * split.groups;
+  uint32_t turn, group;
+  if (!take_tile(split, number, turn, group)) return;
   const int64_t tile = split.tiles - 1 - turn, t0 = tile * kTile + w * kSpan;
   const Group<V, RecurrenceGradArgs> at(a, group);
   if (tile * kTile >= at.length) {  // behind the entry's end
@@ -735,25 +745,30 @@ int waves_of(int64_t steps, bool even) {
 int64_t groups_of(int64_t batch, int64_t n, int V) { return batch * ((n + 64 * V - 1) / (64 * V)); }
 int64_t tiles_of(int64_t steps, int tile) { return (steps + tile - 1) / tile; }
 
-// The form with the least time, by measurement (us; g groups of 64 channels, t tiles of 128 steps).  One workgroup per group takes about 3 + c t for
-// every 256 of them, which is what the card holds at once; a workgroup per tile 9 + e t g / 256, of which 4 are the clearing of the marks.  Steps x
-// channels, one form and the other: 16-bit types 1000 x 4096 23.5 and 14.2, 1000 x 8192 24.1 and 21.1, 1000 x 12288 24.7 and 27.1, 3000 x 16500 137 and
-// 91; backward 34 and 21, 35 and 31, 39 and 43, 257 and 162; float 1000 x 4096 22 and 19, 2000 x 8192 50 and 45, 1000 x 12288 31 and 37; backward
-// 2000 x 8192 95 and 73, 1000 x 12288 53 and 55, 300 x 8192 14.8 and 18.9, 1000 x 20480 110 and 88.
-bool splits(int64_t batch, int64_t n, int64_t steps, bool wide, bool backward) {
-  const int64_t g = groups_of(batch, n, 1), t = tiles_of(steps, kTile), rounds = (g + 255) / 256;
-  const double c = wide ? backward ? 5.5 : 2.8 : backward ? 4.3 : 2.6, e = wide ? backward ? 8.0 : 4.6 : backward ? 5.5 : 2.95;
-  return t > 1 && (double)t * (c * (double)rounds - e * (double)g / 256) > 6.0;
-}
 // Channels of a lane: two of 16 bits where a workgroup walks over tiles forward and groups of 128 channels still fill the card
 // (1000 x 32768 entries 41 us, with one 50; 2000 x 16384 65 and 48); one otherwise (35 x 262144 backward 21.2, with two 23.8).
 bool two_channels(int64_t batch, int64_t n) { return n % 2 == 0 && groups_of(batch, n, 2) >= 256; }
+
+// The form with the least time, by measurement.  Per 128 steps a workgroup per group takes c0 us and all 256 that the card holds at once c0 + c1; a
+// workgroup per tile e for 256 groups, and 6.7 us more for clearing the marks, the second launch and the chain.  Steps x channels, a workgroup per
+// group and one per tile: 16-bit types 300 x 1024 9.5 and 11.0, 500 x 1024 11.7 and 10.2, 1000 x 8192 22.8 and 18.0, 1000 x 12288 22.9 and 23.3,
+// 3000 x 12288 65 and 55, 3000 x 16384 70 and 72, 3000 x 16500 137 and 90; float 1000 x 4096 20.2 and 16.7, 1000 x 12288 30.4 and 33.9; backward
+// 200 x 1024 10.2 and 11.5, 1000 x 1024 33 and 12, 1000 x 16384 44 and 52, 3000 x 12288 121 and 101, float 1000 x 24576 117 and 102.
+bool splits(int64_t batch, int64_t n, int64_t steps, bool wide, bool backward) {
+  const bool pairs = !wide && !backward && two_channels(batch, n);
+  const double c0 = pairs ? 2.6 : wide ? backward ? 3.5 : 2.05 : backward ? 3.85 : 2.4;
+  const double c1 = pairs ? 2.4 : wide ? backward ? 5.0 : 2.5 : backward ? 1.5 : 0.6;
+  const double e = wide ? backward ? 7.8 : 4.6 : backward ? 5.2 : 2.7;
+  const int64_t g = groups_of(batch, n, pairs ? 2 : 1), last = g % 256;
+  const double one = (double)(g / 256) * (c0 + c1) + (last ? c0 + c1 * (double)last / 256 : 0.0);
+  return steps > kTile && (double)steps / kTile * (one - e * (double)groups_of(batch, n, 1) / 256) > 6.7;
+}
 
 hipError_t split_of(int64_t groups, int64_t tiles, void* ws, hipStream_t s, Split& out) {
   const SplitLayout l(groups, tiles);
   char* p = static_cast<char*>(ws);
   out = {reinterpret_cast<uint32_t*>(p), reinterpret_cast<uint32_t*>(p + l.marks), reinterpret_cast<uint64_t*>(p + l.maps),
-         reinterpret_cast<uint32_t*>(p + l.ends), tiles, (uint32_t)groups};
+         reinterpret_cast<uint32_t*>(p + l.ends), tiles, (uint32_t)groups, groups >= 256 ? 1u : groups < kCounters ? (uint32_t)groups : kCounters};
   const int64_t words = (int64_t)(l.maps / sizeof(uint32_t));
   split_clear_kernel<<<dim3((unsigned)(words / 1024 < 256 ? words / 1024 + 1 : 256)), dim3(256), 0, s>>>(out.counter, words);
   return hipGetLastError();
@@ -764,7 +779,9 @@ hipError_t launch_tiles(const A& a, int tile, hipStream_t s, F kernel) {
   Split split;
   const hipError_t e = split_of(groups, tiles_of(a.steps, tile), a.ws, s, split);
   if (e != hipSuccess) return e;
-  kernel<<<dim3((unsigned)(groups * split.tiles)), dim3(64 * kTileWaves), 0, s>>>(a, split);
+  // as many workgroups for every counter as the one with the most tiles needs
+  const int64_t most = (groups + split.kinds - 1) / split.kinds * split.tiles;
+  kernel<<<dim3((unsigned)(split.kinds * most)), dim3(64 * kTileWaves), 0, s>>>(a, split);
   return hipGetLastError();
 }
 template <typename A, typename F>

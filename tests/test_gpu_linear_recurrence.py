@@ -92,7 +92,7 @@ def test_sizes(amq, T, B, n, mode, dtype):
     check_grad(amq, gate, x, h0, mode, what=what)
 
 
-@pytest.mark.parametrize("T,B,n", [(1, 8, 3), (7, 8, 64), (35, 8, 130), (128, 8, 2), (129, 8, 65), (400, 9, 100), (1500, 8, 33)])
+@pytest.mark.parametrize("T,B,n", [(1, 8, 3), (7, 8, 64), (35, 8, 130), (128, 8, 2), (129, 8, 65), (400, 9, 100), (1500, 8, 33), (300, 260, 70), (140, 300, 128)])
 @pytest.mark.parametrize("mode", MODES)
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_lengths(amq, T, B, n, mode, dtype):

@@ -6,14 +6,18 @@
 //
 // About 30 vector operations per entry forward and 50 backward (exponential and reciprocal count four each), against 6 and 10 bytes
 // (16-bit types): bound by memory once enough is under way, by latency for few entries.  A step is an affine map of the
-// state, so time is split: the kSpan steps of a wave are read at once, turned into one map (factor A, offset B) from a zero state, the waves
+// state, so time is split: the 8 steps of a wave are read at once, turned into one map (factor A, offset B) from a zero state, the waves
 // of a workgroup exchange those through LDS, every wave folds the ones before it onto the state and replays its steps, which are still
 // in registers, from the state they really start in.  So inputs are read once, and the results' error is that of steps one after the
-// other but for the folds'.  A tile is up to 16 waves of 8 steps = 128 steps of 64 lanes of V channels.
+// other but for the folds'.  A tile is up to 16 waves of 8 steps = 128 steps of 64 channels (128 where a lane has two).
 //
-// With channels enough for the card a workgroup walks over the tiles of its channels.  Otherwise every tile has a workgroup: it leaves its
-// map in memory, looks back for the nearest tile whose end state is there, folds the maps between and leaves its own end state ("Tiles of
-// one sequence" below).
+// With channels enough for the card a workgroup walks over the tiles of its channels.  Otherwise every tile (of 256 steps forward) has a
+// workgroup: it leaves its map in memory, looks back for the nearest tile whose end state is there, folds the maps between and leaves its
+// own end state ("Tiles of one sequence" below).
+//
+// Measured (steps x channels; a large copy 5.1 TB/s): 2000 x 16384 float 78 us, 5.05 TB/s; 1000 x 32768 bfloat16 40 us, 4.9; 35 x 262144
+// backward 21.4, 4.4; long sequences with the chain 32768 x 1024 bfloat16 56, 3.6; 4001 x 2100 float 28, 3.6, backward 50, 3.4;
+// 2000 x 8192 float backward 72, 4.6.
 //
 // The backward pass takes h_{t-1} in full precision from the states that the forward pass leaves in front of every 128th
 // step (4 / 128 bytes per entry instead of the 2 of reading rounded states): each tile replays the recurrence from there.
@@ -99,15 +103,15 @@ struct Lane {
 // ---- Tiles of one sequence in workgroups of their own.
 //
 // Tiles are taken in the order of counters, those that others wait for first, so that a workgroup waits only
-// for ones that have begun (and those for earlier ones): every wait ends, whatever part of the grid has room at a time.  A tile leaves {A, B} of every channel, raises its mark to 1,
-// and once it knows the state that it starts in leaves the one it ends in and raises it to 2.  The one it starts in is that of the
-// nearest earlier tile with mark 2 folded through the maps between: the same operations in the same order wherever that one is,
-// so results do not depend on the order of execution.  Up to 64 tiles back are looked at.
+// for ones that have begun (and those for earlier ones): every wait ends, whatever part of the grid has room at a time.  A tile leaves
+// {A, B} of every channel, raises its mark to 1, and once it knows the state that it starts in leaves the one it ends in and raises it
+// to 2.  The one it starts in is that of the nearest earlier tile with mark 2 folded through the maps between: the same operations in
+// the same order wherever that one is, so results do not depend on the order of execution.  Up to 64 tiles back are looked at.
 // Values go past the caches of the chip's dies as relaxed atomics of device scope; a mark is written when its values have arrived.
 struct Chain {
-  uint32_t* marks;    // [tiles]
-  uint64_t* maps;     // [tiles][64 V]
-  uint32_t* ends;     // [tiles][64 V]
+  uint32_t* marks;  // [tiles]
+  uint64_t* maps;   // [tiles][64]
+  uint32_t* ends;   // [tiles][64]
 };
 constexpr unsigned kPollLimit = 1u << 22;  // (seconds; a workgroup that gave up would leave NaN)
 
@@ -117,18 +121,13 @@ __device__ __forceinline__ uint32_t look(const uint32_t* p) { return __hip_atomi
 __device__ __forceinline__ uint64_t look(const uint64_t* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 __device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
-template <int V>
-__device__ __forceinline__ void leave_map(const Chain& c, int64_t tile, const float (&A)[V], const float (&B)[V]) {
-#pragma unroll
-  for (int j = 0; j < V; ++j)
-    leave(c.maps + (tile * 64 + lane_id()) * V + j, (uint64_t)__float_as_uint(B[j]) << 32 | __float_as_uint(A[j]));
+__device__ __forceinline__ void leave_map(const Chain& c, int64_t tile, float A, float B) {
+  leave(c.maps + tile * 64 + lane_id(), (uint64_t)__float_as_uint(B) << 32 | __float_as_uint(A));
   arrived();
   if (lane_id() == 0) leave(c.marks + tile, 1u);
 }
-template <int V>
-__device__ __forceinline__ void leave_end(const Chain& c, int64_t tile, const float (&h)[V]) {
-#pragma unroll
-  for (int j = 0; j < V; ++j) leave(c.ends + (tile * 64 + lane_id()) * V + j, __float_as_uint(h[j]));
+__device__ __forceinline__ void leave_end(const Chain& c, int64_t tile, float h) {
+  leave(c.ends + tile * 64 + lane_id(), __float_as_uint(h));
 }
 __device__ __forceinline__ void mark_end(const Chain& c, int64_t tile) {
   arrived();
@@ -137,8 +136,7 @@ __device__ __forceinline__ void mark_end(const Chain& c, int64_t tile) {
 // The state that tile > 0 starts in, for one wave: it polls the marks, all waves of the workgroup bring the maps between to LDS, and it
 // folds them.  (One wave that read up to 63 maps by itself was most of the time of a long sequence.)
 constexpr int kWindow = 64;
-template <int V>
-__device__ __forceinline__ void look_back(const Chain& c, int64_t tile, uint64_t (*stage)[64 * V], int& found, int w, bool mine, float (&h)[V]) {
+__device__ __forceinline__ void look_back(const Chain& c, int64_t tile, uint64_t (*stage)[64], int& found, int w, bool mine, float& h) {
   const int l = lane_id();
   if (mine) {
     int back = -1;  // the nearest tile whose end is known, and all between have left their maps
@@ -158,36 +156,28 @@ __device__ __forceinline__ void look_back(const Chain& c, int64_t tile, uint64_t
   }
   lds_barrier();  // (and what the stage held has been read)
   const int back = __builtin_amdgcn_readfirstlane(found);
-  if (mine)
-#pragma unroll
-    for (int j = 0; j < V; ++j) h[j] = back < 0 ? __builtin_nanf("") : __uint_as_float(look(c.ends + ((tile - 1 - (back < 0 ? 0 : back)) * 64 + l) * V + j));
+  if (mine) h = back < 0 ? __builtin_nanf("") : __uint_as_float(look(c.ends + (tile - 1 - (back < 0 ? 0 : back)) * 64 + l));
 #pragma unroll
   for (int i = 0; i < kWindow / kTileWaves; ++i) {
     const int u = w + i * kTileWaves;
-    if (u < back)
-#pragma unroll
-      for (int j = 0; j < V; ++j) stage[u][l * V + j] = look(c.maps + ((tile - back + u) * 64 + l) * V + j);
+    if (u < back) stage[u][l] = look(c.maps + (tile - back + u) * 64 + l);
   }
   lds_barrier();
   if (mine)
 #pragma unroll 8
-    for (int u = 0; u < back; ++u)
-#pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const uint64_t m = stage[u][l * V + j];
-        h[j] = fmaf(__uint_as_float((uint32_t)m), h[j], __uint_as_float((uint32_t)(m >> 32)));
-      }
+    for (int u = 0; u < back; ++u) {
+      const uint64_t m = stage[u][l];
+      h = fmaf(__uint_as_float((uint32_t)m), h, __uint_as_float((uint32_t)(m >> 32)));
+    }
 }
 // One wave: the state behind a tile, once it is there.
-template <int V>
-__device__ __forceinline__ void end_of(const Chain& c, int64_t tile, float (&h)[V]) {
+__device__ __forceinline__ float end_of(const Chain& c, int64_t tile) {
   bool there = false;
   for (unsigned polls = 0; polls < kPollLimit && !there; ++polls) {
     there = __ballot(look(c.marks + tile) == 2u) != 0;
     if (!there) __builtin_amdgcn_s_sleep(8);
   }
-#pragma unroll
-  for (int j = 0; j < V; ++j) h[j] = there ? __uint_as_float(look(c.ends + (tile * 64 + lane_id()) * V + j)) : __builtin_nanf("");
+  return there ? __uint_as_float(look(c.ends + tile * 64 + lane_id())) : __builtin_nanf("");
 }
 // What a launch with workgroups of their own keeps in the workspace: the counters, then the marks (both cleared first), maps and ends.
 constexpr uint32_t kCounters = 4, kCounterWords = 32;  // a cache line each
@@ -210,9 +200,8 @@ struct Split {
   int64_t tiles;
   uint32_t groups, kinds;
 };
-template <int V>
 __device__ __forceinline__ Chain chain_of(const Split& s, int64_t group) {
-  return {s.marks + group * s.tiles, s.maps + group * s.tiles * 64 * V, s.ends + group * s.tiles * 64 * V};
+  return {s.marks + group * s.tiles, s.maps + group * s.tiles * 64, s.ends + group * s.tiles * 64};
 }
 // A tile that nobody has begun, by its order in the chain of its group, the same in all threads; false if there is none.  Every
 // `kinds`th group shares a counter: four of them (1000 x 8192 bfloat16 18.0 us, with one for all 22.1; 4001 x 2100 float 28.4 and
@@ -330,7 +319,8 @@ struct Steps {
     }
     const int64_t end = t0 + K;
     if (a.h_last && end >= a.steps) at.ch.put(a.h_last + at.state, h);
-    if (a.states && end % AMQ_STATE_STEPS == 0 && end < a.steps) at.ch.put(a.states + (end / AMQ_STATE_STEPS - 1) * (int64_t)a.batch * a.n + at.state, h);
+    if (a.states && end % AMQ_STATE_STEPS == 0 && end < a.steps)
+      at.ch.put(a.states + (end / AMQ_STATE_STEPS - 1) * (int64_t)a.batch * a.n + at.state, h);
   }
 };
 // Rows behind the end of a batch entry: zeros, every `by`-th from t on.
@@ -409,28 +399,29 @@ __global__ __launch_bounds__(64 * kTileWaves, ONE ? 8 : 4) void recurrence_kerne
   if (w == 0 && a.h_last && at.ch.any) at.ch.put(a.h_last + at.state, carry);
 }
 
-// A workgroup per tile, of 16 steps of 16 waves of one channel a lane: a longer tile waits less for others than a wider one (32768 x 1024 bfloat16 57 us, 8
-// steps of two channels 61, 12 steps of one 61; 16384 x 1024 float 50, 51 and 49), and needs no even number of channels.
+// A workgroup per tile, of 16 steps of 16 waves of one channel a lane: a longer tile waits less for others than a wider one
+// (32768 x 1024 bfloat16 57 us, 8 steps of two channels 61, 12 steps of one 61; 16384 x 1024 float 50, 51 and 49), and needs no even
+// number of channels.
 template <typename T, int MODE>
 __global__ __launch_bounds__(64 * kTileWaves, 8) void recurrence_tiles_kernel(RecurrenceArgs a, Split split) {
   constexpr int V = 1, K = kLongSpan;
-  __shared__ uint64_t stage[kWindow][64 * V];
-  __shared__ float begin[64 * V];
+  __shared__ uint64_t stage[kWindow][64];
+  __shared__ float begin[64];
   __shared__ uint32_t number;
   __shared__ int found;
-  auto maps = reinterpret_cast<float(*)[2][64 * V]>(stage);  // [kTileWaves]
+  auto maps = reinterpret_cast<float(*)[2][64]>(stage);  // [kTileWaves]
   const int w = __builtin_amdgcn_readfirstlane(wave_id()), lane = lane_id();
   uint32_t tile, group;
   if (!take_tile(split, number, tile, group)) return;
   const Group<V, RecurrenceArgs> at(a, group);
   const int64_t t0 = (int64_t)tile * kLongTile + w * K;
-  const Chain chain = chain_of<V>(split, group);
+  const Chain chain = chain_of(split, group);
   if ((int64_t)tile * kLongTile >= at.length) {  // behind the entry's end
     clear_rows(a, at, (T*)a.hs, t0, t0 + K < a.steps ? t0 + K : a.steps, 1, a.hs_step, a.hs_batch);
     if (w == 0 && a.h_last && tile == split.tiles - 1) {
       float h[V];
       if (at.length == 0) given<V>(a.h0, at, h);
-      else end_of(chain, (at.length - 1) / kLongTile, h);
+      else h[0] = end_of(chain, (at.length - 1) / kLongTile);
       if (at.ch.any) at.ch.put(a.h_last + at.state, h);
     }
     return;
@@ -441,51 +432,34 @@ __global__ __launch_bounds__(64 * kTileWaves, 8) void recurrence_tiles_kernel(Re
     in.ask(a, at, t0);
     steps.set(in, t0, at.length);
   }
-  float A[V], B[V], h[V];
-#pragma unroll
-  for (int j = 0; j < V; ++j) B[j] = 0.0f;
+  float A[V], B[V] = {0.0f}, h[V];
   steps.map(A, B);
-#pragma unroll
-  for (int j = 0; j < V; ++j) {
-    maps[w][0][lane * V + j] = A[j];
-    maps[w][1][lane * V + j] = B[j];
-  }
+  maps[w][0][lane] = A[0];
+  maps[w][1][lane] = B[0];
   lds_barrier();
   // the maps of the waves before it as one; wave 0 takes those of all
-#pragma unroll
-  for (int j = 0; j < V; ++j) {
-    A[j] = 1.0f;
-    B[j] = 0.0f;
-  }
+  float fa = 1.0f, fb = 0.0f;
   const int before = w == 0 ? kTileWaves : w;
 #pragma unroll 4
-  for (int u = 0; u < before; ++u)
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-      const float fa = maps[u][0][lane * V + j];
-      A[j] *= fa;
-      B[j] = fmaf(fa, B[j], maps[u][1][lane * V + j]);
-    }
+  for (int u = 0; u < before; ++u) {
+    const float one = maps[u][0][lane];
+    fa *= one;
+    fb = fmaf(one, fb, maps[u][1][lane]);
+  }
   if (tile > 0) {
-    if (w == 0) leave_map(chain, tile, A, B);
-    look_back<V>(chain, tile, stage, found, w, w == 0, h);
+    if (w == 0) leave_map(chain, tile, fa, fb);
+    look_back(chain, tile, stage, found, w, w == 0, h[0]);
   } else if (w == 0) {
     given<V>(a.h0, at, h);
   }
   if (w == 0) {
-    float end[V];
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-      begin[lane * V + j] = h[j];
-      end[j] = fmaf(A[j], h[j], B[j]);
-    }
-    leave_end(chain, tile, end);
+    begin[lane] = h[0];
+    leave_end(chain, tile, fmaf(fa, h[0], fb));
     lds_barrier();
     mark_end(chain, tile);
   } else {
     lds_barrier();
-#pragma unroll
-    for (int j = 0; j < V; ++j) h[j] = fmaf(A[j], begin[lane * V + j], B[j]);
+    h[0] = fmaf(fa, begin[lane], fb);
   }
   steps.replay(a, at, t0, h);
 }
@@ -580,9 +554,10 @@ __device__ __forceinline__ void replay_back(const RecurrenceGradArgs& a, const G
   if (t0 == 0 && a.dh0) at.ch.put(a.dh0 + at.state, r);
 }
 
-template <typename T, int MODE, int V, bool ONE>
+template <typename T, int MODE, bool ONE>
 __global__ __launch_bounds__(64 * kTileWaves, ONE ? 8 : 4) void recurrence_grad_kernel(RecurrenceGradArgs a) {
-  __shared__ float maps[ONE ? 1 : 2][kTileWaves][3][64 * V];
+  constexpr int V = 1;
+  __shared__ float maps[ONE ? 1 : 2][kTileWaves][3][64];
   const int w = __builtin_amdgcn_readfirstlane(wave_id()), waves = blockDim.x / 64, lane = lane_id();
   const Group<V, RecurrenceGradArgs> at(a, blockIdx.x);
   float back[V];  // the gradient that reaches a tile's last state from the steps behind it
@@ -605,34 +580,22 @@ __global__ __launch_bounds__(64 * kTileWaves, ONE ? 8 : 4) void recurrence_grad_
     steps.set(in.in, t0, at.length);
     in.clear_behind(t0, at.length);
     // the wave's maps: of the state along time, and of the gradient against it (the same factor)
-    float A[V], B[V], R[V], h[V], r[V];
-#pragma unroll
-    for (int j = 0; j < V; ++j) B[j] = 0.0f;
+    float A[V], B[V] = {0.0f}, R[V], h[V], r[V];
     steps.map(A, B);
     map_back(steps, in.d, R);
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-      maps[turn][w][0][lane * V + j] = A[j];
-      maps[turn][w][1][lane * V + j] = B[j];
-      maps[turn][w][2][lane * V + j] = R[j];
-      h[j] = in.some ? in.h.v[j] : 0.0f;
-    }
+    maps[turn][w][0][lane] = A[0];
+    maps[turn][w][1][lane] = B[0];
+    maps[turn][w][2][lane] = R[0];
+    h[0] = in.some ? in.h.v[0] : 0.0f;
     lds_barrier();
 #pragma unroll 4
-    for (int u = 0; u < w; ++u)
-#pragma unroll
-      for (int j = 0; j < V; ++j) h[j] = fmaf(maps[turn][u][0][lane * V + j], h[j], maps[turn][u][1][lane * V + j]);
+    for (int u = 0; u < w; ++u) h[0] = fmaf(maps[turn][u][0][lane], h[0], maps[turn][u][1][lane]);
 #pragma unroll 4
-    for (int u = waves - 1; u > w; --u)
-#pragma unroll
-      for (int j = 0; j < V; ++j) back[j] = fmaf(maps[turn][u][0][lane * V + j], back[j], maps[turn][u][2][lane * V + j]);
-#pragma unroll
-    for (int j = 0; j < V; ++j) r[j] = back[j];
+    for (int u = waves - 1; u > w; --u) back[0] = fmaf(maps[turn][u][0][lane], back[0], maps[turn][u][2][lane]);
+    r[0] = back[0];
     if (tile > 0)
 #pragma unroll 4
-      for (int u = w; u >= 0; --u)
-#pragma unroll
-        for (int j = 0; j < V; ++j) back[j] = fmaf(maps[turn][u][0][lane * V + j], back[j], maps[turn][u][2][lane * V + j]);
+      for (int u = w; u >= 0; --u) back[0] = fmaf(maps[turn][u][0][lane], back[0], maps[turn][u][2][lane]);
     replay_back(a, at, steps, in, t0, h, r);
     if constexpr (ONE) return;
   }
@@ -641,11 +604,11 @@ __global__ __launch_bounds__(64 * kTileWaves, ONE ? 8 : 4) void recurrence_grad_
 template <typename T, int MODE>
 __global__ __launch_bounds__(64 * kTileWaves, 8) void recurrence_grad_tiles_kernel(RecurrenceGradArgs a, Split split) {
   constexpr int V = 1;
-  __shared__ uint64_t stage[kWindow][64 * V];
-  __shared__ float begin[64 * V];
+  __shared__ uint64_t stage[kWindow][64];
+  __shared__ float begin[64];
   __shared__ uint32_t number;
   __shared__ int found;
-  auto maps = reinterpret_cast<float(*)[3][64 * V]>(stage);  // [kTileWaves]
+  auto maps = reinterpret_cast<float(*)[3][64]>(stage);  // [kTileWaves]
   const int w = __builtin_amdgcn_readfirstlane(wave_id()), lane = lane_id();
   const bool mine = w == kTileWaves - 1;
   uint32_t turn, group;
@@ -669,59 +632,40 @@ __global__ __launch_bounds__(64 * kTileWaves, 8) void recurrence_grad_tiles_kern
   Steps<T, MODE, V> steps;
   steps.set(in.in, t0, at.length);
   in.clear_behind(t0, at.length);
-  float A[V], B[V], R[V], h[V], r[V];
-#pragma unroll
-  for (int j = 0; j < V; ++j) B[j] = 0.0f;
+  float A[V], B[V] = {0.0f}, R[V], h[V], r[V];
   steps.map(A, B);
   map_back(steps, in.d, R);
-#pragma unroll
-  for (int j = 0; j < V; ++j) {
-    maps[w][0][lane * V + j] = A[j];
-    maps[w][1][lane * V + j] = B[j];
-    maps[w][2][lane * V + j] = R[j];
-    h[j] = in.some ? in.h.v[j] : 0.0f;
-  }
+  maps[w][0][lane] = A[0];
+  maps[w][1][lane] = B[0];
+  maps[w][2][lane] = R[0];
+  h[0] = in.some ? in.h.v[0] : 0.0f;
   lds_barrier();
 #pragma unroll 4
-  for (int u = 0; u < w; ++u)
-#pragma unroll
-    for (int j = 0; j < V; ++j) h[j] = fmaf(maps[u][0][lane * V + j], h[j], maps[u][1][lane * V + j]);
+  for (int u = 0; u < w; ++u) h[0] = fmaf(maps[u][0][lane], h[0], maps[u][1][lane]);
   // the maps of the waves behind it as one; the last wave takes those of all
-#pragma unroll
-  for (int j = 0; j < V; ++j) {
-    A[j] = 1.0f;
-    R[j] = 0.0f;
-  }
+  float fa = 1.0f, fr = 0.0f;
   const int until = mine ? 0 : w + 1;
 #pragma unroll 4
-  for (int u = kTileWaves - 1; u >= until; --u)
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-      const float fa = maps[u][0][lane * V + j];
-      A[j] *= fa;
-      R[j] = fmaf(fa, R[j], maps[u][2][lane * V + j]);
-    }
-  const Chain chain = chain_of<V>(split, group);
+  for (int u = kTileWaves - 1; u >= until; --u) {
+    const float one = maps[u][0][lane];
+    fa *= one;
+    fr = fmaf(one, fr, maps[u][2][lane]);
+  }
+  const Chain chain = chain_of(split, group);
   if (order > 0) {
-    if (mine) leave_map(chain, order, A, R);
-    look_back<V>(chain, order, stage, found, w, mine, r);
+    if (mine) leave_map(chain, order, fa, fr);
+    look_back(chain, order, stage, found, w, mine, r[0]);
   } else if (mine) {
     given<V>(a.dh_last, at, r);
   }
   if (mine) {
-    float end[V];
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-      begin[lane * V + j] = r[j];
-      end[j] = fmaf(A[j], r[j], R[j]);
-    }
-    leave_end(chain, order, end);
+    begin[lane] = r[0];
+    leave_end(chain, order, fmaf(fa, r[0], fr));
     lds_barrier();
     mark_end(chain, order);
   } else {
     lds_barrier();
-#pragma unroll
-    for (int j = 0; j < V; ++j) r[j] = fmaf(A[j], begin[lane * V + j], R[j]);
+    r[0] = fmaf(fa, begin[lane], fr);
   }
   replay_back(a, at, steps, in, t0, h, r);
 }
@@ -745,19 +689,21 @@ int waves_of(int64_t steps, bool even) {
 int64_t groups_of(int64_t batch, int64_t n, int V) { return batch * ((n + 64 * V - 1) / (64 * V)); }
 int64_t tiles_of(int64_t steps, int tile) { return (steps + tile - 1) / tile; }
 
-// Channels of a lane: two of 16 bits where a workgroup walks over tiles forward and groups of 128 channels still fill the card
-// (1000 x 32768 entries 41 us, with one 50; 2000 x 16384 65 and 48); one otherwise (35 x 262144 backward 21.2, with two 23.8).
-bool two_channels(int64_t batch, int64_t n) { return n % 2 == 0 && groups_of(batch, n, 2) >= 256; }
+// Channels of a lane: two of 16 bits where a workgroup walks over tiles forward and groups of 64 channels are more than the card holds at
+// once (300 x 17408 14.9 us, with one 18.4; 1000 x 32768 40 and 50; but 2000 x 16384 65 and 48); one otherwise (35 x 262144 backward 21.2,
+// with two 23.8).
+bool two_channels(int64_t batch, int64_t n) { return n % 2 == 0 && groups_of(batch, n, 1) > 256; }
 
-// The form with the least time, by measurement.  Per 128 steps a workgroup per group takes c0 us and all 256 that the card holds at once c0 + c1; a
-// workgroup per tile e for 256 groups, and 6.7 us more for clearing the marks, the second launch and the chain.  Steps x channels, a workgroup per
-// group and one per tile: 16-bit types 300 x 1024 9.5 and 11.0, 500 x 1024 11.7 and 10.2, 1000 x 8192 22.8 and 18.0, 1000 x 12288 22.9 and 23.3,
-// 3000 x 12288 65 and 55, 3000 x 16384 70 and 72, 3000 x 16500 137 and 90; float 1000 x 4096 20.2 and 16.7, 1000 x 12288 30.4 and 33.9; backward
-// 200 x 1024 10.2 and 11.5, 1000 x 1024 33 and 12, 1000 x 16384 44 and 52, 3000 x 12288 121 and 101, float 1000 x 24576 117 and 102.
+// The form with the least time, by measurement.  Per 128 steps a workgroup per group takes c0 us and all 256 that the card holds at once
+// c0 + c1; a workgroup per tile e for 256 groups, and 6.7 us more for clearing the marks, the second launch and the chain.  Steps x
+// channels, a workgroup per group and one per tile: 16-bit types 300 x 1024 9.5 and 11.0, 500 x 1024 11.7 and 10.2, 1000 x 8192 22.8 and
+// 18.0, 1000 x 12288 22.9 and 23.3, 3000 x 12288 65 and 55, 3000 x 16384 70 and 72, 1000 x 24576 36 and 43, 2000 x 33792 139 and 98;
+// float 1000 x 4096 20.2 and 16.7, 1000 x 12288 30.4 and 33.9; backward 200 x 1024 10.2 and 11.5, 1000 x 1024 33 and 12, 1000 x 16384
+// 44 and 52, 3000 x 12288 121 and 101, float 1000 x 24576 117 and 102.
 bool splits(int64_t batch, int64_t n, int64_t steps, bool wide, bool backward) {
   const bool pairs = !wide && !backward && two_channels(batch, n);
-  const double c0 = pairs ? 2.6 : wide ? backward ? 3.5 : 2.05 : backward ? 3.85 : 2.4;
-  const double c1 = pairs ? 2.4 : wide ? backward ? 5.0 : 2.5 : backward ? 1.5 : 0.6;
+  const double c0 = pairs ? 2.9 : wide ? backward ? 3.5 : 2.05 : backward ? 3.85 : 2.4;
+  const double c1 = pairs ? 2.1 : wide ? backward ? 5.0 : 2.5 : backward ? 1.5 : 0.6;
   const double e = wide ? backward ? 7.8 : 4.6 : backward ? 5.2 : 2.7;
   const int64_t g = groups_of(batch, n, pairs ? 2 : 1), last = g % 256;
   const double one = (double)(g / 256) * (c0 + c1) + (last ? c0 + c1 * (double)last / 256 : 0.0);
@@ -825,8 +771,8 @@ hipError_t launch_recurrence_grad(const RecurrenceGradArgs& a, hipStream_t s) {
     constexpr int M = decltype(m)::value;
     constexpr bool wide = sizeof(T) == 4;
     if (splits(a.batch, a.n, a.steps, wide, true)) return launch_tiles(a, kTile, s, recurrence_grad_tiles_kernel<T, M>);
-    if (a.steps <= kTile) return launch_groups(a, 1, false, s, recurrence_grad_kernel<T, M, 1, true>);
-    return launch_groups(a, 1, false, s, recurrence_grad_kernel<T, M, 1, false>);
+    if (a.steps <= kTile) return launch_groups(a, 1, false, s, recurrence_grad_kernel<T, M, true>);
+    return launch_groups(a, 1, false, s, recurrence_grad_kernel<T, M, false>);
   });
 }
 

@@ -137,7 +137,7 @@ def layouts(gate, x):
     yield "slice", inner
 
 
-@pytest.mark.parametrize("T,B,n", [(1, 3, 7), (5, 1, 64), (35, 4, 131), (300, 3, 66)])
+@pytest.mark.parametrize("T,B,n", [(1, 3, 7), (5, 1, 64), (35, 4, 131), (300, 3, 66), (140, 300, 66)])
 @pytest.mark.parametrize("mode", MODES)
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_layouts(amq, T, B, n, mode, dtype):

@@ -8,9 +8,14 @@
 //
 // About 30 operations per entry forward and 60 backward, against 10 and 16 bytes (16-bit types): bound by memory, or by latency
 // for few rows.  So every entry is read once and kept in registers between the four sums of a row and the results; a row belongs to one
-// wave (its sums need no barrier) or to a workgroup of 4, 8 or 16.  Workgroups walk over rows, with the parameters and, in the
-// backward pass, four sums per column in registers; those leave one partial row per workgroup, added up by a second launch in a
-// fixed order.  normed is formed from y before its rounding; statistics and sums are binary32.
+// wave (its sums need no barrier) or to a workgroup of 4, 8 or 16, a short one to 16 or 32 lanes of a wave.  Workgroups walk over rows, with
+// the parameters and, in the backward pass, four sums per column in registers (in LDS where a lane has two pieces of a row); those leave one
+// partial row per workgroup, added up by a second launch in a fixed order.  normed is formed from y before its rounding; statistics and
+// sums are binary32.
+//
+// Measured (a large copy 5.1 TB/s): 8960 x 1024 half 17.6 us, 5.2 TB/s (part of it stays in the memory-side cache); backward 8960 x 1500
+// bfloat16 with a float residual 59 us, 5.0, and 5 for the second launch; 8960 x 1024 bfloat16 backward 43, 3.4, with vector
+// instructions (87 per entry) and latency in the way.
 #include "../../include/amq.h"
 
 #include <type_traits>

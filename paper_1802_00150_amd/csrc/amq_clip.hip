@@ -150,7 +150,6 @@ __global__ __launch_bounds__(kThreads) void scale_tensors_kernel(ScaleArgs a) {
 int64_t fill(const ClipTensors& c, int64_t at, Table& t, uint32_t& pieces, uint32_t& vectors) {
   int used = 0;
   int64_t bytes = 0;
-  const int64_t from = at;
   for (; at < c.count && used < kTensors; ++at)
     if (c.sizes[at] > 0) {
       t.p[used] = c.tensors[at];
@@ -160,7 +159,6 @@ int64_t fill(const ClipTensors& c, int64_t at, Table& t, uint32_t& pieces, uint3
       bytes += c.sizes[at] * (c.types[at] == AMQ_F32 ? 4 : 2);
       ++used;
     }
-  (void)from;
   // pieces of 8 KB while they do not fill the card, of up to 64 KB (or more where their number would pass 32 bits)
   vectors = 1;
   while ((vectors < 8 && bytes / (16 * kThreads * vectors) > 2 * kMostBlocks) || bytes / (16 * kThreads * (int64_t)vectors) > (1 << 30)) vectors *= 2;

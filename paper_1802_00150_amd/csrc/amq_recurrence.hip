@@ -43,40 +43,46 @@ constexpr int kLongSpan = 16, kLongTile = kLongSpan * kTileWaves;  // of tiles w
 static_assert(kLongTile % AMQ_STATE_STEPS == 0 && AMQ_STATE_STEPS % kLongSpan == 0, "states are left behind a wave's steps");
 static_assert(kTile == AMQ_STATE_STEPS, "a backward tile begins where a state was left");
 
-// What a step does to the state: h -> keep(h) + add.
-template <int MODE>
+// What a step does to the state.  BACK: in the backward pass, which needs i and x apart.
+template <int MODE, bool BACK>
 struct Step {
-  float p, add;  // blend: f where g < 0, -i where g >= 0;  decay: the factor
-  bool pos;      // g >= 0
+  float p;  // blend: f where g < 0, -i where g >= 0 (its sign bit says which: a mask per step would not fit the scalar registers);  decay: the factor
+  float v;  // i x;  BACK: x
+  float i;  // (BACK)
   __device__ __forceinline__ void set(float g, float x) {
     if constexpr (MODE == AMQ_RECURRENCE_BLEND) {
       const float e = __expf(-fabsf(g)), r = __builtin_amdgcn_rcpf(1.0f + e), small = e * r;  // sigmoid(|g|), sigmoid(-|g|)
-      pos = g >= 0.0f;
+      const bool pos = g >= 0.0f;
       p = pos ? -small : small;
-      add = (pos ? small : r) * x;
+      i = pos ? small : r;
+      v = BACK ? x : i * x;
     } else {
       p = g;
-      add = x;
+      i = 1.0f;
+      v = x;
     }
   }
   __device__ __forceinline__ void hold() {
-    p = MODE == AMQ_RECURRENCE_BLEND ? 0.0f : 1.0f;
-    add = 0.0f;
-    pos = true;
+    p = MODE == AMQ_RECURRENCE_BLEND ? -0.0f : 1.0f;
+    i = v = 0.0f;
   }
-  __device__ __forceinline__ float keep(float h) const {
-    return MODE == AMQ_RECURRENCE_BLEND ? fmaf(p, h, pos ? h : 0.0f) : p * h;
-  }
+  __device__ __forceinline__ float held(float h) const { return __float_as_int(p) < 0 ? h : 0.0f; }
+  __device__ __forceinline__ float keep(float h) const { return MODE == AMQ_RECURRENCE_BLEND ? fmaf(p, h, held(h)) : p * h; }
   __device__ __forceinline__ float next(float h) const {
-    return MODE == AMQ_RECURRENCE_BLEND ? fmaf(p, h, pos ? add + h : add) : fmaf(p, h, add);
+    if constexpr (MODE == AMQ_RECURRENCE_BLEND) return fmaf(p, h, BACK ? fmaf(i, v, held(h)) : v + held(h));
+    return fmaf(p, h, v);
   }
-  __device__ __forceinline__ float dx(float e) const { return MODE == AMQ_RECURRENCE_BLEND ? (pos ? -p : 1.0f - p) * e : e; }
-  __device__ __forceinline__ float dgate(float e, float h, float x) const {
+  __device__ __forceinline__ float dx(float e) const { return MODE == AMQ_RECURRENCE_BLEND ? i * e : e; }
+  __device__ __forceinline__ float dgate(float e, float h) const {
     if constexpr (MODE == AMQ_RECURRENCE_BLEND) {
       const float small = fabsf(p);
-      return e * (h - x) * fmaf(-small, small, small);
+      return e * (h - v) * fmaf(-small, small, small);
     }
     return e * h;
+  }
+  // (a comparison made again takes one operation, one kept from the maps to the results two scalar registers)
+  __device__ __forceinline__ void again() {
+    if constexpr (MODE == AMQ_RECURRENCE_BLEND) asm volatile("" : "+v"(p));
   }
 };
 
@@ -89,6 +95,12 @@ struct Lane {
     const uint32_t left = (uint32_t)(n - c), at = lane_id() * V;
     any = at < left;
     first = any ? at : left - V;
+  }
+  // The same in the block it is called in, so that the compiler sees 32 bits beside a scalar address there.
+  __device__ __forceinline__ Lane here() const {
+    Lane l = *this;
+    asm volatile("" : "+v"(l.first));
+    return l;
   }
   template <typename T>
   __device__ __forceinline__ Elements<T, V> get(const T* row) const {
@@ -222,11 +234,21 @@ __global__ __launch_bounds__(256) void split_clear_kernel(uint32_t* p, int64_t w
 
 // ---- forward
 
+// k < left, decided by itself (the compiler would join the steps of a tile that ends early, and index what is in registers).
+__device__ __forceinline__ bool within(int k, int left) {
+  asm volatile("" : "+s"(left));
+  return k < left;
+}
+
+// Ends a branch: the compiler would take the same last operations out of both branches, and wait there for what has just been asked for.
+__device__ __forceinline__ void branch_end() { asm volatile(""); }
+
 // Where a group of 64 V channels lies, and the steps of its batch entry that count.
 template <int V, typename A>
 struct Group {
-  int64_t b, length, state;  // batch entry; its steps; of the group's first channel in [B][n]
-  uint32_t c;                // first channel
+  int64_t b, state;   // batch entry; of the group's first channel in [B][n]
+  int steps, length;  // all; the entry's
+  uint32_t c;         // first channel
   Lane<V> ch;
   __device__ __forceinline__ Group(const A& a, uint32_t group) : ch(0, V) {
     const uint32_t pieces = ((uint32_t)a.n + 64 * V - 1) / (64 * V), entry = group / pieces;
@@ -234,10 +256,10 @@ struct Group {
     c = (group - entry * pieces) * 64 * V;
     state = b * a.n + c;
     ch = Lane<V>((int)c, a.n);
-    length = a.steps;
+    length = steps = (int)a.steps;
     if (a.lengths) {
       const int64_t l = a.lengths[b];
-      length = l < 0 ? 0 : l < a.steps ? l : a.steps;
+      length = l < 0 ? 0 : l < steps ? (int)l : steps;
     }
   }
   template <typename T>
@@ -249,38 +271,48 @@ struct Inputs {
   Elements<T, V> g[K], x[K];
   // asks for the steps from t0 on
   template <typename A>
-  __device__ __forceinline__ void ask(const A& a, const Group<V, A>& at, int64_t t0) {
+  __device__ __forceinline__ void ask(const A& a, const Group<V, A>& at, int t0) {
+    const int left = at.length - t0;
     const T *pg = at.row((const T*)a.gate, t0, a.gate_step, a.gate_batch), *px = at.row((const T*)a.x, t0, a.x_step, a.x_batch);
-    if (t0 + K <= at.length) {
+    if (left >= K) {
+      const Lane<V> ch = at.ch.here();
 #pragma unroll
       for (int k = 0; k < K; ++k, pg += a.gate_step, px += a.x_step) {
-        g[k] = at.ch.get(pg);
-        x[k] = at.ch.get(px);
+        g[k] = ch.get(pg);
+        x[k] = ch.get(px);
       }
+      branch_end();
     } else {
 #pragma unroll
       for (int k = 0; k < K; ++k, pg += a.gate_step, px += a.x_step)
-        if (t0 + k < at.length) {
+        if (within(k, left)) {
           g[k] = at.ch.get(pg);
           x[k] = at.ch.get(px);
         }
     }
   }
 };
-template <typename T, int MODE, int V, int K = kSpan>
+template <typename T, int MODE, int V, bool BACK, int K = kSpan>
 struct Steps {
-  Step<MODE> s[K][V];
-  __device__ __forceinline__ void set(const Inputs<T, V, K>& in, int64_t t0, int64_t length) {
+  Step<MODE, BACK> s[K][V];
+  // `left`: of the entry's steps
+  __device__ __forceinline__ void set(const Inputs<T, V, K>& in, int left) {
 #pragma unroll
     for (int k = 0; k < K; ++k)
 #pragma unroll
       for (int j = 0; j < V; ++j) s[k][j].set((float)in.g[k].v[j], (float)in.x[k].v[j]);
-    if (t0 + K > length)
+    if (left < K)
 #pragma unroll
       for (int k = 0; k < K; ++k)
-        if (t0 + k >= length)
+        if (!within(k, left))
 #pragma unroll
           for (int j = 0; j < V; ++j) s[k][j].hold();
+  }
+  __device__ __forceinline__ void again() {
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+      for (int j = 0; j < V; ++j) s[k][j].again();
   }
   // The map of all: A the product of what is kept, B continued from what it holds.
   __device__ __forceinline__ void map(float (&A)[V], float (&B)[V]) const {
@@ -295,16 +327,20 @@ struct Steps {
       }
   }
   // From the state in front of them to the one behind, with everything that is written on the way.
-  __device__ __forceinline__ void replay(const RecurrenceArgs& a, const Group<V, RecurrenceArgs>& at, int64_t t0, float (&h)[V]) const {
-    if (t0 >= a.steps || !at.ch.any) return;
+  __device__ __forceinline__ void replay(const RecurrenceArgs& a, const Group<V, RecurrenceArgs>& at, int t0, float (&h)[V]) {
+    if (t0 >= at.steps || !at.ch.any) return;
+    again();
+    const int left = at.length - t0, end = t0 + K;
     T* py = at.row((T*)a.hs, t0, a.hs_step, a.hs_batch);
-    if (t0 + K <= at.length) {
+    if (left >= K) {
+      const Lane<V> ch = at.ch.here();
 #pragma unroll
       for (int k = 0; k < K; ++k, py += a.hs_step) {
 #pragma unroll
         for (int j = 0; j < V; ++j) h[j] = s[k][j].next(h[j]);
-        at.ch.put(py, h);
+        ch.put(py, h);
       }
+      branch_end();
     } else {
 #pragma unroll
       for (int k = 0; k < K; ++k, py += a.hs_step) {
@@ -312,14 +348,13 @@ struct Steps {
 #pragma unroll
         for (int j = 0; j < V; ++j) {
           h[j] = s[k][j].next(h[j]);
-          out[j] = t0 + k < at.length ? h[j] : 0.0f;
+          out[j] = within(k, left) ? h[j] : 0.0f;
         }
-        if (t0 + k < a.steps) at.ch.put(py, out);
+        if (t0 + k < at.steps) at.ch.put(py, out);
       }
     }
-    const int64_t end = t0 + K;
-    if (a.h_last && end >= a.steps) at.ch.put(a.h_last + at.state, h);
-    if (a.states && end % AMQ_STATE_STEPS == 0 && end < a.steps)
+    if (a.h_last && end >= at.steps) at.ch.put(a.h_last + at.state, h);
+    if (a.states && end % AMQ_STATE_STEPS == 0 && end < at.steps)
       at.ch.put(a.states + (end / AMQ_STATE_STEPS - 1) * (int64_t)a.batch * a.n + at.state, h);
   }
 };
@@ -350,17 +385,17 @@ __global__ __launch_bounds__(64 * kTileWaves, ONE ? 8 : 4) void recurrence_kerne
   const int w = __builtin_amdgcn_readfirstlane(wave_id()), waves = blockDim.x / 64, lane = lane_id();
   const Group<V, RecurrenceArgs> at(a, blockIdx.x);
   Inputs<T, V> in;
-  Steps<T, MODE, V> steps;
+  Steps<T, MODE, V, false> steps;
   float carry[V];  // (wave 0 alone has it, and reads h0: h_last, written behind a barrier, may lie there)
 #pragma unroll
   for (int j = 0; j < V; ++j) carry[j] = 0.0f;
   if (w == 0) given<V>(a.h0, at, carry);
   int turn = 0;
   in.ask(a, at, w * kSpan);
-  int64_t first = 0;
+  int first = 0;
   for (; first < at.length; first += waves * kSpan, turn ^= 1) {
-    const int64_t t0 = first + w * kSpan;
-    steps.set(in, t0, at.length);
+    const int t0 = first + w * kSpan;
+    steps.set(in, at.length - t0);
     if constexpr (!ONE) in.ask(a, at, t0 + waves * kSpan);
     float h[V];
 #pragma unroll
@@ -394,7 +429,7 @@ __global__ __launch_bounds__(64 * kTileWaves, ONE ? 8 : 4) void recurrence_kerne
     steps.replay(a, at, t0, h);
     if constexpr (ONE) return;
   }
-  if (first >= a.steps) return;
+  if (first >= at.steps) return;
   clear_rows(a, at, (T*)a.hs, first + w, a.steps, waves, a.hs_step, a.hs_batch);
   if (w == 0 && a.h_last && at.ch.any) at.ch.put(a.h_last + at.state, carry);
 }
@@ -414,10 +449,10 @@ __global__ __launch_bounds__(64 * kTileWaves, 8) void recurrence_tiles_kernel(Re
   uint32_t tile, group;
   if (!take_tile(split, number, tile, group)) return;
   const Group<V, RecurrenceArgs> at(a, group);
-  const int64_t t0 = (int64_t)tile * kLongTile + w * K;
+  const int t0 = (int)tile * kLongTile + w * K;
   const Chain chain = chain_of(split, group);
-  if ((int64_t)tile * kLongTile >= at.length) {  // behind the entry's end
-    clear_rows(a, at, (T*)a.hs, t0, t0 + K < a.steps ? t0 + K : a.steps, 1, a.hs_step, a.hs_batch);
+  if ((int)tile * kLongTile >= at.length) {  // behind the entry's end
+    clear_rows(a, at, (T*)a.hs, t0, t0 + K < at.steps ? t0 + K : at.steps, 1, a.hs_step, a.hs_batch);
     if (w == 0 && a.h_last && tile == split.tiles - 1) {
       float h[V];
       if (at.length == 0) given<V>(a.h0, at, h);
@@ -426,11 +461,11 @@ __global__ __launch_bounds__(64 * kTileWaves, 8) void recurrence_tiles_kernel(Re
     }
     return;
   }
-  Steps<T, MODE, V, K> steps;
+  Steps<T, MODE, V, false, K> steps;
   {
     Inputs<T, V, K> in;
     in.ask(a, at, t0);
-    steps.set(in, t0, at.length);
+    steps.set(in, at.length - t0);
   }
   float A[V], B[V] = {0.0f}, h[V];
   steps.map(A, B);
@@ -472,33 +507,36 @@ struct GradInputs {
   Elements<T, V> d[kSpan];
   Elements<float, V> h;  // the state in front of the tile
   bool some;             // (there is one)
-  __device__ __forceinline__ void ask(const RecurrenceGradArgs& a, const Group<V, RecurrenceGradArgs>& at, int64_t tile, int64_t t0) {
+  __device__ __forceinline__ void ask(const RecurrenceGradArgs& a, const Group<V, RecurrenceGradArgs>& at, int tile, int t0) {
+    const int left = at.length - t0;
     in.ask(a, at, t0);
     const T* pd = at.row((const T*)a.dhs, t0, a.dhs_step, a.dhs_batch);
-    if (t0 + kSpan <= at.length) {
+    if (left >= kSpan) {
+      const Lane<V> ch = at.ch.here();
 #pragma unroll
-      for (int k = 0; k < kSpan; ++k, pd += a.dhs_step) d[k] = at.ch.get(pd);
+      for (int k = 0; k < kSpan; ++k, pd += a.dhs_step) d[k] = ch.get(pd);
+      branch_end();
     } else {
 #pragma unroll
       for (int k = 0; k < kSpan; ++k, pd += a.dhs_step)
-        if (t0 + k < at.length) d[k] = at.ch.get(pd);
+        if (within(k, left)) d[k] = at.ch.get(pd);
     }
     const float* from = tile == 0 ? a.h0 : a.states + (tile - 1) * (int64_t)a.batch * a.n;
     some = from != nullptr;
     if (some) h = at.ch.get(from + at.state);
   }
-  __device__ __forceinline__ void clear_behind(int64_t t0, int64_t length) {
-    if (t0 + kSpan > length)
+  __device__ __forceinline__ void clear_behind(int left) {
+    if (left < kSpan)
 #pragma unroll
       for (int k = 0; k < kSpan; ++k)
-        if (t0 + k >= length)
+        if (!within(k, left))
 #pragma unroll
           for (int j = 0; j < V; ++j) d[k].v[j] = (T)0.0f;
   }
 };
 // The map of a wave's gradient against time, from nothing behind it.
 template <typename T, int MODE, int V>
-__device__ __forceinline__ void map_back(const Steps<T, MODE, V>& steps, const Elements<T, V> (&d)[kSpan], float (&R)[V]) {
+__device__ __forceinline__ void map_back(const Steps<T, MODE, V, true>& steps, const Elements<T, V> (&d)[kSpan], float (&R)[V]) {
 #pragma unroll
   for (int j = 0; j < V; ++j) R[j] = 0.0f;
 #pragma unroll
@@ -508,9 +546,11 @@ __device__ __forceinline__ void map_back(const Steps<T, MODE, V>& steps, const E
 }
 // From the state h in front of a wave's steps and the gradient r that reaches the last of them from behind, to the one that leaves the first.
 template <typename T, int MODE, int V>
-__device__ __forceinline__ void replay_back(const RecurrenceGradArgs& a, const Group<V, RecurrenceGradArgs>& at, const Steps<T, MODE, V>& steps,
-                                            const GradInputs<T, V>& in, int64_t t0, float (&h)[V], float (&r)[V]) {
-  if (t0 >= a.steps || !at.ch.any) return;
+__device__ __forceinline__ void replay_back(const RecurrenceGradArgs& a, const Group<V, RecurrenceGradArgs>& at, Steps<T, MODE, V, true>& steps,
+                                            const GradInputs<T, V>& in, int t0, float (&h)[V], float (&r)[V]) {
+  if (t0 >= at.steps || !at.ch.any) return;
+  steps.again();
+  const int left = at.length - t0;
   T *qg = at.row((T*)a.dgate, t0, a.dgate_step, a.dgate_batch), *qx = at.row((T*)a.dx, t0, a.dx_step, a.dx_batch);
   float before[kSpan][V];
 #pragma unroll
@@ -524,30 +564,34 @@ __device__ __forceinline__ void replay_back(const RecurrenceGradArgs& a, const G
 #pragma unroll
     for (int j = 0; j < V; ++j) {
       const float e = r[j] + (float)in.d[k].v[j];
-      og[j] = steps.s[k][j].dgate(e, before[k][j], (float)in.in.x[k].v[j]);
+      og[j] = steps.s[k][j].dgate(e, before[k][j]);
       ox[j] = steps.s[k][j].dx(e);
       r[j] = steps.s[k][j].keep(e);
     }
   };
-  if (t0 + kSpan <= at.length) {
+  qg += (kSpan - 1) * a.dgate_step;
+  qx += (kSpan - 1) * a.dx_step;
+  if (left >= kSpan) {
+    const Lane<V> ch = at.ch.here();
 #pragma unroll
-    for (int k = kSpan - 1; k >= 0; --k) {
+    for (int k = kSpan - 1; k >= 0; --k, qg -= a.dgate_step, qx -= a.dx_step) {
       float og[V], ox[V];
       step(k, og, ox);
-      at.ch.put(qg + k * a.dgate_step, og);
-      at.ch.put(qx + k * a.dx_step, ox);
+      ch.put(qg, og);
+      ch.put(qx, ox);
     }
+    branch_end();
   } else {
 #pragma unroll
-    for (int k = kSpan - 1; k >= 0; --k) {
+    for (int k = kSpan - 1; k >= 0; --k, qg -= a.dgate_step, qx -= a.dx_step) {
       float og[V], ox[V];
       step(k, og, ox);
-      if (t0 + k >= at.length)
+      if (!within(k, left))
 #pragma unroll
         for (int j = 0; j < V; ++j) og[j] = ox[j] = 0.0f;
-      if (t0 + k < a.steps) {
-        at.ch.put(qg + k * a.dgate_step, og);
-        at.ch.put(qx + k * a.dx_step, ox);
+      if (t0 + k < at.steps) {
+        at.ch.put(qg, og);
+        at.ch.put(qx, ox);
       }
     }
   }
@@ -560,11 +604,12 @@ __global__ __launch_bounds__(64 * kTileWaves, ONE ? 8 : 4) void recurrence_grad_
   __shared__ float maps[ONE ? 1 : 2][kTileWaves][3][64];
   const int w = __builtin_amdgcn_readfirstlane(wave_id()), waves = blockDim.x / 64, lane = lane_id();
   const Group<V, RecurrenceGradArgs> at(a, blockIdx.x);
-  float back[V];  // the gradient that reaches a tile's last state from the steps behind it
-  given<V>(a.dh_last, at, back);
+  __shared__ float behind[ONE ? 1 : 2][64];
+  float back[V];  // wave 0: the gradient that reaches a tile's last state from the steps behind it
+  if (w == 0) given<V>(a.dh_last, at, back);
   int turn = 0;
-  const int64_t end = at.length == 0 ? 0 : ONE ? kTile : ((at.length - 1) / kTile + 1) * kTile;  // of its last tile
-  if (end < a.steps) {
+  const int end = at.length == 0 ? 0 : ONE ? kTile : ((at.length - 1) / kTile + 1) * kTile;  // of its last tile
+  if (end < at.steps) {
     clear_rows(a, at, (T*)a.dgate, end + w, a.steps, waves, a.dgate_step, a.dgate_batch);
     clear_rows(a, at, (T*)a.dx, end + w, a.steps, waves, a.dx_step, a.dx_batch);
   }
@@ -572,13 +617,17 @@ __global__ __launch_bounds__(64 * kTileWaves, ONE ? 8 : 4) void recurrence_grad_
     if (w == 0 && a.dh0 && at.ch.any) at.ch.put(a.dh0 + at.state, back);
     return;
   }
-  for (int64_t tile = ONE ? 0 : end / kTile - 1; tile >= 0; --tile, turn ^= 1) {
-    const int64_t t0 = tile * kTile + w * kSpan;
-    GradInputs<T, V> in;
-    Steps<T, MODE, V> steps;
-    in.ask(a, at, tile, t0);
-    steps.set(in.in, t0, at.length);
-    in.clear_behind(t0, at.length);
+  int tile = ONE ? 0 : end / kTile - 1;
+  GradInputs<T, V> ahead;
+  ahead.ask(a, at, tile, tile * kTile + w * kSpan);
+  for (; tile >= 0; --tile, turn ^= 1) {
+    const int t0 = tile * kTile + w * kSpan;
+    GradInputs<T, V> in = ahead;
+    Steps<T, MODE, V, true> steps;
+    steps.set(in.in, at.length - t0);
+    if constexpr (!ONE)
+      if (tile > 0) ahead.ask(a, at, tile - 1, t0 - kTile);
+    in.clear_behind(at.length - t0);
     // the wave's maps: of the state along time, and of the gradient against it (the same factor)
     float A[V], B[V] = {0.0f}, R[V], h[V], r[V];
     steps.map(A, B);
@@ -586,16 +635,15 @@ __global__ __launch_bounds__(64 * kTileWaves, ONE ? 8 : 4) void recurrence_grad_
     maps[turn][w][0][lane] = A[0];
     maps[turn][w][1][lane] = B[0];
     maps[turn][w][2][lane] = R[0];
+    if (w == 0) behind[turn][lane] = back[0];
     h[0] = in.some ? in.h.v[0] : 0.0f;
     lds_barrier();
 #pragma unroll 4
     for (int u = 0; u < w; ++u) h[0] = fmaf(maps[turn][u][0][lane], h[0], maps[turn][u][1][lane]);
+    r[0] = behind[turn][lane];
 #pragma unroll 4
-    for (int u = waves - 1; u > w; --u) back[0] = fmaf(maps[turn][u][0][lane], back[0], maps[turn][u][2][lane]);
-    r[0] = back[0];
-    if (tile > 0)
-#pragma unroll 4
-      for (int u = w; u >= 0; --u) back[0] = fmaf(maps[turn][u][0][lane], back[0], maps[turn][u][2][lane]);
+    for (int u = waves - 1; u > w; --u) r[0] = fmaf(maps[turn][u][0][lane], r[0], maps[turn][u][2][lane]);
+    if (!ONE && w == 0) back[0] = fmaf(A[0], r[0], R[0]);
     replay_back(a, at, steps, in, t0, h, r);
     if constexpr (ONE) return;
   }
@@ -613,10 +661,10 @@ __global__ __launch_bounds__(64 * kTileWaves, 8) void recurrence_grad_tiles_kern
   const bool mine = w == kTileWaves - 1;
   uint32_t turn, group;
   if (!take_tile(split, number, turn, group)) return;
-  const int64_t tile = split.tiles - 1 - turn, t0 = tile * kTile + w * kSpan;
+  const int tile = (int)(split.tiles - 1 - turn), t0 = tile * kTile + w * kSpan;
   const Group<V, RecurrenceGradArgs> at(a, group);
   if (tile * kTile >= at.length) {  // behind the entry's end
-    const int64_t end = t0 + kSpan < a.steps ? t0 + kSpan : a.steps;
+    const int end = t0 + kSpan < at.steps ? t0 + kSpan : at.steps;
     clear_rows(a, at, (T*)a.dgate, t0, end, 1, a.dgate_step, a.dgate_batch);
     clear_rows(a, at, (T*)a.dx, t0, end, 1, a.dx_step, a.dx_batch);
     if (t0 == 0 && a.dh0 && at.ch.any) {
@@ -626,12 +674,12 @@ __global__ __launch_bounds__(64 * kTileWaves, 8) void recurrence_grad_tiles_kern
     }
     return;
   }
-  const int64_t order = (at.length - 1) / kTile - tile;  // in the chain, which begins at the entry's end
+  const int order = (at.length - 1) / kTile - tile;  // in the chain, which begins at the entry's end
   GradInputs<T, V> in;
   in.ask(a, at, tile, t0);
-  Steps<T, MODE, V> steps;
-  steps.set(in.in, t0, at.length);
-  in.clear_behind(t0, at.length);
+  Steps<T, MODE, V, true> steps;
+  steps.set(in.in, at.length - t0);
+  in.clear_behind(at.length - t0);
   float A[V], B[V] = {0.0f}, R[V], h[V], r[V];
   steps.map(A, B);
   map_back(steps, in.d, R);
@@ -695,19 +743,21 @@ int64_t tiles_of(int64_t steps, int tile) { return (steps + tile - 1) / tile; }
 bool two_channels(int64_t batch, int64_t n) { return n % 2 == 0 && groups_of(batch, n, 1) > 256; }
 
 // The form with the least time, by measurement.  Per 128 steps a workgroup per group takes c0 us and all 256 that the card holds at once
-// c0 + c1; a workgroup per tile e for 256 groups, and 6.7 us more for clearing the marks, the second launch and the chain.  Steps x
-// channels, a workgroup per group and one per tile: 16-bit types 300 x 1024 9.5 and 11.0, 500 x 1024 11.7 and 10.2, 1000 x 8192 22.8 and
-// 18.0, 1000 x 12288 22.9 and 23.3, 3000 x 12288 65 and 55, 3000 x 16384 70 and 72, 1000 x 24576 36 and 43, 2000 x 33792 139 and 98;
-// float 1000 x 4096 20.2 and 16.7, 1000 x 12288 30.4 and 33.9; backward 200 x 1024 10.2 and 11.5, 1000 x 1024 33 and 12, 1000 x 16384
-// 44 and 52, 3000 x 12288 121 and 101, float 1000 x 24576 117 and 102.
+// c0 + c1; a workgroup per tile e for 256 groups, and 7.5 us more for clearing the marks, the second launch and the chain.  Steps x
+// channels, a workgroup per group and one per tile: 16-bit types 300 x 1024 8.4 and 10.0, 1000 x 1024 18.7 and 11.0, 1000 x 8192 20.3 and
+// 16.4, 1000 x 12288 21.1 and 21.4, 3000 x 12288 62 and 55, 3000 x 16384 67 and 69, 1000 x 24576 35 and 42; float 1000 x 4096 17.8 and
+// 15.4, 1000 x 12288 30.2 and 33.7; backward 200 x 1024 8.9 and 11.1, 1000 x 1024 28 and 11, 1000 x 16384 39 and 50, 3000 x 12288 109 and
+// 98, float 3000 x 8192 113 and 103, 1000 x 24576 107 and 102.  Beyond four rounds of the card the last one's share is small, and the
+// workspace would grow with the channels (64 of them to a tile, used or not).
 bool splits(int64_t batch, int64_t n, int64_t steps, bool wide, bool backward) {
   const bool pairs = !wide && !backward && two_channels(batch, n);
-  const double c0 = pairs ? 2.9 : wide ? backward ? 3.5 : 2.05 : backward ? 3.85 : 2.4;
-  const double c1 = pairs ? 2.1 : wide ? backward ? 5.0 : 2.5 : backward ? 1.5 : 0.6;
-  const double e = wide ? backward ? 7.8 : 4.6 : backward ? 5.2 : 2.7;
-  const int64_t g = groups_of(batch, n, pairs ? 2 : 1), last = g % 256;
+  const double c0 = pairs ? 2.6 : wide ? backward ? 2.7 : 1.75 : backward ? 3.25 : 2.1;
+  const double c1 = pairs ? 2.27 : wide ? backward ? 5.5 : 2.7 : backward ? 1.6 : 0.75;
+  const double e = wide ? backward ? 7.85 : 4.5 : backward ? 5.0 : 2.55;
+  const int64_t groups = groups_of(batch, n, 1), g = groups_of(batch, n, pairs ? 2 : 1), last = g % 256;
+  if (steps <= kTile || groups > 4 * 256) return false;
   const double one = (double)(g / 256) * (c0 + c1) + (last ? c0 + c1 * (double)last / 256 : 0.0);
-  return steps > kTile && (double)steps / kTile * (one - e * (double)groups_of(batch, n, 1) / 256) > 6.7;
+  return (double)steps / kTile * (one - e * (double)groups / 256) > 7.5;
 }
 
 hipError_t split_of(int64_t groups, int64_t tiles, void* ws, hipStream_t s, Split& out) {

@@ -194,7 +194,8 @@ class RecurrentBlock(_Block):
                                          self.next_bias], k, T, lr, momentum, max_norm)
 
     def forward(self, h, state=None, lengths=None):
-        """h [steps, batch, units] in float32, bfloat16 or float16; state [batch, units] float32 or None; lengths as in linear_recurrence
+        """h [steps, batch, units] in float32, bfloat16 or float16; state [batch, units] float32 or None; lengths as in linear_recurrence (of
+        padding the recurrence reads nothing; the rest of the block works row by row, so it has to be finite and to stay out of the loss)
         -> the residual stream behind the block, the same normed for the next one, the last state."""
         n = self.units
         W1, W2 = (binding.fake_quantize(W, self.k, self.T).to(h.dtype) for W in self.matrices)

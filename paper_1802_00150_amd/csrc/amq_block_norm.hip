@@ -15,7 +15,7 @@
 //
 // Measured (a large copy 5.1 TB/s): 8960 x 1024 half 17.6 us, 5.2 TB/s (part of it stays in the memory-side cache); backward 8960 x 1500
 // bfloat16 with a float residual 59 us, 5.0, and 5 for the second launch; 8960 x 1024 bfloat16 backward 43, 3.4, with vector
-// instructions (87 per entry) and latency in the way.
+// instructions (some 80 per entry) and latency in the way.
 #include "../../include/amq.h"
 
 #include <type_traits>

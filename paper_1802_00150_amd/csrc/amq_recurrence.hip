@@ -4,8 +4,8 @@
 //   decay   h_t = a_t h_{t-1} + x_t, the factor a given
 //   back    e_t = dh_t + f_{t+1} e_{t+1} (from dh_last):  dx = i e,  dg = e (h_{t-1} - x) f i;  decay: dx = e, da = e h_{t-1}
 //
-// About 30 vector operations per entry forward and 50 backward (exponential and reciprocal count four each), against 6 and 10 bytes
-// (16-bit types): bound by memory once enough is under way, by latency for few entries.  A step is an affine map of the
+// 27 vector instructions per entry forward and 45 backward, against 6 and 10 bytes (16-bit types): bound by memory once enough is under way
+// (backward with 16-bit types by instructions as much), by latency for few entries.  A step is an affine map of the
 // state, so time is split: the 8 steps of a wave are read at once, turned into one map (factor A, offset B) from a zero state, the waves
 // of a workgroup exchange those through LDS, every wave folds the ones before it onto the state and replays its steps, which are still
 // in registers, from the state they really start in.  So inputs are read once, and the results' error is that of steps one after the
@@ -15,9 +15,9 @@
 // workgroup: it leaves its map in memory, looks back for the nearest tile whose end state is there, folds the maps between and leaves its
 // own end state ("Tiles of one sequence" below).
 //
-// Measured (steps x channels; a large copy 5.1 TB/s): 2000 x 16384 float 78 us, 5.05 TB/s; 1000 x 32768 bfloat16 40 us, 4.9; 35 x 262144
-// backward 21.4, 4.4; long sequences with the chain 32768 x 1024 bfloat16 56, 3.6; 4001 x 2100 float 28, 3.6, backward 50, 3.4;
-// 2000 x 8192 float backward 72, 4.6.
+// Measured (steps x channels; a large copy 5.1 TB/s): 2000 x 16384 float 78 us, 5.05 TB/s; 1000 x 32768 bfloat16 39.5 us, 5.0; 35 x 262144
+// backward 19.7, 4.8; 1000 x 16384 backward 39, 4.2; with the chain 32768 x 1024 bfloat16 55, 3.65; 4001 x 2100 float 28.6, 3.5, backward
+// 50, 3.4; 2000 x 8192 float backward 71, 4.6.
 //
 // The backward pass takes h_{t-1} in full precision from the states that the forward pass leaves in front of every 128th
 // step (4 / 128 bytes per entry instead of the 2 of reading rounded states): each tile replays the recurrence from there.
@@ -738,7 +738,7 @@ int64_t groups_of(int64_t batch, int64_t n, int V) { return batch * ((n + 64 * V
 int64_t tiles_of(int64_t steps, int tile) { return (steps + tile - 1) / tile; }
 
 // Channels of a lane: two of 16 bits where a workgroup walks over tiles forward and groups of 64 channels are more than the card holds at
-// once (300 x 17408 14.9 us, with one 18.4; 1000 x 32768 40 and 50; but 2000 x 16384 65 and 48); one otherwise (35 x 262144 backward 21.2,
+// once (300 x 17408 13.9 us, with one 16.8; 1000 x 32768 41 and 48; but 2000 x 16384 62 and 46); one otherwise (35 x 262144 backward 21.2,
 // with two 23.8).
 bool two_channels(int64_t batch, int64_t n) { return n % 2 == 0 && groups_of(batch, n, 1) > 256; }
 

@@ -635,6 +635,16 @@ def linear_recurrence_backward_workspace(steps, batch, n, dtype, device):
                        device=device)
 
 
+def refuse_held(name, *operands):
+    """Raises where a graph is captured whose gradients would end in leaves that a graph recorded on another stream still holds: torch's backward pass
+    would make the capture wait for that stream, which ends the process."""
+    if not any(isinstance(t, torch.Tensor) and t.is_cuda for t in operands) or not torch.cuda.is_current_stream_capturing():
+        return
+    if (_native_module or _load_native()).held_elsewhere(operands):
+        raise AmqError("%s: a leaf's gradient belongs to a graph recorded on another stream that is still alive; delete its results, or capture with "
+                       "detached leaves" % name)
+
+
 GATES = (None, "none", "sigmoid", "silu")
 
 

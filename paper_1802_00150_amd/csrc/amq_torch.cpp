@@ -9,12 +9,15 @@
 
 #include <initializer_list>
 #include <string>
+#include <set>
 #include <vector>
 
 #include <ATen/hip/EmptyTensor.h>
 #include <c10/core/DeviceGuard.h>
+#include <c10/core/impl/VirtualGuardImpl.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/custom_function.h>
+#include <torch/csrc/autograd/functions/accumulate_grad.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "../../include/amq.h"
@@ -975,6 +978,33 @@ PyObject* clip_gradients(PyObject* const* a) {  // list of tensors, list of resu
   return wrap(norm);
 }
 
+// Whether the gradients of a tuple's tensors end in leaves that a graph recorded on another stream than the current one holds too.
+PyObject* held_elsewhere(PyObject* const* a) {
+  if (!PyTuple_Check(a[0])) fail(PyExc_TypeError, "expected a tuple");
+  std::vector<std::shared_ptr<torch::autograd::Node>> open;
+  std::set<torch::autograd::Node*> seen;
+  auto meet = [&](const std::shared_ptr<torch::autograd::Node>& n) {
+    if (n && seen.insert(n.get()).second) open.push_back(n);
+  };
+  for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(a[0]); ++i) {
+    PyObject* o = PyTuple_GET_ITEM(a[0], i);
+    if (o == Py_None) continue;
+    const at::Tensor& t = tensor(o);
+    if (!t.requires_grad()) continue;
+    meet(t.is_leaf() ? torch::autograd::impl::try_get_grad_accumulator(t) : t.grad_fn());
+  }
+  while (!open.empty()) {
+    const std::shared_ptr<torch::autograd::Node> n = open.back();
+    open.pop_back();
+    if (dynamic_cast<torch::autograd::AccumulateGrad*>(n.get())) {
+      const auto s = n->stream();
+      if (s && *s != c10::impl::VirtualGuardImpl(s->device_type()).getStream(s->device())) Py_RETURN_TRUE;
+    }
+    for (const torch::autograd::Edge& e : n->next_edges()) meet(e.function);
+  }
+  Py_RETURN_FALSE;
+}
+
 // ---- module
 
 template <PyObject* (*F)(PyObject* const*), int N>
@@ -1028,7 +1058,7 @@ PyMethodDef methods[] = {
     AMQ_METHOD(lm_sequence_score, 21), AMQ_METHOD(dequantize, 4), AMQ_METHOD(fake_quantize, 3),
     AMQ_METHOD(layer_norm, 5), AMQ_METHOD(layer_norm_backward, 8), AMQ_METHOD(linear, 8), AMQ_METHOD(linear_backward, 7),
     AMQ_METHOD(orthogonalize, 8), AMQ_METHOD(linear_recurrence, 9), AMQ_METHOD(linear_recurrence_backward, 11), AMQ_METHOD(block_norm, 13),
-    AMQ_METHOD(block_norm_backward, 14), AMQ_METHOD(clip_gradients, 4),
+    AMQ_METHOD(block_norm_backward, 14), AMQ_METHOD(clip_gradients, 4), AMQ_METHOD(held_elsewhere, 1),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_amq_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

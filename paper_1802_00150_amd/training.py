@@ -86,7 +86,9 @@ class _LinearRecurrence(torch.autograd.Function):
 
 
 def linear_recurrence(gate, x, h0=None, mode="blend", lengths=None):
-    """binding.linear_recurrence's states and last state, differentiable in gate, x and h0."""
+    """binding.linear_recurrence's states and last state, differentiable in gate, x and h0.  Forward and backward may be captured into one graph
+    where no graph of the same leaves lives that was recorded outside (refused)."""
+    binding.refuse_held("linear_recurrence", gate, x, h0)
     return _LinearRecurrence.apply(gate, x, h0, mode, lengths)
 
 
@@ -114,7 +116,8 @@ class _BlockNorm(torch.autograd.Function):
 
 def block_norm(x, residual, weight=None, bias=None, gate=None, activation="sigmoid", scale=None, next_weight=None, next_bias=None,
                eps=1e-5):
-    """binding.block_norm's y and normed y, differentiable in x, residual, gate and the parameters."""
+    """binding.block_norm's y and normed y, differentiable in x, residual, gate and the parameters.  Captured as linear_recurrence is."""
+    binding.refuse_held("block_norm", x, residual, gate, weight, bias, scale, next_weight, next_bias)
     return _BlockNorm.apply(x, residual, gate, weight, bias, scale, next_weight, next_bias, activation, eps)
 
 

@@ -1,4 +1,6 @@
 """The recurrent block's operators as they are used together: a training step, its gradients, and single tokens with the state handed on."""
+import gc
+
 import pytest
 import torch
 
@@ -132,6 +134,41 @@ def test_autograd_forms(amq, training, dtype):
     y2, n2, stats = amq.block_norm(a, r.detach(), weight.detach())
     want = amq.block_norm_backward(None, (2 * n2.float()).to(dtype), a, y2, stats, weight.detach())
     assert torch.equal(dr, want[1]) and torch.equal(dw, want[3])
+
+
+def test_captured_with_its_gradients(amq, training):
+    """Forward and backward in one graph; refused where an eager graph holds the same leaves (also behind another operation), since torch's backward
+    pass would then end the process."""
+    T, B, n = 40, 3, 48
+    gate, x, weight = rand(1, T, B, n).to(DEV).requires_grad_(), rand(2, T, B, n).to(DEV), torch.ones(n, device=DEV).requires_grad_()
+    w = rand(3, T, B, n).to(DEV)
+
+    def both():
+        hs, _ = training.linear_recurrence(gate * 1.0, x)
+        y, normed = training.block_norm(hs.view(-1, n), x.view(-1, n), weight)
+        return (y.detach(),) + torch.autograd.grad((normed.view(T, B, n) * w).sum(), [gate, weight])
+
+    stream = torch.cuda.Stream()
+    for eager in (lambda: training.linear_recurrence(gate, x), lambda: training.block_norm(x.view(-1, n), x.view(-1, n), weight * 1.0)):
+        alive = eager()
+        torch.cuda.synchronize()
+        with pytest.raises(amq.AmqError, match="still alive"), torch.cuda.graph(torch.cuda.CUDAGraph(), stream=stream):
+            both()
+        del alive
+        gc.collect()  # (the exception's frames hold what was recorded)
+    with torch.cuda.stream(stream):
+        both()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        out = both()
+    for i in range(4):
+        x.copy_(rand(20 + i, T, B, n))
+        graph.replay()
+        torch.cuda.synchronize()
+        want = both()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(out, want)), i
 
 
 def test_the_module_runs(training, capsys):

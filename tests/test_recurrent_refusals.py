@@ -128,3 +128,18 @@ def test_clip_gradients(L):
     assert run(p, [10, 20, 30, (1 << 40) + 1], types) == UNSUPPORTED
     assert run([], [], [], count=(1 << 20) + 1) in (INVALID, UNSUPPORTED)
 
+
+
+def test_recurrence_workspaces(L):
+    """None for one tile, for single tokens and where the channels fill the card by far; else 12 bytes for 64 channels of every tile and what they need
+    beside it, whether batch entries count as channels or not."""
+    for f in (L.amq_linear_recurrence_workspace_bytes, L.amq_linear_recurrence_backward_workspace_bytes):
+        for type in (F32, BF16, F16):
+            for steps, B, n in ((1, 1, 1), (128, 1, 1), (128, 256, 1024), (1000, 1 << 22, 1), (300, 1 << 20, 3), (1 << 24, 1 << 10, 1 << 17)):
+                assert f(steps, B, n, type) == 0, (steps, B, n)
+            need = f(1 << 24, 1, 64, type)
+            assert need % 256 == 0 and 0 < need <= (1 << 17) * (64 * 12 + 4) + 8192
+            assert f(20000, 4, 64, type) > 0
+            for bad in ((0, 1, 1), (1, 0, 1), (1, 1, -1), ((1 << 24) + 1, 1, 1)):
+                assert f(*bad, type) == 0
+        assert f(1000, 1, 1, 3) == 0

@@ -569,6 +569,7 @@ int amq_orthogonalize(const void* G, int64_t batch, int64_t batch_stride, int64_
  * h0 (dh0 float, may be NULL): with e_t = dhs_t + f_{t+1} e_{t+1},  dx = (1 - f) e,  dgate = e (h_{t-1} - x) f (1 - f),  dh0 = f_0 e_0;
  * of a decay  dx = e,  dgate = e h_{t-1}.  h_{t-1} is formed again in binary32 from `states` (NULL up to 128 steps).  Behind lengths[b] dhs is not read, and
  * dgate and dx are 0.
+ * States are meant to be finite: an infinite one turns into NaN at the next step of a blend whose gate is not negative (padding leaves it).
  * Results do not depend on the order of execution.  Where there are too few channels to fill the card, tiles of steps have workgroups of
  * their own, each of which waits for earlier ones that have begun already; one that had waited for seconds would leave NaN.
  * AMQ_ERR_UNSUPPORTED beyond 2^24 steps, 2^22 batch entries, 2^20 channels, 2^30 of both, strides of 2^36.

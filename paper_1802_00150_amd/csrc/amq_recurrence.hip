@@ -63,7 +63,7 @@ struct Step {
     }
   }
   __device__ __forceinline__ void hold() {
-    p = MODE == AMQ_RECURRENCE_BLEND ? -0.0f : 1.0f;
+    p = 1.0f;  // (times the state, which may be infinite)
     i = v = 0.0f;
   }
   __device__ __forceinline__ float held(float h) const { return __float_as_int(p) < 0 ? h : 0.0f; }

@@ -220,6 +220,25 @@ def test_a_nan_stays_in_its_channel_and_behind_its_step(amq):
         assert torch.equal(got, good)
 
 
+@pytest.mark.parametrize("T,B,n", [(30, 3, 70), (300, 3, 70), (3000, 3, 70), (300, 300, 70)])
+@pytest.mark.parametrize("mode", MODES)
+def test_padding_holds_what_an_entry_ends_in(amq, T, B, n, mode):
+    """Also an infinity or NaN of its last step, in every form of the launch; its neighbours know nothing of it."""
+    gate, x, h0 = case(10, T, B, n, torch.float32, mode)
+    lengths = torch.tensor([T, max(1, T // 2), max(1, T // 2 - 3)]).repeat(B // 3 + 1)[:B]
+    clean = amq.linear_recurrence(gate.to(DEV), x.to(DEV), h0.to(DEV), mode=mode, lengths=lengths.to(DEV))[1].cpu()
+    bad = x.clone()
+    for b in range(B):
+        bad[lengths[b] - 1, b, 5] = float("inf")
+        bad[lengths[b] - 1, b, 69] = float("nan")
+    hs, last, _ = amq.linear_recurrence(gate.to(DEV), bad.to(DEV), h0.to(DEV), mode=mode, lengths=lengths.to(DEV))
+    last, hs = last.cpu(), hs.cpu()
+    assert bool((last[:, 5] == float("inf")).all()) and bool(torch.isnan(last[:, 69]).all())
+    assert all(bool((hs[lengths[b]:, b] == 0).all()) for b in range(B))
+    last[:, [5, 69]] = clean[:, [5, 69]]
+    assert torch.equal(last, clean)
+
+
 @pytest.mark.parametrize("mode", MODES)
 def test_gradients_against_differences(amq, mode):
     """Central differences of the binary64 plain form; their own error is of order step^2."""

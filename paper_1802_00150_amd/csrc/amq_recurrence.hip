@@ -383,7 +383,7 @@ template <typename T, int MODE, int V, bool ONE>
 __global__ __launch_bounds__(64 * kTileWaves, ONE ? 8 : 4) void recurrence_kernel(RecurrenceArgs a) {
   __shared__ float maps[ONE ? 1 : 2][kTileWaves][2][64 * V];
   const int w = __builtin_amdgcn_readfirstlane(wave_id()), waves = blockDim.x / 64, lane = lane_id();
-  const Group<V, RecurrenceArgs> at(a, blockIdx.x);
+  const Group<V, RecurrenceArgs> at(a, a.first + blockIdx.x);
   Inputs<T, V> in;
   Steps<T, MODE, V, false> steps;
   float carry[V];  // (wave 0 alone has it, and reads h0: h_last, written behind a barrier, may lie there)
@@ -603,7 +603,7 @@ __global__ __launch_bounds__(64 * kTileWaves, ONE ? 8 : 4) void recurrence_grad_
   constexpr int V = 1;
   __shared__ float maps[ONE ? 1 : 2][kTileWaves][3][64];
   const int w = __builtin_amdgcn_readfirstlane(wave_id()), waves = blockDim.x / 64, lane = lane_id();
-  const Group<V, RecurrenceGradArgs> at(a, blockIdx.x);
+  const Group<V, RecurrenceGradArgs> at(a, a.first + blockIdx.x);
   __shared__ float behind[ONE ? 1 : 2][64];
   float back[V];  // wave 0: the gradient that reaches a tile's last state from the steps behind it
   if (w == 0) given<V>(a.dh_last, at, back);
@@ -769,21 +769,38 @@ hipError_t split_of(int64_t groups, int64_t tiles, void* ws, hipStream_t s, Spli
   split_clear_kernel<<<dim3((unsigned)(words / 1024 < 256 ? words / 1024 + 1 : 256)), dim3(256), 0, s>>>(out.counter, words);
   return hipGetLastError();
 }
+// A grid has less than 2^32 threads: more workgroups (batches of millions of entries, millions of steps of a thousand) take several launches, each
+// but the last of a multiple of `of` workgroups.
+constexpr int64_t kMostThreads = 1LL << 31;
+template <typename F>
+hipError_t launch_parts(int64_t blocks, int64_t of, int waves, F launch) {
+  const int64_t most = kMostThreads / (64 * waves) / of * of;
+  for (int64_t first = 0; first < blocks; first += most) {
+    launch(first, blocks - first < most ? blocks - first : most);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
 template <typename A, typename F>
 hipError_t launch_tiles(const A& a, int tile, hipStream_t s, F kernel) {
   const int64_t groups = groups_of(a.batch, a.n, 1);
   Split split;
   const hipError_t e = split_of(groups, tiles_of(a.steps, tile), a.ws, s, split);
   if (e != hipSuccess) return e;
-  // as many workgroups for every counter as the one with the most tiles needs
-  const int64_t most = (groups + split.kinds - 1) / split.kinds * split.tiles;
-  kernel<<<dim3((unsigned)(split.kinds * most)), dim3(64 * kTileWaves), 0, s>>>(a, split);
-  return hipGetLastError();
+  // as many workgroups for every counter as the one with the most tiles needs; the counters run on from launch to launch
+  const int64_t blocks = (groups + split.kinds - 1) / split.kinds * split.tiles * split.kinds;
+  return launch_parts(blocks, split.kinds, kTileWaves, [&](int64_t, int64_t part) {
+    kernel<<<dim3((unsigned)part), dim3(64 * kTileWaves), 0, s>>>(a, split);
+  });
 }
 template <typename A, typename F>
-hipError_t launch_groups(const A& a, int channels, bool even, hipStream_t s, F kernel) {
-  kernel<<<dim3((unsigned)groups_of(a.batch, a.n, channels)), dim3(64 * waves_of(a.steps, even)), 0, s>>>(a);
-  return hipGetLastError();
+hipError_t launch_groups(A a, int channels, bool even, hipStream_t s, F kernel) {
+  const int waves = waves_of(a.steps, even);
+  return launch_parts(groups_of(a.batch, a.n, channels), 1, waves, [&](int64_t first, int64_t part) {
+    a.first = (uint32_t)first;
+    kernel<<<dim3((unsigned)part), dim3(64 * waves), 0, s>>>(a);
+  });
 }
 // (batch entries may count as channels of one entry in the launch, so the larger need of either)
 size_t workspace(int64_t steps, int64_t batch, int64_t n, int type, bool backward) {

@@ -383,7 +383,7 @@ template <typename T, int MODE, int V, bool ONE>
 __global__ __launch_bounds__(64 * kTileWaves, ONE ? 8 : 4) void recurrence_kernel(RecurrenceArgs a) {
   __shared__ float maps[ONE ? 1 : 2][kTileWaves][2][64 * V];
   const int w = __builtin_amdgcn_readfirstlane(wave_id()), waves = blockDim.x / 64, lane = lane_id();
-  const Group<V, RecurrenceArgs> at(a, a.first + blockIdx.x);
+  const Group<V, RecurrenceArgs> at(a, blockIdx.x);
   Inputs<T, V> in;
   Steps<T, MODE, V, false> steps;
   float carry[V];  // (wave 0 alone has it, and reads h0: h_last, written behind a barrier, may lie there)
@@ -603,7 +603,7 @@ __global__ __launch_bounds__(64 * kTileWaves, ONE ? 8 : 4) void recurrence_grad_
   constexpr int V = 1;
   __shared__ float maps[ONE ? 1 : 2][kTileWaves][3][64];
   const int w = __builtin_amdgcn_readfirstlane(wave_id()), waves = blockDim.x / 64, lane = lane_id();
-  const Group<V, RecurrenceGradArgs> at(a, a.first + blockIdx.x);
+  const Group<V, RecurrenceGradArgs> at(a, blockIdx.x);
   __shared__ float behind[ONE ? 1 : 2][64];
   float back[V];  // wave 0: the gradient that reaches a tile's last state from the steps behind it
   if (w == 0) given<V>(a.dh_last, at, back);
@@ -769,18 +769,33 @@ hipError_t split_of(int64_t groups, int64_t tiles, void* ws, hipStream_t s, Spli
   split_clear_kernel<<<dim3((unsigned)(words / 1024 < 256 ? words / 1024 + 1 : 256)), dim3(256), 0, s>>>(out.counter, words);
   return hipGetLastError();
 }
-// A grid has less than 2^32 threads: more workgroups (batches of millions of entries, millions of steps of a thousand) take several launches, each
-// but the last of a multiple of `of` workgroups.
-constexpr int64_t kMostThreads = 1LL << 31;
-template <typename F>
-hipError_t launch_parts(int64_t blocks, int64_t of, int waves, F launch) {
-  const int64_t most = kMostThreads / (64 * waves) / of * of;
-  for (int64_t first = 0; first < blocks; first += most) {
-    launch(first, blocks - first < most ? blocks - first : most);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
-  return hipSuccess;
+// A grid has less than 2^32 threads, which batches of millions of entries and millions of steps of a thousand pass: those take several launches.
+int64_t most_blocks(int waves) { return 0xffffffffLL / (64 * waves); }
+// The batch from entry b on.  (`batch` stays what it is: the states in front of two tiles are that many entries apart.)
+RecurrenceArgs from_entry(RecurrenceArgs a, int64_t b) {
+  const int64_t size = a.type == AMQ_F32 ? 4 : 2;
+  a.gate = (const char*)a.gate + b * a.gate_batch * size;
+  a.x = (const char*)a.x + b * a.x_batch * size;
+  a.hs = (char*)a.hs + b * a.hs_batch * size;
+  if (a.lengths) a.lengths += b;
+  if (a.h0) a.h0 += b * a.n;
+  if (a.h_last) a.h_last += b * a.n;
+  if (a.states) a.states += b * a.n;
+  return a;
+}
+RecurrenceGradArgs from_entry(RecurrenceGradArgs a, int64_t b) {
+  const int64_t size = a.type == AMQ_F32 ? 4 : 2;
+  a.dhs = (const char*)a.dhs + b * a.dhs_batch * size;
+  a.gate = (const char*)a.gate + b * a.gate_batch * size;
+  a.x = (const char*)a.x + b * a.x_batch * size;
+  a.dgate = (char*)a.dgate + b * a.dgate_batch * size;
+  a.dx = (char*)a.dx + b * a.dx_batch * size;
+  if (a.lengths) a.lengths += b;
+  if (a.h0) a.h0 += b * a.n;
+  if (a.states) a.states += b * a.n;
+  if (a.dh_last) a.dh_last += b * a.n;
+  if (a.dh0) a.dh0 += b * a.n;
+  return a;
 }
 template <typename A, typename F>
 hipError_t launch_tiles(const A& a, int tile, hipStream_t s, F kernel) {
@@ -789,18 +804,25 @@ hipError_t launch_tiles(const A& a, int tile, hipStream_t s, F kernel) {
   const hipError_t e = split_of(groups, tiles_of(a.steps, tile), a.ws, s, split);
   if (e != hipSuccess) return e;
   // as many workgroups for every counter as the one with the most tiles needs; the counters run on from launch to launch
-  const int64_t blocks = (groups + split.kinds - 1) / split.kinds * split.tiles * split.kinds;
-  return launch_parts(blocks, split.kinds, kTileWaves, [&](int64_t, int64_t part) {
-    kernel<<<dim3((unsigned)part), dim3(64 * kTileWaves), 0, s>>>(a, split);
-  });
+  int64_t blocks = (groups + split.kinds - 1) / split.kinds * split.tiles * split.kinds;
+  for (const int64_t most = most_blocks(kTileWaves) / split.kinds * split.kinds; blocks > 0; blocks -= most) {
+    kernel<<<dim3((unsigned)(blocks < most ? blocks : most)), dim3(64 * kTileWaves), 0, s>>>(a, split);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 template <typename A, typename F>
-hipError_t launch_groups(A a, int channels, bool even, hipStream_t s, F kernel) {
+hipError_t launch_groups(const A& a, int channels, bool even, hipStream_t s, F kernel) {
   const int waves = waves_of(a.steps, even);
-  return launch_parts(groups_of(a.batch, a.n, channels), 1, waves, [&](int64_t first, int64_t part) {
-    a.first = (uint32_t)first;
-    kernel<<<dim3((unsigned)part), dim3(64 * waves), 0, s>>>(a);
-  });
+  const int64_t pieces = groups_of(1, a.n, channels), most = most_blocks(waves) / pieces;  // of an entry; entries of a launch
+  for (int64_t b = 0; b < a.batch; b += most) {
+    const int64_t entries = a.batch - b < most ? a.batch - b : most;
+    kernel<<<dim3((unsigned)(entries * pieces)), dim3(64 * waves), 0, s>>>(from_entry(a, b));
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 // (batch entries may count as channels of one entry in the launch, so the larger need of either)
 size_t workspace(int64_t steps, int64_t batch, int64_t n, int type, bool backward) {
@@ -815,6 +837,12 @@ size_t workspace(int64_t steps, int64_t batch, int64_t n, int type, bool backwar
 }
 
 }  // namespace
+
+bool recurrence_entries_join(int64_t steps, int64_t channels, int type, bool backward) {
+  if (splits(1, channels, steps, type == AMQ_F32, backward)) return true;
+  const bool pairs = type != AMQ_F32 && !backward && steps > kTile && two_channels(1, channels);
+  return groups_of(1, channels, pairs ? 2 : 1) <= most_blocks(waves_of(steps, !backward));
+}
 
 size_t recurrence_workspace(int64_t steps, int64_t batch, int64_t n, int type) { return workspace(steps, batch, n, type, false); }
 size_t recurrence_grad_workspace(int64_t steps, int64_t batch, int64_t n, int type) { return workspace(steps, batch, n, type, true); }

@@ -76,8 +76,9 @@ struct RecurrenceArgs {
   const float* h0;                // null: zeros
   float *h_last, *states;         // null where not wanted
   void* ws;
-  uint32_t first = 0;             // group of channels that a launch begins with
 };
+// Whether one launch has room for `channels`, so that batch entries side by side may count as channels of one wider entry.
+bool recurrence_entries_join(int64_t steps, int64_t channels, int type, bool backward);
 size_t recurrence_workspace(int64_t steps, int64_t batch, int64_t n, int type);
 hipError_t launch_recurrence(const RecurrenceArgs& a, hipStream_t s);
 
@@ -90,7 +91,6 @@ struct RecurrenceGradArgs {
   const float *h0, *states, *dh_last;  // h0, dh_last: null for zeros; states: null up to AMQ_STATE_STEPS steps
   float* dh0;                          // null where not wanted
   void* ws;
-  uint32_t first = 0;
 };
 size_t recurrence_grad_workspace(int64_t steps, int64_t batch, int64_t n, int type);
 hipError_t launch_recurrence_grad(const RecurrenceGradArgs& a, hipStream_t s);

@@ -298,7 +298,7 @@ int amq_linear_recurrence(const void* gate, int64_t gate_step, int64_t gate_batc
     return AMQ_ERR_INVALID;
   if (!workspace_ok(workspace, workspace_bytes, amq::recurrence_workspace(steps, B, n, type))) return AMQ_ERR_INVALID;
   // batch entries side by side are channels of one wider entry
-  if (!lengths && (B == 1 || (gate_batch == n && x_batch == n && hs_batch == n))) n *= B, B = 1;
+  if (!lengths && B > 1 && gate_batch == n && x_batch == n && hs_batch == n && amq::recurrence_entries_join(steps, B * n, type, false)) n *= B, B = 1;
   return amq::status_of(amq::launch_recurrence({gate, x, hs, gate_step, gate_batch, x_step, x_batch, hs_step, hs_batch, steps, B, (int)n, type, mode,
                                                 lengths, h0, h_last, states, workspace},
                                                static_cast<hipStream_t>(stream)));
@@ -336,7 +336,9 @@ int amq_linear_recurrence_backward(const void* dhs, int64_t dhs_step, int64_t dh
   if (meets(rg, {ed, eg, ex, h, st, dl, len, rx, r0}) || meets(rx, {ed, eg, ex, h, st, dl, len, r0}) || meets(r0, {ed, eg, ex, h, st, dl, len}))
     return AMQ_ERR_INVALID;
   if (!workspace_ok(workspace, workspace_bytes, amq::recurrence_grad_workspace(steps, B, n, type))) return AMQ_ERR_INVALID;
-  if (!lengths && (B == 1 || (dhs_batch == n && gate_batch == n && x_batch == n && dgate_batch == n && dx_batch == n))) n *= B, B = 1;
+  if (!lengths && B > 1 && dhs_batch == n && gate_batch == n && x_batch == n && dgate_batch == n && dx_batch == n &&
+      amq::recurrence_entries_join(steps, B * n, type, true))
+    n *= B, B = 1;
   return amq::status_of(amq::launch_recurrence_grad({dhs, gate, x, dgate, dx, dhs_step, dhs_batch, gate_step, gate_batch, x_step, x_batch, dgate_step,
                                                      dgate_batch, dx_step, dx_batch, steps, B, (int)n, type, mode, lengths, h0, states, dh_last,
                                                      dh0, workspace},

@@ -555,7 +555,7 @@ int amq_orthogonalize(const void* G, int64_t batch, int64_t batch_stride, int64_
  * Linear recurrences: every channel of every batch entry has a state of its own, and no product of the state stands between two
  * steps, so that a whole sequence is one pass.
  *   AMQ_RECURRENCE_BLEND: f = sigmoid(gate_t), h_t = f h_{t-1} + (1 - f) x_t   (the update of amq_gru_step, its gate given)
- *   AMQ_RECURRENCE_DECAY: h_t = gate_t h_{t-1} + x_t   (products of the factors over any 256 steps must be finite)
+ *   AMQ_RECURRENCE_DECAY: h_t = gate_t h_{t-1} + x_t
  *   gate, x, hs [steps][B][n] of `type`, n entries side by side, steps and batch entries *_step and *_batch elements apart, any alignment: columns of a
  *   wider projection and tensors whose outer dimension is the batch are taken as they are (gate and x also with strides of 0)
  *   lengths [B] int64 or NULL: entry b has lengths[b] steps (taken as 0 below 0 and as `steps` above).  gate and x behind them are
@@ -569,7 +569,10 @@ int amq_orthogonalize(const void* G, int64_t batch, int64_t batch_stride, int64_
  * h0 (dh0 float, may be NULL): with e_t = dhs_t + f_{t+1} e_{t+1},  dx = (1 - f) e,  dgate = e (h_{t-1} - x) f (1 - f),  dh0 = f_0 e_0;
  * of a decay  dx = e,  dgate = e h_{t-1}.  h_{t-1} is formed again in binary32 from `states` (NULL up to 128 steps).  Behind lengths[b] dhs is not read, and
  * dgate and dx are 0.
- * States are meant to be finite: an infinite one turns into NaN at the next step of a blend whose gate is not negative (padding leaves it).
+ * States are binary32.  An infinite one stays infinite (a factor that binary32 holds as 0 makes it NaN), and factors may be above 1, also where their products
+ * pass binary32 and the states do not: a channel that a product or an infinity spoils is formed again step by step, some microseconds per 128 steps.
+ * A state is otherwise formed from one of up to 256 steps before through the product of the factors between, which binary32 holds to multiples of
+ * 2^-149: what has decayed by more than 2^-126 may be off by 2^-150 of the state that it comes from, which the factors behind carry on as they carry the state.
  * Results do not depend on the order of execution.  Where there are too few channels to fill the card, tiles of steps have workgroups of
  * their own, each of which waits for earlier ones that have begun already; one that had waited for seconds would leave NaN.
  * AMQ_ERR_UNSUPPORTED beyond 2^24 steps, 2^22 batch entries, 2^20 channels, 2^30 of both, strides of 2^36.

@@ -616,7 +616,10 @@ def linear_recurrence(gate, x, h0=None, mode="blend", lengths=None, states=False
     mode "blend": f = sigmoid(gate_t), h_t = f h_{t-1} + (1 - f) x_t;  "decay": h_t = gate_t h_{t-1} + x_t.
     gate, x [steps, batch, n]: float32, bfloat16 or float16, channels side by side, other strides as they are (columns of a wider projection;
     a batch-first tensor transposed).  h0 [batch, n] float32, None for zeros.  lengths [batch] int64: entry b has lengths[b] steps, behind which
-    nothing is read, hs is 0 and the state stays.  h_out receives the last state and may be h0 itself."""
+    nothing is read, hs is 0 and the state stays.  h_out receives the last state and may be h0 itself.
+    States are float32: infinite ones stay infinite, factors of "decay" may be above 1 (and their products pass float32 where the states do
+    not), both at the price of forming those channels step by step.  What has decayed by more than 2^-126 may be off by 2^-150 of what it comes from (as
+    include/amq.h has it)."""
     return (_native_module or _load_native()).linear_recurrence(gate, x, h0, _recurrence(mode), lengths, 1 if states else 0, ws, out, h_out)
 
 

@@ -43,6 +43,8 @@ constexpr int kLongSpan = 16, kLongTile = kLongSpan * kTileWaves;  // of tiles w
 static_assert(kLongTile % AMQ_STATE_STEPS == 0 && AMQ_STATE_STEPS % kLongSpan == 0, "states are left behind a wave's steps");
 static_assert(kTile == AMQ_STATE_STEPS, "a backward tile begins where a state was left");
 
+__device__ __forceinline__ bool is_finite(float v) { return fabsf(v) < __builtin_inff(); }  // (false for NaN)
+
 // What a step does to the state.  BACK: in the backward pass, which needs i and x apart.
 template <int MODE, bool BACK>
 struct Step {
@@ -71,6 +73,16 @@ struct Step {
   __device__ __forceinline__ float next(float h) const {
     if constexpr (MODE == AMQ_RECURRENCE_BLEND) return fmaf(p, h, BACK ? fmaf(i, v, held(h)) : v + held(h));
     return fmaf(p, h, v);
+  }
+  // next() and keep() where they leave the finite numbers: f h by itself, since h - i h of an infinite state is NaN and h + i x may pass the
+  // range that f h + i x is in.
+  __device__ __forceinline__ float next_exact(float h) const {
+    const float n = next(h);
+    return MODE == AMQ_RECURRENCE_BLEND && !is_finite(n) && __float_as_int(p) < 0 ? fmaf(1.0f + p, h, BACK ? i * v : v) : n;
+  }
+  __device__ __forceinline__ float keep_exact(float h) const {
+    const float n = keep(h);
+    return MODE == AMQ_RECURRENCE_BLEND && !is_finite(n) && __float_as_int(p) < 0 ? (1.0f + p) * h : n;
   }
   __device__ __forceinline__ float dx(float e) const { return MODE == AMQ_RECURRENCE_BLEND ? i * e : e; }
   __device__ __forceinline__ float dgate(float e, float h) const {
@@ -110,6 +122,13 @@ struct Lane {
   __device__ __forceinline__ void put(T* row, const float (&v)[V]) const {
     store_whole<T, V>(reinterpret_cast<T*>(reinterpret_cast<char*>(row) + first * (uint32_t)sizeof(T)), v);
   }
+  // those of them that are `wanted`
+  template <typename T>
+  __device__ __forceinline__ void put(T* row, const float (&v)[V], const bool (&wanted)[V]) const {
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+      if (any && wanted[j]) row[first + j] = (T)v[j];
+  }
 };
 
 // ---- Tiles of one sequence in workgroups of their own.
@@ -141,9 +160,11 @@ __device__ __forceinline__ void leave_map(const Chain& c, int64_t tile, float A,
 __device__ __forceinline__ void leave_end(const Chain& c, int64_t tile, float h) {
   leave(c.ends + tile * 64 + lane_id(), __float_as_uint(h));
 }
-__device__ __forceinline__ void mark_end(const Chain& c, int64_t tile) {
+// (mark 2; what it was where the end is not known after all)
+__device__ __forceinline__ void mark_end(const Chain& c, int64_t tile, bool known) {
   arrived();
-  if (lane_id() == 0) leave(c.marks + tile, 2u);
+  const uint32_t mark = known ? 2u : tile > 0 ? 1u : 0u;
+  if (lane_id() == 0) leave(c.marks + tile, mark);
 }
 // The state that tile > 0 starts in, for one wave: it polls the marks, all waves of the workgroup bring the maps between to LDS, and it
 // folds them.  (One wave that read up to 63 maps by itself was most of the time of a long sequence.)
@@ -189,7 +210,9 @@ __device__ __forceinline__ float end_of(const Chain& c, int64_t tile) {
     there = __ballot(look(c.marks + tile) == 2u) != 0;
     if (!there) __builtin_amdgcn_s_sleep(8);
   }
-  return there ? __uint_as_float(look(c.ends + tile * 64 + lane_id())) : __builtin_nanf("");
+  float h = there ? __uint_as_float(look(c.ends + tile * 64 + lane_id())) : __builtin_nanf("");
+  asm volatile("" : "+v"(h));  // (waited for here, not where branches with and without it meet)
+  return h;
 }
 // What a launch with workgroups of their own keeps in the workspace: the counters, then the marks (both cleared first), maps and ends.
 constexpr uint32_t kCounters = 4, kCounterWords = 32;  // a cache line each
@@ -274,7 +297,7 @@ struct Inputs {
   __device__ __forceinline__ void ask(const A& a, const Group<V, A>& at, int t0) {
     const int left = at.length - t0;
     const T *pg = at.row((const T*)a.gate, t0, a.gate_step, a.gate_batch), *px = at.row((const T*)a.x, t0, a.x_step, a.x_batch);
-    if (left >= K) {
+    if (K >= kSpan && left >= K) {
       const Lane<V> ch = at.ch.here();
 #pragma unroll
       for (int k = 0; k < K; ++k, pg += a.gate_step, px += a.x_step) {
@@ -378,6 +401,95 @@ __device__ __forceinline__ void given(const float* p, const Group<V, A>& at, flo
   }
 }
 
+// ---- Steps one after the other, where a map or a fold has left the finite numbers.
+//
+// An infinite state, and a product of factors or an offset that passes binary32 although the states do not (factors above 1 of a state that is 0),
+// make inf - inf or 0 inf in a map or a fold.  What comes of that is infinite or NaN and stays so up to the end of the wave's steps and,
+// through the folds, of the tile and the sequence.  So a look at the end of a wave's replay is enough: a channel that is not finite there is
+// formed again from the state that the wave began in, or where that is not finite from the one in front of the tile, in order, with its inputs
+// read again (few steps at a time: this lies beside what the kernels keep in registers); no other channel and nothing finite changes.  A NaN in
+// front of the tile is one behind it either way.
+constexpr int kMend = 4;
+// A kernel's first argument, AGAIN: read once more, so that what is rare keeps nothing in scalar registers for itself.  (Inside a loop, which needs the
+// argument afterwards, that takes more of them.)
+template <bool AGAIN, typename A>
+__device__ __forceinline__ A argument(const A& a) {
+  if constexpr (AGAIN) {
+    auto p = __builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return *(const A*)p;
+  }
+  return a;
+}
+
+// Whether some lane's value is not finite, which is rare.
+template <int V>
+__device__ __forceinline__ bool leaves(const float (&h)[V]) {
+  bool all = true;
+#pragma unroll
+  for (int j = 0; j < V; ++j) all = all && is_finite(h[j]);
+  return __builtin_expect(__ballot(!all) != 0, 0);
+}
+// Which channels are to be formed again, by their state in front and behind; whether a lane of the wave has any.
+template <int V>
+__device__ __forceinline__ bool spoiled(const float (&begin)[V], const float (&end)[V], bool (&which)[V]) {
+  bool any = false;
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    which[j] = !is_finite(end[j]) && begin[j] == begin[j];
+    any = any || which[j];
+  }
+  return __ballot(any) != 0;
+}
+// h from in front of step t to in front of `end`, or to behind the entry's steps (`end` some steps of kMend on).
+template <typename T, int MODE, int V, bool BACK, typename A>
+__device__ __forceinline__ void advance(const A& a, const Group<V, A>& at, int t, int end, float (&h)[V]) {
+  for (t = __builtin_amdgcn_readfirstlane(t); t < end && t < at.length; t = __builtin_amdgcn_readfirstlane(t + kMend)) {
+    Inputs<T, V, kMend> in;
+    in.ask(a, at, t);
+    Steps<T, MODE, V, BACK, kMend> steps;
+    steps.set(in, at.length - t);
+#pragma unroll
+    for (int k = 0; k < kMend; ++k)
+#pragma unroll
+      for (int j = 0; j < V; ++j) h[j] = steps.s[k][j].next_exact(h[j]);
+  }
+}
+// Takes `start` where it is finite.
+template <int V>
+__device__ __forceinline__ void finite_or(const float (&start)[V], float (&h)[V]) {
+#pragma unroll
+  for (int j = 0; j < V; ++j) h[j] = is_finite(start[j]) ? start[j] : h[j];
+}
+// A wave's steps from t0 to `end` again, from `start`, or from the state h in front of step t.
+template <typename T, int MODE, int V>
+__device__ __forceinline__ void replay_again(const RecurrenceArgs& a, const Group<V, RecurrenceArgs>& at, int t, int t0, int end, const float (&start)[V],
+                                             float (&h)[V], const bool (&which)[V]) {
+  advance<T, MODE, V, false>(a, at, t, t0, h);
+  finite_or<V>(start, h);
+  for (t = __builtin_amdgcn_readfirstlane(t0); t < end; t = __builtin_amdgcn_readfirstlane(t + kMend)) {
+    Inputs<T, V, kMend> in;
+    in.ask(a, at, t);
+    Steps<T, MODE, V, false, kMend> steps;
+    steps.set(in, at.length - t);
+#pragma unroll
+    for (int k = 0; k < kMend; ++k) {
+      const int behind = t + k + 1;
+      float out[V];
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        h[j] = steps.s[k][j].next_exact(h[j]);
+        out[j] = within(k, at.length - t) ? h[j] : 0.0f;
+      }
+      if (!within(k, at.steps - t)) break;
+      at.ch.put(at.row((T*)a.hs, t + k, a.hs_step, a.hs_batch), out, which);
+      if (a.h_last && behind == at.steps) at.ch.put(a.h_last + at.state, h, which);
+      if (a.states && behind % AMQ_STATE_STEPS == 0 && behind < at.steps)
+        at.ch.put(a.states + (behind / AMQ_STATE_STEPS - 1) * (int64_t)a.batch * a.n + at.state, h, which);
+    }
+  }
+}
+
 // A workgroup per group of channels, tile after tile; ONE: there is one.
 template <typename T, int MODE, int V, bool ONE>
 __global__ __launch_bounds__(64 * kTileWaves, ONE ? 8 : 4) void recurrence_kernel(RecurrenceArgs a) {
@@ -408,7 +520,7 @@ __global__ __launch_bounds__(64 * kTileWaves, ONE ? 8 : 4) void recurrence_kerne
       steps.map(A, B);
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        maps[turn][w][0][lane * V + j] = A[j];
+        maps[turn][w][0][lane * V + j] = w == 0 ? carry[j] : A[j];  // (nobody folds wave 0's factor)
         maps[turn][w][1][lane * V + j] = B[j];
       }
       lds_barrier();
@@ -426,7 +538,24 @@ __global__ __launch_bounds__(64 * kTileWaves, ONE ? 8 : 4) void recurrence_kerne
         else h[j] = f[j];
       }
     }
+    float start[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) start[j] = h[j];
     steps.replay(a, at, t0, h);
+    if (leaves(h) || (!ONE && w == 0 && leaves(carry))) {
+      float begin[V], next[V];
+      bool which[V];
+#pragma unroll
+      for (int j = 0; j < V; ++j) begin[j] = next[j] = waves > 1 ? maps[turn][0][0][lane * V + j] : carry[j];
+      const RecurrenceArgs b = argument<ONE>(a);
+      const Group<V, RecurrenceArgs> here = ONE ? Group<V, RecurrenceArgs>(b, blockIdx.x) : at;
+      if (spoiled(begin, h, which)) replay_again<T, MODE, V>(b, here, first, t0, t0 + kSpan, start, begin, which);
+      if (!ONE && w == 0 && spoiled(next, carry, which)) {
+        advance<T, MODE, V, false>(b, here, first, first + waves * kSpan, next);
+#pragma unroll
+        for (int j = 0; j < V; ++j) carry[j] = which[j] ? next[j] : carry[j];
+      }
+    }
     if constexpr (ONE) return;
   }
   if (first >= at.steps) return;
@@ -487,38 +616,66 @@ __global__ __launch_bounds__(64 * kTileWaves, 8) void recurrence_tiles_kernel(Re
   } else if (w == 0) {
     given<V>(a.h0, at, h);
   }
+  bool late = false;  // wave 0: the end is not known
   if (w == 0) {
     begin[lane] = h[0];
-    leave_end(chain, tile, fmaf(fa, h[0], fb));
+    const float end[V] = {fmaf(fa, h[0], fb)};
+    leave_end(chain, tile, end[0]);
+    late = leaves(end);  // (also where h does)
     lds_barrier();
-    mark_end(chain, tile);
+    mark_end(chain, tile, !late);
   } else {
     lds_barrier();
-    h[0] = fmaf(fa, begin[lane], fb);
+    h[0] = begin[lane];
   }
+  if (leaves(h)) {  // (the same in all waves) the maps between may have made that: the state that the tile before ends in, by itself
+    if (w == 0) maps[0][0][lane] = tile > 0 ? end_of(chain, tile - 1) : h[0];
+    lds_barrier();
+    begin[lane] = h[0] = maps[0][0][lane];
+  }
+  if (w > 0) h[0] = fmaf(fa, h[0], fb);
+  const float start[V] = {h[0]};
   steps.replay(a, at, t0, h);
+  bool which[V];
+  if (late) {
+    const float from[V] = {begin[lane]};
+    float end[V] = {fmaf(fa, from[0], fb)};
+    if (spoiled(from, end, which)) {
+      float again[V] = {from[0]};
+      const RecurrenceArgs b = argument<true>(a);
+      advance<T, MODE, V, false>(b, Group<V, RecurrenceArgs>(b, group), t0, t0 + kLongTile, again);
+      end[0] = which[0] ? again[0] : end[0];
+    }
+    leave_end(chain, tile, end[0]);
+    mark_end(chain, tile, true);
+  }
+  if (leaves(h)) {
+    float from[V] = {begin[lane]};
+    const RecurrenceArgs b = argument<true>(a);
+    if (spoiled(from, h, which)) replay_again<T, MODE, V>(b, Group<V, RecurrenceArgs>(b, group), (int)tile * kLongTile, t0, t0 + K, start, from, which);
+  }
 }
 
 // ---- backward
 
-template <typename T, int V>
+template <typename T, int V, int K = kSpan>
 struct GradInputs {
-  Inputs<T, V> in;
-  Elements<T, V> d[kSpan];
+  Inputs<T, V, K> in;
+  Elements<T, V> d[K];
   Elements<float, V> h;  // the state in front of the tile
   bool some;             // (there is one)
   __device__ __forceinline__ void ask(const RecurrenceGradArgs& a, const Group<V, RecurrenceGradArgs>& at, int tile, int t0) {
     const int left = at.length - t0;
     in.ask(a, at, t0);
     const T* pd = at.row((const T*)a.dhs, t0, a.dhs_step, a.dhs_batch);
-    if (left >= kSpan) {
+    if (K >= kSpan && left >= K) {
       const Lane<V> ch = at.ch.here();
 #pragma unroll
-      for (int k = 0; k < kSpan; ++k, pd += a.dhs_step) d[k] = ch.get(pd);
+      for (int k = 0; k < K; ++k, pd += a.dhs_step) d[k] = ch.get(pd);
       branch_end();
     } else {
 #pragma unroll
-      for (int k = 0; k < kSpan; ++k, pd += a.dhs_step)
+      for (int k = 0; k < K; ++k, pd += a.dhs_step)
         if (within(k, left)) d[k] = at.ch.get(pd);
     }
     const float* from = tile == 0 ? a.h0 : a.states + (tile - 1) * (int64_t)a.batch * a.n;
@@ -526,9 +683,9 @@ struct GradInputs {
     if (some) h = at.ch.get(from + at.state);
   }
   __device__ __forceinline__ void clear_behind(int left) {
-    if (left < kSpan)
+    if (left < K)
 #pragma unroll
-      for (int k = 0; k < kSpan; ++k)
+      for (int k = 0; k < K; ++k)
         if (!within(k, left))
 #pragma unroll
           for (int j = 0; j < V; ++j) d[k].v[j] = (T)0.0f;
@@ -598,6 +755,80 @@ __device__ __forceinline__ void replay_back(const RecurrenceGradArgs& a, const G
   if (t0 == 0 && a.dh0) at.ch.put(a.dh0 + at.state, r);
 }
 
+// Steps one after the other again: the gradient r that reaches the last of the steps [t, end) from behind, to the one that leaves step t.  WRITE: with
+// the gradients of these steps, from `first`, the state in front of step t; `which` as above.
+template <typename T, int MODE, int V, bool WRITE>
+__device__ __forceinline__ void retreat(const RecurrenceGradArgs& a, const Group<V, RecurrenceGradArgs>& at, int tile, int t, int end, const float (&first)[V],
+                                        float (&r)[V], const bool (&which)[V]) {
+  const int steps_end = ((WRITE ? at.steps : at.length) + kMend - 1) / kMend * kMend;
+  int u = __builtin_amdgcn_readfirstlane((end < steps_end ? end : steps_end) - kMend);
+  for (; u >= t; u = __builtin_amdgcn_readfirstlane(u - kMend)) {
+    float before[kMend][V], h[V];
+    if constexpr (WRITE) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) h[j] = first[j];
+      advance<T, MODE, V, true>(a, at, t, u, h);
+    }
+    GradInputs<T, V, kMend> in;
+    in.ask(a, at, tile, u);
+    Steps<T, MODE, V, true, kMend> steps;
+    steps.set(in.in, at.length - u);
+    in.clear_behind(at.length - u);
+    if constexpr (WRITE)
+#pragma unroll
+      for (int k = 0; k < kMend; ++k)
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          before[k][j] = h[j];
+          h[j] = steps.s[k][j].next_exact(h[j]);
+        }
+#pragma unroll
+    for (int k = kMend - 1; k >= 0; --k) {
+      float og[V], ox[V];
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const float e = r[j] + (float)in.d[k].v[j];
+        if constexpr (WRITE) {
+          const bool here = within(k, at.length - u);
+          og[j] = here ? steps.s[k][j].dgate(e, before[k][j]) : 0.0f;
+          ox[j] = here ? steps.s[k][j].dx(e) : 0.0f;
+        }
+        r[j] = steps.s[k][j].keep_exact(e);
+      }
+      if constexpr (WRITE)
+        if (within(k, at.steps - u)) {
+          at.ch.put(at.row((T*)a.dgate, u + k, a.dgate_step, a.dgate_batch), og, which);
+          at.ch.put(at.row((T*)a.dx, u + k, a.dx_step, a.dx_batch), ox, which);
+        }
+    }
+  }
+  if constexpr (WRITE)
+    if (t == 0 && a.dh0) at.ch.put(a.dh0 + at.state, r, which);
+}
+// Behind a wave's replay that began in the state h0 and with the gradient r0, and ended in h and r: what is to be formed again is.  `behind`: the
+// gradient that reaches the tile from behind.
+template <typename T, int MODE, int V>
+__device__ __forceinline__ void mend_back(const RecurrenceGradArgs& a, const Group<V, RecurrenceGradArgs>& at, int tile, int t0, const float (&behind)[V],
+                                          const float (&h0)[V], const float (&r0)[V], const float (&h)[V], float (&r)[V]) {
+  float from[V], again[V];
+  bool which[V], of_r[V];
+  given<V>(tile == 0 ? a.h0 : a.states + (tile - 1) * (int64_t)a.batch * a.n, at, from);
+  const bool some_h = spoiled(from, h, which), some_r = spoiled(behind, r, of_r);
+  if (!some_h && !some_r) return;
+  advance<T, MODE, V, true>(a, at, tile * kTile, t0, from);
+  finite_or<V>(h0, from);
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    again[j] = behind[j];
+    which[j] = which[j] || of_r[j];
+  }
+  retreat<T, MODE, V, false>(a, at, tile, t0 + kSpan, (tile + 1) * kTile, from, again, which);
+  finite_or<V>(r0, again);
+  retreat<T, MODE, V, true>(a, at, tile, t0, t0 + kSpan, from, again, which);
+#pragma unroll
+  for (int j = 0; j < V; ++j) r[j] = of_r[j] ? again[j] : r[j];
+}
+
 template <typename T, int MODE, bool ONE>
 __global__ __launch_bounds__(64 * kTileWaves, ONE ? 8 : 4) void recurrence_grad_kernel(RecurrenceGradArgs a) {
   constexpr int V = 1;
@@ -644,8 +875,15 @@ __global__ __launch_bounds__(64 * kTileWaves, ONE ? 8 : 4) void recurrence_grad_
 #pragma unroll 4
     for (int u = waves - 1; u > w; --u) r[0] = fmaf(maps[turn][u][0][lane], r[0], maps[turn][u][2][lane]);
     if (!ONE && w == 0) back[0] = fmaf(A[0], r[0], R[0]);
+    const float h_start[V] = {h[0]}, r_start[V] = {r[0]};
     replay_back(a, at, steps, in, t0, h, r);
+    if (leaves<2>({h[0], r[0]})) {
+      const float from[V] = {behind[turn][lane]};
+      const RecurrenceGradArgs b = argument<ONE>(a);
+      mend_back<T, MODE, V>(b, ONE ? Group<V, RecurrenceGradArgs>(b, blockIdx.x) : at, tile, t0, from, h_start, r_start, h, r);
+    }
     if constexpr (ONE) return;
+    if (w == 0 && !is_finite(back[0])) back[0] = r[0];  // (that of the map may be infinite by the map alone)
   }
 }
 
@@ -706,16 +944,44 @@ __global__ __launch_bounds__(64 * kTileWaves, 8) void recurrence_grad_tiles_kern
   } else if (mine) {
     given<V>(a.dh_last, at, r);
   }
+  bool late = false;  // as forward
   if (mine) {
     begin[lane] = r[0];
-    leave_end(chain, order, fmaf(fa, r[0], fr));
+    const float end[V] = {fmaf(fa, r[0], fr)};
+    leave_end(chain, order, end[0]);
+    late = leaves(end);
     lds_barrier();
-    mark_end(chain, order);
+    mark_end(chain, order, !late);
   } else {
     lds_barrier();
-    r[0] = fmaf(fa, begin[lane], fr);
+    r[0] = begin[lane];
   }
+  if (leaves(r)) {
+    if (mine) maps[0][0][lane] = order > 0 ? end_of(chain, order - 1) : r[0];
+    lds_barrier();
+    begin[lane] = r[0] = maps[0][0][lane];
+  }
+  if (!mine) r[0] = fmaf(fa, r[0], fr);
+  const float h_start[V] = {h[0]}, r_start[V] = {r[0]};
   replay_back(a, at, steps, in, t0, h, r);
+  if (late) {
+    bool which[V];
+    const float from[V] = {begin[lane]};
+    float end[V] = {fmaf(fa, from[0], fr)};
+    if (spoiled(from, end, which)) {
+      float again[V] = {from[0]};
+      const RecurrenceGradArgs b = argument<true>(a);
+      retreat<T, MODE, V, false>(b, Group<V, RecurrenceGradArgs>(b, group), tile, tile * kTile, (tile + 1) * kTile, again, again, which);
+      end[0] = which[0] ? again[0] : end[0];
+    }
+    leave_end(chain, order, end[0]);
+    mark_end(chain, order, true);
+  }
+  if (leaves<2>({h[0], r[0]})) {
+    const float from[V] = {begin[lane]};
+    const RecurrenceGradArgs b = argument<true>(a);
+    mend_back<T, MODE, V>(b, Group<V, RecurrenceGradArgs>(b, group), tile, t0, from, h_start, r_start, h, r);
+  }
 }
 
 // ---- launches

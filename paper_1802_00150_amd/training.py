@@ -86,7 +86,7 @@ class _LinearRecurrence(torch.autograd.Function):
 
 
 def linear_recurrence(gate, x, h0=None, mode="blend", lengths=None):
-    """binding.linear_recurrence's states and last state, differentiable in gate, x and h0.  Forward and backward may be captured into one graph
+    """binding.linear_recurrence's states and last state, differentiable in gate, x and h0, with its range.  Forward and backward may be captured into one graph
     where no graph of the same leaves lives that was recorded outside (refused)."""
     binding.refuse_held("linear_recurrence", gate, x, h0)
     return _LinearRecurrence.apply(gate, x, h0, mode, lengths)

@@ -636,6 +636,9 @@ int amq_block_norm_backward(const void* dy, int64_t ld_dy, const void* dnormed, 
 size_t amq_clip_gradients_workspace_bytes(int64_t count);
 int amq_clip_gradients(int64_t count, const void* const* tensors, const int64_t* sizes, const int* types, float max_norm,
                        void* const* out, float* norm, void* workspace, size_t workspace_bytes, void* stream);
+/* The same with a limit of binary64, which divides the norm, of binary64 too, as it is. */
+int amq_clip_gradients_double(int64_t count, const void* const* tensors, const int64_t* sizes, const int* types, double max_norm,
+                              void* const* out, float* norm, void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -41,7 +41,7 @@ EXPORTS = [
     "amq_linear_recurrence_workspace_bytes", "amq_linear_recurrence",
     "amq_linear_recurrence_backward_workspace_bytes", "amq_linear_recurrence_backward",
     "amq_block_norm", "amq_block_norm_backward_workspace_bytes", "amq_block_norm_backward",
-    "amq_clip_gradients_workspace_bytes", "amq_clip_gradients",
+    "amq_clip_gradients_workspace_bytes", "amq_clip_gradients", "amq_clip_gradients_double",
 ]
 
 _lib = None
@@ -159,7 +159,8 @@ def lib():
         L.amq_block_norm_backward.argtypes = [_p, _i64, _p, _i64, _p, _i64, _p, _i64, _p, _i64, _i64, _i64, _int, _int, _int, _int,
                                               _p, _p, _p, _p, _p, _p, _i64, _p, _i64, _p, _i64, _p, _p, _p, _p, _p, _p, _sz, _p]
         L.amq_clip_gradients_workspace_bytes.argtypes, L.amq_clip_gradients_workspace_bytes.restype = [_i64], _sz
-        L.amq_clip_gradients.argtypes = [_i64, _p, _p, _p, C.c_float, _p, _p, _p, _sz, _p]
+        for name, limit in (("amq_clip_gradients", C.c_float), ("amq_clip_gradients_double", C.c_double)):
+            getattr(L, name).argtypes = [_i64, _p, _p, _p, limit, _p, _p, _p, _sz, _p]
         _lib = L
     return _lib
 

@@ -41,9 +41,9 @@ struct ScaleArgs {
   Table t;
   uint32_t pieces, vectors;
   const double* partial;  // of all launches
-  int partials;
-  float max_norm;
+  double max_norm;
   float* norm;  // null: another launch writes it
+  int partials;
 };
 
 // The tensor that a piece belongs to: the last one that begins at it or before.
@@ -130,7 +130,7 @@ __global__ __launch_bounds__(kThreads) void scale_tensors_kernel(ScaleArgs a) {
   s = sqrt(block_sum<kThreads / 64>(s, scratch));
   if (a.norm && blockIdx.x == 0 && threadIdx.x == 0) *a.norm = (float)s;
   const bool finite = s < __builtin_inf();  // (false for NaN)
-  const double exact = finite && s > (double)a.max_norm ? (double)a.max_norm / s : 1.0;
+  const double exact = finite && s > a.max_norm ? a.max_norm / s : 1.0;
   // a factor that binary32 holds to fewer digits takes binary64 products
   const bool small = exact < 0x1p-100;
   const float c = (float)exact;
@@ -187,7 +187,7 @@ size_t clip_workspace(int64_t count) {
   return (size_t)(launches > 0 ? launches : 1) * kMostBlocks * sizeof(double);
 }
 
-hipError_t launch_clip_gradients(const ClipTensors& c, float max_norm, float* norm, void* ws, hipStream_t s) {
+hipError_t launch_clip_gradients(const ClipTensors& c, double max_norm, float* norm, void* ws, hipStream_t s) {
   double* partial = static_cast<double*>(ws);
   int partials = 0;
   ClipArgs sum;

@@ -39,7 +39,7 @@ namespace {
   X(amq_linear_recurrence_workspace_bytes) X(amq_linear_recurrence)                                                  \
   X(amq_linear_recurrence_backward_workspace_bytes) X(amq_linear_recurrence_backward) X(amq_block_norm)               \
   X(amq_block_norm_backward_workspace_bytes) X(amq_block_norm_backward) X(amq_clip_gradients_workspace_bytes)         \
-  X(amq_clip_gradients)
+  X(amq_clip_gradients) X(amq_clip_gradients_double)
 
 struct Api {
 #define AMQ_MEMBER(name) decltype(&::name) name = nullptr;
@@ -969,12 +969,12 @@ PyObject* clip_gradients(PyObject* const* a) {  // list of tensors, list of resu
     no_graph("clip_gradients", "", {PyList_GET_ITEM(a[1], i)});
     out[i] = q.data_ptr();
   }
-  const float max_norm = (float)real(a[2]);
+  const double max_norm = real(a[2]);
   at::Tensor norm = make({}, at::kFloat, like);
   float* pn = static_cast<float*>(norm.data_ptr());
   Workspace ws(a[3], like, [&] { return api.amq_clip_gradients_workspace_bytes(count); });
   void* s = stream();
-  call([&] { return api.amq_clip_gradients(count, in.data(), sizes.data(), types.data(), max_norm, scale ? out.data() : nullptr, pn, ws.ptr, ws.bytes, s); });
+  call([&] { return api.amq_clip_gradients_double(count, in.data(), sizes.data(), types.data(), max_norm, scale ? out.data() : nullptr, pn, ws.ptr, ws.bytes, s); });
   return wrap(norm);
 }
 

@@ -129,6 +129,6 @@ struct ClipTensors {
   int64_t count;
 };
 size_t clip_workspace(int64_t count);
-hipError_t launch_clip_gradients(const ClipTensors& c, float max_norm, float* norm, void* ws, hipStream_t s);
+hipError_t launch_clip_gradients(const ClipTensors& c, double max_norm, float* norm, void* ws, hipStream_t s);
 
 }  // namespace amq

@@ -425,7 +425,12 @@ size_t amq_clip_gradients_workspace_bytes(int64_t count) {
 
 int amq_clip_gradients(int64_t count, const void* const* tensors, const int64_t* sizes, const int* types, float max_norm,
                        void* const* out, float* norm, void* workspace, size_t workspace_bytes, void* stream) {
-  if (count < 0 || (count > 0 && (!tensors || !sizes || !types)) || !norm || !on_elements(norm, AMQ_F32) || (out && !(max_norm >= 0.0f)))
+  return amq_clip_gradients_double(count, tensors, sizes, types, max_norm, out, norm, workspace, workspace_bytes, stream);
+}
+
+int amq_clip_gradients_double(int64_t count, const void* const* tensors, const int64_t* sizes, const int* types, double max_norm,
+                              void* const* out, float* norm, void* workspace, size_t workspace_bytes, void* stream) {
+  if (count < 0 || (count > 0 && (!tensors || !sizes || !types)) || !norm || !on_elements(norm, AMQ_F32) || (out && !(max_norm >= 0.0)))
     return AMQ_ERR_INVALID;
   if (count > kMaxSize) return AMQ_ERR_UNSUPPORTED;
   for (int64_t i = 0; i < count; ++i) {

@@ -531,7 +531,8 @@ def fake_quantize(W, k, T=2):
 
 # ---- operators of quantization-aware training: float32, bfloat16 or float16 tensors [..., n] (a 2-D tensor's rows may be strided).
 # They record no graph: with gradients on, layer_norm, linear, orthogonalize, linear_recurrence, block_norm and clip_gradients refuse operands that
-# require one (the functions of the same names in training are the differentiable forms).
+# require one (the functions of the same names in training are the differentiable forms), the last three and linear_recurrence_backward also results that
+# do.  A result that is given counts as written in place: a graph that saved what it held raises in its backward pass.
 
 ACTIVATIONS = {None: 0, "none": 0, "relu": 1, "gelu": 2, "silu": 3, "sigmoid": 4, "tanh": 5}
 

@@ -114,6 +114,16 @@ PyObject* again(PyObject* o) {
   Py_INCREF(o);
   return o;
 }
+// A tensor of the caller's that a call has written: graphs that hold what it was say so in their backward pass.
+void wrote(PyObject* o) {
+  if (o == Py_None) return;
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+PyObject* written(PyObject* o) {
+  wrote(o);
+  return again(o);
+}
 
 void* stream() { return c10::hip::getCurrentHIPStream().stream(); }
 
@@ -500,7 +510,7 @@ void no_graph(const char* name, const char* instead, std::initializer_list<PyObj
   if (!at::GradMode::is_enabled()) return;
   for (PyObject* o : operands)
     if (THPVariable_Check(o) && THPVariable_Unpack(o).requires_grad())
-      fail(amq_error, std::string(name) + " records no graph, and an operand requires a gradient: " + instead + "call it under torch.no_grad()");
+      fail(amq_error, std::string(name) + " records no graph, and an operand or result requires a gradient: " + instead + "call it under torch.no_grad()");
 }
 
 int type_of(const at::Tensor& t) {
@@ -579,7 +589,7 @@ struct Result {
       rows = Rows(tensor(o), name, want_rows, want_n, like);
     }
   }
-  PyObject* take() { return given == Py_None ? wrap(own) : again(given); }
+  PyObject* take() { return given == Py_None ? wrap(own) : written(given); }
 };
 
 PyObject* none() { return again(Py_None); }
@@ -663,6 +673,7 @@ PyObject* linear(PyObject* const* a) {  // x, W, bias, activation, residual, ws,
     return api.amq_linear(r.p, r.ld, W.p, W.ld, r.rows, r.n, n, type, b, act, res.p, res.ld, y.rows.p, y.rows.ld, pre.p, pre.ld, ws.ptr,
                           ws.bytes, s);
   });
+  wrote(a[7]);
   return y.take();
 }
 
@@ -723,7 +734,7 @@ PyObject* orthogonalize(PyObject* const* a) {  // G, steps, a, b, c, eps, ws, ou
   call([&] {
     return api.amq_orthogonalize(g.p, g.batch, g.stride, g.rows, g.cols, g.ld, type, steps, coef, eps, o.p, o.stride, o.ld, ws.ptr, ws.bytes, s);
   });
-  return a[7] == Py_None ? wrap(own) : again(a[7]);
+  return a[7] == Py_None ? wrap(own) : written(a[7]);
 }
 
 // ---- linear recurrences, joined norms, clipping: on the operands' device and its current stream
@@ -782,7 +793,7 @@ void* exactly(PyObject* o, const char* name, at::IntArrayRef shape, at::ScalarTy
 }
 
 PyObject* linear_recurrence(PyObject* const* a) {  // gate, x, h0, mode, lengths, states, ws, out, h_out
-  no_graph("linear_recurrence", "take training.linear_recurrence, or ", {a[0], a[1], a[2]});
+  no_graph("linear_recurrence", "take training.linear_recurrence, or ", {a[0], a[1], a[2], a[7], a[8]});
   const at::Tensor& x = on_gpu(a[1]);
   const c10::DeviceGuard guard(x.device());
   const int type = type_of(x), mode = (int)integer(a[3]);
@@ -804,10 +815,11 @@ PyObject* linear_recurrence(PyObject* const* a) {  // gate, x, h0, mode, lengths
     return api.amq_linear_recurrence(g.p, g.step, g.entry, r.p, r.step, r.entry, r.steps, r.batch, r.n, type, mode, lengths, h0, y.p, y.step, y.entry, h,
                                      st, ws.ptr, ws.bytes, s);
   });
-  return tuple({a[7] == Py_None ? wrap(hs) : again(a[7]), a[8] == Py_None ? wrap(last) : again(a[8]), states.defined() ? wrap(states) : none()});
+  return tuple({a[7] == Py_None ? wrap(hs) : written(a[7]), a[8] == Py_None ? wrap(last) : written(a[8]), states.defined() ? wrap(states) : none()});
 }
 
 PyObject* linear_recurrence_backward(PyObject* const* a) {  // dhs, gate, x, h0, states, dh_last, mode, lengths, ws, dgate, dx
+  no_graph("linear_recurrence_backward", "", {a[9], a[10]});
   const at::Tensor& x = on_gpu(a[2]);
   const c10::DeviceGuard guard(x.device());
   const int type = type_of(x), mode = (int)integer(a[6]);
@@ -830,7 +842,7 @@ PyObject* linear_recurrence_backward(PyObject* const* a) {  // dhs, gate, x, h0,
     return api.amq_linear_recurrence_backward(d.p, d.step, d.entry, g.p, g.step, g.entry, r.p, r.step, r.entry, r.steps, r.batch, r.n, type, mode, lengths,
                                               h0, st, dl, rg.p, rg.step, rg.entry, rx.p, rx.step, rx.entry, r0, ws.ptr, ws.bytes, s);
   });
-  return tuple({a[9] == Py_None ? wrap(dg) : again(a[9]), a[10] == Py_None ? wrap(dx) : again(a[10]), h0 ? wrap(dh0) : none()});
+  return tuple({a[9] == Py_None ? wrap(dg) : written(a[9]), a[10] == Py_None ? wrap(dx) : written(a[10]), h0 ? wrap(dh0) : none()});
 }
 
 // n entries of a vector from `at` on, as a tensor on the same storage.
@@ -863,7 +875,7 @@ void residual_type_ok(const at::Tensor& t, const char* name, const at::Tensor& x
 }
 
 PyObject* block_norm(PyObject* const* a) {  // x, residual, weight, bias, gate, activation, scale, next_weight, next_bias, eps, normed, out, out_normed
-  no_graph("block_norm", "take training.block_norm, or ", {a[0], a[1], a[2], a[3], a[4], a[6], a[7], a[8]});
+  no_graph("block_norm", "take training.block_norm, or ", {a[0], a[1], a[2], a[3], a[4], a[6], a[7], a[8], a[11], a[12]});
   const at::Tensor &x = on_gpu(a[0]), &residual = tensor(a[1]);
   const c10::DeviceGuard guard(x.device());
   const int type = type_of(x), act = (int)integer(a[5]);
@@ -975,6 +987,7 @@ PyObject* clip_gradients(PyObject* const* a) {  // list of tensors, list of resu
   Workspace ws(a[3], like, [&] { return api.amq_clip_gradients_workspace_bytes(count); });
   void* s = stream();
   call([&] { return api.amq_clip_gradients_double(count, in.data(), sizes.data(), types.data(), max_norm, scale ? out.data() : nullptr, pn, ws.ptr, ws.bytes, s); });
+  for (Py_ssize_t i = 0; scale && i < count; ++i) wrote(PyList_GET_ITEM(a[1], i));
   return wrap(norm);
 }
 

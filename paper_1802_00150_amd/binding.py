@@ -640,14 +640,22 @@ def linear_recurrence_backward_workspace(steps, batch, n, dtype, device):
                        device=device)
 
 
+def _refuse_held(name, of):
+    if torch.cuda.is_current_stream_capturing() and (_native_module or _load_native()).held_elsewhere(of):
+        raise AmqError("%s: a leaf's gradient belongs to a graph recorded on another stream that is still alive (hooks on leaves keep their part of one); "
+                       "delete its results and such hooks or make them on the stream that captures, or capture with detached leaves or without gradients" % name)
+
+
 def refuse_held(name, *operands):
-    """Raises where a graph is captured whose gradients would end in leaves that a graph recorded on another stream still holds: torch's backward pass
-    would make the capture wait for that stream, which ends the process."""
-    if not any(isinstance(t, torch.Tensor) and t.is_cuda for t in operands) or not torch.cuda.is_current_stream_capturing():
-        return
-    if (_native_module or _load_native()).held_elsewhere(operands):
-        raise AmqError("%s: a leaf's gradient belongs to a graph recorded on another stream that is still alive; delete its results, or capture with "
-                       "detached leaves" % name)
+    """Raises where a forward pass is captured whose gradients would end in leaves that a graph recorded on another stream still holds: torch's backward
+    pass would make the capture wait for that stream, which ends the process."""
+    if torch.is_grad_enabled() and any(isinstance(t, torch.Tensor) and t.is_cuda for t in operands):
+        _refuse_held(name, operands)
+
+
+def refuse_held_behind(name, ctx):
+    """The same in a backward pass, in front of what it hands its gradients to."""
+    _refuse_held(name, (ctx,))
 
 
 GATES = (None, "none", "sigmoid", "silu")

@@ -18,6 +18,7 @@
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/custom_function.h>
 #include <torch/csrc/autograd/functions/accumulate_grad.h>
+#include <torch/csrc/autograd/python_function.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "../../include/amq.h"
@@ -991,7 +992,8 @@ PyObject* clip_gradients(PyObject* const* a) {  // list of tensors, list of resu
   return wrap(norm);
 }
 
-// Whether the gradients of a tuple's tensors end in leaves that a graph recorded on another stream than the current one holds too.
+// Whether the gradients of a tuple's tensors, or those that a backward pass in it (the ctx of a torch.autograd.Function) leaves, end in leaves that a
+// graph recorded on another stream than the current one holds too.
 PyObject* held_elsewhere(PyObject* const* a) {
   if (!PyTuple_Check(a[0])) fail(PyExc_TypeError, "expected a tuple");
   std::vector<std::shared_ptr<torch::autograd::Node>> open;
@@ -1002,6 +1004,11 @@ PyObject* held_elsewhere(PyObject* const* a) {
   for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(a[0]); ++i) {
     PyObject* o = PyTuple_GET_ITEM(a[0], i);
     if (o == Py_None) continue;
+    if (THPFunction_Check(o)) {
+      if (const auto node = reinterpret_cast<THPFunction*>(o)->cdata.lock())
+        for (const torch::autograd::Edge& e : node->next_edges()) meet(e.function);
+      continue;
+    }
     const at::Tensor& t = tensor(o);
     if (!t.requires_grad()) continue;
     meet(t.is_leaf() ? torch::autograd::impl::try_get_grad_accumulator(t) : t.grad_fn());

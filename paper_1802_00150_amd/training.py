@@ -27,6 +27,7 @@ class _LayerNorm(torch.autograd.Function):
     @staticmethod
     @once_differentiable
     def backward(ctx, dy):
+        binding.refuse_held_behind("layer_norm", ctx)
         x, weight, bias, mean, rstd = ctx.saved_tensors
         params = ctx.needs_input_grad[1] or ctx.needs_input_grad[2]
         dx, dw, db = binding.layer_norm_backward(dy.contiguous(), x, weight, mean, rstd, params,
@@ -35,7 +36,8 @@ class _LayerNorm(torch.autograd.Function):
 
 
 def layer_norm(x, weight=None, bias=None, eps=1e-5):
-    """binding.layer_norm's y, differentiable in x, weight and bias."""
+    """binding.layer_norm's y, differentiable in x, weight and bias.  Forward and backward may be captured into one graph where no graph of the same leaves
+    lives that was recorded outside (the backward pass is refused)."""
     return _LayerNorm.apply(x, weight, bias, eps)
 
 
@@ -52,6 +54,7 @@ class _Linear(torch.autograd.Function):
     @staticmethod
     @once_differentiable
     def backward(ctx, dy):
+        binding.refuse_held_behind("linear", ctx)
         x, W, pre = ctx.saved_tensors
         need = ctx.needs_input_grad
         dx = dW = db = None
@@ -61,7 +64,7 @@ class _Linear(torch.autograd.Function):
 
 
 def linear(x, W, bias=None, activation=None, residual=None):
-    """binding.linear, differentiable in x, W, bias and residual."""
+    """binding.linear, differentiable in x, W, bias and residual.  Captured as layer_norm is."""
     return _Linear.apply(x, W, bias, activation, residual)
 
 
@@ -86,8 +89,8 @@ class _LinearRecurrence(torch.autograd.Function):
 
 
 def linear_recurrence(gate, x, h0=None, mode="blend", lengths=None):
-    """binding.linear_recurrence's states and last state, differentiable in gate, x and h0, with its range.  Forward and backward may be captured into one graph
-    where no graph of the same leaves lives that was recorded outside (refused)."""
+    """binding.linear_recurrence's states and last state, differentiable in gate, x and h0, with its range.  Forward and backward may be captured into one
+    graph where no graph of the same leaves lives that was recorded outside (refused with gradients on, already in the forward pass)."""
     binding.refuse_held("linear_recurrence", gate, x, h0)
     return _LinearRecurrence.apply(gate, x, h0, mode, lengths)
 

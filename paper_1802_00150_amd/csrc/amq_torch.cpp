@@ -154,6 +154,9 @@ struct Workspace {
       bytes = (size_t)own.numel();
     } else {
       const at::Tensor& t = tensor(o);
+      // (kernels write all `bytes` behind its address)
+      if (!t.is_cuda() || t.device() != like.device()) fail(amq_error, "workspace: expected a tensor on the same GPU");
+      if (!t.is_contiguous()) fail(PyExc_ValueError, "workspace: expected a contiguous tensor");
       ptr = t.data_ptr();
       bytes = (size_t)t.numel();
     }

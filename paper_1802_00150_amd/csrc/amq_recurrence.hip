@@ -22,9 +22,10 @@
 // The backward pass takes h_{t-1} in full precision from the states that the forward pass leaves in front of every 128th
 // step (4 / 128 bytes per entry instead of the 2 of reading rounded states): each tile replays the recurrence from there.
 //
-// States, products of factors and gradients along time are binary32.  1 - i is never rounded by itself: for g >= 0 the kept
-// state is h - i h in one fused operation, so that units that hold for 10^5 steps do not drift (a rounded f is off by up to
-// 2^-25 the same way in every step), and for g < 0 it is f h with f = sigmoid(g) to its last digits.
+// States, products of factors and gradients along time are binary32; sigmoids are within (2 |g| + 8) 2^-24 of their value.  For g >= 0 a
+// step is h + i x - i h, a rounding of the sum and one of the fused rest, and a map keeps A - i A: 1 - i is not rounded by itself, which would be
+// off by up to 2^-25 the same way in every step of a gate that stays.  (Roundings of states that move by little are alike too: over 20000 steps
+// of gates near 10 the error is half of that of a rounded f with maps of 16 steps, about 0.7 with 8.)  For g < 0 the step is f h + i x.
 #include "../../include/amq.h"
 
 #include <type_traits>

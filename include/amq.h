@@ -563,7 +563,8 @@ int amq_orthogonalize(const void* G, int64_t batch, int64_t batch_stride, int64_
  *   h0 [B][n] float or NULL for zeros;  h_last [B][n] float or NULL: the state behind the last step; may be h0 itself
  *   states [(steps - 1) / AMQ_STATE_STEPS][B][n] float or NULL: the states in front of steps 128, 256, ..., which the backward pass takes (of
  *   each entry those in front of its lengths[b]; the others are not written)
- *   workspace: at least amq_linear_recurrence_workspace_bytes(steps, B, n, type) bytes, 256-byte aligned (0: may be NULL).
+ *   workspace: at least amq_linear_recurrence_workspace_bytes(steps, B, n, type) bytes, 256-byte aligned (0: may be NULL); for one call at a
+ *   time: calls on several streams, and graphs that may be replayed side by side, take one each.
  * One step with h0 and h_last is the form for single tokens.
  * The backward pass takes dhs [steps][B][n] and dh_last [B][n] (NULL: zeros), the gradients of hs and h_last, and leaves those of gate, x and
  * h0 (dh0 float, may be NULL): with e_t = dhs_t + f_{t+1} e_{t+1},  dx = (1 - f) e,  dgate = e (h_{t-1} - x) f (1 - f),  dh0 = f_0 e_0;

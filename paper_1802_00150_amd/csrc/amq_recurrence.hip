@@ -4,7 +4,7 @@
 //   decay   h_t = a_t h_{t-1} + x_t, the factor a given
 //   back    e_t = dh_t + f_{t+1} e_{t+1} (from dh_last):  dx = i e,  dg = e (h_{t-1} - x) f i;  decay: dx = e, da = e h_{t-1}
 //
-// 27 vector instructions per entry forward and 45 backward, against 6 and 10 bytes (16-bit types): bound by memory once enough is under way
+// 28 vector instructions per entry forward and 46 backward, against 6 and 10 bytes (16-bit types): bound by memory once enough is under way
 // (backward with 16-bit types by instructions as much), by latency for few entries.  A step is an affine map of the
 // state, so time is split: the 8 steps of a wave are read at once, turned into one map (factor A, offset B) from a zero state, the waves
 // of a workgroup exchange those through LDS, every wave folds the ones before it onto the state and replays its steps, which are still
@@ -13,11 +13,11 @@
 //
 // With channels enough for the card a workgroup walks over the tiles of its channels.  Otherwise every tile (of 256 steps forward) has a
 // workgroup: it leaves its map in memory, looks back for the nearest tile whose end state is there, folds the maps between and leaves its
-// own end state ("Tiles of one sequence" below).
+// own end state ("Tiles of one sequence" below): a single-pass scan with decoupled look-back, as Merrill and Garland published it in 2016.
 //
-// Measured (steps x channels; a large copy 5.1 TB/s): 2000 x 16384 float 78 us, 5.05 TB/s; 1000 x 32768 bfloat16 39.5 us, 5.0; 35 x 262144
-// backward 19.7, 4.8; 1000 x 16384 backward 39, 4.2; with the chain 32768 x 1024 bfloat16 55, 3.65; 4001 x 2100 float 28.6, 3.5, backward
-// 50, 3.4; 2000 x 8192 float backward 71, 4.6.
+// Measured (steps x channels; a large copy 5.1 TB/s): 2000 x 16384 float 78 us, 5.05 TB/s; 1000 x 32768 bfloat16 39.5 to 41.5 us, 4.9; 35 x 262144
+// backward 20.2, 4.7; 1000 x 16384 backward 40, 4.1; with the chain 32768 x 1024 bfloat16 54, 3.7; 16384 x 1024 float 47, 4.3; 4001 x 2100 float
+// 28, 3.6, backward 50, 3.4; 2000 x 8192 float backward 71, 4.6.  (The second figure is TB/s.)
 //
 // The backward pass takes h_{t-1} in full precision from the states that the forward pass leaves in front of every 128th
 // step (4 / 128 bytes per entry instead of the 2 of reading rounded states): each tile replays the recurrence from there.
@@ -240,9 +240,9 @@ __device__ __forceinline__ Chain chain_of(const Split& s, int64_t group) {
   return {s.marks + group * s.tiles, s.maps + group * s.tiles * 64, s.ends + group * s.tiles * 64};
 }
 // A tile that nobody has begun, by its order in the chain of its group, the same in all threads; false if there is none.  Every
-// `kinds`th group shares a counter: four of them (1000 x 8192 bfloat16 18.0 us, with one for all 22.1; 4001 x 2100 float 28.4 and
-// 31.1; backward 1000 x 4096 bfloat16 17.1 and 21.3; with eight, whose groups each keep to one die, 32768 x 1024 takes 61 us and not
-// 55.6), but one where a row of tiles fills the card (3000 x 16500 90 us, with four 96).
+// `kinds`th group shares a counter: four of them (with one for all 1000 x 8192 bfloat16 takes 1.23 times as long, 4001 x 2100 float 1.10
+// times, backward 1000 x 4096 bfloat16 1.25 times; with eight, whose groups each keep to one die, 32768 x 1024 1.10 times), but one where a row of
+// tiles fills the card (3000 x 16500 with four 1.07 times).
 __device__ __forceinline__ bool take_tile(const Split& s, uint32_t& shared, uint32_t& order, uint32_t& group) {
   const uint32_t kinds = s.kinds, kind = blockIdx.x % kinds;
   if (threadIdx.x == 0) shared = __hip_atomic_fetch_add(s.counter + kind * kCounterWords, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -565,7 +565,7 @@ __global__ __launch_bounds__(64 * kTileWaves, ONE ? 8 : 4) void recurrence_kerne
 }
 
 // A workgroup per tile, of 16 steps of 16 waves of one channel a lane: a longer tile waits less for others than a wider one
-// (32768 x 1024 bfloat16 57 us, 8 steps of two channels 61, 12 steps of one 61; 16384 x 1024 float 50, 51 and 49), and needs no even
+// (8 steps of two channels and 12 of one take 1.07 times as long at 32768 x 1024 bfloat16, 1.02 and 0.98 times at 16384 x 1024 float), and needs no even
 // number of channels.
 template <typename T, int MODE>
 __global__ __launch_bounds__(64 * kTileWaves, 8) void recurrence_tiles_kernel(RecurrenceArgs a, Split split) {
@@ -1005,17 +1005,18 @@ int64_t groups_of(int64_t batch, int64_t n, int V) { return batch * ((n + 64 * V
 int64_t tiles_of(int64_t steps, int tile) { return (steps + tile - 1) / tile; }
 
 // Channels of a lane: two of 16 bits where a workgroup walks over tiles forward and groups of 64 channels are more than the card holds at
-// once (300 x 17408 13.9 us, with one 16.8; 1000 x 32768 41 and 48; but 2000 x 16384 62 and 46); one otherwise (35 x 262144 backward 21.2,
-// with two 23.8).
+// once (300 x 17408 13.9 us, with one 16.8; 1000 x 32768 41 and 48; but 2000 x 16384 62 and 46); one otherwise (35 x 262144 backward
+// takes 1.12 times as long with two).
 bool two_channels(int64_t batch, int64_t n) { return n % 2 == 0 && groups_of(batch, n, 1) > 256; }
 
-// The form with the least time, by measurement.  Per 128 steps a workgroup per group takes c0 us and all 256 that the card holds at once
+// The form with the least time, by measurement.  Per 128 steps a workgroup per group takes c0 us and 256 of them, one on every compute unit,
 // c0 + c1; a workgroup per tile e for 256 groups, and 7.5 us more for clearing the marks, the second launch and the chain.  Steps x
 // channels, a workgroup per group and one per tile: 16-bit types 300 x 1024 8.4 and 10.0, 1000 x 1024 18.7 and 11.0, 1000 x 8192 20.3 and
 // 16.4, 1000 x 12288 21.1 and 21.4, 3000 x 12288 62 and 55, 3000 x 16384 67 and 69, 1000 x 24576 35 and 42; float 1000 x 4096 17.8 and
 // 15.4, 1000 x 12288 30.2 and 33.7; backward 200 x 1024 8.9 and 11.1, 1000 x 1024 28 and 11, 1000 x 16384 39 and 50, 3000 x 12288 109 and
-// 98, float 3000 x 8192 113 and 103, 1000 x 24576 107 and 102.  Beyond four rounds of the card the last one's share is small, and the
-// workspace would grow with the channels (64 of them to a tile, used or not).
+// 98, float 3000 x 8192 113 and 103, 1000 x 24576 107 and 102.  The constants are those of up to 256 groups; for more they are only what
+// the choice goes by: 3000 x 16500 bfloat16 takes 91 us in tiles, by them 68, backward 162 and 126.  Beyond four rounds of the card the last
+// one's share is small, and the workspace would grow with the channels (64 of them to a tile, used or not).
 bool splits(int64_t batch, int64_t n, int64_t steps, bool wide, bool backward) {
   const bool pairs = !wide && !backward && two_channels(batch, n);
   const double c0 = pairs ? 2.6 : wide ? backward ? 2.7 : 1.75 : backward ? 3.25 : 2.1;
